@@ -11,6 +11,10 @@ namespace {
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
+}  // namespace
+
+namespace lg {
+
 lg_status check_cache(const lg_cache *c) {
   if (!c || !c->k || !c->v || !c->seq_off || !c->cap || !c->len || !c->dev_status)
     return LG_ERR_INVALID_ARG;
@@ -32,6 +36,13 @@ lg_status check_params(const lg_guard_params *p) {
   if (!(p->tau_ham >= 0.0 && p->tau_ham <= 1.0)) return LG_ERR_INVALID_ARG;
   return LG_OK;
 }
+
+}  // namespace lg
+
+namespace {
+
+using lg::check_cache;
+using lg::check_params;
 
 lg_status cuda_status(cudaError_t e) { return e == cudaSuccess ? LG_OK : LG_ERR_CUDA; }
 

@@ -1,0 +1,305 @@
+// lg_chunk_attend on the CUDA cores, and the merge of shared items.
+//
+// A query tile is BM rows: the g query heads of BM / g consecutive new tokens (row r: token r / g,
+// head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
+// a running maximum m, normaliser l and sum o per row (log2 units):
+//   m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,  o = o 2^(m - m') + p V.
+// 256 threads as 16 x 16: thread (ty, tx) computes the scores of rows ty TM .. ty TM + TM - 1 and
+// keys tx + 16 j, and the results of the same rows and elements 4 tx + 64 j, so that a row's
+// probabilities pass between lanes of one half-warp only.
+#include <cuda_bf16.h>
+
+#include "lg_chunk_attend.cuh"
+
+namespace lg {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBn = 64;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(const void *p, int64_t i, float *f);
+template <>
+__device__ __forceinline__ void load4<float>(const void *p, int64_t i, float *f) {
+  const float4 v = *(const float4 *)((const float *)p + i);
+  f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+}
+template <>
+__device__ __forceinline__ void load4<__nv_bfloat16>(const void *p, int64_t i, float *f) {
+  const uint2 v = *(const uint2 *)((const __nv_bfloat16 *)p + i);
+  const float2 x = bf16x2_to_float2(v.x), y = bf16x2_to_float2(v.y);
+  f[0] = x.x, f[1] = x.y, f[2] = y.x, f[3] = y.y;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(void *p, int64_t i, const float *f);
+template <>
+__device__ __forceinline__ void store4<float>(void *p, int64_t i, const float *f) {
+  *(float4 *)((float *)p + i) = make_float4(f[0], f[1], f[2], f[3]);
+}
+template <>
+__device__ __forceinline__ void store4<__nv_bfloat16>(void *p, int64_t i, const float *f) {
+  __nv_bfloat162 v[2] = {__floats2bfloat162_rn(f[0], f[1]), __floats2bfloat162_rn(f[2], f[3])};
+  *(uint2 *)((__nv_bfloat16 *)p + i) = *(const uint2 *)v;
+}
+
+template <int D, int BM>
+struct SimtCfg {
+  static constexpr int kRow = D + 4;  // floats of a staged row: 16 rows of 16 bytes, no conflicts
+  static constexpr int kSmem =
+      (BM * kRow + kBn * kRow + kBn * D + BM * (kBn + 4)) * (int)sizeof(float);
+};
+
+template <typename T, int D, int BM>
+__global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs a) {
+  constexpr int TM = BM / 16, NC = D / 64, kRow = SimtCfg<D, BM>::kRow, kPRow = kBn + 4;
+  extern __shared__ __align__(16) float smem[];
+  float *sq = smem, *sk = sq + BM * kRow, *sv = sk + kBn * kRow, *sp = sv + kBn * D;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int H_q = a.H_kv * a.g;
+  pdl_enter();
+  ChunkShare sh;
+  if (!chunk_share<kThreads>(a, blockIdx.x, gridDim.x, sh)) return;
+  ChunkWalk w;
+  for (w.start(a, sh, sh.y0); !w.done(); w.next(a)) {
+    if (w.blk0 == w.blk1) continue;
+    const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
+    const int tok0 = w.off + w.t * a.shape.tok;
+    __syncthreads();
+    for (int e = tid; e < BM * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), c = e % (D / 4) * 4;
+      float f[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < used)
+        load4<T>(a.q, ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D + c, f);
+      *(float4 *)(sq + r * kRow + c) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+    float o[TM][4 * NC], m[TM], l[TM];
+    int qrow[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      qrow[i] = w.rows.first + (ty * TM + i) / a.g;
+#pragma unroll
+      for (int k = 0; k < 4 * NC; ++k) o[i][k] = 0.f;
+    }
+    for (int blk = w.blk0; blk < w.blk1; ++blk) {
+      const int i0 = w.blocks.index(blk) * kBn;
+      __syncthreads();
+      for (int e = tid; e < kBn * (D / 4); e += kThreads) {
+        const int r = e / (D / 4), c = e % (D / 4) * 4;
+        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (i0 + r < w.q.n) {
+          load4<T>(a.K, (w.row0 + i0 + r) * D + c, k);
+          load4<T>(a.V, (w.row0 + i0 + r) * D + c, v);
+        }
+        *(float4 *)(sk + r * kRow + c) = make_float4(k[0], k[1], k[2], k[3]);
+        *(float4 *)(sv + r * D + c) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      __syncthreads();
+      // scores, even and odd elements summed apart
+      float2 acc[TM][4];
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = make_float2(0.f, 0.f);
+#pragma unroll 4
+      for (int c = 0; c < D; c += 4) {
+        float4 kf[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kf[j] = *(const float4 *)(sk + (tx + 16 * j) * kRow + c);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const float4 qf = *(const float4 *)(sq + (ty * TM + i) * kRow + c);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            acc[i][j] = __ffma2_rn(make_float2(qf.x, qf.y), make_float2(kf[j].x, kf[j].y), acc[i][j]);
+            acc[i][j] = __ffma2_rn(make_float2(qf.z, qf.w), make_float2(kf[j].z, kf[j].w), acc[i][j]);
+          }
+        }
+      }
+      bool edge = false;  // some key of the block is hidden from some query of this thread
+      float alpha[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        float s[4], mx = m[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool sees = row_sees(w.rows, a.shape, qrow[i], i0 + tx + 16 * j);
+          edge |= !sees;
+          s[j] = sees ? (acc[i][j].x + acc[i][j].y) * a.qscale : -INFINITY;
+          mx = fmaxf(mx, s[j]);
+        }
+#pragma unroll
+        for (int off = 8; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        const float base = mx == -INFINITY ? 0.f : mx;
+        alpha[i] = exp2_fast(m[i] - base);
+        m[i] = mx;
+        l[i] *= alpha[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = exp2_fast(s[j] - base);
+          l[i] += p;
+          sp[(ty * TM + i) * kPRow + tx + 16 * j] = p;
+        }
+      }
+      edge = __any_sync(0xffffffffu, edge);  // also orders the half-warp's probabilities
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int k = 0; k < 4 * NC; ++k) o[i][k] *= alpha[i];
+#pragma unroll 2
+      for (int r = 0; r < kBn; r += 4) {
+        float4 p[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) p[i] = *(const float4 *)(sp + (ty * TM + i) * kPRow + r);
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+          for (int k = 0; k < NC; ++k) {
+            const float4 v = *(const float4 *)(sv + (r + rr) * D + 4 * tx + 64 * k);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+              const float pr = rr == 0 ? p[i].x : rr == 1 ? p[i].y : rr == 2 ? p[i].z : p[i].w;
+              // a hidden row has probability 0 and may hold anything
+              const bool add = !edge || pr != 0.f;
+              float2 *oo = (float2 *)&o[i][4 * k];
+              oo[0] = __ffma2_rn(make_float2(pr, pr), add ? make_float2(v.x, v.y) : make_float2(0.f, 0.f), oo[0]);
+              oo[1] = __ffma2_rn(make_float2(pr, pr), add ? make_float2(v.z, v.w) : make_float2(0.f, 0.f), oo[1]);
+            }
+          }
+      }
+      __syncwarp();
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int r = ty * TM + i;
+#pragma unroll
+      for (int off = 8; off; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
+      if (r >= used) continue;
+      if (w.whole()) {
+        const float inv = l[i] != 0.f ? 1.f / l[i] : 0.f;
+        const int64_t dst = ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          float f[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = o[i][4 * k + e] * inv;
+          store4<T>(a.out, dst + 4 * tx + 64 * k, f);
+        }
+      } else {
+        float *dst = part_row(a, D, blockIdx.x, w.slot(), r);
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+          *(float4 *)(dst + 4 * tx + 64 * k) =
+              make_float4(o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]);
+        if (tx == 0) *part_ml(a, D, gridDim.x, blockIdx.x, w.slot(), r) = make_float2(m[i], l[i]);
+      }
+    }
+  }
+}
+
+// Merge of the item that the start of CTA c's range cuts, c = blockIdx.x + 1, by the first cut of
+// an item: pieces of CTAs c - 1, c, ... in order, a warp per row, blockIdx.y of gridDim.y in turn.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
+  constexpr int V = D / 32;  // elements a lane
+  pdl_enter();
+  const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ChunkShare sh;
+  if (!chunk_share<kThreads>(a, c, G, sh)) return;
+  ChunkWalk w;
+  w.start(a, sh, sh.y0);
+  if (w.x == sh.y0) return;  // the bound falls between items
+  if (range_bound(sh.W, c - 1, G) > w.x) return;  // an earlier bound cuts the item too
+  int last = c;
+  while (last + 1 < G && range_bound(sh.W, last + 1, G) < w.x + w.cost) ++last;
+  const int used = w.tokens(a) * a.g, tok0 = w.off + w.t * a.shape.tok, H_q = a.H_kv * a.g;
+  for (int r = blockIdx.y * (kThreads / 32) + warp; r < used; r += gridDim.y * (kThreads / 32)) {
+    float m = -INFINITY, l = 0.f, o[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) o[k] = 0.f;
+    bool whole = false;
+    for (int p = c - 1; p <= last; ++p) {
+      const int b0 = cut_block(range_bound(sh.W, p, G) - w.x, w.cost, w.blocks.count);
+      const int b1 = cut_block(range_bound(sh.W, p + 1, G) - w.x, w.cost, w.blocks.count);
+      if (b0 == b1) continue;
+      if (b0 == 0 && b1 == w.blocks.count) {
+        whole = true;  // one piece has every block: its CTA wrote the result
+        break;
+      }
+      const int slot = p == c - 1 ? 1 : 0;
+      const float2 ml = *part_ml(a, D, G, p, slot, r);
+      const float *src = part_row(a, D, p, slot, r);
+      const float mx = fmaxf(m, ml.x), base = mx == -INFINITY ? 0.f : mx;
+      const float f0 = exp2_fast(m - base), f1 = exp2_fast(ml.x - base);
+      l = l * f0 + ml.y * f1;
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] = o[k] * f0 + src[lane + 32 * k] * f1;
+      m = mx;
+    }
+    if (whole) continue;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    const int64_t dst = ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D;
+#pragma unroll
+    for (int k = 0; k < V; ++k) Elem<T>::store(a.out, dst + lane + 32 * k, o[k] * inv);
+  }
+}
+
+template <typename T, int D, int BM>
+cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
+  auto kern = chunk_attend_kernel<T, D, BM>;
+  LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              SimtCfg<D, BM>::kSmem));
+  LG_TRY(launch_pdl(kern, G, kThreads, SimtCfg<D, BM>::kSmem, s, a));
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
+  LG_TRY(launch_pdl(chunk_merge_kernel<T, D>, dim3(G - 1, 4), kThreads, 0, s, a, G));
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_d(ChunkAttendArgs &a, int G, cudaStream_t s) {
+  return a.rows == 16 ? launch_typed<T, D, 16>(a, G, s) : launch_typed<T, D, 128>(a, G, s);
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s) {
+  if (dtype == LG_BF16)
+    return d == 128 ? launch_merge_typed<__nv_bfloat16, 128>(a, G, s)
+                    : launch_merge_typed<__nv_bfloat16, 64>(a, G, s);
+  return d == 128 ? launch_merge_typed<float, 128>(a, G, s)
+                  : launch_merge_typed<float, 64>(a, G, s);
+}
+
+ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
+  ChunkGrid r;
+  r.rows = (int64_t)max_new * g <= 16 ? 16 : 128;
+  r.ctas = 152 * (r.rows == 16 ? 2 : 1);
+  r.tok = r.rows / g;
+  r.bn = kBn;
+  return r;
+}
+
+cudaError_t launch_chunk_attend(ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s) {
+  cudaError_t e;
+  if (dtype == LG_BF16)
+    e = d == 128 ? launch_d<__nv_bfloat16, 128>(a, G, s) : launch_d<__nv_bfloat16, 64>(a, G, s);
+  else
+    e = d == 128 ? launch_d<float, 128>(a, G, s) : launch_d<float, 64>(a, G, s);
+  if (e != cudaSuccess) return e;
+  return launch_chunk_merge(a, dtype, d, G, s);
+}
+
+}  // namespace lg

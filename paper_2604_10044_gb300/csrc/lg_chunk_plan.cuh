@@ -1,0 +1,129 @@
+// How lg_chunk_attend's work is divided, in closed form, so that every CTA finds its share from the
+// lengths alone.
+//
+// An item is (sequence, kv-head, tile): the g query heads of `tok` consecutive new tokens.  Its
+// cost is the rows its queries can see plus kItemCost, a linear function of the tile (constant once
+// a window fills), so the cost of a sequence's first t tiles is a closed form.  The items stand in
+// one line, ordered by sequence, kv-head and tile, W cost units long; CTA c of G takes
+// [W c / G, W (c + 1) / G).  An item cut by such a bound is shared: its key blocks divide in
+// proportion, each CTA's part is a piece, and a second kernel merges the pieces (of partial
+// results in the workspace: slot 0 of a CTA for an item that began before its range, slot 1 for
+// one that ends after it).
+#pragma once
+#include <stdint.h>
+
+#ifndef __CUDACC__
+#define __host__
+#define __device__
+#define __forceinline__ inline
+#endif
+
+namespace lg {
+
+// Cost of an item beside its rows: queries in, results out (in rows of keys).
+constexpr int kItemCost = 96;
+
+struct ChunkShape {
+  int tok;     // tokens of a tile
+  int bn;      // rows of a key block
+  int window;  // 0: none
+  int sink;
+};
+
+// the sequences' numbers: rows n in the cache, m of them new
+struct ChunkSeq {
+  int n, m;
+  __host__ __device__ __forceinline__ int tiles(int tok) const {
+    return m / tok + (m % tok != 0);
+  }
+};
+
+__host__ __device__ __forceinline__ int64_t plan_min(int64_t a, int64_t b) { return a < b ? a : b; }
+__host__ __device__ __forceinline__ int64_t plan_max(int64_t a, int64_t b) { return a > b ? a : b; }
+
+// rows tile t's queries see: first query row `first`, last `last`; rows [0, sinks) and [lo, last]
+struct TileRows {
+  int first, last, lo, sinks;
+};
+
+__host__ __device__ __forceinline__ TileRows tile_rows(const ChunkSeq &q, const ChunkShape &s,
+                                                       int t) {
+  TileRows r;
+  r.first = q.n - q.m + t * s.tok;
+  r.last = q.n - q.m + (int)plan_min(q.m, (int64_t)(t + 1) * s.tok) - 1;
+  r.lo = s.window ? (int)plan_max(0, (int64_t)r.first + 1 - s.window) : 0;
+  r.sinks = (int)plan_min(s.sink, r.lo);
+  return r;
+}
+
+__host__ __device__ __forceinline__ int64_t tile_cost(const ChunkSeq &q, const ChunkShape &s,
+                                                      int t) {
+  const TileRows r = tile_rows(q, s, t);
+  return (int64_t)r.last + 1 - r.lo + r.sinks + kItemCost;
+}
+
+// cost of tiles [0, t), 0 <= t <= tiles
+__host__ __device__ __forceinline__ int64_t tiles_cost(const ChunkSeq &q, const ChunkShape &s,
+                                                       int t) {
+  if (t <= 0) return 0;
+  int64_t extra = 0;
+  if (t == q.tiles(s.tok)) {  // the last tile may be short
+    extra = tile_cost(q, s, t - 1);
+    if (--t == 0) return extra;
+  }
+  // full tiles i < t: (n - m + (i + 1) tok) + kItemCost - max(0, a + i tok)
+  const int64_t T = t, tok = s.tok;
+  int64_t sum = T * ((int64_t)q.n - q.m + kItemCost) + tok * (T * (T + 1) / 2);
+  if (s.window) {
+    const int64_t a = (int64_t)q.n - q.m + 1 - s.window - s.sink;
+    const int64_t i0 = a >= 0 ? 0 : (-a + tok - 1) / tok;
+    if (i0 < T) sum -= (T - i0) * a + tok * ((T * (T - 1) - i0 * (i0 - 1)) / 2);
+  }
+  return sum + extra;
+}
+
+// the tile that cost unit x of a (sequence, kv-head) falls into
+__host__ __device__ __forceinline__ int tile_at(const ChunkSeq &q, const ChunkShape &s,
+                                                int64_t x) {
+  int lo = 0, hi = q.tiles(s.tok) - 1;
+  while (lo < hi) {  // the last tile whose start is <= x
+    const int mid = lo + (hi - lo + 1) / 2;
+    if (tiles_cost(q, s, mid) <= x)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+// a tile's key blocks: block i of `count` holds the rows from block_row(i)
+struct TileBlocks {
+  int sink_blocks, skip, count;
+  __host__ __device__ __forceinline__ int index(int i) const {
+    return i < sink_blocks ? i : i + skip;
+  }
+};
+
+__host__ __device__ __forceinline__ TileBlocks tile_blocks(const TileRows &r, int bn) {
+  TileBlocks b;
+  const int w0 = r.lo / bn, w1 = r.last / bn + 1;
+  b.sink_blocks = (r.sinks + bn - 1) / bn;
+  if (b.sink_blocks > w0) b.sink_blocks = w0;  // a block of both kinds counts once
+  b.skip = w0 - b.sink_blocks;
+  b.count = b.sink_blocks + w1 - w0;
+  return b;
+}
+
+// first cost unit of CTA c
+__host__ __device__ __forceinline__ int64_t range_bound(int64_t W, int c, int G) {
+  return W / G * c + W % G * c / G;
+}
+
+// blocks before a cut at cost unit y (0..cost) of an item
+__host__ __device__ __forceinline__ int cut_block(int64_t y, int64_t cost, int count) {
+  if (y <= 0) return 0;
+  if (y >= cost) return count;
+  return (int)((y * count + cost / 2) / cost);
+}
+
+}  // namespace lg

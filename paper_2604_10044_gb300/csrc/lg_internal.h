@@ -4,8 +4,13 @@
 #include <stdint.h>
 
 #include "lg.h"
+#include "lg_chunk.h"
 
 namespace lg {
+
+// argument checks shared by the calls (lg_api.cu)
+lg_status check_cache(const lg_cache *c);
+lg_status check_params(const lg_guard_params *p);
 
 struct AttendArgs {
   const void *K, *V;       // cache [L][H_kv][S_total][d]
@@ -88,5 +93,35 @@ cudaError_t launch_h2o_evict(const lg_cache &c, const int32_t *budget, const int
 cudaError_t launch_streaming_evict(const lg_cache &c, const int32_t *budget,
                                    const int32_t *pos_now, int n_sink, int max_len,
                                    cudaStream_t s);
+
+
+// chunks of new tokens (lg_chunk.cu)
+cudaError_t launch_begin_chunk(const lg_cache &c, const lg_chunk &ch, cudaStream_t s);
+// turns: rp.rot / 2 frequencies in 2^-64 turns; guard: the layer's V rows are sketched
+cudaError_t launch_rope_append(const lg_cache &c, const lg_chunk &ch, int layer, const void *q,
+                               int64_t q_stride, int H_q, const void *k, int64_t k_stride,
+                               const void *v, int64_t v_stride, const int32_t *pos,
+                               const lg_rope_params &rp, const uint64_t *turns, void *q_out,
+                               bool guard, cudaStream_t s);
+
+// lg_chunk_attend (lg_chunk_attend.cu): the grid and tiles of a call, and the call
+struct ChunkGrid {
+  int ctas;  // of the persistent kernel
+  int rows;  // of an item
+  int tok;   // tokens of an item
+  int bn;    // rows of a key block
+};
+struct ChunkAttendArgs;
+ChunkGrid chunk_grid(int dtype, int d, int g, int max_new);
+cudaError_t launch_chunk_attend(ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s);
+
+// picked tokens (lg_pick.cu)
+cudaError_t launch_pick_token(const lg_logits &x, const uint32_t *seen, const int32_t *counts,
+                              const float *penalty, const lg_bias *bias, const uint32_t *allowed,
+                              int32_t *tokens, float *pmax, void *logits_out, int32_t *status,
+                              cudaStream_t s);
+cudaError_t launch_count_tokens(const int32_t *tokens, const int32_t *off, int T, int batch, int V,
+                                int generated, uint32_t *seen, int32_t *counts, int32_t *status,
+                                cudaStream_t s);
 
 }  // namespace lg

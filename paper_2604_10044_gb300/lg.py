@@ -1,4 +1,4 @@
-"""Python binding of liblg.so (include/lg.h): argument marshalling only.
+"""Python binding of liblg.so (include/lg.h, include/lg_chunk.h): argument marshalling only.
 
 Every function named ``lg_*`` here calls the C function of the same name with raw device
 pointers taken from torch tensors and the caller's CUDA stream; every step of the decode path
@@ -51,6 +51,28 @@ class LgTokenParams(ctypes.Structure):
                 ("theta_cr", ctypes.c_double), ("theta_conf", ctypes.c_double)]
 
 
+class LgChunk(ctypes.Structure):
+    _fields_ = [("off", ctypes.c_void_p), ("T", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+class LgRopeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layout", "rot", "scaling", "orig_len")] + \
+        [(n, ctypes.c_double) for n in ("theta", "factor", "low", "high", "beta_fast",
+                                         "beta_slow", "mscale")]
+
+
+class LgLogits(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("V", ctypes.c_int32), ("pad", ctypes.c_int32), ("stride", ctypes.c_int64)]
+
+
+class LgBias(ctypes.Structure):
+    _fields_ = [("off", ctypes.c_void_p), ("id", ctypes.c_void_p), ("val", ctypes.c_void_p)]
+
+
+LG_ROPE_HALF, LG_ROPE_INTERLEAVED = 0, 1
+LG_ROPE_PLAIN, LG_ROPE_LINEAR, LG_ROPE_BASE, LG_ROPE_BANDS, LG_ROPE_YARN = range(5)
+
 STATE_BYTES = 32  # lg_guard_state: 8 x int32
 STATE_WORD_N_INT = 4  # lg_guard_state.n_int: interventions so far
 
@@ -93,6 +115,15 @@ def lib():
             "lg_decode_attend_noalloc": [P(LgCache), i32, i32, vp, i32, ctypes.c_float, vp, vp,
                                          i32, i32, i32, vp],
             "lg_status_string": [i32],
+            "lg_begin_chunk": [P(LgCache), P(LgChunk), vp],
+            "lg_default_rope_params": [P(LgRopeParams), i32],
+            "lg_rope_append": [P(LgCache), P(LgChunk), i32, vp, i64, i32, vp, i64, vp, i64, vp,
+                               P(LgRopeParams), vp, P(LgGuardParams), vp],
+            "lg_chunk_workspace_size": [P(LgCache), P(LgChunk), i32, i32],
+            "lg_chunk_attend": [P(LgCache), P(LgChunk), i32, vp, i32, ctypes.c_float, i32, i32, vp,
+                                i32, vp, ctypes.c_size_t, vp],
+            "lg_count_tokens": [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp],
+            "lg_pick_token": [P(LgLogits), vp, vp, vp, P(LgBias), vp, vp, vp, vp, vp, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -100,6 +131,7 @@ def lib():
             f.restype = ctypes.c_int
         L.lg_workspace_size.restype = ctypes.c_size_t
         L.lg_detect_state_size.restype = ctypes.c_size_t
+        L.lg_chunk_workspace_size.restype = ctypes.c_size_t
         L.lg_token_state_size.restype = ctypes.c_size_t
         L.lg_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -114,6 +146,14 @@ def exported_symbols():
             "lg_decode_attend_noalloc", "lg_detect_state_size", "lg_streaming_evict",
             "lg_detect_prune", "lg_default_token_params", "lg_token_state_size",
             "lg_token_detect", "lg_token_detect_prune"]
+
+
+
+def chunk_symbols():
+    """names of the C ABI functions declared in include/lg_chunk.h"""
+    return ["lg_begin_chunk", "lg_default_rope_params", "lg_rope_append",
+            "lg_chunk_workspace_size", "lg_chunk_attend", "lg_count_tokens", "lg_pick_token"]
+
 
 NOALLOC_SCRATCH_BYTES = 32 << 20  # LG_NOALLOC_SCRATCH_BYTES in include/lg.h
 
@@ -276,6 +316,93 @@ def lg_read_device_status(cache, stream=None) -> int:
     code = ctypes.c_int32(0)
     _call("lg_read_device_status", ctypes.byref(cache.c), ctypes.byref(code), _stream(stream))
     return code.value
+
+
+# ------------------------------------------------------------------ chunks and picked tokens
+
+class Chunk:
+    """The new tokens of a batch (lg_chunk): off, int32 device tensor [batch + 1]; T, rows of the
+    token arrays; max_new, a bound on the new tokens of one sequence."""
+
+    def __init__(self, off, T, max_new):
+        self.off, self.T, self.max_new = off, int(T), int(max_new)
+        self.c = LgChunk(off=_ptr(off), T=self.T, max_new=self.max_new)
+
+    @classmethod
+    def of(cls, counts, device):
+        """the chunk of counts[b] new tokens of each sequence, rows one after another"""
+        off = np.concatenate([[0], np.cumsum(np.asarray(counts, dtype=np.int64))])
+        return cls(torch.as_tensor(off.astype(np.int32), device=device), int(off[-1]),
+                   int(max(counts)))
+
+
+def _rows_stride(t, name):
+    """elements from token to token of a [T][H][d] tensor whose rows are whole"""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("%s: [T][H][d] with whole rows of H * d elements" % name)
+    return max(t.stride(0), t.shape[1] * t.shape[2])  # one row: its stride says nothing
+
+
+def lg_begin_chunk(cache, chunk, stream=None):
+    _call("lg_begin_chunk", ctypes.byref(cache.c), ctypes.byref(chunk.c), _stream(stream))
+
+
+def lg_default_rope_params(d, **over) -> LgRopeParams:
+    p = LgRopeParams()
+    _call("lg_default_rope_params", ctypes.byref(p), d)
+    for k, v in over.items():
+        setattr(p, k, v)
+    return p
+
+
+def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, params, stream=None):
+    """q [T][H_q][d] (or None with q_out None), k_new, v_new [T][H_kv][d]: slices of one packed
+    projection pass as they are"""
+    H_q = 0 if q is None else q.shape[1]
+    _call("lg_rope_append", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, _ptr(q),
+          0 if q is None else _rows_stride(q, "q"), H_q, _ptr(k_new),
+          _rows_stride(k_new, "k_new"), _ptr(v_new), _rows_stride(v_new, "v_new"), _ptr(pos),
+          ctypes.byref(rope), _ptr(q_out), ctypes.byref(params), _stream(stream))
+
+
+def lg_chunk_workspace_size(cache, chunk, H_q, max_len) -> int:
+    return int(lib().lg_chunk_workspace_size(ctypes.byref(cache.c), ctypes.byref(chunk.c), H_q,
+                                             max_len))
+
+
+def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max_len, ws,
+                    stream=None):
+    _call("lg_chunk_attend", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, _ptr(q), H_q,
+          float(scale), window, n_sink, _ptr(out), max_len, _ptr(ws),
+          ws.numel() * ws.element_size(), _stream(stream))
+
+
+def lg_count_tokens(tokens, off, V, generated, seen, counts, status=None, stream=None):
+    """tokens of row b: tokens[off[b]] .. tokens[off[b + 1] - 1], or tokens[b] with off None"""
+    batch = tokens.numel() if off is None else off.numel() - 1
+    _call("lg_count_tokens", _ptr(tokens), _ptr(off), tokens.numel(), batch, V, generated,
+          _ptr(seen), _ptr(counts), _ptr(status), _stream(stream))
+
+
+def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, status=None,
+                  logits_out=None, stream=None):
+    """logits [batch][V] (rows may be strided); bias: None or (off, id, val); status: the cache's
+    status word or None; logits_out: None or a tensor of the same dtype and strides"""
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("logits: [batch][V] with whole rows")
+    if logits_out is not None and (logits_out.dtype != logits.dtype or
+                                   logits_out.stride() != logits.stride()):
+        raise ValueError("logits_out: dtype and strides of logits")
+    B, V = logits.shape
+    dt = {torch.bfloat16: LG_BF16, torch.float32: LG_F32}.get(logits.dtype, -1)
+    x = LgLogits(x=_ptr(logits), dtype=dt, batch=B, V=V, pad=0,
+                 stride=max(logits.stride(0), V))  # one row: its stride says nothing
+    bs = None
+    if bias is not None:
+        bs = ctypes.byref(LgBias(off=_ptr(bias[0]), id=_ptr(bias[1]), val=_ptr(bias[2])))
+    _call("lg_pick_token", ctypes.byref(x), _ptr(seen), _ptr(counts), _ptr(penalty), bs,
+          _ptr(allowed), _ptr(tokens), _ptr(pmax), _ptr(logits_out), _ptr(status),
+          _stream(stream))
 
 
 # ------------------------------------------------------------------ device buffers of a batch

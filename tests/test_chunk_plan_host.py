@@ -1,0 +1,122 @@
+"""The division of lg_chunk_attend's work (csrc/lg_chunk_plan.cuh), compiled for the host: the
+closed-form costs against their sums, tile_at against a walk, the pieces of random batches (every
+key block of every item exactly once, and never more pieces than the two slots of a CTA), and the
+blocks against the rows that a tile's queries see."""
+import os
+import subprocess
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2604_10044_gb300", "csrc")
+
+PROG = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <set>
+#include <vector>
+#include "lg_chunk_plan.cuh"
+using namespace lg;
+#define CHECK(x) do { if (!(x)) { printf("line %d: %s\n", __LINE__, #x); exit(1); } } while (0)
+
+static std::mt19937_64 rng(7);
+static int64_t uni(int64_t lo, int64_t hi) { return lo + (int64_t)(rng() % (uint64_t)(hi - lo + 1)); }
+static int pick(std::initializer_list<int> l) { return l.begin()[uni(0, (int)l.size() - 1)]; }
+
+static ChunkShape shape() {
+  ChunkShape s;
+  s.tok = (int)uni(1, 256);
+  s.bn = pick({64, 128});
+  s.window = uni(0, 2) ? (int)uni(1, pick({3, 200, 5000, 2147483647})) : 0;
+  s.sink = pick({0, 1, 4, 64, 129, 1000});
+  return s;
+}
+static ChunkSeq seq() {
+  ChunkSeq q;
+  q.n = (int)uni(0, pick({3, 130, 700, 5000}));
+  q.m = (int)uni(0, uni(0, 1) ? q.n : (q.n < 3 ? q.n : 3));
+  return q;
+}
+
+int main() {
+  for (int it = 0; it < 4000; ++it) {  // costs, tiles, blocks
+    const ChunkShape s = shape();
+    const ChunkSeq q = seq();
+    const int tiles = q.tiles(s.tok);
+    int64_t sum = 0;
+    for (int t = 0; t < tiles; ++t) {
+      CHECK(tiles_cost(q, s, t) == sum);
+      const int64_t c = tile_cost(q, s, t);
+      CHECK(c > kItemCost);
+      CHECK(tile_at(q, s, sum) == t && tile_at(q, s, sum + c - 1) == t);
+      const TileRows r = tile_rows(q, s, t);
+      const TileBlocks b = tile_blocks(r, s.bn);
+      // seen by some query of the tile <=> in a block of the tile, up to whole blocks
+      std::set<int> want, got;
+      for (int j = t * s.tok; j < q.m && j < (t + 1) * s.tok; ++j) {
+        const int row = q.n - q.m + j;
+        for (int i = 0; i <= row; ++i)
+          if (s.window == 0 || (int64_t)i > (int64_t)row - s.window || i < s.sink) want.insert(i / s.bn);
+      }
+      for (int i = 0; i < b.count; ++i) CHECK(got.insert(b.index(i)).second);
+      CHECK(want == got);
+      sum += c;
+    }
+    CHECK(tiles_cost(q, s, tiles) == sum);
+  }
+  for (int it = 0; it < 1500; ++it) {  // pieces
+    const ChunkShape s = shape();
+    const int B = (int)uni(1, 12), H = (int)uni(1, 8), G = pick({1, 2, 152, 304});
+    std::vector<ChunkSeq> q(B);
+    int64_t W = 0;
+    std::vector<int64_t> start, cost;
+    std::vector<int> count;
+    for (auto &x : q) {
+      x = seq();
+      for (int h = 0; h < H; ++h)
+        for (int t = 0; t < x.tiles(s.tok); ++t) {
+          start.push_back(W);
+          cost.push_back(tile_cost(x, s, t));
+          count.push_back(tile_blocks(tile_rows(x, s, t), s.bn).count);
+          W += cost.back();
+        }
+    }
+    int64_t end = 0;
+    std::vector<int> next(start.size(), 0);
+    for (int c = 0; c < G; ++c) {
+      const int64_t y0 = range_bound(W, c, G), y1 = range_bound(W, c + 1, G);
+      CHECK(y0 == end && y1 >= y0);
+      end = y1;
+      int slots[2] = {0, 0};
+      for (size_t i = 0; i < start.size(); ++i) {
+        if (start[i] + cost[i] <= y0 || start[i] >= y1) continue;
+        const int b0 = cut_block(y0 - start[i], cost[i], count[i]);
+        const int b1 = cut_block(y1 - start[i], cost[i], count[i]);
+        CHECK(b0 == next[i] && b1 >= b0);
+        next[i] = b1;
+        if (b0 == b1 || (b0 == 0 && b1 == count[i])) continue;
+        ++slots[start[i] < y0 ? 0 : 1];
+      }
+      CHECK(slots[0] <= 1 && slots[1] <= 1);
+    }
+    CHECK(end == W);
+    for (size_t i = 0; i < start.size(); ++i) CHECK(next[i] == count[i]);
+  }
+  // the largest line: no 64-bit overflow in the bounds or the cuts
+  const ChunkSeq big{2147483647, 2147483647};
+  const ChunkShape s{16, 64, 0, 0};
+  const int64_t W = tiles_cost(big, s, big.tiles(s.tok)) / 2;
+  CHECK(W > 0 && range_bound(W, 304, 304) == W && range_bound(W, 152, 304) <= W / 2 + 1);
+  const int64_t c = tile_cost(big, s, big.tiles(16) - 1);
+  CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1) <= 2147483647 / 64 + 1);
+  puts("ok");
+}
+"""
+
+
+def test_plan(tmp_path):
+    src = tmp_path / "plan.cpp"
+    src.write_text(PROG)
+    exe = tmp_path / "plan"
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, str(src), "-o",
+                    str(exe)], check=True)
+    assert subprocess.run([str(exe)], capture_output=True, text=True).stdout.strip() == "ok"

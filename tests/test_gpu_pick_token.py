@@ -1,0 +1,201 @@
+"""lg_pick_token and lg_count_tokens against the documented steps in fp32 and 64-bit sums.
+
+Tokens and processed logits are exact.  pmax is 1 / s with s a sum of V exponentials of fp32
+differences d: each off by |d| 2^-23 + 2^-22 of itself (the difference times log2 e, the
+exponential), and |d| e^d <= 1/e, so s is off by at most V 2^-24 + 2^-20 of itself (s >= 1)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import chunk_ref
+from paper_2604_10044_gb300 import lg
+
+pytestmark = pytest.mark.gpu
+
+
+def _dev(x, cuda, dt=None):
+    t = torch.as_tensor(np.ascontiguousarray(x), device=cuda)
+    return t if dt is None else t.to(dt)
+
+
+def _run(cuda, logits, seen=None, counts=None, penalty=None, bias=None, allowed=None, keep=True,
+         in_place=False):
+    """logits: device [B][V] (maybe strided); the others numpy [B][V], [B][V], [B][3], lists"""
+    B, V = logits.shape
+    args = [None, None, None]
+    if seen is not None:
+        pen = np.zeros((B, 4), dtype=np.float32)
+        pen[:, :3] = penalty
+        args = [_dev(np.stack([chunk_ref.pack(s) for s in seen]), cuda),
+                _dev(counts.astype(np.int32), cuda), _dev(pen, cuda)]
+    bs = None
+    if bias is not None:
+        off = np.concatenate([[0], np.cumsum([len(x) for x in bias])]).astype(np.int32)
+        flat = [e for x in bias for e in x] + [(0, 0.0)]
+        bs = (_dev(off, cuda), _dev(np.array([e[0] for e in flat], dtype=np.int32), cuda),
+              _dev(np.array([e[1] for e in flat], dtype=np.float32), cuda))
+    al = None if allowed is None else _dev(np.stack([chunk_ref.pack(a) for a in allowed]), cuda)
+    host = logits.float().cpu().numpy()
+    tok = torch.full((B,), -9, dtype=torch.int32, device=cuda)
+    pm = torch.full((B,), -9.0, device=cuda)
+    out = logits if in_place else torch.empty_strided(logits.shape, logits.stride(),
+                                                      dtype=logits.dtype, device=cuda) if keep else None
+    status = torch.zeros(1, dtype=torch.int32, device=cuda)
+    lg.lg_pick_token(logits, *args, bs, al, tok, pm, status, out)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    for b in range(B):
+        t, p, x = chunk_ref.pick(host[b], None if seen is None else seen[b],
+                                 None if counts is None else counts[b],
+                                 None if penalty is None else penalty[b],
+                                 None if bias is None else bias[b],
+                                 None if allowed is None else allowed[b])
+        assert tok[b].item() == t, (b, tok[b].item(), t, x[tok[b].item()], x[t])
+        assert abs(pm[b].item() - p) <= p * (V * 2.0 ** -24 + 2.0 ** -20), (b, pm[b].item(), p)
+        if out is not None:
+            want = torch.as_tensor(x).to(logits.dtype).float()
+            assert torch.equal(out[b].float().cpu(), want), b
+    return tok, pm
+
+
+def _history(rng, B, V, n):
+    seen = np.zeros((B, V), dtype=bool)
+    counts = np.zeros((B, V), dtype=np.int64)
+    for b in range(B):
+        ids = rng.integers(0, V, n)
+        seen[b, ids] = True
+        np.add.at(counts[b], ids[n // 2:], 1)
+    pen = rng.random((B, 3)).astype(np.float32) + np.array([0.7, -0.3, -0.2], dtype=np.float32)
+    return seen, counts, pen
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,V", [(1, 1), (2, 7), (1, 31), (3, 33), (5, 1000), (2, 4099),
+                                 (1, 50257), (3, 131072), (1, 151936), (40, 8191), (200, 513)])
+def test_sizes(cuda, dtype, B, V):
+    rng = np.random.default_rng(B * V)
+    x = _dev(rng.standard_normal((B, V)).astype(np.float32) * 3, cuda, chunk_ref.tdtype(dtype))
+    _run(cuda, x)
+    seen, counts, pen = _history(rng, B, V, min(V, 300))
+    bias = [[(int(t), float(v)) for t, v in zip(rng.integers(0, V, 9), rng.standard_normal(9) * 4)]
+            for _ in range(B)]
+    allowed = rng.random((B, V)) < 0.6
+    _run(cuda, x, seen, counts, pen, bias, allowed)
+    _run(cuda, x, seen, counts, pen, keep=False)
+    _run(cuda, x, allowed=allowed, bias=bias)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strided_and_in_place(cuda, dtype):
+    rng = np.random.default_rng(1)
+    for V, pad in ((1001, 6), (777, 0), (640, 3)):
+        for shift in (0, 1, 3):  # rows at every alignment
+            buf = torch.randn((7, V + pad + shift), device=cuda).to(chunk_ref.tdtype(dtype))
+            x = buf[:, shift:shift + V]
+            keep = buf.clone()
+            seen, counts, pen = _history(rng, 7, V, 100)
+            allowed = rng.random((7, V)) < 0.5
+            _run(cuda, x, seen, counts, pen, None, allowed)
+            assert torch.equal(buf, keep)
+            _run(cuda, x, seen, counts, pen, None, allowed, in_place=True)
+            assert torch.equal(buf[:, :shift], keep[:, :shift])
+            assert torch.equal(buf[:, shift + V:], keep[:, shift + V:])
+
+
+def test_ties_go_to_the_lowest_token(cuda):
+    for V in (100, 5000, 140001):
+        x = torch.zeros((4, V), device=cuda)
+        for b, ids in enumerate(([V - 1, 0], [V // 2, V // 2 + 1, V - 1], [17], list(range(V)))):
+            x[b, ids] = 2.5
+        _run(cuda, x)
+        _run(cuda, x.bfloat16())
+
+
+def test_rows_with_nothing_left_and_infinities(cuda):
+    V = 9000
+    x = torch.randn((6, V), device=cuda)
+    allowed = np.ones((6, V), dtype=bool)
+    allowed[0] = False
+    allowed[1] = False
+    allowed[1, V - 1] = True
+    x[1, V - 1] = -50.0
+    x[2] = -math.inf
+    x[3, 5] = math.nan
+    x[3, 100:] = math.nan
+    x[4, [70, 8000]] = math.inf
+    x[5] = float(torch.finfo(torch.float32).min)
+    tok, pm = _run(cuda, x, allowed=allowed)
+    assert tok[0].item() == -1 and pm[0].item() == 0.0 and tok[1].item() == V - 1
+    assert pm[1].item() == 1.0 and tok[2].item() == -1 and pm[4].item() == 0.5
+    _run(cuda, x.bfloat16(), allowed=allowed)
+
+
+def test_bias_lists(cuda):
+    """empty lists, one token twice, tokens outside the vocabulary, long lists"""
+    V = 3001
+    x = torch.randn((4, V), device=cuda)
+    rng = np.random.default_rng(3)
+    bias = [[], [(5, 2.0), (5, 7.25), (5, -1.5)], [(-1, 99.0), (V, 99.0), (V - 1, 9.0), (2 ** 30, 99.0)],
+            [(int(t), float(v)) for t, v in zip(rng.integers(0, V, 2000), rng.standard_normal(2000))]]
+    _run(cuda, x, bias=bias)
+
+
+def test_count_tokens(cuda):
+    V, B = 1003, 3
+    nw = (V + 31) // 32
+    seen = torch.zeros((B, nw), dtype=torch.int32, device=cuda)
+    counts = torch.zeros((B, V), dtype=torch.int32, device=cuda)
+    want_s, want_c = np.zeros((B, V), dtype=bool), np.zeros((B, V), dtype=np.int64)
+    rng = np.random.default_rng(2)
+    rows = [rng.integers(0, V, 400), rng.integers(-5, V + 5, 0), np.full(70000, 17)]
+    rows[0][:50] = 31
+    for generated in (0, 1):
+        off = np.concatenate([[0], np.cumsum([len(r) for r in rows])]).astype(np.int32)
+        ids = np.concatenate(rows + [[-1, V, 2 ** 31 - 1]]).astype(np.int32)
+        off[-1] += 2  # the last row ends with a token of -1 and one past the vocabulary
+        lg.lg_count_tokens(_dev(ids, cuda), _dev(off, cuda), V, generated, seen, counts)
+        for b, r in enumerate(rows):
+            want_s[b, r] = True
+            if generated:
+                np.add.at(want_c[b], r, 1)
+    step = np.array([5, -1, 17], dtype=np.int32)
+    lg.lg_count_tokens(_dev(step, cuda), None, V, 1, seen, counts)
+    want_s[0, 5] = True
+    want_c[0, 5] += 1
+    want_c[2, 17] += 1
+    assert np.array_equal(counts.cpu().numpy(), want_c)
+    assert np.array_equal(seen.cpu().numpy(), np.stack([chunk_ref.pack(s) for s in want_s]))
+
+
+def test_status_and_streams_and_graphs(cuda):
+    V = 20000
+    x = torch.randn((2, V), device=cuda)
+    tok = torch.full((2,), -9, dtype=torch.int32, device=cuda)
+    pm = torch.full((2,), -9.0, device=cuda)
+    status = torch.full((1,), 4, dtype=torch.int32, device=cuda)
+    seen = torch.zeros((2, V // 32), dtype=torch.int32, device=cuda)
+    counts = torch.zeros((2, V), dtype=torch.int32, device=cuda)
+    lg.lg_pick_token(x, None, None, None, None, None, tok, pm, status)
+    lg.lg_count_tokens(tok, None, V, 1, seen, counts, status)
+    assert (tok == -9).all() and (pm == -9.0).all()
+    status.zero_()
+    side = torch.cuda.Stream(device=cuda)
+    torch.cuda.synchronize()
+    pen = torch.tensor([[1.3, 0.1, 0.2, 0.0]] * 2, device=cuda)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side, capture_error_mode="thread_local"):
+        lg.lg_pick_token(x, seen, counts, pen, None, None, tok, pm, status)
+        lg.lg_count_tokens(tok, None, V, 1, seen, counts, status)
+    s, c = np.zeros((2, V), dtype=bool), np.zeros((2, V), dtype=np.int64)
+    host = x.cpu().numpy()
+    for _ in range(8):  # the picked token is penalised, so another comes to the top in time
+        g.replay()
+        torch.cuda.synchronize()
+        for b in range(2):
+            t, _, _ = chunk_ref.pick(host[b], s[b], c[b], [1.3, 0.1, 0.2], None, None)
+            assert tok[b].item() == t
+            s[b, t] = True
+            c[b, t] += 1
+    assert len(np.nonzero(c[0])[0]) > 1
