@@ -622,8 +622,6 @@ __global__ void zero_counters_kernel(int *p, int n) {
 
 // ------------------------------------------------------------------ host side
 
-namespace {
-
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
     void *p = nullptr;
@@ -636,6 +634,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   }();
   return fn;
 }
+
+namespace {
 
 template <int D, int G>
 cudaError_t launch_mma_typed(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,

@@ -169,6 +169,7 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
   a.status = c->dev_status;
   a.part = (float *)ws;
   a.S_total = c->S_total;
+  a.cache_rows = (int64_t)c->L * c->H_kv * c->S_total;
   a.layer = layer;
   a.batch = c->batch;
   a.H_kv = c->H_kv;

@@ -268,9 +268,9 @@ cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) 
   return cudaGetLastError();
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch_d(ChunkAttendArgs &a, int G, cudaStream_t s) {
-  return a.rows == 16 ? launch_typed<T, D, 16>(a, G, s) : launch_typed<T, D, 128>(a, G, s);
+  return a.rows == 16 ? launch_typed<float, D, 16>(a, G, s) : launch_typed<float, D, 128>(a, G, s);
 }
 
 }  // namespace
@@ -284,6 +284,7 @@ cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G
 }
 
 ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
+  if (dtype == LG_BF16) return chunk_grid_tc(g, max_new);
   ChunkGrid r;
   r.rows = (int64_t)max_new * g <= 16 ? 16 : 128;
   r.ctas = 152 * (r.rows == 16 ? 2 : 1);
@@ -295,9 +296,9 @@ ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
 cudaError_t launch_chunk_attend(ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s) {
   cudaError_t e;
   if (dtype == LG_BF16)
-    e = d == 128 ? launch_d<__nv_bfloat16, 128>(a, G, s) : launch_d<__nv_bfloat16, 64>(a, G, s);
+    e = launch_chunk_attend_tc(a, d, G, s);
   else
-    e = d == 128 ? launch_d<float, 128>(a, G, s) : launch_d<float, 64>(a, G, s);
+    e = d == 128 ? launch_d<128>(a, G, s) : launch_d<64>(a, G, s);
   if (e != cudaSuccess) return e;
   return launch_chunk_merge(a, dtype, d, G, s);
 }

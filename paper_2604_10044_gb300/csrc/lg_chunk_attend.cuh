@@ -21,6 +21,7 @@ struct ChunkAttendArgs {
   int32_t *status;
   float *part;             // [2 G][rows][d] partial sums, then [2 G][rows][2] maxima and normalisers
   int64_t S_total;
+  int64_t cache_rows;      // L * H_kv * S_total
   int layer, batch, H_kv, g, T, max_new, max_len;
   int rows;                // of an item: tok * g rounded up to whole query tiles
   float qscale;            // softmax scale * log2(e)
@@ -181,6 +182,10 @@ __device__ __forceinline__ bool row_sees(const TileRows &r, const ChunkShape &s,
                                          int i) {
   return i <= query_row && (s.window == 0 || i > query_row - s.window || i < s.sink);
 }
+
+// bf16: the kernel on the tensor cores (lg_chunk_attend_tc.cu)
+ChunkGrid chunk_grid_tc(int g, int max_new);
+cudaError_t launch_chunk_attend_tc(const ChunkAttendArgs &a, int d, int G, cudaStream_t s);
 
 // the merge of items that several CTAs share (lg_chunk_attend.cu)
 cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s);
