@@ -14,7 +14,7 @@ LIB = os.path.join(_HERE, "liblg.so")
 SOURCES = ["lg_attend.cu", "lg_attend_mma.cu", "lg_attend_cluster.cu",
            "lg_attend_cluster_f32.cu", "lg_guard.cu", "lg_token.cu", "lg_api.cu",
            "lg_noalloc.cu", "lg_chunk.cu", "lg_chunk_attend.cu",
-           "lg_chunk_attend_tc.cu", "lg_pick.cu",
+           "lg_chunk_attend_tc.cu", "lg_chunk_attend_few.cu", "lg_pick.cu",
            "lg_chunk_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-fvisibility=hidden",

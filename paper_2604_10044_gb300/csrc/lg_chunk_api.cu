@@ -180,7 +180,7 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
   a.rows = grid.rows;
   a.qscale = scale * 1.4426950408889634f;
   a.shape.tok = grid.tok;
-  a.shape.bn = grid.bn;
+  a.shape.bn2 = grid.bn2;
   a.shape.window = window;
   a.shape.sink = n_sink;
   return cuda_status(lg::launch_chunk_attend(a, c->dtype, c->d, grid.ctas, s));

@@ -222,28 +222,45 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
   int last = c;
   while (last + 1 < G && range_bound(sh.W, last + 1, G) < w.x + w.cost) ++last;
   const int used = w.tokens(a) * a.g, tok0 = w.off + w.t * a.shape.tok, H_q = a.H_kv * a.g;
+  auto cut = [&](int p) {
+    return cut_block(range_bound(sh.W, p, G) - w.x, w.cost, w.blocks.count, a.shape.bn2);
+  };
+  // 32 pieces at a time, a lane each: whether it has blocks, its maximum and normaliser
   for (int r = blockIdx.y * (kThreads / 32) + warp; r < used; r += gridDim.y * (kThreads / 32)) {
     float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) o[k] = 0.f;
     bool whole = false;
-    for (int p = c - 1; p <= last; ++p) {
-      const int b0 = cut_block(range_bound(sh.W, p, G) - w.x, w.cost, w.blocks.count);
-      const int b1 = cut_block(range_bound(sh.W, p + 1, G) - w.x, w.cost, w.blocks.count);
-      if (b0 == b1) continue;
-      if (b0 == 0 && b1 == w.blocks.count) {
-        whole = true;  // one piece has every block: its CTA wrote the result
-        break;
-      }
-      const int slot = p == c - 1 ? 1 : 0;
-      const float2 ml = *part_ml(a, D, G, p, slot, r);
-      const float *src = part_row(a, D, p, slot, r);
-      const float mx = fmaxf(m, ml.x), base = mx == -INFINITY ? 0.f : mx;
-      const float f0 = exp2_fast(m - base), f1 = exp2_fast(ml.x - base);
-      l = l * f0 + ml.y * f1;
+    for (int p0 = c - 1; p0 <= last && !whole; p0 += 32) {
+      const int p = p0 + lane;
+      const int b0 = p <= last ? cut(p) : 0, b1 = p <= last ? cut(p + 1) : 0;
+      const bool some = b0 < b1;
+      // one piece has every block: its CTA wrote the result
+      whole = __any_sync(0xffffffffu, some && b0 == 0 && b1 == w.blocks.count);
+      if (whole) break;
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (some) ml = *part_ml(a, D, G, p, p == c - 1 ? 1 : 0, r);
+      float mx = fmaxf(m, ml.x);
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = o[k] * f0 + src[lane + 32 * k] * f1;
+      for (int i = 16; i; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, i));
+      const float base = mx == -INFINITY ? 0.f : mx;
+      const float f0 = exp2_fast(m - base), f = some ? exp2_fast(ml.x - base) : 0.f;
+      float lp = ml.y * f;
+#pragma unroll
+      for (int i = 16; i; i >>= 1) lp += __shfl_xor_sync(0xffffffffu, lp, i);
+      l = l * f0 + lp;
       m = mx;
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] *= f0;
+      const unsigned have = __ballot_sync(0xffffffffu, some);
+#pragma unroll 4
+      for (int i = 0; i < 32; ++i) {
+        if (!(have >> i & 1)) continue;
+        const float fi = __shfl_sync(0xffffffffu, f, i);
+        const float *src = part_row(a, D, p0 + i, p0 + i == c - 1 ? 1 : 0, r);
+#pragma unroll
+        for (int k = 0; k < V; ++k) o[k] += src[lane + 32 * k] * fi;
+      }
     }
     if (whole) continue;
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -289,7 +306,7 @@ ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
   r.rows = (int64_t)max_new * g <= 16 ? 16 : 128;
   r.ctas = 152 * (r.rows == 16 ? 2 : 1);
   r.tok = r.rows / g;
-  r.bn = kBn;
+  r.bn2 = 6;
   return r;
 }
 

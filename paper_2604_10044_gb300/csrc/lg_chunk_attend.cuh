@@ -128,9 +128,9 @@ struct ChunkWalk {
     row0 = ((int64_t)a.layer * a.H_kv + kvh) * a.S_total + a.seq_off[b];
     rows = tile_rows(q, a.shape, t);
     cost = tile_cost(q, a.shape, t);
-    blocks = tile_blocks(rows, a.shape.bn);
-    blk0 = cut_block(y0 - x, cost, blocks.count);
-    blk1 = cut_block(y1 - x, cost, blocks.count);
+    blocks = tile_blocks(rows, a.shape.bn2);
+    blk0 = cut_block(y0 - x, cost, blocks.count, a.shape.bn2);
+    blk1 = cut_block(y1 - x, cost, blocks.count, a.shape.bn2);
   }
   // the item that cost unit y falls into, y in sequence sh.b
   __device__ __forceinline__ void start(const ChunkAttendArgs &a, const ChunkShare &sh, int64_t y) {
@@ -139,7 +139,7 @@ struct ChunkWalk {
     y1 = sh.y1;
     load_seq(a);
     per_head = tiles_cost(q, a.shape, tiles);
-    kvh = (int)((y - sh.x) / per_head);
+    kvh = (int)plan_div(y - sh.x, per_head);
     const int64_t in = y - sh.x - kvh * per_head;
     t = tile_at(q, a.shape, in);
     x = sh.x + kvh * per_head + tiles_cost(q, a.shape, t);
@@ -186,6 +186,8 @@ __device__ __forceinline__ bool row_sees(const TileRows &r, const ChunkShape &s,
 // bf16: the kernel on the tensor cores (lg_chunk_attend_tc.cu)
 ChunkGrid chunk_grid_tc(int g, int max_new);
 cudaError_t launch_chunk_attend_tc(const ChunkAttendArgs &a, int d, int G, cudaStream_t s);
+
+cudaError_t launch_chunk_attend_few(const ChunkAttendArgs &a, int d, int G, cudaStream_t s);
 
 // the merge of items that several CTAs share (lg_chunk_attend.cu)
 cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G, cudaStream_t s);

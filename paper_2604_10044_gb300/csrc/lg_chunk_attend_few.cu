@@ -1,0 +1,448 @@
+// lg_chunk_attend of bf16 caches for few query rows of a kv-head (a token, or some proposed tokens,
+// a sequence): the call reads the cache once and computes little, so the products are turned round,
+//   S^T = K Q^T  (M = 128 keys, N query rows),  O^T += V^T P^T  (M = head elements),
+// and no part of them is padding.  A thread holds one key's scores of all N rows (N = 16, 32 or 64:
+// row r is token r / g, head r % g); it exponentiates them, adds them to its own sums of the
+// normalisers and writes its row of P^T to shared memory, the products' second operand.  The maxima
+// are the CTA's: as in the kernel for many rows they may lag by a factor 2^8, so a block asks only
+// whether any score passed that bound (one barrier), and the exact maxima are formed in the first
+// block and when one did.
+//
+// Scores are two blocks ahead of the sums (two buffers of S^T and P^T), and the ring holds five
+// blocks of keys or values.
+//
+// Warps: 0-3 the keys (and the results: a thread a head element), 4 walks along the work and copies, 5 issues the products,
+// 6 and 7 clear what is not a number from values of blocks that hide a row from a query.
+#include "lg_chunk_tc.cuh"
+
+namespace lg {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBn = kTcBn;
+constexpr int kPBytes = kBn * 128;  // a buffer of P^T: 128-byte rows, swizzled
+constexpr float kLazy = 8.f;
+constexpr uint32_t kTmemCols = 256;
+
+template <int D, int N>
+struct FewCfg {
+  static constexpr int kBoxes = D / 64;
+  static constexpr int kTile = kBn * D * 2;
+  static constexpr int kQBox = N * 128;
+  static constexpr int kQBytes = (kBoxes * kQBox + 1023) / 1024 * 1024;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kSmem = kQBytes + 2 * kPBytes + kStages * kTile + 1024;
+};
+
+template <int ST, int N>
+struct FewBars {
+  uint64_t full[ST], empty[ST], fixed[ST];
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2], p_full[2];
+  uint64_t o_full[2], o_free;  // sums of even and odd blocks ready: a wait is never two phases away
+  TcQueue queue;
+  uint32_t tmem;
+  volatile int give_up;
+  float col[4][N];  // a warp's maxima or normalisers
+};
+
+// a barrier of the 128 key threads; with a condition: whether it held for any
+__device__ __forceinline__ void keys_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool keys_any(bool p) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n"
+      " selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"((uint32_t)p)
+      : "memory");
+  return r != 0;
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+template <int N>
+__device__ __forceinline__ void load_cols(uint32_t addr, uint32_t *v) {
+  if constexpr (N == 16) {
+    tmem_load16(addr, v);
+  } else {
+#pragma unroll
+    for (int x = 0; x < N; x += 32) tmem_load32(addr + x, v + x);
+  }
+  tmem_wait_load();
+}
+
+template <int N>
+__device__ __forceinline__ void store_cols(uint32_t addr, const uint32_t *v) {
+  if constexpr (N == 16) {
+    tmem_store16(addr, v);
+  } else {
+#pragma unroll
+    for (int x = 0; x < N; x += 32) tmem_store32(addr + x, v + x);
+  }
+  tmem_wait_store();
+}
+
+template <int D, int N>
+__global__ void __launch_bounds__(kThreads, 1)
+    chunk_attend_few_kernel(const __grid_constant__ CUtensorMap mq,
+                            const __grid_constant__ CUtensorMap mk,
+                            const __grid_constant__ CUtensorMap mv, ChunkAttendArgs a) {
+  using C = FewCfg<D, N>;
+  constexpr int ST = C::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(16) FewBars<ST, N> bars;
+  uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t *sq = smem, *sp = sq + C::kQBytes, *ring = sp + 2 * kPBytes;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  if (tid == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(&bars.full[i], 1);
+      mbar_init(&bars.empty[i], 3);
+      mbar_init(&bars.fixed[i], 2);
+    }
+    mbar_init(&bars.q_full, 1);
+    mbar_init(&bars.q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.s_full[i], 1);
+      mbar_init(&bars.p_full[i], 4);
+      mbar_init(&bars.o_full[i], 1);
+    }
+    mbar_init(&bars.o_free, 4);
+    bars.queue.init(7);  // the products, two clearing warps, four warps of keys
+    bars.give_up = 0;
+    mbar_fence_init();
+  }
+  if (warp == 5) tmem_alloc(&bars.tmem, kTmemCols);
+  pdl_enter();
+  ChunkShare sh;
+  tc_fence_before();
+  bool work = chunk_share<kThreads>(a, blockIdx.x, gridDim.x, sh);
+  __syncthreads();
+  tc_fence_after();
+  work = work && sh.y0 < sh.y1;
+  const uint32_t tmem = bars.tmem;  // S^T at columns 0 and N, O^T at 2 N
+
+  if (work && warp == 4) {
+    if (lane == 0) {
+      ChunkWalk w;
+      uint32_t n = 0, pieces = 0;
+      bool ok = true;
+      auto load = [&](const CUtensorMap *map, int row) {
+        const uint32_t st = n % ST;
+        ok = ok && tc_wait(bars, &bars.empty[st], ((n / ST) & 1) ^ 1);
+        if (!ok) return;
+        mbar_arrive_expect_tx(&bars.full[st], C::kTile);
+#pragma unroll
+        for (int x = 0; x < C::kBoxes; ++x)
+          tma_box_2d(ring + st * C::kTile + x * (kBn * 128), map, 64 * x, row, &bars.full[st]);
+        ++n;
+      };
+      for (w.start(a, sh, sh.y0); ok && !w.done(); w.next(a)) {
+        if (w.blk0 == w.blk1) continue;
+        const int r0 = (int)w.row0;
+        ok = bars.queue.put(bars, pieces, &w, a) && tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
+        if (!ok) break;
+        mbar_arrive_expect_tx(&bars.q_full, C::kBoxes * a.shape.tok * a.g * 128);
+#pragma unroll
+        for (int x = 0; x < C::kBoxes; ++x)
+          tma_box_3d(sq + x * C::kQBox, &mq, 64 * x, w.kvh * a.g, w.off + w.t * a.shape.tok,
+                     &bars.q_full);
+        ++pieces;
+        // keys a block ahead of the values, as the products take them
+        load(&mk, r0 + w.blocks.index(w.blk0) * kBn);
+        for (int j = w.blk0; ok && j < w.blk1; ++j) {
+          if (j + 1 < w.blk1) load(&mk, r0 + w.blocks.index(j + 1) * kBn);
+          load(&mv, r0 + w.blocks.index(j) * kBn);
+        }
+      }
+      if (ok) bars.queue.put(bars, pieces, nullptr, a);
+    }
+  } else if (work && warp == 5) {
+    if (lane == 0) {
+      uint32_t n = 0, c = 0;
+      bool ok = true;
+      constexpr uint32_t kIdS = mma_idesc(128, N, false, false);
+      constexpr uint32_t kIdO = mma_idesc(128, N, true, true);
+      // a head of 64 elements fills 64 of the 128 rows: the others repeat them
+      constexpr uint32_t kLboV = D == 128 ? kBn * 128 : 0;
+      const uint64_t dq = smem_desc(smem_addr(sq), 16, 1024);
+      auto stage = [&](uint32_t i) { return smem_addr(ring + i % ST * C::kTile); };
+      auto wait_full = [&](uint32_t i) {
+        ok = ok && tc_wait(bars, &bars.full[i % ST], (i / ST) & 1);
+      };
+      for (uint32_t pc = 0;; ++pc) {
+        ok = bars.queue.wait(bars, pc);
+        if (!ok) break;
+        const TcPiece &p = bars.queue.at(pc);
+        if (p.blk1 < 0) break;
+        const int blk0 = p.blk0, blocks = p.blk1 - blk0;
+        const TileRows rows = p.rows;
+        const TileBlocks tb = p.blocks;
+        bars.queue.done(pc);
+        ok = tc_wait(bars, &bars.q_full, pc & 1);
+        auto k_at = [&](int j) { return n + (j == 0 ? 0 : 2 * j - 1); };
+        auto scores = [&](int j) {
+          wait_full(k_at(j));
+          if (!ok) return;
+          tc_fence_after();
+          const uint64_t dk = smem_desc(stage(k_at(j)), 16, 1024);
+          const uint32_t b = (c + j) & 1;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            tc_mma_ss(tmem + b * N, dk + (uint64_t)(((k / 4) * (kBn * 128) + (k % 4) * 32) >> 4),
+                      dq + (uint64_t)(((k / 4) * C::kQBox + (k % 4) * 32) >> 4), kIdS, k > 0);
+          tc_commit(&bars.s_full[b]);
+          tc_commit(&bars.empty[k_at(j) % ST]);
+          if (j + 1 == blocks) tc_commit(&bars.q_empty);
+        };
+        scores(0);
+        for (int j = 0; ok && j < blocks; ++j) {
+          if (j + 1 < blocks) scores(j + 1);
+          const uint32_t iv = n + (j + 1 < blocks ? 2 * j + 2 : 2 * j + 1), b = (c + j) & 1;
+          wait_full(iv);
+          if (block_hides(rows, a.shape, tb.index(blk0 + j) * kBn))
+            ok = ok && tc_wait(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
+          if (j == 0) ok = ok && tc_wait(bars, &bars.o_free, (pc & 1) ^ 1);
+          ok = ok && tc_wait(bars, &bars.p_full[b], ((c + j) >> 1) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t dv = smem_desc(stage(iv), kLboV, 1024);
+          const uint64_t dp = smem_desc(smem_addr(sp + b * kPBytes), 16, 1024);
+#pragma unroll
+          for (int k = 0; k < kBn / 16; ++k)
+            tc_mma_ss(tmem + 2 * N, dv + (uint64_t)(k * 2048 >> 4), dp + (uint64_t)(k * 2048 >> 4),
+                      kIdO, j > 0 || k > 0);
+          tc_commit(&bars.o_full[b]);
+          tc_commit(&bars.empty[iv % ST]);
+        }
+        if (!ok) break;
+        c += blocks;
+        n += 2 * blocks;
+      }
+    }
+  } else if (work && warp >= 6) {
+    uint32_t n = 0;
+    bool ok = true;
+    for (uint32_t pc = 0; ok; ++pc) {
+      ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+      if (!ok) break;
+      TcPiece &p = bars.queue.at(pc);
+      if (p.blk1 < 0) break;
+      const int blocks = p.blk1 - p.blk0;
+      for (int i = 0; i < 2 * blocks; ++i, ++n) {
+        // the i-th copy of the piece: the values of block j, or keys
+        const int j = i == 2 * blocks - 1 ? blocks - 1 : i >= 2 && !(i & 1) ? i / 2 - 1 : -1;
+        ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.full[n % ST], (n / ST) & 1));
+        if (!ok) break;
+        const int i0 = j < 0 ? 0 : p.blocks.index(p.blk0 + j) * kBn;
+        if (j >= 0 && block_hides(p.rows, a.shape, i0)) {
+          if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 192, 64)) p.bad = 1;
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        if (lane == 0) {
+          mbar_arrive(&bars.fixed[n % ST]);
+          mbar_arrive(&bars.empty[n % ST]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) bars.queue.done(pc);
+    }
+  } else if (work) {
+    const uint32_t lanes = (uint32_t)warp << 21;
+    const int H_q = a.H_kv * a.g;
+    uint32_t c = 0;
+    bool ok = true;
+    for (uint32_t pc = 0; ok; ++pc) {
+      ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+      if (keys_any(!ok)) break;
+      const TcPiece &w = bars.queue.at(pc);
+      if (w.blk1 < 0) break;
+      const int used = w.tokens * a.g;
+      float m[N], l[N];
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        m[q] = -INFINITY;
+        l[q] = 0.f;
+      }
+      for (int blk = w.blk0; blk < w.blk1; ++blk, ++c) {
+        const uint32_t b = c & 1;
+        ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[b], (c >> 1) & 1));
+        // a role that gave up is seen by every key warp before the barriers below
+        if (keys_any(!ok)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t u[N];
+        load_cols<N>(tmem + b * N + lanes, u);
+        float *v = (float *)u;
+        const int i0 = w.blocks.index(blk) * kBn;
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] *= a.qscale;
+        if (block_hides(w.rows, a.shape, i0)) {
+#pragma unroll
+          for (int q = 0; q < N; ++q)
+            if (!row_sees(w.rows, a.shape, w.rows.first + q / a.g, i0 + tid)) v[q] = -INFINITY;
+        }
+        bool rise = blk == w.blk0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) rise |= q < used && v[q] > m[q] + kLazy;
+        if (keys_any(rise)) {
+#pragma unroll
+          for (int q = 0; q < N; ++q) {
+            const float x = warp_max(v[q]);
+            if (lane == 0) bars.col[warp][q] = x;
+          }
+          keys_sync();
+          float f[N];
+#pragma unroll
+          for (int q = 0; q < N; ++q) {
+            const float x = fmaxf(fmaxf(bars.col[0][q], bars.col[1][q]),
+                                  fmaxf(bars.col[2][q], bars.col[3][q]));
+            const float m1 = fmaxf(m[q], x);
+            f[q] = m1 == -INFINITY ? 0.f : exp2_fast(m[q] - m1);
+            m[q] = m1;
+            l[q] *= f[q];
+          }
+          keys_sync();  // the maxima have been read
+          if (blk > w.blk0) {
+            ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
+            if (keys_any(!ok)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            uint32_t o[N];
+            load_cols<N>(tmem + 2 * N + lanes, o);
+#pragma unroll
+            for (int q = 0; q < N; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f[q]);
+            store_cols<N>(tmem + 2 * N + lanes, o);
+            tc_fence_before();
+          }
+        }
+        uint8_t *row = sp + b * kPBytes + tid * 128;
+#pragma unroll
+        for (int q = 0; q < N; q += 8) {
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            float p[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const float mm = m[q + e + x];
+              p[x] = exp2_fast(v[q + e + x] - (mm == -INFINITY ? 0.f : mm));
+              l[q + e + x] += p[x];
+            }
+            const __nv_bfloat162 z = __floats2bfloat162_rn(p[0], p[1]);
+            h[e / 2] = *(const uint32_t *)&z;
+          }
+          *(uint4 *)(row + (((q / 8) ^ (tid & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.p_full[b]);
+      }
+      if (!ok) break;
+      // normalisers: a warp's sums, then the CTA's
+#pragma unroll
+      for (int q0 = 0; q0 < N; q0 += 32) {
+        constexpr int M = N < 32 ? N : 32;
+        HeadReduce<M, 16>::run(l + q0, lane);  // lane: column q0 + lane / (32 / M)
+        if (lane % (32 / M) == 0) bars.col[warp][q0 + lane / (32 / M)] = l[q0];
+      }
+      ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
+      if (keys_any(!ok)) break;
+      tc_fence_after();
+      uint32_t o[N];
+      load_cols<N>(tmem + 2 * N + lanes, o);
+      const bool whole = w.slot < 0;
+      const int tok0 = w.tok0;
+      if (w.bad) {  // what was cleared, for the queries that see it
+        for (int blk = w.blk0; blk < w.blk1; ++blk) {
+          const int i0 = w.blocks.index(blk) * kBn;
+          if (!block_hides(w.rows, a.shape, i0)) continue;
+          for (int i = i0; i < i0 + kBn && i < w.n; ++i) {
+            const float z = __bfloat162float(
+                ((const __nv_bfloat16 *)a.V)[(w.row0 + i) * D + tid % D]);
+            if (isfinite(z)) continue;
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+              if (row_sees(w.rows, a.shape, w.rows.first + q / a.g, i))
+                o[q] = __float_as_uint(__uint_as_float(o[q]) + z);
+          }
+        }
+      }
+      if (tid < D) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+          if (q >= used) continue;
+          const float sum = (bars.col[0][q] + bars.col[1][q]) + (bars.col[2][q] + bars.col[3][q]);
+          const float x = __uint_as_float(o[q]);
+          if (whole) {
+            ((__nv_bfloat16 *)a.out)[((int64_t)(tok0 + q / a.g) * H_q + w.kvh * a.g + q % a.g) * D +
+                                     tid] = __float2bfloat16_rn(sum != 0.f ? x / sum : 0.f);
+          } else {
+            part_row(a, D, blockIdx.x, w.slot, q)[tid] = x;
+            if (tid == 0) *part_ml(a, D, gridDim.x, blockIdx.x, w.slot, q) = make_float2(m[q], sum);
+          }
+        }
+      }
+      keys_sync();  // the normalisers have been read
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&bars.o_free);
+        bars.queue.done(pc);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (bars.give_up) {  // copies and products in flight end before the memory is handed on
+    if (tid == 0) set_status(a.status, LG_ERR_TIMEOUT);
+    linger();
+    __syncthreads();
+  }
+  if (warp == 5) {
+    tc_fence_after();
+    tmem_free(tmem, kTmemCols);
+  }
+}
+
+template <int D, int N>
+cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
+  CUtensorMap mq, mk, mv;
+  if (!make_q_map(&mq, a.q, D, a.H_kv * a.g, a.T, a.g, a.shape.tok) ||
+      !make_kv_map(&mk, a.K, LG_BF16, D, a.cache_rows, kBn) ||
+      !make_kv_map(&mv, a.V, LG_BF16, D, a.cache_rows, kBn))
+    return cudaErrorInvalidValue;
+  auto kern = chunk_attend_few_kernel<D, N>;
+  LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              FewCfg<D, N>::kSmem));
+  LG_TRY(launch_pdl(kern, G, kThreads, FewCfg<D, N>::kSmem, s, mq, mk, mv, a));
+  return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_d(const ChunkAttendArgs &a, int G, cudaStream_t s) {
+  return a.rows == 16 ? launch_typed<D, 16>(a, G, s)
+         : a.rows == 32 ? launch_typed<D, 32>(a, G, s)
+                        : launch_typed<D, 64>(a, G, s);
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_attend_few(const ChunkAttendArgs &a, int d, int G, cudaStream_t s) {
+  return d == 128 ? launch_d<128>(a, G, s) : launch_d<64>(a, G, s);
+}
+
+}  // namespace lg

@@ -25,7 +25,7 @@ constexpr int kItemCost = 96;
 
 struct ChunkShape {
   int tok;     // tokens of a tile
-  int bn;      // rows of a key block
+  int bn2;     // log2 of the rows of a key block
   int window;  // 0: none
   int sink;
 };
@@ -40,6 +40,12 @@ struct ChunkSeq {
 
 __host__ __device__ __forceinline__ int64_t plan_min(int64_t a, int64_t b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int64_t plan_max(int64_t a, int64_t b) { return a > b ? a : b; }
+
+// a / b of numbers that mostly fit 32 bits (a 64-bit division takes some 100 instructions)
+__host__ __device__ __forceinline__ int64_t plan_div(int64_t a, int64_t b) {
+  if (((uint64_t)a | (uint64_t)b) >> 32 == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
 
 // rows tile t's queries see: first query row `first`, last `last`; rows [0, sinks) and [lo, last]
 struct TileRows {
@@ -76,7 +82,7 @@ __host__ __device__ __forceinline__ int64_t tiles_cost(const ChunkSeq &q, const 
   int64_t sum = T * ((int64_t)q.n - q.m + kItemCost) + tok * (T * (T + 1) / 2);
   if (s.window) {
     const int64_t a = (int64_t)q.n - q.m + 1 - s.window - s.sink;
-    const int64_t i0 = a >= 0 ? 0 : (-a + tok - 1) / tok;
+    const int64_t i0 = a >= 0 ? 0 : -a >= T * tok ? T : plan_div(-a + tok - 1, tok);
     if (i0 < T) sum -= (T - i0) * a + tok * ((T * (T - 1) - i0 * (i0 - 1)) / 2);
   }
   return sum + extra;
@@ -104,26 +110,28 @@ struct TileBlocks {
   }
 };
 
-__host__ __device__ __forceinline__ TileBlocks tile_blocks(const TileRows &r, int bn) {
+__host__ __device__ __forceinline__ TileBlocks tile_blocks(const TileRows &r, int bn2) {
   TileBlocks b;
-  const int w0 = r.lo / bn, w1 = r.last / bn + 1;
-  b.sink_blocks = (r.sinks + bn - 1) / bn;
+  const int w0 = r.lo >> bn2, w1 = (r.last >> bn2) + 1;
+  b.sink_blocks = (int)(((int64_t)r.sinks + (1 << bn2) - 1) >> bn2);
   if (b.sink_blocks > w0) b.sink_blocks = w0;  // a block of both kinds counts once
   b.skip = w0 - b.sink_blocks;
   b.count = b.sink_blocks + w1 - w0;
   return b;
 }
 
-// first cost unit of CTA c
+// first cost unit of CTA c of G
 __host__ __device__ __forceinline__ int64_t range_bound(int64_t W, int c, int G) {
-  return W / G * c + W % G * c / G;
+  const int64_t per = plan_div(W, G);
+  return per * c + (uint32_t)(W - per * G) * (uint32_t)c / (uint32_t)G;
 }
 
-// blocks before a cut at cost unit y (0..cost) of an item
-__host__ __device__ __forceinline__ int cut_block(int64_t y, int64_t cost, int count) {
-  if (y <= 0) return 0;
+// blocks before a cut at cost unit y of an item: in whole blocks of the rows that the units stand
+// for, the item's own cost first
+__host__ __device__ __forceinline__ int cut_block(int64_t y, int64_t cost, int count, int bn2) {
   if (y >= cost) return count;
-  return (int)((y * count + cost / 2) / cost);
+  const int64_t rows = y - kItemCost + ((1 << bn2) >> 1);
+  return rows <= 0 ? 0 : (int)plan_min(rows >> bn2, count);
 }
 
 }  // namespace lg

@@ -109,7 +109,7 @@ struct ChunkGrid {
   int ctas;  // of the persistent kernel
   int rows;  // of an item
   int tok;   // tokens of an item
-  int bn;    // rows of a key block
+  int bn2;   // log2 of the rows of a key block
 };
 struct ChunkAttendArgs;
 ChunkGrid chunk_grid(int dtype, int d, int g, int max_new);

@@ -50,9 +50,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint3
          (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-// Instruction descriptor: bf16 x bf16 -> fp32, A K-major, B K-major or MN-major
-__host__ __device__ constexpr uint32_t mma_idesc(int m, int n, bool b_mn_major) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 |
+// Instruction descriptor: bf16 x bf16 -> fp32, each operand K-major or MN-major
+__host__ __device__ constexpr uint32_t mma_idesc(int m, int n, bool a_mn_major, bool b_mn_major) {
+  return 1u << 4 | 1u << 7 | 1u << 10 | (a_mn_major ? 1u << 15 : 0u) |
+         (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 |
          (uint32_t)(m >> 4) << 24;
 }
 
@@ -98,6 +99,23 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t *v) {
       "%11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, "
       "%29, %30, %31};" ::LG_W8(v, 0),
       LG_W8(v, 8), LG_W8(v, 16), LG_W8(v, 24), "r"(addr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t *v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
+      "%12, %13, %14, %15}, [%16];"
+      : LG_R8(v, 0), LG_R8(v, 8)
+      : "r"(addr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t *v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, "
+      "%10, %11, %12, %13, %14, %15};" ::LG_W8(v, 0),
+      LG_W8(v, 8), "r"(addr)
       : "memory");
 }
 

@@ -25,7 +25,7 @@ static int pick(std::initializer_list<int> l) { return l.begin()[uni(0, (int)l.s
 static ChunkShape shape() {
   ChunkShape s;
   s.tok = (int)uni(1, 256);
-  s.bn = pick({64, 128});
+  s.bn2 = pick({6, 7});
   s.window = uni(0, 2) ? (int)uni(1, pick({3, 200, 5000, 2147483647})) : 0;
   s.sink = pick({0, 1, 4, 64, 129, 1000});
   return s;
@@ -49,13 +49,13 @@ int main() {
       CHECK(c > kItemCost);
       CHECK(tile_at(q, s, sum) == t && tile_at(q, s, sum + c - 1) == t);
       const TileRows r = tile_rows(q, s, t);
-      const TileBlocks b = tile_blocks(r, s.bn);
+      const TileBlocks b = tile_blocks(r, s.bn2);
       // seen by some query of the tile <=> in a block of the tile, up to whole blocks
       std::set<int> want, got;
       for (int j = t * s.tok; j < q.m && j < (t + 1) * s.tok; ++j) {
         const int row = q.n - q.m + j;
         for (int i = 0; i <= row; ++i)
-          if (s.window == 0 || (int64_t)i > (int64_t)row - s.window || i < s.sink) want.insert(i / s.bn);
+          if (s.window == 0 || (int64_t)i > (int64_t)row - s.window || i < s.sink) want.insert(i >> s.bn2);
       }
       for (int i = 0; i < b.count; ++i) CHECK(got.insert(b.index(i)).second);
       CHECK(want == got);
@@ -76,7 +76,7 @@ int main() {
         for (int t = 0; t < x.tiles(s.tok); ++t) {
           start.push_back(W);
           cost.push_back(tile_cost(x, s, t));
-          count.push_back(tile_blocks(tile_rows(x, s, t), s.bn).count);
+          count.push_back(tile_blocks(tile_rows(x, s, t), s.bn2).count);
           W += cost.back();
         }
     }
@@ -89,8 +89,8 @@ int main() {
       int slots[2] = {0, 0};
       for (size_t i = 0; i < start.size(); ++i) {
         if (start[i] + cost[i] <= y0 || start[i] >= y1) continue;
-        const int b0 = cut_block(y0 - start[i], cost[i], count[i]);
-        const int b1 = cut_block(y1 - start[i], cost[i], count[i]);
+        const int b0 = cut_block(y0 - start[i], cost[i], count[i], s.bn2);
+        const int b1 = cut_block(y1 - start[i], cost[i], count[i], s.bn2);
         CHECK(b0 == next[i] && b1 >= b0);
         next[i] = b1;
         if (b0 == b1 || (b0 == 0 && b1 == count[i])) continue;
@@ -103,11 +103,11 @@ int main() {
   }
   // the largest line: no 64-bit overflow in the bounds or the cuts
   const ChunkSeq big{2147483647, 2147483647};
-  const ChunkShape s{16, 64, 0, 0};
+  const ChunkShape s{16, 6, 0, 0};
   const int64_t W = tiles_cost(big, s, big.tiles(s.tok)) / 2;
   CHECK(W > 0 && range_bound(W, 304, 304) == W && range_bound(W, 152, 304) <= W / 2 + 1);
   const int64_t c = tile_cost(big, s, big.tiles(16) - 1);
-  CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1) <= 2147483647 / 64 + 1);
+  CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1, 6) <= 2147483647 / 64 + 1);
   puts("ok");
 }
 """
