@@ -30,12 +30,6 @@ __device__ __forceinline__ void load4<float>(const void *p, int64_t i, float *f)
   const float4 v = *(const float4 *)((const float *)p + i);
   f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
 }
-template <>
-__device__ __forceinline__ void load4<__nv_bfloat16>(const void *p, int64_t i, float *f) {
-  const uint2 v = *(const uint2 *)((const __nv_bfloat16 *)p + i);
-  const float2 x = bf16x2_to_float2(v.x), y = bf16x2_to_float2(v.y);
-  f[0] = x.x, f[1] = x.y, f[2] = y.x, f[3] = y.y;
-}
 
 template <typename T>
 __device__ __forceinline__ void store4(void *p, int64_t i, const float *f);
@@ -43,12 +37,6 @@ template <>
 __device__ __forceinline__ void store4<float>(void *p, int64_t i, const float *f) {
   *(float4 *)((float *)p + i) = make_float4(f[0], f[1], f[2], f[3]);
 }
-template <>
-__device__ __forceinline__ void store4<__nv_bfloat16>(void *p, int64_t i, const float *f) {
-  __nv_bfloat162 v[2] = {__floats2bfloat162_rn(f[0], f[1]), __floats2bfloat162_rn(f[2], f[3])};
-  *(uint2 *)((__nv_bfloat16 *)p + i) = *(const uint2 *)v;
-}
-
 template <int D, int BM>
 struct SimtCfg {
   static constexpr int kRow = D + 4;  // floats of a staged row: 16 rows of 16 bytes, no conflicts
@@ -65,9 +53,9 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
   const int H_q = a.H_kv * a.g;
   pdl_enter();
   ChunkShare sh;
-  if (!chunk_share<kThreads>(a, blockIdx.x, gridDim.x, sh)) return;
+  if (!chunk_share(a, blockIdx.x, gridDim.x, sh)) return;
   ChunkWalk w;
-  for (w.start(a, sh, sh.y0); !w.done(); w.next(a)) {
+  for (w.start(a, sh); !w.done(); w.next(a)) {
     if (w.blk0 == w.blk1) continue;
     const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
     const int tok0 = w.off + w.t * a.shape.tok;
@@ -214,9 +202,9 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
   pdl_enter();
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ChunkShare sh;
-  if (!chunk_share<kThreads>(a, c, G, sh)) return;
+  if (!chunk_share(a, c, G, sh)) return;
   ChunkWalk w;
-  w.start(a, sh, sh.y0);
+  w.start(a, sh);
   if (w.x == sh.y0) return;  // the bound falls between items
   if (range_bound(sh.W, c - 1, G) > w.x) return;  // an earlier bound cuts the item too
   int last = c;

@@ -28,121 +28,121 @@ struct ChunkAttendArgs {
   ChunkShape shape;
 };
 
-// a CTA's share: cost units [y0, y1) of the line, and the sequence that y0 falls into
+// a CTA's share: cost units [y0, y1) of the line of W, and the sequence that y0 falls into
 struct ChunkShare {
-  int64_t y0, y1, W, x;  // W: the whole line; x: where sequence b starts in it
-  int b;
+  int64_t y0, y1, W;
+  int64_t x;         // where sequence b starts in the line
+  int64_t per_head;  // cost of a kv-head's tiles
+  int64_t slot;      // its first cache slot
+  ChunkSeq q;
+  int b, off;        // off: its first token row
 };
 
-__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkAttendArgs &a, int b, int &off) {
-  off = a.off[b];
-  return ChunkSeq{a.len[b], a.off[b + 1] - off};
-}
-
-__device__ __forceinline__ int64_t seq_cost(const ChunkAttendArgs &a, const ChunkSeq &q) {
-  return a.H_kv * tiles_cost(q, a.shape, q.tiles(a.shape.tok));
-}
-
-// The share of CTA `cta` of G, which may be empty; false (for every thread) when it starts at the
-// end of the line, the device status is set or a length is out of its bounds (recorded).  Every
-// thread of the CTA calls it; the lengths are read once for a batch of at most NT.
-template <int NT>
-__device__ bool chunk_share(const ChunkAttendArgs &a, int cta, int G, ChunkShare &sh) {
-  __shared__ int64_t s_warp[NT / 32];
-  __shared__ ChunkShare s_share;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  bool bad = false, stop = tid == 0 && status_bad(a.status);
-  int64_t mine = 0, first = 0;  // this thread's sequences; the one of the first round
-  for (int b = tid; b < a.batch; b += NT) {
-    int off;
-    const ChunkSeq q = chunk_seq(a, b, off);
+// The share of CTA `cta` of G, which may be empty; false when it starts at the end of the line, the
+// device status is set or a length is out of its bounds (recorded).  Every lane of a warp calls it;
+// a batch of at most 32 is read once, in one round trip.
+__device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, int G,
+                                            ChunkShare &sh) {
+  const int lane = threadIdx.x & 31;
+  bool bad = false;
+  int off = 0;
+  int64_t slot = 0, c = 0;
+  ChunkSeq q{0, 0};
+  auto load = [&](int b) {  // a lane's sequence and the cost of one kv-head of it
+    c = 0;
+    if (b >= a.batch) return;
+    off = a.off[b];
+    const int end = a.off[b + 1];
+    q = ChunkSeq{a.len[b], end - off};
+    slot = a.seq_off[b];
     if (q.n < 0 || q.n > a.max_len || q.m < 0 || q.m > a.max_new || q.m > q.n || off < 0 ||
-        (int64_t)off + q.m > a.T) {
+        end > a.T)
       bad = true;
-      continue;
-    }
-    const int64_t cost = seq_cost(a, q);
-    if (b == tid) first = cost;
-    mine += cost;
-  }
-  if (bad) set_status(a.status, LG_ERR_CAPACITY);
-  if (__syncthreads_or(bad || stop)) return false;
-
-  auto scan = [&](int64_t v, int64_t &total) {  // inclusive prefix over the CTA's threads
+    else
+      c = tiles_cost(q, a.shape, q.tiles(a.shape.tok));
+  };
+  auto scan = [&](int64_t v) {  // inclusive prefix over the lanes
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
       if (lane >= o) v += u;
     }
-    __syncthreads();
-    if (lane == 31) s_warp[warp] = v;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-    for (int w = 0; w < NT / 32; ++w) {
-      if (w < warp) before += s_warp[w];
-      total += s_warp[w];
-    }
-    return v + before;
+    return v;
   };
-  int64_t W, incl = scan(mine, W);
-  const int64_t y0 = range_bound(W, cta, G), y1 = range_bound(W, cta + 1, G);
-  if (y0 >= W) return false;
-  int64_t base = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += NT) {
-    int64_t cost = first, total = W;
-    if (a.batch > NT) {  // rounds of NT sequences in order
-      int off;
-      cost = 0;
-      if (b0 + tid < a.batch) cost = seq_cost(a, chunk_seq(a, b0 + tid, off));
-      incl = scan(cost, total);
+  const bool stop = lane == 0 && status_bad(a.status);
+  load(lane);
+  int64_t incl = scan(a.H_kv * c);
+  sh.W = __shfl_sync(0xffffffffu, incl, 31);
+  if (a.batch > 32) {
+    int64_t mine = 0;
+    for (int b = 32 + lane; b < a.batch; b += 32) {
+      load(b);
+      mine += a.H_kv * c;
     }
-    const int64_t x = base + incl - cost;
-    if (y0 >= x && y0 < x + cost) s_share = ChunkShare{y0, y1, W, x, b0 + tid};
-    base += total;
-    if (y0 < base) break;
+    sh.W += __shfl_sync(0xffffffffu, scan(mine), 31);
+    load(lane);
   }
-  __syncthreads();
-  sh = s_share;
-  return true;
+  if (bad) set_status(a.status, LG_ERR_CAPACITY);
+  if (__any_sync(0xffffffffu, bad || stop)) return false;
+  sh.y0 = range_bound(sh.W, cta, G);
+  sh.y1 = range_bound(sh.W, cta + 1, G);
+  if (sh.y0 >= sh.W) return false;
+  int64_t base = 0;
+  for (int b0 = 0;; b0 += 32) {
+    if (b0 > 0) {
+      load(b0 + lane);
+      incl = scan(a.H_kv * c);
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, base + incl > sh.y0);
+    if (past) {
+      const int f = __ffs((int)past) - 1;
+      sh.x = base + __shfl_sync(0xffffffffu, incl - a.H_kv * c, f);
+      sh.per_head = __shfl_sync(0xffffffffu, c, f);
+      sh.slot = __shfl_sync(0xffffffffu, slot, f);
+      sh.q.n = __shfl_sync(0xffffffffu, q.n, f);
+      sh.q.m = __shfl_sync(0xffffffffu, q.m, f);
+      sh.off = __shfl_sync(0xffffffffu, off, f);
+      sh.b = b0 + f;
+      return true;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
 }
 
-// The walk along a CTA's share, piece by piece; every role of a CTA walks by itself.
+// The walk along a CTA's share, piece by piece.
 struct ChunkWalk {
   int b, kvh, t, tiles;
   ChunkSeq q;
   int off;           // first token row of the sequence
+  int64_t slot0;     // first cache slot of the sequence
   int64_t row0;      // first cache row of the (layer, kv-head, sequence)
   int64_t x, cost;   // the item's start in the line, and its cost
-  int64_t per_head;  // cost of a kv-head's tiles
   int64_t y0, y1;
   TileRows rows;
   TileBlocks blocks;
   int blk0, blk1;    // the piece's key blocks
 
-  __device__ __forceinline__ void load_seq(const ChunkAttendArgs &a) {
-    q = chunk_seq(a, b, off);
-    tiles = q.tiles(a.shape.tok);
-  }
   __device__ __forceinline__ void load_item(const ChunkAttendArgs &a) {
-    row0 = ((int64_t)a.layer * a.H_kv + kvh) * a.S_total + a.seq_off[b];
+    row0 = ((int64_t)a.layer * a.H_kv + kvh) * a.S_total + slot0;
     rows = tile_rows(q, a.shape, t);
     cost = tile_cost(q, a.shape, t);
     blocks = tile_blocks(rows, a.shape.bn2);
     blk0 = cut_block(y0 - x, cost, blocks.count, a.shape.bn2);
     blk1 = cut_block(y1 - x, cost, blocks.count, a.shape.bn2);
   }
-  // the item that cost unit y falls into, y in sequence sh.b
-  __device__ __forceinline__ void start(const ChunkAttendArgs &a, const ChunkShare &sh, int64_t y) {
+  // the item that the share's start falls into
+  __device__ __forceinline__ void start(const ChunkAttendArgs &a, const ChunkShare &sh) {
     b = sh.b;
     y0 = sh.y0;
     y1 = sh.y1;
-    load_seq(a);
-    per_head = tiles_cost(q, a.shape, tiles);
-    kvh = (int)plan_div(y - sh.x, per_head);
-    const int64_t in = y - sh.x - kvh * per_head;
-    t = tile_at(q, a.shape, in);
-    x = sh.x + kvh * per_head + tiles_cost(q, a.shape, t);
+    q = sh.q;
+    off = sh.off;
+    slot0 = sh.slot;
+    tiles = q.tiles(a.shape.tok);
+    kvh = (int)plan_div(y0 - sh.x, sh.per_head);
+    x = sh.x + kvh * sh.per_head;
+    t = tiles > 1 ? tile_at(q, a.shape, y0 - x) : 0;
+    if (t) x += tiles_cost(q, a.shape, t);
     load_item(a);
   }
   __device__ __forceinline__ bool done() const { return x >= y1; }
@@ -155,7 +155,10 @@ struct ChunkWalk {
         kvh = 0;
         do {
           ++b;
-          load_seq(a);
+          off = a.off[b];
+          q = ChunkSeq{a.len[b], a.off[b + 1] - off};
+          slot0 = a.seq_off[b];
+          tiles = q.tiles(a.shape.tok);
         } while (tiles == 0);
       }
     }

@@ -1,24 +1,25 @@
 // lg_chunk_attend of bf16 caches for few query rows of a kv-head (a token, or some proposed tokens,
 // a sequence): the call reads the cache once and computes little, so the products are turned round,
 //   S^T = K Q^T  (M = 128 keys, N query rows),  O^T += V^T P^T  (M = head elements),
-// and no part of them is padding.  A thread holds one key's scores of all N rows (N = 16, 32 or 64:
-// row r is token r / g, head r % g); it exponentiates them, adds them to its own sums of the
-// normalisers and writes its row of P^T to shared memory, the products' second operand.  The maxima
-// are the CTA's: as in the kernel for many rows they may lag by a factor 2^8, so a block asks only
+// and no part of them is padding.  A thread holds one key's scores of 16 or 32 of the N rows (N = 16,
+// 32 or 64: row r is token r / g, head r % g; one group of four warps takes 16 rows, two take 32 or
+// 64); it exponentiates them, adds them to its own sums of the normalisers and writes them to its
+// key's row of P^T in shared memory, the products' second operand.  The maxima
+// are the group's: as in the kernel for many rows they may lag by a factor 2^8, so a block asks only
 // whether any score passed that bound (one barrier), and the exact maxima are formed in the first
 // block and when one did.
 //
 // Scores are two blocks ahead of the sums (two buffers of S^T and P^T), and the ring holds five
 // blocks of keys or values.
 //
-// Warps: 0-3 the keys (and the results: a thread a head element), 4 walks along the work and copies, 5 issues the products,
-// 6 and 7 clear what is not a number from values of blocks that hide a row from a query.
+// Warps: the keys' (and the results': a thread a head element), one that walks along the work and
+// copies, one that issues the products, two that clear what is not a number from values of blocks
+// that hide a row from a query.
 #include "lg_chunk_tc.cuh"
 
 namespace lg {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kBn = kTcBn;
 constexpr int kPBytes = kBn * 128;  // a buffer of P^T: 128-byte rows, swizzled
 constexpr float kLazy = 8.f;
@@ -31,6 +32,10 @@ struct FewCfg {
   static constexpr int kQBox = N * 128;
   static constexpr int kQBytes = (kBoxes * kQBox + 1023) / 1024 * 1024;
   static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kGroups = N > 16 ? 2 : 1;  // groups of four warps that share a block's keys
+  static constexpr int kCols = N / kGroups;       // query rows of a thread
+  static constexpr int kWarps = 4 * kGroups;      // ... and the other roles' first warp
+  static constexpr int kThreads = 32 * (kWarps + 4);
   static constexpr int kSmem = kQBytes + 2 * kPBytes + kStages * kTile + 1024;
 };
 
@@ -46,15 +51,17 @@ struct FewBars {
   float col[4][N];  // a warp's maxima or normalisers
 };
 
-// a barrier of the 128 key threads; with a condition: whether it held for any
-__device__ __forceinline__ void keys_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool keys_any(bool p) {
+// a barrier of a group's 128 key threads; with a condition: whether it held for any
+__device__ __forceinline__ void keys_sync(int group) {
+  asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory");
+}
+__device__ __forceinline__ bool keys_any(int group, bool p) {
   uint32_t r;
   asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n"
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n"
       " selp.u32 %0, 1, 0, q;\n}\n"
       : "=r"(r)
-      : "r"((uint32_t)p)
+      : "r"((uint32_t)p), "r"(group + 1)
       : "memory");
   return r != 0;
 }
@@ -87,13 +94,24 @@ __device__ __forceinline__ void store_cols(uint32_t addr, const uint32_t *v) {
   tmem_wait_store();
 }
 
+// bit q: query row q (token q / g of the tile) sees row i
+__device__ __forceinline__ uint64_t columns_seeing(const TileRows &r, const ChunkShape &s, int g,
+                                                   int i) {
+  auto below = [](int64_t n) {  // bits 0 .. n - 1
+    return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+  };
+  const uint64_t from = ~below(((int64_t)i - r.first) * g);  // tokens at row i or behind it
+  if (s.window == 0 || i < s.sink) return from;
+  return from & below(((int64_t)i + s.window - r.first) * g);
+}
+
 template <int D, int N>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
     chunk_attend_few_kernel(const __grid_constant__ CUtensorMap mq,
                             const __grid_constant__ CUtensorMap mk,
                             const __grid_constant__ CUtensorMap mv, ChunkAttendArgs a) {
   using C = FewCfg<D, N>;
-  constexpr int ST = C::kStages;
+  constexpr int ST = C::kStages, NC = C::kCols, W0 = C::kWarps;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) FewBars<ST, N> bars;
   uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -110,25 +128,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars.q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.s_full[i], 1);
-      mbar_init(&bars.p_full[i], 4);
+      mbar_init(&bars.p_full[i], W0);
       mbar_init(&bars.o_full[i], 1);
     }
-    mbar_init(&bars.o_free, 4);
-    bars.queue.init(7);  // the products, two clearing warps, four warps of keys
+    mbar_init(&bars.o_free, W0);
+    bars.queue.init(3 + W0);  // the products, two clearing warps, the keys' warps
     bars.give_up = 0;
     mbar_fence_init();
   }
-  if (warp == 5) tmem_alloc(&bars.tmem, kTmemCols);
-  pdl_enter();
-  ChunkShare sh;
+  if (warp == W0 + 1) tmem_alloc(&bars.tmem, kTmemCols);
   tc_fence_before();
-  bool work = chunk_share<kThreads>(a, blockIdx.x, gridDim.x, sh);
   __syncthreads();
   tc_fence_after();
-  work = work && sh.y0 < sh.y1;
+  pdl_enter();
   const uint32_t tmem = bars.tmem;  // S^T at columns 0 and N, O^T at 2 N
 
-  if (work && warp == 4) {
+  if (warp == W0) {
+    ChunkShare sh;
+    const bool work = chunk_share(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
     if (lane == 0) {
       ChunkWalk w;
       uint32_t n = 0, pieces = 0;
@@ -143,7 +160,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           tma_box_2d(ring + st * C::kTile + x * (kBn * 128), map, 64 * x, row, &bars.full[st]);
         ++n;
       };
-      for (w.start(a, sh, sh.y0); ok && !w.done(); w.next(a)) {
+      if (work) w.start(a, sh);
+      for (; work && ok && !w.done(); w.next(a)) {
         if (w.blk0 == w.blk1) continue;
         const int r0 = (int)w.row0;
         ok = bars.queue.put(bars, pieces, &w, a) && tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
@@ -163,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (ok) bars.queue.put(bars, pieces, nullptr, a);
     }
-  } else if (work && warp == 5) {
+  } else if (warp == W0 + 1) {
     if (lane == 0) {
       uint32_t n = 0, c = 0;
       bool ok = true;
@@ -226,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         n += 2 * blocks;
       }
     }
-  } else if (work && warp >= 6) {
+  } else if (warp >= W0 + 2) {
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
@@ -242,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         const int i0 = j < 0 ? 0 : p.blocks.index(p.blk0 + j) * kBn;
         if (j >= 0 && block_hides(p.rows, a.shape, i0)) {
-          if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 192, 64)) p.bad = 1;
+          if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64)) p.bad = 1;
           fence_proxy_async_smem();
           __syncwarp();
         }
@@ -254,20 +272,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) bars.queue.done(pc);
     }
-  } else if (work) {
-    const uint32_t lanes = (uint32_t)warp << 21;
-    const int H_q = a.H_kv * a.g;
+  } else {
+    const int grp = warp >> 2, q0 = grp * NC;  // this thread's query rows: q0 .. q0 + NC - 1
+    const int key = tid & 127;                 // of a block; of the results: the head element
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     uint32_t c = 0;
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
       ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
-      if (keys_any(!ok)) break;
+      if (keys_any(grp, !ok)) break;
       const TcPiece &w = bars.queue.at(pc);
       if (w.blk1 < 0) break;
       const int used = w.tokens * a.g;
-      float m[N], l[N];
+      float m[NC], l[NC];
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
+      for (int q = 0; q < NC; ++q) {
         m[q] = -INFINITY;
         l[q] = 0.f;
       }
@@ -275,61 +294,62 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t b = c & 1;
         ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[b], (c >> 1) & 1));
         // a role that gave up is seen by every key warp before the barriers below
-        if (keys_any(!ok)) {
+        if (keys_any(grp, !ok)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        uint32_t u[N];
-        load_cols<N>(tmem + b * N + lanes, u);
+        uint32_t u[NC];
+        load_cols<NC>(tmem + b * N + q0 + lanes, u);
         float *v = (float *)u;
         const int i0 = w.blocks.index(blk) * kBn;
 #pragma unroll
-        for (int q = 0; q < N; ++q) v[q] *= a.qscale;
+        for (int q = 0; q < NC; ++q) v[q] *= a.qscale;
         if (block_hides(w.rows, a.shape, i0)) {
+          const uint64_t see = columns_seeing(w.rows, a.shape, a.g, i0 + key) >> q0;
 #pragma unroll
-          for (int q = 0; q < N; ++q)
-            if (!row_sees(w.rows, a.shape, w.rows.first + q / a.g, i0 + tid)) v[q] = -INFINITY;
+          for (int q = 0; q < NC; ++q)
+            if (!(see >> q & 1)) v[q] = -INFINITY;
         }
         bool rise = blk == w.blk0;
 #pragma unroll
-        for (int q = 0; q < N; ++q) rise |= q < used && v[q] > m[q] + kLazy;
-        if (keys_any(rise)) {
+        for (int q = 0; q < NC; ++q) rise |= q0 + q < used && v[q] > m[q] + kLazy;
+        if (keys_any(grp, rise)) {
 #pragma unroll
-          for (int q = 0; q < N; ++q) {
+          for (int q = 0; q < NC; ++q) {
             const float x = warp_max(v[q]);
-            if (lane == 0) bars.col[warp][q] = x;
+            if (lane == 0) bars.col[warp & 3][q0 + q] = x;
           }
-          keys_sync();
-          float f[N];
+          keys_sync(grp);
+          float f[NC];
 #pragma unroll
-          for (int q = 0; q < N; ++q) {
-            const float x = fmaxf(fmaxf(bars.col[0][q], bars.col[1][q]),
-                                  fmaxf(bars.col[2][q], bars.col[3][q]));
+          for (int q = 0; q < NC; ++q) {
+            const float x = fmaxf(fmaxf(bars.col[0][q0 + q], bars.col[1][q0 + q]),
+                                  fmaxf(bars.col[2][q0 + q], bars.col[3][q0 + q]));
             const float m1 = fmaxf(m[q], x);
             f[q] = m1 == -INFINITY ? 0.f : exp2_fast(m[q] - m1);
             m[q] = m1;
             l[q] *= f[q];
           }
-          keys_sync();  // the maxima have been read
+          keys_sync(grp);  // the maxima have been read
           if (blk > w.blk0) {
             ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
-            if (keys_any(!ok)) {
+            if (keys_any(grp, !ok)) {
               ok = false;
               break;
             }
             tc_fence_after();
-            uint32_t o[N];
-            load_cols<N>(tmem + 2 * N + lanes, o);
+            uint32_t o[NC];
+            load_cols<NC>(tmem + 2 * N + q0 + lanes, o);
 #pragma unroll
-            for (int q = 0; q < N; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f[q]);
-            store_cols<N>(tmem + 2 * N + lanes, o);
+            for (int q = 0; q < NC; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f[q]);
+            store_cols<NC>(tmem + 2 * N + q0 + lanes, o);
             tc_fence_before();
           }
         }
-        uint8_t *row = sp + b * kPBytes + tid * 128;
+        uint8_t *row = sp + b * kPBytes + key * 128;
 #pragma unroll
-        for (int q = 0; q < N; q += 8) {
+        for (int q = 0; q < NC; q += 8) {
           uint32_t h[4];
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
@@ -343,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const __nv_bfloat162 z = __floats2bfloat162_rn(p[0], p[1]);
             h[e / 2] = *(const uint32_t *)&z;
           }
-          *(uint4 *)(row + (((q / 8) ^ (tid & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *(uint4 *)(row + ((((q0 + q) / 8) ^ (key & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         fence_proxy_async_smem();
         tc_fence_before();
@@ -352,17 +372,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       // normalisers: a warp's sums, then the CTA's
-#pragma unroll
-      for (int q0 = 0; q0 < N; q0 += 32) {
-        constexpr int M = N < 32 ? N : 32;
-        HeadReduce<M, 16>::run(l + q0, lane);  // lane: column q0 + lane / (32 / M)
-        if (lane % (32 / M) == 0) bars.col[warp][q0 + lane / (32 / M)] = l[q0];
-      }
+      HeadReduce<NC, 16>::run(l, lane);  // lane: column lane / (32 / NC)
+      if (lane % (32 / NC) == 0) bars.col[warp & 3][q0 + lane / (32 / NC)] = l[0];
       ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
-      if (keys_any(!ok)) break;
+      if (keys_any(grp, !ok)) break;
+      if (key < NC) {
+        const int q = q0 + key;
+        const float sum = (bars.col[0][q] + bars.col[1][q]) + (bars.col[2][q] + bars.col[3][q]);
+        bars.col[0][q] = w.slot >= 0 ? sum : sum != 0.f ? 1.f / sum : 0.f;
+      }
+      keys_sync(grp);
       tc_fence_after();
-      uint32_t o[N];
-      load_cols<N>(tmem + 2 * N + lanes, o);
+      uint32_t o[NC];
+      load_cols<NC>(tmem + 2 * N + q0 + lanes, o);
       const bool whole = w.slot < 0;
       const int tok0 = w.tok0;
       if (w.bad) {  // what was cleared, for the queries that see it
@@ -371,31 +393,42 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!block_hides(w.rows, a.shape, i0)) continue;
           for (int i = i0; i < i0 + kBn && i < w.n; ++i) {
             const float z = __bfloat162float(
-                ((const __nv_bfloat16 *)a.V)[(w.row0 + i) * D + tid % D]);
+                ((const __nv_bfloat16 *)a.V)[(w.row0 + i) * D + key % D]);
             if (isfinite(z)) continue;
+            const uint64_t see = columns_seeing(w.rows, a.shape, a.g, i) >> q0;
 #pragma unroll
-            for (int q = 0; q < N; ++q)
-              if (row_sees(w.rows, a.shape, w.rows.first + q / a.g, i))
-                o[q] = __float_as_uint(__uint_as_float(o[q]) + z);
+            for (int q = 0; q < NC; ++q)
+              if (see >> q & 1) o[q] = __float_as_uint(__uint_as_float(o[q]) + z);
           }
         }
       }
-      if (tid < D) {
+      if (key < D) {
+        // row q of the tile is head q % g of token q / g
+        int h = q0 % a.g;
+        __nv_bfloat16 *out = (__nv_bfloat16 *)a.out + key +
+                             ((int64_t)(tok0 + q0 / a.g) * (a.H_kv * a.g) + w.kvh * a.g + h) * D;
+        float *part = whole ? nullptr : part_row(a, D, blockIdx.x, w.slot, q0) + key;
+        const int64_t skip = (int64_t)(a.H_kv - 1) * a.g * D;
 #pragma unroll
-        for (int q = 0; q < N; ++q) {
-          if (q >= used) continue;
-          const float sum = (bars.col[0][q] + bars.col[1][q]) + (bars.col[2][q] + bars.col[3][q]);
+        for (int q = 0; q < NC; ++q) {
+          if (q0 + q >= used) break;
           const float x = __uint_as_float(o[q]);
           if (whole) {
-            ((__nv_bfloat16 *)a.out)[((int64_t)(tok0 + q / a.g) * H_q + w.kvh * a.g + q % a.g) * D +
-                                     tid] = __float2bfloat16_rn(sum != 0.f ? x / sum : 0.f);
+            *out = __float2bfloat16_rn(x * bars.col[0][q0 + q]);
+            out += D;
+            if (++h == a.g) h = 0, out += skip;
           } else {
-            part_row(a, D, blockIdx.x, w.slot, q)[tid] = x;
-            if (tid == 0) *part_ml(a, D, gridDim.x, blockIdx.x, w.slot, q) = make_float2(m[q], sum);
+            part[q * D] = x;
           }
         }
       }
-      keys_sync();  // the normalisers have been read
+      if (!whole && key == 0)
+#pragma unroll
+        for (int q = 0; q < NC; ++q)
+          if (q0 + q < used)
+            *part_ml(a, D, gridDim.x, blockIdx.x, w.slot, q0 + q) =
+                make_float2(m[q], bars.col[0][q0 + q]);
+      keys_sync(grp);  // the normalisers have been read
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -412,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     linger();
     __syncthreads();
   }
-  if (warp == 5) {
+  if (warp == W0 + 1) {
     tc_fence_after();
     tmem_free(tmem, kTmemCols);
   }
@@ -428,7 +461,7 @@ cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
   auto kern = chunk_attend_few_kernel<D, N>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               FewCfg<D, N>::kSmem));
-  LG_TRY(launch_pdl(kern, G, kThreads, FewCfg<D, N>::kSmem, s, mq, mk, mv, a));
+  LG_TRY(launch_pdl(kern, G, FewCfg<D, N>::kThreads, FewCfg<D, N>::kSmem, s, mq, mk, mv, a));
   return cudaGetLastError();
 }
 

@@ -80,21 +80,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_fence_init();
   }
   if (warp == 9) tmem_alloc(&bars.tmem, kTmemCols);
-  pdl_enter();
-  ChunkShare sh;
-  // (its barriers also publish the mbarriers and the tensor memory's address)
   tc_fence_before();
-  bool work = chunk_share<kThreads>(a, blockIdx.x, gridDim.x, sh);
   __syncthreads();
   tc_fence_after();
-  work = work && sh.y0 < sh.y1;
+  pdl_enter();
   const uint32_t tmem = bars.tmem;
 
   // registers: 168 a thread at launch, 64512 in all; the rows' warps take 208, the others 88
   // (256 x 208 + 128 x 88 = 64512)
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    if (work && warp == 8) {
+    if (warp == 8) {
+      ChunkShare sh;
+      const bool work = chunk_share(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
       if (lane == 0) {
         ChunkWalk w;
         uint32_t n = 0, pieces = 0;  // ring position, pieces so far
@@ -109,7 +107,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_box_2d(ring + st * C::kTile + x * (kBn * 128), map, 64 * x, row, &bars.full[st]);
           ++n;
         };
-        for (w.start(a, sh, sh.y0); ok && !w.done(); w.next(a)) {
+        if (work) w.start(a, sh);
+        for (; work && ok && !w.done(); w.next(a)) {
           if (w.blk0 == w.blk1) continue;
           const int tiles = w.tokens(a) > tpt ? 2 : 1;
           ok = bars.queue.put(bars, pieces, &w, a) &&
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok) bars.queue.put(bars, pieces, nullptr, a);
       }
-    } else if (work && warp == 9) {
+    } else if (warp == 9) {
       if (lane == 0) {
         uint32_t n = 0, c[2] = {0, 0}, used[2] = {0, 0};
         bool ok = true;
@@ -213,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           n += 2 * blocks;
         }
       }
-    } else if (work) {
+    } else {
       uint32_t n = 0;
       bool ok = true;
       for (uint32_t pc = 0; ok; ++pc) {
@@ -249,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t to = tmem + kColO + s * D + lanes, ts = tmem + s * 128 + lanes;
     const int j_tok = s * tpt + r / a.g;      // token of the row in the item
     uint32_t c = 0, mine = 0;                 // blocks and pieces of this stream so far
-    bool ok = work;
+    bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
       ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
       if (!ok) break;
