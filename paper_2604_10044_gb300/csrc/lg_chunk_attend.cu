@@ -23,20 +23,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-template <typename T>
-__device__ __forceinline__ void load4(const void *p, int64_t i, float *f);
-template <>
-__device__ __forceinline__ void load4<float>(const void *p, int64_t i, float *f) {
+__device__ __forceinline__ void load4(const void *p, int64_t i, float *f) {
   const float4 v = *(const float4 *)((const float *)p + i);
   f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
 }
-
-template <typename T>
-__device__ __forceinline__ void store4(void *p, int64_t i, const float *f);
-template <>
-__device__ __forceinline__ void store4<float>(void *p, int64_t i, const float *f) {
+__device__ __forceinline__ void store4(void *p, int64_t i, const float *f) {
   *(float4 *)((float *)p + i) = make_float4(f[0], f[1], f[2], f[3]);
 }
+
 template <int D, int BM>
 struct SimtCfg {
   static constexpr int kRow = D + 4;  // floats of a staged row: 16 rows of 16 bytes, no conflicts
@@ -44,7 +38,7 @@ struct SimtCfg {
       (BM * kRow + kBn * kRow + kBn * D + BM * (kBn + 4)) * (int)sizeof(float);
 };
 
-template <typename T, int D, int BM>
+template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs a) {
   constexpr int TM = BM / 16, NC = D / 64, kRow = SimtCfg<D, BM>::kRow, kPRow = kBn + 4;
   extern __shared__ __align__(16) float smem[];
@@ -53,8 +47,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
   const int H_q = a.H_kv * a.g;
   pdl_enter();
   ChunkShare sh;
-  if (!chunk_share(a, blockIdx.x, gridDim.x, sh)) return;
-  ChunkWalk w;
+  if (!chunk_share<BM == 16>(a, blockIdx.x, gridDim.x, sh)) return;
+  ChunkWalk<BM == 16> w;
   for (w.start(a, sh); !w.done(); w.next(a)) {
     if (w.blk0 == w.blk1) continue;
     const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
@@ -64,7 +58,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
       const int r = e / (D / 4), c = e % (D / 4) * 4;
       float f[4] = {0.f, 0.f, 0.f, 0.f};
       if (r < used)
-        load4<T>(a.q, ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D + c, f);
+        load4(a.q, ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D + c, f);
       *(float4 *)(sq + r * kRow + c) = make_float4(f[0], f[1], f[2], f[3]);
     }
     float o[TM][4 * NC], m[TM], l[TM];
@@ -84,8 +78,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
         const int r = e / (D / 4), c = e % (D / 4) * 4;
         float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
         if (i0 + r < w.q.n) {
-          load4<T>(a.K, (w.row0 + i0 + r) * D + c, k);
-          load4<T>(a.V, (w.row0 + i0 + r) * D + c, v);
+          load4(a.K, (w.row0 + i0 + r) * D + c, k);
+          load4(a.V, (w.row0 + i0 + r) * D + c, v);
         }
         *(float4 *)(sk + r * kRow + c) = make_float4(k[0], k[1], k[2], k[3]);
         *(float4 *)(sv + r * D + c) = make_float4(v[0], v[1], v[2], v[3]);
@@ -180,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
           float f[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = o[i][4 * k + e] * inv;
-          store4<T>(a.out, dst + 4 * tx + 64 * k, f);
+          store4(a.out, dst + 4 * tx + 64 * k, f);
         }
       } else {
         float *dst = part_row(a, D, blockIdx.x, w.slot(), r);
@@ -196,22 +190,30 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
 
 // Merge of the item that the start of CTA c's range cuts, c = blockIdx.x + 1, by the first cut of
 // an item: pieces of CTAs c - 1, c, ... in order, a warp per row, blockIdx.y of gridDim.y in turn.
-template <typename T, int D>
+//
+// Which pieces there are follows from the lengths, and is found before the dependency wait: this
+// kernel can start once every CTA of the attention kernel is past its own wait, so everything that
+// wrote the lengths is complete by then, and the attention kernel leaves them alone.
+template <typename T, int D, bool ONE>
 __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
   constexpr int V = D / 32;  // elements a lane
-  pdl_enter();
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ChunkShare sh;
-  if (!chunk_share(a, c, G, sh)) return;
-  ChunkWalk w;
-  w.start(a, sh);
-  if (w.x == sh.y0) return;  // the bound falls between items
-  if (range_bound(sh.W, c - 1, G) > w.x) return;  // an earlier bound cuts the item too
-  int last = c;
-  while (last + 1 < G && range_bound(sh.W, last + 1, G) < w.x + w.cost) ++last;
+  ChunkWalk<ONE> w;
+  const bool work = chunk_share<ONE>(a, c, G, sh);
+  bool mine = false;
+  if (work) {
+    w.start(a, sh);
+    // the bound falls inside the item, and no earlier one does
+    mine = w.x < sh.y0 && sh.y0 - sh.step <= w.x;
+  }
+  pdl_enter();
+  if (!mine || __any_sync(0xffffffffu, lane == 0 && status_bad(a.status))) return;
+  int last = c;  // the last CTA that has a part of the item
+  for (int64_t y = sh.y0 + sh.step; y < w.x + w.cost; y += sh.step) ++last;
   const int used = w.tokens(a) * a.g, tok0 = w.off + w.t * a.shape.tok, H_q = a.H_kv * a.g;
   auto cut = [&](int p) {
-    return cut_block(range_bound(sh.W, p, G) - w.x, w.cost, w.blocks.count, a.shape.bn2);
+    return cut_block(p * sh.step - w.x, w.cost, w.blocks.count, a.shape.bn2);
   };
   // 32 pieces at a time, a lane each: whether it has blocks, its maximum and normaliser
   for (int r = blockIdx.y * (kThreads / 32) + warp; r < used; r += gridDim.y * (kThreads / 32)) {
@@ -258,9 +260,9 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
   }
 }
 
-template <typename T, int D, int BM>
+template <int D, int BM>
 cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
-  auto kern = chunk_attend_kernel<T, D, BM>;
+  auto kern = chunk_attend_kernel<D, BM>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               SimtCfg<D, BM>::kSmem));
   LG_TRY(launch_pdl(kern, G, kThreads, SimtCfg<D, BM>::kSmem, s, a));
@@ -269,13 +271,18 @@ cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
 
 template <typename T, int D>
 cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
-  LG_TRY(launch_pdl(chunk_merge_kernel<T, D>, dim3(G - 1, 4), kThreads, 0, s, a, G));
+  const int rows = kThreads / 32;  // a CTA's at once
+  const dim3 grid(G - 1, a.rows <= 4 * rows ? (a.rows + rows - 1) / rows : 4);
+  if (a.max_new <= a.shape.tok)
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, true>, grid, kThreads, 0, s, a, G));
+  else
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, false>, grid, kThreads, 0, s, a, G));
   return cudaGetLastError();
 }
 
 template <int D>
 cudaError_t launch_d(ChunkAttendArgs &a, int G, cudaStream_t s) {
-  return a.rows == 16 ? launch_typed<float, D, 16>(a, G, s) : launch_typed<float, D, 128>(a, G, s);
+  return a.rows == 16 ? launch_typed<D, 16>(a, G, s) : launch_typed<D, 128>(a, G, s);
 }
 
 }  // namespace

@@ -30,7 +30,7 @@ struct ChunkAttendArgs {
 
 // a CTA's share: cost units [y0, y1) of the line of W, and the sequence that y0 falls into
 struct ChunkShare {
-  int64_t y0, y1, W;
+  int64_t y0, y1, W, step;
   int64_t x;         // where sequence b starts in the line
   int64_t per_head;  // cost of a kv-head's tiles
   int64_t slot;      // its first cache slot
@@ -40,7 +40,9 @@ struct ChunkShare {
 
 // The share of CTA `cta` of G, which may be empty; false when it starts at the end of the line, the
 // device status is set or a length is out of its bounds (recorded).  Every lane of a warp calls it;
-// a batch of at most 32 is read once, in one round trip.
+// a batch of at most 32 is read once, in one round trip.  ONE: no sequence has more than one tile.
+// The merge calls it before its dependency wait (chunk_merge_kernel), hence the loads past L1.
+template <bool ONE>
 __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, int G,
                                             ChunkShare &sh) {
   const int lane = threadIdx.x & 31;
@@ -51,13 +53,15 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
   auto load = [&](int b) {  // a lane's sequence and the cost of one kv-head of it
     c = 0;
     if (b >= a.batch) return;
-    off = a.off[b];
-    const int end = a.off[b + 1];
-    q = ChunkSeq{a.len[b], end - off};
-    slot = a.seq_off[b];
+    off = __ldcg(a.off + b);
+    const int end = __ldcg(a.off + b + 1);
+    q = ChunkSeq{__ldcg(a.len + b), end - off};
+    slot = __ldcg(a.seq_off + b);
     if (q.n < 0 || q.n > a.max_len || q.m < 0 || q.m > a.max_new || q.m > q.n || off < 0 ||
         end > a.T)
       bad = true;
+    else if (ONE)
+      c = q.m ? tile_cost(q, a.shape, 0) : 0;
     else
       c = tiles_cost(q, a.shape, q.tiles(a.shape.tok));
   };
@@ -84,8 +88,9 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
   }
   if (bad) set_status(a.status, LG_ERR_CAPACITY);
   if (__any_sync(0xffffffffu, bad || stop)) return false;
-  sh.y0 = range_bound(sh.W, cta, G);
-  sh.y1 = range_bound(sh.W, cta + 1, G);
+  sh.step = range_step(sh.W, G);
+  sh.y0 = plan_min(sh.W, cta * sh.step);
+  sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
   if (sh.y0 >= sh.W) return false;
   int64_t base = 0;
   for (int b0 = 0;; b0 += 32) {
@@ -110,6 +115,7 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
 }
 
 // The walk along a CTA's share, piece by piece.
+template <bool ONE>
 struct ChunkWalk {
   int b, kvh, t, tiles;
   ChunkSeq q;
@@ -138,18 +144,18 @@ struct ChunkWalk {
     q = sh.q;
     off = sh.off;
     slot0 = sh.slot;
-    tiles = q.tiles(a.shape.tok);
+    tiles = ONE ? 1 : q.tiles(a.shape.tok);
     kvh = (int)plan_div(y0 - sh.x, sh.per_head);
     x = sh.x + kvh * sh.per_head;
-    t = tiles > 1 ? tile_at(q, a.shape, y0 - x) : 0;
-    if (t) x += tiles_cost(q, a.shape, t);
+    t = !ONE && tiles > 1 ? tile_at(q, a.shape, y0 - x) : 0;
+    if (!ONE && t) x += tiles_cost(q, a.shape, t);
     load_item(a);
   }
   __device__ __forceinline__ bool done() const { return x >= y1; }
   __device__ __forceinline__ void next(const ChunkAttendArgs &a) {
     x += cost;
     if (x >= y1) return;
-    if (++t == tiles) {
+    if (ONE || ++t == tiles) {
       t = 0;
       if (++kvh == a.H_kv) {
         kvh = 0;
@@ -158,7 +164,7 @@ struct ChunkWalk {
           off = a.off[b];
           q = ChunkSeq{a.len[b], a.off[b + 1] - off};
           slot0 = a.seq_off[b];
-          tiles = q.tiles(a.shape.tok);
+          tiles = ONE ? q.m > 0 : q.tiles(a.shape.tok);
         } while (tiles == 0);
       }
     }

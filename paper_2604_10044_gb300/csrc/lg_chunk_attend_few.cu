@@ -15,6 +15,8 @@
 // Warps: the keys' (and the results': a thread a head element), one that walks along the work and
 // copies, one that issues the products, two that clear what is not a number from values of blocks
 // that hide a row from a query.
+#include <stddef.h>
+
 #include "lg_chunk_tc.cuh"
 
 namespace lg {
@@ -48,7 +50,10 @@ struct FewBars {
   TcQueue queue;
   uint32_t tmem;
   volatile int give_up;
-  float col[4][N];  // a warp's maxima or normalisers
+  __align__(16) float col[4][N];  // a warp's maxima or normalisers
+  // the maxima in use; what the sums so far are multiplied by (both read as 16-byte vectors)
+  __align__(16) float m[N];
+  __align__(16) float f[N];
 };
 
 // a barrier of a group's 128 key threads; with a condition: whether it held for any
@@ -111,6 +116,9 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
                             const __grid_constant__ CUtensorMap mk,
                             const __grid_constant__ CUtensorMap mv, ChunkAttendArgs a) {
   using C = FewCfg<D, N>;
+  using B = FewBars<C::kStages, N>;
+  static_assert(offsetof(B, m) % 16 == 0 && offsetof(B, f) % 16 == 0 && alignof(B) % 16 == 0,
+                "read as 16-byte vectors");
   constexpr int ST = C::kStages, NC = C::kCols, W0 = C::kWarps;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) FewBars<ST, N> bars;
@@ -145,9 +153,9 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
 
   if (warp == W0) {
     ChunkShare sh;
-    const bool work = chunk_share(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
+    const bool work = chunk_share<true>(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
     if (lane == 0) {
-      ChunkWalk w;
+      ChunkWalk<true> w;
       uint32_t n = 0, pieces = 0;
       bool ok = true;
       auto load = [&](const CUtensorMap *map, int row) {
@@ -164,22 +172,23 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (; work && ok && !w.done(); w.next(a)) {
         if (w.blk0 == w.blk1) continue;
         const int r0 = (int)w.row0;
-        ok = bars.queue.put(bars, pieces, &w, a) && tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
+        ok = tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
         if (!ok) break;
         mbar_arrive_expect_tx(&bars.q_full, C::kBoxes * a.shape.tok * a.g * 128);
 #pragma unroll
         for (int x = 0; x < C::kBoxes; ++x)
           tma_box_3d(sq + x * C::kQBox, &mq, 64 * x, w.kvh * a.g, w.off + w.t * a.shape.tok,
                      &bars.q_full);
-        ++pieces;
         // keys a block ahead of the values, as the products take them
         load(&mk, r0 + w.blocks.index(w.blk0) * kBn);
+        ok = ok && bars.queue.put(bars, pieces, w, a);
+        ++pieces;
         for (int j = w.blk0; ok && j < w.blk1; ++j) {
           if (j + 1 < w.blk1) load(&mk, r0 + w.blocks.index(j + 1) * kBn);
           load(&mv, r0 + w.blocks.index(j) * kBn);
         }
       }
-      if (ok) bars.queue.put(bars, pieces, nullptr, a);
+      if (ok) bars.queue.end(bars, pieces);
     }
   } else if (warp == W0 + 1) {
     if (lane == 0) {
@@ -284,14 +293,20 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       const TcPiece &w = bars.queue.at(pc);
       if (w.blk1 < 0) break;
       const int used = w.tokens * a.g;
-      float m[NC], l[NC];
+      // base: the maxima in use (0 while a query has seen nothing), l: normalisers in pairs
+      float base[NC];
+      float2 l2[NC / 2];
 #pragma unroll
-      for (int q = 0; q < NC; ++q) {
-        m[q] = -INFINITY;
-        l[q] = 0.f;
-      }
+      for (int q = 0; q < NC; ++q) base[q] = 0.f;
+#pragma unroll
+      for (int q = 0; q < NC / 2; ++q) l2[q] = make_float2(0.f, 0.f);
+      if (key < NC) bars.m[q0 + key] = -INFINITY;
+      const float2 sc = make_float2(a.qscale, a.qscale);
       for (int blk = w.blk0; blk < w.blk1; ++blk, ++c) {
         const uint32_t b = c & 1;
+        const int i0 = w.blocks.index(blk) * kBn;
+        const bool hides = block_hides(w.rows, a.shape, i0);
+        const uint64_t see = hides ? columns_seeing(w.rows, a.shape, a.g, i0 + key) >> q0 : ~0ull;
         ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[b], (c >> 1) & 1));
         // a role that gave up is seen by every key warp before the barriers below
         if (keys_any(grp, !ok)) {
@@ -302,38 +317,56 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         uint32_t u[NC];
         load_cols<NC>(tmem + b * N + q0 + lanes, u);
         float *v = (float *)u;
-        const int i0 = w.blocks.index(blk) * kBn;
-#pragma unroll
-        for (int q = 0; q < NC; ++q) v[q] *= a.qscale;
-        if (block_hides(w.rows, a.shape, i0)) {
-          const uint64_t see = columns_seeing(w.rows, a.shape, a.g, i0 + key) >> q0;
+        if (hides) {
 #pragma unroll
           for (int q = 0; q < NC; ++q)
             if (!(see >> q & 1)) v[q] = -INFINITY;
         }
-        bool rise = blk == w.blk0;
+        float2 z[NC / 2];  // scores over the maxima in use
+        float top = -INFINITY;
 #pragma unroll
-        for (int q = 0; q < NC; ++q) rise |= q0 + q < used && v[q] > m[q] + kLazy;
-        if (keys_any(grp, rise)) {
+        for (int q = 0; q < NC; q += 2) {
+          z[q / 2] = __ffma2_rn(make_float2(v[q], v[q + 1]), sc, make_float2(-base[q], -base[q + 1]));
+          top = max3(top, z[q / 2].x, z[q / 2].y);
+        }
+        // (rows of the tile that are no query may hold anything; they only ask too often)
+        if (keys_any(grp, top > kLazy || blk == w.blk0)) {
+          float mine = -INFINITY;  // lane q: the warp's maximum of row q
 #pragma unroll
           for (int q = 0; q < NC; ++q) {
             const float x = warp_max(v[q]);
-            if (lane == 0) bars.col[warp & 3][q0 + q] = x;
+            if (lane == q) mine = x;
+          }
+          if (lane < NC) bars.col[warp & 3][q0 + lane] = mine;
+          keys_sync(grp);
+          if (key < NC) {
+            const int q = q0 + key;
+            const float x = fmaxf(fmaxf(bars.col[0][q], bars.col[1][q]),
+                                  fmaxf(bars.col[2][q], bars.col[3][q])) * a.qscale;
+            const float m0 = bars.m[q], m1 = fmaxf(m0, x);
+            bars.m[q] = m1;
+            bars.f[q] = m1 == -INFINITY ? 0.f : exp2_fast(m0 - m1);
           }
           keys_sync(grp);
           float f[NC];
 #pragma unroll
-          for (int q = 0; q < NC; ++q) {
-            const float x = fmaxf(fmaxf(bars.col[0][q0 + q], bars.col[1][q0 + q]),
-                                  fmaxf(bars.col[2][q0 + q], bars.col[3][q0 + q]));
-            const float m1 = fmaxf(m[q], x);
-            f[q] = m1 == -INFINITY ? 0.f : exp2_fast(m[q] - m1);
-            m[q] = m1;
-            l[q] *= f[q];
+          for (int q = 0; q < NC; q += 4) {
+            const float4 m4 = *(const float4 *)&bars.m[q0 + q], f4 = *(const float4 *)&bars.f[q0 + q];
+            base[q] = m4.x, base[q + 1] = m4.y, base[q + 2] = m4.z, base[q + 3] = m4.w;
+            f[q] = f4.x, f[q + 1] = f4.y, f[q + 2] = f4.z, f[q + 3] = f4.w;
           }
-          keys_sync(grp);  // the maxima have been read
+#pragma unroll
+          for (int q = 0; q < NC; ++q)
+            if (base[q] == -INFINITY) base[q] = 0.f;
+#pragma unroll
+          for (int q = 0; q < NC; q += 2) {
+            z[q / 2] = __ffma2_rn(make_float2(v[q], v[q + 1]), sc, make_float2(-base[q], -base[q + 1]));
+            l2[q / 2].x *= f[q];
+            l2[q / 2].y *= f[q + 1];
+          }
           if (blk > w.blk0) {
-            ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
+            ok = __all_sync(0xffffffffu,
+                            tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
             if (keys_any(grp, !ok)) {
               ok = false;
               break;
@@ -352,16 +385,13 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         for (int q = 0; q < NC; q += 8) {
           uint32_t h[4];
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            float p[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const float mm = m[q + e + x];
-              p[x] = exp2_fast(v[q + e + x] - (mm == -INFINITY ? 0.f : mm));
-              l[q + e + x] += p[x];
-            }
-            const __nv_bfloat162 z = __floats2bfloat162_rn(p[0], p[1]);
-            h[e / 2] = *(const uint32_t *)&z;
+          for (int e = 0; e < 4; ++e) {
+            float2 p = z[q / 2 + e];
+            p.x = exp2_fast(p.x);
+            p.y = exp2_fast(p.y);
+            l2[q / 2 + e] = __fadd2_rn(l2[q / 2 + e], p);
+            const __nv_bfloat162 y = __floats2bfloat162_rn(p.x, p.y);
+            h[e] = *(const uint32_t *)&y;
           }
           *(uint4 *)(row + ((((q0 + q) / 8) ^ (key & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
@@ -372,6 +402,9 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       }
       if (!ok) break;
       // normalisers: a warp's sums, then the CTA's
+      float l[NC];
+#pragma unroll
+      for (int q = 0; q < NC / 2; ++q) l[2 * q] = l2[q].x, l[2 * q + 1] = l2[q].y;
       HeadReduce<NC, 16>::run(l, lane);  // lane: column lane / (32 / NC)
       if (lane % (32 / NC) == 0) bars.col[warp & 3][q0 + lane / (32 / NC)] = l[0];
       ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[(c - 1) & 1], ((c - 1) >> 1) & 1));
@@ -422,12 +455,9 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
           }
         }
       }
-      if (!whole && key == 0)
-#pragma unroll
-        for (int q = 0; q < NC; ++q)
-          if (q0 + q < used)
-            *part_ml(a, D, gridDim.x, blockIdx.x, w.slot, q0 + q) =
-                make_float2(m[q], bars.col[0][q0 + q]);
+      if (!whole && key < NC && q0 + key < used)
+        *part_ml(a, D, gridDim.x, blockIdx.x, w.slot, q0 + key) =
+            make_float2(bars.m[q0 + key], bars.col[0][q0 + key]);
       keys_sync(grp);  // the normalisers have been read
       tc_fence_before();
       __syncwarp();

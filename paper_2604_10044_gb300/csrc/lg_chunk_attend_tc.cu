@@ -92,9 +92,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8) {
       ChunkShare sh;
-      const bool work = chunk_share(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
+      const bool work = chunk_share<false>(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
       if (lane == 0) {
-        ChunkWalk w;
+        ChunkWalk<false> w;
         uint32_t n = 0, pieces = 0;  // ring position, pieces so far
         bool ok = true;
         auto load = [&](const CUtensorMap *map, int row) {
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (; work && ok && !w.done(); w.next(a)) {
           if (w.blk0 == w.blk1) continue;
           const int tiles = w.tokens(a) > tpt ? 2 : 1;
-          ok = bars.queue.put(bars, pieces, &w, a) &&
+          ok = bars.queue.put(bars, pieces, w, a) &&
                tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
           if (!ok) break;
           mbar_arrive_expect_tx(&bars.q_full, tiles * C::kBoxes * tpt * a.g * 128);
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             load(&mv, row);
           }
         }
-        if (ok) bars.queue.put(bars, pieces, nullptr, a);
+        if (ok) bars.queue.end(bars, pieces);
       }
     } else if (warp == 9) {
       if (lane == 0) {

@@ -4,8 +4,8 @@
 // An item is (sequence, kv-head, tile): the g query heads of `tok` consecutive new tokens.  Its
 // cost is the rows its queries can see plus kItemCost, a linear function of the tile (constant once
 // a window fills), so the cost of a sequence's first t tiles is a closed form.  The items stand in
-// one line, ordered by sequence, kv-head and tile, W cost units long; CTA c of G takes
-// [W c / G, W (c + 1) / G).  An item cut by such a bound is shared: its key blocks divide in
+// one line, ordered by sequence, kv-head and tile, W cost units long, and each of G CTAs takes
+// ceil(W / G) of it.  An item cut by such a bound is shared: its key blocks divide in
 // proportion, each CTA's part is a piece, and a second kernel merges the pieces (of partial
 // results in the workspace: slot 0 of a CTA for an item that began before its range, slot 1 for
 // one that ends after it).
@@ -120,10 +120,9 @@ __host__ __device__ __forceinline__ TileBlocks tile_blocks(const TileRows &r, in
   return b;
 }
 
-// first cost unit of CTA c of G
-__host__ __device__ __forceinline__ int64_t range_bound(int64_t W, int c, int G) {
-  const int64_t per = plan_div(W, G);
-  return per * c + (uint32_t)(W - per * G) * (uint32_t)c / (uint32_t)G;
+// cost units of a CTA of G: CTA c takes [c step, (c + 1) step) of the line, up to its end W
+__host__ __device__ __forceinline__ int64_t range_step(int64_t W, int G) {
+  return plan_div(W + G - 1, G);
 }
 
 // blocks before a cut at cost unit y of an item: in whole blocks of the rows that the units stand

@@ -108,28 +108,30 @@ struct TcQueue {
       mbar_init(&empty[i], readers);
     }
   }
-  // piece i into its slot (w: null ends the queue); false when a wait ran out
-  template <typename B>
-  __device__ __forceinline__ bool put(B &b, uint32_t i, const ChunkWalk *w,
-                                      const ChunkAttendArgs &a) {
+  // piece i into its slot; false when a wait ran out
+  template <typename B, typename W>
+  __device__ __forceinline__ bool put(B &b, uint32_t i, const W &w, const ChunkAttendArgs &a) {
     if (!tc_wait(b, &empty[i % kPieces], ((i / kPieces) & 1) ^ 1)) return false;
     TcPiece &p = piece[i % kPieces];
-    p.blk1 = -1;
-    if (w) {
-      p.rows = w->rows;
-      p.blocks = w->blocks;
-      p.blk0 = w->blk0;
-      p.blk1 = w->blk1;
-      p.n = w->q.n;
-      p.tok0 = w->off + w->t * a.shape.tok;
-      p.tokens = w->tokens(a);
-      p.kvh = w->kvh;
-      p.slot = w->whole() ? -1 : w->slot();
-      p.bad = 0;
-      p.row0 = w->row0;
-    }
+    p.rows = w.rows;
+    p.blocks = w.blocks;
+    p.blk0 = w.blk0;
+    p.blk1 = w.blk1;
+    p.n = w.q.n;
+    p.tok0 = w.off + w.t * a.shape.tok;
+    p.tokens = w.tokens(a);
+    p.kvh = w.kvh;
+    p.slot = w.whole() ? -1 : w.slot();
+    p.bad = 0;
+    p.row0 = w.row0;
     mbar_arrive(&full[i % kPieces]);
     return true;
+  }
+  template <typename B>
+  __device__ __forceinline__ void end(B &b, uint32_t i) {
+    if (!tc_wait(b, &empty[i % kPieces], ((i / kPieces) & 1) ^ 1)) return;
+    piece[i % kPieces].blk1 = -1;
+    mbar_arrive(&full[i % kPieces]);
   }
   template <typename B>
   __device__ __forceinline__ bool wait(B &b, uint32_t i) {

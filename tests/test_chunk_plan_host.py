@@ -81,9 +81,10 @@ int main() {
         }
     }
     int64_t end = 0;
+    const int64_t step = range_step(W, G);
     std::vector<int> next(start.size(), 0);
     for (int c = 0; c < G; ++c) {
-      const int64_t y0 = range_bound(W, c, G), y1 = range_bound(W, c + 1, G);
+      const int64_t y0 = plan_min(W, c * step), y1 = plan_min(W, y0 + step);
       CHECK(y0 == end && y1 >= y0);
       end = y1;
       int slots[2] = {0, 0};
@@ -105,7 +106,7 @@ int main() {
   const ChunkSeq big{2147483647, 2147483647};
   const ChunkShape s{16, 6, 0, 0};
   const int64_t W = tiles_cost(big, s, big.tiles(s.tok)) / 2;
-  CHECK(W > 0 && range_bound(W, 304, 304) == W && range_bound(W, 152, 304) <= W / 2 + 1);
+  CHECK(W > 0 && range_step(W, 304) * 304 >= W && range_step(W, 304) * 304 - W < 304);
   const int64_t c = tile_cost(big, s, big.tiles(16) - 1);
   CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1, 6) <= 2147483647 / 64 + 1);
   puts("ok");
