@@ -2,12 +2,15 @@
 //
 // One pass over a row: each thread keeps the largest processed logit m it has seen, the lowest
 // token that has it, and the sum s of exp(x - m) (s falls by exp(m - m') when a larger m' comes),
-// and the threads' triples merge in a tree.  A row is split over a cluster of CTAs that merge
-// through distributed shared memory, so a batch of one still spreads over 16 SMs.
+// and the threads' triples merge in a tree.  A row is split over a cluster of CTAs that send theirs
+// to the first CTA through distributed shared memory, so a batch of one still spreads over many SMs.
 //
-// The penalties touch few tokens: a row's seen bits say which, one bit beside each logit, and the
-// count of a token is read only where its bit is set.  Biased tokens get a bit in shared memory;
-// only they look through the row's list.
+// The call reads the logits once and is bound by that, so a thread does little for a vector of 16
+// bytes: its maximum, and an exponential an element.  The penalties touch few tokens: a row's seen
+// bits say which, one bit beside each logit.  Those tokens, and the biased ones, are listed first and
+// left out of the pass; they are processed after it, a thread each, so that the reads of their
+// counts wait together.  What is left for the pass is one bit a token in shared memory; a vector
+// with no bit set is not even read.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -19,7 +22,8 @@
 namespace lg {
 namespace {
 
-constexpr int kPickThreads = 512;
+constexpr int kAhead = 4;     // vectors of a thread in flight
+constexpr int kAside = 2048;  // listed tokens of a CTA
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -60,162 +64,327 @@ struct PickArgs {
   int V, words, slice;  // slice: tokens a CTA of the cluster takes, a multiple of 32
 };
 
-template <typename T>
-__device__ __forceinline__ float to_float(T v);
-template <>
-__device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-// bits t .. t + n - 1 of a row of words (n <= 16, t + n within the row's 32 * words bits)
-__device__ __forceinline__ uint32_t bits_at(const uint32_t *w, int t, int words) {
-  const int i = t >> 5;
-  const uint32_t lo = w[i], hi = i + 1 < words ? w[i + 1] : 0u;
-  return __funnelshift_r(lo, hi, t & 31);
+// bits sh .. sh + 31 of two words, sh < 32
+__device__ __forceinline__ uint32_t window(const uint32_t *w, int sh) {
+  return __funnelshift_r(w[0], w[1], sh);
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+// the largest element of 16 bytes, NaN if one is
+template <typename T>
+__device__ __forceinline__ float max16(const uint4 &u);
+template <>
+__device__ __forceinline__ float max16<__nv_bfloat16>(const uint4 &u) {
+  const __nv_bfloat162 *h = (const __nv_bfloat162 *)&u;
+  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  return __bfloat162float(__hmax_nan(m.x, m.y));
+}
+template <>
+__device__ __forceinline__ float max16<float>(const uint4 &u) {
+  auto two = [](float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  };
+  const float *f = (const float *)&u;
+  return two(two(f[0], f[1]), two(f[2], f[3]));
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float *f) {
+  if constexpr (sizeof(T) == 2) {
+    uint4 w;
+    __nv_bfloat162 *h = (__nv_bfloat162 *)&w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+    return w;
+  } else {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+  }
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
 
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+// the lanes' triples merged, the same in every lane
+__device__ __forceinline__ Top warp_top(const Top &t) {
+  Top r;
+  r.m = warp_max(t.m);
+  r.id = (int)__reduce_min_sync(0xffffffffu, (unsigned)(t.m == r.m ? t.id : INT_MAX));
+  r.s = t.m == -INFINITY ? 0.f : t.s * share(t.m, r.m);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+  return r;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kPickThreads) pick_token_kernel(PickArgs a, int csize) {
+constexpr int kMaxCluster = 16;
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, int csize) {
   constexpr int N = 16 / (int)sizeof(T);
-  extern __shared__ uint32_t s_biased[];  // [slice / 32] when there are biases
-  __shared__ Top s_top[kPickThreads / 32];
-  __shared__ Top s_cta;
+  constexpr uint32_t kAll = (1u << N) - 1;
+  extern __shared__ uint32_t s_bits[];  // [4][slice / 32]: allowed tokens, those of the pass, listed ones, biased ones
+  __shared__ Top s_top[NT / 32];
+  __shared__ float s_max[NT / 32];
+  __shared__ Top s_ranks[kMaxCluster];
+  __shared__ int s_aside, s_fit;        // tokens to be listed; entries of the list that hold one
+  __shared__ uint32_t s_list[kAside];   // token, bit 30: seen, bit 31: biased
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int b = blockIdx.x / csize;
-  const int rank = csize > 1 ? (int)cluster_rank() : 0;
+  const int b = blockIdx.x / csize, rank = blockIdx.x % csize;
+  if (csize > 1)  // (waited for before anything is sent: the peers have started)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   pdl_enter();
-  const bool skip = cta_status_bad(a.status);
-  Top top{-INFINITY, 0.f, INT_MAX};
-  const int lo = rank * a.slice, hi = min(a.V, lo + a.slice);  // this CTA's tokens
-  int b0 = 0, b1 = 0;
-  if (a.bias_off && !skip) {
-    b0 = a.bias_off[b];
-    b1 = a.bias_off[b + 1];
-    for (int i = tid; i < a.slice / 32; i += kPickThreads) s_biased[i] = 0;
-    __syncthreads();
-    for (int e = b0 + tid; e < b1; e += kPickThreads) {
-      const int t = a.bias_id[e];
-      if (t >= lo && t < hi) atomicOr(&s_biased[(t - lo) >> 5], 1u << ((t - lo) & 31));
-    }
-    __syncthreads();
+  if (tid == 0) {
+    s_aside = 0;
+    s_fit = kAside;
   }
-  if (lo < hi && !skip) {
+  const bool skip = cta_status_bad(a.status);
+  Top top{-INFINITY, 0.f, INT_MAX};  // of the tokens processed one by one
+  float m = -INFINITY, sum = 0.f;    // of this thread's vectors
+  int best = 0;                      // the first vector that has m
+  const int lo = rank * a.slice, hi = skip ? lo : min(a.V, lo + a.slice);  // this CTA's tokens
+  if (lo < hi) {
     const T *x = (const T *)a.x + b * a.stride;
     T *out = a.out ? (T *)a.out + b * a.stride : nullptr;
     const uint32_t *seen = a.seen ? a.seen + (int64_t)b * a.words : nullptr;
     const uint32_t *allowed = a.allowed ? a.allowed + (int64_t)b * a.words : nullptr;
     const int32_t *counts = a.seen ? a.counts + (int64_t)b * a.V : nullptr;
     const float4 pen = a.seen ? a.penalty[b] : make_float4(1.f, 0.f, 0.f, 0.f);
+    const int w0 = lo >> 5, nw = ((hi + 31) >> 5) - w0, sw = a.slice / 32 + 1;
+    uint32_t *s_ok = s_bits, *s_pass = s_bits + sw, *s_apart = s_bits + 2 * sw,
+             *s_bias = s_bits + 3 * sw;
+    int b0 = 0, b1 = 0;
+    if (a.bias_off) {
+      b0 = a.bias_off[b];
+      b1 = a.bias_off[b + 1];
+    }
     // one token's processed logit
-    auto process = [&](float v, int t, bool was_seen, bool biased, bool ok) {
+    auto process = [&](float v, int t, bool was_seen, bool biased, int n) {
       if (was_seen) {
         v = v > 0.f ? __fdiv_rn(v, pen.x) : __fmul_rn(v, pen.x);
-        const int n = counts[t];
         if (n > 0) v = __fsub_rn(__fsub_rn(v, __fmul_rn(pen.z, (float)n)), pen.y);
       }
       if (biased)
+#pragma unroll 4
         for (int e = b0; e < b1; ++e)
           if (a.bias_id[e] == t) v = __fadd_rn(v, a.bias_val[e]);
-      return ok && v == v ? v : -INFINITY;
+      return v == v ? v : -INFINITY;
     };
-    auto add = [&](float v, int t) {
-      if (v > top.m) {
-        top.s = top.m == -INFINITY ? 0.f : top.s * share(top.m, v);
-        top.m = v;
-        top.id = t;
+    // one more token
+    auto add = [&](float v, int t) { top = merge(top, Top{v, v == -INFINITY ? 0.f : 1.f, t}); };
+    // n listed tokens, their logits and counts read together
+    auto apart = [&](const uint32_t *entry, int n) {
+      float v[kAhead];
+      int c[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int t = (int)(entry[k] & 0x3fffffffu);
+        v[k] = k < n ? Elem<T>::load(x, t) : 0.f;
+        c[k] = k < n && (entry[k] >> 30 & 1) ? counts[t] : 0;
       }
-      if (v != -INFINITY) top.s += share(v, top.m);
+#pragma unroll 1
+      for (int k = 0; k < n; ++k) {
+        float w = v[0];
+        int cn = c[0];
+#pragma unroll
+        for (int j = 1; j < kAhead; ++j) {
+          w = k == j ? v[j] : w;
+          cn = k == j ? c[j] : cn;
+        }
+        const int t = (int)(entry[k] & 0x3fffffffu);
+        w = process(w, t, entry[k] >> 30 & 1, entry[k] >> 31, cn);
+        if (out) Elem<T>::store(out, t, w);
+        add(w, t);
+      }
     };
-    auto one = [&](int t) {
-      const bool s = seen && (seen[t >> 5] >> (t & 31) & 1);
-      const bool bi = b0 < b1 && (s_biased[(t - lo) >> 5] >> ((t - lo) & 31) & 1);
-      const bool ok = !allowed || (allowed[t >> 5] >> (t & 31) & 1);
-      const float v = process(to_float<T>(x[t]), t, s, bi, ok);
-      if (out) Elem<T>::store(out, t, v);
-      add(v, t);
+
+    // the bits: every token, or the allowed ones, but for the seen and biased ones
+#pragma unroll 4
+    for (int i = tid; i < nw; i += NT) {
+      const int left = a.V - ((w0 + i) << 5);
+      const uint32_t ok =
+          (allowed ? __ldg(allowed + w0 + i) : ~0u) & (left >= 32 ? ~0u : (1u << left) - 1);
+      s_ok[i] = ok;
+      s_pass[i] = ok;
+      s_apart[i] = seen ? seen[w0 + i] & ok : 0u;
+      s_bias[i] = 0;
+    }
+    if (b0 < b1) {
+      __syncthreads();
+      for (int e = b0 + tid; e < b1; e += NT) {
+        const int t = a.bias_id[e] - lo;
+        if (t >= 0 && t < hi - lo) atomicOr(&s_bias[t >> 5], s_pass[t >> 5] & 1u << (t & 31));
+      }
+      __syncthreads();
+    }
+    auto entry = [&](int i, int j, uint32_t was_seen) {  // token j of word i
+      return (uint32_t)(lo + 32 * i + j) | (was_seen >> j & 1u) << 30 | (s_bias[i] >> j & 1u) << 31;
     };
+    for (int i = tid; i < nw; i += NT) {
+      const uint32_t was_seen = s_apart[i];
+      uint32_t w = was_seen | s_bias[i];
+      if (w == 0) continue;
+      s_pass[i] &= ~w;
+      int at = atomicAdd(&s_aside, __popc(w));
+      if (at + __popc(w) > kAside) {  // (the word stays, and so does every later one)
+        s_apart[i] = w;
+        atomicMin(&s_fit, at);
+        continue;
+      }
+      s_apart[i] = 0;
+      for (; w; w &= w - 1) s_list[at++] = entry(i, __ffs((int)w) - 1, was_seen);
+    }
+    __syncthreads();
+
     // 16-byte vectors where the row is aligned for them, single tokens around
     const int to16 = (int)((16 - ((uintptr_t)(x + lo) & 15)) & 15) / (int)sizeof(T);
     const int v0 = min(hi, lo + to16), nvec = (hi - v0) / N;
     const bool out16 = out && (((uintptr_t)(out + v0)) & 15) == 0;
+    const uint4 *xv = (const uint4 *)(x + v0);
+    // a thread's vectors are NT vectors apart: whole words of bits, at one place in a word
+    constexpr int kStep = NT * N / 32;
+    const int sh = (v0 - lo + tid * N) & 31;
+    const uint32_t *pass0 = s_pass + ((v0 - lo + tid * N) >> 5), *ok0 = pass0 - sw;
+    for (int i0 = tid; i0 < nvec; i0 += kAhead * NT, pass0 += kAhead * kStep, ok0 += kAhead * kStep) {
+      uint4 u[kAhead];
+      uint32_t kb[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * NT;
+        kb[k] = 0;
+        u[k] = make_uint4(0, 0, 0, 0);
+        if (i >= nvec) continue;
+        kb[k] = window(pass0 + k * kStep, sh) & kAll;
+        if (kb[k] || out) u[k] = __ldcs(xv + i);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * NT, t = v0 + i * N;
+        float f[N], vm = max16<T>(u[k]);
+        Elem<T>::unpack(u[k], (float2 *)f);
+        const bool nan = vm != vm;
+        if (nan) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) f[e] = f[e] == f[e] ? f[e] : -INFINITY;
+        }
+        if (out && i < nvec) {  // (listed tokens are written again after the pass)
+          const uint32_t ab = allowed ? window(ok0 + k * kStep, sh) & kAll : kAll;
+          uint4 w = u[k];
+          if (nan || ab != kAll) {
+            float g[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] = ab >> e & 1 ? f[e] : -INFINITY;
+            w = pack16<T>(g);
+          }
+          if (out16) {
+            __stcs((uint4 *)(out + t), w);
+          } else {
+            const T *h = (const T *)&w;
+#pragma unroll
+            for (int e = 0; e < N; ++e) out[t + e] = h[e];
+          }
+        }
+        if (nan || kb[k] != kAll) {
+          vm = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            f[e] = kb[k] >> e & 1 ? f[e] : -INFINITY;
+            vm = fmaxf(vm, f[e]);
+          }
+        }
+        best = vm > m ? i : best;
+        const float m1 = fmaxf(m, vm), base = m1 == -INFINITY ? 0.f : m1;
+        sum *= exp2_fast((m - base) * kLog2e);
+        m = m1;
+        float2 p[N / 2];
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+          const float2 d = __fadd2_rn(make_float2(f[2 * e], f[2 * e + 1]), make_float2(-base, -base));
+          const float2 z = __fmul2_rn(d, make_float2(kLog2e, kLog2e));
+          p[e] = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+        }
+#pragma unroll
+        for (int w = N / 4; w; w /= 2)
+#pragma unroll
+          for (int e = 0; e < w; ++e) p[e] = __fadd2_rn(p[e], p[e + w]);
+        sum += p[0].x + p[0].y;
+      }
+    }
+    // the ends of the row, then the listed tokens
+    auto one = [&](int t) {
+      if (!(s_pass[(t - lo) >> 5] >> ((t - lo) & 31) & 1)) {
+        if (out && allowed && !(allowed[t >> 5] >> (t & 31) & 1)) Elem<T>::store(out, t, -INFINITY);
+        return;
+      }
+      float v = Elem<T>::load(x, t);
+      v = v == v ? v : -INFINITY;
+      if (out) Elem<T>::store(out, t, v);
+      add(v, t);
+    };
     if (tid < v0 - lo) one(lo + tid);
     if (tid < hi - v0 - nvec * N) one(v0 + nvec * N + tid);
-    const uint4 *xv = (const uint4 *)(x + v0);
-    for (int i = tid; i < nvec; i += kPickThreads) {
-      const uint4 u = xv[i];
-      const int t = v0 + i * N;
-      const uint32_t all = (1u << N) - 1;
-      const uint32_t sb = seen ? bits_at(seen, t, a.words) & all : 0u;
-      const uint32_t ab = allowed ? bits_at(allowed, t, a.words) & all : all;
-      const uint32_t bb = b0 < b1 ? bits_at(s_biased, t - lo, a.slice / 32) & all : 0u;
-      float f[N];
-      Elem<T>::unpack(u, (float2 *)f);
+    __syncthreads();  // the pass has stored the listed tokens' logits as they came
+    const int listed = min(s_aside, s_fit);
+    if (s_aside > kAside)
+      for (int i = tid; i < nw; i += NT)
+        for (uint32_t w = s_apart[i]; w; w &= w - 1) {
+          uint32_t e[kAhead] = {entry(i, __ffs((int)w) - 1, seen ? seen[w0 + i] : 0u)};
+          apart(e, 1);
+        }
+    for (int i = tid; i < listed; i += kAhead * NT) {
+      uint32_t e[kAhead];
+      int n = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const uint32_t bit = 1u << e;
-        f[e] = process(f[e], t + e, sb & bit, bb & bit, ab & bit);
-      }
-      if (out) {
-        if (out16) {
-          uint4 w;
-          if constexpr (sizeof(T) == 2) {
-            __nv_bfloat162 *h = (__nv_bfloat162 *)&w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-          } else {
-            w = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-                           __float_as_uint(f[3]));
-          }
-          *(uint4 *)(out + t) = w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < N; ++e) Elem<T>::store(out, t + e, f[e]);
+      for (int k = 0; k < kAhead; ++k) {
+        e[k] = 0;
+        if (i + k * NT < listed) {
+          e[k] = s_list[i + k * NT];
+          n = k + 1;
         }
       }
-#pragma unroll
-      for (int e = 0; e < N; ++e) add(f[e], t + e);
+      apart(e, n);
     }
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    Top u;
-    u.m = __shfl_xor_sync(0xffffffffu, top.m, o);
-    u.s = __shfl_xor_sync(0xffffffffu, top.s, o);
-    u.id = __shfl_xor_sync(0xffffffffu, top.id, o);
-    // the same order on both sides, so that both get the same bits
-    top = (lane & o) ? merge(u, top) : merge(top, u);
-  }
-  if (lane == 0) s_top[warp] = top;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kPickThreads / 32; ++w) top = merge(top, s_top[w]);
-    s_cta = top;
-  }
-  if (csize > 1) {
-    cluster_sync();
-    if (rank == 0 && tid == 0) {
-      const uint32_t mine = smem_addr(&s_cta);
-      for (int r = 1; r < csize; ++r) {
-        uint32_t at;
-        Top u;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(r));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u.m) : "r"(at));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u.s) : "r"(at + 4));
-        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(u.id) : "r"(at + 8));
-        top = merge(top, u);
+    // the CTA's maximum; the token only from threads whose vectors have it
+    const float wm = warp_max(fmaxf(m, top.m));
+    if (lane == 0) s_max[warp] = wm;
+    __syncthreads();
+    const float cm = warp_max(s_max[lane & (NT / 32 - 1)]);
+    Top vec{m, sum, INT_MAX};
+    if (m == cm && cm != -INFINITY) {
+      if (cm == INFINITY) vec.s = 0.f;
+      for (int i = best; i < nvec; i += NT) {
+        const int at = v0 + i * N;
+        const uint32_t kb = window(s_pass + ((at - lo) >> 5), (at - lo) & 31) & kAll;
+        for (int e = N - 1; e >= 0; --e)
+          if ((kb >> e & 1) && Elem<T>::load(x, at + e) == m) {
+            vec.id = min(vec.id, at + e);
+            if (cm == INFINITY) vec.s += 1.f;
+          }
+        if (cm != INFINITY) break;
       }
     }
-    cluster_sync();  // the peers' shared memory lives until it has been read
+    top = merge(top, vec);
+  }
+  top = warp_top(top);
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+  if (warp == 0) top = warp_top(lane < NT / 32 ? s_top[lane] : Top{-INFINITY, 0.f, INT_MAX});
+  if (csize > 1) {
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (tid == 0) {  // to the first CTA
+      uint32_t at;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(&s_ranks[rank])), "r"(0));
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(top.m) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(top.s) : "memory");
+      asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at + 8), "r"(top.id) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::
+                     : "memory");
+    if (rank == 0 && warp == 0)
+      top = warp_top(lane < csize ? s_ranks[lane] : Top{-INFINITY, 0.f, INT_MAX});
   }
   if (rank == 0 && tid == 0 && !skip) {
     const bool none = top.m == -INFINITY;
@@ -249,21 +418,18 @@ __global__ void count_tokens_kernel(const int32_t *tokens, const int32_t *off, i
   if (generated) atomicAdd(&counts[(int64_t)b * V + t], 1);
 }
 
-template <typename T>
-cudaError_t launch_pick_typed(PickArgs &a, int batch, cudaStream_t s) {
-  // CTAs a row: as many as keep about two CTAs an SM busy, at most 16, each with at least 4096
-  // tokens of its own
-  int c = 1;
-  while (c < 16 && (int64_t)batch * c < 152 && a.V / (2 * c) >= 4096) c *= 2;
+template <typename T, int NT>
+cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
   a.slice = ((a.V + c - 1) / c + 31) / 32 * 32;
-  const size_t smem = a.bias_off ? (size_t)a.slice / 8 : 0;
-  auto kern = pick_token_kernel<T>;
+  // (a word more each: a vector's bits are read from two)
+  const size_t smem = (size_t)(a.slice / 32 + 1) * 4 * sizeof(uint32_t);
+  auto kern = pick_token_kernel<T, NT>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-  if (smem > 32 * 1024)
+  if (smem > 36 * 1024)
     LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(batch * c));
-  cfg.blockDim = dim3(kPickThreads);
+  cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -277,6 +443,18 @@ cudaError_t launch_pick_typed(PickArgs &a, int batch, cudaStream_t s) {
   cfg.numAttrs = 2;
   LG_TRY(cudaLaunchKernelEx(&cfg, kern, a, c));
   return cudaGetLastError();
+}
+
+// CTAs a row: as many as fit the GPU at once (a kernel of 512 threads twice an SM, of 256 four
+// times), at most 16, each with 2048 tokens or more.
+template <typename T>
+cudaError_t launch_pick_sized(PickArgs &a, int batch, cudaStream_t s) {
+  const int nt = batch * kMaxCluster <= 2 * 152 ? 512 : 256;
+  int c = (nt == 512 ? 2 : 4) * 152 / batch, most = a.V / 2048;
+  c = c < 1 ? 1 : c > kMaxCluster ? kMaxCluster : c;
+  c = c > most ? (most < 1 ? 1 : most) : c;
+  if (nt == 512) return launch_pick_typed<T, 512>(a, batch, c, s);
+  return launch_pick_typed<T, 256>(a, batch, c, s);
 }
 
 }  // namespace
@@ -299,8 +477,8 @@ cudaError_t launch_pick_token(const lg_logits &x, const uint32_t *seen, const in
   a.stride = x.stride;
   a.V = x.V;
   a.words = (x.V + 31) / 32;
-  return x.dtype == LG_BF16 ? launch_pick_typed<__nv_bfloat16>(a, x.batch, s)
-                            : launch_pick_typed<float>(a, x.batch, s);
+  return x.dtype == LG_BF16 ? launch_pick_sized<__nv_bfloat16>(a, x.batch, s)
+                            : launch_pick_sized<float>(a, x.batch, s);
 }
 
 cudaError_t launch_count_tokens(const int32_t *tokens, const int32_t *off, int T, int batch, int V,

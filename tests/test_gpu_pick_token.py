@@ -88,6 +88,22 @@ def test_sizes(cuda, dtype, B, V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [3, 96])
+def test_many_seen_tokens(cuda, dtype, B):
+    """histories that fill stretches of the vocabulary, more of them than a CTA lists"""
+    V = 60013
+    rng = np.random.default_rng(B)
+    x = _dev(rng.standard_normal((B, V)).astype(np.float32) * 3, cuda, chunk_ref.tdtype(dtype))
+    seen, counts, pen = _history(rng, B, V, 4000)
+    seen[:, 100:9000] = True
+    counts[:, 200:5000] += rng.integers(0, 3, (B, 4800))
+    bias = [[(int(t), 1.5) for t in rng.integers(0, V, 5)] for _ in range(B)]
+    _run(cuda, x, seen, counts, pen, bias)
+    _run(cuda, x, seen, counts, pen, bias, rng.random((B, V)) < 0.5)
+    _run(cuda, x, seen, counts, pen, bias, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_and_in_place(cuda, dtype):
     rng = np.random.default_rng(1)
     for V, pad in ((1001, 6), (777, 0), (640, 3)):
