@@ -95,26 +95,18 @@ __device__ __forceinline__ void token_slots(const lg_cache &c, const lg_chunk &c
 }
 
 template <typename T>
-struct Chunk16 {
-  static constexpr int N = 16 / (int)sizeof(T);
-  float f[N];
-  __device__ __forceinline__ void load(const T *p) {
-    const uint4 u = *(const uint4 *)p;
-    Elem<T>::unpack(u, (float2 *)f);
-  }
-  __device__ __forceinline__ void store(T *p) const {
-    uint4 u;
-    if constexpr (sizeof(T) == 2) {
-      __nv_bfloat162 *h = (__nv_bfloat162 *)&u;
+__device__ __forceinline__ void store16(T *p, const float *f) {
+  uint4 u;
+  if constexpr (sizeof(T) == 2) {
+    __nv_bfloat162 *h = (__nv_bfloat162 *)&u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    } else {
-      u = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-                     __float_as_uint(f[3]));
-    }
-    *(uint4 *)p = u;
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+  } else {
+    u = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                   __float_as_uint(f[3]));
   }
-};
+  *(uint4 *)p = u;
+}
 
 // cosine and sine of the angle `turn` * 2^-64 turns
 __device__ __forceinline__ void turn_cos_sin(uint64_t turn, float &co, float &si) {
@@ -130,12 +122,13 @@ __device__ __forceinline__ void turn_cos_sin(uint64_t turn, float &co, float &si
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 64;  // tokens a CTA at most
+constexpr int kTogether = 2;     // heads of a thread in flight
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kRopeThreads)
     rope_append_kernel(lg_cache c, lg_chunk ch, RopeArgs a, const __grid_constant__ RopeTable tab,
                        int layout) {
-  constexpr int N = Chunk16<T>::N;
+  constexpr int N = 16 / (int)sizeof(T);
   __shared__ int64_t s_slot[kRopeTokens];
   // no early trigger: the loop-onset test reads the sketches before its own wait and re-checks the
   // newest row alone, so a kernel that may write others has to be complete before it starts
@@ -166,36 +159,48 @@ __global__ void __launch_bounds__(kRopeThreads)
         si[e] *= a.mscale;
       }
       const int h1 = min(a.H_q + c.H_kv, (grp + 1) * a.heads);
-      for (int h = grp * a.heads; h < h1; ++h) {
-        const T *src;
-        T *dst;
-        if (h < a.H_q) {
-          src = (const T *)a.q + t * a.q_stride + (int64_t)h * D;
-          dst = (T *)a.q_out + ((int64_t)t * a.H_q + h) * D;
-        } else {
-          src = (const T *)a.k + t * a.k_stride + (int64_t)(h - a.H_q) * D;
-          dst = K + (row0 + (h - a.H_q) * c.S_total + slot) * D;
-        }
-        Chunk16<T> x0, x1, y0, y1;
-        x0.load(src + pc * N);
-        x1.load(src + pc * N + half);
-        if (layout == LG_ROPE_HALF) {
+      // kTogether heads' chunks are requested before the first is rotated
+      const T *qs = (const T *)a.q + t * a.q_stride + pc * N;
+      const T *ks = (const T *)a.k + t * a.k_stride + pc * N;
+      T *qd = (T *)a.q_out + (int64_t)t * a.H_q * D + pc * N;
+      T *kd = K + (row0 + slot) * D + pc * N;
+      for (int h0 = grp * a.heads; h0 < h1; h0 += kTogether) {
+        uint4 u0[kTogether], u1[kTogether];
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            y0.f[e] = x0.f[e] * co[e] - x1.f[e] * si[e];
-            y1.f[e] = x0.f[e] * si[e] + x1.f[e] * co[e];
-          }
-        } else {
+        for (int k = 0; k < kTogether; ++k) {
+          const int h = h0 + k;
+          if (h >= h1) break;
+          const T *src = h < a.H_q ? qs + (int64_t)h * D : ks + (int64_t)(h - a.H_q) * D;
+          u0[k] = *(const uint4 *)src;
+          u1[k] = *(const uint4 *)(src + half);
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+          const int h = h0 + k;
+          if (h >= h1) break;
+          T *dst = h < a.H_q ? qd + (int64_t)h * D : kd + (h - a.H_q) * c.S_total * D;
+          float2 p[N / 2], q[N / 2], y0[N / 2], y1[N / 2];
+          Elem<T>::unpack(u0[k], p);
+          Elem<T>::unpack(u1[k], q);
 #pragma unroll
           for (int e = 0; e < N / 2; ++e) {
-            y0.f[2 * e] = x0.f[2 * e] * co[e] - x0.f[2 * e + 1] * si[e];
-            y0.f[2 * e + 1] = x0.f[2 * e] * si[e] + x0.f[2 * e + 1] * co[e];
-            y1.f[2 * e] = x1.f[2 * e] * co[e + N / 2] - x1.f[2 * e + 1] * si[e + N / 2];
-            y1.f[2 * e + 1] = x1.f[2 * e] * si[e + N / 2] + x1.f[2 * e + 1] * co[e + N / 2];
+            if (layout == LG_ROPE_HALF) {  // two pairs at a time
+              const float2 cc = make_float2(co[2 * e], co[2 * e + 1]);
+              const float2 ss = make_float2(si[2 * e], si[2 * e + 1]);
+              const float2 neg = make_float2(-ss.x, -ss.y);
+              y0[e] = __ffma2_rn(p[e], cc, __fmul2_rn(q[e], neg));
+              y1[e] = __ffma2_rn(q[e], cc, __fmul2_rn(p[e], ss));
+            } else {  // the pair (x, y): (x, y) c + (-y, x) s
+              const int f = e + N / 2;
+              y0[e] = __ffma2_rn(p[e], make_float2(co[e], co[e]),
+                                 __fmul2_rn(make_float2(-p[e].y, p[e].x), make_float2(si[e], si[e])));
+              y1[e] = __ffma2_rn(q[e], make_float2(co[f], co[f]),
+                                 __fmul2_rn(make_float2(-q[e].y, q[e].x), make_float2(si[f], si[f])));
+            }
           }
+          store16<T>(dst, (const float *)y0);
+          store16<T>(dst + half, (const float *)y1);
         }
-        y0.store(dst + pc * N);
-        y1.store(dst + pc * N + half);
       }
     }
     return;
@@ -247,16 +252,18 @@ cudaError_t launch_rope_typed(const lg_cache &c, const lg_chunk &ch, RopeArgs &a
                               const RopeTable &tab, cudaStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   const int pieces = a.rot / 2 / N, heads = a.H_q + c.H_kv;
-  // few tokens: a head or so a thread, so that one token spreads over many threads; many tokens:
-  // eight heads a thread, so that its sines and cosines serve eight rotations
-  a.heads = ch.T >= 512 ? 8 : ch.T >= 64 ? 4 : 1;
+  // as many heads a thread, for its sines and cosines to serve, as leave the GPU four CTAs an SM
+  const int64_t full = (int64_t)4 * 152 * kRopeThreads;
+  int groups = 1;
+  while (groups < heads && (int64_t)ch.T * groups * pieces < full) groups *= 2;
+  a.heads = (heads + groups - 1) / groups;
   a.units = (heads + a.heads - 1) / a.heads * pieces;
-  a.tok = kRopeThreads * 2 / a.units;
+  a.tok = kRopeThreads / a.units;
   a.tok = a.tok < 1 ? 1 : a.tok > kRopeTokens ? kRopeTokens : a.tok;
   a.rot_blocks = (ch.T + a.tok - 1) / a.tok;
   a.copy_units = c.H_kv * (D / N) + heads * ((D - a.rot) / N) + (c.pos ? c.H_kv : 0);
   a.copy_units = (a.copy_units + 31) / 32 * 32;
-  a.copy_tok = kRopeThreads * 4 / a.copy_units;
+  a.copy_tok = kRopeThreads * (ch.T * (int64_t)a.copy_units > 4 * full ? 4 : 1) / a.copy_units;
   a.copy_tok = a.copy_tok < 1 ? 1 : a.copy_tok > kRopeTokens ? kRopeTokens : a.copy_tok;
   const int64_t grid = (int64_t)a.rot_blocks + (ch.T + a.copy_tok - 1) / a.copy_tok;
   LG_TRY(launch_pdl(rope_append_kernel<T, D>, dim3((unsigned)grid), kRopeThreads, 0, s, c, ch, a,
