@@ -34,7 +34,7 @@ __global__ void begin_chunk_kernel(lg_cache c, lg_chunk ch) {
 //
 // A thread owns two 16-byte chunks of a token's heads: for the half layout the chunks that hold
 // its pairs' first and second elements, for the interleaved one two chunks of whole pairs.  It
-// takes its sines and cosines once and walks over `heads` heads.  Queries, then keys; the
+// takes its sines and cosines once and walks over heads.  Queries, then keys; the
 // unrotated chunks of a head and the values are copied by the other blocks.
 
 struct RopeTable {
@@ -50,8 +50,8 @@ struct RopeArgs {
   float mscale;
   int guard;        // the layer's V rows are sketched
   int tok;          // tokens a CTA (rotation)
-  int heads;        // heads a thread (rotation)
-  int units;        // threads a token (rotation) = head groups * rot chunks / 2
+  int groups;       // threads that share a token's heads: every groups-th head each
+  int units;        // threads a token (rotation) = groups * rot chunks / 2
   int rot_blocks;   // CTAs of the rotation part
   int copy_units;   // 16-byte chunks a token in the copy part, whole warps
   int copy_tok;
@@ -158,17 +158,17 @@ __global__ void __launch_bounds__(kRopeThreads)
         co[e] *= a.mscale;
         si[e] *= a.mscale;
       }
-      const int h1 = min(a.H_q + c.H_kv, (grp + 1) * a.heads);
+      const int h1 = a.H_q + c.H_kv;
       // kTogether heads' chunks are requested before the first is rotated
       const T *qs = (const T *)a.q + t * a.q_stride + pc * N;
       const T *ks = (const T *)a.k + t * a.k_stride + pc * N;
       T *qd = (T *)a.q_out + (int64_t)t * a.H_q * D + pc * N;
       T *kd = K + (row0 + slot) * D + pc * N;
-      for (int h0 = grp * a.heads; h0 < h1; h0 += kTogether) {
+      for (int h0 = grp; h0 < h1; h0 += kTogether * a.groups) {
         uint4 u0[kTogether], u1[kTogether];
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
-          const int h = h0 + k;
+          const int h = h0 + k * a.groups;
           if (h >= h1) break;
           const T *src = h < a.H_q ? qs + (int64_t)h * D : ks + (int64_t)(h - a.H_q) * D;
           u0[k] = *(const uint4 *)src;
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kRopeThreads)
         }
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
-          const int h = h0 + k;
+          const int h = h0 + k * a.groups;
           if (h >= h1) break;
           T *dst = h < a.H_q ? qd + (int64_t)h * D : kd + (h - a.H_q) * c.S_total * D;
           float2 p[N / 2], q[N / 2], y0[N / 2], y1[N / 2];
@@ -252,12 +252,13 @@ cudaError_t launch_rope_typed(const lg_cache &c, const lg_chunk &ch, RopeArgs &a
                               const RopeTable &tab, cudaStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   const int pieces = a.rot / 2 / N, heads = a.H_q + c.H_kv;
-  // as many heads a thread, for its sines and cosines to serve, as leave the GPU four CTAs an SM
+  // a warp's threads side by side on one token's heads, so that it reads and writes whole stretches;
+  // then as many heads a thread, for its sines and cosines to serve, as leave the GPU four CTAs an SM
   const int64_t full = (int64_t)4 * 152 * kRopeThreads;
-  int groups = 1;
-  while (groups < heads && (int64_t)ch.T * groups * pieces < full) groups *= 2;
-  a.heads = (heads + groups - 1) / groups;
-  a.units = (heads + a.heads - 1) / a.heads * pieces;
+  a.groups = pieces < 32 ? 32 / pieces : 1;
+  while (a.groups < heads && (int64_t)ch.T * a.groups * pieces < full) a.groups *= 2;
+  a.groups = a.groups < heads ? a.groups : heads;
+  a.units = a.groups * pieces;
   a.tok = kRopeThreads / a.units;
   a.tok = a.tok < 1 ? 1 : a.tok > kRopeTokens ? kRopeTokens : a.tok;
   a.rot_blocks = (ch.T + a.tok - 1) / a.tok;

@@ -59,14 +59,25 @@ void rope_turns(const lg_rope_params &p, uint64_t *turns) {
     const double b = fmin(ceil(pair_at(p.beta_slow)), rot - 1.0);
     span = fmax(b - a, 0.001);
   }
+  // theta^(-2i/rot) from the powers at i = 1, 2, 4, ..: at most six products, so at most twelve
+  // roundings, for a seventh of the time of a pow a pair
+  double power[6], f[64];
+  for (int k = 0; 1 << k < p.rot / 2; ++k) power[k] = pow(theta, -2.0 * (1 << k) / rot);
+  const double inv = p.scaling == LG_ROPE_PLAIN || p.scaling == LG_ROPE_BASE ? 1.0 : 1.0 / p.factor;
+  f[0] = 1.0;
   for (int i = 0; i < p.rot / 2; ++i) {
-    double f = pow(theta, -2.0 * i / rot), w = 1.0;
+    if (i) {
+      int k = 0;
+      while (!(i >> k & 1)) ++k;
+      f[i] = f[i & (i - 1)] * power[k];
+    }
+    double w = 1.0;  // the share that keeps its frequency
     if (p.scaling == LG_ROPE_LINEAR) w = 0.0;
     if (p.scaling == LG_ROPE_BANDS)
-      w = fmin(fmax((p.orig_len * f / kTwoPi - p.low) / (p.high - p.low), 0.0), 1.0);
+      w = fmin(fmax((p.orig_len * f[i] / kTwoPi - p.low) / (p.high - p.low), 0.0), 1.0);
     if (p.scaling == LG_ROPE_YARN) w = 1.0 - fmin(fmax((i - a) / span, 0.0), 1.0);
-    f = w * f + (1.0 - w) * f / (w < 1.0 ? p.factor : 1.0);
-    turns[i] = (uint64_t)llrint(ldexp(f / kTwoPi, 64));  // f <= 1: below 2^62
+    const double t = (w * f[i] + (1.0 - w) * f[i] * inv) * (0x1p64 / kTwoPi);
+    turns[i] = (uint64_t)llrint(t);  // f <= 1: below 2^62
   }
 }
 

@@ -338,9 +338,10 @@ class Chunk:
 
 def _rows_stride(t, name):
     """elements from token to token of a [T][H][d] tensor whose rows are whole"""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    st, sh = t.stride(), t.shape
+    if len(sh) != 3 or st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]):
         raise ValueError("%s: [T][H][d] with whole rows of H * d elements" % name)
-    return max(t.stride(0), t.shape[1] * t.shape[2])  # one row: its stride says nothing
+    return max(st[0], sh[1] * sh[2])  # one row: its stride says nothing
 
 
 def lg_begin_chunk(cache, chunk, stream=None):
