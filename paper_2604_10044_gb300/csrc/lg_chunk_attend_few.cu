@@ -191,73 +191,75 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       if (ok) bars.queue.end(bars, pieces);
     }
   } else if (warp == W0 + 1) {
-    if (lane == 0) {
-      uint32_t n = 0, c = 0;
-      bool ok = true;
-      constexpr uint32_t kIdS = mma_idesc(128, N, false, false);
-      constexpr uint32_t kIdO = mma_idesc(128, N, true, true);
-      // a head of 64 elements fills 64 of the 128 rows: the others repeat them
-      constexpr uint32_t kLboV = D == 128 ? kBn * 128 : 0;
-      const uint64_t dq = smem_desc(smem_addr(sq), 16, 1024);
-      auto stage = [&](uint32_t i) { return smem_addr(ring + i % ST * C::kTile); };
-      auto wait_full = [&](uint32_t i) {
-        ok = ok && tc_wait(bars, &bars.full[i % ST], (i / ST) & 1);
-      };
-      for (uint32_t pc = 0;; ++pc) {
-        ok = bars.queue.wait(bars, pc);
-        if (!ok) break;
-        const TcPiece &p = bars.queue.at(pc);
-        if (p.blk1 < 0) break;
-        const int blk0 = p.blk0, blocks = p.blk1 - blk0;
-        const TileRows rows = p.rows;
-        const TileBlocks tb = p.blocks;
-        bars.queue.done(pc);
-        ok = tc_wait(bars, &bars.q_full, pc & 1);
-        auto k_at = [&](int j) { return n + (j == 0 ? 0 : 2 * j - 1); };
-        auto scores = [&](int j) {
-          wait_full(k_at(j));
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t dk = smem_desc(stage(k_at(j)), 16, 1024);
-          const uint32_t b = (c + j) & 1;
+    const bool one = elect_one();
+    uint32_t n = 0, c = 0;
+    bool ok = true;
+    constexpr uint32_t kIdS = mma_idesc(128, N, false, false);
+    constexpr uint32_t kIdO = mma_idesc(128, N, true, true);
+    // a head of 64 elements fills 64 of the 128 rows: the others repeat them
+    constexpr uint32_t kLboV = D == 128 ? kBn * 128 : 0;
+    const uint32_t q_lo = desc_lo(smem_addr(sq), 16), p_lo = desc_lo(smem_addr(sp), 16);
+    const uint32_t k_lo = desc_lo(smem_addr(ring), 16), v_lo = desc_lo(smem_addr(ring), kLboV);
+    auto wait_full = [&](uint32_t i) {
+      ok = ok && tc_wait_warp(bars, &bars.full[i % ST], (i / ST) & 1);
+    };
+    for (uint32_t pc = 0;; ++pc) {
+      ok = bars.queue.wait(bars, pc);
+      if (!ok) break;
+      const TcPiece &p = bars.queue.at(pc);
+      const int blk0 = uniform(p.blk0), blocks = uniform(p.blk1) - blk0;
+      if (uniform(p.blk1) < 0) break;
+      const TileRows rows = p.rows;
+      const TileBlocks tb = p.blocks;
+      __syncwarp();
+      if (one) bars.queue.done(pc);
+      ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
+      auto k_at = [&](int j) { return n + (j == 0 ? 0 : 2 * j - 1); };
+      auto scores = [&](int j) {
+        wait_full(k_at(j));
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t b = (c + j) & 1, k0 = k_lo + k_at(j) % ST * (C::kTile >> 4);
+        if (one) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
-            tc_mma_ss(tmem + b * N, dk + (uint64_t)(((k / 4) * (kBn * 128) + (k % 4) * 32) >> 4),
-                      dq + (uint64_t)(((k / 4) * C::kQBox + (k % 4) * 32) >> 4), kIdS, k > 0);
+            tc_mma_ss(tmem + b * N, k0 + (((k / 4) * (kBn * 128) + (k % 4) * 32) >> 4),
+                      q_lo + (((k / 4) * C::kQBox + (k % 4) * 32) >> 4), kIdS, k > 0);
           tc_commit(&bars.s_full[b]);
           tc_commit(&bars.empty[k_at(j) % ST]);
           if (j + 1 == blocks) tc_commit(&bars.q_empty);
-        };
-        scores(0);
-        for (int j = 0; ok && j < blocks; ++j) {
-          if (j + 1 < blocks) scores(j + 1);
-          const uint32_t iv = n + (j + 1 < blocks ? 2 * j + 2 : 2 * j + 1), b = (c + j) & 1;
-          wait_full(iv);
-          if (block_hides(rows, a.shape, tb.index(blk0 + j) * kBn))
-            ok = ok && tc_wait(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-          if (j == 0) ok = ok && tc_wait(bars, &bars.o_free, (pc & 1) ^ 1);
-          ok = ok && tc_wait(bars, &bars.p_full[b], ((c + j) >> 1) & 1);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t dv = smem_desc(stage(iv), kLboV, 1024);
-          const uint64_t dp = smem_desc(smem_addr(sp + b * kPBytes), 16, 1024);
+        }
+      };
+      scores(0);
+      for (int j = 0; ok && j < blocks; ++j) {
+        if (j + 1 < blocks) scores(j + 1);
+        const uint32_t iv = n + (j + 1 < blocks ? 2 * j + 2 : 2 * j + 1), b = (c + j) & 1;
+        wait_full(iv);
+        if (uniform(block_hides(rows, a.shape, tb.index(blk0 + j) * kBn)))
+          ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
+        if (j == 0) ok = ok && tc_wait_warp(bars, &bars.o_free, (pc & 1) ^ 1);
+        ok = ok && tc_wait_warp(bars, &bars.p_full[b], ((c + j) >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t v0 = v_lo + iv % ST * (C::kTile >> 4), p0 = p_lo + b * (kPBytes >> 4);
+        if (one) {
 #pragma unroll
           for (int k = 0; k < kBn / 16; ++k)
-            tc_mma_ss(tmem + 2 * N, dv + (uint64_t)(k * 2048 >> 4), dp + (uint64_t)(k * 2048 >> 4),
-                      kIdO, j > 0 || k > 0);
+            tc_mma_ss(tmem + 2 * N, v0 + (k * 2048 >> 4), p0 + (k * 2048 >> 4), kIdO,
+                      j > 0 || k > 0);
           tc_commit(&bars.o_full[b]);
           tc_commit(&bars.empty[iv % ST]);
         }
-        if (!ok) break;
-        c += blocks;
-        n += 2 * blocks;
       }
+      if (!ok) break;
+      c += blocks;
+      n += 2 * blocks;
     }
   } else if (warp >= W0 + 2) {
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
-      ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+      ok = bars.queue.wait(bars, pc);
       if (!ok) break;
       TcPiece &p = bars.queue.at(pc);
       if (p.blk1 < 0) break;
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
     uint32_t c = 0;
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
-      ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+      ok = bars.queue.wait(bars, pc);
       if (keys_any(grp, !ok)) break;
       const TcPiece &w = bars.queue.at(pc);
       if (w.blk1 < 0) break;

@@ -130,93 +130,101 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ok) bars.queue.end(bars, pieces);
       }
     } else if (warp == 9) {
-      if (lane == 0) {
-        uint32_t n = 0, c[2] = {0, 0}, used[2] = {0, 0};
-        bool ok = true;
-        constexpr uint32_t kIdS = mma_idesc(128, kBn, false, false);
-        constexpr uint32_t kIdO = mma_idesc(128, D, false, true);
-        auto stage = [&](uint32_t i) { return smem_addr(ring + i % ST * C::kTile); };
-        auto wait_full = [&](uint32_t i) {
-          ok = ok && tc_wait(bars, &bars.full[i % ST], (i / ST) & 1);
-        };
-        // S = Q K^T of stream s with the key block at ring position i
-        auto qk = [&](int s, uint32_t i) {
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t dq = smem_desc(smem_addr(sq + s * C::kQTile), 16, 1024);
-          const uint64_t dk = smem_desc(stage(i), 16, 1024);
+      const bool one = elect_one();
+      uint32_t n = 0, c[2] = {0, 0}, used[2] = {0, 0};
+      bool ok = true;
+      constexpr uint32_t kIdS = mma_idesc(128, kBn, false, false);
+      constexpr uint32_t kIdO = mma_idesc(128, D, false, true);
+      const uint32_t q_lo = desc_lo(smem_addr(sq), 16);
+      const uint32_t k_lo = desc_lo(smem_addr(ring), 16), v_lo = desc_lo(smem_addr(ring), kBn * 128);
+      auto wait_full = [&](uint32_t i) {
+        ok = ok && tc_wait_warp(bars, &bars.full[i % ST], (i / ST) & 1);
+      };
+      // S = Q K^T of stream s with the key block at ring position i
+      auto qk = [&](int s, uint32_t i) {
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t q = q_lo + s * (C::kQTile >> 4), k0 = k_lo + i % ST * (C::kTile >> 4);
+        if (one) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint64_t at = (uint64_t)(((k / 4) * (128 * 128) + (k % 4) * 32) >> 4);
-            tc_mma_ss(tmem + s * 128, dq + at, dk + at, kIdS, k > 0);
+            const uint32_t at = ((k / 4) * (128 * 128) + (k % 4) * 32) >> 4;
+            tc_mma_ss(tmem + s * 128, q + at, k0 + at, kIdS, k > 0);
           }
           tc_commit(&bars.s_full[s]);
-        };
-        // O += P V of stream s with the value block at ring position i
-        auto pv = [&](int s, uint32_t i, bool add) {
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t dv = smem_desc(stage(i), kBn * 128, 1024);
+        }
+      };
+      // O += P V of stream s with the value block at ring position i
+      auto pv = [&](int s, uint32_t i, bool add) {
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t v0 = v_lo + i % ST * (C::kTile >> 4);
+        if (one) {
 #pragma unroll
           for (int k = 0; k < kBn / 16; ++k)
-            tc_mma_ts(tmem + kColO + s * D, tmem + s * 128 + k * 8, dv + (uint64_t)(k * 2048 >> 4),
-                      kIdO, add || k > 0);
-        };
-        for (uint32_t pc = 0;; ++pc) {
-          ok = bars.queue.wait(bars, pc);
-          if (!ok) break;
-          const TcPiece &p = bars.queue.at(pc);
-          const int blk0 = p.blk0, blocks = p.blk1 - blk0;
-          if (p.blk1 < 0) break;
-          const TileRows rows = p.rows;
-          const TileBlocks tb = p.blocks;
-          const bool two = p.tokens > tpt;
-          bars.queue.done(pc);
-          ok = tc_wait(bars, &bars.q_full, pc & 1);
-          wait_full(n);
-          qk(0, n);
-          if (two) qk(1, n);
-          if (!ok) break;
-          tc_commit(&bars.empty[n % ST]);
-          if (blocks == 1) tc_commit(&bars.q_empty);
-          for (int j = 0; ok && j < blocks; ++j) {
-            const bool more = j + 1 < blocks;
-            const uint32_t iv = n + 2 * j + 1, ik = iv + 1;
-            wait_full(iv);
-            if (block_hides(rows, a.shape, tb.index(blk0 + j) * kBn))
-              ok = ok && tc_wait(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-#pragma unroll 1
-            for (int s = 0; s < (two ? 2 : 1); ++s) {
-              if (j == 0) {
-                ok = ok && tc_wait(bars, &bars.o_free[s], (used[s] & 1) ^ 1);
-                ++used[s];
-              }
-              ok = ok && tc_wait(bars, &bars.p_full[s], c[s] & 1);
-              ++c[s];
-              pv(s, iv, j > 0);
-              if (more) {
-                if (s == 0) wait_full(ik);
-                qk(s, ik);
-              } else if (ok) {
-                tc_commit(&bars.o_full[s]);
-              }
+            tc_mma_ts(tmem + kColO + s * D, tmem + s * 128 + k * 8, v0 + (k * 2048 >> 4), kIdO,
+                      add || k > 0);
+        }
+      };
+      auto commit = [&](uint64_t *bar) {
+        if (one) tc_commit(bar);
+      };
+      for (uint32_t pc = 0;; ++pc) {
+        ok = bars.queue.wait(bars, pc);
+        if (!ok) break;
+        const TcPiece &p = bars.queue.at(pc);
+        const int blk0 = uniform(p.blk0), blocks = uniform(p.blk1) - blk0;
+        if (uniform(p.blk1) < 0) break;
+        const TileRows rows = p.rows;
+        const TileBlocks tb = p.blocks;
+        const bool two = uniform(p.tokens) > tpt;
+        __syncwarp();
+        if (one) bars.queue.done(pc);
+        ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
+        wait_full(n);
+        qk(0, n);
+        if (two) qk(1, n);
+        if (!ok) break;
+        commit(&bars.empty[n % ST]);
+        if (blocks == 1) commit(&bars.q_empty);
+        for (int j = 0; ok && j < blocks; ++j) {
+          const bool more = j + 1 < blocks;
+          const uint32_t iv = n + 2 * j + 1, ik = iv + 1;
+          wait_full(iv);
+          if (uniform(block_hides(rows, a.shape, tb.index(blk0 + j) * kBn)))
+            ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (s == 1 && !two) break;
+            if (j == 0) {
+              ok = ok && tc_wait_warp(bars, &bars.o_free[s], (used[s] & 1) ^ 1);
+              ++used[s];
             }
-            if (!ok) break;
-            tc_commit(&bars.empty[iv % ST]);
+            ok = ok && tc_wait_warp(bars, &bars.p_full[s], c[s] & 1);
+            ++c[s];
+            pv(s, iv, j > 0);
             if (more) {
-              tc_commit(&bars.empty[ik % ST]);
-              if (j + 2 == blocks) tc_commit(&bars.q_empty);
+              if (s == 0) wait_full(ik);
+              qk(s, ik);
+            } else if (ok) {
+              commit(&bars.o_full[s]);
             }
           }
           if (!ok) break;
-          n += 2 * blocks;
+          commit(&bars.empty[iv % ST]);
+          if (more) {
+            commit(&bars.empty[ik % ST]);
+            if (j + 2 == blocks) commit(&bars.q_empty);
+          }
         }
+        if (!ok) break;
+        n += 2 * blocks;
       }
     } else {
       uint32_t n = 0;
       bool ok = true;
       for (uint32_t pc = 0; ok; ++pc) {
-        ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+        ok = bars.queue.wait(bars, pc);
         if (!ok) break;
         TcPiece &p = bars.queue.at(pc);
         if (p.blk1 < 0) break;
@@ -250,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t c = 0, mine = 0;                 // blocks and pieces of this stream so far
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
-      ok = __all_sync(0xffffffffu, bars.queue.wait(bars, pc));
+      ok = bars.queue.wait(bars, pc);
       if (!ok) break;
       const TcPiece &p = bars.queue.at(pc);
       if (p.blk1 < 0) break;

@@ -56,6 +56,15 @@ __device__ __forceinline__ bool tc_wait(B &b, uint64_t *bar, uint32_t parity) {
   }
 }
 
+// the same for a converged warp: one answer, known to be the same in every lane
+template <typename B>
+__device__ __forceinline__ bool tc_wait_warp(B &b, uint64_t *bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, tc_wait(b, bar, parity));
+}
+
+// a value that is the same in every lane, as the compiler can know it
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // an element of a bf16 pair that is infinite or NaN: bit 15 or 31 of the result
 __device__ __forceinline__ uint32_t not_numbers(uint32_t w) {
   return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
@@ -134,8 +143,8 @@ struct TcQueue {
     mbar_arrive(&full[i % kPieces]);
   }
   template <typename B>
-  __device__ __forceinline__ bool wait(B &b, uint32_t i) {
-    return tc_wait(b, &full[i % kPieces], (i / kPieces) & 1);
+  __device__ __forceinline__ bool wait(B &b, uint32_t i) {  // whole warp
+    return tc_wait_warp(b, &full[i % kPieces], (i / kPieces) & 1);
   }
   __device__ __forceinline__ TcPiece &at(uint32_t i) { return piece[i % kPieces]; }
   __device__ __forceinline__ void done(uint32_t i) { mbar_arrive(&empty[i % kPieces]); }

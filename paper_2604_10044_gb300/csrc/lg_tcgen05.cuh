@@ -41,13 +41,26 @@ __device__ __forceinline__ void tc_commit(uint64_t *bar) {
                : "memory");
 }
 
-// Descriptor of a bf16 operand in shared memory in 128-byte-swizzled rows.  For rows of 64
-// consecutive contraction elements (K-major): `sbo` bytes from 8 rows to the next 8.  For rows of
-// 64 consecutive row/column elements (MN-major): `lbo` bytes from one 64 of them to the next, `sbo`
-// bytes from 8 contraction steps to the next 8.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lbo >> 4) << 16 |
-         (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// Descriptor of a bf16 operand in shared memory in 128-byte-swizzled rows, as its two halves (the
+// upper one is the same for every operand here, and moving along an operand adds to the lower one).
+// For rows of 64 consecutive contraction elements (K-major): 1024 bytes from 8 rows to the next 8.
+// For rows of 64 consecutive row/column elements (MN-major): `lbo` bytes from one 64 of them to the
+// next, 1024 bytes from 8 contraction steps to the next 8.
+constexpr uint32_t kDescHi = 1024u >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) {
+  return ((addr & 0x3ffff) >> 4) | (lbo >> 4) << 16;
+}
+
+// One lane of a converged warp, always the same.  The products are issued by a whole warp's code of
+// which one lane executes the instructions: their operands live in uniform registers, and only for
+// code that all lanes run does the compiler keep them there (issued from a branch of one lane, 16
+// products took 1600 to 2400 cycles to issue; they run for 1024).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(r));
+  return r != 0;
 }
 
 // Instruction descriptor: bf16 x bf16 -> fp32, each operand K-major or MN-major
@@ -57,23 +70,23 @@ __host__ __device__ constexpr uint32_t mma_idesc(int m, int n, bool a_mn_major, 
          (uint32_t)(m >> 4) << 24;
 }
 
-// d (tensor memory) = [d +] A B, A in shared memory
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+// d (tensor memory) = [d +] A B, A in shared memory (lower halves of the descriptors)
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
                                           bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 da, db;\n setp.ne.u32 p, %4, 0;\n mov.b64 da, {%1, %5};\n"
+      " mov.b64 db, {%2, %5};\n tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHi)
       : "memory");
 }
 
 // the same with A in tensor memory (two bf16 a column)
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
                                           bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 db;\n setp.ne.u32 p, %4, 0;\n mov.b64 db, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHi)
       : "memory");
 }
 
