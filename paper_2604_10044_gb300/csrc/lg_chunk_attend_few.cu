@@ -209,8 +209,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       const TcPiece &p = bars.queue.at(pc);
       const int blk0 = uniform(p.blk0), blocks = uniform(p.blk1) - blk0;
       if (uniform(p.blk1) < 0) break;
-      const TileRows rows = p.rows;
-      const TileBlocks tb = p.blocks;
+      const int open0 = uniform(p.open0) - blk0, open1 = uniform(p.open1) - blk0;
       __syncwarp();
       if (one) bars.queue.done(pc);
       ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
@@ -234,9 +233,10 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (int j = 0; ok && j < blocks; ++j) {
         if (j + 1 < blocks) scores(j + 1);
         const uint32_t iv = n + (j + 1 < blocks ? 2 * j + 2 : 2 * j + 1), b = (c + j) & 1;
-        wait_full(iv);
-        if (uniform(block_hides(rows, a.shape, tb.index(blk0 + j) * kBn)))
+        if (j < open0 || j >= open1)
           ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
+        else
+          wait_full(iv);
         if (j == 0) ok = ok && tc_wait_warp(bars, &bars.o_free, (pc & 1) ^ 1);
         ok = ok && tc_wait_warp(bars, &bars.p_full[b], ((c + j) >> 1) & 1);
         if (!ok) break;
@@ -269,8 +269,8 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         const int j = i == 2 * blocks - 1 ? blocks - 1 : i >= 2 && !(i & 1) ? i / 2 - 1 : -1;
         ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.full[n % ST], (n / ST) & 1));
         if (!ok) break;
-        const int i0 = j < 0 ? 0 : p.blocks.index(p.blk0 + j) * kBn;
-        if (j >= 0 && block_hides(p.rows, a.shape, i0)) {
+        if (j >= 0 && p.hides(p.blk0 + j)) {
+          const int i0 = p.blocks.index(p.blk0 + j) * kBn;
           if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64)) p.bad = 1;
           fence_proxy_async_smem();
           __syncwarp();
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (int blk = w.blk0; blk < w.blk1; ++blk, ++c) {
         const uint32_t b = c & 1;
         const int i0 = w.blocks.index(blk) * kBn;
-        const bool hides = block_hides(w.rows, a.shape, i0);
+        const bool hides = w.hides(blk);
         const uint64_t see = hides ? columns_seeing(w.rows, a.shape, a.g, i0 + key) >> q0 : ~0ull;
         ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[b], (c >> 1) & 1));
         // a role that gave up is seen by every key warp before the barriers below
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       if (w.bad) {  // what was cleared, for the queries that see it
         for (int blk = w.blk0; blk < w.blk1; ++blk) {
           const int i0 = w.blocks.index(blk) * kBn;
-          if (!block_hides(w.rows, a.shape, i0)) continue;
+          if (!w.hides(blk)) continue;
           for (int i = i0; i < i0 + kBn && i < w.n; ++i) {
             const float z = __bfloat162float(
                 ((const __nv_bfloat16 *)a.V)[(w.row0 + i) * D + key % D]);

@@ -11,8 +11,8 @@
 // lose nothing in bf16 or in the fp32 sums.  P is rounded to bf16 (half a step, 2^-8 of a weight at
 // most: the precision of the values it multiplies); l sums the unrounded weights in fp32.
 //
-// Warps: 0-3 and 4-7 the rows of streams 0 and 1; 8 walks along the work and copies (TMA), 9 issues the products, 10 and 11
-// clear what is not a number from the values of blocks in which some row is hidden from some query
+// Warps: 0-3 and 4-7 the rows of streams 0 and 1; 8 walks along the work and copies (TMA), 9 and 10
+// issue the products of a stream each, 11 clears what is not a number from the values of blocks in which some row is hidden from some query
 // (0 x NaN would reach the hidden one's sums).  Those values are added again, at the end, for the
 // queries that see them.
 #include "lg_chunk_tc.cuh"
@@ -42,6 +42,7 @@ struct TcBars {
   uint64_t q_full, q_empty;
   uint64_t s_full[2], p_full[2];     // scores ready, weights ready
   uint64_t o_full[2], o_free[2];     // sums ready, sums read
+  uint64_t turn[2];                  // the stream's products are next
   TcQueue queue;
   uint32_t tmem;
   volatile int give_up;              // a bounded wait ran out
@@ -64,18 +65,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
       mbar_init(&bars.full[i], 1);
-      mbar_init(&bars.empty[i], 3);  // the products and both clearing warps
-      mbar_init(&bars.fixed[i], 2);
+      mbar_init(&bars.empty[i], 3);  // both streams' products and the clearing warp
+      mbar_init(&bars.fixed[i], 1);
     }
     mbar_init(&bars.q_full, 1);
-    mbar_init(&bars.q_empty, 1);
+    mbar_init(&bars.q_empty, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.s_full[i], 1);
       mbar_init(&bars.p_full[i], 4);
       mbar_init(&bars.o_full[i], 1);
       mbar_init(&bars.o_free[i], 4);
+      mbar_init(&bars.turn[i], 1);
     }
-    bars.queue.init(11);               // the products, two clearing warps, eight warps of rows
+    bars.queue.init(11);               // the products' two warps, the clearing one, eight of rows
     bars.give_up = 0;
     mbar_fence_init();
   }
@@ -129,93 +131,93 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok) bars.queue.end(bars, pieces);
       }
-    } else if (warp == 9) {
+    } else if (warp <= 10) {
+      // One warp a stream: what surrounds the products (waits, commits) takes as long as the products
+      // of one stream, and one warp for both kept the tensor cores waiting (56 % busy).  They take
+      // turns, a stream's sums and next scores at a time: products that both have in flight finish
+      // together, then both streams form weights and the tensor cores stand still.
+      const int s = warp - 9;
       const bool one = elect_one();
-      uint32_t n = 0, c[2] = {0, 0}, used[2] = {0, 0};
+      uint32_t n = 0, c = 0, mine = 0;  // ring position; blocks and pieces of the stream
+      uint32_t turns = 0;               // blocks that both streams had
       bool ok = true;
       constexpr uint32_t kIdS = mma_idesc(128, kBn, false, false);
       constexpr uint32_t kIdO = mma_idesc(128, D, false, true);
-      const uint32_t q_lo = desc_lo(smem_addr(sq), 16);
+      const uint32_t ts = tmem + s * 128, to = tmem + kColO + s * D;
+      const uint32_t q_lo = desc_lo(smem_addr(sq + s * C::kQTile), 16);
       const uint32_t k_lo = desc_lo(smem_addr(ring), 16), v_lo = desc_lo(smem_addr(ring), kBn * 128);
       auto wait_full = [&](uint32_t i) {
         ok = ok && tc_wait_warp(bars, &bars.full[i % ST], (i / ST) & 1);
       };
-      // S = Q K^T of stream s with the key block at ring position i
-      auto qk = [&](int s, uint32_t i) {
-        if (!ok) return;
-        tc_fence_after();
-        const uint32_t q = q_lo + s * (C::kQTile >> 4), k0 = k_lo + i % ST * (C::kTile >> 4);
+      // S = Q K^T with the key block at ring position i (which has arrived)
+      auto qk = [&](uint32_t i, bool last) {
+        const uint32_t k0 = k_lo + i % ST * (C::kTile >> 4);
         if (one) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t at = ((k / 4) * (128 * 128) + (k % 4) * 32) >> 4;
-            tc_mma_ss(tmem + s * 128, q + at, k0 + at, kIdS, k > 0);
+            tc_mma_ss(ts, q_lo + at, k0 + at, kIdS, k > 0);
           }
           tc_commit(&bars.s_full[s]);
+          tc_commit(&bars.empty[i % ST]);
+          if (last) tc_commit(&bars.q_empty);
         }
-      };
-      // O += P V of stream s with the value block at ring position i
-      auto pv = [&](int s, uint32_t i, bool add) {
-        if (!ok) return;
-        tc_fence_after();
-        const uint32_t v0 = v_lo + i % ST * (C::kTile >> 4);
-        if (one) {
-#pragma unroll
-          for (int k = 0; k < kBn / 16; ++k)
-            tc_mma_ts(tmem + kColO + s * D, tmem + s * 128 + k * 8, v0 + (k * 2048 >> 4), kIdO,
-                      add || k > 0);
-        }
-      };
-      auto commit = [&](uint64_t *bar) {
-        if (one) tc_commit(bar);
       };
       for (uint32_t pc = 0;; ++pc) {
         ok = bars.queue.wait(bars, pc);
         if (!ok) break;
         const TcPiece &p = bars.queue.at(pc);
-        const int blk0 = uniform(p.blk0), blocks = uniform(p.blk1) - blk0;
-        if (uniform(p.blk1) < 0) break;
-        const TileRows rows = p.rows;
-        const TileBlocks tb = p.blocks;
-        const bool two = uniform(p.tokens) > tpt;
+        const int blk1 = uniform(p.blk1);
+        if (blk1 < 0) break;
+        const int blocks = blk1 - uniform(p.blk0);
+        const int open0 = uniform(p.open0 - p.blk0), open1 = uniform(p.open1 - p.blk0);
+        const bool two = uniform(p.tokens) > tpt, active = s == 0 || two;
         __syncwarp();
         if (one) bars.queue.done(pc);
-        ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
-        wait_full(n);
-        qk(0, n);
-        if (two) qk(1, n);
-        if (!ok) break;
-        commit(&bars.empty[n % ST]);
-        if (blocks == 1) commit(&bars.q_empty);
-        for (int j = 0; ok && j < blocks; ++j) {
-          const bool more = j + 1 < blocks;
-          const uint32_t iv = n + 2 * j + 1, ik = iv + 1;
-          wait_full(iv);
-          if (uniform(block_hides(rows, a.shape, tb.index(blk0 + j) * kBn)))
-            ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (s == 1 && !two) break;
-            if (j == 0) {
-              ok = ok && tc_wait_warp(bars, &bars.o_free[s], (used[s] & 1) ^ 1);
-              ++used[s];
-            }
-            ok = ok && tc_wait_warp(bars, &bars.p_full[s], c[s] & 1);
-            ++c[s];
-            pv(s, iv, j > 0);
-            if (more) {
-              if (s == 0) wait_full(ik);
-              qk(s, ik);
-            } else if (ok) {
-              commit(&bars.o_full[s]);
-            }
+        if (!active) {  // the other stream's blocks pass
+          for (int i = 0; ok && i < 2 * blocks; ++i, ++n) {
+            wait_full(n);
+            if (ok && one) mbar_arrive(&bars.empty[n % ST]);
           }
           if (!ok) break;
-          commit(&bars.empty[iv % ST]);
-          if (more) {
-            commit(&bars.empty[ik % ST]);
-            if (j + 2 == blocks) commit(&bars.q_empty);
+          if (one) mbar_arrive(&bars.q_empty);
+          continue;
+        }
+        ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
+        wait_full(n);
+        if (!ok) break;
+        tc_fence_after();
+        qk(n, blocks == 1);
+        ok = tc_wait_warp(bars, &bars.o_free[s], (mine & 1) ^ 1);
+        ++mine;
+        for (int j = 0; ok && j < blocks; ++j, ++c) {
+          const uint32_t iv = n + 2 * j + 1;
+          if (j < open0 || j >= open1)
+            ok = tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
+          else
+            wait_full(iv);
+          if (j + 1 < blocks) wait_full(iv + 1);
+          ok = ok && tc_wait_warp(bars, &bars.p_full[s], c & 1);
+          if (two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));
+          if (!ok) break;
+          tc_fence_after();
+          // O += P V
+          const uint32_t v0 = v_lo + iv % ST * (C::kTile >> 4);
+          if (one) {
+#pragma unroll
+            for (int k = 0; k < kBn / 16; ++k)
+              tc_mma_ts(to, ts + k * 8, v0 + (k * 2048 >> 4), kIdO, j > 0 || k > 0);
           }
+          if (j + 1 < blocks) {
+            qk(iv + 1, j + 2 == blocks);
+          } else if (one) {
+            tc_commit(&bars.o_full[s]);
+          }
+          if (two) {
+            if (one) mbar_arrive(&bars.turn[s ^ 1]);
+            ++turns;
+          }
+          if (one) tc_commit(&bars.empty[iv % ST]);
         }
         if (!ok) break;
         n += 2 * blocks;
@@ -233,9 +235,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.full[n % ST], (n / ST) & 1));
           if (!ok) break;
           // keys and values in turn
-          const int i0 = p.blocks.index(p.blk0 + (i >> 1)) * kBn;
-          if ((i & 1) && block_hides(p.rows, a.shape, i0)) {
-            if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 320, 64)) p.bad = 1;
+          if ((i & 1) && p.hides(p.blk0 + (i >> 1))) {
+            const int i0 = p.blocks.index(p.blk0 + (i >> 1)) * kBn;
+            if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, lane, 32)) p.bad = 1;
             fence_proxy_async_smem();
             __syncwarp();
           }
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int blk0 = p.blk0, blk1 = p.blk1;
         for (int blk = blk0; blk < blk1; ++blk, ++c) {
           const int i0 = p.blocks.index(blk) * kBn;
-          const bool hides = block_hides(p.rows, a.shape, i0);
+          const bool hides = p.hides(blk);
           ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[s], c & 1));
           if (!ok) break;
           if (!idle) {
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (bad) {  // what was cleared and this query sees
                 for (int blk = blk0; blk < blk1; ++blk) {
                   const int i0 = p.blocks.index(blk) * kBn;
-                  if (!block_hides(p.rows, a.shape, i0)) continue;
+                  if (!p.hides(blk)) continue;
                   for (int i = i0; i < i0 + kBn && i < p.n; ++i) {
                     if (!row_sees(p.rows, a.shape, qrow, i)) continue;
                     const __nv_bfloat16 *vr = (const __nv_bfloat16 *)a.V + (p.row0 + i) * D + x;

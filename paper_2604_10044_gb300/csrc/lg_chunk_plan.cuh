@@ -120,6 +120,18 @@ __host__ __device__ __forceinline__ TileBlocks tile_blocks(const TileRows &r, in
   return b;
 }
 
+// The blocks, by their number among the tile's, that hide no row from any of its queries and hold
+// none past the rows: the run [open0, open1) between the window's (hidden rows end at last - window)
+// and the queries' own rows.  (A block with sinks may hide nothing either; it counts as hiding.)
+__host__ __device__ __forceinline__ void open_blocks(const TileRows &r, const ChunkShape &s,
+                                                     const TileBlocks &b, int &open0, int &open1) {
+  const int64_t bn = (int64_t)1 << s.bn2;
+  const int64_t from = s.window ? plan_max(0, (int64_t)r.last - s.window + 1) : 0;
+  const int lo = (int)((from + bn - 1) >> s.bn2), hi = (int)(((int64_t)r.first + 1) >> s.bn2);
+  open0 = lo - b.skip;
+  open1 = hi > lo ? hi - b.skip : open0;
+}
+
 // cost units of a CTA of G: CTA c takes [c step, (c + 1) step) of the line, up to its end W
 __host__ __device__ __forceinline__ int64_t range_step(int64_t W, int G) {
   return plan_div(W + G - 1, G);

@@ -22,14 +22,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Some row of the block from row i0 is hidden from some query of the item (or lies past the rows).
-__device__ __forceinline__ bool block_hides(const TileRows &r, const ChunkShape &s, int i0) {
-  if (i0 + kTcBn - 1 > r.first) return true;
-  if (s.window == 0) return false;
-  const int64_t a = plan_max(i0, s.sink);
-  return a <= plan_min((int64_t)i0 + kTcBn - 1, (int64_t)r.last - s.window);
-}
-
 // bit e: the query at row qrow sees row i0 + e, e < 32
 __device__ __forceinline__ uint32_t rows_seen(const ChunkShape &s, int qrow, int i0) {
   auto below = [](int64_t n) {  // bits 0 .. n - 1
@@ -99,11 +91,14 @@ struct TcPiece {
   TileRows rows;
   TileBlocks blocks;
   int blk0, blk1;         // key blocks; blk1 < 0: no more pieces
+  int open0, open1;       // of them, the last run that hides no row: [open0, open1)
   int n;                  // rows of the sequence
   int tok0, tokens, kvh;  // token rows [tok0, tok0 + tokens), kv-head
   int slot;               // of the partial result, -1: the piece is its whole item
   volatile int bad;       // something that is not a number was cleared
   int64_t row0;           // first cache row
+
+  __device__ __forceinline__ bool hides(int blk) const { return blk < open0 || blk >= open1; }
 };
 constexpr int kPieces = 4;
 
@@ -126,6 +121,7 @@ struct TcQueue {
     p.blocks = w.blocks;
     p.blk0 = w.blk0;
     p.blk1 = w.blk1;
+    open_blocks(w.rows, a.shape, w.blocks, p.open0, p.open1);
     p.n = w.q.n;
     p.tok0 = w.off + w.t * a.shape.tok;
     p.tokens = w.tokens(a);

@@ -59,6 +59,18 @@ int main() {
       }
       for (int i = 0; i < b.count; ++i) CHECK(got.insert(b.index(i)).second);
       CHECK(want == got);
+      // an open block hides no row of its own from any query; others do, or hold sinks
+      int o0, o1;
+      open_blocks(r, s, b, o0, o1);
+      CHECK(o0 >= 0 && o1 >= o0);
+      for (int i = 0; i < b.count; ++i) {
+        const int64_t i0 = (int64_t)b.index(i) << s.bn2, i1 = i0 + ((int64_t)1 << s.bn2) - 1;
+        bool hides = i1 > r.first;
+        if (s.window)
+          for (int64_t x = i0; x <= i1 && x <= (int64_t)r.last - s.window; ++x) hides |= x >= s.sink;
+        if (i >= o0 && i < o1) CHECK(!hides);
+        else CHECK(hides || i0 < s.sink);
+      }
       sum += c;
     }
     CHECK(tiles_cost(q, s, tiles) == sum);
