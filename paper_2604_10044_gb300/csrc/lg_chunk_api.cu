@@ -90,7 +90,7 @@ lg_status attend_shape(const lg_cache *c, const lg_chunk *ch, int H_q, int max_l
 }
 
 size_t part_bytes(const lg::ChunkGrid &g, int d) {
-  const size_t n = (size_t)g.ctas * 2 * g.rows * (d + 2) * sizeof(float);
+  const size_t n = (size_t)g.ctas * (2 * g.rows * (d + 2) * sizeof(float) + sizeof(lg::ChunkCut));
   return (n + 255) / 256 * 256;
 }
 

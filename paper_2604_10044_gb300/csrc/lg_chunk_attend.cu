@@ -47,9 +47,11 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
   const int H_q = a.H_kv * a.g;
   pdl_enter();
   ChunkShare sh;
-  if (!chunk_share<BM == 16>(a, blockIdx.x, gridDim.x, sh)) return;
   ChunkWalk<BM == 16> w;
-  for (w.start(a, sh); !w.done(); w.next(a)) {
+  const bool work = chunk_share<BM == 16>(a, blockIdx.x, gridDim.x, sh);
+  if (work) w.start(a, sh);
+  if (tid == 0) put_cut(a, D, gridDim.x, blockIdx.x, work, sh, w);
+  for (; work && !w.done(); w.next(a)) {
     if (w.blk0 == w.blk1) continue;
     const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
     const int tok0 = w.off + w.t * a.shape.tok;
@@ -188,35 +190,21 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
   }
 }
 
-// Merge of the item that the start of CTA c's range cuts, c = blockIdx.x + 1, by the first cut of
-// an item: pieces of CTAs c - 1, c, ... in order, a warp per row, blockIdx.y of gridDim.y in turn.
-//
-// Which pieces there are follows from the lengths, and is found before the dependency wait: this
-// kernel can start once every CTA of the attention kernel is past its own wait, so everything that
-// wrote the lengths is complete by then, and the attention kernel leaves them alone.
-template <typename T, int D, bool ONE>
+// Merge of the item that CTA c's start is the first to cut, c = blockIdx.x + 1, from the parts of
+// CTAs c - 1, c, ...: a warp per row, 32 parts at a time, a lane each for maximum and normaliser.
+template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
   constexpr int V = D / 32;  // elements a lane
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  ChunkShare sh;
-  ChunkWalk<ONE> w;
-  const bool work = chunk_share<ONE>(a, c, G, sh);
-  bool mine = false;
-  if (work) {
-    w.start(a, sh);
-    // the bound falls inside the item, and no earlier one does
-    mine = w.x < sh.y0 && sh.y0 - sh.step <= w.x;
-  }
   pdl_enter();
-  if (!mine || __any_sync(0xffffffffu, lane == 0 && status_bad(a.status))) return;
-  int last = c;  // the last CTA that has a part of the item
-  for (int64_t y = sh.y0 + sh.step; y < w.x + w.cost; y += sh.step) ++last;
-  const int used = w.tokens(a) * a.g, tok0 = w.off + w.t * a.shape.tok, H_q = a.H_kv * a.g;
+  const ChunkCut w = *cut_at(a, D, G, c);
+  if (__any_sync(0xffffffffu, lane == 0 && status_bad(a.status))) return;
+  if (w.parts == 0) return;
+  const int H_q = a.H_kv * a.g, last = c - 2 + w.parts;
   auto cut = [&](int p) {
-    return cut_block(p * sh.step - w.x, w.cost, w.blocks.count, a.shape.bn2);
+    return cut_block(w.in + (p - c) * w.step, w.cost, w.blocks, a.shape.bn2);
   };
-  // 32 pieces at a time, a lane each: whether it has blocks, its maximum and normaliser
-  for (int r = blockIdx.y * (kThreads / 32) + warp; r < used; r += gridDim.y * (kThreads / 32)) {
+  for (int r = blockIdx.y * (kThreads / 32) + warp; r < w.used; r += gridDim.y * (kThreads / 32)) {
     float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) o[k] = 0.f;
@@ -226,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
       const int b0 = p <= last ? cut(p) : 0, b1 = p <= last ? cut(p + 1) : 0;
       const bool some = b0 < b1;
       // one piece has every block: its CTA wrote the result
-      whole = __any_sync(0xffffffffu, some && b0 == 0 && b1 == w.blocks.count);
+      whole = __any_sync(0xffffffffu, some && b0 == 0 && b1 == w.blocks);
       if (whole) break;
       float2 ml = make_float2(-INFINITY, 0.f);
       if (some) ml = *part_ml(a, D, G, p, p == c - 1 ? 1 : 0, r);
@@ -254,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
     }
     if (whole) continue;
     const float inv = l != 0.f ? 1.f / l : 0.f;
-    const int64_t dst = ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D;
+    const int64_t dst = ((int64_t)(w.tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D;
 #pragma unroll
     for (int k = 0; k < V; ++k) Elem<T>::store(a.out, dst + lane + 32 * k, o[k] * inv);
   }
@@ -271,12 +259,9 @@ cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
 
 template <typename T, int D>
 cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
-  const int rows = kThreads / 32;  // a CTA's at once
-  const dim3 grid(G - 1, a.rows <= 4 * rows ? (a.rows + rows - 1) / rows : 4);
-  if (a.max_new <= a.shape.tok)
-    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, true>, grid, kThreads, 0, s, a, G));
-  else
-    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, false>, grid, kThreads, 0, s, a, G));
+  const int rows = kThreads / 32;  // a CTA's at once; two rows a warp at most
+  const dim3 grid(G - 1, a.rows <= 16 * rows ? (a.rows + rows - 1) / rows : 16);
+  LG_TRY(launch_pdl(chunk_merge_kernel<T, D>, grid, kThreads, 0, s, a, G));
   return cudaGetLastError();
 }
 

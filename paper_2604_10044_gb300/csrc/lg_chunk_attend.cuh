@@ -19,7 +19,8 @@ struct ChunkAttendArgs {
   const int32_t *len;      // [batch]
   const int32_t *off;      // [batch + 1]
   int32_t *status;
-  float *part;             // [2 G][rows][d] partial sums, then [2 G][rows][2] maxima and normalisers
+  float *part;             // [2 G][rows][d] partial sums, [2 G][rows][2] maxima and normalisers,
+                           // then [G] ChunkCut
   int64_t S_total;
   int64_t cache_rows;      // L * H_kv * S_total
   int layer, batch, H_kv, g, T, max_new, max_len;
@@ -41,7 +42,6 @@ struct ChunkShare {
 // The share of CTA `cta` of G, which may be empty; false when it starts at the end of the line, the
 // device status is set or a length is out of its bounds (recorded).  Every lane of a warp calls it;
 // a batch of at most 32 is read once, in one round trip.  ONE: no sequence has more than one tile.
-// The merge calls it before its dependency wait (chunk_merge_kernel), hence the loads past L1.
 template <bool ONE>
 __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, int G,
                                             ChunkShare &sh) {
@@ -53,10 +53,10 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
   auto load = [&](int b) {  // a lane's sequence and the cost of one kv-head of it
     c = 0;
     if (b >= a.batch) return;
-    off = __ldcg(a.off + b);
-    const int end = __ldcg(a.off + b + 1);
-    q = ChunkSeq{__ldcg(a.len + b), end - off};
-    slot = __ldcg(a.seq_off + b);
+    off = a.off[b];
+    const int end = a.off[b + 1];
+    q = ChunkSeq{a.len[b], end - off};
+    slot = a.seq_off[b];
     if (q.n < 0 || q.n > a.max_len || q.m < 0 || q.m > a.max_new || q.m > q.n || off < 0 ||
         end > a.T)
       bad = true;
@@ -185,6 +185,38 @@ __device__ __forceinline__ float *part_row(const ChunkAttendArgs &a, int d, int 
 __device__ __forceinline__ float2 *part_ml(const ChunkAttendArgs &a, int d, int G, int cta,
                                            int slot, int r) {
   return (float2 *)(a.part + (int64_t)G * 2 * a.rows * d) + ((int64_t)cta * 2 + slot) * a.rows + r;
+}
+
+// What the merge has to know of the item that a CTA's start cuts, written by that CTA.
+struct ChunkCut {
+  int64_t in, step, cost;  // cost units: of the start in the item, of a CTA, of the item
+  int parts;               // CTAs from the one before on that have a part; 0: nothing to merge
+  int blocks, used, tok0;  // key blocks and query rows of the item, its first token row
+  int kvh, pad;
+};
+
+__device__ __forceinline__ ChunkCut *cut_at(const ChunkAttendArgs &a, int d, int G, int cta) {
+  return (ChunkCut *)(a.part + (int64_t)G * 2 * a.rows * (d + 2)) + cta;
+}
+
+// One thread of every CTA calls it: `work` as chunk_share gave it, w at its start.
+template <bool ONE>
+__device__ __forceinline__ void put_cut(const ChunkAttendArgs &a, int d, int G, int cta, bool work,
+                                        const ChunkShare &sh, const ChunkWalk<ONE> &w) {
+  ChunkCut c = {};
+  // the start falls inside the item, and no earlier one does
+  if (work && w.x < sh.y0 && sh.y0 - sh.step <= w.x) {
+    c.in = sh.y0 - w.x;
+    c.step = sh.step;
+    c.cost = w.cost;
+    c.parts = 2;
+    for (int64_t y = c.in + c.step; y < c.cost; y += c.step) ++c.parts;
+    c.blocks = w.blocks.count;
+    c.used = w.tokens(a) * a.g;
+    c.tok0 = w.off + w.t * a.shape.tok;
+    c.kvh = w.kvh;
+  }
+  *cut_at(a, d, G, cta) = c;
 }
 
 __device__ __forceinline__ bool row_sees(const TileRows &r, const ChunkShape &s, int query_row,

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
 
   if (warp == W0) {
     ChunkShare sh;
-    const bool work = chunk_share<true>(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
+    const bool work = chunk_share<true>(a, blockIdx.x, gridDim.x, sh);
     if (lane == 0) {
       ChunkWalk<true> w;
       uint32_t n = 0, pieces = 0;
@@ -169,6 +169,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         ++n;
       };
       if (work) w.start(a, sh);
+      const ChunkWalk<true> first = w;
       for (; work && ok && !w.done(); w.next(a)) {
         if (w.blk0 == w.blk1) continue;
         const int r0 = (int)w.row0;
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         }
       }
       if (ok) bars.queue.end(bars, pieces);
+      put_cut(a, D, gridDim.x, blockIdx.x, work, sh, first);
     }
   } else if (warp == W0 + 1) {
     const bool one = elect_one();

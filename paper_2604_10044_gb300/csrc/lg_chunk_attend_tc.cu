@@ -40,13 +40,28 @@ struct TcBars {
   uint64_t full[ST], empty[ST];      // ring of key and value blocks
   uint64_t fixed[ST];                // what hidden rows hold is cleared
   uint64_t q_full, q_empty;
-  uint64_t s_full[2], p_full[2];     // scores ready, weights ready
+  uint64_t s_full[2], p_half[2], p_full[2];  // scores ready, half of and all weights ready
   uint64_t o_full[2], o_free[2];     // sums ready, sums read
   uint64_t turn[2];                  // the stream's products are next
   TcQueue queue;
   uint32_t tmem;
   volatile int give_up;              // a bounded wait ran out
 };
+
+// Lanes that differ in bit B of their number exchange: the lower one its b for the upper one's a.
+template <int B>
+__device__ __forceinline__ void swap_pieces(uint4 &a, uint4 &b, int lane) {
+  const bool up = (lane & B) != 0;
+  uint32_t *x = (uint32_t *)&a, *y = (uint32_t *)&b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x[i] : y[i], B);
+    if (up)
+      x[i] = got;
+    else
+      y[i] = got;
+  }
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -72,6 +87,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars.q_empty, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.s_full[i], 1);
+      mbar_init(&bars.p_half[i], 4);
       mbar_init(&bars.p_full[i], 4);
       mbar_init(&bars.o_full[i], 1);
       mbar_init(&bars.o_free[i], 4);
@@ -94,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8) {
       ChunkShare sh;
-      const bool work = chunk_share<false>(a, blockIdx.x, gridDim.x, sh) && sh.y0 < sh.y1;
+      const bool work = chunk_share<false>(a, blockIdx.x, gridDim.x, sh);
       if (lane == 0) {
         ChunkWalk<false> w;
         uint32_t n = 0, pieces = 0;  // ring position, pieces so far
@@ -110,6 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n;
         };
         if (work) w.start(a, sh);
+        put_cut(a, D, gridDim.x, blockIdx.x, work, sh, w);
         for (; work && ok && !w.done(); w.next(a)) {
           if (w.blk0 == w.blk1) continue;
           const int tiles = w.tokens(a) > tpt ? 2 : 1;
@@ -197,17 +214,25 @@ __global__ void __launch_bounds__(kThreads, 1)
           else
             wait_full(iv);
           if (j + 1 < blocks) wait_full(iv + 1);
-          ok = ok && tc_wait_warp(bars, &bars.p_full[s], c & 1);
+          ok = ok && tc_wait_warp(bars, &bars.p_half[s], c & 1);
           if (two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));
           if (!ok) break;
           tc_fence_after();
-          // O += P V
+          // O += P V, the block's first half while the second one's weights are formed
           const uint32_t v0 = v_lo + iv % ST * (C::kTile >> 4);
-          if (one) {
+          auto pv = [&](int k0) {
+            if (one) {
 #pragma unroll
-            for (int k = 0; k < kBn / 16; ++k)
-              tc_mma_ts(to, ts + k * 8, v0 + (k * 2048 >> 4), kIdO, j > 0 || k > 0);
-          }
+              for (int k = 0; k < kBn / 32; ++k)
+                tc_mma_ts(to, ts + (k0 + k) * 8, v0 + (k0 + k) * (2048 >> 4), kIdO,
+                          j > 0 || k0 + k > 0);
+            }
+          };
+          pv(0);
+          ok = tc_wait_warp(bars, &bars.p_full[s], c & 1);
+          if (!ok) break;
+          tc_fence_after();
+          pv(kBn / 32);
           if (j + 1 < blocks) {
             qk(iv + 1, j + 2 == blocks);
           } else if (one) {
@@ -268,6 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (used > 0) {
         const bool idle = (warp & 3) * 32 >= used;  // no row of this warp is one
         const int qrow = p.rows.first + j_tok;
+        const int hid = a.shape.window ? max(qrow - a.shape.window, -1) : -1;
         float m = -INFINITY;
         float2 l2 = make_float2(0.f, 0.f);
         const int blk0 = p.blk0, blk1 = p.blk1;
@@ -286,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (hides) {
 #pragma unroll
               for (int x = 0; x < kBn; x += 32) {
-                const uint32_t see = rows_seen(a.shape, qrow, i0 + x);
+                const uint32_t see = rows_seen(a.shape, qrow, hid, i0 + x);
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                   if (!(see >> e & 1)) v[x + e] = -INFINITY;
@@ -334,12 +360,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                 h[e] = *(const uint32_t *)&y;
               }
               tmem_store16(ts + x / 2, h);  // over scores that have been read
+              if (x == kBn / 2 - 32) {
+                tmem_wait_store();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.p_half[s]);
+              }
             }
             tmem_wait_store();
             tc_fence_before();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bars.p_full[s]);
+          if (lane == 0) {
+            if (idle) mbar_arrive(&bars.p_half[s]);
+            mbar_arrive(&bars.p_full[s]);
+          }
         }
         if (!ok) break;
         ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[s], mine & 1));
@@ -350,48 +385,60 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float l = l2.x + l2.y;
           const bool whole = p.slot < 0, bad = p.bad;
           const float inv = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
-          const int64_t dst =
-              ((int64_t)(p.tok0 + j_tok) * (a.H_kv * a.g) + p.kvh * a.g + r % a.g) * D;
           const int pr = s * tpt * a.g + r;
+          // results leave in stretches of 64 bytes a row: lane 4 i + j writes the j-th 16 bytes of rows
+          // 4 i .. 4 i + 3 (a lane writing its own row would touch 32 lines an instruction)
+          int64_t dst[4];
+          {
+            const int64_t own =
+                r < used ? ((int64_t)(p.tok0 + j_tok) * (a.H_kv * a.g) + p.kvh * a.g + r % a.g) * D
+                         : -1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = __shfl_sync(0xffffffffu, own, (lane & 28) + i);
+          }
 #pragma unroll 1
           for (int x = 0; x < D; x += 32) {
             uint32_t o[32];
             tmem_load32(to + x, o);
             tmem_wait_load();
-            if (r < used) {
-              if (bad) {  // what was cleared and this query sees
-                for (int blk = blk0; blk < blk1; ++blk) {
-                  const int i0 = p.blocks.index(blk) * kBn;
-                  if (!p.hides(blk)) continue;
-                  for (int i = i0; i < i0 + kBn && i < p.n; ++i) {
-                    if (!row_sees(p.rows, a.shape, qrow, i)) continue;
-                    const __nv_bfloat16 *vr = (const __nv_bfloat16 *)a.V + (p.row0 + i) * D + x;
+            if (bad && r < used) {  // what was cleared and this query sees
+              for (int blk = blk0; blk < blk1; ++blk) {
+                const int i0 = p.blocks.index(blk) * kBn;
+                if (!p.hides(blk)) continue;
+                for (int i = i0; i < i0 + kBn && i < p.n; ++i) {
+                  if (!row_sees(p.rows, a.shape, qrow, i)) continue;
+                  const __nv_bfloat16 *vr = (const __nv_bfloat16 *)a.V + (p.row0 + i) * D + x;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                      const float z = __bfloat162float(vr[e]);
-                      if (!isfinite(z)) o[e] = __float_as_uint(__uint_as_float(o[e]) + z);
-                    }
+                  for (int e = 0; e < 32; ++e) {
+                    const float z = __bfloat162float(vr[e]);
+                    if (!isfinite(z)) o[e] = __float_as_uint(__uint_as_float(o[e]) + z);
                   }
                 }
               }
-              if (whole) {
-                uint32_t h[16];
+            }
+            __syncwarp();
+            if (whole) {
+              uint4 h[4];  // the row's four 16-byte pieces
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const __nv_bfloat162 z = __floats2bfloat162_rn(
-                      __uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-                  h[e] = *(const uint32_t *)&z;
-                }
-                uint4 *d4 = (uint4 *)((__nv_bfloat16 *)a.out + dst + x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  d4[e] = make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]);
-              } else {
-                uint4 *d4 = (uint4 *)(part_row(a, D, blockIdx.x, p.slot, pr) + x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  d4[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+              for (int e = 0; e < 16; ++e) {
+                const __nv_bfloat162 z = __floats2bfloat162_rn(
+                    __uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                ((uint32_t *)h)[e] = *(const uint32_t *)&z;
               }
+              // transposed among four lanes: piece i of this row <-> piece of row i
+              swap_pieces<1>(h[0], h[1], lane);
+              swap_pieces<1>(h[2], h[3], lane);
+              swap_pieces<2>(h[0], h[2], lane);
+              swap_pieces<2>(h[1], h[3], lane);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (dst[i] >= 0)
+                  *(uint4 *)((__nv_bfloat16 *)a.out + dst[i] + x + 8 * (lane & 3)) = h[i];
+            } else if (r < used) {
+              uint4 *d4 = (uint4 *)(part_row(a, D, blockIdx.x, p.slot, pr) + x);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                d4[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             }
             __syncwarp();  // every lane loads the next columns together
           }

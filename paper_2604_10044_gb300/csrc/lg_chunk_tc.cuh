@@ -23,13 +23,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // bit e: the query at row qrow sees row i0 + e, e < 32
-__device__ __forceinline__ uint32_t rows_seen(const ChunkShape &s, int qrow, int i0) {
-  auto below = [](int64_t n) {  // bits 0 .. n - 1
-    return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1;
+// (hid: the last row that the window hides from it, -1 for none)
+__device__ __forceinline__ uint32_t rows_seen(const ChunkShape &s, int qrow, int hid, int i0) {
+  auto below = [](int n) {  // bits 0 .. n - 1; shifts of 32 and more give 0
+    uint32_t r;
+    asm("shr.b32 %0, %1, %2;" : "=r"(r) : "r"(0xffffffffu), "r"(max(32 - n, 0)));
+    return r;
   };
-  const uint32_t past = below((int64_t)qrow + 1 - i0);
-  if (s.window == 0) return past;
-  return past & (~below((int64_t)qrow + 1 - s.window - i0) | below((int64_t)s.sink - i0));
+  return below(qrow + 1 - i0) & (~below(hid + 1 - i0) | below(s.sink - i0));
 }
 
 // bounded wait that also ends when another role has given up
