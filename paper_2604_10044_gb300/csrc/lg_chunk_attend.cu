@@ -179,10 +179,9 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
           store4(a.out, dst + 4 * tx + 64 * k, f);
         }
       } else {
-        float *dst = part_row(a, D, blockIdx.x, w.slot(), r);
 #pragma unroll
         for (int k = 0; k < NC; ++k)
-          *(float4 *)(dst + 4 * tx + 64 * k) =
+          *part_at(a, D, blockIdx.x, w.slot(), tx + 16 * k, r) =
               make_float4(o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]);
         if (tx == 0) *part_ml(a, D, gridDim.x, blockIdx.x, w.slot(), r) = make_float2(m[i], l[i]);
       }
@@ -191,60 +190,78 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
 }
 
 // Merge of the item that CTA c's start is the first to cut, c = blockIdx.x + 1, from the parts of
-// CTAs c - 1, c, ...: a warp per row, 32 parts at a time, a lane each for maximum and normaliser.
+// CTAs c - 1, c, ...: 32 rows a CTA, a lane each, the elements spread over the eight warps; the rows
+// leave through shared memory, 16 bytes a thread.
+constexpr int kMergeRows = 32;
+constexpr int kAtOnce = 4;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
-  constexpr int V = D / 32;  // elements a lane
+  constexpr int NE = D / 4 / (kThreads / 32);  // groups of four elements a thread
+  constexpr int kRow = D * (int)sizeof(T) + 16;
+  __shared__ __align__(16) uint8_t s_out[kMergeRows * kRow];
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_enter();
   const ChunkCut w = *cut_at(a, D, G, c);
-  if (__any_sync(0xffffffffu, lane == 0 && status_bad(a.status))) return;
-  if (w.parts == 0) return;
-  const int H_q = a.H_kv * a.g, last = c - 2 + w.parts;
-  auto cut = [&](int p) {
-    return cut_block(w.in + (p - c) * w.step, w.cost, w.blocks, a.shape.bn2);
-  };
-  for (int r = blockIdx.y * (kThreads / 32) + warp; r < w.used; r += gridDim.y * (kThreads / 32)) {
-    float m = -INFINITY, l = 0.f, o[V];
+  if (cta_status_bad(a.status)) return;
+  const int r0 = blockIdx.y * kMergeRows, r = r0 + lane;
+  if (w.parts == 0 || r0 >= w.used) return;
+  float m = -INFINITY, l = 0.f;
+  float4 o[NE];
 #pragma unroll
-    for (int k = 0; k < V; ++k) o[k] = 0.f;
-    bool whole = false;
-    for (int p0 = c - 1; p0 <= last && !whole; p0 += 32) {
-      const int p = p0 + lane;
-      const int b0 = p <= last ? cut(p) : 0, b1 = p <= last ? cut(p + 1) : 0;
-      const bool some = b0 < b1;
-      // one piece has every block: its CTA wrote the result
-      whole = __any_sync(0xffffffffu, some && b0 == 0 && b1 == w.blocks);
-      if (whole) break;
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (some) ml = *part_ml(a, D, G, p, p == c - 1 ? 1 : 0, r);
-      float mx = fmaxf(m, ml.x);
+  for (int e = 0; e < NE; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+  int before = 0;
+  for (int p0 = 0; p0 < w.parts; p0 += kAtOnce) {
+    float2 ml[kAtOnce];
+    float4 x[kAtOnce][NE];
 #pragma unroll
-      for (int i = 16; i; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, i));
-      const float base = mx == -INFINITY ? 0.f : mx;
-      const float f0 = exp2_fast(m - base), f = some ? exp2_fast(ml.x - base) : 0.f;
-      float lp = ml.y * f;
+    for (int k = 0; k < kAtOnce; ++k) {  // the loads of kAtOnce parts wait together
+      const int p = p0 + k, from = before;
+      if (p < w.parts) before = cut_block(w.in + p * w.step, w.cost, w.blocks, a.shape.bn2);
+      if (from == 0 && before == w.blocks) return;  // one part has every block and wrote the result
+      ml[k] = make_float2(-INFINITY, 0.f);
+      if (from == before || r >= w.used) continue;
+      const int cta = c - 1 + p, slot = p == 0 ? 1 : 0;
+      ml[k] = *part_ml(a, D, G, cta, slot, r);
 #pragma unroll
-      for (int i = 16; i; i >>= 1) lp += __shfl_xor_sync(0xffffffffu, lp, i);
-      l = l * f0 + lp;
+      for (int e = 0; e < NE; ++e) x[k][e] = *part_at(a, D, cta, slot, warp * NE + e, r);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;  // (no part, or nothing was seen in it)
+      const float mx = fmaxf(m, ml[k].x), base = mx == -INFINITY ? 0.f : mx;
+      const float f0 = exp2_fast(m - base), f1 = exp2_fast(ml[k].x - base);
       m = mx;
+      l = l * f0 + ml[k].y * f1;
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] *= f0;
-      const unsigned have = __ballot_sync(0xffffffffu, some);
-#pragma unroll 4
-      for (int i = 0; i < 32; ++i) {
-        if (!(have >> i & 1)) continue;
-        const float fi = __shfl_sync(0xffffffffu, f, i);
-        const float *src = part_row(a, D, p0 + i, p0 + i == c - 1 ? 1 : 0, r);
-#pragma unroll
-        for (int k = 0; k < V; ++k) o[k] += src[lane + 32 * k] * fi;
+      for (int e = 0; e < NE; ++e) {
+        o[e].x = o[e].x * f0 + x[k][e].x * f1;
+        o[e].y = o[e].y * f0 + x[k][e].y * f1;
+        o[e].z = o[e].z * f0 + x[k][e].z * f1;
+        o[e].w = o[e].w * f0 + x[k][e].w * f1;
       }
     }
-    if (whole) continue;
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    const int64_t dst = ((int64_t)(w.tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D;
+  }
+  const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int k = 0; k < V; ++k) Elem<T>::store(a.out, dst + lane + 32 * k, o[k] * inv);
+  for (int e = 0; e < NE; ++e) {
+    uint8_t *at = s_out + lane * kRow + (warp * NE + e) * 4 * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+      *(float4 *)at = make_float4(o[e].x * inv, o[e].y * inv, o[e].z * inv, o[e].w * inv);
+    } else {
+      const __nv_bfloat162 h[2] = {__floats2bfloat162_rn(o[e].x * inv, o[e].y * inv),
+                                   __floats2bfloat162_rn(o[e].z * inv, o[e].w * inv)};
+      *(uint2 *)at = *(const uint2 *)h;
+    }
+  }
+  __syncthreads();
+  constexpr int kPer = D * (int)sizeof(T) / 16;  // 16-byte pieces of a row
+  for (int i = threadIdx.x; i < kMergeRows * kPer; i += kThreads) {
+    const int rr = i / kPer, q = r0 + rr;
+    if (q >= w.used) break;
+    const int64_t dst = ((int64_t)(w.tok0 + q / a.g) * (a.H_kv * a.g) + w.kvh * a.g + q % a.g) * D;
+    *(uint4 *)((T *)a.out + dst + i % kPer * (16 / (int)sizeof(T))) =
+        *(const uint4 *)(s_out + rr * kRow + i % kPer * 16);
   }
 }
 
@@ -259,8 +276,7 @@ cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
 
 template <typename T, int D>
 cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
-  const int rows = kThreads / 32;  // a CTA's at once; two rows a warp at most
-  const dim3 grid(G - 1, a.rows <= 16 * rows ? (a.rows + rows - 1) / rows : 16);
+  const dim3 grid(G - 1, (a.rows + kMergeRows - 1) / kMergeRows);
   LG_TRY(launch_pdl(chunk_merge_kernel<T, D>, grid, kThreads, 0, s, a, G));
   return cudaGetLastError();
 }

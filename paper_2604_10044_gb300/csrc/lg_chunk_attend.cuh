@@ -19,8 +19,8 @@ struct ChunkAttendArgs {
   const int32_t *len;      // [batch]
   const int32_t *off;      // [batch + 1]
   int32_t *status;
-  float *part;             // [2 G][rows][d] partial sums, [2 G][rows][2] maxima and normalisers,
-                           // then [G] ChunkCut
+  float *part;             // [2 G][d / 4][rows][4] partial sums, [2 G][rows][2] maxima and
+                           // normalisers, then [G] ChunkCut
   int64_t S_total;
   int64_t cache_rows;      // L * H_kv * S_total
   int layer, batch, H_kv, g, T, max_new, max_len;
@@ -88,7 +88,7 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
   }
   if (bad) set_status(a.status, LG_ERR_CAPACITY);
   if (__any_sync(0xffffffffu, bad || stop)) return false;
-  sh.step = range_step(sh.W, G);
+  sh.step = range_step(sh.W, G, a.shape.bn2);
   sh.y0 = plan_min(sh.W, cta * sh.step);
   sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
   if (sh.y0 >= sh.W) return false;
@@ -177,9 +177,11 @@ struct ChunkWalk {
   }
 };
 
-__device__ __forceinline__ float *part_row(const ChunkAttendArgs &a, int d, int cta, int slot,
+// four elements (4 e ..) of row r of a partial result: rows side by side, so that a warp whose lanes
+// hold a row each writes and reads whole stretches
+__device__ __forceinline__ float4 *part_at(const ChunkAttendArgs &a, int d, int cta, int slot, int e,
                                            int r) {
-  return a.part + (((int64_t)cta * 2 + slot) * a.rows + r) * d;
+  return (float4 *)a.part + (((int64_t)cta * 2 + slot) * (d / 4) + e) * a.rows + r;
 }
 
 __device__ __forceinline__ float2 *part_ml(const ChunkAttendArgs &a, int d, int G, int cta,

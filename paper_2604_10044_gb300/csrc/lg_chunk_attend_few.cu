@@ -444,7 +444,8 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         int h = q0 % a.g;
         __nv_bfloat16 *out = (__nv_bfloat16 *)a.out + key +
                              ((int64_t)(tok0 + q0 / a.g) * (a.H_kv * a.g) + w.kvh * a.g + h) * D;
-        float *part = whole ? nullptr : part_row(a, D, blockIdx.x, w.slot, q0) + key;
+        float *part =
+            whole ? nullptr : (float *)part_at(a, D, blockIdx.x, w.slot, key / 4, q0) + key % 4;
         const int64_t skip = (int64_t)(a.H_kv - 1) * a.g * D;
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
@@ -455,7 +456,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
             out += D;
             if (++h == a.g) h = 0, out += skip;
           } else {
-            part[q * D] = x;
+            part[q * 4] = x;
           }
         }
       }

@@ -435,10 +435,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (dst[i] >= 0)
                   *(uint4 *)((__nv_bfloat16 *)a.out + dst[i] + x + 8 * (lane & 3)) = h[i];
             } else if (r < used) {
-              uint4 *d4 = (uint4 *)(part_row(a, D, blockIdx.x, p.slot, pr) + x);
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                d4[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                *(uint4 *)part_at(a, D, blockIdx.x, p.slot, x / 4 + e, pr) =
+                    make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             }
             __syncwarp();  // every lane loads the next columns together
           }

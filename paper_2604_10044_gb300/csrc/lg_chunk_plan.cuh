@@ -5,7 +5,7 @@
 // cost is the rows its queries can see plus kItemCost, a linear function of the tile (constant once
 // a window fills), so the cost of a sequence's first t tiles is a closed form.  The items stand in
 // one line, ordered by sequence, kv-head and tile, W cost units long, and each of G CTAs takes
-// ceil(W / G) of it.  An item cut by such a bound is shared: its key blocks divide in
+// ceil(W / G) of it (or a block's rows, if that is more).  An item cut by such a bound is shared: its key blocks divide in
 // proportion, each CTA's part is a piece, and a second kernel merges the pieces (of partial
 // results in the workspace: slot 0 of a CTA for an item that began before its range, slot 1 for
 // one that ends after it).
@@ -132,9 +132,10 @@ __host__ __device__ __forceinline__ void open_blocks(const TileRows &r, const Ch
   open1 = hi > lo ? hi - b.skip : open0;
 }
 
-// cost units of a CTA of G: CTA c takes [c step, (c + 1) step) of the line, up to its end W
-__host__ __device__ __forceinline__ int64_t range_step(int64_t W, int G) {
-  return plan_div(W + G - 1, G);
+// cost units of a CTA of G: CTA c takes [c step, (c + 1) step) of the line, up to its end W; a block's
+// rows at least, as a smaller share would leave CTAs without a block and the merge with empty parts
+__host__ __device__ __forceinline__ int64_t range_step(int64_t W, int G, int bn2) {
+  return plan_max(plan_div(W + G - 1, G), (int64_t)1 << bn2);
 }
 
 // blocks before a cut at cost unit y of an item: in whole blocks of the rows that the units stand

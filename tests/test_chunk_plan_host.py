@@ -93,7 +93,7 @@ int main() {
         }
     }
     int64_t end = 0;
-    const int64_t step = range_step(W, G);
+    const int64_t step = range_step(W, G, s.bn2);
     std::vector<int> next(start.size(), 0);
     for (int c = 0; c < G; ++c) {
       const int64_t y0 = plan_min(W, c * step), y1 = plan_min(W, y0 + step);
@@ -111,14 +111,14 @@ int main() {
       }
       CHECK(slots[0] <= 1 && slots[1] <= 1);
     }
-    CHECK(end == W);
+    CHECK(end == W && (step == 1 << s.bn2 || step * G - W < G));
     for (size_t i = 0; i < start.size(); ++i) CHECK(next[i] == count[i]);
   }
   // the largest line: no 64-bit overflow in the bounds or the cuts
   const ChunkSeq big{2147483647, 2147483647};
   const ChunkShape s{16, 6, 0, 0};
   const int64_t W = tiles_cost(big, s, big.tiles(s.tok)) / 2;
-  CHECK(W > 0 && range_step(W, 304) * 304 >= W && range_step(W, 304) * 304 - W < 304);
+  CHECK(W > 0 && range_step(W, 304, 6) * 304 >= W && range_step(W, 304, 6) * 304 - W < 304);
   const int64_t c = tile_cost(big, s, big.tiles(16) - 1);
   CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1, 6) <= 2147483647 / 64 + 1);
   puts("ok");
