@@ -38,6 +38,11 @@ struct SimtCfg {
       (BM * kRow + kBn * kRow + kBn * D + BM * (kBn + 4)) * (int)sizeof(float);
 };
 
+template <bool E>
+struct Edge {
+  static constexpr bool value = E;
+};
+
 template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs a) {
   constexpr int TM = BM / 16, NC = D / 64, kRow = SimtCfg<D, BM>::kRow, kPRow = kBn + 4;
@@ -73,19 +78,25 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
 #pragma unroll
       for (int k = 0; k < 4 * NC; ++k) o[i][k] = 0.f;
     }
-    for (int blk = w.blk0; blk < w.blk1; ++blk) {
+    int open0, open1;
+    open_blocks(w.rows, a.shape, w.blocks, open0, open1);
+    // rows i0 .. of the keys or values into shared memory, those past the sequence as zeros
+    auto copy = [&](float *dst, int row, const void *src, int blk) {
       const int i0 = w.blocks.index(blk) * kBn;
-      __syncthreads();
       for (int e = tid; e < kBn * (D / 4); e += kThreads) {
         const int r = e / (D / 4), c = e % (D / 4) * 4;
-        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (i0 + r < w.q.n) {
-          load4(a.K, (w.row0 + i0 + r) * D + c, k);
-          load4(a.V, (w.row0 + i0 + r) * D + c, v);
-        }
-        *(float4 *)(sk + r * kRow + c) = make_float4(k[0], k[1], k[2], k[3]);
-        *(float4 *)(sv + r * D + c) = make_float4(v[0], v[1], v[2], v[3]);
+        const bool in = i0 + r < w.q.n;
+        cp_async16_or_zero(dst + r * row + c,
+                           (const float *)src + (w.row0 + (in ? i0 + r : 0)) * D + c, in);
       }
+      cp_async_commit();
+    };
+    copy(sk, kRow, a.K, w.blk0);
+    for (int blk = w.blk0; blk < w.blk1; ++blk) {
+      const int i0 = w.blocks.index(blk) * kBn;
+      const bool hides = blk < open0 || blk >= open1;
+      copy(sv, D, a.V, blk);  // (on its way while the scores are formed)
+      cp_async_wait<1>();
       __syncthreads();
       // scores, even and odd elements summed apart
       float2 acc[TM][4];
@@ -108,15 +119,13 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
           }
         }
       }
-      bool edge = false;  // some key of the block is hidden from some query of this thread
       float alpha[TM];
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         float s[4], mx = m[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool sees = row_sees(w.rows, a.shape, qrow[i], i0 + tx + 16 * j);
-          edge |= !sees;
+          const bool sees = !hides || row_sees(w.rows, a.shape, qrow[i], i0 + tx + 16 * j);
           s[j] = sees ? (acc[i][j].x + acc[i][j].y) * a.qscale : -INFINITY;
           mx = fmaxf(mx, s[j]);
         }
@@ -133,35 +142,48 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
           sp[(ty * TM + i) * kPRow + tx + 16 * j] = p;
         }
       }
-      edge = __any_sync(0xffffffffu, edge);  // also orders the half-warp's probabilities
-      __syncwarp();
+      __syncthreads();  // the keys have been read (and a half-warp's probabilities are written)
+      if (blk + 1 < w.blk1)
+        copy(sk, kRow, a.K, blk + 1);
+      else
+        cp_async_commit();
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int k = 0; k < 4 * NC; ++k) o[i][k] *= alpha[i];
+      cp_async_wait<1>();
+      __syncthreads();
+      auto sums = [&](auto edge) {
 #pragma unroll 2
-      for (int r = 0; r < kBn; r += 4) {
-        float4 p[TM];
+        for (int r = 0; r < kBn; r += 4) {
+          float4 p[TM];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) p[i] = *(const float4 *)(sp + (ty * TM + i) * kPRow + r);
+          for (int i = 0; i < TM; ++i) p[i] = *(const float4 *)(sp + (ty * TM + i) * kPRow + r);
 #pragma unroll
-        for (int rr = 0; rr < 4; ++rr)
+          for (int rr = 0; rr < 4; ++rr)
 #pragma unroll
-          for (int k = 0; k < NC; ++k) {
-            const float4 v = *(const float4 *)(sv + (r + rr) * D + 4 * tx + 64 * k);
+            for (int k = 0; k < NC; ++k) {
+              const float4 v = *(const float4 *)(sv + (r + rr) * D + 4 * tx + 64 * k);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-              const float pr = rr == 0 ? p[i].x : rr == 1 ? p[i].y : rr == 2 ? p[i].z : p[i].w;
-              // a hidden row has probability 0 and may hold anything
-              const bool add = !edge || pr != 0.f;
-              float2 *oo = (float2 *)&o[i][4 * k];
-              oo[0] = __ffma2_rn(make_float2(pr, pr), add ? make_float2(v.x, v.y) : make_float2(0.f, 0.f), oo[0]);
-              oo[1] = __ffma2_rn(make_float2(pr, pr), add ? make_float2(v.z, v.w) : make_float2(0.f, 0.f), oo[1]);
+              for (int i = 0; i < TM; ++i) {
+                const float pr = rr == 0 ? p[i].x : rr == 1 ? p[i].y : rr == 2 ? p[i].z : p[i].w;
+                // a hidden row has probability 0 and may hold anything
+                const bool add = !decltype(edge)::value || pr != 0.f;
+                float2 *oo = (float2 *)&o[i][4 * k];
+                const float2 pp = make_float2(pr, pr);
+                oo[0] = __ffma2_rn(pp, add ? make_float2(v.x, v.y) : make_float2(0.f, 0.f), oo[0]);
+                oo[1] = __ffma2_rn(pp, add ? make_float2(v.z, v.w) : make_float2(0.f, 0.f), oo[1]);
+              }
             }
-          }
-      }
-      __syncwarp();
+        }
+      };
+      if (hides)
+        sums(Edge<true>{});
+      else
+        sums(Edge<false>{});
+      __syncthreads();  // the values have been read
     }
+    cp_async_wait<0>();
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int r = ty * TM + i;
@@ -191,11 +213,11 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
 
 // Merge of the item that CTA c's start is the first to cut, c = blockIdx.x + 1, from the parts of
 // CTAs c - 1, c, ...: 32 rows a CTA, a lane each, the elements spread over the eight warps; the rows
-// leave through shared memory, 16 bytes a thread.
+// leave through shared memory, 16 bytes a thread.  The loads of kAtOnce parts wait together: 8 where
+// items are short and have many, 4 where they are long (fewer registers, more CTAs an SM).
 constexpr int kMergeRows = 32;
-constexpr int kAtOnce = 4;
 
-template <typename T, int D>
+template <typename T, int D, int kAtOnce>
 __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
   constexpr int NE = D / 4 / (kThreads / 32);  // groups of four elements a thread
   constexpr int kRow = D * (int)sizeof(T) + 16;
@@ -215,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
     float2 ml[kAtOnce];
     float4 x[kAtOnce][NE];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {  // the loads of kAtOnce parts wait together
+    for (int k = 0; k < kAtOnce; ++k) {
       const int p = p0 + k, from = before;
       if (p < w.parts) before = cut_block(w.in + p * w.step, w.cost, w.blocks, a.shape.bn2);
       if (from == 0 && before == w.blocks) return;  // one part has every block and wrote the result
@@ -277,7 +299,10 @@ cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
   const dim3 grid(G - 1, (a.rows + kMergeRows - 1) / kMergeRows);
-  LG_TRY(launch_pdl(chunk_merge_kernel<T, D>, grid, kThreads, 0, s, a, G));
+  if (a.rows <= 64)
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 8>, grid, kThreads, 0, s, a, G));
+  else
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 4>, grid, kThreads, 0, s, a, G));
   return cudaGetLastError();
 }
 

@@ -196,6 +196,13 @@ __device__ __forceinline__ void cp_async16(void *smem_dst, const void *gmem_src)
                : "memory");
 }
 
+// the same, or 16 zero bytes where `copy` is false (the source is not read, but is an address)
+__device__ __forceinline__ void cp_async16_or_zero(void *smem_dst, const void *gmem_src, bool copy) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(smem_dst)),
+               "l"(gmem_src), "r"(copy ? 16 : 0)
+               : "memory");
+}
+
 // 4-byte asynchronous copy global -> shared, in the same commit groups
 __device__ __forceinline__ void cp_async4(void *smem_dst, const void *gmem_src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(smem_dst)),
