@@ -1,7 +1,7 @@
-// lg_chunk_attend on the CUDA cores, and the merge of shared items.
+// lg_chunk_attend of fp32 caches on the CUDA cores, and the merge of shared items.
 //
-// A query tile is BM rows: the g query heads of BM / g consecutive new tokens (row r: token r / g,
-// head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
+// chunk_attend_kernel's query tile is 128 rows: the g query heads of 128 / g consecutive new
+// tokens (row r: token r / g, head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
 // a running maximum m, normaliser l and sum o per row (log2 units):
 //   m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,  o = o 2^(m - m') + p V.
 // 256 threads as 16 x 16: thread (ty, tx) computes the scores of rows ty TM .. ty TM + TM - 1 and
@@ -31,11 +31,13 @@ __device__ __forceinline__ void store4(void *p, int64_t i, const float *f) {
   *(float4 *)((float *)p + i) = make_float4(f[0], f[1], f[2], f[3]);
 }
 
-template <int D, int BM>
+constexpr int kBm = 128;  // rows of a query tile
+
+template <int D>
 struct SimtCfg {
   static constexpr int kRow = D + 4;  // floats of a staged row: 16 rows of 16 bytes, no conflicts
   static constexpr int kSmem =
-      (BM * kRow + kBn * kRow + kBn * D + BM * (kBn + 4)) * (int)sizeof(float);
+      (kBm * kRow + kBn * kRow + kBn * D + kBm * (kBn + 4)) * (int)sizeof(float);
 };
 
 template <bool E>
@@ -43,17 +45,17 @@ struct Edge {
   static constexpr bool value = E;
 };
 
-template <int D, int BM>
+template <int D>
 __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs a) {
-  constexpr int TM = BM / 16, NC = D / 64, kRow = SimtCfg<D, BM>::kRow, kPRow = kBn + 4;
+  constexpr int TM = kBm / 16, NC = D / 64, kRow = SimtCfg<D>::kRow, kPRow = kBn + 4;
   extern __shared__ __align__(16) float smem[];
-  float *sq = smem, *sk = sq + BM * kRow, *sv = sk + kBn * kRow, *sp = sv + kBn * D;
+  float *sq = smem, *sk = sq + kBm * kRow, *sv = sk + kBn * kRow, *sp = sv + kBn * D;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int H_q = a.H_kv * a.g;
   pdl_enter();
   ChunkShare sh;
-  ChunkWalk<BM == 16> w;
-  const bool work = chunk_share<BM == 16>(a, blockIdx.x, gridDim.x, sh);
+  ChunkWalk<false> w;
+  const bool work = chunk_share<false>(a, blockIdx.x, gridDim.x, sh);
   if (work) w.start(a, sh);
   if (tid == 0) put_cut(a, D, gridDim.x, blockIdx.x, work, sh, w);
   for (; work && !w.done(); w.next(a)) {
@@ -61,7 +63,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
     const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
     const int tok0 = w.off + w.t * a.shape.tok;
     __syncthreads();
-    for (int e = tid; e < BM * (D / 4); e += kThreads) {
+    for (int e = tid; e < kBm * (D / 4); e += kThreads) {
       const int r = e / (D / 4), c = e % (D / 4) * 4;
       float f[4] = {0.f, 0.f, 0.f, 0.f};
       if (r < used)
@@ -211,6 +213,190 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
   }
 }
 
+// The same for at most 16 query rows of a kv-head, where reading the cache is all of the work: a warp
+// takes eight keys of every block, a row of them at a load (two of 64 elements), each lane four
+// elements.  The products of a key with all R query rows are summed over the lanes by halving (each
+// level hands half of the rows over), which leaves a row's score to 32 / R lanes; its weights go
+// through shared memory to all lanes, which add weight x value to R x 4 sums of their own.  m lags
+// as in the tensor-core kernels.  The eight warps' results are merged at the end of a piece.
+template <int D, int R>
+struct FewF32 {
+  static constexpr int kLanes = D / 4;          // lanes of a row
+  static constexpr int kKeys = 32 / kLanes;     // keys of a load
+  static constexpr int kWarps = kThreads / 32;
+  static constexpr int kSmem =
+      kWarps * R * (D + 2) * (int)sizeof(float);  // results, maxima and normalisers
+};
+constexpr int kFewKeys = kBn / (kThreads / 32);  // of a warp in a block
+constexpr float kLazy = 8.f;
+
+template <int D, int R>
+__global__ void __launch_bounds__(kThreads, R == 4 ? 2 : 1)
+    chunk_attend_few_f32_kernel(ChunkAttendArgs a) {
+  using C = FewF32<D, R>;
+  constexpr int LPR = C::kLanes, KPL = C::kKeys, NL = kFewKeys / KPL;  // loads of a block
+  extern __shared__ __align__(16) float smem[];
+  __shared__ __align__(16) float s_p[C::kWarps][kFewKeys + 1][R];  // weights; what sums are scaled by
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int half = lane / LPR, el = lane % LPR;       // key of a load, group of four elements
+  const int row = el / (LPR / R);                     // the row whose scores this lane keeps
+  const bool keeper = el % (LPR / R) == 0;
+  const int H_q = a.H_kv * a.g;
+  float *s_o = smem, *s_m = smem + C::kWarps * R * D, *s_l = s_m + C::kWarps * R;
+  pdl_enter();
+  ChunkShare sh;
+  ChunkWalk<true> w;
+  const bool work = chunk_share<true>(a, blockIdx.x, gridDim.x, sh);
+  if (work) w.start(a, sh);
+  if (tid == 0) put_cut(a, D, gridDim.x, blockIdx.x, work, sh, w);
+  for (; work && !w.done(); w.next(a)) {
+    if (w.blk0 == w.blk1) continue;
+    const int used = w.tokens(a) * a.g, tok0 = w.off + w.t * a.shape.tok;
+    const int qrow = w.rows.first + row / a.g;
+    float4 q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      q[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < used)
+        q[r] = *(const float4 *)((const float *)a.q +
+                                 ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D +
+                                 4 * el);
+    }
+    float2 o[R][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) o[r][0] = o[r][1] = make_float2(0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    int open0, open1;
+    open_blocks(w.rows, a.shape, w.blocks, open0, open1);
+    for (int blk = w.blk0; blk < w.blk1; ++blk) {
+      const int i0 = w.blocks.index(blk) * kBn + warp * kFewKeys + half;  // this lane's first key
+      const bool hides = blk < open0 || blk >= open1;
+      float4 k[NL], v[NL];
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        const int i = i0 + j * KPL;
+        k[j] = v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < w.q.n) {
+          k[j] = *(const float4 *)((const float *)a.K + (w.row0 + i) * D + 4 * el);
+          v[j] = *(const float4 *)((const float *)a.V + (w.row0 + i) * D + 4 * el);
+        }
+      }
+      float sc[NL], top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        float x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float2 t = __fmul2_rn(make_float2(q[r].x, q[r].y), make_float2(k[j].x, k[j].y));
+          t = __ffma2_rn(make_float2(q[r].z, q[r].w), make_float2(k[j].z, k[j].w), t);
+          x[r] = t.x + t.y;
+        }
+        HeadReduce<R, LPR / 2>::run(x, lane);
+        const int i = i0 + j * KPL;
+        const bool sees = !hides || row_sees(w.rows, a.shape, qrow, i);
+        sc[j] = sees ? x[0] * a.qscale : -INFINITY;
+        top = fmaxf(top, sc[j]);
+      }
+      if (KPL == 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      const bool rise = top > m + kLazy || (m == -INFINITY && top > m);
+      if (__any_sync(0xffffffffu, rise)) {
+        const float m1 = rise ? top : m;
+        const float f = rise ? exp2_fast(m - m1) : 1.f;
+        m = m1;
+        l *= f;
+        __syncwarp();
+        if (keeper && half == 0) s_p[warp][kFewKeys][row] = f;
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float fr = s_p[warp][kFewKeys][r];
+          o[r][0] = __fmul2_rn(o[r][0], make_float2(fr, fr));
+          o[r][1] = __fmul2_rn(o[r][1], make_float2(fr, fr));
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        const float p = exp2_fast(sc[j] - base);
+        l += p;
+        if (keeper) s_p[warp][j * KPL + half][row] = p;
+      }
+      __syncwarp();
+      auto sums = [&](auto edge) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+          for (int r = 0; r < R; r += 4) {
+            const float4 p4 = *(const float4 *)&s_p[warp][j * KPL + half][r];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = e == 0 ? p4.x : e == 1 ? p4.y : e == 2 ? p4.z : p4.w;
+              // a hidden row has weight 0 and may hold anything
+              const bool add = !decltype(edge)::value || p != 0.f;
+              o[r + e][0] = __ffma2_rn(make_float2(p, p),
+                                       add ? make_float2(v[j].x, v[j].y) : make_float2(0.f, 0.f),
+                                       o[r + e][0]);
+              o[r + e][1] = __ffma2_rn(make_float2(p, p),
+                                       add ? make_float2(v[j].z, v[j].w) : make_float2(0.f, 0.f),
+                                       o[r + e][1]);
+            }
+          }
+      };
+      if (hides)
+        sums(Edge<true>{});
+      else
+        sums(Edge<false>{});
+    }
+    // the warps' results meet in shared memory
+    if (KPL == 2) {
+      l += __shfl_xor_sync(0xffffffffu, l, 16);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          o[r][e].x += __shfl_xor_sync(0xffffffffu, o[r][e].x, 16);
+          o[r][e].y += __shfl_xor_sync(0xffffffffu, o[r][e].y, 16);
+        }
+    }
+    __syncthreads();  // (the previous piece's have been read)
+    if (half == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        *(float4 *)(s_o + (warp * R + r) * D + 4 * el) =
+            make_float4(o[r][0].x, o[r][0].y, o[r][1].x, o[r][1].y);
+      if (keeper) {
+        s_m[warp * R + row] = m;
+        s_l[warp * R + row] = l;
+      }
+    }
+    __syncthreads();
+    for (int e = tid; e < used * LPR; e += kThreads) {
+      const int r = e / LPR, c = e % LPR;
+      float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < C::kWarps; ++x) mx = fmaxf(mx, s_m[x * R + r]);
+      const float base = mx == -INFINITY ? 0.f : mx;
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int x = 0; x < C::kWarps; ++x) {
+        const float f = exp2_fast(s_m[x * R + r] - base);
+        const float4 y = *(const float4 *)(s_o + (x * R + r) * D + 4 * c);
+        sum += s_l[x * R + r] * f;
+        t.x += y.x * f, t.y += y.y * f, t.z += y.z * f, t.w += y.w * f;
+      }
+      if (w.whole()) {
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+        const float f[4] = {t.x * inv, t.y * inv, t.z * inv, t.w * inv};
+        store4(a.out, ((int64_t)(tok0 + r / a.g) * H_q + w.kvh * a.g + r % a.g) * D + 4 * c, f);
+      } else {
+        *part_at(a, D, blockIdx.x, w.slot(), c, r) = t;
+        if (c == 0) *part_ml(a, D, gridDim.x, blockIdx.x, w.slot(), r) = make_float2(mx, sum);
+      }
+    }
+  }
+}
+
 // Merge of the item that CTA c's start is the first to cut, c = blockIdx.x + 1, from the parts of
 // CTAs c - 1, c, ...: 32 rows a CTA, a lane each, the elements spread over the eight warps; the rows
 // leave through shared memory, 16 bytes a thread.  The loads of kAtOnce parts wait together: 8 where
@@ -287,12 +473,10 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
   }
 }
 
-template <int D, int BM>
-cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
-  auto kern = chunk_attend_kernel<D, BM>;
-  LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              SimtCfg<D, BM>::kSmem));
-  LG_TRY(launch_pdl(kern, G, kThreads, SimtCfg<D, BM>::kSmem, s, a));
+cudaError_t launch_f32(void (*kern)(ChunkAttendArgs), int smem, const ChunkAttendArgs &a, int G,
+                       cudaStream_t s) {
+  LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  LG_TRY(launch_pdl(kern, G, kThreads, smem, s, a));
   return cudaGetLastError();
 }
 
@@ -308,7 +492,12 @@ cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) 
 
 template <int D>
 cudaError_t launch_d(ChunkAttendArgs &a, int G, cudaStream_t s) {
-  return a.rows == 16 ? launch_typed<D, 16>(a, G, s) : launch_typed<D, 128>(a, G, s);
+  switch (a.rows) {
+    case 4: return launch_f32(chunk_attend_few_f32_kernel<D, 4>, FewF32<D, 4>::kSmem, a, G, s);
+    case 8: return launch_f32(chunk_attend_few_f32_kernel<D, 8>, FewF32<D, 8>::kSmem, a, G, s);
+    case 16: return launch_f32(chunk_attend_few_f32_kernel<D, 16>, FewF32<D, 16>::kSmem, a, G, s);
+  }
+  return launch_f32(chunk_attend_kernel<D>, SimtCfg<D>::kSmem, a, G, s);
 }
 
 }  // namespace
@@ -324,8 +513,9 @@ cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G
 ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
   if (dtype == LG_BF16) return chunk_grid_tc(g, max_new);
   ChunkGrid r;
-  r.rows = (int64_t)max_new * g <= 16 ? 16 : 128;
-  r.ctas = 152 * (r.rows == 16 ? 2 : 1);
+  const int64_t rows = (int64_t)max_new * g;
+  r.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : kBm;
+  r.ctas = 152 * (r.rows == 4 ? 2 : 1);
   r.tok = r.rows / g;
   r.bn2 = 6;
   return r;
