@@ -1,7 +1,7 @@
 // lg_chunk_attend of fp32 caches on the CUDA cores, and the merge of shared items.
 //
-// chunk_attend_kernel's query tile is 128 rows: the g query heads of 128 / g consecutive new
-// tokens (row r: token r / g, head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
+// chunk_attend_kernel's query tile is BM (64 or 128) rows: the g query heads of BM / g consecutive
+// new tokens (row r: token r / g, head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
 // a running maximum m, normaliser l and sum o per row (log2 units):
 //   m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,  o = o 2^(m - m') + p V.
 // 256 threads as 16 x 16: thread (ty, tx) computes the scores of rows ty TM .. ty TM + TM - 1 and
@@ -31,13 +31,11 @@ __device__ __forceinline__ void store4(void *p, int64_t i, const float *f) {
   *(float4 *)((float *)p + i) = make_float4(f[0], f[1], f[2], f[3]);
 }
 
-constexpr int kBm = 128;  // rows of a query tile
-
-template <int D>
+template <int D, int BM>
 struct SimtCfg {
   static constexpr int kRow = D + 4;  // floats of a staged row: 16 rows of 16 bytes, no conflicts
   static constexpr int kSmem =
-      (kBm * kRow + kBn * kRow + kBn * D + kBm * (kBn + 4)) * (int)sizeof(float);
+      (BM * kRow + kBn * kRow + kBn * D + BM * (kBn + 4)) * (int)sizeof(float);
 };
 
 template <bool E>
@@ -45,11 +43,11 @@ struct Edge {
   static constexpr bool value = E;
 };
 
-template <int D>
+template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs a) {
-  constexpr int TM = kBm / 16, NC = D / 64, kRow = SimtCfg<D>::kRow, kPRow = kBn + 4;
+  constexpr int TM = BM / 16, NC = D / 64, kRow = SimtCfg<D, BM>::kRow, kPRow = kBn + 4;
   extern __shared__ __align__(16) float smem[];
-  float *sq = smem, *sk = sq + kBm * kRow, *sv = sk + kBn * kRow, *sp = sv + kBn * D;
+  float *sq = smem, *sk = sq + BM * kRow, *sv = sk + kBn * kRow, *sp = sv + kBn * D;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int H_q = a.H_kv * a.g;
   pdl_enter();
@@ -63,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(ChunkAttendArgs 
     const int used = w.tokens(a) * a.g;  // rows of the tile that are queries
     const int tok0 = w.off + w.t * a.shape.tok;
     __syncthreads();
-    for (int e = tid; e < kBm * (D / 4); e += kThreads) {
+    for (int e = tid; e < BM * (D / 4); e += kThreads) {
       const int r = e / (D / 4), c = e % (D / 4) * 4;
       float f[4] = {0.f, 0.f, 0.f, 0.f};
       if (r < used)
@@ -497,7 +495,9 @@ cudaError_t launch_d(ChunkAttendArgs &a, int G, cudaStream_t s) {
     case 8: return launch_f32(chunk_attend_few_f32_kernel<D, 8>, FewF32<D, 8>::kSmem, a, G, s);
     case 16: return launch_f32(chunk_attend_few_f32_kernel<D, 16>, FewF32<D, 16>::kSmem, a, G, s);
   }
-  return launch_f32(chunk_attend_kernel<D>, SimtCfg<D>::kSmem, a, G, s);
+  if (a.rows == 64)
+    return launch_f32(chunk_attend_kernel<D, 64>, SimtCfg<D, 64>::kSmem, a, G, s);
+  return launch_f32(chunk_attend_kernel<D, 128>, SimtCfg<D, 128>::kSmem, a, G, s);
 }
 
 }  // namespace
@@ -514,7 +514,7 @@ ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
   if (dtype == LG_BF16) return chunk_grid_tc(g, max_new);
   ChunkGrid r;
   const int64_t rows = (int64_t)max_new * g;
-  r.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : kBm;
+  r.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
   r.ctas = 152 * (r.rows == 4 ? 2 : 1);
   r.tok = r.rows / g;
   r.bn2 = 6;
