@@ -511,7 +511,7 @@ cudaError_t launch_chunk_merge(const ChunkAttendArgs &a, int dtype, int d, int G
 }
 
 ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
-  if (dtype == LG_BF16) return chunk_grid_tc(g, max_new);
+  if (dtype == LG_BF16) return chunk_grid_tc(d, g, max_new);
   ChunkGrid r;
   const int64_t rows = (int64_t)max_new * g;
   r.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;

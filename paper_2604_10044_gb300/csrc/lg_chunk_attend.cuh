@@ -227,7 +227,7 @@ __device__ __forceinline__ bool row_sees(const TileRows &r, const ChunkShape &s,
 }
 
 // bf16: the kernel on the tensor cores (lg_chunk_attend_tc.cu)
-ChunkGrid chunk_grid_tc(int g, int max_new);
+ChunkGrid chunk_grid_tc(int d, int g, int max_new);
 cudaError_t launch_chunk_attend_tc(const ChunkAttendArgs &a, int d, int G, cudaStream_t s);
 
 cudaError_t launch_chunk_attend_few(const ChunkAttendArgs &a, int d, int G, cudaStream_t s);

@@ -22,7 +22,7 @@
 namespace lg {
 namespace {
 
-constexpr int kBn = kTcBn;
+constexpr int kBn = 128;            // rows of a key block
 constexpr int kPBytes = kBn * 128;  // a buffer of P^T: 128-byte rows, swizzled
 constexpr float kLazy = 8.f;
 constexpr uint32_t kTmemCols = 256;
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         if (!ok) break;
         if (j >= 0 && p.hides(p.blk0 + j)) {
           const int i0 = p.blocks.index(p.blk0 + j) * kBn;
-          if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64)) p.bad = 1;
+          if (clear_block<C::kTile, kBn>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64)) p.bad = 1;
           fence_proxy_async_smem();
           __syncwarp();
         }

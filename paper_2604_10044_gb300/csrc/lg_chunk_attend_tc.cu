@@ -3,13 +3,19 @@
 // A query tile is 128 rows of the products' M: the g query heads of tok / 2 consecutive new tokens
 // (row r: token r / g, head r % g), copied as one box of the queries.  An item has two tiles
 // ("streams"), so that every key block serves 256 query rows and the products of one stream run
-// while the other's weights are formed.  For each key block of 128 rows
+// while the other's weights are formed.  For each key block of 128 rows (64 for heads of 64 elements)
 //   S = Q K^T   (tensor memory, fp32),  P = 2^(S scale - m) (bf16, over S),  O += P V
 // with the running maximum m and normaliser l in registers, one thread a row.  m follows the true
 // maximum lazily: O and l are rescaled only when a maximum rose by more than 2^8, so that the
 // rescaling, a pass over O in tensor memory, happens in the first blocks only; weights up to 2^8
 // lose nothing in bf16 or in the fp32 sums.  P is rounded to bf16 (half a step, 2^-8 of a weight at
 // most: the precision of the values it multiplies); l sums the unrounded weights in fp32.
+//
+// Heads of 128 elements: the products of a stream take as long as its weights, S and O of two streams
+// fill the tensor memory, and a stream's next scores follow its sums.  Heads of 64: half the products
+// for the same weights, so the weights are the bound; blocks of 64 keys leave room for two buffers of
+// S a stream, scores are formed two blocks ahead, and the rows' warps never wait for them.  (Products
+// with N = 64 read the queries as often as the keys, 1.5 x the time of N = 128: too slow for 128.)
 //
 // Warps: 0-3 and 4-7 the rows of streams 0 and 1; 8 walks along the work and copies (TMA), 9 and 10
 // issue the products of a stream each, 11 clears what is not a number from the values of blocks in which some row is hidden from some query
@@ -21,17 +27,18 @@ namespace lg {
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kBn = kTcBn;
 constexpr float kLazy = 8.f;        // log2 of the factor that m may lag behind
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColO = 256;     // S at columns 0 and 128, O at 256 and 256 + D
+constexpr uint32_t kColO = 256;     // S below column 256 (a stream's buffers together), O from there
 
 template <int D>
 struct TcCfg {
+  static constexpr int kBn = D == 128 ? 128 : 64;       // rows of a key block
+  static constexpr int kBufs = 128 / kBn;               // buffers of S of a stream
   static constexpr int kBoxes = D / 64;                 // boxes of 64 columns
   static constexpr int kTile = kBn * D * 2;             // bytes of a key or value block
   static constexpr int kQTile = 128 * D * 2;
-  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kStages = D == 128 ? 5 : 16;
   static constexpr int kSmem = 2 * kQTile + kStages * kTile + 1024;  // + alignment
 };
 
@@ -40,8 +47,10 @@ struct TcBars {
   uint64_t full[ST], empty[ST];      // ring of key and value blocks
   uint64_t fixed[ST];                // what hidden rows hold is cleared
   uint64_t q_full, q_empty;
-  uint64_t s_full[2], p_half[2], p_full[2];  // scores ready, half of and all weights ready
-  uint64_t o_full[2], o_free[2];     // sums ready, sums read
+  // of stream s and buffer b, at 2 s + b: scores ready, half of and all weights ready, sums ready (with
+  // one buffer: the piece's)
+  uint64_t s_full[4], p_half[4], p_full[4], o_full[4];
+  uint64_t o_free[2];                // sums read
   uint64_t turn[2];                  // the stream's products are next
   TcQueue queue;
   uint32_t tmem;
@@ -69,7 +78,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                            const __grid_constant__ CUtensorMap mk,
                            const __grid_constant__ CUtensorMap mv, ChunkAttendArgs a) {
   using C = TcCfg<D>;
-  constexpr int ST = C::kStages;
+  constexpr int ST = C::kStages, kBn = C::kBn, NB = C::kBufs;
   extern __shared__ uint8_t smem_raw[];
   __shared__ TcBars<ST> bars;
   uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -85,11 +94,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(&bars.q_full, 1);
     mbar_init(&bars.q_empty, 2);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&bars.s_full[i], 1);
       mbar_init(&bars.p_half[i], 4);
       mbar_init(&bars.p_full[i], 4);
       mbar_init(&bars.o_full[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.o_free[i], 4);
       mbar_init(&bars.turn[i], 1);
     }
@@ -140,10 +151,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               tma_box_3d(sq + s * C::kQTile + x * (128 * 128), &mq, 64 * x, w.kvh * a.g,
                          w.off + w.t * a.shape.tok + s * tpt, &bars.q_full);
           ++pieces;
+          // keys NB blocks ahead of the values, as the products take them
+          auto row = [&](int j) { return (int)w.row0 + w.blocks.index(j) * kBn; };
+          for (int j = w.blk0; ok && j < w.blk1 && j < w.blk0 + NB; ++j) load(&mk, row(j));
           for (int j = w.blk0; ok && j < w.blk1; ++j) {
-            const int row = (int)w.row0 + w.blocks.index(j) * kBn;
-            load(&mk, row);
-            load(&mv, row);
+            load(&mv, row(j));
+            if (j + NB < w.blk1) load(&mk, row(j + NB));
           }
         }
         if (ok) bars.queue.end(bars, pieces);
@@ -160,22 +173,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       constexpr uint32_t kIdS = mma_idesc(128, kBn, false, false);
       constexpr uint32_t kIdO = mma_idesc(128, D, false, true);
-      const uint32_t ts = tmem + s * 128, to = tmem + kColO + s * D;
+      const uint32_t ts0 = tmem + s * 128, to = tmem + kColO + s * D;
       const uint32_t q_lo = desc_lo(smem_addr(sq + s * C::kQTile), 16);
       const uint32_t k_lo = desc_lo(smem_addr(ring), 16), v_lo = desc_lo(smem_addr(ring), kBn * 128);
       auto wait_full = [&](uint32_t i) {
         ok = ok && tc_wait_warp(bars, &bars.full[i % ST], (i / ST) & 1);
       };
-      // S = Q K^T with the key block at ring position i (which has arrived)
-      auto qk = [&](uint32_t i, bool last) {
+      // S = Q K^T into buffer b with the key block at ring position i (which has arrived)
+      auto qk = [&](uint32_t b, uint32_t i, bool last) {
         const uint32_t k0 = k_lo + i % ST * (C::kTile >> 4);
         if (one) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint32_t at = ((k / 4) * (128 * 128) + (k % 4) * 32) >> 4;
-            tc_mma_ss(ts, q_lo + at, k0 + at, kIdS, k > 0);
+            tc_mma_ss(ts0 + b * kBn, q_lo + (((k / 4) * (128 * 128) + (k % 4) * 32) >> 4),
+                      k0 + (((k / 4) * (kBn * 128) + (k % 4) * 32) >> 4), kIdS, k > 0);
           }
-          tc_commit(&bars.s_full[s]);
+          tc_commit(&bars.s_full[2 * s + b]);
           tc_commit(&bars.empty[i % ST]);
           if (last) tc_commit(&bars.q_empty);
         }
@@ -201,24 +214,29 @@ __global__ void __launch_bounds__(kThreads, 1)
           continue;
         }
         ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
-        wait_full(n);
-        if (!ok) break;
-        tc_fence_after();
-        qk(n, blocks == 1);
-        ok = tc_wait_warp(bars, &bars.o_free[s], (mine & 1) ^ 1);
+        const int ahead = blocks < NB ? blocks : NB;
+        for (int i = 0; i < ahead; ++i) {
+          wait_full(n + i);
+          if (!ok) break;
+          tc_fence_after();
+          qk((c + i) % NB, n + i, i + 1 == blocks);
+        }
+        ok = ok && tc_wait_warp(bars, &bars.o_free[s], (mine & 1) ^ 1);
         ++mine;
         for (int j = 0; ok && j < blocks; ++j, ++c) {
-          const uint32_t iv = n + 2 * j + 1;
+          // (value block j follows the keys ahead of it and j pairs, or what pairs there are)
+          const uint32_t iv = n + ahead + j + (j < blocks - ahead ? j : blocks - ahead);
+          const uint32_t b = c % NB, par = (c / NB) & 1, ts = ts0 + b * kBn;
           if (j < open0 || j >= open1)
             ok = tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
           else
             wait_full(iv);
-          if (j + 1 < blocks) wait_full(iv + 1);
-          ok = ok && tc_wait_warp(bars, &bars.p_half[s], c & 1);
-          if (two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));
+          if (j + NB < blocks) wait_full(iv + 1);
+          ok = ok && tc_wait_warp(bars, &(NB == 1 ? bars.p_half : bars.p_full)[2 * s + b], par);
+          if (NB == 1 && two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));
           if (!ok) break;
           tc_fence_after();
-          // O += P V, the block's first half while the second one's weights are formed
+          // O += P V (one buffer: the block's first half while the second one's weights are formed)
           const uint32_t v0 = v_lo + iv % ST * (C::kTile >> 4);
           auto pv = [&](int k0) {
             if (one) {
@@ -229,16 +247,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           };
           pv(0);
-          ok = tc_wait_warp(bars, &bars.p_full[s], c & 1);
-          if (!ok) break;
-          tc_fence_after();
-          pv(kBn / 32);
-          if (j + 1 < blocks) {
-            qk(iv + 1, j + 2 == blocks);
-          } else if (one) {
-            tc_commit(&bars.o_full[s]);
+          if (NB == 1) {
+            ok = tc_wait_warp(bars, &bars.p_full[2 * s + b], par);
+            if (!ok) break;
+            tc_fence_after();
           }
-          if (two) {
+          pv(kBn / 32);
+          if (one && (NB == 2 || j + 1 == blocks)) tc_commit(&bars.o_full[2 * s + b]);
+          if (j + NB < blocks) qk(b, iv + 1, j + NB + 1 == blocks);
+          if (NB == 1 && two) {
             if (one) mbar_arrive(&bars.turn[s ^ 1]);
             ++turns;
           }
@@ -256,13 +273,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         TcPiece &p = bars.queue.at(pc);
         if (p.blk1 < 0) break;
         const int blocks = p.blk1 - p.blk0;
+        const int ahead = blocks < NB ? blocks : NB;
         for (int i = 0; i < 2 * blocks; ++i, ++n) {
           ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.full[n % ST], (n / ST) & 1));
           if (!ok) break;
-          // keys and values in turn
-          if ((i & 1) && p.hides(p.blk0 + (i >> 1))) {
-            const int i0 = p.blocks.index(p.blk0 + (i >> 1)) * kBn;
-            if (clear_block<C::kTile>(ring + n % ST * C::kTile, i0, p.n, lane, 32)) p.bad = 1;
+          // the i-th copy of the piece: keys ahead, then values and keys in turn, then values
+          const int x = i - ahead, pairs = blocks - ahead;
+          const int j = x < 0 ? -1 : x >= 2 * pairs ? x - pairs : x & 1 ? -1 : x >> 1;
+          if (j >= 0 && p.hides(p.blk0 + j)) {
+            const int i0 = p.blocks.index(p.blk0 + j) * kBn;
+            if (clear_block<C::kTile, kBn>(ring + n % ST * C::kTile, i0, p.n, lane, 32)) p.bad = 1;
             fence_proxy_async_smem();
             __syncwarp();
           }
@@ -280,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int s = warp >> 2;                  // stream
     const int r = tid & 127;                  // row of the tile
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // lane 32 (warp % 4) in bits 16..
-    const uint32_t to = tmem + kColO + s * D + lanes, ts = tmem + s * 128 + lanes;
+    const uint32_t to = tmem + kColO + s * D + lanes;
     const int j_tok = s * tpt + r / a.g;      // token of the row in the item
     uint32_t c = 0, mine = 0;                 // blocks and pieces of this stream so far
     bool ok = true;
@@ -300,7 +320,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int blk = blk0; blk < blk1; ++blk, ++c) {
           const int i0 = p.blocks.index(blk) * kBn;
           const bool hides = p.hides(blk);
-          ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[s], c & 1));
+          const uint32_t b = c % NB, ts = tmem + s * 128 + b * kBn + lanes;
+          ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[2 * s + b], (c / NB) & 1));
           if (!ok) break;
           if (!idle) {
             tc_fence_after();
@@ -328,12 +349,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.qscale;
             const bool rise = top > m + kLazy || m == -INFINITY;
             if (__any_sync(0xffffffffu, rise)) {
+              if (NB == 2 && blk > blk0) {
+                ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[2 * s + (c - 1) % NB],
+                                                     ((c - 1) / NB) & 1));
+                if (!ok) break;
+                tc_fence_after();
+              }
               const float m1 = rise ? fmaxf(m, top) : m;
               const float f = rise ? (m == -INFINITY ? 0.f : exp2_fast(m - m1)) : 1.f;
               m = m1;
               l2.x *= f;
               l2.y *= f;
-              if (blk > blk0) {  // (the scores were formed after the previous block's sums)
+              if (blk > blk0) {  // (with one buffer the scores followed the previous block's sums)
 #pragma unroll 1
                 for (int x = 0; x < D; x += 16) {
                   uint32_t o[16];
@@ -360,11 +387,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 h[e] = *(const uint32_t *)&y;
               }
               tmem_store16(ts + x / 2, h);  // over scores that have been read
-              if (x == kBn / 2 - 32) {
+              if (NB == 1 && x == kBn / 2 - 32) {
                 tmem_wait_store();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.p_half[s]);
+                if (lane == 0) mbar_arrive(&bars.p_half[2 * s + b]);
               }
             }
             tmem_wait_store();
@@ -372,12 +399,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
           if (lane == 0) {
-            if (idle) mbar_arrive(&bars.p_half[s]);
-            mbar_arrive(&bars.p_full[s]);
+            if (NB == 1 && idle) mbar_arrive(&bars.p_half[2 * s + b]);
+            mbar_arrive(&bars.p_full[2 * s + b]);
           }
         }
         if (!ok) break;
-        ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[s], mine & 1));
+        // (two buffers: the last block's sums; one: the piece's)
+        ok = __all_sync(0xffffffffu, NB == 2 ? tc_wait(bars, &bars.o_full[2 * s + (c - 1) % NB],
+                                                       ((c - 1) / NB) & 1)
+                                             : tc_wait(bars, &bars.o_full[2 * s], mine & 1));
         if (!ok) break;
         ++mine;
         tc_fence_after();
@@ -471,8 +501,8 @@ template <int D>
 cudaError_t launch_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
   CUtensorMap mq, mk, mv;
   if (!make_q_map(&mq, a.q, D, a.H_kv * a.g, a.T, a.g, a.shape.tok / 2) ||
-      !make_kv_map(&mk, a.K, LG_BF16, D, a.cache_rows, kBn) ||
-      !make_kv_map(&mv, a.V, LG_BF16, D, a.cache_rows, kBn))
+      !make_kv_map(&mk, a.K, LG_BF16, D, a.cache_rows, TcCfg<D>::kBn) ||
+      !make_kv_map(&mv, a.V, LG_BF16, D, a.cache_rows, TcCfg<D>::kBn))
     return cudaErrorInvalidValue;
   auto kern = chunk_attend_tc_kernel<D>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<D>::kSmem));
@@ -495,14 +525,14 @@ bool make_q_map(CUtensorMap *m, const void *q, int d, int H_q, int T, int g, int
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-ChunkGrid chunk_grid_tc(int g, int max_new) {
+ChunkGrid chunk_grid_tc(int d, int g, int max_new) {
   ChunkGrid r;
   const int64_t rows = (int64_t)max_new * g;
   // few rows: the kernel that takes them as the products' N (lg_chunk_attend_few.cu)
   r.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
   r.ctas = 152;
   r.tok = r.rows == 256 ? 128 / g * 2 : r.rows / g;
-  r.bn2 = 7;
+  r.bn2 = r.rows == 256 && d == 64 ? 6 : 7;  // TcCfg<D>::kBn
   return r;
 }
 

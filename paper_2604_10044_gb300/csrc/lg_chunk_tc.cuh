@@ -8,8 +8,6 @@
 
 namespace lg {
 
-constexpr int kTcBn = 128;  // rows of a key block
-
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -65,7 +63,7 @@ __device__ __forceinline__ uint32_t not_numbers(uint32_t w) {
 
 // Clears a value block from row i0 of a sequence of n rows, `nthreads` threads together; whether
 // something of the sequence's own rows was cleared (by this thread).
-template <int BYTES>
+template <int BYTES, int BN>
 __device__ __forceinline__ bool clear_block(uint8_t *block, int i0, int n, int t, int nthreads) {
   uint4 *v = (uint4 *)block;
   bool bad = false;
@@ -79,7 +77,7 @@ __device__ __forceinline__ bool clear_block(uint8_t *block, int i0, int n, int t
         uw[x] &= (b & 0x8000u ? 0u : 0xffffu) | (b & 0x80000000u ? 0u : 0xffff0000u);
       }
       v[e] = u;
-      bad |= i0 + e / 8 % kTcBn < n;
+      bad |= i0 + e / 8 % BN < n;
     }
   }
   return bad;
