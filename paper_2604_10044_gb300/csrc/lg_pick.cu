@@ -130,8 +130,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
   __shared__ Top s_top[NT / 32];
   __shared__ float s_max[NT / 32];
   __shared__ Top s_ranks[kMaxCluster];
-  __shared__ int s_aside, s_fit;        // tokens to be listed; entries of the list that hold one
-  __shared__ uint32_t s_list[kAside];   // token, bit 30: seen, bit 31: biased
+  __shared__ int s_aside, s_fit;    // seen tokens to be listed; entries of the list that hold one
+  __shared__ int s_list[kAside];
+  __shared__ int s_twice;           // some token is biased more than once
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.x / csize, rank = blockIdx.x % csize;
   if (csize > 1)  // (waited for before anything is sent: the peers have started)
@@ -140,6 +141,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
   if (tid == 0) {
     s_aside = 0;
     s_fit = kAside;
+    s_twice = 0;
   }
   const bool skip = cta_status_bad(a.status);
   Top top{-INFINITY, 0.f, INT_MAX};  // of the tokens processed one by one
@@ -161,44 +163,30 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
       b0 = a.bias_off[b];
       b1 = a.bias_off[b + 1];
     }
-    // one token's processed logit
-    auto process = [&](float v, int t, bool was_seen, bool biased, int n) {
-      if (was_seen) {
-        v = v > 0.f ? __fdiv_rn(v, pen.x) : __fmul_rn(v, pen.x);
-        if (n > 0) v = __fsub_rn(__fsub_rn(v, __fmul_rn(pen.z, (float)n)), pen.y);
-      }
-      if (biased)
-#pragma unroll 4
-        for (int e = b0; e < b1; ++e)
-          if (a.bias_id[e] == t) v = __fadd_rn(v, a.bias_val[e]);
-      return v == v ? v : -INFINITY;
+    // the penalties of a seen token with its count
+    auto penalised = [&](float v, int n) {
+      v = v > 0.f ? __fdiv_rn(v, pen.x) : __fmul_rn(v, pen.x);
+      return n > 0 ? __fsub_rn(__fsub_rn(v, __fmul_rn(pen.z, (float)n)), pen.y) : v;
     };
     // one more token
     auto add = [&](float v, int t) { top = merge(top, Top{v, v == -INFINITY ? 0.f : 1.f, t}); };
+    auto finish = [&](float v, int t) {  // a token processed by itself
+      v = v == v ? v : -INFINITY;
+      if (out) Elem<T>::store(out, t, v);
+      add(v, t);
+    };
     // n listed tokens, their logits and counts read together
-    auto apart = [&](const uint32_t *entry, int n) {
+    auto apart = [&](const int *t, int n) {
       float v[kAhead];
       int c[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int t = (int)(entry[k] & 0x3fffffffu);
-        v[k] = k < n ? Elem<T>::load(x, t) : 0.f;
-        c[k] = k < n && (entry[k] >> 30 & 1) ? counts[t] : 0;
+        v[k] = k < n ? Elem<T>::load(x, t[k]) : 0.f;
+        c[k] = k < n ? counts[t[k]] : 0;
       }
-#pragma unroll 1
-      for (int k = 0; k < n; ++k) {
-        float w = v[0];
-        int cn = c[0];
 #pragma unroll
-        for (int j = 1; j < kAhead; ++j) {
-          w = k == j ? v[j] : w;
-          cn = k == j ? c[j] : cn;
-        }
-        const int t = (int)(entry[k] & 0x3fffffffu);
-        w = process(w, t, entry[k] >> 30 & 1, entry[k] >> 31, cn);
-        if (out) Elem<T>::store(out, t, w);
-        add(w, t);
-      }
+      for (int k = 0; k < kAhead; ++k)
+        if (k < n) finish(penalised(v[k], c[k]), t[k]);
     };
 
     // the bits: every token, or the allowed ones, but for the seen and biased ones
@@ -209,33 +197,32 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
           (allowed ? __ldg(allowed + w0 + i) : ~0u) & (left >= 32 ? ~0u : (1u << left) - 1);
       s_ok[i] = ok;
       s_pass[i] = ok;
-      s_apart[i] = seen ? seen[w0 + i] & ok : 0u;
+      s_apart[i] = seen ? __ldg(seen + w0 + i) & ok : 0u;
       s_bias[i] = 0;
     }
     if (b0 < b1) {
       __syncthreads();
       for (int e = b0 + tid; e < b1; e += NT) {
         const int t = a.bias_id[e] - lo;
-        if (t >= 0 && t < hi - lo) atomicOr(&s_bias[t >> 5], s_pass[t >> 5] & 1u << (t & 31));
+        if (t >= 0 && t < hi - lo) {
+          const uint32_t bit = s_pass[t >> 5] & 1u << (t & 31);
+          if (atomicOr(&s_bias[t >> 5], bit) & bit) s_twice = 1;
+        }
       }
       __syncthreads();
     }
-    auto entry = [&](int i, int j, uint32_t was_seen) {  // token j of word i
-      return (uint32_t)(lo + 32 * i + j) | (was_seen >> j & 1u) << 30 | (s_bias[i] >> j & 1u) << 31;
-    };
     for (int i = tid; i < nw; i += NT) {
-      const uint32_t was_seen = s_apart[i];
-      uint32_t w = was_seen | s_bias[i];
+      uint32_t w = s_apart[i] & ~s_bias[i];
+      s_pass[i] &= ~(w | s_bias[i]);
       if (w == 0) continue;
-      s_pass[i] &= ~w;
       int at = atomicAdd(&s_aside, __popc(w));
+      s_apart[i] = 0;
       if (at + __popc(w) > kAside) {  // (the word stays, and so does every later one)
         s_apart[i] = w;
         atomicMin(&s_fit, at);
         continue;
       }
-      s_apart[i] = 0;
-      for (; w; w &= w - 1) s_list[at++] = entry(i, __ffs((int)w) - 1, was_seen);
+      for (; w; w &= w - 1) s_list[at++] = lo + 32 * i + __ffs((int)w) - 1;
     }
     __syncthreads();
 
@@ -331,21 +318,36 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
     if (s_aside > kAside)
       for (int i = tid; i < nw; i += NT)
         for (uint32_t w = s_apart[i]; w; w &= w - 1) {
-          uint32_t e[kAhead] = {entry(i, __ffs((int)w) - 1, seen ? seen[w0 + i] : 0u)};
-          apart(e, 1);
+          const int t[kAhead] = {lo + 32 * i + __ffs((int)w) - 1};
+          apart(t, 1);
         }
     for (int i = tid; i < listed; i += kAhead * NT) {
-      uint32_t e[kAhead];
-      int n = 0;
+      int t[kAhead], n = 0;
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        e[k] = 0;
+        t[k] = 0;
         if (i + k * NT < listed) {
-          e[k] = s_list[i + k * NT];
+          t[k] = s_list[i + k * NT];
           n = k + 1;
         }
       }
-      apart(e, n);
+      apart(t, n);
+    }
+    // biased tokens: the first thread to take a token's bit processes it
+    for (int e = b0 + tid; e < b1; e += NT) {
+      const int t = a.bias_id[e];
+      if (t < lo || t >= hi) continue;
+      const uint32_t bit = 1u << ((t - lo) & 31);
+      if (!(atomicAnd(&s_bias[(t - lo) >> 5], ~bit) & bit)) continue;
+      float v = Elem<T>::load(x, t);
+      if (seen && (seen[t >> 5] >> (t & 31) & 1)) v = penalised(v, counts[t]);
+      if (s_twice) {
+        for (int f = b0; f < b1; ++f)
+          if (a.bias_id[f] == t) v = __fadd_rn(v, a.bias_val[f]);
+      } else {
+        v = __fadd_rn(v, a.bias_val[e]);
+      }
+      finish(v, t);
     }
     // the CTA's maximum; the token only from threads whose vectors have it
     const float wm = warp_max(fmaxf(m, top.m));
