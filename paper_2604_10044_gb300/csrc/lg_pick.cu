@@ -121,6 +121,7 @@ __device__ __forceinline__ Top warp_top(const Top &t) {
 }
 
 constexpr int kMaxCluster = 16;
+constexpr int kMaxSlice = 320 << 10;  // tokens of a CTA: 16 bytes of bits for every 32
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, int csize) {
@@ -448,13 +449,17 @@ cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
 }
 
 // CTAs a row: as many as fit the GPU at once (a kernel of 512 threads twice an SM, of 256 four
-// times), at most 16, each with 2048 tokens or more.
+// times), at most 16, each with 2048 tokens or more, and enough that a slice's bits fit shared memory.
+// (GB300, 192 rows of 128257 bf16 logits, 256 threads: 2 CTAs a row 57 us, 3 39.5, 4 45, 8 50, 16 72;
+// one row of 151936 fp32, 512 threads: 4 CTAs 11.1 us, 8 8.8, 16 7.1, and 16 of 256 threads 8.3.)
 template <typename T>
 cudaError_t launch_pick_sized(PickArgs &a, int batch, cudaStream_t s) {
   const int nt = batch * kMaxCluster <= 2 * 152 ? 512 : 256;
   int c = (nt == 512 ? 2 : 4) * 152 / batch, most = a.V / 2048;
   c = c < 1 ? 1 : c > kMaxCluster ? kMaxCluster : c;
   c = c > most ? (most < 1 ? 1 : most) : c;
+  const int least = (a.V + kMaxSlice - 1) / kMaxSlice;
+  c = c < least ? least : c;
   if (nt == 512) return launch_pick_typed<T, 512>(a, batch, c, s);
   return launch_pick_typed<T, 256>(a, batch, c, s);
 }

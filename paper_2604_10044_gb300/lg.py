@@ -360,6 +360,8 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
     """q [T][H_q][d] (or None with q_out None), k_new, v_new [T][H_kv][d]: slices of one packed
     projection pass as they are"""
     H_q = 0 if q is None else q.shape[1]
+    if q_out is not None and not q_out.is_contiguous():
+        raise ValueError("q_out: dense [T][H_q][d]")
     _call("lg_rope_append", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, _ptr(q),
           0 if q is None else _rows_stride(q, "q"), H_q, _ptr(k_new),
           _rows_stride(k_new, "k_new"), _ptr(v_new), _rows_stride(v_new, "v_new"), _ptr(pos),
@@ -373,6 +375,8 @@ def lg_chunk_workspace_size(cache, chunk, H_q, max_len) -> int:
 
 def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max_len, ws,
                     stream=None):
+    if not (q.is_contiguous() and out.is_contiguous()):
+        raise ValueError("q, out: dense [T][H_q][d]")
     _call("lg_chunk_attend", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, _ptr(q), H_q,
           float(scale), window, n_sink, _ptr(out), max_len, _ptr(ws),
           ws.numel() * ws.element_size(), _stream(stream))

@@ -176,6 +176,10 @@ def test_binding_refuses_broken_rows():
         with pytest.raises(ValueError):
             lg._rows_stride(bad, "x")
     with pytest.raises(ValueError):
+        lg.lg_chunk_attend(None, None, 0, x.transpose(0, 1), 4, 1.0, 0, 0, x, 8, x)
+    with pytest.raises(ValueError):
+        lg.lg_rope_append(None, None, 0, x, x, x, x, None, x.transpose(0, 1), None)
+    with pytest.raises(ValueError):
         lg.lg_pick_token(torch.zeros(3, 8).t(), None, None, None, None, None, None, None)
     with pytest.raises(ValueError):
         lg.lg_pick_token(torch.zeros(3, 8), None, None, None, None, None, None, None,

@@ -148,6 +148,24 @@ def test_rows_with_nothing_left_and_infinities(cuda):
     _run(cuda, x.bfloat16(), allowed=allowed)
 
 
+def test_large_vocabulary_and_batch(cuda):
+    """a row's bits take several CTAs' shared memory although the batch alone fills the GPU"""
+    B, V = 400, 350003
+    x = torch.zeros((B, V), dtype=torch.bfloat16, device=cuda)
+    at = torch.arange(B, device=cuda) * 875 % V
+    x[torch.arange(B, device=cuda), at] = 3.0
+    tok = torch.zeros(B, dtype=torch.int32, device=cuda)
+    pm = torch.zeros(B, device=cuda)
+    lg.lg_pick_token(x, None, None, None, None, None, tok, pm)
+    assert torch.equal(tok.long(), at)
+    want = 1.0 / (1.0 + (V - 1) * math.exp(-3.0))
+    assert ((pm - want).abs() <= want * (V * 2.0 ** -24 + 2.0 ** -20)).all()
+    x = torch.zeros((2, 1 << 20), device=cuda)     # the largest vocabulary
+    x[0, -1] = x[1, 777777] = 1.0
+    lg.lg_pick_token(x, None, None, None, None, None, tok[:2], pm[:2])
+    assert tok[:2].tolist() == [(1 << 20) - 1, 777777]
+
+
 def test_bias_lists(cuda):
     """empty lists, one token twice, tokens outside the vocabulary, long lists"""
     V = 3001
