@@ -74,6 +74,22 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
     return v;
   };
   const bool stop = lane == 0 && status_bad(a.status);
+  if (a.batch == 1) {  // nothing to search (the shortest call's latency is mostly this and its like)
+    load(0);
+    if (bad) set_status(a.status, LG_ERR_CAPACITY);
+    if (__any_sync(0xffffffffu, bad || stop)) return false;
+    sh.W = a.H_kv * c;
+    sh.step = range_step(sh.W, G, a.shape.bn2);
+    sh.y0 = cta * sh.step;
+    sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
+    sh.x = 0;
+    sh.per_head = c;
+    sh.slot = slot;
+    sh.q = q;
+    sh.off = off;
+    sh.b = 0;
+    return sh.y0 < sh.W;
+  }
   load(lane);
   int64_t incl = scan(a.H_kv * c);
   sh.W = __shfl_sync(0xffffffffu, incl, 31);
