@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r = tid & 127;                  // row of the tile
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // lane 32 (warp % 4) in bits 16..
     const uint32_t to = tmem + kColO + s * D + lanes;
-    const int j_tok = s * tpt + r / a.g;      // token of the row in the item
+    const int j_tok = s * tpt + r / a.g, head = r % a.g;  // the row's token in the item, and its head
     uint32_t c = 0, mine = 0;                 // blocks and pieces of this stream so far
     bool ok = true;
     for (uint32_t pc = 0; ok; ++pc) {
@@ -316,10 +316,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int hid = a.shape.window ? max(qrow - a.shape.window, -1) : -1;
         float m = -INFINITY;
         float2 l2 = make_float2(0.f, 0.f);
-        const int blk0 = p.blk0, blk1 = p.blk1;
+        const int blk0 = p.blk0, blk1 = p.blk1, open0 = p.open0, open1 = p.open1;
+        const bool alive = r < used;
         for (int blk = blk0; blk < blk1; ++blk, ++c) {
-          const int i0 = p.blocks.index(blk) * kBn;
-          const bool hides = p.hides(blk);
+          const bool hides = blk < open0 || blk >= open1;
           const uint32_t b = c % NB, ts = tmem + s * 128 + b * kBn + lanes;
           ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.s_full[2 * s + b], (c / NB) & 1));
           if (!ok) break;
@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int x = 0; x < kBn; x += 32) tmem_load32(ts + x, u + x);
             tmem_wait_load();
             if (hides) {
+              const int i0 = p.blocks.index(blk) * kBn;
 #pragma unroll
               for (int x = 0; x < kBn; x += 32) {
                 const uint32_t see = rows_seen(a.shape, qrow, hid, i0 + x);
@@ -347,7 +348,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], v[e + x], v[e + x + 4]);
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.qscale;
-            const bool rise = top > m + kLazy || m == -INFINITY;
+            // (rows that are no query may hold anything, a NaN in every block too)
+            const bool rise = alive && (top > m + kLazy || m == -INFINITY);
             if (__any_sync(0xffffffffu, rise)) {
               if (NB == 2 && blk > blk0) {
                 ok = __all_sync(0xffffffffu, tc_wait(bars, &bars.o_full[2 * s + (c - 1) % NB],
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           int64_t dst[4];
           {
             const int64_t own =
-                r < used ? ((int64_t)(p.tok0 + j_tok) * (a.H_kv * a.g) + p.kvh * a.g + r % a.g) * D
+                r < used ? ((int64_t)(p.tok0 + j_tok) * (a.H_kv * a.g) + p.kvh * a.g + head) * D
                          : -1;
 #pragma unroll
             for (int i = 0; i < 4; ++i) dst[i] = __shfl_sync(0xffffffffu, own, (lane & 28) + i);
