@@ -102,11 +102,13 @@ LG_API size_t lg_chunk_workspace_size(const lg_cache *c, const lg_chunk *ch, int
    window > 0 only those with i > r - window or i < n_sink (a sliding window and first rows that
    stay visible; window counts the query's own row).
      out[t][h][:] = sum_i a_i v_i,  a = softmax_i(<q[t][h], k_i> * scale) over the rows seen
-   q: device [T][H_q][d] dense, dtype; out: device same shape, dtype, may not overlap q.  Query head h reads kv-head
-   h / (H_q/H_kv).  What lies in rows that a query does not see never reaches its result, whatever
-   it holds.  max_len: host bound on every len[b] (a longer sequence sets LG_ERR_CAPACITY, as does
-   an m_b above max_new or len[b], or an off[] outside [0, T]; nothing of that call's output is
-   then defined).
+   q: device [T][H_q][d] dense, dtype; out: device same shape, dtype, may not overlap q.  Query
+   head h reads kv-head h / (H_q/H_kv).  What lies in rows that a query does not see never reaches
+   its result, whatever it holds.  bf16: the weights enter the product with the values in bf16;
+   scores and sums are fp32.  max_len: host bound on every len[b], best a near one, as the division
+   of the work (and so the order of sums) goes by it.  A longer sequence sets LG_ERR_CAPACITY, as
+   does an m_b above max_new or len[b], or an off[] outside [0, T]; nothing of that call's output is
+   then defined.
    ws: device workspace of lg_chunk_workspace_size bytes, 256-byte aligned, any contents; calls
    that may overlap on the GPU need one each. */
 LG_API lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, const void *q,

@@ -29,41 +29,44 @@ struct ChunkAttendArgs {
   ChunkShape shape;
 };
 
-// a CTA's share: cost units [y0, y1) of the line of W, and the sequence that y0 falls into
+// a CTA's share: cost units [y0, y1) of its line of W, and the item that y0 falls into
 struct ChunkShare {
   int64_t y0, y1, W, step;
-  int64_t x;         // where sequence b starts in the line
-  int64_t per_head;  // cost of a kv-head's tiles
-  int64_t slot;      // its first cache slot
+  int64_t x;         // where the item starts in the line
+  int64_t slot;      // its sequence's first cache slot
   ChunkSeq q;
-  int b, off;        // off: its first token row
+  int b, off;        // off: its sequence's first token row
+  int kvh, t;
+  int lane;          // the line
 };
 
 // The share of CTA `cta` of G, which may be empty; false when it starts at the end of the line, the
 // device status is set or a length is out of its bounds (recorded).  Every lane of a warp calls it;
-// a batch of at most 32 is read once, in one round trip.  ONE: no sequence has more than one tile.
+// a batch of at most 32 is read once, in one round trip.  ONE: no sequence has more than one tile,
+// and there is one line.
 template <bool ONE>
 __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, int G,
                                             ChunkShare &sh) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, ctas = ONE ? G : G >> a.shape.lanes2;
+  sh.lane = ONE ? 0 : cta / ctas;
   bool bad = false;
   int off = 0;
-  int64_t slot = 0, c = 0;
+  int64_t slot = 0, c = 0, head = 0;
   ChunkSeq q{0, 0};
-  auto load = [&](int b) {  // a lane's sequence and the cost of one kv-head of it
-    c = 0;
+  auto load = [&](int b) {  // a lane's sequence, and its cost in the line: `head` a kv-head (or as many
+    c = head = 0;           // as there are lines)
     if (b >= a.batch) return;
     off = a.off[b];
     const int end = a.off[b + 1];
     q = ChunkSeq{a.len[b], end - off};
     slot = a.seq_off[b];
     if (q.n < 0 || q.n > a.max_len || q.m < 0 || q.m > a.max_new || q.m > q.n || off < 0 ||
-        end > a.T)
+        end > a.T) {
       bad = true;
-    else if (ONE)
-      c = q.m ? tile_cost(q, a.shape, 0) : 0;
-    else
-      c = tiles_cost(q, a.shape, q.tiles(a.shape.tok));
+    } else {
+      head = !ONE ? head_cost(q, a.shape) : q.m ? tile_cost(q, a.shape, 0) : 0;
+      c = (ONE ? a.H_kv : a.H_kv >> a.shape.lanes2) * head;
+    }
   };
   auto scan = [&](int64_t v) {  // inclusive prefix over the lanes
 #pragma unroll
@@ -73,57 +76,90 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
     }
     return v;
   };
+  auto range = [&] {
+    const int k = ONE ? cta : cta - sh.lane * ctas;
+    sh.step = range_step(sh.W, ctas, a.shape.bn2);
+    sh.y0 = plan_min(sh.W, k * sh.step);
+    sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
+    return sh.y0 < sh.W;
+  };
+  auto item = [&](int64_t per) {  // of sequence sh.b, which starts at sh.x
+    const ChunkSeq q = sh.q;
+    const int k = (int)plan_div(sh.y0 - sh.x, per);
+    sh.x += k * per;
+    sh.kvh = k;
+    sh.t = 0;
+    if (ONE) return;
+    if (a.shape.lanes2) {  // which of the group's kv-heads: a lane each
+      const int lanes = 1 << a.shape.lanes2;
+      sh.kvh = k * lanes;
+      const int r = first_tile(a.shape, sh.lane, sh.kvh + lane);
+      const int64_t mine = lane < lanes ? tiles_cost(q, a.shape, r, lane_tiles(q, a.shape, r)) : 0;
+      const int64_t incl = scan(mine);
+      const int f = __ffs((int)__ballot_sync(0xffffffffu, sh.x + incl > sh.y0)) - 1;
+      sh.x += __shfl_sync(0xffffffffu, incl - mine, f);
+      sh.kvh += f;
+    }
+    // the last tile whose start is <= y0, among 32 at a time
+    const int r = first_tile(a.shape, sh.lane, sh.kvh);
+    const int64_t x0 = sh.x;
+    int lo = 0;
+    for (int n = lane_tiles(q, a.shape, r); n > 1;) {
+      const int step = (n + 31) >> 5, i = lane * step;
+      const int64_t start = x0 + (i < n ? tiles_cost(q, a.shape, r, lo + i) : 0);
+      const int f = 31 - __clz((int)__ballot_sync(0xffffffffu, i < n && start <= sh.y0));
+      sh.x = __shfl_sync(0xffffffffu, start, f);
+      lo += f * step;
+      n = (int)plan_min(step, n - f * step);
+    }
+    sh.t = r + (lo << a.shape.lanes2);
+  };
   const bool stop = lane == 0 && status_bad(a.status);
   if (a.batch == 1) {  // nothing to search (the shortest call's latency is mostly this and its like)
     load(0);
     if (bad) set_status(a.status, LG_ERR_CAPACITY);
     if (__any_sync(0xffffffffu, bad || stop)) return false;
-    sh.W = a.H_kv * c;
-    sh.step = range_step(sh.W, G, a.shape.bn2);
-    sh.y0 = cta * sh.step;
-    sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
+    sh.W = c;
     sh.x = 0;
-    sh.per_head = c;
     sh.slot = slot;
     sh.q = q;
     sh.off = off;
     sh.b = 0;
-    return sh.y0 < sh.W;
+    if (!range()) return false;
+    item(head);
+    return true;
   }
   load(lane);
-  int64_t incl = scan(a.H_kv * c);
+  int64_t incl = scan(c);
   sh.W = __shfl_sync(0xffffffffu, incl, 31);
   if (a.batch > 32) {
     int64_t mine = 0;
     for (int b = 32 + lane; b < a.batch; b += 32) {
       load(b);
-      mine += a.H_kv * c;
+      mine += c;
     }
     sh.W += __shfl_sync(0xffffffffu, scan(mine), 31);
     load(lane);
   }
   if (bad) set_status(a.status, LG_ERR_CAPACITY);
   if (__any_sync(0xffffffffu, bad || stop)) return false;
-  sh.step = range_step(sh.W, G, a.shape.bn2);
-  sh.y0 = plan_min(sh.W, cta * sh.step);
-  sh.y1 = plan_min(sh.W, sh.y0 + sh.step);
-  if (sh.y0 >= sh.W) return false;
+  if (!range()) return false;
   int64_t base = 0;
   for (int b0 = 0;; b0 += 32) {
     if (b0 > 0) {
       load(b0 + lane);
-      incl = scan(a.H_kv * c);
+      incl = scan(c);
     }
     const unsigned past = __ballot_sync(0xffffffffu, base + incl > sh.y0);
     if (past) {
       const int f = __ffs((int)past) - 1;
-      sh.x = base + __shfl_sync(0xffffffffu, incl - a.H_kv * c, f);
-      sh.per_head = __shfl_sync(0xffffffffu, c, f);
+      sh.x = base + __shfl_sync(0xffffffffu, incl - c, f);
       sh.slot = __shfl_sync(0xffffffffu, slot, f);
       sh.q.n = __shfl_sync(0xffffffffu, q.n, f);
       sh.q.m = __shfl_sync(0xffffffffu, q.m, f);
       sh.off = __shfl_sync(0xffffffffu, off, f);
       sh.b = b0 + f;
+      item(__shfl_sync(0xffffffffu, head, f));
       return true;
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
@@ -133,7 +169,7 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendArgs &a, int cta, i
 // The walk along a CTA's share, piece by piece.
 template <bool ONE>
 struct ChunkWalk {
-  int b, kvh, t, tiles;
+  int b, kvh, t, tiles, lane;
   ChunkSeq q;
   int off;           // first token row of the sequence
   int64_t slot0;     // first cache slot of the sequence
@@ -160,29 +196,28 @@ struct ChunkWalk {
     q = sh.q;
     off = sh.off;
     slot0 = sh.slot;
+    lane = sh.lane;
+    x = sh.x;
+    kvh = sh.kvh;
+    t = sh.t;
     tiles = ONE ? 1 : q.tiles(a.shape.tok);
-    kvh = (int)plan_div(y0 - sh.x, sh.per_head);
-    x = sh.x + kvh * sh.per_head;
-    t = !ONE && tiles > 1 ? tile_at(q, a.shape, y0 - x) : 0;
-    if (!ONE && t) x += tiles_cost(q, a.shape, t);
     load_item(a);
   }
   __device__ __forceinline__ bool done() const { return x >= y1; }
   __device__ __forceinline__ void next(const ChunkAttendArgs &a) {
     x += cost;
     if (x >= y1) return;
-    if (ONE || ++t == tiles) {
-      t = 0;
+    t += ONE ? 1 : 1 << a.shape.lanes2;
+    while (t >= tiles) {  // (the line goes on, so there is another item)
       if (++kvh == a.H_kv) {
         kvh = 0;
-        do {
-          ++b;
-          off = a.off[b];
-          q = ChunkSeq{a.len[b], a.off[b + 1] - off};
-          slot0 = a.seq_off[b];
-          tiles = ONE ? q.m > 0 : q.tiles(a.shape.tok);
-        } while (tiles == 0);
+        ++b;
+        off = a.off[b];
+        q = ChunkSeq{a.len[b], a.off[b + 1] - off};
+        slot0 = a.seq_off[b];
+        tiles = ONE ? q.m > 0 : q.tiles(a.shape.tok);
       }
+      t = ONE ? 0 : first_tile(a.shape, lane, kvh);
     }
     load_item(a);
   }

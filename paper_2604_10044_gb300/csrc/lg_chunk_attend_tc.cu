@@ -123,7 +123,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       ChunkShare sh;
       const bool work = chunk_share<false>(a, blockIdx.x, gridDim.x, sh);
       if (lane == 0) {
-        ChunkWalk<false> w;
+        // Heads of 64 keep the walk in shared memory (two prompts of 8192, 32/8 heads: 557 us, 585
+        // in registers), heads of 128 in registers (16 x 512 new rows: 78.7 us, 79.9 in shared
+        // memory).
+        __shared__ ChunkWalk<false> far;
+        ChunkWalk<false> near;
+        ChunkWalk<false> &w = D == 64 ? far : near;
         uint32_t n = 0, pieces = 0;  // ring position, pieces so far
         bool ok = true;
         auto load = [&](const CUtensorMap *map, int row) {
@@ -538,9 +543,27 @@ ChunkGrid chunk_grid_tc(int d, int g, int max_new) {
   return r;
 }
 
+// How many lines (lg_chunk_plan.cuh): on one, a CTA comes back to a kv-head's rows when all CTAs
+// have walked a tile's rows of theirs; past the L2's 126 MB it reads them from HBM again.  At 8 x
+// 512 new tokens over 8192 rows, 32/8 heads of 128, one, two, four and eight lines take 378, 352,
+// 338 and 330 us; two prompts of 12288 1682, 1659, 1625 and 1586.  Where the rows of the tiles under
+// way fit the L2 there is nothing to gain: one prompt of 1024 takes 21.3 us on one line and 24.2 on
+// eight, eight of 2048 under a window of 1024 take 142 and 141.
+int chunk_lanes2(const ChunkAttendArgs &a, int d, int G) {
+  int64_t rows = a.max_len;
+  if (a.shape.window) rows = plan_min(rows, (int64_t)a.shape.window + a.shape.sink + a.shape.tok);
+  if (rows * (4 * d) * G <= 126 << 20) return 0;
+  const int tiles = ChunkSeq{0, a.max_new}.tiles(a.shape.tok);
+  int n = 3;
+  while (((a.H_kv | G) & ((1 << n) - 1)) || 1 << n > tiles) --n;
+  return n;
+}
+
 cudaError_t launch_chunk_attend_tc(const ChunkAttendArgs &a, int d, int G, cudaStream_t s) {
   if (a.rows < 256) return launch_chunk_attend_few(a, d, G, s);
-  return d == 128 ? launch_typed<128>(a, G, s) : launch_typed<64>(a, G, s);
+  ChunkAttendArgs b = a;
+  b.shape.lanes2 = chunk_lanes2(a, d, G);
+  return d == 128 ? launch_typed<128>(b, G, s) : launch_typed<64>(b, G, s);
 }
 
 }  // namespace lg

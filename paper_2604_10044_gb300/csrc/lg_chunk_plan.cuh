@@ -5,10 +5,17 @@
 // cost is the rows its queries can see plus kItemCost, a linear function of the tile (constant once
 // a window fills), so the cost of a sequence's first t tiles is a closed form.  The items stand in
 // one line, ordered by sequence, kv-head and tile, W cost units long, and each of G CTAs takes
-// ceil(W / G) of it (or a block's rows, if that is more).  An item cut by such a bound is shared: its key blocks divide in
-// proportion, each CTA's part is a piece, and a second kernel merges the pieces (of partial
-// results in the workspace: slot 0 of a CTA for an item that began before its range, slot 1 for
-// one that ends after it).
+// ceil(W / G) of it (or a block's rows, if that is more).  An item cut by such a bound is shared: its
+// key blocks divide in proportion, each CTA's part is a piece, and a second kernel merges the pieces
+// (of partial results in the workspace: slot 0 of a CTA for an item that began before its range,
+// slot 1 for one that ends after it).
+//
+// Many items of a kv-head read the same rows.  One after the other on one CTA they read them from
+// HBM once each, when the caches of all kv-heads together pass the L2; so the tiles of a kv-head can
+// be dealt to `lanes` lines, tile t of kv-head h to line (t + h) mod lanes, each walked by G / lanes
+// CTAs.  `lanes` divides G and the kv-heads, so a line holds every residue of a sequence's tiles
+// equally often and all have the same length W; CTAs at the same place of each read the same
+// kv-head's rows at about the same time.
 #pragma once
 #include <stdint.h>
 
@@ -28,13 +35,14 @@ struct ChunkShape {
   int bn2;     // log2 of the rows of a key block
   int window;  // 0: none
   int sink;
+  int lanes2;  // log2 of the lines
 };
 
 // the sequences' numbers: rows n in the cache, m of them new
 struct ChunkSeq {
   int n, m;
   __host__ __device__ __forceinline__ int tiles(int tok) const {
-    return m / tok + (m % tok != 0);
+    return (unsigned)m / (unsigned)tok + ((unsigned)m % (unsigned)tok != 0);
   }
 };
 
@@ -68,38 +76,40 @@ __host__ __device__ __forceinline__ int64_t tile_cost(const ChunkSeq &q, const C
   return (int64_t)r.last + 1 - r.lo + r.sinks + kItemCost;
 }
 
-// cost of tiles [0, t), 0 <= t <= tiles
-__host__ __device__ __forceinline__ int64_t tiles_cost(const ChunkSeq &q, const ChunkShape &s,
-                                                       int t) {
-  if (t <= 0) return 0;
+// the first tile of a kv-head in line `lane`; the others follow `lanes` apart
+__host__ __device__ __forceinline__ int first_tile(const ChunkShape &s, int lane, int kvh) {
+  return (lane - kvh) & ((1 << s.lanes2) - 1);
+}
+__host__ __device__ __forceinline__ int lane_tiles(const ChunkSeq &q, const ChunkShape &s, int r) {
+  const int tiles = q.tiles(s.tok);
+  return tiles > r ? ((tiles - r - 1) >> s.lanes2) + 1 : 0;
+}
+
+// cost of the first k tiles of r, r + lanes, .., 0 <= k <= lane_tiles
+__host__ __device__ __forceinline__ int64_t tiles_cost(const ChunkSeq &q, const ChunkShape &s, int r,
+                                                       int k) {
+  if (k <= 0) return 0;
   int64_t extra = 0;
-  if (t == q.tiles(s.tok)) {  // the last tile may be short
-    extra = tile_cost(q, s, t - 1);
-    if (--t == 0) return extra;
+  const int t = r + ((k - 1) << s.lanes2);
+  if (t == q.tiles(s.tok) - 1) {  // the last tile may be short
+    extra = tile_cost(q, s, t);
+    if (--k == 0) return extra;
   }
-  // full tiles i < t: (n - m + (i + 1) tok) + kItemCost - max(0, a + i tok)
-  const int64_t T = t, tok = s.tok;
-  int64_t sum = T * ((int64_t)q.n - q.m + kItemCost) + tok * (T * (T + 1) / 2);
+  // full tiles t = r + j lanes, j < k: (n - m + (t + 1) tok) + kItemCost - max(0, a + t tok)
+  const int64_t K = k, step = (int64_t)s.tok << s.lanes2, at = (int64_t)r * s.tok;
+  int64_t sum = K * ((int64_t)q.n - q.m + kItemCost + at + s.tok) + step * (K * (K - 1) / 2);
   if (s.window) {
-    const int64_t a = (int64_t)q.n - q.m + 1 - s.window - s.sink;
-    const int64_t i0 = a >= 0 ? 0 : -a >= T * tok ? T : plan_div(-a + tok - 1, tok);
-    if (i0 < T) sum -= (T - i0) * a + tok * ((T * (T - 1) - i0 * (i0 - 1)) / 2);
+    const int64_t a = (int64_t)q.n - q.m + 1 - s.window - s.sink + at;
+    const int64_t j0 = a >= 0 ? 0 : -a >= K * step ? K : plan_div(-a + step - 1, step);
+    if (j0 < K) sum -= (K - j0) * a + step * ((K * (K - 1) - j0 * (j0 - 1)) / 2);
   }
   return sum + extra;
 }
 
-// the tile that cost unit x of a (sequence, kv-head) falls into
-__host__ __device__ __forceinline__ int tile_at(const ChunkSeq &q, const ChunkShape &s,
-                                                int64_t x) {
-  int lo = 0, hi = q.tiles(s.tok) - 1;
-  while (lo < hi) {  // the last tile whose start is <= x
-    const int mid = lo + (hi - lo + 1) / 2;
-    if (tiles_cost(q, s, mid) <= x)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
+// cost of all tiles of a kv-head, which is that of `lanes` kv-heads in a line
+__host__ __device__ __forceinline__ int64_t head_cost(const ChunkSeq &q, ChunkShape s) {
+  s.lanes2 = 0;
+  return tiles_cost(q, s, 0, q.tiles(s.tok));
 }
 
 // a tile's key blocks: block i of `count` holds the rows from block_row(i)

@@ -1,5 +1,5 @@
 """The division of lg_chunk_attend's work (csrc/lg_chunk_plan.cuh), compiled for the host: the
-closed-form costs against their sums, tile_at against a walk, the pieces of random batches (every
+closed-form costs against their sums, the pieces of random batches (every
 key block of every item exactly once, and never more pieces than the two slots of a CTA), and the
 blocks against the rows that a tile's queries see."""
 import os
@@ -28,6 +28,7 @@ static ChunkShape shape() {
   s.bn2 = pick({6, 7});
   s.window = uni(0, 2) ? (int)uni(1, pick({3, 200, 5000, 2147483647})) : 0;
   s.sink = pick({0, 1, 4, 64, 129, 1000});
+  s.lanes2 = pick({0, 0, 1, 3});
   return s;
 }
 static ChunkSeq seq() {
@@ -41,13 +42,21 @@ int main() {
   for (int it = 0; it < 4000; ++it) {  // costs, tiles, blocks
     const ChunkShape s = shape();
     const ChunkSeq q = seq();
-    const int tiles = q.tiles(s.tok);
-    int64_t sum = 0;
+    const int tiles = q.tiles(s.tok), lanes = 1 << s.lanes2;
+    int seen = 0;
+    for (int r = 0; r < lanes; ++r) {  // the tiles of a line, r, r + lanes, ..
+      int64_t sum = 0;
+      int k = 0;
+      for (int t = r; t < tiles; t += lanes, ++k, ++seen) {
+        CHECK(tiles_cost(q, s, r, k) == sum);
+        const int64_t c = tile_cost(q, s, t);
+        CHECK(c > kItemCost);
+        sum += c;
+      }
+      CHECK(lane_tiles(q, s, r) == k && tiles_cost(q, s, r, k) == sum);
+    }
+    CHECK(seen == tiles);
     for (int t = 0; t < tiles; ++t) {
-      CHECK(tiles_cost(q, s, t) == sum);
-      const int64_t c = tile_cost(q, s, t);
-      CHECK(c > kItemCost);
-      CHECK(tile_at(q, s, sum) == t && tile_at(q, s, sum + c - 1) == t);
       const TileRows r = tile_rows(q, s, t);
       const TileBlocks b = tile_blocks(r, s.bn2);
       // seen by some query of the tile <=> in a block of the tile, up to whole blocks
@@ -71,27 +80,32 @@ int main() {
         if (i >= o0 && i < o1) CHECK(!hides);
         else CHECK(hides || i0 < s.sink);
       }
-      sum += c;
     }
-    CHECK(tiles_cost(q, s, tiles) == sum);
   }
   for (int it = 0; it < 1500; ++it) {  // pieces
     const ChunkShape s = shape();
-    const int B = (int)uni(1, 12), H = (int)uni(1, 8), G = pick({1, 2, 152, 304});
+    const int lanes = 1 << s.lanes2;
+    const int B = (int)uni(1, 12), H = lanes * (int)uni(1, 3), G = pick({1, 2, 19, 152, 304});
+    const int lane = (int)uni(0, lanes - 1);  // one line
     std::vector<ChunkSeq> q(B);
-    int64_t W = 0;
+    int64_t W = 0, all = 0;
     std::vector<int64_t> start, cost;
     std::vector<int> count;
-    for (auto &x : q) {
-      x = seq();
-      for (int h = 0; h < H; ++h)
-        for (int t = 0; t < x.tiles(s.tok); ++t) {
+    for (int b = 0; b < B; ++b) {
+      const ChunkSeq x = q[b] = seq();
+      all += H / lanes * head_cost(x, s);
+      for (int h = 0; h < H; ++h) {
+        const int r = first_tile(s, lane, h);
+        CHECK(r >= 0 && r < lanes && (r + h) % lanes == lane);
+        for (int t = r; t < x.tiles(s.tok); t += lanes) {
           start.push_back(W);
           cost.push_back(tile_cost(x, s, t));
           count.push_back(tile_blocks(tile_rows(x, s, t), s.bn2).count);
           W += cost.back();
         }
+      }
     }
+    CHECK(all == W);  // every line is as long
     int64_t end = 0;
     const int64_t step = range_step(W, G, s.bn2);
     std::vector<int> next(start.size(), 0);
@@ -116,8 +130,8 @@ int main() {
   }
   // the largest line: no 64-bit overflow in the bounds or the cuts
   const ChunkSeq big{2147483647, 2147483647};
-  const ChunkShape s{16, 6, 0, 0};
-  const int64_t W = tiles_cost(big, s, big.tiles(s.tok)) / 2;
+  const ChunkShape s{16, 6, 0, 0, 0};
+  const int64_t W = tiles_cost(big, s, 0, big.tiles(s.tok)) / 2;
   CHECK(W > 0 && range_step(W, 304, 6) * 304 >= W && range_step(W, 304, 6) * 304 - W < 304);
   const int64_t c = tile_cost(big, s, big.tiles(16) - 1);
   CHECK(cut_block(c - 1, c, 2147483647 / 64 + 1, 6) <= 2147483647 / 64 + 1);

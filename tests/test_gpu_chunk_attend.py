@@ -165,6 +165,26 @@ def test_a_wider_bound_gives_the_same_answers(cuda):
         b.check(b.attend())
 
 
+@pytest.mark.parametrize("H_kv,g,d,ns,ms", [
+    (2, 4, 128, [600], [600]), (4, 4, 128, [700, 300, 900], [513, 0, 64 * 9]),
+    (8, 2, 64, [1100, 40, 300], [1100, 40, 129]), (6, 8, 128, [300, 290], [290, 290]),
+    (8, 1, 128, [2300, 5, 2048], [2300, 5, 1792]), (8, 7, 64, [500], [300]),
+    (16, 2, 64, [130] * 35 + [700], [130] * 5 + [0, 1, 90] * 10 + [640]),
+    (4, 5, 128, [9] * 33 + [1000], [1] * 33 + [1000])])
+def test_tiles_dealt_to_lines(cuda, H_kv, g, d, ns, ms):
+    """a bound on the lengths past what the L2 holds deals a kv-head's tiles to several lines"""
+    b = Batch(ns, ms, "bf16", H_kv=H_kv, g=g, d=d, seed=12).to_device()
+    b.check(b.attend())
+    for b.max_len in (20000, 2 ** 31 - 1):
+        b.check(b.attend())
+
+
+def test_tiles_dealt_to_lines_under_a_window(cuda):
+    for H_kv, n, m, window, sink in ((2, 3100, 650, 1700, 4), (4, 2600, 2600, 1600, 130)):
+        b = Batch([n, 50], [m, 50], "bf16", H_kv=H_kv, g=4, seed=13).to_device()
+        b.check(b.attend(window, sink), window, sink)
+
+
 @pytest.mark.parametrize("what", ["max_len", "max_new", "more new rows than rows", "T", "order"])
 def test_lengths_out_of_bounds_are_an_error(cuda, what):
     b = Batch([200, 90], [30, 20], "bf16", seed=11).to_device()
