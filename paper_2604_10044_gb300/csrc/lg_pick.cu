@@ -89,6 +89,25 @@ __device__ __forceinline__ float max16<float>(const uint4 &u) {
   return two(two(f[0], f[1]), two(f[2], f[3]));
 }
 
+// 16 bytes with the elements whose bit is clear set to -infinity
+template <typename T>
+__device__ __forceinline__ uint4 keep(const uint4 &u, uint32_t bits) {
+  uint4 w = u;
+  uint32_t *h = (uint32_t *)&w;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t two = (bits & 0x55u) | (bits & 0xaau) << 15;  // a pair's bits 16 apart
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t mask = (two >> (2 * e) & 0x00010001u) * 0xffffu;
+      h[e] = (h[e] & mask) | (0xff80ff80u & ~mask);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = bits >> e & 1 ? h[e] : 0xff800000u;
+  }
+  return w;
+}
+
 template <typename T>
 __device__ __forceinline__ uint4 pack16(const float *f) {
   if constexpr (sizeof(T) == 2) {
@@ -251,22 +270,19 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int i = i0 + k * NT, t = v0 + i * N;
-        float f[N], vm = max16<T>(u[k]);
-        Elem<T>::unpack(u[k], (float2 *)f);
-        const bool nan = vm != vm;
-        if (nan) {
+        uint4 w = u[k];
+        float vm = max16<T>(w), f[N];
+        if (vm != vm) {
+          Elem<T>::unpack(w, (float2 *)f);
 #pragma unroll
           for (int e = 0; e < N; ++e) f[e] = f[e] == f[e] ? f[e] : -INFINITY;
+          w = pack16<T>(f);
+          vm = max16<T>(w);
         }
+        uint32_t left = kAll;  // tokens that w holds still
         if (out && i < nvec) {  // (listed tokens are written again after the pass)
-          const uint32_t ab = allowed ? window(ok0 + k * kStep, sh) & kAll : kAll;
-          uint4 w = u[k];
-          if (nan || ab != kAll) {
-            float g[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) g[e] = ab >> e & 1 ? f[e] : -INFINITY;
-            w = pack16<T>(g);
-          }
+          if (allowed) left = window(ok0 + k * kStep, sh) & kAll;
+          if (left != kAll) w = keep<T>(w, left);
           if (out16) {
             __stcs((uint4 *)(out + t), w);
           } else {
@@ -275,14 +291,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
             for (int e = 0; e < N; ++e) out[t + e] = h[e];
           }
         }
-        if (nan || kb[k] != kAll) {
-          vm = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            f[e] = kb[k] >> e & 1 ? f[e] : -INFINITY;
-            vm = fmaxf(vm, f[e]);
-          }
-        }
+        if (kb[k] != left) w = keep<T>(w, kb[k]);
+        if (kb[k] != kAll) vm = max16<T>(w);
+        Elem<T>::unpack(w, (float2 *)f);
         best = vm > m ? i : best;
         const float m1 = fmaxf(m, vm), base = m1 == -INFINITY ? 0.f : m1;
         sum *= exp2_fast((m - base) * kLog2e);
