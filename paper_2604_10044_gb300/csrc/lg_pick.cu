@@ -16,6 +16,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "lg_common.cuh"
 #include "lg_internal.h"
 
@@ -140,7 +142,10 @@ __device__ __forceinline__ Top warp_top(const Top &t) {
 }
 
 constexpr int kMaxCluster = 16;
-constexpr int kMaxSlice = 320 << 10;  // tokens of a CTA: 16 bytes of bits for every 32
+constexpr int kMinFew = 2 << 10;       // tokens a CTA takes at least: of few rows
+constexpr int kMinSlice = 8 << 10;     // of more
+constexpr int kMaxSlice = 320 << 10;   // and at most: 16 bytes of bits for every 32
+constexpr int kFourBits = 88 << 10;    // and of four on an SM
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, int csize) {
@@ -433,46 +438,83 @@ __global__ void count_tokens_kernel(const int32_t *tokens, const int32_t *off, i
 }
 
 template <typename T, int NT>
-cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
-  a.slice = ((a.V + c - 1) / c + 31) / 32 * 32;
-  // (a word more each: a vector's bits are read from two)
-  const size_t smem = (size_t)(a.slice / 32 + 1) * 4 * sizeof(uint32_t);
+cudaError_t pick_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int batch, int c,
+                        size_t smem) {
   auto kern = pick_token_kernel<T, NT>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   if (smem > 36 * 1024)
     LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(batch * c));
   cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = c;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = c;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  LG_TRY(cudaLaunchKernelEx(&cfg, kern, a, c));
+  return cudaSuccess;
+}
+
+// Clusters of c CTAs that run at once: a cluster stands within one GPC, so those of more CTAs leave
+// some of the GPU's places empty.  Asked once a size.
+template <typename T, int NT>
+int clusters_at_once(int c) {
+  static std::atomic<int> known[kMaxCluster + 1];
+  int n = known[c].load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    if (pick_config<T, NT>(cfg, attr, 1, c, 32 * 1024) != cudaSuccess) return 0;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, pick_token_kernel<T, NT>, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      n = 0;
+    }
+    known[c].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+template <typename T, int NT>
+cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
+  a.slice = ((a.V + c - 1) / c + 31) / 32 * 32;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  // (a word more each: a vector's bits are read from two)
+  LG_TRY((pick_config<T, NT>(cfg, attr, batch, c,
+                             (size_t)(a.slice / 32 + 1) * 4 * sizeof(uint32_t))));
+  cfg.stream = s;
+  LG_TRY(cudaLaunchKernelEx(&cfg, pick_token_kernel<T, NT>, a, c));
   return cudaGetLastError();
 }
 
-// CTAs a row: as many as fit the GPU at once (a kernel of 512 threads twice an SM, of 256 four
-// times), at most 16, each with 2048 tokens or more, and enough that a slice's bits fit shared memory.
-// (GB300, 192 rows of 128257 bf16 logits, 256 threads: 2 CTAs a row 57 us, 3 39.5, 4 45, 8 50, 16 72;
-// one row of 151936 fp32, 512 threads: 4 CTAs 11.1 us, 8 8.8, 16 7.1, and 16 of 256 threads 8.3.)
+// CTAs a row, of 512 threads (two an SM): the most whose clusters run at once, at most ten, each with
+// 8192 tokens or more (16, and 2048, where rows are so few that every CTA finds an SM of its own), and
+// enough that a slice's bits fit shared memory.  Rows too many for two CTAs each and not for three of 256
+// threads (four an SM) take those; rows too many for one of 512 threads take one of 256, as long as
+// four CTAs' bits fit an SM.  Measured on a GB300, calls back to back, us by threads x CTAs a row:
+//   rows of 128257 bf16:   8  512x10  6.8, 512x16  8.2     16  512x8  7.8, 512x16 12.5 (do not fit)
+//                         48  512x5  11.1, 512x6  16.0    152  512x2 16.1, 256x4  23.2
+//                        192  256x3  22.0, 512x1  25.0    256  512x1 25.7, 256x2  26.9
+//                        608  512x1  52.6, 256x1  79.3 (three an SM)
+//   rows of 32000 bf16:   16  512x3   6.8, 512x10  7.7    608  256x1 17.2, 512x1  21.4
+//   rows of 32000 fp32:    1  512x15  5.6, 512x3   6.6
 template <typename T>
 cudaError_t launch_pick_sized(PickArgs &a, int batch, cudaStream_t s) {
-  const int nt = batch * kMaxCluster <= 2 * 152 ? 512 : 256;
-  int c = (nt == 512 ? 2 : 4) * 152 / batch, most = a.V / 2048;
-  c = c < 1 ? 1 : c > kMaxCluster ? kMaxCluster : c;
-  c = c > most ? (most < 1 ? 1 : most) : c;
   const int least = (a.V + kMaxSlice - 1) / kMaxSlice;
+  const bool few = batch <= 4;
+  int c = few ? kMaxCluster : 10, most = a.V / (few ? kMinFew : kMinSlice);
+  c = c > most ? (most < 1 ? 1 : most) : c;
+  while (c > 1 && clusters_at_once<T, 512>(c) < batch) --c;
+  if (c == 1 && least <= 3 && most >= 3 && batch <= clusters_at_once<T, 256>(3))
+    return launch_pick_typed<T, 256>(a, batch, 3, s);
   c = c < least ? least : c;
-  if (nt == 512) return launch_pick_typed<T, 512>(a, batch, c, s);
-  return launch_pick_typed<T, 256>(a, batch, c, s);
+  if (c == 1 && a.V <= kFourBits && batch > clusters_at_once<T, 512>(1))
+    return launch_pick_typed<T, 256>(a, batch, 1, s);
+  return launch_pick_typed<T, 512>(a, batch, c, s);
 }
 
 }  // namespace

@@ -88,6 +88,17 @@ def test_sizes(cuda, dtype, B, V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,V", [(4, 90001), (8, 90001), (30, 40961), (60, 33001), (100, 24577),
+                                 (150, 16385), (200, 24577), (310, 8193), (306, 90113)])
+def test_rows_split_over_ctas(cuda, dtype, B, V):
+    """every number of CTAs a row, and more rows than run at once"""
+    rng = np.random.default_rng(B)
+    x = _dev(rng.standard_normal((B, V), dtype=np.float32) * 3, cuda, chunk_ref.tdtype(dtype))
+    seen, counts, pen = _history(rng, B, V, 300)
+    _run(cuda, x, seen, counts, pen, None, rng.random((B, V), dtype=np.float32) < 0.6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B", [3, 96])
 def test_many_seen_tokens(cuda, dtype, B):
     """histories that fill stretches of the vocabulary, more of them than a CTA lists"""
