@@ -397,12 +397,15 @@ __global__ void __launch_bounds__(kThreads, R == 4 ? 2 : 1)
 
 // Merge of the item that CTA c's start is the first to cut, c = blockIdx.x + 1, from the parts of
 // CTAs c - 1, c, ...: 32 rows a CTA, a lane each, the elements spread over the eight warps; the rows
-// leave through shared memory, 16 bytes a thread.  The loads of kAtOnce parts wait together: 8 where
-// items are short and have many, 4 where they are long (fewer registers, more CTAs an SM; 12 took
-// 16 x 7 proposed tokens from 23.0 to 25.5 us).
+// leave through shared memory, 16 bytes a thread.  SHARE, for items of few rows and many parts: two or
+// four lanes share a row and take every second or fourth part (a token over 16000 rows, bf16, two
+// kv-heads of 64, 76 parts: 24.9 us without, 14.4; eight of 128, 19 parts: 17.8 and 14.9; eight
+// sequences of them, three parts: 48.0 without, 49.3; one over 200 rows: 9.3 and 9.9).  The loads of
+// kAtOnce parts wait together: 8 where items are short and have many, 4 where they are long (fewer
+// registers, more CTAs an SM; 12 took 16 x 7 proposed tokens from 23.0 to 25.5 us).
 constexpr int kMergeRows = 32;
 
-template <typename T, int D, int kAtOnce>
+template <typename T, int D, int kAtOnce, bool SHARE>
 __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a, int G) {
   constexpr int NE = D / 4 / (kThreads / 32);  // groups of four elements a thread
   constexpr int kRow = D * (int)sizeof(T) + 16;
@@ -411,23 +414,32 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
   pdl_enter();
   const ChunkCut w = *cut_at(a, D, G, c);
   if (cta_status_bad(a.status)) return;
-  const int r0 = blockIdx.y * kMergeRows, r = r0 + lane;
+  const int r0 = blockIdx.y * kMergeRows;
   if (w.parts == 0 || r0 >= w.used) return;
+  // log2 of the lanes of a row
+  const int share = !SHARE || w.parts <= kAtOnce ? 0
+                    : w.used <= 8 && w.parts > 2 * kAtOnce ? 2 : w.used <= 16 ? 1 : 0;
+  const int r = r0 + (lane & (kMergeRows >> share) - 1), first = lane / (kMergeRows >> share);
   float m = -INFINITY, l = 0.f;
   float4 o[NE];
 #pragma unroll
   for (int e = 0; e < NE; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
   int before = 0;
-  for (int p0 = 0; p0 < w.parts; p0 += kAtOnce) {
+  for (int p0 = 0; p0 < w.parts; p0 += kAtOnce << share) {
     float2 ml[kAtOnce];
     float4 x[kAtOnce][NE];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const int p = p0 + k, from = before;
-      if (p < w.parts) before = cut_block(w.in + p * w.step, w.cost, w.blocks, a.shape.bn2);
-      if (from == 0 && before == w.blocks) return;  // one part has every block and wrote the result
+      const int p = p0 + (k << share) + first;
       ml[k] = make_float2(-INFINITY, 0.f);
-      if (from == before || r >= w.used) continue;
+      const int64_t y = w.in + p * w.step;
+      if (share && p > 0) before = cut_block(y - w.step, w.cost, w.blocks, a.shape.bn2);
+      const int from = before, to = cut_block(y, w.cost, w.blocks, a.shape.bn2);
+      before = to;
+      // one part has every block and wrote the result
+      const bool whole = p < w.parts && from == 0 && to == w.blocks;
+      if (SHARE ? __any_sync(0xffffffffu, whole) : whole) return;
+      if (p >= w.parts || from == to || r >= w.used) continue;
       const int cta = c - 1 + p, slot = p == 0 ? 1 : 0;
       ml[k] = *part_ml(a, D, G, cta, slot, r);
 #pragma unroll
@@ -449,10 +461,25 @@ __global__ void __launch_bounds__(kThreads) chunk_merge_kernel(ChunkAttendArgs a
       }
     }
   }
+  for (int off = kMergeRows >> share; off < kMergeRows; off <<= 1) {
+    const float m1 = __shfl_xor_sync(0xffffffffu, m, off), l1 = __shfl_xor_sync(0xffffffffu, l, off);
+    const float mx = fmaxf(m, m1), base = mx == -INFINITY ? 0.f : mx;
+    const float f0 = exp2_fast(m - base), f1 = exp2_fast(m1 - base);
+    m = mx;
+    l = l * f0 + l1 * f1;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      o[e].x = o[e].x * f0 + __shfl_xor_sync(0xffffffffu, o[e].x, off) * f1;
+      o[e].y = o[e].y * f0 + __shfl_xor_sync(0xffffffffu, o[e].y, off) * f1;
+      o[e].z = o[e].z * f0 + __shfl_xor_sync(0xffffffffu, o[e].z, off) * f1;
+      o[e].w = o[e].w * f0 + __shfl_xor_sync(0xffffffffu, o[e].w, off) * f1;
+    }
+  }
   const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < NE; ++e) {
-    uint8_t *at = s_out + lane * kRow + (warp * NE + e) * 4 * (int)sizeof(T);
+    if (first) break;
+    uint8_t *at = s_out + (r - r0) * kRow + (warp * NE + e) * 4 * (int)sizeof(T);
     if constexpr (sizeof(T) == 4) {
       *(float4 *)at = make_float4(o[e].x * inv, o[e].y * inv, o[e].z * inv, o[e].w * inv);
     } else {
@@ -482,10 +509,13 @@ cudaError_t launch_f32(void (*kern)(ChunkAttendArgs), int smem, const ChunkAtten
 template <typename T, int D>
 cudaError_t launch_merge_typed(const ChunkAttendArgs &a, int G, cudaStream_t s) {
   const dim3 grid(G - 1, (a.rows + kMergeRows - 1) / kMergeRows);
-  if (a.rows <= 64)
-    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 8>, grid, kThreads, 0, s, a, G));
+  // more than eight parts an item, and blocks for them
+  if (a.rows <= 16 && (int64_t)a.batch * a.H_kv * 8 < G && a.max_len > 8 << a.shape.bn2)
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 8, true>, grid, kThreads, 0, s, a, G));
+  else if (a.rows <= 64)
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 8, false>, grid, kThreads, 0, s, a, G));
   else
-    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 4>, grid, kThreads, 0, s, a, G));
+    LG_TRY(launch_pdl(chunk_merge_kernel<T, D, 4, false>, grid, kThreads, 0, s, a, G));
   return cudaGetLastError();
 }
 

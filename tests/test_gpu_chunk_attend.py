@@ -131,6 +131,24 @@ def test_long_cache(cuda, dtype, m):
     b.check(b.attend(1000, 4), 1000, 4)
 
 
+@pytest.mark.parametrize("dtype,g,m", [("bf16", 1, 1), ("bf16", 8, 1), ("bf16", 5, 2),
+                                       ("bf16", 8, 2), ("f32", 3, 1), ("f32", 8, 1),
+                                       ("f32", 5, 3), ("f32", 8, 2)])
+def test_few_rows_in_many_parts(cuda, dtype, g, m):
+    """items of up to 16 rows that are cut into 9, 17 and more parts; a window that empties some"""
+    for H_kv, ns in ((1, [20000]), (2, [9001]), (1, [1500, 8000]), (3, [5000, 0])):
+        ms = [min(n, m) for n in ns]
+        d = 64 if g == 8 and H_kv % 2 == 0 else 128  # (a cache's H_kv d is a multiple of 128)
+        b = Batch(ns, ms, dtype, H_kv=H_kv, g=g, d=d, seed=14).to_device()
+        out = b.attend()
+        b.check(out)
+        assert torch.equal(out, b.attend())
+        b.check(b.attend(1200, 4), 1200, 4)
+    b.v[:, :, 77, :5] = math.inf  # a value that every query sees, in one part of many
+    b.to_device()
+    b.check(b.attend())
+
+
 def test_many_sequences(cuda):
     """more sequences than a CTA has threads, empty ones and empty chunks among them"""
     rng = np.random.default_rng(7)
