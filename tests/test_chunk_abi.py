@@ -4,6 +4,7 @@ import ctypes
 import inspect
 import os
 import re
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -164,6 +165,80 @@ def test_count_tokens_refusals():
     assert f(F, F, 4, 0, 10, 1, F, F, None, None) == 1
     assert f(F, F, 4, 2, 0, 1, F, F, None, None) == 1
     assert f(F, F, 0, 2, 10, 1, F, F, None, None) == 0
+
+
+def test_binding_refuses_tensors_that_the_kernels_cannot_read(monkeypatch):
+    """another device than the current one, another type than the cache's, too few elements"""
+    z, i32 = torch.zeros, torch.int32
+
+    class At:  # a tensor on a device of one's choice
+        def __init__(self, t, dev):
+            self.t, self.dev, self.device = t, dev, "cuda:%d" % dev
+
+        def get_device(self):
+            return self.dev
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+    def args(dev=1, **over):
+        t = dict(status=z(1, dtype=i32), off=z(2, dtype=i32), q=z(3, 4, 64), k=z(3, 2, 64),
+                 v=z(3, 2, 64), pos=z(3, dtype=i32), out=z(3, 4, 64), ws=z(64))
+        t = {n: At(x, dev) for n, x in t.items()}
+        t.update(over)
+        cache = SimpleNamespace(c=lg.LgCache(), status=t["status"], d=64, H_kv=2, k=z(1))
+        chunk = SimpleNamespace(c=lg.LgChunk(), off=t["off"], T=3, max_new=3)
+        return cache, chunk, t
+
+    def attend(*a, **over):
+        cache, chunk, t = args(*a, **over)
+        lg.lg_chunk_attend(cache, chunk, 0, t["q"], 4, 1.0, 0, 0, t["out"], 8, t["ws"], 0)
+
+    def rope(*a, **over):
+        cache, chunk, t = args(*a, **over)
+        lg.lg_rope_append(cache, chunk, 0, t["q"], t["k"], t["v"], t["pos"], lg.LgRopeParams(),
+                          t["out"], lg.LgGuardParams(), 0)
+
+    def pick(dev=1, **over):
+        t = dict(logits=z(2, 33), seen=z(4, dtype=i32), counts=z(66, dtype=i32), penalty=z(2, 4),
+                 allowed=z(4, dtype=i32), tokens=z(2, dtype=i32), pmax=z(2))
+        t = {n: At(x, dev) for n, x in t.items()}
+        t.update(over)
+        lg.lg_pick_token(t["logits"], t["seen"], t["counts"], t["penalty"], None, t["allowed"],
+                         t["tokens"], t["pmax"], stream=0)
+
+    def count(dev=1, **over):
+        t = dict(tokens=z(2, dtype=i32), seen=z(4, dtype=i32), counts=z(66, dtype=i32))
+        t = {n: At(x, dev) for n, x in t.items()}
+        t.update(over)
+        lg.lg_count_tokens(t["tokens"], None, 33, 1, t["seen"], t["counts"], stream=0)
+
+    class Launched(Exception):
+        pass
+
+    def call(*a):
+        raise Launched
+
+    monkeypatch.setattr(lg, "_call", call)
+    monkeypatch.setattr(lg, "_device", lambda: 1)
+    for f in (attend, rope, pick, count):
+        with pytest.raises(Launched):
+            f()
+        for dev in (-1, 0, 2):
+            with pytest.raises(ValueError):
+                f(dev)
+    bad = {attend: dict(q=[z(3, 4, 64, dtype=torch.bfloat16), z(2, 4, 64)], out=[z(3, 2, 64)]),
+           rope: dict(q=[z(2, 4, 64)], k=[z(3, 2, 32), z(3, 2, 64).double()], v=[z(1, 2, 64)],
+                      pos=[z(2, dtype=i32), z(3)], out=[z(3, 3, 64), z(3, 4, 64).double()]),
+           pick: dict(seen=[z(3, dtype=i32)], counts=[z(65, dtype=i32), z(66)], penalty=[z(7)],
+                      allowed=[z(3, dtype=i32), z(4).double()],
+                      tokens=[z(1, dtype=i32), z(2)], pmax=[z(1), z(2, dtype=torch.bfloat16)]),
+           count: dict(tokens=[z(2)], seen=[z(3, dtype=i32)], counts=[z(65, dtype=i32)])}
+    for f, cases in bad.items():
+        for name, values in cases.items():
+            for v in values:
+                with pytest.raises(ValueError):
+                    f(**{name: At(v, 1)})
 
 
 def test_binding_refuses_broken_rows():
