@@ -347,8 +347,8 @@ def _rows_stride(t, name):
 
 # The calls below refuse what their kernels could not read: tensors of another type, too short, or
 # (its first tensor is looked at) of another device than the current one, whose stream
-# the call takes.  The conditions stand in place and look at each thing once: they are 0.4 to 0.7 us
-# of the 7 to 9 that a call takes its caller (Grace).
+# the call takes.  Those that a decode step makes have the conditions and the call in place: functions
+# around them took 0.5 to 2 us of the 6 to 8 that a call takes its caller (Grace).
 def _refuse(what, needs):
     raise ValueError("%s: on the current CUDA device, %s" % (what, needs))
 
@@ -392,10 +392,14 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
     at = k_new.get_device()
     if at < 0 or at != _device():
         _refuse("k_new", "the other tensors too")
-    _call("lg_rope_append", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, _ptr(q), qs, H_q,
-          k_new.data_ptr(), _rows_stride(k_new, "k_new"), v_new.data_ptr(),
-          _rows_stride(v_new, "v_new"), _ptr(pos), ctypes.byref(rope), _ptr(q_out),
-          ctypes.byref(params), _stream(stream))
+    rc = (_lib or lib()).lg_rope_append(
+        ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, None if q is None else q.data_ptr(), qs,
+        H_q, k_new.data_ptr(), _rows_stride(k_new, "k_new"), v_new.data_ptr(),
+        _rows_stride(v_new, "v_new"), None if pos is None else pos.data_ptr(), ctypes.byref(rope),
+        None if q_out is None else q_out.data_ptr(), ctypes.byref(params),
+        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        raise LgError("lg_rope_append", rc)
 
 
 def lg_chunk_workspace_size(cache, chunk, H_q, max_len) -> int:
@@ -413,9 +417,12 @@ def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max
     at = q.get_device()
     if at < 0 or at != _device():
         _refuse("q", "the other tensors too")
-    _call("lg_chunk_attend", ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, q.data_ptr(),
-          H_q, float(scale), window, n_sink, out.data_ptr(), max_len, ws.data_ptr(),
-          ws.numel() * ws.element_size(), _stream(stream))
+    rc = (_lib or lib()).lg_chunk_attend(
+        ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, q.data_ptr(), H_q,
+        float(scale), window, n_sink, out.data_ptr(), max_len, ws.data_ptr(), ws.nbytes,
+        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        raise LgError("lg_chunk_attend", rc)
 
 
 def lg_count_tokens(tokens, off, V, generated, seen, counts, status=None, stream=None):
@@ -470,9 +477,16 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
         bs = ctypes.byref(LgBias(off.data_ptr(), ids.data_ptr(), val.data_ptr()))
     x = LgLogits(logits.data_ptr(), _LOGITS.get(logits.dtype, -1), B, V, 0,
                  max(st[0], V))  # one row: its stride says nothing
-    _call("lg_pick_token", ctypes.byref(x), _ptr(seen), _ptr(counts), _ptr(penalty), bs,
-          _ptr(allowed), tokens.data_ptr(), pmax.data_ptr(), _ptr(logits_out), _ptr(status),
-          _stream(stream))
+    rc = (_lib or lib()).lg_pick_token(
+        ctypes.byref(x), None if seen is None else seen.data_ptr(),
+        None if counts is None else counts.data_ptr(),
+        None if penalty is None else penalty.data_ptr(), bs,
+        None if allowed is None else allowed.data_ptr(), tokens.data_ptr(), pmax.data_ptr(),
+        None if logits_out is None else logits_out.data_ptr(),
+        None if status is None else status.data_ptr(),
+        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        raise LgError("lg_pick_token", rc)
 
 
 # ------------------------------------------------------------------ device buffers of a batch

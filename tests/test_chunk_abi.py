@@ -219,7 +219,8 @@ def test_binding_refuses_tensors_that_the_kernels_cannot_read(monkeypatch):
     def call(*a):
         raise Launched
 
-    monkeypatch.setattr(lg, "_call", call)
+    names = ("lg_chunk_attend", "lg_rope_append", "lg_pick_token", "lg_count_tokens")
+    monkeypatch.setattr(lg, "_lib", SimpleNamespace(**{n: call for n in names}))
     monkeypatch.setattr(lg, "_device", lambda: 1)
     for f in (attend, rope, pick, count):
         with pytest.raises(Launched):
