@@ -1,5 +1,9 @@
 """The calls of include/lg_chunk.h as a model step makes them, one after another on the guard's
 cache: a prompt in chunks, then guarded decode steps whose tokens come from the step's logits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -157,3 +161,35 @@ def test_a_guarded_decode_from_logits(cuda):
         pruned += int((g.kept_count >= 0).sum().item())
         assert (cache.lengths() <= budget).all()
     assert pruned > 0 and cache.lengths().min() > 8
+
+
+FIRST = """
+import torch
+from paper_2604_10044_gb300 import lg
+import chunk_ref
+b = chunk_ref.Batch([300, 2000], [200, 2000], "bf16", H_kv=8, g=2).to_device()
+b.max_len = 20000
+x = torch.randn((20, 50000), device="cuda")
+tok = torch.zeros(20, dtype=torch.int32, device="cuda")
+pm = torch.zeros(20, device="cuda")
+out = torch.full_like(b.qd, 7.0)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    lg.lg_chunk_attend(b.cache, b.chunk, 0, b.qd, b.H_q, b.d ** -0.5, 0, 0, out, b.max_len, b.ws)
+    lg.lg_pick_token(x, None, None, None, None, None, tok, pm)
+g.replay()
+torch.cuda.synchronize()
+b.check(out)
+assert torch.equal(tok.long(), x.argmax(-1))
+print("ok")
+"""
+
+
+def test_a_process_may_begin_with_captured_calls(cuda):
+    """nothing that a first call sets up is forbidden while a stream is captured"""
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([os.path.dirname(here), here]))
+    r = subprocess.run([sys.executable, "-c", FIRST], env=env, capture_output=True, text=True,
+                       timeout=240)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr[-2000:]
