@@ -214,6 +214,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait_full(n);
             if (ok && one) mbar_arrive(&bars.empty[n % ST]);
           }
+          // This piece's queries too, though they are the other stream's: a wait for the next piece's
+          // knows only that the phase's parity has passed, and would pass before these arrived.
+          ok = ok && tc_wait_warp(bars, &bars.q_full, pc & 1);
           if (!ok) break;
           if (one) mbar_arrive(&bars.q_empty);
           continue;

@@ -203,6 +203,20 @@ def test_tiles_dealt_to_lines_under_a_window(cuda):
         b.check(b.attend(window, sink), window, sink)
 
 
+@pytest.mark.parametrize("d,H_kv,g", [(128, 2, 4), (128, 1, 8), (64, 2, 4), (64, 4, 1)])
+def test_short_last_tiles_one_after_another(cuda, d, H_kv, g):
+    """pieces of one stream's tile alone, short enough that all their blocks arrive at once, followed
+    by pieces of both: every piece computes with its own queries"""
+    tile = 128 // g
+    ms = [tile // 2, 2 * tile, tile, 1, 2 * tile - 1, 2 * tile + 3, tile + 1] * 60
+    ns = [m + x for m, x in zip(ms, [0, 0, 90, 100, 0, 40, 3] * 60)]
+    b = Batch(ns, ms, "bf16", H_kv=H_kv, g=g, d=d, seed=15, spread=2.0).to_device()
+    out = b.attend()
+    b.check(out)
+    for _ in range(20):
+        assert torch.equal(out, b.attend())
+
+
 @pytest.mark.parametrize("what", ["max_len", "max_new", "more new rows than rows", "T", "order"])
 def test_lengths_out_of_bounds_are_an_error(cuda, what):
     b = Batch([200, 90], [30, 20], "bf16", seed=11).to_device()
