@@ -235,10 +235,11 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (int j = 0; ok && j < blocks; ++j) {
         if (j + 1 < blocks) scores(j + 1);
         const uint32_t iv = n + (j + 1 < blocks ? 2 * j + 2 : 2 * j + 1), b = (c + j) & 1;
+        // (the copy before the clearing: its arrival says that the ring's slot has been through the
+        // clearing warps before, and so which phase of `fixed` the parity means)
+        wait_full(iv);
         if (j < open0 || j >= open1)
           ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-        else
-          wait_full(iv);
         if (j == 0) ok = ok && tc_wait_warp(bars, &bars.o_free, (pc & 1) ^ 1);
         ok = ok && tc_wait_warp(bars, &bars.p_full[b], ((c + j) >> 1) & 1);
         if (!ok) break;

@@ -235,10 +235,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           // (value block j follows the keys ahead of it and j pairs, or what pairs there are)
           const uint32_t iv = n + ahead + j + (j < blocks - ahead ? j : blocks - ahead);
           const uint32_t b = c % NB, par = (c / NB) & 1, ts = ts0 + b * kBn;
+          // (the copy before the clearing: its arrival says that the ring's slot has been through the
+          // clearing warp before, and so which phase of `fixed` the parity means)
+          wait_full(iv);
           if (j < open0 || j >= open1)
-            ok = tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-          else
-            wait_full(iv);
+            ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
           if (j + NB < blocks) wait_full(iv + 1);
           ok = ok && tc_wait_warp(bars, &(NB == 1 ? bars.p_half : bars.p_full)[2 * s + b], par);
           if (NB == 1 && two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));

@@ -103,6 +103,25 @@ def test_what_hidden_rows_hold_is_nothing(cuda, dtype, window, sink):
     b.check(out, window, sink)
 
 
+@pytest.mark.parametrize("d,m", [(128, 1), (128, 5), (128, 200), (64, 1), (64, 5), (64, 200)])
+def test_hidden_rows_again_and_again(cuda, d, m):
+    """rows without numbers behind every window, at every place of the ring that blocks pass through:
+    none of them reaches a result, in any of many calls"""
+    window, ns = 300, [m + 1500 + 37 * i for i in range(24)]
+    b = Batch(ns, [m] * 24, "bf16", d=d, seed=16)
+    for o, n in zip(b.seq, ns):
+        b.k[:, :, o:o + n - m + 1 - window] = math.nan
+        b.v[:, :, o:o + n - m + 1 - window] = math.nan
+    b.to_device()
+    out = b.attend(window)
+    for o, n in zip(b.seq, ns):  # (the reference multiplies hidden rows)
+        b.k[:, :, o:o + n - m + 1 - window] = 0.0
+        b.v[:, :, o:o + n - m + 1 - window] = 0.0
+    b.check(out, window)
+    for _ in range(20):
+        assert torch.equal(out, b.attend(window))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_later_keys_that_are_not_numbers(cuda, dtype):
     """a NaN key in a later row leaves the queries before it alone"""
