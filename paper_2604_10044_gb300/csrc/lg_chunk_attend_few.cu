@@ -4,10 +4,11 @@
 // and no part of them is padding.  A thread holds one key's scores of 16 or 32 of the N rows (N = 16,
 // 32 or 64: row r is token r / g, head r % g; one group of four warps takes 16 rows, two take 32 or
 // 64); it exponentiates them, adds them to its own sums of the normalisers and writes them to its
-// key's row of P^T in shared memory, the products' second operand.  The maxima
-// are the group's: as in the kernel for many rows they may lag by a factor 2^8, so a block asks only
-// whether any score passed that bound (one barrier), and the exact maxima are formed in the first
-// block and when one did.
+// key's row of P^T in shared memory, the products' second operand.  The maxima are the group's: as in
+// the kernel for many rows they may lag by a factor 2^8, so a block asks only whether any score passed
+// that bound (one barrier), and the exact maxima are formed in the first block, when one did, and when
+// a query that has seen nothing so far sees a row (a window may begin in a later block for a tile's
+// later tokens; until then the query has no maximum that its weights could be measured by).
 //
 // Scores are two blocks ahead of the sums (two buffers of S^T and P^T), and the ring holds five
 // blocks of keys or values.
@@ -25,6 +26,7 @@ namespace {
 constexpr int kBn = 128;            // rows of a key block
 constexpr int kPBytes = kBn * 128;  // a buffer of P^T: 128-byte rows, swizzled
 constexpr float kLazy = 8.f;
+constexpr float kNothing = -3e38f;  // below every score by more than kLazy, and finite
 constexpr uint32_t kTmemCols = 256;
 
 template <int D, int N>
@@ -298,7 +300,8 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       const TcPiece &w = bars.queue.at(pc);
       if (w.blk1 < 0) break;
       const int used = w.tokens * a.g;
-      // base: the maxima in use (0 while a query has seen nothing), l: normalisers in pairs
+      // base: the maxima in use (kNothing while a query has seen nothing: its first score passes the
+      // bound, and its hidden rows' weights are 0), l: normalisers in pairs
       float base[NC];
       float2 l2[NC / 2];
 #pragma unroll
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
           }
 #pragma unroll
           for (int q = 0; q < NC; ++q)
-            if (base[q] == -INFINITY) base[q] = 0.f;
+            if (base[q] == -INFINITY) base[q] = kNothing;
 #pragma unroll
           for (int q = 0; q < NC; q += 2) {
             z[q / 2] = __ffma2_rn(make_float2(v[q], v[q + 1]), sc, make_float2(-base[q], -base[q + 1]));

@@ -103,6 +103,48 @@ def test_what_hidden_rows_hold_is_nothing(cuda, dtype, window, sink):
     b.check(out, window, sink)
 
 
+def _under_a_window(b, d, how):
+    """the batch's scores as they are, all lower by 100, far apart, or far apart for each sequence's
+    first token only (its maxima rise in later blocks, beside the others')"""
+    if how == "first token":
+        at = np.concatenate([[0], np.cumsum(b.ms)[:-1]])
+        b.q[at] *= 12.0
+    if how == "low":  # one element of every query and key makes -100 of each score
+        b.q[..., 0] = 16.0
+        b.k[..., 0] = torch.where(b.k[..., 0].isnan(), b.k[..., 0],
+                                  torch.full_like(b.k[..., 0], -100.0 * d ** 0.5 / 16.0))
+    return b.to_device()
+
+
+@pytest.mark.parametrize("how", ["even", "low", "far apart", "first token"])
+@pytest.mark.parametrize("d,H_kv,g,m", [(128, 2, 4, 2), (128, 2, 4, 4), (128, 1, 8, 2), (64, 2, 4, 3),
+                                        (128, 2, 4, 7), (64, 2, 4, 8), (128, 1, 1, 16),
+                                        (128, 2, 4, 16), (64, 4, 1, 50), (128, 1, 3, 21)])
+@pytest.mark.parametrize("window,sink", [(512, 0), (1000, 4), (1024, 0), (4096, 0)])
+def test_some_tokens_whose_windows_start_in_other_blocks(cuda, d, H_kv, g, m, window, sink, how):
+    """a tile of few rows whose first block only some of its tokens see, in whole items and in items
+    that are cut after several blocks"""
+    # the first row that the tile sees stands 1 to 12 rows before a block's end
+    ns = [window + m - 1 + 128 * (1 + i) + 116 + i for i in range(12)]
+    b = Batch(ns, [m] * 12, "bf16", H_kv=H_kv, g=g, d=d, seed=window + m,
+              spread=12.0 if how == "far apart" else 1.0)
+    _under_a_window(b, d, how)
+    b.check(b.attend(window, sink), window, sink)
+    one = Batch(ns[5:6], [m], "bf16", H_kv=H_kv, g=g, d=d, seed=window + m,
+                spread=12.0 if how == "far apart" else 1.0)
+    _under_a_window(one, d, how)
+    one.check(one.attend(window, sink), window, sink)
+
+
+@pytest.mark.parametrize("window,sink", [(1000, 0), (1000, 4)])
+def test_proposed_tokens_of_a_batch_under_a_window(cuda, window, sink):
+    """16 sequences of up to 4099 rows, 32/8 heads, 7 tokens each"""
+    rng = np.random.default_rng(3)
+    ns = [4099] + [int(x) for x in np.exp(rng.uniform(np.log(256), np.log(4099), 15))]
+    b = Batch(ns, [7] * 16, "bf16", H_kv=8, g=4, seed=17).to_device()
+    b.check(b.attend(window, sink), window, sink)
+
+
 @pytest.mark.parametrize("d,m", [(128, 1), (128, 5), (128, 200), (64, 1), (64, 5), (64, 200)])
 def test_hidden_rows_again_and_again(cuda, d, m):
     """rows without numbers behind every window, at every place of the ring that blocks pass through:
