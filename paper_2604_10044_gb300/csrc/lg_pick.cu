@@ -239,9 +239,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, i
     for (int i = tid; i < nw; i += NT) {
       uint32_t w = s_apart[i] & ~s_bias[i];
       s_pass[i] &= ~(w | s_bias[i]);
+      s_apart[i] = 0;
       if (w == 0) continue;
       int at = atomicAdd(&s_aside, __popc(w));
-      s_apart[i] = 0;
       if (at + __popc(w) > kAside) {  // (the word stays, and so does every later one)
         s_apart[i] = w;
         atomicMin(&s_fit, at);

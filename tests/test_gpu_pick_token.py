@@ -115,6 +115,32 @@ def test_many_seen_tokens(cuda, dtype, B):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [3, 200])
+def test_seen_and_biased_beside_many_seen_tokens(cuda, dtype, B):
+    """more seen tokens than a CTA lists, and behind them seen tokens that stand alone in their word of
+    bits and are biased: each counts once, with its bias, however far up it was or is moved"""
+    V = 60013
+    rng = np.random.default_rng(B)
+    host = rng.standard_normal((B, V)).astype(np.float32) * 3
+    alone = np.arange(2600, 3600, 100)
+    host[:, alone[:5]] = 60.0              # on top but for their bias
+    x = _dev(host, cuda, chunk_ref.tdtype(dtype))
+    seen, counts = np.zeros((B, V), dtype=bool), np.zeros((B, V), dtype=np.int64)
+    seen[:, :2500] = True
+    seen[:, alone] = True
+    counts[:, 1000:2000] = rng.integers(0, 3, (B, 1000))
+    counts[:, alone[::2]] = 2
+    pen = rng.random((B, 3)).astype(np.float32) + np.array([1.0, 0.0, 0.0], dtype=np.float32)
+    low = [[(int(t), -100.0) for t in alone] for _ in range(B)]
+    high = [[(int(t), 40.0) for t in alone[5:]] + [(int(t), -100.0) for t in alone[:5]]
+            for _ in range(B)]
+    for bias in (low, high):
+        _run(cuda, x, seen, counts, pen, bias)
+        _run(cuda, x, seen, counts, pen, bias, keep=False)
+        _run(cuda, x.clone(), seen, counts, pen, bias, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_and_in_place(cuda, dtype):
     rng = np.random.default_rng(1)
     for V, pad in ((1001, 6), (777, 0), (640, 3)):
