@@ -213,6 +213,30 @@ def test_bias_lists(cuda):
     _run(cuda, x, bias=bias)
 
 
+@pytest.mark.parametrize("B,V", [(1, 151936), (16, 60013), (200, 33001)])
+def test_the_same_call_gives_the_same_bits(cuda, B, V):
+    """listed tokens, more of them than are listed, and biased ones, some repeatedly: the sums are taken
+    in one order"""
+    rng = np.random.default_rng(V)
+    x = torch.randn((B, V), device=cuda)
+    for n, lists in ((1500, 0), (1500, 200), (30000, 200)):
+        seen, counts, pen = _history(rng, B, V, n)
+        args = [_dev(np.stack([chunk_ref.pack(s) for s in seen]), cuda),
+                _dev(counts.astype(np.int32), cuda),
+                _dev(np.concatenate([pen, np.zeros((B, 1), dtype=np.float32)], 1), cuda)]
+        bias = None
+        if lists:
+            ids = rng.integers(0, V, (B, lists))
+            ids[:, lists // 2:] = ids[:, :lists // 2]      # each of them twice
+            bias = (_dev(np.arange(0, B * lists + 1, lists, dtype=np.int32), cuda),
+                    _dev(ids.reshape(-1).astype(np.int32), cuda), torch.randn(B * lists, device=cuda))
+        tok = torch.zeros((30, B), dtype=torch.int32, device=cuda)
+        pm = torch.zeros((30, B), device=cuda)
+        for i in range(30):
+            lg.lg_pick_token(x, *args, bias, None, tok[i], pm[i])
+        assert (tok == tok[0]).all() and (pm == pm[0]).all(), (n, lists)
+
+
 def test_count_tokens(cuda):
     V, B = 1003, 3
     nw = (V + 31) // 32
