@@ -477,8 +477,10 @@ cudaError_t pick_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int 
                         size_t smem) {
   auto kern = pick_token_kernel<T, NT>;
   LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  // (every call sets the same limit: another thread's call may come between it and the launch)
   if (smem > 36 * 1024)
-    LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LG_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (kMaxSlice / 32 + 1) * 4 * (int)sizeof(uint32_t)));
   cfg.gridDim = dim3((unsigned)(batch * c));
   cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;

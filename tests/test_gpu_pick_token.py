@@ -4,6 +4,7 @@ Tokens and processed logits are exact.  pmax is 1 / s with s a sum of V exponent
 differences d: each off by |d| 2^-23 + 2^-22 of itself (the difference times log2 e, the
 exponential), and |d| e^d <= 1/e, so s is off by at most V 2^-24 + 2^-20 of itself (s >= 1)."""
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -201,6 +202,34 @@ def test_large_vocabulary_and_batch(cuda):
     x[0, -1] = x[1, 777777] = 1.0
     lg.lg_pick_token(x, None, None, None, None, None, tok[:2], pm[:2])
     assert tok[:2].tolist() == [(1 << 20) - 1, 777777]
+
+
+def test_calls_of_several_threads(cuda):
+    """rows whose bits take different amounts of shared memory, from host threads at once"""
+    def calls(V, errors):
+        try:
+            s = torch.cuda.Stream(device=cuda)
+            with torch.cuda.stream(s):
+                x = torch.zeros((310, V), dtype=torch.bfloat16, device=cuda)
+                x[:, V - 7] = 2.0
+                tok = torch.zeros(310, dtype=torch.int32, device=cuda)
+                pm = torch.zeros(310, device=cuda)
+                status = torch.ones(1, dtype=torch.int32, device=cuda)  # (the work is skipped)
+                for _ in range(20000):
+                    lg.lg_pick_token(x, None, None, None, None, None, tok, pm, status)
+                status.zero_()
+                lg.lg_pick_token(x, None, None, None, None, None, tok, pm, status)
+                assert (tok == V - 7).all()
+        except Exception as e:
+            errors.append(e)
+
+    errors = []
+    threads = [threading.Thread(target=calls, args=(V, errors)) for V in (150000, 90000, 250000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
 
 
 def test_bias_lists(cuda):
