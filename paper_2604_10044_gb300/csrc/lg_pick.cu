@@ -146,7 +146,8 @@ constexpr int kMaxCluster = 16;
 constexpr int kMinFew = 2 << 10;       // tokens a CTA takes at least: of few rows
 constexpr int kMinSlice = 8 << 10;     // of more
 constexpr int kMaxSlice = 320 << 10;   // and at most: 16 bytes of bits for every 32
-constexpr int kFourBits = 88 << 10;    // and of four on an SM
+constexpr int kTwoBits = 204 << 10;    // and of two on an SM
+constexpr int kFourBits = 88 << 10;    // and of four
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, int csize) {
@@ -496,11 +497,17 @@ cudaError_t pick_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int 
 }
 
 // Clusters of c CTAs that run at once: a cluster stands within one GPC, so those of more CTAs leave
-// some of the GPU's places empty.  Asked once a size.
+// some of the GPU's places empty.  Asked once a size and device, for bits that leave an SM all the CTAs
+// that it has threads for.  (With the bits of a slice of 208 K tokens and more, one CTA of 512 threads
+// fits an SM instead of two; dividing by that instead was slower: 140 rows of 500000 57 -> 67 us.)
+constexpr int kDevices = 16;
 template <typename T, int NT>
 int clusters_at_once(int c) {
-  static std::atomic<int> known[kMaxCluster + 1];
-  int n = known[c].load(std::memory_order_relaxed);
+  static std::atomic<int> known[kDevices][kMaxCluster + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::atomic<int> *const at = dev < kDevices ? &known[dev][c] : nullptr;
+  int n = at ? at->load(std::memory_order_relaxed) : 0;
   if (n == 0) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -510,7 +517,7 @@ int clusters_at_once(int c) {
       (void)cudaGetLastError();
       n = 0;
     }
-    known[c].store(n, std::memory_order_relaxed);
+    if (at) at->store(n, std::memory_order_relaxed);
   }
   return n;
 }
@@ -531,12 +538,14 @@ cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
 // CTAs a row, of 512 threads (two an SM): the most whose clusters run at once, at most ten, each with
 // 8192 tokens or more (16, and 2048, where rows are so few that every CTA finds an SM of its own), and
 // enough that a slice's bits fit shared memory.  Rows too many for two CTAs each and not for three of 256
-// threads (four an SM) take those; rows too many for one of 512 threads take one of 256, as long as
-// four CTAs' bits fit an SM.  Measured on a GB300, calls back to back, us by threads x CTAs a row:
+// threads (four an SM) take those, while their bits leave room for two an SM; rows too many for one of
+// 512 threads take one of 256, as long as four CTAs' bits fit an SM.  Measured on a GB300, calls back to back, us by threads x CTAs a row:
 //   rows of 128257 bf16:   8  512x10  6.8, 512x16  8.2     16  512x8  7.8, 512x16 12.5 (do not fit)
 //                         48  512x5  11.1, 512x6  16.0    152  512x2 16.1, 256x4  23.2
 //                        192  256x3  22.0, 512x1  25.0    256  512x1 25.7, 256x2  26.9
 //                        608  512x1  52.6, 256x1  79.3 (three an SM)
+//   180 rows of bf16: of 320000 (room for three an SM) 256x3 48, 512x1 62; of 500000 (two) 256x3 69,
+//                     512x2 83; of 900000 (one) 256x3 210, 512x3 129
 //   rows of 32000 bf16:   16  512x3   6.8, 512x10  7.7    608  256x1 17.2, 512x1  21.4
 //   rows of 32000 fp32:    1  512x15  5.6, 512x3   6.6
 template <typename T>
@@ -546,7 +555,7 @@ cudaError_t launch_pick_sized(PickArgs &a, int batch, cudaStream_t s) {
   int c = few ? kMaxCluster : 10, most = a.V / (few ? kMinFew : kMinSlice);
   c = c > most ? (most < 1 ? 1 : most) : c;
   while (c > 1 && clusters_at_once<T, 512>(c) < batch) --c;
-  if (c == 1 && least <= 3 && most >= 3 && batch <= clusters_at_once<T, 256>(3))
+  if (c == 1 && a.V <= 3 * kTwoBits && most >= 3 && batch <= clusters_at_once<T, 256>(3))
     return launch_pick_typed<T, 256>(a, batch, 3, s);
   c = c < least ? least : c;
   if (c == 1 && a.V <= kFourBits && batch > clusters_at_once<T, 512>(1))

@@ -204,6 +204,20 @@ def test_large_vocabulary_and_batch(cuda):
     assert tok[:2].tolist() == [(1 << 20) - 1, 777777]
 
 
+@pytest.mark.parametrize("B,V", [(180, 626688), (180, 626689), (170, 900001), (140, 500001)])
+def test_divisions_of_large_vocabularies(cuda, B, V):
+    """rows on both sides of what leaves room for two CTAs' bits an SM"""
+    x = torch.zeros((B, V), dtype=torch.bfloat16, device=cuda)
+    at = torch.arange(B, device=cuda) * 3001 % V
+    x[torch.arange(B, device=cuda), at] = 3.0
+    tok = torch.zeros(B, dtype=torch.int32, device=cuda)
+    pm = torch.zeros(B, device=cuda)
+    lg.lg_pick_token(x, None, None, None, None, None, tok, pm)
+    assert torch.equal(tok.long(), at)
+    want = 1.0 / (1.0 + (V - 1) * math.exp(-3.0))
+    assert ((pm - want).abs() <= want * (V * 2.0 ** -24 + 2.0 ** -20)).all()
+
+
 def test_calls_of_several_threads(cuda):
     """rows whose bits take different amounts of shared memory, from host threads at once"""
     def calls(V, errors):
