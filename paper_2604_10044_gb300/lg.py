@@ -342,7 +342,11 @@ def _rows_stride(t, name):
     if len(sh) != 3 or st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]):
         raise ValueError("%s: [T][H][d] with whole rows of H * d elements" % name)
     row = sh[1] * sh[2]
-    return st[0] if st[0] > row else row  # one row: its stride says nothing
+    if sh[0] == 1:  # its stride says nothing
+        return row
+    if st[0] < row:  # one row for every token, for instance
+        raise ValueError("%s: [T][H][d] with rows that do not overlap" % name)
+    return st[0]
 
 
 # The calls below refuse what their kernels could not read: tensors of another type, too short, or
@@ -450,6 +454,8 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
     if len(st) != 2 or st[1] != 1:
         raise ValueError("logits: [batch][V] with whole rows")
     B, V = logits.shape
+    if B > 1 and st[0] < V:
+        raise ValueError("logits: [batch][V] with rows that do not overlap")
     if logits_out is not None and (logits_out.dtype is not logits.dtype or
                                    logits_out.stride() != st or logits_out.shape != (B, V)):
         raise ValueError("logits_out: dtype, strides and shape of logits")
@@ -476,7 +482,7 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
             _refuse("bias", "[batch + 1] int32, int32, fp32")
         bs = ctypes.byref(LgBias(off.data_ptr(), ids.data_ptr(), val.data_ptr()))
     x = LgLogits(logits.data_ptr(), _LOGITS.get(logits.dtype, -1), B, V, 0,
-                 max(st[0], V))  # one row: its stride says nothing
+                 st[0] if B > 1 else V)  # one row: its stride says nothing
     rc = (_lib or lib()).lg_pick_token(
         ctypes.byref(x), None if seen is None else seen.data_ptr(),
         None if counts is None else counts.data_ptr(),
