@@ -325,6 +325,8 @@ class Chunk:
     token arrays; max_new, a bound on the new tokens of one sequence."""
 
     def __init__(self, off, T, max_new):
+        if off.dtype is not torch.int32 or not off.is_contiguous():
+            raise ValueError("off: dense [batch + 1] int32")
         self.off, self.T, self.max_new = off, int(T), int(max_new)
         self.c = LgChunk(off=_ptr(off), T=self.T, max_new=self.max_new)
 
@@ -349,12 +351,23 @@ def _rows_stride(t, name):
     return st[0]
 
 
-# The calls below refuse what their kernels could not read: tensors of another type, too short, or
-# (its first tensor is looked at) of another device than the current one, whose stream
-# the call takes.  Those that a decode step makes have the conditions and the call in place: functions
-# around them took 0.5 to 2 us of the 6 to 8 that a call takes its caller (Grace).
+# The calls below refuse what their kernels could not read: tensors of another type, too short, not
+# dense (a slice, one row expanded over the batch), or (its first tensor is looked at) of another device
+# than the current one, whose stream the call takes.
 def _refuse(what, needs):
-    raise ValueError("%s: on the current CUDA device, %s" % (what, needs))
+    raise ValueError("%s: on the current CUDA device, dense, %s" % (what, needs))
+
+
+def _dense(t, dt, n):
+    """n elements of the type dt at t's address, at least"""
+    return t.dtype is dt and t.numel() >= n and t.is_contiguous()
+
+
+def _dense_rows(t, dt, rows, cols):
+    """the same of rows of cols, as a matrix of them or flat; dt None: any words of 32 bits"""
+    sh = t.shape
+    return ((t.element_size() == 4 if dt is None else t.dtype is dt) and t.is_contiguous() and
+            (sh[0] >= rows and sh[1] == cols if len(sh) == 2 else t.numel() >= rows * cols))
 
 
 _device = _get_device or torch.cuda.current_device
@@ -391,7 +404,7 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
         _refuse("q_out", "[T][H_q][d] of the cache's type")
     if k_new.dtype is not dt or v_new.dtype is not dt or k_new.numel() < n or v_new.numel() < n:
         _refuse("k_new, v_new", "[T][H_kv][d] of the cache's type")
-    if pos is not None and (pos.dtype is not torch.int32 or pos.numel() < T):
+    if pos is not None and not _dense(pos, torch.int32, T):
         _refuse("pos", "[T] int32")
     at = k_new.get_device()
     if at < 0 or at != _device():
@@ -418,6 +431,8 @@ def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max
     n, dt = chunk.T * H_q * cache.d, cache.k.dtype
     if q.dtype is not dt or out.dtype is not dt or q.numel() < n or out.numel() < n:
         _refuse("q, out", "[T][H_q][d] of the cache's type")
+    if not ws.is_contiguous():
+        _refuse("ws", "bytes")
     at = q.get_device()
     if at < 0 or at != _device():
         _refuse("q", "the other tensors too")
@@ -432,10 +447,13 @@ def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max
 def lg_count_tokens(tokens, off, V, generated, seen, counts, status=None, stream=None):
     """tokens of row b: tokens[off[b]] .. tokens[off[b + 1] - 1], or tokens[b] with off None"""
     batch = tokens.numel() if off is None else off.numel() - 1
-    if (tokens.dtype is not torch.int32 or counts.dtype is not torch.int32 or
-            counts.numel() < batch * V or seen.element_size() != 4 or
-            seen.numel() < batch * ((V + 31) // 32)):
+    if (not _dense(tokens, torch.int32, 0) or not _dense_rows(counts, torch.int32, batch, V) or
+            not _dense_rows(seen, None, batch, (V + 31) // 32)):
         _refuse("tokens, seen, counts", "int32, [batch][ceil(V/32)] words, [batch][V] int32")
+    if off is not None and not _dense(off, torch.int32, 0):
+        _refuse("off", "[batch + 1] int32")
+    if status is not None and not _dense(status, torch.int32, 1):
+        _refuse("status", "a word of int32")
     at = tokens.get_device()
     if at < 0 or at != _device():
         _refuse("tokens", "the other tensors too")
@@ -459,27 +477,27 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
     if logits_out is not None and (logits_out.dtype is not logits.dtype or
                                    logits_out.stride() != st or logits_out.shape != (B, V)):
         raise ValueError("logits_out: dtype, strides and shape of logits")
-    if (tokens.dtype is not torch.int32 or pmax.dtype is not torch.float32 or
-            tokens.numel() < B or pmax.numel() < B):
+    if not _dense(tokens, torch.int32, B) or not _dense(pmax, torch.float32, B):
         _refuse("tokens, pmax", "[batch] int32, fp32")
-    if seen is not None and (seen.element_size() != 4 or seen.numel() < B * ((V + 31) // 32) or
-                             counts is not None and (counts.dtype is not torch.int32 or
-                                                     counts.numel() < B * V)):
+    nw = (V + 31) // 32
+    if seen is not None and not _dense_rows(seen, None, B, nw) or \
+            counts is not None and not _dense_rows(counts, torch.int32, B, V):
         _refuse("seen, counts", "[batch][ceil(V/32)] words, [batch][V] int32")
-    if penalty is not None and (penalty.dtype is not torch.float32 or penalty.numel() < 4 * B):
+    if penalty is not None and not _dense_rows(penalty, torch.float32, B, 4):
         _refuse("penalty", "[batch][4] fp32")
-    if allowed is not None and (allowed.element_size() != 4 or
-                                allowed.numel() < B * ((V + 31) // 32)):
+    if allowed is not None and not _dense_rows(allowed, None, B, nw):
         _refuse("allowed", "[batch][ceil(V/32)] words")
+    if status is not None and not _dense(status, torch.int32, 1):
+        _refuse("status", "a word of int32")
     at = logits.get_device()
     if at < 0 or at != _device():
         _refuse("logits", "the other tensors too")
     bs = None
     if bias is not None:
         off, ids, val = bias
-        if (off.dtype is not torch.int32 or ids.dtype is not torch.int32 or
-                val.dtype is not torch.float32 or off.numel() < B + 1):
-            _refuse("bias", "[batch + 1] int32, int32, fp32")
+        if (not _dense(off, torch.int32, B + 1) or not _dense(ids, torch.int32, 0) or
+                not _dense(val, torch.float32, ids.numel())):
+            _refuse("bias", "[batch + 1] int32, int32, as many fp32")
         bs = ctypes.byref(LgBias(off.data_ptr(), ids.data_ptr(), val.data_ptr()))
     x = LgLogits(logits.data_ptr(), _LOGITS.get(logits.dtype, -1), B, V, 0,
                  st[0] if B > 1 else V)  # one row: its stride says nothing

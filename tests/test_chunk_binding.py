@@ -130,3 +130,60 @@ def test_one_row_may_have_any_stride():
     """the stride between rows says nothing of one"""
     assert lg._rows_stride(z(H_Q * D).as_strided((1, H_Q, D), (1, D, 1)), "q") == H_Q * D
     assert lg._rows_stride(z(H_Q * D + 9).as_strided((1, H_Q, D), (H_Q * D + 9, D, 1)), "q") == H_Q * D
+
+
+def _sliced(t):
+    """the same shape and values, every second element of a larger tensor"""
+    return torch.stack([t, t], -1)[..., 0]
+
+
+def _broadcast(t):
+    """the same shape from one element"""
+    return t.reshape(-1)[:1].expand(t.numel()).view(t.shape) if t.dim() == 1 else \
+        t[:1].expand(t.shape)
+
+
+DENSE = {begin: ["off"], rope: ["off", "pos", "out"], attend: ["off", "q", "out"],
+         pick: ["seen", "counts", "penalty", "off", "id", "val", "allowed", "tokens", "pmax"],
+         count: ["tokens", "off", "seen", "counts"]}
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c in CALLS for n in DENSE[c]])
+def test_tensors_that_are_not_dense(call, name):
+    """a slice of a larger tensor; one element or row for all of them"""
+    shapes = dict(seen=z(B, NW), counts=z(B, V), allowed=z(B, NW), penalty=z(B, 4, dtype=torch.float32),
+                  id=z(9), val=z(9, dtype=torch.float32), pmax=z(B, dtype=torch.float32),
+                  pos=z(T), out=z(T, H_Q, D, dtype=BF16), q=z(T, H_Q, D, dtype=BF16), off=z(B + 1),
+                  tokens=z(20) if call is count else z(B))
+    for bad in (_sliced(shapes[name]), _broadcast(shapes[name])):
+        assert bad.shape == shapes[name].shape and not bad.is_contiguous()
+        with pytest.raises(ValueError):
+            call(**{name: bad})
+
+
+@pytest.mark.parametrize("call,name,bad", [
+    (pick, "seen", z(B, NW + 1)), (pick, "counts", z(B, V + 2)), (pick, "allowed", z(B, NW + 1)),
+    (pick, "penalty", z(B, 8, dtype=torch.float32)), (count, "seen", z(B, NW + 1)),
+    (count, "counts", z(B, V + 2))])
+def test_rows_of_another_length(call, name, bad):
+    """long enough, but row b does not begin where the kernels take it from"""
+    with pytest.raises(ValueError):
+        call(**{name: bad})
+
+
+def test_more_rows_and_flat_rows_are_passed_on():
+    with pytest.raises(Launched):
+        pick(seen=z(B + 2, NW), counts=z((B + 1) * V), allowed=z(B * NW), tokens=z(B + 4))
+    with pytest.raises(Launched):
+        count(seen=z(B * NW), counts=z(B + 2, V))
+
+
+def test_workspaces_and_status_words():
+    with pytest.raises(ValueError):
+        attend(ws=z(2048, dtype=torch.uint8)[::2])
+    for call in (pick, count):
+        for bad in (z(0), z(1, dtype=torch.int64)):
+            with pytest.raises(ValueError):
+                call(status=bad)
+        with pytest.raises(Launched):
+            call(status=None)
