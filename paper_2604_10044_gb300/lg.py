@@ -338,10 +338,12 @@ class Chunk:
                    int(max(counts)))
 
 
-def _rows_stride(t, name):
-    """elements from token to token of a [T][H][d] tensor whose rows are whole"""
+def _rows_stride(t, name, T=0, H=0, d=None):
+    """elements from token to token of a [T][H][d] tensor whose rows are whole (T rows and H heads at
+    least)"""
     st, sh = t.stride(), t.shape
-    if len(sh) != 3 or st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]):
+    if (len(sh) != 3 or st[2] != 1 or (sh[1] > 1 and st[1] != sh[2]) or sh[0] < T or sh[1] < H or
+            d is not None and sh[2] != d):
         raise ValueError("%s: [T][H][d] with whole rows of H * d elements" % name)
     row = sh[1] * sh[2]
     if sh[0] == 1:  # its stride says nothing
@@ -370,6 +372,11 @@ def _dense_rows(t, dt, rows, cols):
             (sh[0] >= rows and sh[1] == cols if len(sh) == 2 else t.numel() >= rows * cols))
 
 
+def _covers(chunk, cache):
+    if chunk.off.numel() <= cache.c.batch:
+        _refuse("off", "[batch + 1] int32")
+
+
 _device = _get_device or torch.cuda.current_device
 
 
@@ -377,6 +384,7 @@ def lg_begin_chunk(cache, chunk, stream=None):
     at = cache.status.get_device()
     if at < 0 or at != _device():
         _refuse("cache", "chunk too")
+    _covers(chunk, cache)
     _call("lg_begin_chunk", ctypes.byref(cache.c), ctypes.byref(chunk.c), _stream(stream))
 
 
@@ -393,17 +401,18 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
     projection pass as they are"""
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out: dense [T][H_q][d]")
-    T, d, dt = chunk.T, cache.d, cache.k.dtype
-    n = T * cache.H_kv * d
+    T, H_kv, d, dt = chunk.T, cache.H_kv, cache.d, cache.k.dtype
     H_q = qs = 0
     if q is not None:
-        H_q, qs = q.shape[1], _rows_stride(q, "q")
-        if q.dtype is not dt or q.numel() < T * H_q * d:
+        H_q, qs = q.shape[1], _rows_stride(q, "q", T, 0, d)
+        if q.dtype is not dt:
             _refuse("q", "[T][H_q][d] of the cache's type")
-    if q_out is not None and (q_out.dtype is not dt or q_out.numel() < T * H_q * d):
+    if q_out is not None and not _dense(q_out, dt, T * H_q * d):
         _refuse("q_out", "[T][H_q][d] of the cache's type")
-    if k_new.dtype is not dt or v_new.dtype is not dt or k_new.numel() < n or v_new.numel() < n:
+    ks, vs = _rows_stride(k_new, "k_new", T, H_kv, d), _rows_stride(v_new, "v_new", T, H_kv, d)
+    if k_new.dtype is not dt or v_new.dtype is not dt:
         _refuse("k_new, v_new", "[T][H_kv][d] of the cache's type")
+    _covers(chunk, cache)
     if pos is not None and not _dense(pos, torch.int32, T):
         _refuse("pos", "[T] int32")
     at = k_new.get_device()
@@ -411,10 +420,9 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
         _refuse("k_new", "the other tensors too")
     rc = (_lib or lib()).lg_rope_append(
         ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, None if q is None else q.data_ptr(), qs,
-        H_q, k_new.data_ptr(), _rows_stride(k_new, "k_new"), v_new.data_ptr(),
-        _rows_stride(v_new, "v_new"), None if pos is None else pos.data_ptr(), ctypes.byref(rope),
-        None if q_out is None else q_out.data_ptr(), ctypes.byref(params),
-        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+        H_q, k_new.data_ptr(), ks, v_new.data_ptr(), vs, None if pos is None else pos.data_ptr(),
+        ctypes.byref(rope), None if q_out is None else q_out.data_ptr(),
+        ctypes.byref(params), _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
     if rc:
         raise LgError("lg_rope_append", rc)
 
@@ -433,6 +441,7 @@ def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max
         _refuse("q, out", "[T][H_q][d] of the cache's type")
     if not ws.is_contiguous():
         _refuse("ws", "bytes")
+    _covers(chunk, cache)
     at = q.get_device()
     if at < 0 or at != _device():
         _refuse("q", "the other tensors too")

@@ -187,3 +187,23 @@ def test_workspaces_and_status_words():
                 call(status=bad)
         with pytest.raises(Launched):
             call(status=None)
+
+
+@pytest.mark.parametrize("name,bad", [
+    ("k", z(T - 1, H_KV * 2, D, dtype=BF16)), ("k", z(1, T * H_KV, D, dtype=BF16)),
+    ("k", z(T, H_KV * 2, D // 2, dtype=BF16)), ("k", z(2 * T, H_KV - 1, D, dtype=BF16)),
+    ("v", z(T - 1, H_KV, D * 2, dtype=BF16)), ("v", z(T * 2, H_KV, D // 2, dtype=BF16)),
+    ("q", z(T - 1, H_Q, D * 2, dtype=BF16)), ("q", z(T, H_Q, D * 2, dtype=BF16)),
+    ("q", z(T * 2, H_Q, D // 2, dtype=BF16))])
+def test_tokens_of_another_shape(name, bad):
+    """as many elements as are needed, but in fewer rows, or of heads of another size or number"""
+    with pytest.raises(ValueError):
+        rope(**{name: bad}, **(dict(out=z(4 * T, H_Q, D, dtype=BF16)) if name == "q" else {}))
+
+
+@pytest.mark.parametrize("call", [begin, rope, attend])
+def test_offsets_of_fewer_sequences(call):
+    with pytest.raises(ValueError):
+        call(off=z(B))
+    with pytest.raises(Launched):
+        call(off=z(B + 3))
