@@ -207,3 +207,24 @@ def test_offsets_of_fewer_sequences(call):
         call(off=z(B))
     with pytest.raises(Launched):
         call(off=z(B + 3))
+
+
+ALL = {begin: ["status", "off"], rope: ["off", "q", "k", "v", "pos", "out"],
+       attend: ["off", "q", "out", "ws"],
+       pick: ["logits", "seen", "counts", "penalty", "off", "id", "val", "allowed", "tokens", "pmax",
+              "status", "kept"],
+       count: ["tokens", "off", "seen", "counts", "status"]}
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c in CALLS for n in ALL[c]])
+@pytest.mark.parametrize("dev", [-1, 0, 2])
+def test_one_tensor_on_another_device(call, name, dev):
+    """any of them, on the CPU or on another GPU than the current one"""
+    shapes = dict(q=z(T, H_Q, D, dtype=BF16), k=z(T, H_KV, D, dtype=BF16), v=z(T, H_KV, D, dtype=BF16),
+                  out=z(T, H_Q, D, dtype=BF16), ws=z(1024, dtype=torch.uint8), pos=z(T), off=z(B + 1),
+                  logits=z(B, V, dtype=BF16), kept=z(B, V, dtype=BF16), seen=z(B, NW), counts=z(B, V),
+                  allowed=z(B, NW), penalty=z(B, 4, dtype=torch.float32), id=z(9),
+                  val=z(9, dtype=torch.float32), pmax=z(B, dtype=torch.float32), status=z(1),
+                  tokens=z(20) if call is count else z(B))
+    with pytest.raises(ValueError):
+        call(**{name: On(shapes[name], dev)})
