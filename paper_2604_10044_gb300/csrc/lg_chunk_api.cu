@@ -202,6 +202,9 @@ lg_status lg_count_tokens(const int32_t *tokens, const int32_t *off, int T, int 
                           cudaStream_t s) {
   if (!tokens || !seen || !counts || T < 0 || batch < 1 || V < 1 || (!off && T != batch))
     return LG_ERR_INVALID_ARG;
+  if (!aligned(tokens, 4) || !aligned(off, 4) || !aligned(seen, 4) || !aligned(counts, 4) ||
+      !aligned(dev_status, 4))
+    return LG_ERR_INVALID_ARG;
   return cuda_status(lg::launch_count_tokens(tokens, off, T, batch, V, generated, seen, counts,
                                              dev_status, s));
 }
@@ -216,10 +219,15 @@ lg_status lg_pick_token(const lg_logits *x, const uint32_t *seen, const int32_t 
   if (x->batch < 1 || x->V < 1 || x->stride < x->V) return LG_ERR_INVALID_ARG;
   if (x->V > 1 << 20 || x->batch > 1 << 20) return LG_ERR_UNSUPPORTED;
   if (!aligned(x->x, es) || !aligned(logits_out, es)) return LG_ERR_INVALID_ARG;
+  if (!aligned(seen, 4) || !aligned(counts, 4) || !aligned(allowed, 4) || !aligned(tokens, 4) ||
+      !aligned(pmax, 4) || !aligned(dev_status, 4))
+    return LG_ERR_INVALID_ARG;
   if ((seen == nullptr) != (counts == nullptr) || (seen == nullptr) != (penalty == nullptr) ||
       !aligned(penalty, 16))
     return LG_ERR_INVALID_ARG;
-  if (bias && (!bias->off || !bias->id || !bias->val)) return LG_ERR_INVALID_ARG;
+  if (bias && (!bias->off || !bias->id || !bias->val || !aligned(bias->off, 4) ||
+               !aligned(bias->id, 4) || !aligned(bias->val, 4)))
+    return LG_ERR_INVALID_ARG;
   return cuda_status(lg::launch_pick_token(*x, seen, counts, penalty, bias, allowed, tokens, pmax,
                                            logits_out, dev_status, s));
 }
