@@ -85,7 +85,7 @@ LG_API lg_status lg_default_rope_params(lg_rope_params *p, int d);
    q: device [T][H_q][d] dtype; k_new, v_new: device [T][H_kv][d]; each with its own stride from
    token to token in elements (a multiple of 16 bytes, at least the row), so that slices of one
    projection's output pass as they are.  q_out: device [T][H_q][d] dense; it may be q itself when
-   q is dense.  q and q_out may be null together with H_q = 0 (keys and values only).  pos: device
+   q is dense, and overlaps none of the inputs otherwise.  q and q_out may be null together with H_q = 0 (keys and values only).  pos: device
    [T].  16-byte alignment throughout (pos 4).  Call after lg_begin_chunk. */
 LG_API lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const void *q,
                                 int64_t q_stride, int H_q, const void *k_new, int64_t k_stride,
@@ -158,8 +158,8 @@ LG_API lg_status lg_count_tokens(const int32_t *tokens, const int32_t *off, int 
    {repetition > 0, presence, frequency, unused}, 16-byte aligned, with seen; bias, allowed
    (device [batch][ceil(V/32)] words) nullable.  tokens: device [batch] int32; pmax: device [batch]
    fp32.  logits_out: nullable, device, dtype and stride of x, the processed logits (masked ones
-   -infinity) rounded once; may be x itself.  x and logits_out need the alignment of their
-   elements only.  dev_status: nullable, a cache's sticky status word. */
+   -infinity) rounded once; may be x itself, or rows that share nothing with x's.  x and logits_out
+   need the alignment of their elements only.  dev_status: nullable, a cache's sticky status word. */
 LG_API lg_status lg_pick_token(const lg_logits *x, const uint32_t *seen, const int32_t *counts,
                                const float *penalty, const lg_bias *bias, const uint32_t *allowed,
                                int32_t *tokens, float *pmax, void *logits_out,

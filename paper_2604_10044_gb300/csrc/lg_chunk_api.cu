@@ -15,6 +15,12 @@ using lg::check_params;
 
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+// n and m bytes at a and b have some in common
+bool overlap(const void *a, uint64_t n, const void *b, uint64_t m) {
+  const uint64_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + m && y < x + n;
+}
+
 lg_status cuda_status(cudaError_t e) { return e == cudaSuccess ? LG_OK : LG_ERR_CUDA; }
 
 lg_status check_chunk(const lg_cache *c, const lg_chunk *ch) {
@@ -142,7 +148,16 @@ lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const
       v_stride < (int64_t)c->H_kv * c->d)
     return LG_ERR_INVALID_ARG;
   if (H_q > 0 && (q_stride % el || q_stride < (int64_t)H_q * c->d)) return LG_ERR_INVALID_ARG;
-  if (H_q > 0 && q == q_out && q_stride != (int64_t)H_q * c->d) return LG_ERR_INVALID_ARG;
+  if (H_q > 0) {  // the rotated queries overwrite none that other threads still read
+    const uint64_t es = 16 / el, row = (uint64_t)H_q * c->d * es;
+    const uint64_t kv_row = (uint64_t)c->H_kv * c->d * es, last = (uint64_t)(ch->T - 1) * es;
+    if (q == q_out ? q_stride != (int64_t)H_q * c->d
+                   : overlap(q_out, ch->T * row, q, last * q_stride + row))
+      return LG_ERR_INVALID_ARG;
+    if (overlap(q_out, ch->T * row, k_new, last * k_stride + kv_row) ||
+        overlap(q_out, ch->T * row, v_new, last * v_stride + kv_row))
+      return LG_ERR_INVALID_ARG;
+  }
   uint64_t turns[64];
   rope_turns(*rp, turns);
   return cuda_status(lg::launch_rope_append(*c, *ch, layer, q, q_stride, H_q, k_new, k_stride,
@@ -169,6 +184,8 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
   const int g = H_q / c->H_kv;
   const lg::ChunkGrid grid = lg::chunk_grid(c->dtype, c->d, g, ch->max_new);
   if (!ws || !aligned(ws, 256) || ws_bytes < part_bytes(grid, c->d)) return LG_ERR_WORKSPACE;
+  const uint64_t bytes = (uint64_t)ch->T * H_q * c->d * (c->dtype == LG_BF16 ? 2 : 4);
+  if (overlap(q, bytes, out, bytes)) return LG_ERR_INVALID_ARG;
   lg::ChunkAttendArgs a = {};
   a.K = c->k;
   a.V = c->v;
@@ -228,6 +245,14 @@ lg_status lg_pick_token(const lg_logits *x, const uint32_t *seen, const int32_t 
   if (bias && (!bias->off || !bias->id || !bias->val || !aligned(bias->off, 4) ||
                !aligned(bias->id, 4) || !aligned(bias->val, 4)))
     return LG_ERR_INVALID_ARG;
+  if (logits_out && logits_out != x->x) {  // rows beside x's in one buffer, or apart from them
+    const uint64_t step = (uint64_t)x->stride * es, row = (uint64_t)x->V * es;
+    const uint64_t all = (uint64_t)(x->batch - 1) * step + row;
+    const uint64_t from = (uintptr_t)x->x, to = (uintptr_t)logits_out;
+    const uint64_t d = to > from ? (to - from) % step : (step - (from - to) % step) % step;
+    const bool beside = d >= row && d + row <= step;
+    if (overlap(x->x, all, logits_out, all) && !beside) return LG_ERR_INVALID_ARG;
+  }
   return cuda_status(lg::launch_pick_token(*x, seen, counts, penalty, bias, allowed, tokens, pmax,
                                            logits_out, dev_status, s));
 }
