@@ -591,7 +591,7 @@ cudaError_t launch_count_tokens(const int32_t *tokens, const int32_t *off, int T
                                 int generated, uint32_t *seen, int32_t *counts, int32_t *status,
                                 cudaStream_t s) {
   if (T == 0) return cudaSuccess;
-  LG_TRY(launch_pdl(count_tokens_kernel, (T + 255) / 256, 256, 0, s, tokens, off, T, batch, V,
+  LG_TRY(launch_pdl(count_tokens_kernel, ((unsigned)T + 255) / 256, 256, 0, s, tokens, off, T, batch, V,
                     (V + 31) / 32, generated, seen, counts, status));
   return cudaGetLastError();
 }

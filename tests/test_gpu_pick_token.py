@@ -307,6 +307,22 @@ def test_count_tokens(cuda):
     assert np.array_equal(seen.cpu().numpy(), np.stack([chunk_ref.pack(s) for s in want_s]))
 
 
+def test_count_as_many_tokens_as_fit(cuda):
+    """2^31 - 10 tokens, most of them none of the vocabulary"""
+    T, V = 2 ** 31 - 10, 40
+    tokens = torch.full((T,), -1, dtype=torch.int32, device=cuda)
+    tokens[-3:] = torch.tensor([7, 39, 7], dtype=torch.int32)
+    off = torch.tensor([0, T - 1, T], dtype=torch.int32, device=cuda)
+    seen = torch.zeros((2, 2), dtype=torch.int32, device=cuda)
+    counts = torch.zeros((2, V), dtype=torch.int32, device=cuda)
+    lg.lg_count_tokens(tokens, off, V, 1, seen, counts)
+    want = torch.zeros((2, V), dtype=torch.int32)
+    want[0, [7, 39]] = 1
+    want[1, 7] = 1
+    assert torch.equal(counts.cpu(), want)
+    assert seen.tolist() == [[1 << 7, 1 << 7], [1 << 7, 0]]
+
+
 def test_status_and_streams_and_graphs(cuda):
     V = 20000
     x = torch.randn((2, V), device=cuda)
