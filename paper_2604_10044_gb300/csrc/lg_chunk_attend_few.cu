@@ -308,7 +308,9 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (int q = 0; q < NC; ++q) base[q] = 0.f;
 #pragma unroll
       for (int q = 0; q < NC / 2; ++q) l2[q] = make_float2(0.f, 0.f);
-      if (key < NC) bars.m[q0 + key] = -INFINITY;
+      // (rows of the tile that are no query, which may hold anything: their scores are below it always,
+      // so that they never ask for the maxima, by which the queries' weights would be rounded otherwise)
+      if (key < NC) bars.m[q0 + key] = q0 + key < used ? -INFINITY : INFINITY;
       const float2 sc = make_float2(a.qscale, a.qscale);
       for (int blk = w.blk0; blk < w.blk1; ++blk, ++c) {
         const uint32_t b = c & 1;
@@ -337,7 +339,6 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
           z[q / 2] = __ffma2_rn(make_float2(v[q], v[q + 1]), sc, make_float2(-base[q], -base[q + 1]));
           top = max3(top, z[q / 2].x, z[q / 2].y);
         }
-        // (rows of the tile that are no query may hold anything; they only ask too often)
         if (keys_any(grp, top > kLazy || blk == w.blk0)) {
           float mine = -INFINITY;  // lane q: the warp's maximum of row q
 #pragma unroll

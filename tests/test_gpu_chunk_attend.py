@@ -278,6 +278,25 @@ def test_short_last_tiles_one_after_another(cuda, d, H_kv, g):
         assert torch.equal(out, b.attend())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("g,m", [(3, 1), (5, 1), (6, 4), (7, 2), (4, 3), (1, 7), (5, 12), (3, 90)])
+def test_rows_beside_a_tiles_queries_change_no_bit(cuda, dtype, g, m):
+    """rows of a tile that are no query: what the shared memory held before the call, and the queries of
+    the sequences behind"""
+    ns = [1500 + 31 * i for i in range(40)]
+    b = Batch(ns, [m] * 40, dtype, H_kv=2, g=g, seed=18).to_device()
+    full = Batch([1500] * 40, [m] * 40, dtype, H_kv=1, g=8, seed=18).to_device()
+    q, out = b.qd.clone(), b.attend()
+    b.check(out)
+    for value in (0.0, 300.0, -300.0, 1e30, math.inf, math.nan):
+        full.qd.fill_(value)  # (its tiles' rows are queries all)
+        full.attend()
+        assert torch.equal(out, b.attend()), value
+        b.qd[m:] = value
+        assert torch.equal(out[:m], b.attend()[:m]), value
+        b.qd.copy_(q)
+
+
 @pytest.mark.parametrize("what", ["max_len", "max_new", "more new rows than rows", "T", "order"])
 def test_lengths_out_of_bounds_are_an_error(cuda, what):
     b = Batch([200, 90], [30, 20], "bf16", seed=11).to_device()
