@@ -46,7 +46,7 @@ template <int ST>
 struct TcBars {
   uint64_t full[ST], empty[ST];      // ring of key and value blocks
   uint64_t fixed[ST];                // what hidden rows hold is cleared
-  uint64_t q_full, q_empty;
+  uint64_t q_full[2], q_empty;       // a stream's queries, of the pieces that it has part in; all read
   // of stream s and buffer b, at 2 s + b: scores ready, half of and all weights ready, sums ready (with
   // one buffer: the piece's)
   uint64_t s_full[4], p_half[4], p_full[4], o_full[4];
@@ -92,7 +92,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars.empty[i], 3);  // both streams' products and the clearing warp
       mbar_init(&bars.fixed[i], 1);
     }
-    mbar_init(&bars.q_full, 1);
     mbar_init(&bars.q_empty, 2);
     for (int i = 0; i < 4; ++i) {
       mbar_init(&bars.s_full[i], 1);
@@ -101,6 +100,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars.o_full[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.q_full[i], 1);
       mbar_init(&bars.o_free[i], 4);
       mbar_init(&bars.turn[i], 1);
     }
@@ -149,12 +149,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = bars.queue.put(bars, pieces, w, a) &&
                tc_wait(bars, &bars.q_empty, (pieces & 1) ^ 1);
           if (!ok) break;
-          mbar_arrive_expect_tx(&bars.q_full, tiles * C::kBoxes * tpt * a.g * 128);
-          for (int s = 0; s < tiles; ++s)
+          for (int s = 0; s < tiles; ++s) {
+            mbar_arrive_expect_tx(&bars.q_full[s], C::kBoxes * tpt * a.g * 128);
 #pragma unroll
             for (int x = 0; x < C::kBoxes; ++x)
               tma_box_3d(sq + s * C::kQTile + x * (128 * 128), &mq, 64 * x, w.kvh * a.g,
-                         w.off + w.t * a.shape.tok + s * tpt, &bars.q_full);
+                         w.off + w.t * a.shape.tok + s * tpt, &bars.q_full[s]);
+          }
           ++pieces;
           // keys NB blocks ahead of the values, as the products take them
           auto row = [&](int j) { return (int)w.row0 + w.blocks.index(j) * kBn; };
@@ -214,14 +215,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait_full(n);
             if (ok && one) mbar_arrive(&bars.empty[n % ST]);
           }
-          // This piece's queries too, though they are the other stream's: a wait for the next piece's
-          // knows only that the phase's parity has passed, and would pass before these arrived.
-          ok = ok && tc_wait_warp(bars, &bars.q_full, pc & 1);
           if (!ok) break;
           if (one) mbar_arrive(&bars.q_empty);
           continue;
         }
-        ok = tc_wait_warp(bars, &bars.q_full, pc & 1);
+        ok = tc_wait_warp(bars, &bars.q_full[s], mine & 1);
         const int ahead = blocks < NB ? blocks : NB;
         for (int i = 0; i < ahead; ++i) {
           wait_full(n + i);
@@ -235,12 +233,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           // (value block j follows the keys ahead of it and j pairs, or what pairs there are)
           const uint32_t iv = n + ahead + j + (j < blocks - ahead ? j : blocks - ahead);
           const uint32_t b = c % NB, par = (c / NB) & 1, ts = ts0 + b * kBn;
-          // (the copy before the clearing: its arrival says that the ring's slot has been through the
-          // clearing warp before, and so which phase of `fixed` the parity means)
-          wait_full(iv);
+          // The next keys, and the values, or, where the block hides rows, their clearing.  A copy's
+          // arrival, the values' own or a later one's, says that the ring's slot has been through the
+          // clearing warp before, and so which phase of `fixed` the parity means.
+          const bool last = j + NB >= blocks;
+          wait_full(last ? iv : iv + 1);
           if (j < open0 || j >= open1)
             ok = ok && tc_wait_warp(bars, &bars.fixed[iv % ST], (iv / ST) & 1);
-          if (j + NB < blocks) wait_full(iv + 1);
+          else if (!last)
+            wait_full(iv);
           ok = ok && tc_wait_warp(bars, &(NB == 1 ? bars.p_half : bars.p_full)[2 * s + b], par);
           if (NB == 1 && two) ok = ok && tc_wait_warp(bars, &bars.turn[s], (turns & 1) ^ (s ^ 1));
           if (!ok) break;
