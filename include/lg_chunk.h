@@ -8,9 +8,14 @@
  * A prompt, or a chunk of one, on this ABI:
  *   lg_begin_chunk, then for each layer lg_rope_append -> lg_chunk_attend, then lg_pick_token on
  *   the last rows' logits and lg_count_tokens
- * after which the decode steps of lg.h follow.  A decode step whose keys come unrotated, or whose
- * attention has a sliding window, is a chunk of one token a sequence.  lg_pick_token's outputs are
- * what lg_token_detect and lg_token_detect_prune read.
+ * after which the decode steps of lg.h follow.  A decode step whose keys come unrotated is
+ * lg_begin_chunk and, for each layer, lg_rope_append -> lg_decode_attend; one whose attention has a
+ * sliding window is a chunk of one token a sequence through lg_chunk_attend.
+ *
+ * What lg_chunk_attend does not do: it returns no statistics (lg_detect cannot follow such a step;
+ * lg_token_detect can, from tokens and probabilities) and adds to no H2O scores.  A single token
+ * without a window belongs into lg_decode_attend, which does both, in half the time for one short
+ * sequence.
  *
  * These calls have no counterpart in the paper (arXiv 2604.10044): its guard reads keys, values,
  * tokens and top-1 probabilities (Sec. 3.1, Sec. 5.2, Eq. 8) that a model step produces here.
@@ -75,8 +80,10 @@ typedef struct {
 LG_API lg_status lg_default_rope_params(lg_rope_params *p, int d);
 
 /* Rotary positions of one layer's queries and keys, and the keys and values joining the cache:
-   with angle a = pos[t] f_i (exact modulo a turn at any 32-bit position), a pair (x, y) becomes
-   mscale (x cos a - y sin a, x sin a + y cos a); the other elements of a head are copied.
+   with angle a = pos[t] f_i, a pair (x, y) becomes mscale (x cos a - y sin a, x sin a + y cos a);
+   the other elements of a head are copied.  The product with the position is exact modulo a turn;
+   the frequency has the 53 bits of a double and some twenty roundings, so an angle is off by less
+   than pos[t] f_i 2^-48 radians (1e-6 at position 2^28) beside the fp32 steps after it.
      q_out[t][h][:]                      = rotated q[t][h][:]
      K row len[b] - m_b + j of kv-head h = rotated k_new[t][h][:],  t = off[b] + j
      V row                               = v_new[t][h][:]
@@ -85,8 +92,9 @@ LG_API lg_status lg_default_rope_params(lg_rope_params *p, int d);
    q: device [T][H_q][d] dtype; k_new, v_new: device [T][H_kv][d]; each with its own stride from
    token to token in elements (a multiple of 16 bytes, at least the row), so that slices of one
    projection's output pass as they are.  q_out: device [T][H_q][d] dense; it may be q itself when
-   q is dense, and overlaps none of the inputs otherwise.  q and q_out may be null together with H_q = 0 (keys and values only).  pos: device
-   [T].  16-byte alignment throughout (pos 4).  Call after lg_begin_chunk. */
+   q is dense, and overlaps none of the inputs otherwise.  q and q_out may be null together with
+   H_q = 0 (keys and values only).  pos: device [T].  16-byte alignment throughout (pos 4).  Call
+   after lg_begin_chunk. */
 LG_API lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const void *q,
                                 int64_t q_stride, int H_q, const void *k_new, int64_t k_stride,
                                 const void *v_new, int64_t v_stride, const int32_t *pos,
@@ -104,8 +112,9 @@ LG_API size_t lg_chunk_workspace_size(const lg_cache *c, const lg_chunk *ch, int
      out[t][h][:] = sum_i a_i v_i,  a = softmax_i(<q[t][h], k_i> * scale) over the rows seen
    q: device [T][H_q][d] dense, dtype; out: device same shape, dtype, may not overlap q.  Query
    head h reads kv-head h / (H_q/H_kv).  What lies in rows that a query does not see never reaches
-   its result, whatever it holds.  bf16: the weights enter the product with the values in bf16;
-   scores and sums are fp32.  max_len: host bound on every len[b], best a near one, as the division
+   its result, whatever it holds.  bf16: the weights enter the product with the values in bf16
+   (off by 2^-8 of each at most; lg_decode_attend carries them in two terms), scores and sums are
+   fp32.  max_len: host bound on every len[b], best a near one, as the division
    of the work (and so the order of sums) goes by it.  A longer sequence sets LG_ERR_CAPACITY, as
    does an m_b above max_new or len[b], or an off[] outside [0, T]; nothing of that call's output is
    then defined.
@@ -154,6 +163,11 @@ LG_API lg_status lg_count_tokens(const int32_t *tokens, const int32_t *off, int 
      tokens[b] = the lowest token with the largest x;  pmax[b] = exp(x - max) share of it
    A row with nothing left gives token -1 and pmax 0.  The mass of a row with infinite logits is
    shared evenly among those.
+   pmax is of what is left after the penalties, biases and masks: a row with one allowed token has
+   pmax 1.  The confidence that lg_token_detect's streak counts is the model's own; where any of the
+   three changes the logits, it takes a second call on the logits as they came (seen, bias, allowed
+   and logits_out null, other tokens), before this one where this one works in place.  The same call
+   again gives the same bits.
    seen, counts: as lg_count_tokens keeps them, both or neither; penalty: device [batch][4]
    {repetition > 0, presence, frequency, unused}, 16-byte aligned, with seen; bias, allowed
    (device [batch][ceil(V/32)] words) nullable.  tokens: device [batch] int32; pmax: device [batch]

@@ -1,8 +1,8 @@
 // lg_chunk_attend of fp32 caches on the CUDA cores, and the merge of shared items.
 //
 // chunk_attend_kernel's query tile is BM (64 or 128) rows: the g query heads of BM / g consecutive
-// new tokens (row r: token r / g, head r % g), so every key row read serves all of them.  One pass over the tile's key blocks with
-// a running maximum m, normaliser l and sum o per row (log2 units):
+// new tokens (row r: token r / g, head r % g), so every key row read serves all of them.  One pass over
+// the tile's key blocks with a running maximum m, normaliser l and sum o per row (log2 units):
 //   m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,  o = o 2^(m - m') + p V.
 // 256 threads as 16 x 16: thread (ty, tx) computes the scores of rows ty TM .. ty TM + TM - 1 and
 // keys tx + 16 j, and the results of the same rows and elements 4 tx + 64 j, so that a row's
@@ -16,12 +16,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBn = 64;
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 __device__ __forceinline__ void load4(const void *p, int64_t i, float *f) {
   const float4 v = *(const float4 *)((const float *)p + i);
@@ -546,6 +540,7 @@ ChunkGrid chunk_grid(int dtype, int d, int g, int max_new) {
   ChunkGrid r;
   const int64_t rows = (int64_t)max_new * g;
   r.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+  // what the 152 SMs of a GB300 hold at once (on fewer the others follow: no CTA waits for another)
   r.ctas = 152 * (r.rows == 4 ? 2 : 1);
   r.tok = r.rows / g;
   r.bn2 = 6;

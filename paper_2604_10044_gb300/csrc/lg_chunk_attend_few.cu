@@ -73,12 +73,6 @@ __device__ __forceinline__ bool keys_any(int group, bool p) {
   return r != 0;
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-
 template <int N>
 __device__ __forceinline__ void load_cols(uint32_t addr, uint32_t *v) {
   if constexpr (N == 16) {
@@ -276,7 +270,8 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
         if (!ok) break;
         if (j >= 0 && p.hides(p.blk0 + j)) {
           const int i0 = p.blocks.index(p.blk0 + j) * kBn;
-          if (clear_block<C::kTile, kBn>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64)) p.bad = 1;
+          if (clear_block<C::kTile, kBn>(ring + n % ST * C::kTile, i0, p.n, tid - 32 * (W0 + 2), 64))
+            p.bad = 1;
           fence_proxy_async_smem();
           __syncwarp();
         }
@@ -308,8 +303,8 @@ __global__ void __launch_bounds__((FewCfg<D, N>::kThreads), 1)
       for (int q = 0; q < NC; ++q) base[q] = 0.f;
 #pragma unroll
       for (int q = 0; q < NC / 2; ++q) l2[q] = make_float2(0.f, 0.f);
-      // (rows of the tile that are no query, which may hold anything: their scores are below it always,
-      // so that they never ask for the maxima, by which the queries' weights would be rounded otherwise)
+      // (rows of the tile that are no query, which may hold anything: their scores are always below
+      // it, so that they never ask for new maxima, which would round the queries' weights otherwise)
       if (key < NC) bars.m[q0 + key] = q0 + key < used ? -INFINITY : INFINITY;
       const float2 sc = make_float2(a.qscale, a.qscale);
       for (int blk = w.blk0; blk < w.blk1; ++blk, ++c) {

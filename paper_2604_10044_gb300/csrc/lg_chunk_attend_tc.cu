@@ -18,9 +18,9 @@
 // with N = 64 read the queries as often as the keys, 1.5 x the time of N = 128: too slow for 128.)
 //
 // Warps: 0-3 and 4-7 the rows of streams 0 and 1; 8 walks along the work and copies (TMA), 9 and 10
-// issue the products of a stream each, 11 clears what is not a number from the values of blocks in which some row is hidden from some query
-// (0 x NaN would reach the hidden one's sums).  Those values are added again, at the end, for the
-// queries that see them.
+// issue the products of a stream each, 11 clears what is not a number from the values of blocks in
+// which some row is hidden from some query (0 x NaN would reach the hidden one's sums).  Those values
+// are added again, at the end, for the queries that see them.
 #include "lg_chunk_tc.cuh"
 
 namespace lg {
@@ -542,7 +542,7 @@ ChunkGrid chunk_grid_tc(int d, int g, int max_new) {
   const int64_t rows = (int64_t)max_new * g;
   // few rows: the kernel that takes them as the products' N (lg_chunk_attend_few.cu)
   r.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
-  r.ctas = 152;
+  r.ctas = 152;  // one an SM of a GB300 (on fewer SMs the others follow: no CTA waits for another)
   r.tok = r.rows == 256 ? 128 / g * 2 : r.rows / g;
   r.bn2 = r.rows == 256 && d == 64 ? 6 : 7;  // TcCfg<D>::kBn
   return r;

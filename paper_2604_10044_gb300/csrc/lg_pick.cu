@@ -29,12 +29,6 @@ constexpr int kAhead = 4;     // vectors of a thread in flight
 constexpr int kAside = 2048;  // listed tokens of a CTA
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 struct Top {
   float m, s;
   int id;
@@ -125,12 +119,6 @@ __device__ __forceinline__ uint4 pack16(const float *f) {
   }
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-
 // the lanes' triples merged, the same in every lane
 __device__ __forceinline__ Top warp_top(const Top &t) {
   Top r;
@@ -153,7 +141,8 @@ template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) pick_token_kernel(PickArgs a, int csize) {
   constexpr int N = 16 / (int)sizeof(T);
   constexpr uint32_t kAll = (1u << N) - 1;
-  extern __shared__ uint32_t s_bits[];  // [4][slice / 32]: allowed tokens, those of the pass, listed ones, biased ones
+  // [4][slice / 32 + 1]: allowed tokens, those of the pass, listed ones, biased ones
+  extern __shared__ uint32_t s_bits[];
   __shared__ Top s_top[NT / 32];
   __shared__ float s_max[NT / 32];
   __shared__ Top s_ranks[kMaxCluster];
@@ -537,9 +526,10 @@ cudaError_t launch_pick_typed(PickArgs &a, int batch, int c, cudaStream_t s) {
 
 // CTAs a row, of 512 threads (two an SM): the most whose clusters run at once, at most ten, each with
 // 8192 tokens or more (16, and 2048, where rows are so few that every CTA finds an SM of its own), and
-// enough that a slice's bits fit shared memory.  Rows too many for two CTAs each and not for three of 256
-// threads (four an SM) take those, while their bits leave room for two an SM; rows too many for one of
-// 512 threads take one of 256, as long as four CTAs' bits fit an SM.  Measured on a GB300, calls back to back, us by threads x CTAs a row:
+// enough that a slice's bits fit shared memory.  Rows too many for two CTAs each and not for three of
+// 256 threads (four an SM) take those, while their bits leave room for two an SM; rows too many for one
+// of 512 threads take one of 256, as long as four CTAs' bits fit an SM.  Measured on a GB300, calls
+// back to back, us by threads x CTAs a row:
 //   rows of 128257 bf16:   8  512x10  6.8, 512x16  8.2     16  512x8  7.8, 512x16 12.5 (do not fit)
 //                         48  512x5  11.1, 512x6  16.0    152  512x2 16.1, 256x4  23.2
 //                        192  256x3  22.0, 512x1  25.0    256  512x1 25.7, 256x2  26.9
