@@ -44,7 +44,8 @@
  *    max_len, a budget too small for the anchors, a bounded wait that ran out) are written
  *    once to *dev_status (first error wins) and every later kernel on that cache skips its
  *    work while the status is non-zero.  No kernel traps or asserts.
- *  - Shapes: head_dim d in {64, 128}; dtype bf16 or fp32; GQA group g = H_q / H_kv in 1..8.
+ *  - Shapes: head_dim d in {64, 128}; dtype bf16, fp32 or 4 bits (LG_Q4); GQA group g = H_q / H_kv in
+ *    1..8.
  */
 #ifndef LG_H
 #define LG_H
@@ -76,14 +77,29 @@ typedef enum {
   LG_ERR_BUDGET = 7       /* device: a budget leaves no room for the retained set */
 } lg_status;
 
-typedef enum { LG_BF16 = 0, LG_F32 = 1 } lg_dtype;
+/* LG_Q4 (a cache's dtype alone): rows in four bits.  A head of d elements is four groups of d/4; a
+   group holds a scale s and a least value lo, both bf16, and a code c of 0..15 an element, which stands
+   for lo + s c.  A row is d/2 + 16 bytes (80 for d = 128, 48 for d = 64): d/8 little-endian words of
+   eight codes, element 2i of a word in bits 4i and element 2i + 1 in bits 16 + 4i (i < 4), then a word
+   a group, s in its low half and lo in its high one.
+   lg_append and lg_rope_append quantise what they are given (bf16): lo is the group's least element,
+   s = (largest - lo) times the fp32 number 1/15, rounded to bf16 (0 where that is below 2^-126: every element
+   is held as lo), c the integer nearest to (x - lo) / s, ties to even.  So an element is off by half a
+   scale at most, and the largest by 2^-9 of the range more.  A group that holds a NaN or an infinity, or whose range is 2^118 or more,
+   reads back as NaN.  Queries, new rows and results of such a cache are bf16.
+   Its calls: lg_begin_step, lg_append, lg_decode_attend (and _noalloc), lg_state_init, the detect and
+   prune calls, lg_read_device_status, and those of lg_chunk.h and lg_draft.h.  lg_sketch_build is
+   refused (rows near zero have lost their sign; every append writes its sketch from the values as they
+   came), and so are h2o and pos, and with them the comparators' calls. */
+typedef enum { LG_BF16 = 0, LG_F32 = 1, LG_Q4 = 2 } lg_dtype;
 
 /* The KV cache of a batch of sequences (Sec. 3.1).  Row i of sequence b, layer l, kv-head h
    lives at slot seq_off[b] + i of the [L][H_kv][S_total][d] arrays; slots [0, len[b]) are the
    retained set S_t in ascending token order (on the H2O path, in slot order with pos[]
    holding each slot's token position). */
 typedef struct {
-  void *k;               /* device [L][H_kv][S_total][d], dtype; 16-byte aligned          */
+  void *k;               /* device [L][H_kv][S_total][d], dtype; 16-byte aligned (LG_Q4: rows of
+                            d/2 + 16 bytes)                                               */
   void *v;               /* device [L][H_kv][S_total][d], dtype; 16-byte aligned          */
   int32_t dtype;         /* lg_dtype                                                      */
   int32_t L, H_kv, d;    /* layers, kv-heads, head_dim                                    */

@@ -1,7 +1,7 @@
 """Build of liblg.so: every .cu of csrc/ compiled for sm_103a in parallel, then linked.
 
 The library links the CUDA runtime statically and exports only the lg_* C ABI declared in
-include/lg.h and include/lg_chunk.h.
+include/lg.h, include/lg_chunk.h and include/lg_draft.h.
 """
 import os
 import subprocess
@@ -15,7 +15,7 @@ SOURCES = ["lg_attend.cu", "lg_attend_mma.cu", "lg_attend_cluster.cu",
            "lg_attend_cluster_f32.cu", "lg_guard.cu", "lg_token.cu", "lg_api.cu",
            "lg_noalloc.cu", "lg_chunk.cu", "lg_chunk_attend.cu",
            "lg_chunk_attend_tc.cu", "lg_chunk_attend_few.cu", "lg_pick.cu",
-           "lg_chunk_api.cu"]
+           "lg_chunk_api.cu", "lg_q4_rows.cu", "lg_q4_attend.cu", "lg_verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-fvisibility=hidden",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

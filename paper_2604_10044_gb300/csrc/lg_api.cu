@@ -6,6 +6,7 @@
 
 #include "lg.h"
 #include "lg_internal.h"
+#include "lg_q4.cuh"
 
 namespace {
 
@@ -19,7 +20,8 @@ lg_status check_cache(const lg_cache *c) {
   if (!c || !c->k || !c->v || !c->seq_off || !c->cap || !c->len || !c->dev_status)
     return LG_ERR_INVALID_ARG;
   if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->sketch)) return LG_ERR_INVALID_ARG;
-  if (c->dtype != LG_BF16 && c->dtype != LG_F32) return LG_ERR_UNSUPPORTED;
+  if (c->dtype != LG_BF16 && c->dtype != LG_F32 && c->dtype != LG_Q4) return LG_ERR_UNSUPPORTED;
+  if (c->dtype == LG_Q4 && (c->h2o || c->pos)) return LG_ERR_UNSUPPORTED;
   if (c->d != 64 && c->d != 128) return LG_ERR_UNSUPPORTED;
   if (c->L < 1 || c->H_kv < 1 || c->batch < 1 || c->S_total < 1) return LG_ERR_INVALID_ARG;
   if ((c->H_kv * c->d) % 128) return LG_ERR_UNSUPPORTED;  // sketch rows of whole 16-byte chunks
@@ -100,6 +102,31 @@ AttendLayout attend_layout(const lg_cache *c, int H_q, int n_layers, int max_len
   return L;
 }
 
+lg::Q4Grid q4_decode_grid(const lg_cache *c, int H_q, int n_layers, int max_len) {
+  return lg::q4_grid(n_layers, c->batch, c->H_kv, H_q / c->H_kv, c->d, 1, max_len, 0, 0);
+}
+
+// lg_decode_attend over a 4-bit cache
+lg_status q4_decode_attend(const lg_cache *c, int layer0, int n_layers, const void *q, int H_q,
+                           float scale, void *out, float *stats, int suffix_w, int max_len, void *ws,
+                           size_t ws_bytes, cudaStream_t s) {
+  const lg::Q4Grid grid = q4_decode_grid(c, H_q, n_layers, max_len);
+  if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < grid.part_bytes) return LG_ERR_WORKSPACE;
+  if (!lg::q4_grid_fits(grid, n_layers, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
+  lg::Q4AttendArgs a = {};
+  a.q = q;
+  a.out = out;
+  a.stats = stats;
+  a.layer0 = layer0;
+  a.n_layers = n_layers;
+  a.T = c->batch;
+  a.max_new = 1;
+  a.max_len = max_len;
+  a.suffix_w = suffix_w;
+  lg::q4_fill(a, *c, H_q / c->H_kv, scale, grid, ws);
+  return cuda_status(lg::launch_q4_attend(a, c->d, s));
+}
+
 }  // namespace
 
 extern "C" {
@@ -147,6 +174,11 @@ const char *lg_status_string(lg_status s) {
 size_t lg_workspace_size(const lg_cache *c, int H_q, int n_layers, int max_len,
                          int accumulate_h2o) {
   if (check_cache(c) != LG_OK || H_q < 1 || n_layers < 1 || max_len < 1) return 0;
+  if (c->dtype == LG_Q4) {
+    if (H_q % c->H_kv || H_q / c->H_kv > 8 || accumulate_h2o) return 0;
+    const size_t n = q4_decode_grid(c, H_q, n_layers, max_len).part_bytes;
+    return n > 256 ? n : 256;
+  }
   return attend_layout(c, H_q, n_layers, max_len, accumulate_h2o).total;
 }
 
@@ -171,6 +203,8 @@ lg_status lg_append(const lg_cache *c, int layer0, int n_layers, const void *k_n
   if ((st = check_params(p)) != LG_OK) return st;
   if (layer0 < 0 || n_layers < 1 || layer0 + n_layers > c->L) return LG_ERR_INVALID_ARG;
   if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return LG_ERR_INVALID_ARG;
+  if (c->dtype == LG_Q4)
+    return cuda_status(lg::launch_q4_append(*c, layer0, n_layers, k_new, v_new, p->guard_layer, s));
   if (c->pos && !pos_new) return LG_ERR_INVALID_ARG;
   return cuda_status(lg::launch_append(*c, layer0, n_layers, k_new, v_new, pos_new,
                                        p->guard_layer, s));
@@ -183,6 +217,7 @@ lg_status lg_sketch_build(const lg_cache *c, const lg_guard_params *p, int max_l
   if ((st = check_params(p)) != LG_OK) return st;
   if (!c->sketch || p->guard_layer < 0 || p->guard_layer >= c->L || max_len < 0)
     return LG_ERR_INVALID_ARG;
+  if (c->dtype == LG_Q4) return LG_ERR_UNSUPPORTED;  // signs of rows near zero are lost
   return cuda_status(lg::launch_sketch_build(*c, p->guard_layer, max_len, s));
 }
 
@@ -200,6 +235,9 @@ lg_status lg_decode_attend(const lg_cache *c, int layer0, int n_layers, const vo
     return LG_ERR_INVALID_ARG;
   if (suffix_w < 1 || max_len < 1 || !(scale > 0.f) || !isfinite(scale)) return LG_ERR_INVALID_ARG;
   if (accumulate_h2o && !c->h2o) return LG_ERR_INVALID_ARG;
+  if (c->dtype == LG_Q4)
+    return q4_decode_attend(c, layer0, n_layers, q, H_q, scale, out, stats, suffix_w, max_len, ws,
+                            ws_bytes, s);
   const AttendLayout L = attend_layout(c, H_q, n_layers, max_len, accumulate_h2o);
   if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < L.total) return LG_ERR_WORKSPACE;
   lg::AttendArgs a;

@@ -7,6 +7,7 @@
 #include "lg_chunk.h"
 #include "lg_chunk_attend.cuh"
 #include "lg_internal.h"
+#include "lg_q4.cuh"
 
 namespace {
 
@@ -100,6 +101,31 @@ size_t part_bytes(const lg::ChunkGrid &g, int d) {
   return (n + 255) / 256 * 256;
 }
 
+lg_status check_rows(const lg_logits *x) {
+  if (!x || !x->x) return LG_ERR_INVALID_ARG;
+  if (x->dtype != LG_BF16 && x->dtype != LG_F32) return LG_ERR_UNSUPPORTED;
+  if (x->batch < 1 || x->V < 1 || x->stride < x->V) return LG_ERR_INVALID_ARG;
+  if (x->V > 1 << 20) return LG_ERR_UNSUPPORTED;
+  return aligned(x->x, x->dtype == LG_BF16 ? 2 : 4) ? LG_OK : LG_ERR_INVALID_ARG;
+}
+
+// lg_chunk_attend over a 4-bit cache: few query rows of a kv-head read the codes themselves
+bool q4_few(const lg_chunk *ch, int g) { return (int64_t)ch->max_new * g <= lg::kQ4FewRows; }
+
+// bytes of one layer's keys (or values) in bf16
+size_t q4_plane_bytes(const lg_cache *c) {
+  return ((size_t)c->H_kv * c->S_total * c->d * 2 + 255) / 256 * 256;
+}
+
+// for any window: without one an item has the most key blocks
+size_t q4_chunk_bytes(const lg_cache *c, const lg_chunk *ch, int g, int max_len) {
+  if (q4_few(ch, g)) {
+    const size_t n = lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, 0, 0).part_bytes;
+    return n > 256 ? n : 256;
+  }
+  return 2 * q4_plane_bytes(c) + part_bytes(lg::chunk_grid(LG_BF16, c->d, g, ch->max_new), c->d);
+}
+
 }  // namespace
 
 extern "C" {
@@ -143,7 +169,7 @@ lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const
   if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) ||
       !aligned(pos, 4))
     return LG_ERR_INVALID_ARG;
-  const int64_t el = c->dtype == LG_BF16 ? 8 : 4;  // elements of 16 bytes
+  const int64_t el = c->dtype == LG_F32 ? 4 : 8;  // elements of 16 bytes
   if (k_stride % el || v_stride % el || k_stride < (int64_t)c->H_kv * c->d ||
       v_stride < (int64_t)c->H_kv * c->d)
     return LG_ERR_INVALID_ARG;
@@ -160,6 +186,10 @@ lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const
   }
   uint64_t turns[64];
   rope_turns(*rp, turns);
+  if (c->dtype == LG_Q4)
+    return cuda_status(lg::launch_q4_rope_append(
+        *c, *ch, layer, q, q_stride, H_q, k_new, k_stride, v_new, v_stride, pos, *rp, turns, q_out,
+        c->sketch && p->guard_layer == layer, s));
   return cuda_status(lg::launch_rope_append(*c, *ch, layer, q, q_stride, H_q, k_new, k_stride,
                                             v_new, v_stride, pos, *rp, turns, q_out,
                                             c->sketch && p->guard_layer == layer, s));
@@ -167,6 +197,7 @@ lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer, const
 
 size_t lg_chunk_workspace_size(const lg_cache *c, const lg_chunk *ch, int H_q, int max_len) {
   if (attend_shape(c, ch, H_q, max_len) != LG_OK) return 0;
+  if (c->dtype == LG_Q4) return q4_chunk_bytes(c, ch, H_q / c->H_kv, max_len);
   return part_bytes(lg::chunk_grid(c->dtype, c->d, H_q / c->H_kv, ch->max_new), c->d);
 }
 
@@ -179,12 +210,54 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
   if (!(scale > 0.f) || !isfinite(scale)) return LG_ERR_INVALID_ARG;
   if (c->dtype == LG_BF16 && (int64_t)c->L * c->H_kv * c->S_total >= ((int64_t)1 << 31))
     return LG_ERR_UNSUPPORTED;
+  if (c->dtype == LG_Q4 && !q4_few(ch, H_q / c->H_kv) &&
+      (int64_t)c->H_kv * c->S_total >= ((int64_t)1 << 31))
+    return LG_ERR_UNSUPPORTED;
   if (ch->T == 0 || ch->max_new == 0) return LG_OK;
   if (!q || !out || q == out || !aligned(q, 16) || !aligned(out, 16)) return LG_ERR_INVALID_ARG;
   const int g = H_q / c->H_kv;
+  const uint64_t bytes = (uint64_t)ch->T * H_q * c->d * (c->dtype == LG_F32 ? 4 : 2);
+  if (c->dtype == LG_Q4) {
+    if (!ws || !aligned(ws, 256) || ws_bytes < q4_chunk_bytes(c, ch, g, max_len))
+      return LG_ERR_WORKSPACE;
+    if (overlap(q, bytes, out, bytes)) return LG_ERR_INVALID_ARG;
+    if (q4_few(ch, g)) {
+      const lg::Q4Grid grid =
+          lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, window, n_sink);
+      if (!lg::q4_grid_fits(grid, 1, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
+      lg::Q4AttendArgs a = {};
+      a.q = q;
+      a.out = out;
+      a.off = ch->off;
+      a.layer0 = layer;
+      a.n_layers = 1;
+      a.T = ch->T;
+      a.max_new = ch->max_new;
+      a.max_len = max_len;
+      a.window = window;
+      a.sink = n_sink;
+      lg::q4_fill(a, *c, g, scale, grid, ws);
+      return cuda_status(lg::launch_q4_attend(a, c->d, s));
+    }
+  }
+  // many query rows over four bits: a 16-bit layer of the rows' values, then the kernels of such
+  lg_cache wide = *c;
+  if (c->dtype == LG_Q4) {
+    const size_t plane = q4_plane_bytes(c);
+    wide.k = ws;
+    wide.v = (char *)ws + plane;
+    wide.dtype = LG_BF16;
+    wide.L = 1;
+    const cudaError_t e = lg::launch_q4_expand(*c, *ch, layer, window, n_sink, max_len, wide.k,
+                                               wide.v, s);
+    if (e != cudaSuccess) return LG_ERR_CUDA;
+    ws = (char *)ws + 2 * plane;
+    ws_bytes -= 2 * plane;
+    layer = 0;
+    c = &wide;
+  }
   const lg::ChunkGrid grid = lg::chunk_grid(c->dtype, c->d, g, ch->max_new);
   if (!ws || !aligned(ws, 256) || ws_bytes < part_bytes(grid, c->d)) return LG_ERR_WORKSPACE;
-  const uint64_t bytes = (uint64_t)ch->T * H_q * c->d * (c->dtype == LG_BF16 ? 2 : 4);
   if (overlap(q, bytes, out, bytes)) return LG_ERR_INVALID_ARG;
   lg::ChunkAttendArgs a = {};
   a.K = c->k;
@@ -212,6 +285,67 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
   a.shape.window = window;
   a.shape.sink = n_sink;
   return cuda_status(lg::launch_chunk_attend(a, c->dtype, c->d, grid.ctas, s));
+}
+
+lg_status lg_end_chunk(const lg_cache *c, const lg_chunk *ch, const int32_t *accepted,
+                       cudaStream_t s) {
+  const lg_status st = check_chunk(c, ch);
+  if (st != LG_OK) return st;
+  if (!accepted || !aligned(accepted, 4)) return LG_ERR_INVALID_ARG;
+  return cuda_status(lg::launch_end_chunk(*c, *ch, accepted, s));
+}
+
+lg_status lg_read_rows(const lg_cache *c, const lg_chunk *ch, int layer, void *k_out, void *v_out,
+                       cudaStream_t s) {
+  const lg_status st = check_chunk(c, ch);
+  if (st != LG_OK) return st;
+  if (c->dtype != LG_Q4) return LG_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= c->L) return LG_ERR_INVALID_ARG;
+  if (ch->T == 0) return LG_OK;
+  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return LG_ERR_INVALID_ARG;
+  const uint64_t bytes = (uint64_t)ch->T * c->H_kv * c->d * 2;
+  if (overlap(k_out, bytes, v_out, bytes)) return LG_ERR_INVALID_ARG;
+  return cuda_status(lg::launch_q4_read(*c, *ch, layer, k_out, v_out, s));
+}
+
+size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch) {
+  if (check_rows(x) != LG_OK || !ch || ch->T < 0 || ch->T > 65535) return 0;
+  const size_t n = lg::verify_ws_bytes(*x, ch->T);
+  return n > 16 ? n : 16;
+}
+
+lg_status lg_verify_draft(const lg_logits *x, const lg_chunk *ch, int batch, const int32_t *tokens,
+                          const lg_logits *draft, const float *temperature, const float *u,
+                          const float *r, int32_t *picked, int32_t *accepted, void *ws,
+                          size_t ws_bytes, int32_t *dev_status, cudaStream_t s) {
+  lg_status st = check_rows(x);
+  if (st != LG_OK) return st;
+  if (draft && (st = check_rows(draft)) != LG_OK) return st;
+  if (!ch || !ch->off || !aligned(ch->off, 4) || ch->T < 0 || ch->max_new < 0 || batch < 1)
+    return LG_ERR_INVALID_ARG;
+  if (ch->T > 65535 || batch > 1 << 20) return LG_ERR_UNSUPPORTED;
+  if (x->batch < ch->T || (draft && (draft->batch < ch->T || draft->V != x->V)))
+    return LG_ERR_INVALID_ARG;
+  if (!tokens || !u || !r || !picked || !accepted || !aligned(tokens, 4) || !aligned(u, 4) ||
+      !aligned(r, 4) || !aligned(temperature, 4) || !aligned(picked, 4) || !aligned(accepted, 4) ||
+      !aligned(dev_status, 4))
+    return LG_ERR_INVALID_ARG;
+  if (ch->T == 0) return LG_OK;
+  if (!ws || !aligned(ws, 16) || ws_bytes < lg::verify_ws_bytes(*x, ch->T)) return LG_ERR_WORKSPACE;
+  // results over anything that is read, or over one another
+  const uint64_t n = (uint64_t)ch->T * 4, nb = (uint64_t)batch * 4;
+  auto rows = [&](const lg_logits *l) {
+    return ((uint64_t)(ch->T - 1) * l->stride + l->V) * (l->dtype == LG_BF16 ? 2 : 4);
+  };
+  auto taken = [&](const void *p, uint64_t bytes) {
+    return p && (overlap(picked, n, p, bytes) || overlap(accepted, nb, p, bytes));
+  };
+  if (overlap(picked, n, accepted, nb) || taken(tokens, n) || taken(u, n) || taken(r, nb) ||
+      taken(temperature, nb) || taken(ch->off, nb + 4) || taken(x->x, rows(x)) ||
+      (draft && taken(draft->x, rows(draft))) || taken(ws, lg::verify_ws_bytes(*x, ch->T)))
+    return LG_ERR_INVALID_ARG;
+  return cuda_status(lg::launch_verify(*x, *ch, batch, tokens, draft, temperature, u, r, picked,
+                                       accepted, ws, dev_status, s));
 }
 
 lg_status lg_count_tokens(const int32_t *tokens, const int32_t *off, int T, int batch, int V,

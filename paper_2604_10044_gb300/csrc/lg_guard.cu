@@ -780,7 +780,7 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(lg_cache c,
   __shared__ int s_seq[kCompactSeqList], s_cnt[kCompactSeqList];
   __shared__ int s_wtot[kCompactThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row_bytes_kv = c.d * (c.dtype == LG_BF16 ? 2 : 4);
+  const int row_bytes_kv = c.dtype == LG_Q4 ? c.d / 2 + 16 : c.d * (c.dtype == LG_BF16 ? 2 : 4);
   const int nwords = c.H_kv * c.d / 32;
   const int n_kv = 2 * c.L * c.H_kv;
   const int per_seq = n_kv + 1;

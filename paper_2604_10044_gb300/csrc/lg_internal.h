@@ -5,6 +5,7 @@
 
 #include "lg.h"
 #include "lg_chunk.h"
+#include "lg_draft.h"
 
 namespace lg {
 
@@ -103,6 +104,29 @@ cudaError_t launch_rope_append(const lg_cache &c, const lg_chunk &ch, int layer,
                                const void *v, int64_t v_stride, const int32_t *pos,
                                const lg_rope_params &rp, const uint64_t *turns, void *q_out,
                                bool guard, cudaStream_t s);
+
+// rows of a 4-bit cache (lg_q4_rows.cu): new ones, one or a chunk a sequence, and read back; expand:
+// layer's rows that some query of the chunk sees, at the same slots of one bf16 layer
+cudaError_t launch_q4_append(const lg_cache &c, int layer0, int n_layers, const void *k_new,
+                             const void *v_new, int guard_layer, cudaStream_t s);
+cudaError_t launch_q4_rope_append(const lg_cache &c, const lg_chunk &ch, int layer, const void *q,
+                                  int64_t q_stride, int H_q, const void *k, int64_t k_stride,
+                                  const void *v, int64_t v_stride, const int32_t *pos,
+                                  const lg_rope_params &rp, const uint64_t *turns, void *q_out,
+                                  bool guard, cudaStream_t s);
+cudaError_t launch_q4_read(const lg_cache &c, const lg_chunk &ch, int layer, void *k_out,
+                           void *v_out, cudaStream_t s);
+cudaError_t launch_q4_expand(const lg_cache &c, const lg_chunk &ch, int layer, int window, int sink,
+                             int max_len, void *K, void *V, cudaStream_t s);
+
+// drafted tokens (lg_verify.cu)
+size_t verify_ws_bytes(const lg_logits &x, int T);
+cudaError_t launch_verify(const lg_logits &x, const lg_chunk &ch, int batch, const int32_t *tokens,
+                          const lg_logits *draft, const float *temp, const float *u, const float *r,
+                          int32_t *picked, int32_t *accepted, void *ws, int32_t *status,
+                          cudaStream_t s);
+cudaError_t launch_end_chunk(const lg_cache &c, const lg_chunk &ch, const int32_t *accepted,
+                             cudaStream_t s);
 
 // lg_chunk_attend (lg_chunk_attend.cu): the grid and tiles of a call, and the call
 struct ChunkGrid {

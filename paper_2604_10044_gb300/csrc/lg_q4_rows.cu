@@ -1,0 +1,307 @@
+// Rows of a 4-bit cache: new keys and values rotated, quantised and stored, and rows read back as the
+// bf16 values that they stand for.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "lg_q4.cuh"
+#include "lg_rope.cuh"
+
+namespace lg {
+namespace {
+
+// ---------------------------------------------------------------- new rows
+//
+// A thread holds 16 bytes (8 elements) of a token's heads: one word of codes.  It takes its cosines
+// and sines once and walks over heads: queries (rotated, stored as they are), keys (rotated, rounded
+// to bf16 as a 16-bit cache would hold them, quantised), values.  The other elements of its pairs come
+// by shuffles (so queries may be rotated in place), as do the least and largest element of a group, over
+// the 4 (d = 128) or 2 lanes that hold it.
+
+struct Q4AppendArgs {
+  const __nv_bfloat16 *q, *k, *v;
+  __nv_bfloat16 *q_out;
+  const int32_t *pos;
+  int64_t q_stride, k_stride, v_stride;  // elements from token to token
+  int layer, H_q, rot;                   // rot 0: keys come as they are to be held
+  int layout;
+  float mscale;
+  int guard;     // the layer whose V rows are sketched, -1: none
+  int groups;    // threads that share a token's heads: every groups-th head each
+  int tok;       // tokens a CTA
+  int T;
+};
+
+constexpr int kQ4Threads = 256;
+constexpr int kQ4Tokens = 64;  // tokens a CTA at most
+
+// ONE: token t is the one new row of sequence t, and blockIdx.y the layer
+template <int D, bool ONE>
+__global__ void __launch_bounds__(kQ4Threads)
+    q4_append_kernel(lg_cache c, lg_chunk ch, Q4AppendArgs a, const __grid_constant__ RopeTable tab) {
+  constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
+  __shared__ int64_t s_slot[kQ4Tokens];
+  // no early trigger: the loop-onset test reads sketches before its own wait
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (cta_status_bad(c.dev_status)) return;
+  const int t0 = blockIdx.x * a.tok;
+  const int layer = a.layer + (ONE ? (int)blockIdx.y : 0);
+  if constexpr (ONE) {
+    for (int i = threadIdx.x; i < a.tok; i += kQ4Threads) {
+      const int b = t0 + i;
+      int64_t slot = -1;
+      if (b < c.batch) {
+        const int n = c.len[b];
+        if (n > 0)
+          slot = c.seq_off[b] + n - 1;
+        else
+          set_status(c.dev_status, LG_ERR_CAPACITY);
+      }
+      s_slot[i] = slot;
+    }
+  } else {
+    token_slots(c, ch, t0, a.tok, s_slot);
+  }
+  __syncthreads();
+  const int pc = threadIdx.x % kLanes;
+  const int unit = threadIdx.x / kLanes, i = unit / a.groups, grp = unit % a.groups;
+  const int t = t0 + i;
+  const int64_t slot = i < a.tok && t < a.T ? s_slot[i] : -1;
+  const bool live = slot >= 0;
+  const bool turned = 8 * pc < a.rot, half_lay = a.layout == LG_ROPE_HALF;
+  const int hp = a.rot / 16;  // 16-byte pieces of half of the rotated elements
+  const int other = (threadIdx.x & 31) - pc + (turned && half_lay ? (pc < hp ? pc + hp : pc - hp) : pc);
+  float co[8], si[8];  // of the element's pair; si with the sign of its product with the other element
+  if (live && turned) {
+    const uint64_t p = (uint64_t)(int64_t)a.pos[t];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int pair = half_lay ? (pc < hp ? pc : pc - hp) * 8 + e : pc * 4 + e / 2;
+      if (half_lay || e % 2 == 0) {
+        turn_cos_sin(p * tab.turn[pair], co[e], si[e]);
+        co[e] *= a.mscale;
+        si[e] *= half_lay && pc >= hp ? a.mscale : -a.mscale;
+      } else {
+        co[e] = co[e - 1];
+        si[e] = -si[e - 1];
+      }
+    }
+  }
+  const int64_t layer_row = (int64_t)layer * c.H_kv * c.S_total;
+  const int64_t in = ONE ? (int64_t)blockIdx.y * c.batch + t : t;  // token row of the inputs
+  const int h1 = a.H_q + c.H_kv, h2 = h1 + c.H_kv;
+  // every lane of a warp makes the same number of turns, as the groups' shuffles need them all
+  const int turns = (h2 + a.groups - 1) / a.groups;
+  for (int n = 0; n < turns; ++n) {
+    const int h = grp + n * a.groups;
+    const bool mine = live && h < h2;
+    const bool isq = h < a.H_q, isk = !isq && h < h1;
+    float x[8];
+    uint4 raw = make_uint4(0, 0, 0, 0), far;
+    if (mine) {
+      const __nv_bfloat16 *src = isq   ? a.q + in * a.q_stride + (int64_t)h * D
+                                 : isk ? a.k + in * a.k_stride + (int64_t)(h - a.H_q) * D
+                                       : a.v + in * a.v_stride + (int64_t)(h - h1) * D;
+      raw = *(const uint4 *)(src + 8 * pc);
+    }
+    if (half_lay && a.rot) {  // the other elements of its pairs
+      far.x = __shfl_sync(0xffffffffu, raw.x, other);
+      far.y = __shfl_sync(0xffffffffu, raw.y, other);
+      far.z = __shfl_sync(0xffffffffu, raw.z, other);
+      far.w = __shfl_sync(0xffffffffu, raw.w, other);
+    } else {
+      far = raw;
+    }
+    if (mine && (isq || isk)) {
+      if (turned) {
+        float2 f[4], g[4];
+        Elem<__nv_bfloat16>::unpack(raw, f);
+        Elem<__nv_bfloat16>::unpack(far, g);
+        uint32_t r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float gx = half_lay ? g[e].x : g[e].y, gy = half_lay ? g[e].y : g[e].x;
+          const __nv_bfloat162 y =
+              __floats2bfloat162_rn(__fmaf_rn(f[e].x, co[2 * e], gx * si[2 * e]),
+                                    __fmaf_rn(f[e].y, co[2 * e + 1], gy * si[2 * e + 1]));
+          r[e] = *(const uint32_t *)&y;
+        }
+        raw = make_uint4(r[0], r[1], r[2], r[3]);
+      }
+      if (isq) *(uint4 *)(a.q_out + ((int64_t)t * a.H_q + h) * D + 8 * pc) = raw;
+    }
+    if (__all_sync(0xffffffffu, !mine || isq)) continue;
+    Elem<__nv_bfloat16>::unpack(raw, (float2 *)x);
+    uint32_t par;
+    const uint32_t word = q4_encode<kGroup>(x, par);
+    if (!mine || isq) continue;
+    const int kvh = isk ? h - a.H_q : h - h1;
+    uint8_t *row = (uint8_t *)(isk ? c.k : c.v) +
+                   (layer_row + kvh * c.S_total + slot) * (int64_t)kRow;
+    ((uint32_t *)row)[pc] = word;
+    if (pc % kGroup == 0) ((uint32_t *)row)[kLanes + pc / kGroup] = par;
+    if (!isk && layer == a.guard)  // signs of the values as they came
+      ((uint8_t *)c.sketch)[slot * (c.H_kv * D / 8) + kvh * kLanes + pc] =
+          (uint8_t)Elem<__nv_bfloat16>::signs(raw);
+  }
+}
+
+template <int D>
+cudaError_t launch_append_d(const lg_cache &c, const lg_chunk *ch, Q4AppendArgs &a, int n_layers,
+                            const RopeTable &tab, cudaStream_t s) {
+  constexpr int kLanes = D / 8;
+  const int heads = a.H_q + 2 * c.H_kv;
+  // as many heads a thread, for its cosines and sines to serve, as leave the GPU four CTAs an SM
+  const int64_t full = (int64_t)4 * 152 * kQ4Threads;
+  a.groups = 1;
+  while (a.groups * 2 <= kQ4Threads / kLanes && a.groups < heads &&
+         (int64_t)a.T * n_layers * a.groups * kLanes < full)
+    a.groups *= 2;
+  a.tok = kQ4Threads / kLanes / a.groups;
+  const dim3 grid((a.T + a.tok - 1) / a.tok, n_layers);
+  if (ch)
+    LG_TRY(launch_pdl(q4_append_kernel<D, false>, grid, kQ4Threads, 0, s, c, *ch, a, tab));
+  else
+    LG_TRY(launch_pdl(q4_append_kernel<D, true>, grid, kQ4Threads, 0, s, c, lg_chunk{}, a, tab));
+  return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------- rows read back
+
+struct Q4ReadArgs {
+  int layer;
+  __nv_bfloat16 *k_out, *v_out;  // [T][H_kv][d]
+  int tok;
+};
+
+// the chunk's rows as values: a thread a word, bound by its stores
+template <int D>
+__global__ void __launch_bounds__(kQ4Threads)
+    q4_read_kernel(lg_cache c, lg_chunk ch, Q4ReadArgs a) {
+  constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
+  __shared__ int64_t s_slot[kQ4Tokens];
+  pdl_enter();
+  if (cta_status_bad(c.dev_status)) return;
+  const int t0 = blockIdx.x * a.tok;
+  token_slots(c, ch, t0, a.tok, s_slot);
+  __syncthreads();
+  const int units = c.H_kv * kLanes;
+  for (int u = threadIdx.x; u < a.tok * units; u += kQ4Threads) {
+    const int i = u / units, x = u - i * units, h = x / kLanes, pc = x % kLanes;
+    const int64_t slot = s_slot[i];
+    if (slot < 0) continue;
+    const int64_t at =
+        (((int64_t)a.layer * c.H_kv + h) * c.S_total + slot) * kRow;
+    const uint32_t *k = (const uint32_t *)((const uint8_t *)c.k + at);
+    const uint32_t *v = (const uint32_t *)((const uint8_t *)c.v + at);
+    const int64_t to = ((int64_t)(t0 + i) * c.H_kv + h) * D + 8 * pc;
+    const uint32_t kw = k[pc], kp = k[kLanes + pc / kGroup];
+    const uint32_t vw = v[pc], vp = v[kLanes + pc / kGroup];
+    *(uint4 *)(a.k_out + to) = q4_values(kw, kp);
+    *(uint4 *)(a.v_out + to) = q4_values(vw, vp);
+  }
+}
+
+// A layer's rows as values at the same slots of two 16-bit caches of one layer, for the kernels of
+// many query rows: what some query of the chunk sees.  blockIdx = (rows, kv-head, sequence).
+constexpr int kExpandRows = 64;
+
+template <int D>
+__global__ void __launch_bounds__(kQ4Threads)
+    q4_expand_kernel(lg_cache c, lg_chunk ch, int layer, int window, int sink, __nv_bfloat16 *K,
+                     __nv_bfloat16 *V) {
+  constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
+  pdl_enter();
+  if (cta_status_bad(c.dev_status)) return;
+  const int h = blockIdx.y;
+  for (int b = blockIdx.z; b < c.batch; b += gridDim.z) {
+    const int n = c.len[b], m = ch.off[b + 1] - ch.off[b];
+    if (m <= 0 || n > c.cap[b]) continue;
+    const int64_t lo = window ? (int64_t)n - m + 1 - window : 0;  // rows from here on are seen
+    for (int64_t r0 = (int64_t)blockIdx.x * kExpandRows; r0 < n;
+         r0 += (int64_t)gridDim.x * kExpandRows) {
+      if (r0 + kExpandRows <= lo && r0 >= sink) continue;
+      const int64_t src = ((int64_t)layer * c.H_kv + h) * c.S_total + c.seq_off[b] + r0;
+      const int64_t dst = h * c.S_total + c.seq_off[b] + r0;
+      const int rows = n - r0 < kExpandRows ? (int)(n - r0) : kExpandRows;
+#pragma unroll 4
+      for (int u = threadIdx.x; u < rows * kLanes; u += kQ4Threads) {
+        const int i = u / kLanes, pc = u % kLanes;
+        const uint32_t *k = (const uint32_t *)((const uint8_t *)c.k + (src + i) * kRow);
+        const uint32_t *v = (const uint32_t *)((const uint8_t *)c.v + (src + i) * kRow);
+        const uint32_t kw = k[pc], kp = k[kLanes + pc / kGroup];
+        const uint32_t vw = v[pc], vp = v[kLanes + pc / kGroup];
+        *(uint4 *)(K + (dst + i) * D + 8 * pc) = q4_values(kw, kp);
+        *(uint4 *)(V + (dst + i) * D + 8 * pc) = q4_values(vw, vp);
+      }
+    }
+  }
+}
+
+template <int D>
+cudaError_t launch_read_d(const lg_cache &c, const lg_chunk &ch, Q4ReadArgs &a, cudaStream_t s) {
+  const int units = c.H_kv * (D / 8);
+  a.tok = 2 * kQ4Threads / units;
+  a.tok = a.tok < 1 ? 1 : a.tok > kQ4Tokens ? kQ4Tokens : a.tok;
+  LG_TRY(launch_pdl(q4_read_kernel<D>, (ch.T + a.tok - 1) / a.tok, kQ4Threads, 0, s, c, ch, a));
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_q4_append(const lg_cache &c, int layer0, int n_layers, const void *k_new,
+                             const void *v_new, int guard_layer, cudaStream_t s) {
+  Q4AppendArgs a = {};
+  a.k = (const __nv_bfloat16 *)k_new;
+  a.v = (const __nv_bfloat16 *)v_new;
+  a.k_stride = a.v_stride = (int64_t)c.H_kv * c.d;
+  a.layer = layer0;
+  a.guard = c.sketch ? guard_layer : -1;
+  a.T = c.batch;
+  const RopeTable tab = {};
+  return c.d == 128 ? launch_append_d<128>(c, nullptr, a, n_layers, tab, s)
+                    : launch_append_d<64>(c, nullptr, a, n_layers, tab, s);
+}
+
+cudaError_t launch_q4_rope_append(const lg_cache &c, const lg_chunk &ch, int layer, const void *q,
+                                  int64_t q_stride, int H_q, const void *k, int64_t k_stride,
+                                  const void *v, int64_t v_stride, const int32_t *pos,
+                                  const lg_rope_params &rp, const uint64_t *turns, void *q_out,
+                                  bool guard, cudaStream_t s) {
+  Q4AppendArgs a = {};
+  a.q = (const __nv_bfloat16 *)q;
+  a.k = (const __nv_bfloat16 *)k;
+  a.v = (const __nv_bfloat16 *)v;
+  a.q_out = (__nv_bfloat16 *)q_out;
+  a.pos = pos;
+  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.layer = layer, a.H_q = H_q, a.rot = rp.rot, a.layout = rp.layout;
+  a.mscale = (float)rp.mscale;
+  a.guard = guard ? layer : -1;
+  a.T = ch.T;
+  RopeTable tab = {};
+  for (int i = 0; i < rp.rot / 2; ++i) tab.turn[i] = turns[i];
+  return c.d == 128 ? launch_append_d<128>(c, &ch, a, 1, tab, s)
+                    : launch_append_d<64>(c, &ch, a, 1, tab, s);
+}
+
+cudaError_t launch_q4_read(const lg_cache &c, const lg_chunk &ch, int layer, void *k_out,
+                           void *v_out, cudaStream_t s) {
+  Q4ReadArgs a = {layer, (__nv_bfloat16 *)k_out, (__nv_bfloat16 *)v_out, 0};
+  return c.d == 128 ? launch_read_d<128>(c, ch, a, s) : launch_read_d<64>(c, ch, a, s);
+}
+
+cudaError_t launch_q4_expand(const lg_cache &c, const lg_chunk &ch, int layer, int window, int sink,
+                             int max_len, void *K, void *V, cudaStream_t s) {
+  int gx = (max_len + kExpandRows - 1) / kExpandRows;
+  if (gx > 4096) gx = 4096;
+  const dim3 grid(gx, c.H_kv, c.batch < 65535 ? c.batch : 65535);
+  __nv_bfloat16 *k = (__nv_bfloat16 *)K, *v = (__nv_bfloat16 *)V;
+  if (c.d == 128)
+    LG_TRY(launch_pdl(q4_expand_kernel<128>, grid, kQ4Threads, 0, s, c, ch, layer, window, sink, k, v));
+  else
+    LG_TRY(launch_pdl(q4_expand_kernel<64>, grid, kQ4Threads, 0, s, c, ch, layer, window, sink, k, v));
+  return cudaGetLastError();
+}
+
+}  // namespace lg

@@ -1,0 +1,437 @@
+// Drafted tokens against the target's probabilities, and the rows of those that fall.
+//
+// lg_verify_draft is two kernels.  The first reads every row of logits once: a CTA a slice of a row,
+// kept in registers between its maximum and its sum of exponentials.  The second, a cluster a
+// sequence, joins the slices, decides which drafts stand, and looks the random number up in the
+// distribution of the one row that the next token comes from.
+//
+// Which token a number falls on is exact only as far as the sums are: a bound between two tokens that
+// moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's bounds
+// on the way.  So weights go into the sums as integers in units of 2^-62 (of a mass of one), which add
+// up in any order and division to the same; the quotient by a temperature keeps a second term; and
+// what is formed once a row (the joining of slices, the test of a draft) is in 64 bits.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "lg_common.cuh"
+#include "lg_internal.h"
+#include "lg_rope.cuh"
+
+namespace lg {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kRowThreads = 256;
+constexpr int kRowVecs = 4;  // 16-byte vectors a thread
+
+__host__ __device__ constexpr int slice_elems(int es) { return kRowThreads * kRowVecs * 16 / es; }
+// a row that starts inside a vector reaches one vector further
+__host__ __device__ inline int row_slices(int V, int es) {
+  return (V + 16 / es - 1 + slice_elems(es) - 1) / slice_elems(es);
+}
+
+struct RowPart {     // of a slice of a row
+  float m;           // largest logit, -infinity where none is left
+  int32_t at;        // its lowest place
+  uint64_t z;        // sum of exp((x - m) / temperature) in 2^-40
+};
+
+// log2(e) / temperature in two terms; a temperature of zero (or nothing above it) takes the top token
+struct Heat {
+  float hi, lo;
+  bool greedy;
+};
+
+__device__ __forceinline__ float clamp_temperature(float t) {
+  return t > 0x1p-100f ? fminf(t, 0x1p100f) : 0.f;
+}
+
+__device__ __forceinline__ Heat heat_of(float t) {
+  Heat h{0.f, 0.f, !(t > 0.f)};
+  if (h.greedy) return h;
+  const double e = 1.4426950408889634;
+  const float e_hi = (float)e, e_lo = (float)(e - (double)e_hi);
+  h.hi = __fdiv_rn(e_hi, t);
+  h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t);
+  return h;
+}
+
+// exp((x - m) / temperature), within some 2^-22 and without a drift over the range; the maximum
+// itself is 1 also where it is infinite
+__device__ __forceinline__ float weight(float x, float m, const Heat &h) {
+  const float d = x == m ? 0.f : x - m;
+  const float y = d * h.hi;
+  const float rest = __fmaf_rn(d, h.hi, -y) + d * h.lo;
+  const float e = exp2_fast(y);
+  return y > -126.f ? __fmaf_rn(e, rest * 0.6931471805599453f, e) : 0.f;
+}
+
+template <typename T>
+__device__ __forceinline__ float logit(const void *p, int64_t i) {
+  const float x = Elem<T>::load(p, i);
+  return x == x ? x : -INFINITY;  // a NaN counts as masked
+}
+
+struct VerifyArgs {
+  lg_logits x, draft;
+  int has_draft, batch, T, max_new, slices;
+  const int32_t *off, *tokens;
+  const float *temp, *u, *r;
+  int32_t *picked, *accepted, *status;
+  RowPart *part;  // [T][slices]
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) {
+  constexpr int kVec = 16 / (int)sizeof(T), kN = kRowVecs * kVec;
+  __shared__ float s_m[kRowThreads / 32];
+  __shared__ int s_at[kRowThreads / 32];
+  __shared__ uint64_t s_z[kRowThreads / 32];
+  __shared__ float s_t;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_enter();
+  if (cta_status_bad(a.status)) return;
+  const int row = blockIdx.y, V = a.x.V;
+  if (warp == 0) {
+    const int b = seq_of(a.off, a.batch, row, lane);
+    if (lane == 0) s_t = b < 0 ? -1.f : clamp_temperature(a.temp ? a.temp[b] : 1.f);
+  }
+  const T *x = (const T *)a.x.x + row * a.x.stride;
+  const int head = (int)(((uintptr_t)x & 15) / sizeof(T));  // elements of the first vector before the row
+  float v[kN];
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kRowVecs; ++k) {
+    const int i0 = ((blockIdx.x * kRowVecs + k) * kRowThreads + tid) * kVec - head;
+    if (i0 >= 0 && i0 + kVec <= V) {
+      Elem<T>::unpack(*(const uint4 *)(x + i0), (float2 *)(v + k * kVec));
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        v[k * kVec + e] = i0 + e >= 0 && i0 + e < V ? Elem<T>::load(x, i0 + e) : -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kN; ++e) {
+    v[e] = v[e] == v[e] ? v[e] : -INFINITY;
+    m = fmaxf(m, v[e]);
+  }
+  const float wm = warp_max(m);
+  if (lane == 0) s_m[warp] = wm;
+  __syncthreads();
+  const float t = s_t;
+  if (t < 0.f) return;  // a row of no sequence
+#pragma unroll
+  for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, s_m[w]);
+  const Heat h = heat_of(t);
+  float sum = 0.f;
+  int at = 0x7fffffff;
+#pragma unroll
+  for (int e = 0; e < kN; ++e) {
+    if (!h.greedy) sum += weight(v[e], m, h);
+    if (v[e] == m) {
+      const int i = ((blockIdx.x * kRowVecs + e / kVec) * kRowThreads + tid) * kVec - head + e % kVec;
+      at = min(at, i);
+    }
+  }
+  uint64_t z = m == -INFINITY ? 0 : __float2ull_rn(sum * 0x1p40f);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  at = __reduce_min_sync(0xffffffffu, at);
+  if (lane == 0) {
+    s_at[warp] = at;
+    s_z[warp] = z;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kRowThreads / 32; ++w) {
+      at = min(at, s_at[w]);
+      z += s_z[w];
+    }
+    a.part[(int64_t)row * a.slices + blockIdx.x] = RowPart{m, at, z};
+  }
+}
+
+// ---------------------------------------------------------------- the decision and the next token
+
+constexpr int kPickThreads = 512;
+constexpr int kPickWarps = kPickThreads / 32;
+constexpr int kSeg = 16;             // elements a lane and segment
+constexpr int kSegElems = 32 * kSeg;
+constexpr float kUnit = 0x1p62f;     // a mass of one
+
+struct Row {
+  float m;    // largest logit
+  int at;     // its lowest place
+  double z;   // sum of exp((x - m) / temperature); 0: nothing is left
+};
+
+// a row's slices joined; every lane of a warp calls it
+__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, float t, int lane) {
+  const RowPart *p = a.part + row * a.slices;
+  Row r{-INFINITY, 0x7fffffff, 0.0};
+  for (int i = lane; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
+  r.m = warp_max(r.m);
+  if (r.m == -INFINITY) return r;
+  for (int i = lane; i < a.slices; i += 32) {
+    const RowPart s = p[i];
+    if (s.m == r.m) r.at = min(r.at, s.at);
+    if (t > 0.f && s.z) {
+      const double d = s.m == r.m ? 0.0 : ((double)s.m - (double)r.m) / (double)t;
+      r.z += (double)s.z * 0x1p-40 * (d == 0.0 ? 1.0 : exp(d));
+    }
+  }
+  r.at = __reduce_min_sync(0xffffffffu, r.at);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
+  if (!(t > 0.f)) r.z = 1.0;
+  return r;
+}
+
+// The draft's probability of a token: what is not above zero (a NaN too) counts as zero.
+template <typename Q>
+__device__ __forceinline__ float draft_at(const VerifyArgs &a, int64_t row, int i) {
+  const float q = Elem<Q>::load((const Q *)a.draft.x + row * a.draft.stride, i);
+  return q > 0.f ? q : 0.f;
+}
+
+template <typename T, typename Q>
+__global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a) {
+  cg::cluster_group cl = cg::this_cluster();
+  const int n_cta = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int b = blockIdx.x / n_cta;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  __shared__ uint64_t s_total;                // of this CTA's part of the vocabulary
+  __shared__ uint64_t s_warp[kPickWarps];
+  __shared__ int s_first, s_bad;
+  __shared__ Row s_row;
+  pdl_enter();
+  // one decision for the cluster (its CTAs meet at barriers): the first CTA's
+  if (rank == 0 && tid == 0) s_bad = status_bad(a.status);
+  const int o0 = a.off[b], o1 = a.off[b + 1], m = o1 - o0, V = a.x.V;
+  cl.sync();
+  const bool wrong = o0 < 0 || m < 0 || m > a.max_new || o1 > a.T;
+  const bool bad = *cl.map_shared_rank(&s_bad, 0) != 0;
+  cl.sync();  // read before the first CTA may end
+  if (bad) return;
+  if (wrong) {
+    if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
+    return;
+  }
+  if (m == 0) {
+    if (rank == 0 && tid == 0) a.accepted[b] = 0;
+    return;
+  }
+  const float t = clamp_temperature(a.temp ? a.temp[b] : 1.f);
+  const Heat h = heat_of(t);
+  if (tid == 0) s_first = m - 1;
+  __syncthreads();
+  // the first draft that does not stand: a warp a row
+  for (int j = warp; j < m - 1; j += kPickWarps) {
+    const int64_t row = o0 + j;
+    const int y = a.tokens[row + 1];
+    const Row r = join_row(a, row, t, lane);
+    if (lane == 0) {
+      bool stands = false;
+      if (y >= 0 && y < V && r.z > 0.0) {
+        const float q = a.has_draft ? draft_at<Q>(a, row, y) : 1.f;
+        const float x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
+        double e;  // the token's weight
+        if (h.greedy)
+          e = y == r.at ? 1.0 : 0.0;
+        else
+          e = x == r.m ? 1.0 : exp(((double)x - (double)r.m) / (double)t);
+        stands = (double)a.u[row] * (double)q * r.z < e;
+      }
+      if (!stands) atomicMin(&s_first, j);
+    }
+  }
+  __syncthreads();
+  const int first = s_first;
+  const int64_t row = o0 + first;
+  if (warp == 0) {
+    const Row r = join_row(a, row, t, lane);
+    if (lane == 0) s_row = r;
+  }
+  __syncthreads();
+  const Row r = s_row;
+  const int fallen = first < m - 1 ? a.tokens[row + 1] : -1;
+  // the distribution of the next token, p less what the draft had of it
+  const T *x = (const T *)a.x.x + row * a.x.stride;
+  const double inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
+  const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
+  bool less = first < m - 1;
+  auto mass = [&](int i) -> uint64_t {  // of token i in 2^-62
+    float q = 0.f;
+    if (less) q = a.has_draft ? (fallen >= 0 && fallen < V ? draft_at<Q>(a, row, i) : 0.f)
+                              : (i == fallen ? 2.f : 0.f);
+    float w;
+    if (h.greedy) {
+      w = i == r.at ? 1.f - q : 0.f;
+    } else {
+      const float e = weight(logit<T>(x, i), r.m, h);
+      w = __fmaf_rn(e, inv_hi, __fmaf_rn(e, inv_lo, -q));
+    }
+    return w > 0.f ? __float2ull_rn(fminf(w, 1.f) * kUnit) : 0;
+  };
+  // whole segments a warp, in order over the cluster's warps
+  const int segs = (V + kSegElems - 1) / kSegElems;
+  const int per = (segs + n_cta * kPickWarps - 1) / (n_cta * kPickWarps);
+  const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
+  auto segment = [&](int g) {  // a lane's share: elements lane, lane + 32, ..
+    uint64_t s = 0;
+    const int base = g * kSegElems + lane;
+#pragma unroll
+    for (int k = 0; k < kSeg; ++k)
+      if (base + 32 * k < V) s += mass(base + 32 * k);
+    return s;
+  };
+  auto warp_sum = [&](uint64_t s) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+  };
+  uint64_t total = 0, before = 0;
+  for (int pass = 0; pass < 2; ++pass) {  // a second one where the draft leaves nothing: p itself
+    uint64_t s = 0;
+    if (r.z > 0.0)
+      for (int g = g0; g < g1; ++g) s += segment(g);
+    s = warp_sum(s);
+    if (lane == 0) s_warp[warp] = s;
+    __syncthreads();
+    if (tid == 0) {
+      uint64_t sum = 0;
+      for (int w = 0; w < kPickWarps; ++w) sum += s_warp[w];
+      s_total = sum;
+    }
+    cl.sync();
+    total = before = 0;
+    for (int c = 0; c < n_cta; ++c) {
+      const uint64_t v = *cl.map_shared_rank(&s_total, c);
+      if (c < rank) before += v;
+      total += v;
+    }
+    cl.sync();  // read by all before it is written again, or its CTA ends
+    if (total || !less) break;
+    less = false;
+  }
+  // the lowest token whose sum passes r of the total
+  const float rnd = a.r[b];
+  uint64_t want = rnd > 0.f ? (rnd < 1.f ? __double2ull_rd((double)rnd * (double)total) : total) : 0;
+  if (want >= total) want = total ? total - 1 : 0;
+  for (int w = 0; w < warp; ++w) before += s_warp[w];
+  if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
+    int token = -1;
+    for (int g = g0; g < g1; ++g) {
+      const uint64_t s = warp_sum(segment(g));
+      if (want >= before + s) {
+        before += s;
+        continue;
+      }
+      for (int k = 0; k < kSeg; ++k) {
+        const int i = g * kSegElems + 32 * k + lane;
+        uint64_t c = i < V ? mass(i) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint64_t u = __shfl_up_sync(0xffffffffu, c, o);
+          if (lane >= o) c += u;
+        }
+        const unsigned over = __ballot_sync(0xffffffffu, before + c > want);
+        if (over) {
+          token = g * kSegElems + 32 * k + __ffs((int)over) - 1;
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, c, 31);
+      }
+      break;
+    }
+    if (lane == 0) a.picked[row] = token;
+  }
+  if (rank == 0) {
+    if (tid == 0) {
+      a.accepted[b] = first;
+      if (total == 0) a.picked[row] = -1;
+    }
+    for (int j = tid; j < m; j += kPickThreads)
+      if (j != first) a.picked[o0 + j] = j < first ? a.tokens[o0 + j + 1] : -1;
+  }
+}
+
+// ---------------------------------------------------------------- rows of fallen drafts
+
+__global__ void end_chunk_kernel(lg_cache c, lg_chunk ch, const int32_t *accepted) {
+  pdl_enter();
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= c.batch) return;
+  const int64_t o0 = ch.off[b], o1 = ch.off[b + 1];
+  const int n = c.len[b], a = accepted[b];
+  if (status_bad(c.dev_status)) return;
+  const int64_t m = o1 - o0;
+  if (o0 < 0 || m < 0 || o1 > ch.T || m > ch.max_new || m > n || a < 0 || (m > 0 && a > m - 1))
+    set_status(c.dev_status, LG_ERR_CAPACITY);
+  else if (m > 0)
+    c.len[b] = n - (int)(m - 1 - a);
+}
+
+template <typename T, typename Q>
+cudaError_t launch_pick_typed(const VerifyArgs &a, cudaStream_t s) {
+  // as many CTAs a sequence as leave each an SM of its own
+  int n = 8;
+  while (n > 1 && a.batch * n > 152) n /= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.batch * n));
+  cfg.blockDim = kPickThreads;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = n;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, verify_pick_kernel<T, Q>, a);
+}
+
+template <typename T>
+cudaError_t launch_verify_typed(const VerifyArgs &a, cudaStream_t s) {
+  LG_TRY(launch_pdl(verify_rows_kernel<T>, dim3(a.slices, a.T), kRowThreads, 0, s, a));
+  return a.draft.dtype == LG_BF16 ? launch_pick_typed<T, __nv_bfloat16>(a, s)
+                                  : launch_pick_typed<T, float>(a, s);
+}
+
+}  // namespace
+
+size_t verify_ws_bytes(const lg_logits &x, int T) {
+  return (size_t)T * row_slices(x.V, x.dtype == LG_BF16 ? 2 : 4) * sizeof(RowPart);
+}
+
+cudaError_t launch_verify(const lg_logits &x, const lg_chunk &ch, int batch, const int32_t *tokens,
+                          const lg_logits *draft, const float *temp, const float *u, const float *r,
+                          int32_t *picked, int32_t *accepted, void *ws, int32_t *status,
+                          cudaStream_t s) {
+  VerifyArgs a = {};
+  a.x = x;
+  a.has_draft = draft != nullptr;
+  if (draft) a.draft = *draft;
+  a.batch = batch, a.T = ch.T, a.max_new = ch.max_new;
+  a.slices = row_slices(x.V, x.dtype == LG_BF16 ? 2 : 4);
+  a.off = ch.off, a.tokens = tokens;
+  a.temp = temp, a.u = u, a.r = r;
+  a.picked = picked, a.accepted = accepted, a.status = status;
+  a.part = (RowPart *)ws;
+  return x.dtype == LG_BF16 ? launch_verify_typed<__nv_bfloat16>(a, s)
+                            : launch_verify_typed<float>(a, s);
+}
+
+cudaError_t launch_end_chunk(const lg_cache &c, const lg_chunk &ch, const int32_t *accepted,
+                             cudaStream_t s) {
+  LG_TRY(launch_pdl(end_chunk_kernel, (c.batch + 127) / 128, 128, 0, s, c, ch, accepted));
+  return cudaGetLastError();
+}
+
+}  // namespace lg

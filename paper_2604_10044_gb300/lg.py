@@ -1,4 +1,4 @@
-"""Python binding of liblg.so (include/lg.h, include/lg_chunk.h): argument marshalling only.
+"""Python binding of liblg.so (include/lg.h, lg_chunk.h, lg_draft.h): argument marshalling only.
 
 Every function named ``lg_*`` here calls the C function of the same name with raw device
 pointers taken from torch tensors and the caller's CUDA stream; every step of the decode path
@@ -18,7 +18,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblg.so")
 
-LG_OK, LG_BF16, LG_F32 = 0, 0, 1
+LG_OK, LG_BF16, LG_F32, LG_Q4 = 0, 0, 1, 2
 STATUS = {0: "LG_OK", 1: "LG_ERR_INVALID_ARG", 2: "LG_ERR_UNSUPPORTED", 3: "LG_ERR_CUDA",
           4: "LG_ERR_CAPACITY", 5: "LG_ERR_TIMEOUT", 6: "LG_ERR_WORKSPACE", 7: "LG_ERR_BUDGET"}
 
@@ -125,6 +125,11 @@ def lib():
                                 i32, vp, ctypes.c_size_t, vp],
             "lg_count_tokens": [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp],
             "lg_pick_token": [vp, vp, vp, vp, P(LgBias), vp, vp, vp, vp, vp, vp],
+            "lg_verify_workspace_size": [vp, P(LgChunk)],
+            "lg_verify_draft": [vp, P(LgChunk), i32, vp, vp, vp, vp, vp, vp, vp, vp,
+                                ctypes.c_size_t, vp, vp],
+            "lg_end_chunk": [P(LgCache), P(LgChunk), vp, vp],
+            "lg_read_rows": [P(LgCache), P(LgChunk), i32, vp, vp, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -134,6 +139,7 @@ def lib():
         L.lg_detect_state_size.restype = ctypes.c_size_t
         L.lg_chunk_workspace_size.restype = ctypes.c_size_t
         L.lg_token_state_size.restype = ctypes.c_size_t
+        L.lg_verify_workspace_size.restype = ctypes.c_size_t
         L.lg_status_string.restype = ctypes.c_char_p
         _lib = L
     return _lib
@@ -154,6 +160,11 @@ def chunk_symbols():
     """names of the C ABI functions declared in include/lg_chunk.h"""
     return ["lg_begin_chunk", "lg_default_rope_params", "lg_rope_append",
             "lg_chunk_workspace_size", "lg_chunk_attend", "lg_count_tokens", "lg_pick_token"]
+
+
+def draft_symbols():
+    """names of the C ABI functions declared in include/lg_draft.h"""
+    return ["lg_verify_workspace_size", "lg_verify_draft", "lg_end_chunk", "lg_read_rows"]
 
 
 NOALLOC_SCRATCH_BYTES = 32 << 20  # LG_NOALLOC_SCRATCH_BYTES in include/lg.h
@@ -389,6 +400,12 @@ def _device_of(cache, chunk):
     return at
 
 
+def _row_type(cache):
+    """the type of queries, new rows and results: the cache's, bf16 for one of four bits"""
+    dt = cache.k.dtype
+    return torch.bfloat16 if dt is torch.uint8 else dt
+
+
 def lg_begin_chunk(cache, chunk, stream=None):
     _device_of(cache, chunk)
     _call("lg_begin_chunk", ctypes.byref(cache.c), ctypes.byref(chunk.c), _stream(stream))
@@ -407,7 +424,7 @@ def lg_rope_append(cache, chunk, layer, q, k_new, v_new, pos, rope, q_out, param
     projection pass as they are"""
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out: dense [T][H_q][d]")
-    T, H_kv, d, dt = chunk.T, cache.H_kv, cache.d, cache.k.dtype
+    T, H_kv, d, dt = chunk.T, cache.H_kv, cache.d, _row_type(cache)
     at = _device_of(cache, chunk)
     H_q = qs = 0
     if q is not None:
@@ -441,7 +458,7 @@ def lg_chunk_attend(cache, chunk, layer, q, H_q, scale, window, n_sink, out, max
                     stream=None):
     if not (q.is_contiguous() and out.is_contiguous()):
         raise ValueError("q, out: dense [T][H_q][d]")
-    n, dt, at = chunk.T * H_q * cache.d, cache.k.dtype, _device_of(cache, chunk)
+    n, dt, at = chunk.T * H_q * cache.d, _row_type(cache), _device_of(cache, chunk)
     if (q.dtype is not dt or out.dtype is not dt or q.numel() < n or out.numel() < n or
             q.get_device() != at or out.get_device() != at):
         _refuse("q, out", "[T][H_q][d] of the cache's type")
@@ -540,15 +557,83 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
         raise LgError("lg_pick_token", rc)
 
 
+# ------------------------------------------------------------------ drafted tokens, 4-bit rows
+
+def _logits_of(t, name):
+    """an lg_logits of [rows][V] with whole rows that do not overlap"""
+    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("%s: [T][V] with whole rows that do not overlap" % name)
+    B, V = t.shape
+    return _lg_logits(t.data_ptr(), _LOGITS.get(t.dtype, -1), B, V, 0, t.stride(0) if B > 1 else V)
+
+
+def lg_verify_workspace_size(logits, chunk) -> int:
+    return int(lib().lg_verify_workspace_size(_logits_of(logits, "logits"), ctypes.byref(chunk.c)))
+
+
+def lg_verify_draft(logits, chunk, tokens, draft, temperature, u, r, picked, accepted, ws,
+                    status=None, stream=None):
+    """logits [T][V], row t the target's after tokens[t]; draft: probabilities [T][V] (its own type and
+    stride) or None; temperature [batch] or None, u [T], r [batch] fp32; picked [T], accepted [batch]
+    int32; ws: lg_verify_workspace_size bytes"""
+    T, batch, at = chunk.T, chunk.off.numel() - 1, _device()
+    x = _logits_of(logits, "logits")
+    y = None if draft is None else _logits_of(draft, "draft")
+    if chunk.off.get_device() != at:
+        _refuse("off", "[batch + 1] int32")
+    if logits.get_device() != at or draft is not None and draft.get_device() != at:
+        _refuse("logits, draft", "[T][V]")
+    if not (_dense(tokens, _I32, T, at) and _dense(picked, _I32, T, at) and
+            _dense(accepted, _I32, batch, at)):
+        _refuse("tokens, picked, accepted", "[T], [T], [batch] int32")
+    if not (_dense(u, _F32, T, at) and _dense(r, _F32, batch, at) and
+            (temperature is None or _dense(temperature, _F32, batch, at))):
+        _refuse("u, r, temperature", "[T], [batch], [batch] fp32")
+    if status is not None and not _dense(status, _I32, 1, at):
+        _refuse("status", "a word of int32")
+    if not ws.is_contiguous() or ws.get_device() != at:
+        _refuse("ws", "bytes")
+    rc = (_lib or lib()).lg_verify_draft(
+        x, ctypes.byref(chunk.c), batch, tokens.data_ptr(), y, _ptr(temperature), u.data_ptr(),
+        r.data_ptr(), picked.data_ptr(), accepted.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(status),
+        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        raise LgError("lg_verify_draft", rc)
+
+
+def lg_end_chunk(cache, chunk, accepted, stream=None):
+    at = _device_of(cache, chunk)
+    if not _dense(accepted, _I32, cache.c.batch, at):
+        _refuse("accepted", "[batch] int32")
+    _call("lg_end_chunk", ctypes.byref(cache.c), ctypes.byref(chunk.c), _ptr(accepted),
+          _stream(stream))
+
+
+def lg_read_rows(cache, chunk, layer, k_out, v_out, stream=None):
+    """the chunk's rows of a 4-bit cache as values: k_out, v_out [T][H_kv][d] bf16"""
+    n, at = chunk.T * cache.H_kv * cache.d, _device_of(cache, chunk)
+    if not (_dense(k_out, torch.bfloat16, n, at) and _dense(v_out, torch.bfloat16, n, at)):
+        _refuse("k_out, v_out", "[T][H_kv][d] bf16")
+    rc = (_lib or lib()).lg_read_rows(
+        ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, k_out.data_ptr(), v_out.data_ptr(),
+        _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        raise LgError("lg_read_rows", rc)
+
+
 # ------------------------------------------------------------------ device buffers of a batch
 
 def _torch_dtype(dtype: str):
-    return torch.bfloat16 if dtype == "bf16" else torch.float32
+    """of queries, new rows and results"""
+    return torch.float32 if dtype == "f32" else torch.bfloat16
+
+
+_DTYPES = {"bf16": LG_BF16, "f32": LG_F32, "q4": LG_Q4}
 
 
 def host_to_device(a: np.ndarray, device, dtype: str):
     """numpy cache-dtype array (bf16 as uint16 bits, or float32) -> torch tensor on device"""
-    if dtype == "bf16":
+    if dtype != "f32":
         return torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(
             torch.bfloat16).to(device)
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(device)
@@ -563,7 +648,8 @@ def device_to_host(t: torch.Tensor) -> np.ndarray:
 
 class Cache:
     """Device KV cache of a batch laid out as lg_cache documents, plus its metadata.
-    policy 'loopguard' allocates sketches; 'h2o' allocates scores and positions."""
+    policy 'loopguard' allocates sketches; 'h2o' allocates scores and positions.  dtype 'bf16', 'f32' or
+    'q4': rows in four bits, k and v then bytes [L][H_kv][S_total][d/2 + 16] (LG_Q4 of lg.h)."""
 
     def __init__(self, L, H_kv, d, dtype, seq_off, cap, n0, device, policy="loopguard",
                  k=None, v=None):
@@ -571,8 +657,10 @@ class Cache:
         self.device = torch.device(device)
         self.batch = len(cap)
         self.S_total = int(np.asarray(cap, dtype=np.int64).sum())
-        tdt = _torch_dtype(dtype)
-        shape = (L, H_kv, self.S_total, d)
+        if dtype == "q4" and policy not in ("loopguard", "none"):
+            raise ValueError("a cache of four bits has no scores and positions")
+        tdt = torch.uint8 if dtype == "q4" else _torch_dtype(dtype)
+        shape = (L, H_kv, self.S_total, d // 2 + 16 if dtype == "q4" else d)
         self.k = k if k is not None else torch.zeros(shape, dtype=tdt, device=self.device)
         self.v = v if v is not None else torch.zeros(shape, dtype=tdt, device=self.device)
         self.seq_off = torch.as_tensor(np.asarray(seq_off, dtype=np.int64), device=self.device)
@@ -590,8 +678,7 @@ class Cache:
             self.pos = torch.zeros((L, H_kv, self.S_total), dtype=torch.int32,
                                    device=self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self.c = LgCache(k=_ptr(self.k), v=_ptr(self.v), dtype=LG_BF16 if dtype == "bf16" else
-                         LG_F32, L=L, H_kv=H_kv, d=d, batch=self.batch, pad=0,
+        self.c = LgCache(k=_ptr(self.k), v=_ptr(self.v), dtype=_DTYPES[dtype], L=L, H_kv=H_kv, d=d, batch=self.batch, pad=0,
                          S_total=self.S_total, seq_off=_ptr(self.seq_off), cap=_ptr(self.cap),
                          len=_ptr(self.len), sketch=_ptr(self.sketch), h2o=_ptr(self.h2o),
                          pos=_ptr(self.pos), dev_status=_ptr(self.status))
@@ -606,8 +693,9 @@ class Cache:
         return c
 
     def prepare(self, max_len, params=None):
-        """after a prefill: sketches of the guard layer, or H2O positions and scores"""
-        if self.sketch is not None:
+        """after a prefill: sketches of the guard layer, or H2O positions and scores (a cache of four
+        bits has its sketches from the appends)"""
+        if self.sketch is not None and self.dtype != "q4":
             lg_sketch_build(self, params or lg_default_params(), max_len)
         if self.h2o is not None:
             lg_h2o_reset(self, max_len)
