@@ -21,15 +21,6 @@ __host__ __device__ constexpr int q4_row_bytes(int d) { return d / 2 + 16; }
 constexpr float kQ4Range = 0x1p118f;
 constexpr uint32_t kQ4NaN = 0x7fffu;  // the word of such a group: scale NaN, least value 0
 
-// bf16 numbers 128 + code from the low four bits of either half
-constexpr uint32_t kQ4Mask = 0x000f000fu, kQ4Magic = 0x43004300u;
-
-__device__ __forceinline__ uint32_t q4_pair(uint32_t x) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(kQ4Mask), "n"(kQ4Magic));
-  return r;
-}
-
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 

@@ -2,19 +2,23 @@
 // cache, with the statistics that the guard reads of a single token.
 //
 // A warp takes 16 rows of keys and values at a time through mma.sync (M = 16 keys or 16 elements, N = 8
-// query rows, K = 16), and no value is ever formed from its code:
-//   scores   q . k = sum over groups of (s_g sum_e q_e c_e) + sum_g lo_g sum_{e in g} q_e.  The codes enter
-//            as the bf16 numbers 128 + c (a shift and a mask and an or for two), the products of a group
-//            start from -128 sum q instead of zero, and the four sums are joined by the rows' scales in
-//            fp32.  The least values are one more product, with sums of q in two bf16 terms.  q and the
-//            codes are exact, so are the products.
-//   results  sum_k p_k v_k = sum_k (p_k s_kg)(c - 8) + sum_k p_k (lo_kg + 8 s_kg): for each group the weights
-//            times its scales, rounded to bf16, are the second operand, and one more product takes the
-//            groups' middles.  Codes about zero, not 128 + c with the 128 taken off at the end: sums then
-//            stay small beside what the matrix unit drops of them (over 262143 rows of independent values
-//            the result was off by 1.5 % with 128), and a weight's second rounding meets |c - 8|, not c.
-// A row's pair of codes for the results is a pair of keys: two rows' half words joined by one byte
-// permutation, then the same shift and mask.
+// query rows, K = 16), and a value is never formed from its code and parameters:
+//   scores   q . k = sum over groups of (s_g sum_e q_e c_e) + sum_g lo_g sum_{e in g} q_e.  A code masked out
+//            of its word is a bf16 number as it stands: the low eight bits of one count in units of 2^-133
+//            (its subnormal numbers, and the first normal ones), so bits 0-3 are c and bits 4-7 16 c of them.
+//            The queries bring the factor, 2^120 over the power of two of the row's largest element (and a
+//            sixteenth of that for the 16 c); both are exact, so are the products.  The groups' sums are
+//            joined by the rows' scales in fp32; the least values are one more product, with sums of q
+//            in two bf16 terms.
+//   results  sum_k p_k v_k = sum_k (p_k s_kg)(c - 8) + sum_k p_k lo_kg + 8 sum_k p_k s_kg: the second operand
+//            is the weights times a group's scales, rounded to bf16; the last two are one product whose
+//            first operand is the rows' parameters.  One fused operation turns the masked code into
+//            (c - 8) / 64 or / 4: with codes about zero sums stay small beside what the matrix unit drops
+//            of them, and a weight's second rounding meets |c - 8|, not c.
+// Codes and parameters come by ldmatrix: a 16-byte piece of a row is a group (two of them, for d = 64), and
+// transposed a register holds a half word of codes of two neighbouring keys, which is a pair of each of
+// its nibbles.  For d = 64 a product of the scores takes one group of the two, the other's queries being
+// zero, and of the results half of the rows are of use.
 //
 // Weights are 2^(z - m) with a maximum m that may lag: it is formed anew only when a score passes it
 // by 8, so a tile asks one vote.  Every warp has its own m and sums; the CTA's four are merged at its
@@ -54,33 +58,21 @@ struct Q4Cfg {
   static constexpr int kSmem = (kRing > kOut ? kRing : kOut) + kQ;
 };
 
-// A group's second operands of the scores for thread t, from a query row (null: zeros): slots 2t, 2t+1
-// and 2t+8, 2t+9 of each product hold the elements that q4_pair leaves of the thread's codes.
+// The 16-byte piece of a row that holds group gr, and whether word (or half word) i of it, of four
+// (eight), belongs to the group.
 template <int D>
-__device__ __forceinline__ void query_fragment(const __nv_bfloat16 *q, int gr, int t,
-                                               uint32_t (&f)[D / 32]) {
-  uint4 v = make_uint4(0, 0, 0, 0);
-  if constexpr (D == 128) {  // one word of codes a row: its eight elements in order
-    if (q) v = *(const uint4 *)(q + 8 * (4 * gr + t));
-    f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
-  } else {  // half a word: the even elements or the odd ones
-    if (q) v = *(const uint4 *)(q + 8 * (2 * gr + (t >> 1)));
-    const uint32_t sel = t & 1 ? 0x7632 : 0x5410;
-    f[0] = __byte_perm(v.x, v.y, sel);
-    f[1] = __byte_perm(v.z, v.w, sel);
-  }
+__device__ __forceinline__ constexpr int piece_of(int gr) {
+  return D == 128 ? gr : gr >> 1;
+}
+template <int D, int N>
+__device__ __forceinline__ bool of_group(int gr, int i) {
+  return D == 128 || i / (N / 2) == (gr & 1);
 }
 
-// the element of row r (g or g + 8) of result tile u of group gr
+// the element of row r (g or g + 8) of result tile u of group gr: nibble 2u or 2u + 1 of half word g
 template <int D>
-__device__ __forceinline__ int value_element(int gr, int u, int r) {
-  const int g = r & 7, up = r >> 3;
-  if constexpr (D == 128) {
-    return 8 * (4 * gr + (g >> 1)) + 2 * (2 * u + up) + (g & 1);
-  } else {
-    const int n = 2 * (g & 3) + up;  // nibble of the word
-    return 8 * (2 * gr + (g >> 2)) + (n < 4 ? 2 * n : 2 * (n - 4) + 1);
-  }
+__device__ __forceinline__ int value_element(int gr, int u, int g, int up) {
+  return 8 * (4 * piece_of<D>(gr) + (g >> 1)) + 2 * (2 * u + up) + (g & 1);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -93,20 +85,43 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return *(const uint32_t *)&r;
 }
 
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 r = __hsub2(*(const __nv_bfloat162 *)&a, *(const __nv_bfloat162 *)&b);
+// masked codes, c or 16 c in units of 2^-133, to (c - 8) / 64 or (c - 8) / 4
+__device__ __forceinline__ uint32_t centred(uint32_t raw, bool high) {
+  const uint32_t by = 0x7f007f00u, less = high ? 0xc000c000u : 0xbe00be00u;  // 2^127; -2 or -1/8
+  const __nv_bfloat162 r = __hfma2(*(const __nv_bfloat162 *)&raw, *(const __nv_bfloat162 *)&by,
+                                   *(const __nv_bfloat162 *)&less);
   return *(const uint32_t *)&r;
 }
 
-constexpr uint32_t k136 = 0x43084308u;  // two bf16 numbers 136: 128 + c less 136 is c - 8, exactly
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 
-// lo + 8 s of a group of two rows, rounded once
-__device__ __forceinline__ uint32_t middles(uint32_t par0, uint32_t par1) {
-  const uint32_t s = __byte_perm(par0, par1, 0x5410), lo = __byte_perm(par0, par1, 0x7632);
-  const uint32_t eight = 0x41004100u;
-  const __nv_bfloat162 r = __hfma2(*(const __nv_bfloat162 *)&s, *(const __nv_bfloat162 *)&eight,
-                                   *(const __nv_bfloat162 *)&lo);
-  return *(const uint32_t *)&r;
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix2(uint32_t &a, uint32_t &b, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];"
+               : "=r"(a), "=r"(b) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix2_trans(uint32_t &a, uint32_t &b, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];"
+               : "=r"(a), "=r"(b) : "r"(at) : "memory");
+}
+
+// a half that is not finite, or whose key is past the last row, becomes zero
+__device__ __forceinline__ uint32_t finite_pair(uint32_t x, bool keep0, bool keep1) {
+  uint32_t mask = 0;
+  if (keep0 && (x & 0x7f80u) != 0x7f80u) mask |= 0xffffu;
+  if (keep1 && (x & 0x7f800000u) != 0x7f800000u) mask |= 0xffff0000u;
+  return x & mask;
 }
 
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
@@ -160,7 +175,7 @@ __device__ __forceinline__ bool q4_item(const Q4AttendArgs &a, int64_t item, Q4I
 template <int D, int NT, bool STATS>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_attend_kernel(Q4AttendArgs a) {
   using C = Q4Cfg<D, NT>;
-  constexpr int kMpg = D == 128 ? 2 : 1;  // products of a group
+  constexpr int kPieces = D / 32;  // 16-byte pieces of a row's codes
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t s_full[kWarps][C::kStages];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -213,33 +228,54 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     r += w.tile * a.rows;
     return r < w.tile * a.rows + w.used ? q + ((int64_t)(r / a.g) * H_q + r % a.g) * D : nullptr;
   };
-  uint32_t qf[NT <= 2 ? NT : 1][4][2 * kMpg];
+  uint32_t qf[NT <= 2 ? NT : 1][4][4];
   uint4 *s_q = (uint4 *)(smem + C::kSmem - C::kQ);
-  float init[NT][4][2];   // [group][column 2t, 2t+1]
   uint32_t sum_hi[NT], sum_lo[NT];
+  float cm[NT][2];  // column 2t, 2t+1: what turns its sums into log2 units
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const __nv_bfloat16 *src = q_row(8 * nt + g);
+    uint4 v[kPieces];  // words t of the pieces: eight elements each
+    float big = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      v[j] = src ? *(const uint4 *)(src + 8 * (4 * j + t)) : make_uint4(0, 0, 0, 0);
+      const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        big = fmaxf(big, fmaxf(fabsf(bf16_low(x[i])), fabsf(bf16_high(x[i]))));
+    }
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+    // the power of two of the largest, kept where 2^120 over it is a number
+    const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -7), 114);
+    const float up = __uint_as_float((uint32_t)(120 - ex + 127) << 23);
+    const float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
+    cm[nt][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
+    cm[nt][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
     float mine = 0.f;
 #pragma unroll
     for (int gr = 0; gr < 4; ++gr) {
-      uint32_t f[2 * kMpg];
-      query_fragment<D>(src, gr, t, f);
+      const uint4 w4 = v[piece_of<D>(gr)];
+      const uint32_t x[4] = {w4.x, w4.y, w4.z, w4.w};
+      const bool in = of_group<D, 4>(gr, t);
+      uint32_t f[4];
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2 * kMpg; ++i) sum += bf16_low(f[i]) + bf16_high(f[i]);
+      for (int i = 0; i < 4; ++i) {  // pair i of a word; odd ones meet 16 c
+        const float lo = in ? bf16_low(x[i]) : 0.f, hi = in ? bf16_high(x[i]) : 0.f;
+        const float by = i & 1 ? up * 0.0625f : up;
+        f[i] = pack_bf16(lo * by, hi * by);
+        sum += lo + hi;
+      }
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (t == gr) mine = sum;
-      // columns 2t, 2t+1 of the scores belong to the query rows of lanes 8t and 8t + 4
-      init[nt][gr][0] = -128.f * __shfl_sync(0xffffffffu, sum, 8 * t);
-      init[nt][gr][1] = -128.f * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+      if (t == gr) mine = sum * (up * 0x1p-120f) * 0x1p-13f;
       if constexpr (NT <= 2) {
 #pragma unroll
-        for (int i = 0; i < 2 * kMpg; ++i) qf[nt][gr][i] = f[i];
+        for (int i = 0; i < 4; ++i) qf[nt][gr][i] = f[i];
       } else if (warp == 0) {
-        s_q[(nt * 4 + gr) * 32 + lane] =
-            make_uint4(f[0], f[1], kMpg == 2 ? f[2 * kMpg - 2] : 0u, kMpg == 2 ? f[2 * kMpg - 1] : 0u);
+        s_q[(nt * 4 + gr) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
       }
     }
     const float hi = __bfloat162float(__float2bfloat16_rn(mine));
@@ -251,9 +287,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   const int low_max = a.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.window) : 0;
   const int suffix0 = w.q.n - a.suffix_w;  // (n and suffix_w are positive)
 
-  float o[NT][4][kMpg][4] = {};
-  float ox[NT][4] = {};  // rows gr: the weights times the middles of group gr
-  float m[NT][2], top[NT][2], l[NT][2], hs[NT][2], sf[NT][2];
+  float o[NT][4][2][4] = {};
+  float ox[NT][4] = {};  // rows 2 gr: the weights times group gr's scales; rows 2 gr + 1: times least values
+  float m[NT][2], top[NT][2], l[NT][2], hs[NT][2], sf[NT][2];  // top: the largest score, less m
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -262,76 +298,74 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       l[nt][c] = hs[nt][c] = sf[nt][c] = 0.f;
     }
 
+  // this lane's row and 16-byte piece of an ldmatrix of four, and its row of one of two
+  const uint32_t ring_at = smem_addr(ring);
+  const uint32_t at4 = (lane & 15) * C::kRow + 16 * (lane >> 4);
+  const uint32_t at2 = (lane & 15) * C::kRow + D / 2;
+
   bool gave_up = false;
+  int st = 0, phase = 0;
   for (int i = blk0; i < blk1; ++i) {
     const int r0 = tile_row(i);
-    const int st = (i - blk0) % C::kStages;
     if (r0 <= w.rows.last) {  // (the same for the whole warp)
-      if (!mbar_wait_warp(&s_full[warp][st], ((i - blk0) / C::kStages) & 1)) {
+      if (!mbar_wait_warp(&s_full[warp][st], phase)) {
         gave_up = true;
         break;
       }
       const uint8_t *sk = ring + st * 2 * C::kTile, *sv = sk + C::kTile;
+      const uint32_t k_at = ring_at + st * 2 * C::kTile, v_at = k_at + C::kTile;
       // ---- scores
-      float z[NT][4];
+      float raw[NT][4], z[NT][4];
       {
-        const uint8_t *ka = sk + g * C::kRow, *kb = ka + 8 * C::kRow;
-        const uint4 pa = *(const uint4 *)(ka + D / 2), pb = *(const uint4 *)(kb + D / 2);
-        const uint32_t ga = *(const uint32_t *)(ka + D / 2 + 4 * t);
-        const uint32_t gb = *(const uint32_t *)(kb + D / 2 + 4 * t);
+        uint32_t ga, gb;
+        ldmatrix2(ga, gb, k_at + at2);
+        // (the scales in the even slots meet zeros)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-          mma_bf16(z[nt], ga & 0xffff0000u, gb & 0xffff0000u, ga & 0xffff0000u, gb & 0xffff0000u,
-                   sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
+          mma_bf16(raw[nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
+        const uint4 pa = *(const uint4 *)(sk + g * C::kRow + D / 2);
+        const uint4 pb = *(const uint4 *)(sk + (g + 8) * C::kRow + D / 2);
         const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-          uint32_t wa, wb;
-          if constexpr (D == 128) {
-            wa = *(const uint32_t *)(ka + 16 * gr + 4 * t);
-            wb = *(const uint32_t *)(kb + 16 * gr + 4 * t);
-          } else {
-            wa = *(const uint16_t *)(ka + 8 * gr + 2 * t);
-            wb = *(const uint16_t *)(kb + 8 * gr + 2 * t);
-            wa |= wa << 12;
-            wb |= wb << 12;
-          }
-          constexpr int kStep = D == 128 ? 4 : 8;
-          uint32_t fa[2 * kMpg], fb[2 * kMpg];
+        for (int j2 = 0; j2 < kPieces; j2 += 2) {
+          uint32_t kw[4];
+          ldmatrix4(kw, k_at + at4 + 16 * j2);
 #pragma unroll
-          for (int j = 0; j < 2 * kMpg; ++j) {
-            fa[j] = q4_pair(wa >> (kStep * j));
-            fb[j] = q4_pair(wb >> (kStep * j));
-          }
-          const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
+          for (int jj = 0; jj < 2; ++jj) {
+            const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
+            const uint32_t fa[4] = {wa & kLow, wa & kHigh, va & kLow, va & kHigh};
+            const uint32_t fb[4] = {wb & kLow, wb & kHigh, vb & kLow, vb & kHigh};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t f[2 * kMpg];
-            if constexpr (NT <= 2) {
+            for (int gi = 0; gi < 4 / kPieces; ++gi) {
+              const int gr = (j2 + jj) * (4 / kPieces) + gi;
+              const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
 #pragma unroll
-              for (int j = 0; j < 2 * kMpg; ++j) f[j] = qf[nt][gr][j];
-            } else {
-              const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
-              f[0] = v.x;
-              f[1] = v.y;
-              if constexpr (kMpg == 2) f[2] = v.z, f[3] = v.w;
+              for (int nt = 0; nt < NT; ++nt) {
+                uint32_t f[4];
+                if constexpr (NT <= 2) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) f[e] = qf[nt][gr][e];
+                } else {
+                  const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
+                  f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+                }
+                float d[4];
+                mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], 0.f, 0.f, 0.f, 0.f);
+                mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
+                raw[nt][0] = __fmaf_rn(s_a, d[0], raw[nt][0]);
+                raw[nt][1] = __fmaf_rn(s_a, d[1], raw[nt][1]);
+                raw[nt][2] = __fmaf_rn(s_b, d[2], raw[nt][2]);
+                raw[nt][3] = __fmaf_rn(s_b, d[3], raw[nt][3]);
+              }
             }
-            float d[4];
-            mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], init[nt][gr][0], init[nt][gr][1],
-                     init[nt][gr][0], init[nt][gr][1]);
-            if constexpr (kMpg == 2)
-              mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
-            z[nt][0] = __fmaf_rn(s_a, d[0], z[nt][0]);
-            z[nt][1] = __fmaf_rn(s_a, d[1], z[nt][1]);
-            z[nt][2] = __fmaf_rn(s_b, d[2], z[nt][2]);
-            z[nt][3] = __fmaf_rn(s_b, d[3], z[nt][3]);
           }
         }
       }
+      // ---- scores in log2 units, less the maximum in use
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[nt][j] *= a.qscale;
+        for (int j = 0; j < 4; ++j) z[nt][j] = __fmaf_rn(raw[nt][j], cm[nt][j & 1], -m[nt][j & 1]);
       // ---- what each query may see
       const bool open = r0 + kSub - 1 <= w.rows.first && r0 >= low_max;
       if (!open) {
@@ -350,36 +384,46 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
           }
       }
       // ---- maxima, kept while no score passes them by kLazy
-      bool past = false;
+      float past = kHidden;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) past |= z[nt][j] > m[nt][j & 1] + kLazy;
-      if (__any_sync(0xffffffffu, past)) {
+        for (int c = 0; c < 2; ++c) {
+          past = fmaxf(past, fmaxf(z[nt][c], z[nt][2 + c]));
+        }
+      if (__any_sync(0xffffffffu, past > kLazy)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float x = fmaxf(fmaxf(z[nt][c], z[nt][2 + c]), m[nt][c]);
+            // (from the sums again: a first maximum is no difference to kNone)
+            const float z0 = z[nt][c] == kHidden ? kHidden : raw[nt][c] * cm[nt][c];
+            const float z1 = z[nt][2 + c] == kHidden ? kHidden : raw[nt][2 + c] * cm[nt][c];
+            float x = fmaxf(fmaxf(z0, z1), m[nt][c]);
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
             const float by = m[nt][c] - x, f = exp2_fast(by);
             m[nt][c] = x;
-            if (STATS) hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
+            z[nt][c] = z0 == kHidden ? kHidden : z0 - x;
+            z[nt][2 + c] = z1 == kHidden ? kHidden : z1 - x;
+            if (STATS) {
+              top[nt][c] += by;
+              hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
+              sf[nt][c] *= f;
+            }
             l[nt][c] *= f;
-            if (STATS) sf[nt][c] *= f;
 #pragma unroll
             for (int j = c; j < 4; j += 2) {
               ox[nt][j] *= f;
 #pragma unroll
               for (int gr = 0; gr < 4; ++gr)
 #pragma unroll
-                for (int u = 0; u < kMpg; ++u) o[nt][gr][u][j] *= f;
+                for (int u = 0; u < 2; ++u) o[nt][gr][u][j] *= f;
             }
           }
       }
-      // ---- weights: b0 = keys 2t, 2t+1 and b1 = keys 2t+8, 2t+9 of query row g
+      // ---- weights: p0 = keys 2t, 2t+1 and p1 = keys 2t+8, 2t+9 of query row g
       uint32_t p0[NT], p1[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -387,12 +431,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int c = j & 1;
-          const float d = z[nt][j] - m[nt][c];
-          p[j] = exp2_fast(d);
+          p[j] = exp2_fast(z[nt][j]);
           l[nt][c] += p[j];
           if (STATS) {
             top[nt][c] = fmaxf(top[nt][c], z[nt][j]);
-            hs[nt][c] = __fmaf_rn(p[j], d, hs[nt][c]);
+            hs[nt][c] = __fmaf_rn(p[j], z[nt][j], hs[nt][c]);
           }
         }
         if (STATS && r0 + kSub > suffix0) {
@@ -405,64 +448,60 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       }
       // ---- results: this thread's keys
       {
-        const uint8_t *v0 = sv + (2 * t) * C::kRow, *v1 = v0 + C::kRow, *v2 = v0 + 8 * C::kRow,
-                      *v3 = v0 + 9 * C::kRow;
-        const int lw = D / 2 + 4 * (g & 3);
-        uint32_t l0 = *(const uint32_t *)(v0 + lw), l1 = *(const uint32_t *)(v1 + lw);
-        uint32_t l2 = *(const uint32_t *)(v2 + lw), l3 = *(const uint32_t *)(v3 + lw);
+        uint32_t xa, xb;
+        ldmatrix2_trans(xa, xb, v_at + at2);
         if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
           const int r = r0 + 2 * t, e = w.rows.last;
-          l0 = r > e || (l0 & 0x7f80u) == 0x7f80u ? 0u : l0;
-          l1 = r + 1 > e || (l1 & 0x7f80u) == 0x7f80u ? 0u : l1;
-          l2 = r + 8 > e || (l2 & 0x7f80u) == 0x7f80u ? 0u : l2;
-          l3 = r + 9 > e || (l3 & 0x7f80u) == 0x7f80u ? 0u : l3;
+          xa = finite_pair(xa, r <= e, r + 1 <= e);
+          xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
         }
-        const uint32_t la = middles(l0, l1), lb = middles(l2, l3);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-          mma_bf16(ox[nt], la, la, lb, lb, p0[nt], p1[nt], ox[nt][0], ox[nt][1], ox[nt][2],
-                   ox[nt][3]);
-        const uint4 s0 = *(const uint4 *)(v0 + D / 2), s1 = *(const uint4 *)(v1 + D / 2);
-        const uint4 s2 = *(const uint4 *)(v2 + D / 2), s3 = *(const uint4 *)(v3 + D / 2);
+          mma_bf16(ox[nt], xa, 0u, xb, 0u, p0[nt], p1[nt], ox[nt][0], ox[nt][1], ox[nt][2], ox[nt][3]);
+        const uint8_t *v0 = sv + 2 * t * C::kRow + D / 2;
+        const uint4 s0 = *(const uint4 *)v0, s1 = *(const uint4 *)(v0 + C::kRow);
+        const uint4 s2 = *(const uint4 *)(v0 + 8 * C::kRow), s3 = *(const uint4 *)(v0 + 9 * C::kRow);
         const uint32_t sa[4] = {__byte_perm(s0.x, s1.x, 0x5410), __byte_perm(s0.y, s1.y, 0x5410),
                                 __byte_perm(s0.z, s1.z, 0x5410), __byte_perm(s0.w, s1.w, 0x5410)};
         const uint32_t sb[4] = {__byte_perm(s2.x, s3.x, 0x5410), __byte_perm(s2.y, s3.y, 0x5410),
                                 __byte_perm(s2.z, s3.z, 0x5410), __byte_perm(s2.w, s3.w, 0x5410)};
 #pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-          uint32_t xa, xb;
-          if constexpr (D == 128) {
-            const int at = 16 * gr + 2 * g;
-            xa = *(const uint16_t *)(v0 + at) | (uint32_t)*(const uint16_t *)(v1 + at) << 16;
-            xb = *(const uint16_t *)(v2 + at) | (uint32_t)*(const uint16_t *)(v3 + at) << 16;
-          } else {
-            const int at = 8 * gr + g;
-            xa = v0[at] | (uint32_t)v1[at] << 16;
-            xb = v2[at] | (uint32_t)v3[at] << 16;
-          }
-          uint32_t fa[2 * kMpg], fb[2 * kMpg];
+        for (int j2 = 0; j2 < kPieces; j2 += 2) {
+          uint32_t vw[4];
+          ldmatrix4_trans(vw, v_at + at4 + 16 * j2);
 #pragma unroll
-          for (int j = 0; j < 2 * kMpg; ++j) {
-            fa[j] = sub_bf16x2(q4_pair(xa >> (4 * j)), k136);
-            fb[j] = sub_bf16x2(q4_pair(xb >> (4 * j)), k136);
-          }
+          for (int jj = 0; jj < 2; ++jj) {
+            const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
+            const uint32_t fa[4] = {centred(wa & kLow, false), centred(wa & kHigh, true),
+                                    centred(ua & kLow, false), centred(ua & kHigh, true)};
+            const uint32_t fb[4] = {centred(wb & kLow, false), centred(wb & kHigh, true),
+                                    centred(ub & kLow, false), centred(ub & kHigh, true)};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t b0 = mul_bf16x2(p0[nt], sa[gr]), b1 = mul_bf16x2(p1[nt], sb[gr]);
-            if (!open) {  // a weight of zero stays zero, whatever the scale holds
-              b0 &= (p0[nt] & 0xffffu ? 0xffffu : 0u) | (p0[nt] >> 16 ? 0xffff0000u : 0u);
-              b1 &= (p1[nt] & 0xffffu ? 0xffffu : 0u) | (p1[nt] >> 16 ? 0xffff0000u : 0u);
+            for (int gi = 0; gi < 4 / kPieces; ++gi) {
+              const int gr = (j2 + jj) * (4 / kPieces) + gi;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                uint32_t b0 = mul_bf16x2(p0[nt], sa[gr]), b1 = mul_bf16x2(p1[nt], sb[gr]);
+                if (!open) {  // a weight of zero stays zero, whatever the scale holds
+                  b0 &= (p0[nt] & 0xffffu ? 0xffffu : 0u) | (p0[nt] >> 16 ? 0xffff0000u : 0u);
+                  b1 &= (p1[nt] & 0xffffu ? 0xffffu : 0u) | (p1[nt] >> 16 ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                  mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
+                           o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
+              }
             }
-#pragma unroll
-            for (int u = 0; u < kMpg; ++u)
-              mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
-                       o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
           }
         }
       }
     }
     __syncwarp();  // the stage has been read
     if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages);
+    if (++st == C::kStages) {
+      st = 0;
+      phase ^= 1;
+    }
   }
   if (gave_up && lane == 0) {
     set_status(a.status, LG_ERR_TIMEOUT);
@@ -478,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      float x[4] = {STATS ? top[nt][c] : m[nt][c], l[nt][c], hs[nt][c], sf[nt][c]};
+      float x[4] = {m[nt][c] + (STATS ? top[nt][c] : 0.f), l[nt][c], hs[nt][c], sf[nt][c]};
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) {
         if (STATS) x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], off));
@@ -500,13 +539,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       if (g == 0) s_st[warp][row] = make_float4(x[0], x[1], x[2], x[3]);
 #pragma unroll
       for (int gr = 0; gr < 4; ++gr) {
-        const float base = __shfl_sync(0xffffffffu, ox[nt][c], 4 * gr + t);
+        const float base = __fmaf_rn(8.f, __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + t),
+                                     __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + 4 + t));
 #pragma unroll
-        for (int u = 0; u < kMpg; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int up = 0; up < 2; ++up)
-            s_o[(warp * C::kRows + row) * (D + 1) + value_element<D>(gr, u, g + 8 * up)] =
-                f * (o[nt][gr][u][2 * up + c] + base);
+            if (of_group<D, 8>(gr, g))
+              s_o[(warp * C::kRows + row) * (D + 1) + value_element<D>(gr, u, g, up)] =
+                  f * __fmaf_rn(up ? 4.f : 64.f, o[nt][gr][u][2 * up + c], base);
       }
     }
   }

@@ -3,14 +3,16 @@ tokens.
 
 Tolerances of the attention for few query rows (w the weights, s and lo a value's scale and least value,
 c its code; a rounding to bf16 is off by 2^-8 at most):
-  score   the products are exact; a group's sum holds (128 + c) q and 128 q, so two matrix products of it
-          and their joining lose 2^-22 of Z = scale sum_e s |q_e| (271); the sum of q times lo enters in
-          two bf16 terms, off by 2^-16 of scale sum_groups |lo| |sum q|:  z_err is the sum of both
-  result  with mid = lo + 8 s: a weight rounded to bf16 and again with the scale: 2 2^-8 of w s |c - 8|; with
-          mid, itself rounded to bf16, 2 2^-8 of w |mid|; sums over at most 64 products of a warp lose
-          64 2^-23 of what they sum; the result's own rounding 2^-8; every weight and the normaliser off by
-          z_err + 2^-20 each:
-          |d| <= 2^-8 |ref| + (2^-7 + 2^-17) sum w (s |c - 8| + |mid|) + 2 (z_err + 2^-20) sum w |v|
+  score   the products are exact; two matrix products of a group's sum and the groups' joining lose 2^-22
+          of Z = scale sum_e s |q_e| 15; the sum of q times lo enters in two bf16 terms, off by 2^-16 of
+          scale sum_groups |lo| |sum q|:  z_err is the sum of both
+  result  a weight rounded to bf16 and again with the scale: 2 2^-8 of w s |c - 8|; the weights of lo + 8 s
+          rounded once, alike for both: 2^-8 of w |lo + 8 s|; sums over at most 64 products of a warp lose
+          64 2^-23 = 2^-17 of what they sum, which is w |lo|, w s (8 of it at the end) and w s |c - 8|, each
+          by itself, also where the three cancel; the result's own rounding 2^-8; every weight and the
+          normaliser off by z_err + 2^-20 each:
+          |d| <= 2^-8 |ref| + 2^-7 sum w s |c - 8| + 2^-8 sum w |lo + 8 s|
+                 + 2^-17 sum w (s |c - 8| + |lo| + 8 s) + 2 (z_err + 2^-20) sum w |v|
 For many query rows the values are rounded to bf16 (2^-8 of each key element in a score: z_err grows by
 2^-8 scale sum |q| |k|; 2^-8 of each value) and then go the way of a bf16 cache, whose weights are rounded
 once.
@@ -140,7 +142,7 @@ def attention(q, K, V, n, m, scale, window=0, sink=0, wide=False, suffix=0):
         see &= (i > r - window) | (i < sink)
     z = torch.where(see, q @ k.T * scale, -math.inf)
     # what the scores lose, the largest over the rows a query sees
-    zb = scale * 271 * (q.abs() @ sk.T) * 2.0 ** -22
+    zb = scale * 15 * (q.abs() @ sk.T) * 2.0 ** -22
     d = q.shape[-1]
     sums = q.unflatten(-1, (4, d // 4)).sum(-1).abs().repeat_interleave(d // 4, -1) / (d // 4)
     zb += scale * (sums @ lk.abs().T) * 2.0 ** -16
@@ -154,7 +156,9 @@ def attention(q, K, V, n, m, scale, window=0, sink=0, wide=False, suffix=0):
     if wide:
         tol += 2 * 2.0 ** -8 * big + 2.0 ** -12 * big
     else:
-        tol += (2.0 ** -7 + 2.0 ** -17) * (w @ (sv * (cv - 8).abs() + (lv + 8 * sv).abs()))
+        mid = (lv + 8 * sv).abs()
+        tol += 2.0 ** -7 * (w @ (sv * (cv - 8).abs())) + 2.0 ** -8 * (w @ mid)
+        tol += 2.0 ** -17 * (w @ (sv * (cv - 8).abs() + lv.abs() + 8 * sv))
     top = z.amax(-1)
     p = (z - top[:, None]).exp()
     l = p.sum(-1)
