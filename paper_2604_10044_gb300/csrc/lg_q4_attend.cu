@@ -24,7 +24,7 @@
 // by 8, so a tile asks one vote.  Every warp has its own m and sums; the CTA's four are merged at its
 // end, and the CTAs of an item by a second kernel.
 //
-// Every warp copies its own 16 rows a block (bulk copies into a ring of its own), so warps never wait
+// Every warp copies its own 32 rows a block (bulk copies into a ring of its own), so warps never wait
 // for one another.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -38,9 +38,15 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kSub = 16;             // rows of a warp's tile
-constexpr int kBn2 = 6;              // log2 of a CTA's block: kWarps tiles
+constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
+constexpr int kBn2 = 7;              // log2 of a CTA's block: kWarps tiles
 constexpr int kBn = 1 << kBn2;
+#ifndef Q4_WAVES
+#define Q4_WAVES 3
+#define Q4_MOST 16
+#endif
+constexpr int kWaves = Q4_WAVES;      // of CTAs in a call, while an item has the blocks
+constexpr int kMostBlocks = Q4_MOST;  // of a CTA
 constexpr float kLazy = 8.f;         // log2 units that a weight may pass 1 by
 constexpr float kHidden = -1e38f;    // score of a row that a query does not see
 constexpr float kNone = -1e30f;      // maximum of a query that has seen nothing
@@ -50,7 +56,8 @@ template <int D, int NT>
 struct Q4Cfg {
   static constexpr int kRow = q4_row_bytes(D);
   static constexpr int kTile = kSub * kRow;         // of keys, or of values
-  static constexpr int kStages = 4;
+  static constexpr int kStages = D == 64 ? 4 : NT == 1 ? 2 : NT == 2 ? 3 : 4;
+  static constexpr int kJoint = NT == 1 ? 2 : 1;    // products of 16 rows that go through the softmax together
   static constexpr int kRing = kWarps * kStages * 2 * kTile;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
@@ -201,25 +208,26 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   const int blk0 = chunk * a.blocks, blk1 = min(blk0 + a.blocks, w.blocks.count);
   if (blk0 >= blk1) return;
 
-  // this warp's copies: its 16 rows of each block
+  // this warp's copies: its rows of each block
   uint8_t *ring = smem + warp * C::kStages * 2 * C::kTile;
   const int64_t row0 = ((int64_t)w.layer * a.H_kv + w.kvh) * a.S_total + a.seq_off[w.b];
   const uint8_t *gk = a.K + row0 * C::kRow, *gv = a.V + row0 * C::kRow;
   auto tile_row = [&](int i) { return (w.blocks.index(i) << kBn2) + warp * kSub; };
-  auto copy = [&](int i) {  // lane 0: block i into its stage
+  auto copy = [&](int i, uint8_t *to, uint64_t *bar) {  // lane 0: block i into a stage
     const int r = tile_row(i);
     const int n = min(kSub, w.rows.last + 1 - r);
     if (n <= 0) return;
-    const int st = (i - blk0) % C::kStages;
-    uint8_t *to = ring + st * 2 * C::kTile;
-    mbar_arrive_expect_tx(&s_full[warp][st], 2 * n * C::kRow);
-    bulk_load(to, gk + (int64_t)r * C::kRow, n * C::kRow, &s_full[warp][st]);
-    bulk_load(to + C::kTile, gv + (int64_t)r * C::kRow, n * C::kRow, &s_full[warp][st]);
+    const int bytes = n * C::kRow;
+    const int64_t from = (int64_t)r * C::kRow;
+    mbar_arrive_expect_tx(bar, 2 * bytes);
+    bulk_load(to, gk + from, bytes, bar);
+    bulk_load(to + C::kTile, gv + from, bytes, bar);
   };
   if (lane == 0)
-    for (int i = blk0; i < min(blk1, blk0 + C::kStages); ++i) copy(i);
+    for (int k = 0; k < C::kStages && blk0 + k < blk1; ++k)
+      copy(blk0 + k, ring + k * 2 * C::kTile, &s_full[warp][k]);
 
-  // q as second operands, -128 times its groups' sums, and the sums in two terms for the least values
+  // q as second operands, and its groups' sums in two terms for the least values
   const int H_q = a.H_kv * a.g;
   const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q +
                            (((int64_t)w.layer - a.layer0) * a.T + w.off) * H_q * D +
@@ -299,197 +307,218 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     }
 
   // this lane's row and 16-byte piece of an ldmatrix of four, and its row of one of two
-  const uint32_t ring_at = smem_addr(ring);
   const uint32_t at4 = (lane & 15) * C::kRow + 16 * (lane >> 4);
   const uint32_t at2 = (lane & 15) * C::kRow + D / 2;
 
+  constexpr int J = C::kJoint;
   bool gave_up = false;
   int st = 0, phase = 0;
   for (int i = blk0; i < blk1; ++i) {
     const int r0 = tile_row(i);
+    uint8_t *stage = ring + st * 2 * C::kTile;
+    uint64_t *bar = &s_full[warp][st];
     if (r0 <= w.rows.last) {  // (the same for the whole warp)
-      if (!mbar_wait_warp(&s_full[warp][st], phase)) {
+      if (!mbar_wait_warp(bar, phase)) {
         gave_up = true;
         break;
       }
-      const uint8_t *sk = ring + st * 2 * C::kTile, *sv = sk + C::kTile;
-      const uint32_t k_at = ring_at + st * 2 * C::kTile, v_at = k_at + C::kTile;
-      // ---- scores
-      float raw[NT][4], z[NT][4];
-      {
-        uint32_t ga, gb;
-        ldmatrix2(ga, gb, k_at + at2);
-        // (the scales in the even slots meet zeros)
+      const bool open = r0 + kSub - 1 <= w.rows.first && r0 >= low_max;
+#pragma unroll 1
+      for (int h0 = 0; h0 < kSub / 16; h0 += J) {
+        const uint8_t *sk = stage + h0 * 16 * C::kRow;
+        const uint32_t k_at = smem_addr(sk), v_at = k_at + C::kTile;
+        const int rh = r0 + 16 * h0;
+        // ---- scores
+        float raw[J][NT][4], z[J][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma_bf16(raw[nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
-        const uint4 pa = *(const uint4 *)(sk + g * C::kRow + D / 2);
-        const uint4 pb = *(const uint4 *)(sk + (g + 8) * C::kRow + D / 2);
-        const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
+        for (int h = 0; h < J; ++h) {
+          uint32_t ga, gb;
+          ldmatrix2(ga, gb, k_at + at2 + h * 16 * C::kRow);
+          // (the scales in the even slots meet zeros)
 #pragma unroll
-        for (int j2 = 0; j2 < kPieces; j2 += 2) {
-          uint32_t kw[4];
-          ldmatrix4(kw, k_at + at4 + 16 * j2);
+          for (int nt = 0; nt < NT; ++nt)
+            mma_bf16(raw[h][nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
+          const uint4 pa = *(const uint4 *)(sk + (16 * h + g) * C::kRow + D / 2);
+          const uint4 pb = *(const uint4 *)(sk + (16 * h + g + 8) * C::kRow + D / 2);
+          const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
-            const uint32_t fa[4] = {wa & kLow, wa & kHigh, va & kLow, va & kHigh};
-            const uint32_t fb[4] = {wb & kLow, wb & kHigh, vb & kLow, vb & kHigh};
+          for (int j2 = 0; j2 < kPieces; j2 += 2) {
+            uint32_t kw[4];
+            ldmatrix4(kw, k_at + at4 + h * 16 * C::kRow + 16 * j2);
 #pragma unroll
-            for (int gi = 0; gi < 4 / kPieces; ++gi) {
-              const int gr = (j2 + jj) * (4 / kPieces) + gi;
-              const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
+            for (int jj = 0; jj < 2; ++jj) {
+              const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
+              const uint32_t fa[4] = {wa & kLow, wa & kHigh, va & kLow, va & kHigh};
+              const uint32_t fb[4] = {wb & kLow, wb & kHigh, vb & kLow, vb & kHigh};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                uint32_t f[4];
-                if constexpr (NT <= 2) {
+              for (int gi = 0; gi < 4 / kPieces; ++gi) {
+                const int gr = (j2 + jj) * (4 / kPieces) + gi;
+                const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) f[e] = qf[nt][gr][e];
-                } else {
-                  const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
-                  f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+                for (int nt = 0; nt < NT; ++nt) {
+                  uint32_t f[4];
+                  if constexpr (NT <= 2) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] = qf[nt][gr][e];
+                  } else {
+                    const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
+                    f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+                  }
+                  float d[4];
+                  mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], 0.f, 0.f, 0.f, 0.f);
+                  mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
+                  raw[h][nt][0] = __fmaf_rn(s_a, d[0], raw[h][nt][0]);
+                  raw[h][nt][1] = __fmaf_rn(s_a, d[1], raw[h][nt][1]);
+                  raw[h][nt][2] = __fmaf_rn(s_b, d[2], raw[h][nt][2]);
+                  raw[h][nt][3] = __fmaf_rn(s_b, d[3], raw[h][nt][3]);
                 }
-                float d[4];
-                mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], 0.f, 0.f, 0.f, 0.f);
-                mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
-                raw[nt][0] = __fmaf_rn(s_a, d[0], raw[nt][0]);
-                raw[nt][1] = __fmaf_rn(s_a, d[1], raw[nt][1]);
-                raw[nt][2] = __fmaf_rn(s_b, d[2], raw[nt][2]);
-                raw[nt][3] = __fmaf_rn(s_b, d[3], raw[nt][3]);
               }
             }
           }
+          // in log2 units, less the maximum in use
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              z[h][nt][j] = __fmaf_rn(raw[h][nt][j], cm[nt][j & 1], -m[nt][j & 1]);
         }
-      }
-      // ---- scores in log2 units, less the maximum in use
+        // ---- what each query may see
+        if (!open) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[nt][j] = __fmaf_rn(raw[nt][j], cm[nt][j & 1], -m[nt][j & 1]);
-      // ---- what each query may see
-      const bool open = r0 + kSub - 1 <= w.rows.first && r0 >= low_max;
-      if (!open) {
+            for (int c = 0; c < 2; ++c) {
+              const int qr = min(8 * nt + 2 * t + c, w.used - 1) + w.tile * a.rows;
+              const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
+              const int low = a.window ? (int)plan_max(0, (int64_t)last + 1 - a.window) : 0;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+              for (int h = 0; h < J; ++h)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int qr = min(8 * nt + 2 * t + c, w.used - 1) + w.tile * a.rows;
-            const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
-            const int low = a.window ? (int)plan_max(0, (int64_t)last + 1 - a.window) : 0;
-#pragma unroll
-            for (int j = c; j < 4; j += 2) {
-              const int r = r0 + g + 8 * (j >> 1);
-              if (r > last || (r < low && r >= a.sink)) z[nt][j] = kHidden;
-            }
-          }
-      }
-      // ---- maxima, kept while no score passes them by kLazy
-      float past = kHidden;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          past = fmaxf(past, fmaxf(z[nt][c], z[nt][2 + c]));
-        }
-      if (__any_sync(0xffffffffu, past > kLazy)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            // (from the sums again: a first maximum is no difference to kNone)
-            const float z0 = z[nt][c] == kHidden ? kHidden : raw[nt][c] * cm[nt][c];
-            const float z1 = z[nt][2 + c] == kHidden ? kHidden : raw[nt][2 + c] * cm[nt][c];
-            float x = fmaxf(fmaxf(z0, z1), m[nt][c]);
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float by = m[nt][c] - x, f = exp2_fast(by);
-            m[nt][c] = x;
-            z[nt][c] = z0 == kHidden ? kHidden : z0 - x;
-            z[nt][2 + c] = z1 == kHidden ? kHidden : z1 - x;
-            if (STATS) {
-              top[nt][c] += by;
-              hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
-              sf[nt][c] *= f;
-            }
-            l[nt][c] *= f;
-#pragma unroll
-            for (int j = c; j < 4; j += 2) {
-              ox[nt][j] *= f;
-#pragma unroll
-              for (int gr = 0; gr < 4; ++gr)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) o[nt][gr][u][j] *= f;
-            }
-          }
-      }
-      // ---- weights: p0 = keys 2t, 2t+1 and p1 = keys 2t+8, 2t+9 of query row g
-      uint32_t p0[NT], p1[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = j & 1;
-          p[j] = exp2_fast(z[nt][j]);
-          l[nt][c] += p[j];
-          if (STATS) {
-            top[nt][c] = fmaxf(top[nt][c], z[nt][j]);
-            hs[nt][c] = __fmaf_rn(p[j], z[nt][j], hs[nt][c]);
-          }
-        }
-        if (STATS && r0 + kSub > suffix0) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (r0 + g + 8 * (j >> 1) >= suffix0) sf[nt][j & 1] += p[j];
-        }
-        p0[nt] = transposed(pack_bf16(p[0], p[1]));
-        p1[nt] = transposed(pack_bf16(p[2], p[3]));
-      }
-      // ---- results: this thread's keys
-      {
-        uint32_t xa, xb;
-        ldmatrix2_trans(xa, xb, v_at + at2);
-        if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
-          const int r = r0 + 2 * t, e = w.rows.last;
-          xa = finite_pair(xa, r <= e, r + 1 <= e);
-          xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma_bf16(ox[nt], xa, 0u, xb, 0u, p0[nt], p1[nt], ox[nt][0], ox[nt][1], ox[nt][2], ox[nt][3]);
-        const uint8_t *v0 = sv + 2 * t * C::kRow + D / 2;
-        const uint4 s0 = *(const uint4 *)v0, s1 = *(const uint4 *)(v0 + C::kRow);
-        const uint4 s2 = *(const uint4 *)(v0 + 8 * C::kRow), s3 = *(const uint4 *)(v0 + 9 * C::kRow);
-        const uint32_t sa[4] = {__byte_perm(s0.x, s1.x, 0x5410), __byte_perm(s0.y, s1.y, 0x5410),
-                                __byte_perm(s0.z, s1.z, 0x5410), __byte_perm(s0.w, s1.w, 0x5410)};
-        const uint32_t sb[4] = {__byte_perm(s2.x, s3.x, 0x5410), __byte_perm(s2.y, s3.y, 0x5410),
-                                __byte_perm(s2.z, s3.z, 0x5410), __byte_perm(s2.w, s3.w, 0x5410)};
-#pragma unroll
-        for (int j2 = 0; j2 < kPieces; j2 += 2) {
-          uint32_t vw[4];
-          ldmatrix4_trans(vw, v_at + at4 + 16 * j2);
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
-            const uint32_t fa[4] = {centred(wa & kLow, false), centred(wa & kHigh, true),
-                                    centred(ua & kLow, false), centred(ua & kHigh, true)};
-            const uint32_t fb[4] = {centred(wb & kLow, false), centred(wb & kHigh, true),
-                                    centred(ub & kLow, false), centred(ub & kHigh, true)};
-#pragma unroll
-            for (int gi = 0; gi < 4 / kPieces; ++gi) {
-              const int gr = (j2 + jj) * (4 / kPieces) + gi;
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                uint32_t b0 = mul_bf16x2(p0[nt], sa[gr]), b1 = mul_bf16x2(p1[nt], sb[gr]);
-                if (!open) {  // a weight of zero stays zero, whatever the scale holds
-                  b0 &= (p0[nt] & 0xffffu ? 0xffffu : 0u) | (p0[nt] >> 16 ? 0xffff0000u : 0u);
-                  b1 &= (p1[nt] & 0xffffu ? 0xffffu : 0u) | (p1[nt] >> 16 ? 0xffff0000u : 0u);
+                for (int j = c; j < 4; j += 2) {
+                  const int r = rh + 16 * h + g + 8 * (j >> 1);
+                  if (r > last || (r < low && r >= a.sink)) z[h][nt][j] = kHidden;
                 }
+            }
+        }
+        // ---- maxima, kept while no score passes them by kLazy
+        float past = kHidden;
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                  mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
-                           o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
+        for (int h = 0; h < J; ++h)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) past = fmaxf(past, z[h][nt][j]);
+        if (__any_sync(0xffffffffu, past > kLazy)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              // (from the sums again: a first maximum is no difference to kNone)
+              float x = m[nt][c];
+#pragma unroll
+              for (int h = 0; h < J; ++h)
+#pragma unroll
+                for (int j = c; j < 4; j += 2) {
+                  raw[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] * cm[nt][c];
+                  x = fmaxf(x, raw[h][nt][j]);
+                }
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+              const float by = m[nt][c] - x, f = exp2_fast(by);
+              m[nt][c] = x;
+#pragma unroll
+              for (int h = 0; h < J; ++h)
+#pragma unroll
+                for (int j = c; j < 4; j += 2)
+                  z[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] - x;
+              if (STATS) {
+                top[nt][c] += by;
+                hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
+                sf[nt][c] *= f;
+              }
+              l[nt][c] *= f;
+#pragma unroll
+              for (int j = c; j < 4; j += 2) {
+                ox[nt][j] *= f;
+#pragma unroll
+                for (int gr = 0; gr < 4; ++gr)
+#pragma unroll
+                  for (int u = 0; u < 2; ++u) o[nt][gr][u][j] *= f;
+              }
+            }
+        }
+        // ---- weights: p0 = keys 2t, 2t+1 and p1 = keys 2t+8, 2t+9 of query row g
+        uint32_t p0[J][NT], p1[J][NT];
+#pragma unroll
+        for (int h = 0; h < J; ++h)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float p[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int c = j & 1;
+              p[j] = exp2_fast(z[h][nt][j]);
+              l[nt][c] += p[j];
+              if (STATS) {
+                top[nt][c] = fmaxf(top[nt][c], z[h][nt][j]);
+                hs[nt][c] = __fmaf_rn(p[j], z[h][nt][j], hs[nt][c]);
+              }
+            }
+            if (STATS && r0 + kSub > suffix0) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (rh + 16 * h + g + 8 * (j >> 1) >= suffix0) sf[nt][j & 1] += p[j];
+            }
+            p0[h][nt] = transposed(pack_bf16(p[0], p[1]));
+            p1[h][nt] = transposed(pack_bf16(p[2], p[3]));
+          }
+        // ---- results: this thread's keys
+#pragma unroll
+        for (int h = 0; h < J; ++h) {
+          uint32_t xa, xb;  // half word g of the parameters of two keys: scales (g even) or least values
+          ldmatrix2_trans(xa, xb, v_at + at2 + h * 16 * C::kRow);
+          uint32_t sa[4], sb[4];
+#pragma unroll
+          for (int gr = 0; gr < 4; ++gr) {
+            sa[gr] = __shfl_sync(0xffffffffu, xa, 8 * gr + t);
+            sb[gr] = __shfl_sync(0xffffffffu, xb, 8 * gr + t);
+          }
+          if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
+            const int r = rh + 16 * h + 2 * t, e = w.rows.last;
+            xa = finite_pair(xa, r <= e, r + 1 <= e);
+            xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            mma_bf16(ox[nt], xa, 0u, xb, 0u, p0[h][nt], p1[h][nt], ox[nt][0], ox[nt][1], ox[nt][2], ox[nt][3]);
+#pragma unroll
+          for (int j2 = 0; j2 < kPieces; j2 += 2) {
+            uint32_t vw[4];
+            ldmatrix4_trans(vw, v_at + at4 + h * 16 * C::kRow + 16 * j2);
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+              const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
+              const uint32_t fa[4] = {centred(wa & kLow, false), centred(wa & kHigh, true),
+                                      centred(ua & kLow, false), centred(ua & kHigh, true)};
+              const uint32_t fb[4] = {centred(wb & kLow, false), centred(wb & kHigh, true),
+                                      centred(ub & kLow, false), centred(ub & kHigh, true)};
+#pragma unroll
+              for (int gi = 0; gi < 4 / kPieces; ++gi) {
+                const int gr = (j2 + jj) * (4 / kPieces) + gi;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  const uint32_t pa = p0[h][nt], pb = p1[h][nt];
+                  uint32_t b0 = mul_bf16x2(pa, sa[gr]), b1 = mul_bf16x2(pb, sb[gr]);
+                  if (!open) {  // a weight of zero stays zero, whatever the scale holds
+                    b0 &= (pa & 0xffffu ? 0xffffu : 0u) | (pa >> 16 ? 0xffff0000u : 0u);
+                    b1 &= (pb & 0xffffu ? 0xffffu : 0u) | (pb >> 16 ? 0xffff0000u : 0u);
+                  }
+#pragma unroll
+                  for (int u = 0; u < 2; ++u)
+                    mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
+                             o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
+                }
               }
             }
           }
@@ -497,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       }
     }
     __syncwarp();  // the stage has been read
-    if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages);
+    if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages, stage, bar);
     if (++st == C::kStages) {
       st = 0;
       phase ^= 1;
@@ -684,17 +713,17 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   int64_t blocks = ((int64_t)max_len + kBn - 1) / kBn;
   if (window)
     blocks = plan_min(blocks, ((int64_t)window + max_new + kBn - 2) / kBn + 1 + ((int64_t)sink + kBn - 1) / kBn);
-  // about two waves of the CTAs that the 152 SMs of a GB300 hold, as lengths differ; two blocks at
-  // least, as a CTA has its start and end to pay
-  const int64_t want = (int64_t)152 * (r.rows <= 16 ? 4 : 2) * 2;
+  // some waves of the CTAs that the 152 SMs of a GB300 hold, as lengths differ
+  const int64_t want = (int64_t)152 * (r.rows <= 8 ? 4 : r.rows <= 16 ? 3 : 2) * kWaves;
   int64_t per = (blocks * items + want - 1) / want;
-  if (per < 2) per = 2;
-  if (per > 64) per = 64;
+  if (per < 1) per = 1;
+  if (per > kMostBlocks) per = kMostBlocks;
   r.blocks = (int)per;
   r.chunks = (int)((blocks + per - 1) / per);
   // room for any division of as many blocks or fewer, so that a call with a window fits the workspace of
-  // one without: a CTA has two blocks and its share of `want` at least, or 64
-  const int64_t most = plan_max(plan_min((blocks + 1) / 2, (want + items - 1) / items), (blocks + 63) / 64);
+  // one without: a CTA has its share of `want` at least, or kMostBlocks
+  const int64_t most = plan_max(plan_min(blocks, (want + items - 1) / items),
+                                (blocks + kMostBlocks - 1) / kMostBlocks);
   r.part_bytes = ((size_t)items * most * r.rows * (d + 4) * sizeof(float) + 255) / 256 * 256;
   return r;
 }
