@@ -87,6 +87,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *(const uint32_t *)&h;
 }
 
+__device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmax2(__habs2(*(const __nv_bfloat162 *)&a), __habs2(*(const __nv_bfloat162 *)&b));
+  return *(const uint32_t *)&r;
+}
+
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 r = __hmul2(*(const __nv_bfloat162 *)&a, *(const __nv_bfloat162 *)&b);
   return *(const uint32_t *)&r;
@@ -152,13 +157,20 @@ struct Q4Item {
 };
 
 // item number -> what it is; false for one without queries, or a length out of bounds (recorded)
-__device__ __forceinline__ bool q4_item(const Q4AttendArgs &a, int64_t item, Q4Item &w) {
-  w.tile = (int)(item % a.tiles);
-  item /= a.tiles;
-  w.kvh = (int)(item % a.H_kv);
-  item /= a.H_kv;
-  w.b = (int)(item % a.batch);
-  w.layer = a.layer0 + (int)(item / a.batch);
+__device__ __forceinline__ bool q4_item(const Q4AttendArgs &a, unsigned item, Q4Item &w) {
+  w.tile = 0;
+  if (a.tiles > 1) {
+    w.tile = (int)(item % (unsigned)a.tiles);
+    item /= (unsigned)a.tiles;
+  }
+  w.kvh = (int)(item % (unsigned)a.H_kv);
+  item /= (unsigned)a.H_kv;
+  w.b = (int)item;
+  w.layer = a.layer0;
+  if (a.n_layers > 1) {
+    w.b = (int)(item % (unsigned)a.batch);
+    w.layer += (int)(item / (unsigned)a.batch);
+  }
   w.q.n = a.len[w.b];
   w.off = a.off ? a.off[w.b] : w.b;
   w.q.m = a.off ? a.off[w.b + 1] - w.off : (w.q.n > 0 ? 1 : 0);
@@ -194,8 +206,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   __syncwarp();
   pdl_enter();
   if (cta_status_bad(a.status)) return;
-  const int64_t item = blockIdx.x / a.chunks;
-  const int chunk = blockIdx.x % a.chunks;
+  const unsigned item = blockIdx.x / (unsigned)a.chunks;
+  const int chunk = (int)(blockIdx.x % (unsigned)a.chunks);
   Q4Item w;
   if (!q4_item(a, item, w)) {
     if (STATS && w.q.n == 0 && chunk == 0) {  // an empty sequence attends to nothing
@@ -244,15 +256,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   for (int nt = 0; nt < NT; ++nt) {
     const __nv_bfloat16 *src = q_row(8 * nt + g);
     uint4 v[kPieces];  // words t of the pieces: eight elements each
-    float big = 0.f;
+    uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
       v[j] = src ? *(const uint4 *)(src + 8 * (4 * j + t)) : make_uint4(0, 0, 0, 0);
-      const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        big = fmaxf(big, fmaxf(fabsf(bf16_low(x[i])), fabsf(bf16_high(x[i]))));
+      most = max_abs(max_abs(max_abs(most, v[j].x), max_abs(v[j].y, v[j].z)), v[j].w);
     }
+    float big = fmaxf(bf16_low(most), bf16_high(most));
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
     // the power of two of the largest, kept where 2^120 over it is a number
@@ -261,6 +271,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     const float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
     cm[nt][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
     cm[nt][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
+    const uint32_t up_even = pack_bf16(up, up), up_odd = pack_bf16(up * 0.0625f, up * 0.0625f);
     float mine = 0.f;
 #pragma unroll
     for (int gr = 0; gr < 4; ++gr) {
@@ -271,11 +282,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {  // pair i of a word; odd ones meet 16 c
-        const float lo = in ? bf16_low(x[i]) : 0.f, hi = in ? bf16_high(x[i]) : 0.f;
-        const float by = i & 1 ? up * 0.0625f : up;
-        f[i] = pack_bf16(lo * by, hi * by);
-        sum += lo + hi;
+        f[i] = in ? mul_bf16x2(x[i], i & 1 ? up_odd : up_even) : 0u;
+        sum += bf16_low(x[i]) + bf16_high(x[i]);
       }
+      sum = in ? sum : 0.f;
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       if (t == gr) mine = sum * (up * 0x1p-120f) * 0x1p-13f;
@@ -625,49 +635,85 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   }
 }
 
-// The CTAs' results of an item's row, a warp a row, four elements (two) a lane.
-template <int D, bool STATS>
-__global__ void __launch_bounds__(kThreads) q4_merge_kernel(Q4AttendArgs a) {
+// The CTAs' results of an item's row, W warps a row: the maximum of all parts first (a lane a part),
+// then their sums with nothing but additions between the loads, a warp every W-th part.
+constexpr int kMergeThreads = 256;
+constexpr int kMergeWarps = kMergeThreads / 32;
+
+template <int D, bool STATS, int W>
+__global__ void __launch_bounds__(kMergeThreads) q4_merge_kernel(Q4AttendArgs a) {
+  constexpr int kE = D / 32;
+  __shared__ float s_x[W == 1 ? 1 : W][D];
+  __shared__ float4 s_v[W == 1 ? 1 : W];
+  __shared__ float s_m[W];
   pdl_enter();
   if (cta_status_bad(a.status)) return;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int64_t item = row / a.rows;
-  const int r = (int)(row % a.rows);
-  if (item >= (int64_t)a.n_layers * a.batch * a.H_kv * a.tiles) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned row = W == 1 ? blockIdx.x * kMergeWarps + warp : blockIdx.x;
+  const unsigned item = row / (unsigned)a.rows;
+  const int r = (int)(row % (unsigned)a.rows);
+  if (item >= (unsigned)a.n_layers * a.batch * a.H_kv * a.tiles) return;
   Q4Item w;
   if (!q4_item(a, item, w)) return;
+  if (r >= w.used || w.blocks.count <= a.blocks) return;  // (W > 1: the same for the CTA)
   const int H_q = a.H_kv * a.g;
-  if (r >= w.used || w.blocks.count <= a.blocks) return;
   const int parts = (w.blocks.count + a.blocks - 1) / a.blocks;
-  float mx = kNone, sl = 0.f, sh = 0.f, ss = 0.f, x[D / 32] = {};
+  const int k0 = W == 1 ? 0 : warp;
+  float mx = kNone;
+  for (int c = k0 + W * lane; c < parts; c += 32 * W)
+    mx = fmaxf(mx, part_row<D>(a, item, c, r)[D]);
+  mx = warp_max(mx);
+  if constexpr (W > 1) {
+    if (lane == 0) s_m[warp] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < W; ++k) mx = fmaxf(mx, s_m[k]);
+  }
+  float sl = 0.f, sh = 0.f, ss = 0.f, x[kE] = {};
 #pragma unroll 4
-  for (int c = 0; c < parts; ++c) {
+  for (int c = k0; c < parts; c += W) {
     const float *part = part_row<D>(a, item, c, r);
     const float4 v = *(const float4 *)(part + D);
-    float y[D / 32];
+    float y[kE];
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) y[e] = part[lane + 32 * e];
-    if (v.y == 0.f) continue;
-    const float up = fmaxf(mx, v.x), by0 = mx - up, by1 = v.x - up;
-    const float f0 = exp2_fast(by0), f1 = exp2_fast(by1);
+    for (int e = 0; e < kE; ++e) y[e] = part[lane + 32 * e];
+    const bool any = v.y != 0.f;
+    const float by = v.x - mx, f = any ? exp2_fast(by) : 0.f;
+    sl += f * v.y;
     if (STATS) {
-      sh = (sl != 0.f ? f0 * __fmaf_rn(by0, sl, sh) : 0.f) + f1 * __fmaf_rn(by1, v.y, v.z);
-      ss = f0 * ss + f1 * v.w;
+      sh += any ? f * __fmaf_rn(by, v.y, v.z) : 0.f;
+      ss += f * v.w;
     }
-    sl = f0 * sl + f1 * v.y;
-    mx = up;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) x[e] = f0 * x[e] + f1 * y[e];
+    for (int e = 0; e < kE; ++e) x[e] += any ? f * y[e] : 0.f;
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) s_x[warp][lane + 32 * e] = x[e];
+    if (lane == 0) s_v[warp] = make_float4(0.f, sl, sh, ss);
+    __syncthreads();
+    if (warp >= kE) return;
+    sl = sh = ss = x[0] = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      sl += s_v[k].y;
+      sh += s_v[k].z;
+      ss += s_v[k].w;
+      x[0] += s_x[k][32 * warp + lane];
+    }
   }
   const float inv = sl != 0.f ? 1.f / sl : 0.f;
   const int rr = r + w.tile * a.rows;
   const int64_t head = (((int64_t)w.layer - a.layer0) * a.T + w.off + rr / a.g) * H_q +
                        w.kvh * a.g + rr % a.g;
+  __nv_bfloat16 *out = (__nv_bfloat16 *)a.out + head * D + lane;
+  if constexpr (W > 1) {
+    out[32 * warp] = __float2bfloat16_rn(x[0] * inv);
+  } else {
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
-    ((__nv_bfloat16 *)a.out)[head * D + lane + 32 * e] = __float2bfloat16_rn(x[e] * inv);
-  if (STATS && lane == 0)
+    for (int e = 0; e < kE; ++e) out[32 * e] = __float2bfloat16_rn(x[e] * inv);
+  }
+  if (STATS && lane == 0 && k0 == 0)
     ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
                                             logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
 }
@@ -694,8 +740,14 @@ cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
   }
   if (e != cudaSuccess) return e;
   if (a.chunks > 1) {
-    const int64_t ctas = (items * a.rows + kWarps - 1) / kWarps;
-    LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>, dim3((unsigned)ctas), kThreads, 0, s, a));
+    // a CTA a row where a row has many parts, a warp where not
+    const int64_t rows = items * a.rows;
+    if (a.chunks > 8)
+      LG_TRY(launch_pdl(q4_merge_kernel<D, STATS, kMergeWarps>, dim3((unsigned)rows), kMergeThreads, 0, s,
+                        a));
+    else
+      LG_TRY(launch_pdl(q4_merge_kernel<D, STATS, 1>,
+                        dim3((unsigned)((rows + kMergeWarps - 1) / kMergeWarps)), kMergeThreads, 0, s, a));
   }
   return cudaGetLastError();
 }
