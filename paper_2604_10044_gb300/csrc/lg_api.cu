@@ -103,7 +103,7 @@ AttendLayout attend_layout(const lg_cache *c, int H_q, int n_layers, int max_len
 }
 
 lg::Q4Grid q4_decode_grid(const lg_cache *c, int H_q, int n_layers, int max_len) {
-  return lg::q4_grid(n_layers, c->batch, c->H_kv, H_q / c->H_kv, c->d, 1, max_len, 0, 0);
+  return lg::q4_grid(n_layers, c->batch, c->H_kv, H_q / c->H_kv, c->d, 1, max_len);
 }
 
 // lg_decode_attend over a 4-bit cache
@@ -112,7 +112,7 @@ lg_status q4_decode_attend(const lg_cache *c, int layer0, int n_layers, const vo
                            size_t ws_bytes, cudaStream_t s) {
   const lg::Q4Grid grid = q4_decode_grid(c, H_q, n_layers, max_len);
   if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < grid.part_bytes) return LG_ERR_WORKSPACE;
-  if (!lg::q4_grid_fits(grid, n_layers, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
+  if (!lg::q4_grid_fits(n_layers, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
   lg::Q4AttendArgs a = {};
   a.q = q;
   a.out = out;

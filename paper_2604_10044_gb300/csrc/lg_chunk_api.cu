@@ -117,10 +117,9 @@ size_t q4_plane_bytes(const lg_cache *c) {
   return ((size_t)c->H_kv * c->S_total * c->d * 2 + 255) / 256 * 256;
 }
 
-// for any window: without one an item has the most key blocks
 size_t q4_chunk_bytes(const lg_cache *c, const lg_chunk *ch, int g, int max_len) {
   if (q4_few(ch, g)) {
-    const size_t n = lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, 0, 0).part_bytes;
+    const size_t n = lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len).part_bytes;
     return n > 256 ? n : 256;
   }
   return 2 * q4_plane_bytes(c) + part_bytes(lg::chunk_grid(LG_BF16, c->d, g, ch->max_new), c->d);
@@ -223,8 +222,8 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
     if (overlap(q, bytes, out, bytes)) return LG_ERR_INVALID_ARG;
     if (q4_few(ch, g)) {
       const lg::Q4Grid grid =
-          lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, window, n_sink);
-      if (!lg::q4_grid_fits(grid, 1, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
+          lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len);
+      if (!lg::q4_grid_fits(1, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
       lg::Q4AttendArgs a = {};
       a.q = q;
       a.out = out;
@@ -234,8 +233,8 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
       a.T = ch->T;
       a.max_new = ch->max_new;
       a.max_len = max_len;
-      a.window = window;
-      a.sink = n_sink;
+      a.shape.window = window;
+      a.shape.sink = n_sink;
       lg::q4_fill(a, *c, g, scale, grid, ws);
       return cuda_status(lg::launch_q4_attend(a, c->d, s));
     }

@@ -11,6 +11,7 @@
 
 #include "lg_common.cuh"
 #include "lg_internal.h"
+#include "lg_q4_plan.cuh"
 
 namespace lg {
 
@@ -110,31 +111,26 @@ struct Q4AttendArgs {
   const int32_t *len;
   const int32_t *off;      // nullable [batch + 1]; null: one token a sequence
   int32_t *status;
-  float *part;             // [items][chunks][rows][d + 4]
+  float *part;             // [n_layers][ctas][2][rows][d + 4]
   int64_t S_total;
   int layer0, n_layers, batch, H_kv, g, T, max_new, max_len;
-  int rows;                // query rows of an item
-  int tiles;               // items of a (layer, sequence, kv-head)
-  int chunks;              // CTAs of an item
-  int blocks;              // key blocks of a CTA
+  int ctas;                // of a layer
   int suffix_w;
-  int window, sink;
   float qscale;            // softmax scale * log2(e)
+  Q4Shape shape;
 };
 
 // how a call is divided, and the bytes of its partial results
 struct Q4Grid {
-  int rows, tiles, chunks, blocks;
+  int rows, ctas;
   size_t part_bytes;
 };
-Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,
-               int sink);
+Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len);
 cudaError_t launch_q4_attend(const Q4AttendArgs &a, int d, cudaStream_t s);
 
-// the kernels' grids fit their limit
-inline bool q4_grid_fits(const Q4Grid &g, int n_layers, int batch, int H_kv) {
-  const int64_t items = (int64_t)n_layers * batch * H_kv * g.tiles;
-  return items < (1 << 28) && items * g.chunks < ((int64_t)1 << 31);
+// the kernels' grids fit their limits
+inline bool q4_grid_fits(int n_layers, int batch, int H_kv) {
+  return n_layers <= 65535 && batch <= 65535 && H_kv <= 1 << 20;
 }
 
 // the arguments that both calls fill alike
@@ -148,12 +144,10 @@ inline void q4_fill(Q4AttendArgs &a, const lg_cache &c, int g, float scale, cons
   a.part = (float *)ws;
   a.S_total = c.S_total;
   a.batch = c.batch;
-  a.H_kv = c.H_kv;
-  a.g = g;
-  a.rows = grid.rows;
-  a.tiles = grid.tiles;
-  a.chunks = grid.chunks;
-  a.blocks = grid.blocks;
+  a.H_kv = a.shape.H_kv = c.H_kv;
+  a.g = a.shape.g = g;
+  a.shape.rows = grid.rows;
+  a.ctas = grid.ctas;
   a.qscale = scale * 1.4426950408889634f;
 }
 

@@ -30,7 +30,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "lg_chunk_plan.cuh"
+#include <type_traits>
+
 #include "lg_q4.cuh"
 
 namespace lg {
@@ -39,18 +40,11 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
-constexpr int kBn2 = 7;              // log2 of a CTA's block: kWarps tiles
-constexpr int kBn = 1 << kBn2;
-#ifndef Q4_WAVES
-#define Q4_WAVES 3
-#define Q4_MOST 16
-#endif
-constexpr int kWaves = Q4_WAVES;      // of CTAs in a call, while an item has the blocks
-constexpr int kMostBlocks = Q4_MOST;  // of a CTA
+constexpr int kBn2 = kQ4Bn2;         // a CTA's block: kWarps tiles
 constexpr float kLazy = 8.f;         // log2 units that a weight may pass 1 by
 constexpr float kHidden = -1e38f;    // score of a row that a query does not see
 constexpr float kNone = -1e30f;      // maximum of a query that has seen nothing
-static_assert(kWarps * kSub == kBn, "a tile a warp");
+static_assert(kWarps * kSub == 1 << kBn2, "a tile a warp");
 
 template <int D, int NT>
 struct Q4Cfg {
@@ -144,51 +138,108 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 
 // a partial result: [rows][D + 4], the sums and {m, l, sum p (z - m), suffix}; m the true maximum
 template <int D>
-__device__ __forceinline__ float *part_row(const Q4AttendArgs &a, int64_t item, int chunk, int r) {
-  return a.part + ((item * a.chunks + chunk) * a.rows + r) * (int64_t)(D + 4);
+__device__ __forceinline__ float *part_row(const Q4AttendArgs &a, int layer, int cta, int slot, int r) {
+  return a.part + (((int64_t)layer * a.ctas + cta) * 2 + slot) * a.shape.rows * (int64_t)(D + 4) +
+         r * (D + 4);
 }
 
-struct Q4Item {
-  int layer, b, kvh, tile, off;
-  ChunkSeq q;
-  TileRows rows;
-  TileBlocks blocks;
-  int used;  // query rows
-};
+// A sequence's numbers; false where they are out of bounds.  Without offsets every sequence that has
+// rows has one query, for its last.
+__device__ __forceinline__ bool q4_seq(const Q4AttendArgs &a, int b, ChunkSeq &q, int &off) {
+  q.n = a.len[b];
+  off = a.off ? a.off[b] : b;
+  q.m = a.off ? a.off[b + 1] - off : (q.n > 0 ? 1 : 0);
+  return q.n >= 0 && q.n <= a.max_len && q.m >= 0 && q.m <= a.max_new && q.m <= q.n && off >= 0 &&
+         off + q.m <= a.T;
+}
 
-// item number -> what it is; false for one without queries, or a length out of bounds (recorded)
-__device__ __forceinline__ bool q4_item(const Q4AttendArgs &a, unsigned item, Q4Item &w) {
-  w.tile = 0;
-  if (a.tiles > 1) {
-    w.tile = (int)(item % (unsigned)a.tiles);
-    item /= (unsigned)a.tiles;
+__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
   }
-  w.kvh = (int)(item % (unsigned)a.H_kv);
-  item /= (unsigned)a.H_kv;
-  w.b = (int)item;
-  w.layer = a.layer0;
-  if (a.n_layers > 1) {
-    w.b = (int)(item % (unsigned)a.batch);
-    w.layer += (int)(item / (unsigned)a.batch);
+  return v;
+}
+
+// The line's units W, and the sequence that CTA `cta`'s first unit falls into, with its start and its
+// numbers (nothing where the CTA's share starts at the end of the line).  False when a number is out of
+// bounds (recorded).  Every lane of a warp calls it; a batch of at most 32 is read once.
+struct Q4Line {
+  int64_t W, step;
+  int64_t x;
+  ChunkSeq q;
+  int b, off;
+};
+__device__ __forceinline__ bool q4_line(const Q4AttendArgs &a, int cta, Q4Line &f) {
+  const int lane = threadIdx.x & 31;
+  ChunkSeq q{0, 0};
+  int off = 0;
+  bool bad = false;
+  auto units = [&](int i) -> int64_t {
+    if (i >= a.batch) return 0;
+    if (!q4_seq(a, i, q, off)) {
+      bad = true;
+      return 0;
+    }
+    return q4_seq_units(q, a.shape);
+  };
+  f.x = 0;
+  f.b = 0;
+  const int64_t c0 = units(a.batch == 1 ? 0 : lane);
+  int64_t s0 = c0;
+  if (a.batch == 1) {  // nothing to search: the shortest call's latency is mostly this and its like
+    f.W = c0;
+  } else {
+    s0 = warp_scan(c0, lane);
+    f.W = __shfl_sync(0xffffffffu, s0, 31);
+    if (a.batch > 32) {
+      const ChunkSeq q0 = q;
+      const int off0 = off;
+      int64_t mine = 0;
+      for (int i = 32 + lane; i < a.batch; i += 32) mine += units(i);
+      f.W += __shfl_sync(0xffffffffu, warp_scan(mine, lane), 31);
+      q = q0;
+      off = off0;
+    }
   }
-  w.q.n = a.len[w.b];
-  w.off = a.off ? a.off[w.b] : w.b;
-  w.q.m = a.off ? a.off[w.b + 1] - w.off : (w.q.n > 0 ? 1 : 0);
-  if (w.q.n < 0 || w.q.n > a.max_len || w.q.m < 0 || w.q.m > a.max_new || w.q.m > w.q.n ||
-      w.off < 0 || w.off + w.q.m > a.T) {
+  if (__any_sync(0xffffffffu, bad)) {
     if (threadIdx.x == 0) set_status(a.status, LG_ERR_CAPACITY);
     return false;
   }
-  w.used = min(a.rows, w.q.m * a.g - w.tile * a.rows);
-  if (w.used <= 0) return false;
-  // the rows that its first and last query see
-  const int t0 = w.tile * a.rows / a.g, t1 = (w.tile * a.rows + w.used - 1) / a.g;
-  w.rows.first = w.q.n - w.q.m + t0;
-  w.rows.last = w.q.n - w.q.m + t1;
-  w.rows.lo = a.window ? (int)plan_max(0, (int64_t)w.rows.first + 1 - a.window) : 0;
-  w.rows.sinks = min(a.sink, w.rows.lo);
-  w.blocks = tile_blocks(w.rows, kBn2);
-  return true;
+  f.step = plan_max(1, plan_div(f.W + a.ctas - 1, a.ctas));
+  f.q = q;
+  f.off = off;
+  const int64_t y0 = cta * f.step;
+  if (a.batch == 1 || y0 >= f.W) return true;
+  for (int i0 = 0;; i0 += 32) {
+    const int64_t c = i0 ? units(i0 + lane) : c0;
+    const int64_t incl = i0 ? warp_scan(c, lane) : s0;
+    const unsigned past = __ballot_sync(0xffffffffu, f.x + incl > y0);
+    if (past) {
+      const int k = __ffs((int)past) - 1;
+      f.x += __shfl_sync(0xffffffffu, incl - c, k);
+      f.b = i0 + k;
+      f.q.n = __shfl_sync(0xffffffffu, q.n, k);
+      f.q.m = __shfl_sync(0xffffffffu, q.m, k);
+      f.off = __shfl_sync(0xffffffffu, off, k);
+      return true;
+    }
+    f.x += __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+
+// What the merge has to know of the item that a CTA's start cuts, written by that CTA if no earlier
+// start cuts the item.
+struct Q4Cut {
+  int64_t x0;    // the item's start in the line
+  int64_t step;  // 0: nothing to merge
+  int64_t head;  // its first query head's row in the outputs
+  int units, count, used, row_1;
+};
+__device__ __forceinline__ Q4Cut *cut_at(const Q4AttendArgs &a, int d, int layer, int cta) {
+  return (Q4Cut *)(a.part + (int64_t)a.n_layers * a.ctas * 2 * a.shape.rows * (d + 4)) +
+         (int64_t)layer * a.ctas + cta;
 }
 
 template <int D, int NT, bool STATS>
@@ -206,23 +257,61 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   __syncwarp();
   pdl_enter();
   if (cta_status_bad(a.status)) return;
-  const unsigned item = blockIdx.x / (unsigned)a.chunks;
-  const int chunk = (int)(blockIdx.x % (unsigned)a.chunks);
-  Q4Item w;
-  if (!q4_item(a, item, w)) {
-    if (STATS && w.q.n == 0 && chunk == 0) {  // an empty sequence attends to nothing
-      const int64_t head = (((int64_t)w.layer - a.layer0) * a.T + w.off) * a.H_kv * a.g + w.kvh * a.g;
-      for (int e = tid; e < a.g * D / 2; e += kThreads) ((uint32_t *)a.out)[head * D / 2 + e] = 0u;
-      if (tid < a.g) ((float4 *)a.stats)[head + tid] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-    }
+  const int layer = blockIdx.y, cta = blockIdx.x;  // (layer of the call)
+  const int H_q = a.H_kv * a.g;
+  float *s_o = (float *)smem;  // [warp][row][D + 1], the warps' results
+  __shared__ float4 s_st[kWarps][8 * NT];
+  Q4Line line;
+  if (!q4_line(a, cta, line)) return;
+  const int64_t y0 = cta * line.step, y1 = plan_min(y0 + line.step, line.W);
+  if (y0 >= y1) {
+    if (tid == 0) cut_at(a, D, layer, cta)->step = 0;
     return;
   }
-  const int blk0 = chunk * a.blocks, blk1 = min(blk0 + a.blocks, w.blocks.count);
-  if (blk0 >= blk1) return;
-
-  // this warp's copies: its rows of each block
+  struct {
+    ChunkSeq q;
+    TileRows rows;
+    TileBlocks blocks;
+    int kvh, tile, off, used;
+  } w;
+  int seq = line.b;
+  int64_t x = line.x;  // the item's start
+  w.q = line.q;
+  w.off = line.off;
+  int units = q4_units(w.q, a.shape), tiles = q4_tiles(w.q, a.shape);
+  {
+    const int64_t k = plan_div(y0 - x, units);
+    x += k * units;
+    w.kvh = (int)plan_div(k, tiles);
+    w.tile = (int)(k - (int64_t)w.kvh * tiles);
+  }
+  if (tid == 0) {
+    Q4Cut c = {};
+    if (x < y0 && y0 - line.step <= x) {
+      const TileRows rows = q4_rows(w.q, a.shape, w.tile, c.used);
+      c.x0 = x;
+      c.step = line.step;
+      c.head = ((int64_t)layer * a.T + w.off) * H_q + w.kvh * a.g;
+      c.units = units;
+      c.count = tile_blocks(rows, kBn2).count;
+      c.row_1 = w.tile * a.shape.rows;
+    }
+    *cut_at(a, D, layer, cta) = c;
+  }
+  // this lane's row and 16-byte piece of an ldmatrix of four, and its row of one of two
+  const uint32_t at4 = (lane & 15) * C::kRow + 16 * (lane >> 4);
+  const uint32_t at2 = (lane & 15) * C::kRow + D / 2;
   uint8_t *ring = smem + warp * C::kStages * 2 * C::kTile;
-  const int64_t row0 = ((int64_t)w.layer * a.H_kv + w.kvh) * a.S_total + a.seq_off[w.b];
+  int st = 0, phase = 0;  // of the next block to be read: they go on over the pieces
+  bool gave_up = false;
+
+  for (; x < y1 && !gave_up; x += units) {
+  w.rows = q4_rows(w.q, a.shape, w.tile, w.used);
+  w.blocks = tile_blocks(w.rows, kBn2);
+  const int blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
+  if (blk0 < blk1) {
+  // this warp's copies: its rows of each block
+  const int64_t row0 = ((int64_t)(a.layer0 + layer) * a.H_kv + w.kvh) * a.S_total + a.seq_off[seq];
   const uint8_t *gk = a.K + row0 * C::kRow, *gv = a.V + row0 * C::kRow;
   auto tile_row = [&](int i) { return (w.blocks.index(i) << kBn2) + warp * kSub; };
   auto copy = [&](int i, uint8_t *to, uint64_t *bar) {  // lane 0: block i into a stage
@@ -236,17 +325,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     bulk_load(to + C::kTile, gv + from, bytes, bar);
   };
   if (lane == 0)
-    for (int k = 0; k < C::kStages && blk0 + k < blk1; ++k)
-      copy(blk0 + k, ring + k * 2 * C::kTile, &s_full[warp][k]);
+    for (int k = 0, to = st; k < C::kStages && blk0 + k < blk1; ++k) {
+      copy(blk0 + k, ring + to * 2 * C::kTile, &s_full[warp][to]);
+      if (++to == C::kStages) to = 0;
+    }
 
   // q as second operands, and its groups' sums in two terms for the least values
-  const int H_q = a.H_kv * a.g;
   const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q +
-                           (((int64_t)w.layer - a.layer0) * a.T + w.off) * H_q * D +
-                           (int64_t)w.kvh * a.g * D;
+                           ((int64_t)layer * a.T + w.off) * H_q * D + (int64_t)w.kvh * a.g * D;
+  const int row_1 = w.tile * a.shape.rows;  // the tile's first query row
   auto q_row = [&](int r) {  // row r of the item, or null
-    r += w.tile * a.rows;
-    return r < w.tile * a.rows + w.used ? q + ((int64_t)(r / a.g) * H_q + r % a.g) * D : nullptr;
+    r += row_1;
+    return r < row_1 + w.used ? q + ((int64_t)(r / a.g) * H_q + r % a.g) * D : nullptr;
   };
   uint32_t qf[NT <= 2 ? NT : 1][4][4];
   uint4 *s_q = (uint4 *)(smem + C::kSmem - C::kQ);
@@ -302,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
   }
   if constexpr (NT > 2) __syncthreads();
 
-  const int low_max = a.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.window) : 0;
+  const int low_max = a.shape.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.shape.window) : 0;
   const int suffix0 = w.q.n - a.suffix_w;  // (n and suffix_w are positive)
 
   float o[NT][4][2][4] = {};
@@ -316,13 +406,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
       l[nt][c] = hs[nt][c] = sf[nt][c] = 0.f;
     }
 
-  // this lane's row and 16-byte piece of an ldmatrix of four, and its row of one of two
-  const uint32_t at4 = (lane & 15) * C::kRow + 16 * (lane >> 4);
-  const uint32_t at2 = (lane & 15) * C::kRow + D / 2;
-
   constexpr int J = C::kJoint;
-  bool gave_up = false;
-  int st = 0, phase = 0;
   for (int i = blk0; i < blk1; ++i) {
     const int r0 = tile_row(i);
     uint8_t *stage = ring + st * 2 * C::kTile;
@@ -332,9 +416,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
         gave_up = true;
         break;
       }
-      const bool open = r0 + kSub - 1 <= w.rows.first && r0 >= low_max;
-#pragma unroll 1
-      for (int h0 = 0; h0 < kSub / 16; h0 += J) {
+      // `open`: every query sees every row (and, for the statistics, none is in the suffix)
+      auto tile = [&](auto open_tile, int h0) {
+        constexpr bool open = decltype(open_tile)::value;
         const uint8_t *sk = stage + h0 * 16 * C::kRow;
         const uint32_t k_at = smem_addr(sk), v_at = k_at + C::kTile;
         const int rh = r0 + 16 * h0;
@@ -398,15 +482,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const int qr = min(8 * nt + 2 * t + c, w.used - 1) + w.tile * a.rows;
+              const int qr = min(8 * nt + 2 * t + c, w.used - 1) + row_1;
               const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
-              const int low = a.window ? (int)plan_max(0, (int64_t)last + 1 - a.window) : 0;
+              const int low = a.shape.window ? (int)plan_max(0, (int64_t)last + 1 - a.shape.window) : 0;
 #pragma unroll
               for (int h = 0; h < J; ++h)
 #pragma unroll
                 for (int j = c; j < 4; j += 2) {
                   const int r = rh + 16 * h + g + 8 * (j >> 1);
-                  if (r > last || (r < low && r >= a.sink)) z[h][nt][j] = kHidden;
+                  if (r > last || (r < low && r >= a.shape.sink)) z[h][nt][j] = kHidden;
                 }
             }
         }
@@ -475,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
                 hs[nt][c] = __fmaf_rn(p[j], z[h][nt][j], hs[nt][c]);
               }
             }
-            if (STATS && r0 + kSub > suffix0) {
+            if (STATS && !open) {
 #pragma unroll
               for (int j = 0; j < 4; ++j)
                 if (rh + 16 * h + g + 8 * (j >> 1) >= suffix0) sf[nt][j & 1] += p[j];
@@ -533,13 +617,20 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
             }
           }
         }
+      };
+      if (r0 + kSub - 1 <= w.rows.first && r0 >= low_max && (!STATS || r0 + kSub <= suffix0)) {
+#pragma unroll 1
+        for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::true_type(), h0);
+      } else {
+#pragma unroll 1
+        for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::false_type(), h0);
       }
-    }
-    __syncwarp();  // the stage has been read
-    if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages, stage, bar);
-    if (++st == C::kStages) {
-      st = 0;
-      phase ^= 1;
+      __syncwarp();  // the stage has been read
+      if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages, stage, bar);
+      if (++st == C::kStages) {
+        st = 0;
+        phase ^= 1;
+      }
     }
   }
   if (gave_up && lane == 0) {
@@ -547,11 +638,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     linger();
   }
   // every warp's copies have landed (or lingered): the ring becomes the results' place
-  __syncthreads();
+  gave_up = __syncthreads_or(gave_up);
 
   // ---- the warps' results: sums of a query row over the key lanes, then over the warps
-  float *s_o = (float *)smem;                     // [warp][row][D + 1]
-  __shared__ float4 s_st[kWarps][8 * NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -591,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
     }
   }
   __syncthreads();
-  const bool alone = a.chunks == 1 || (chunk == 0 && w.blocks.count <= a.blocks);
+  const bool alone = blk0 == 0 && blk1 == w.blocks.count;
   for (int r = warp; r < w.used; r += kWarps) {
     float mx = kNone;
 #pragma unroll
@@ -608,10 +697,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
         ss += f[k] * v.w;
       }
     }
-    const int rr = r + w.tile * a.rows;
-    const int64_t head = (((int64_t)w.layer - a.layer0) * a.T + w.off + rr / a.g) * H_q +
-                         w.kvh * a.g + rr % a.g;
-    float *part = part_row<D>(a, item, chunk, r);
+    const int rr = r + row_1;
+    const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
+    float *part = part_row<D>(a, layer, cta, x < y0 ? 0 : 1, r);
     const float inv = sl != 0.f ? 1.f / sl : 0.f;
 #pragma unroll
     for (int e = lane; e < D; e += 32) {
@@ -633,46 +721,80 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_at
                         logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
     }
   }
+  fence_proxy_async_smem();
+  __syncthreads();  // the results have been read: the ring is the next piece's
+  }
+  // the next item
+  if (++w.tile == tiles) {
+    w.tile = 0;
+    if (++w.kvh == a.H_kv) {
+      w.kvh = 0;
+      if (x + units >= y1) break;
+      do q4_seq(a, ++seq, w.q, w.off);
+      while (w.q.m == 0);
+      // (x is the old sequence's last item: the loop adds its units)
+      x += units;
+      units = q4_units(w.q, a.shape);
+      x -= units;
+      tiles = q4_tiles(w.q, a.shape);
+    }
+  }
+  }
 }
 
-// The CTAs' results of an item's row, W warps a row: the maximum of all parts first (a lane a part),
-// then their sums with nothing but additions between the loads, a warp every W-th part.
-constexpr int kMergeThreads = 256;
-constexpr int kMergeWarps = kMergeThreads / 32;
+// The CTAs' results of a row of a cut item, a CTA a row (blockIdx = (row, the CTA whose start cuts it,
+// layer)): the maximum of all parts first, a lane a part, then their sums with nothing but additions
+// between the loads, a warp every fourth part.
+constexpr int kMergeWarps = 4;
 
-template <int D, bool STATS, int W>
-__global__ void __launch_bounds__(kMergeThreads) q4_merge_kernel(Q4AttendArgs a) {
+template <int D, bool STATS>
+__global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs a) {
   constexpr int kE = D / 32;
-  __shared__ float s_x[W == 1 ? 1 : W][D];
-  __shared__ float4 s_v[W == 1 ? 1 : W];
-  __shared__ float s_m[W];
+  __shared__ float s_x[kMergeWarps][D];
+  __shared__ float4 s_v[kMergeWarps];
+  __shared__ float s_m[kMergeWarps];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x, layer = blockIdx.z;
   pdl_enter();
-  if (cta_status_bad(a.status)) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const unsigned row = W == 1 ? blockIdx.x * kMergeWarps + warp : blockIdx.x;
-  const unsigned item = row / (unsigned)a.rows;
-  const int r = (int)(row % (unsigned)a.rows);
-  if (item >= (unsigned)a.n_layers * a.batch * a.H_kv * a.tiles) return;
-  Q4Item w;
-  if (!q4_item(a, item, w)) return;
-  if (r >= w.used || w.blocks.count <= a.blocks) return;  // (W > 1: the same for the CTA)
-  const int H_q = a.H_kv * a.g;
-  const int parts = (w.blocks.count + a.blocks - 1) / a.blocks;
-  const int k0 = W == 1 ? 0 : warp;
-  float mx = kNone;
-  for (int c = k0 + W * lane; c < parts; c += 32 * W)
-    mx = fmaxf(mx, part_row<D>(a, item, c, r)[D]);
-  mx = warp_max(mx);
-  if constexpr (W > 1) {
-    if (lane == 0) s_m[warp] = mx;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < W; ++k) mx = fmaxf(mx, s_m[k]);
+  const Q4Cut w = *cut_at(a, D, layer, blockIdx.y);
+  if (tid == 0) s_bad = status_bad(a.status);
+  __syncthreads();
+  if (s_bad) return;
+  if (STATS && r == 0) {  // empty sequences attend to nothing
+    const int H_q = a.H_kv * a.g;
+    for (int b = blockIdx.y; b < a.batch; b += a.ctas) {
+      if (a.len[b] != 0) continue;
+      const int64_t head = ((int64_t)layer * a.T + b) * H_q;
+      for (int e = tid; e < H_q * D / 2; e += 32 * kMergeWarps) ((uint32_t *)a.out)[head * D / 2 + e] = 0u;
+      for (int h = tid; h < H_q; h += 32 * kMergeWarps)
+        ((float4 *)a.stats)[head + h] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    }
   }
+  if (w.step == 0 || r >= w.used) return;
+  const int c0 = blockIdx.y - 1;  // the CTA that the item began in
+  auto cut = [&](int c) { return q4_cut(c * w.step - w.x0, w.count); };  // blocks before CTA c
+  // one part has every block and wrote the result: the first that has any, then
+  int some = c0 + 1;
+  while (cut(some) == 0) ++some;
+  if (cut(some) == w.count) return;
+  int parts = 1;
+  for (int64_t y = (c0 + 1) * w.step; y < w.x0 + w.units; y += w.step) ++parts;
+  auto part_of = [&](int k) { return part_row<D>(a, layer, c0 + k, k == 0, r); };
+  auto has = [&](int k) { return cut(c0 + k) < cut(c0 + k + 1); };
+  float mx = kNone;
+  for (int c = tid; c < parts; c += 32 * kMergeWarps)
+    if (has(c)) mx = fmaxf(mx, part_of(c)[D]);
+  mx = warp_max(mx);
+  if (lane == 0) s_m[warp] = mx;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kMergeWarps; ++k) mx = fmaxf(mx, s_m[k]);
   float sl = 0.f, sh = 0.f, ss = 0.f, x[kE] = {};
 #pragma unroll 4
-  for (int c = k0; c < parts; c += W) {
-    const float *part = part_row<D>(a, item, c, r);
+  for (int c = warp; c < parts; c += kMergeWarps) {
+    if (!has(c)) continue;
+    const float *part = part_of(c);
     const float4 v = *(const float4 *)(part + D);
     float y[kE];
 #pragma unroll
@@ -687,96 +809,64 @@ __global__ void __launch_bounds__(kMergeThreads) q4_merge_kernel(Q4AttendArgs a)
 #pragma unroll
     for (int e = 0; e < kE; ++e) x[e] += any ? f * y[e] : 0.f;
   }
-  if constexpr (W > 1) {
 #pragma unroll
-    for (int e = 0; e < kE; ++e) s_x[warp][lane + 32 * e] = x[e];
-    if (lane == 0) s_v[warp] = make_float4(0.f, sl, sh, ss);
-    __syncthreads();
-    if (warp >= kE) return;
-    sl = sh = ss = x[0] = 0.f;
+  for (int e = 0; e < kE; ++e) s_x[warp][lane + 32 * e] = x[e];
+  if (lane == 0) s_v[warp] = make_float4(0.f, sl, sh, ss);
+  __syncthreads();
+  if (warp >= kE) return;
+  sl = sh = ss = x[0] = 0.f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      sl += s_v[k].y;
-      sh += s_v[k].z;
-      ss += s_v[k].w;
-      x[0] += s_x[k][32 * warp + lane];
-    }
+  for (int k = 0; k < kMergeWarps; ++k) {
+    sl += s_v[k].y;
+    sh += s_v[k].z;
+    ss += s_v[k].w;
+    x[0] += s_x[k][32 * warp + lane];
   }
   const float inv = sl != 0.f ? 1.f / sl : 0.f;
-  const int rr = r + w.tile * a.rows;
-  const int64_t head = (((int64_t)w.layer - a.layer0) * a.T + w.off + rr / a.g) * H_q +
-                       w.kvh * a.g + rr % a.g;
-  __nv_bfloat16 *out = (__nv_bfloat16 *)a.out + head * D + lane;
-  if constexpr (W > 1) {
-    out[32 * warp] = __float2bfloat16_rn(x[0] * inv);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kE; ++e) out[32 * e] = __float2bfloat16_rn(x[e] * inv);
-  }
-  if (STATS && lane == 0 && k0 == 0)
+  const int rr = r + w.row_1, H_q = a.H_kv * a.g;
+  const int64_t head = w.head + (int64_t)(rr / a.g) * H_q + rr % a.g;
+  ((__nv_bfloat16 *)a.out)[head * D + 32 * warp + lane] = __float2bfloat16_rn(x[0] * inv);
+  if (STATS && tid == 0)
     ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
                                             logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
 }
 
 template <int D, int NT, bool STATS>
-cudaError_t launch_nt(const Q4AttendArgs &a, int64_t items, cudaStream_t s) {
+cudaError_t launch_nt(const Q4AttendArgs &a, cudaStream_t s) {
   using C = Q4Cfg<D, NT>;
   LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-  LG_TRY(launch_pdl(q4_attend_kernel<D, NT, STATS>, dim3((unsigned)(items * a.chunks)), kThreads,
-                    C::kSmem, s, a));
+  LG_TRY(launch_pdl(q4_attend_kernel<D, NT, STATS>, dim3(a.ctas, a.n_layers), kThreads, C::kSmem, s, a));
   return cudaGetLastError();
 }
 
 template <int D, bool STATS>
 cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
-  const int64_t items = (int64_t)a.n_layers * a.batch * a.H_kv * a.tiles;
-  cudaError_t e = cudaSuccess;
-  switch (a.rows) {
-    case 8: e = launch_nt<D, 1, STATS>(a, items, s); break;
-    case 16: if constexpr (!STATS) e = launch_nt<D, 2, STATS>(a, items, s); break;
-    case 24: if constexpr (!STATS) e = launch_nt<D, 3, STATS>(a, items, s); break;
-    default: if constexpr (!STATS) e = launch_nt<D, 4, STATS>(a, items, s); break;
+  switch (a.shape.rows) {
+    case 8: LG_TRY((launch_nt<D, 1, STATS>(a, s))); break;
+    case 16: if constexpr (!STATS) LG_TRY((launch_nt<D, 2, STATS>(a, s))); break;
+    case 24: if constexpr (!STATS) LG_TRY((launch_nt<D, 3, STATS>(a, s))); break;
+    default: if constexpr (!STATS) LG_TRY((launch_nt<D, 4, STATS>(a, s))); break;
   }
-  if (e != cudaSuccess) return e;
-  if (a.chunks > 1) {
-    // a CTA a row where a row has many parts, a warp where not
-    const int64_t rows = items * a.rows;
-    if (a.chunks > 8)
-      LG_TRY(launch_pdl(q4_merge_kernel<D, STATS, kMergeWarps>, dim3((unsigned)rows), kMergeThreads, 0, s,
-                        a));
-    else
-      LG_TRY(launch_pdl(q4_merge_kernel<D, STATS, 1>,
-                        dim3((unsigned)((rows + kMergeWarps - 1) / kMergeWarps)), kMergeThreads, 0, s, a));
-  }
+  LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>, dim3(a.shape.rows, a.ctas, a.n_layers), 32 * kMergeWarps, 0,
+                    s, a));
   return cudaGetLastError();
 }
 
 }  // namespace
 
-Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,
-               int sink) {
+Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len) {
   Q4Grid r;
   const int64_t rows = (int64_t)max_new * g;
   r.rows = rows >= 32 ? 32 : (int)((rows + 7) / 8 * 8);
-  r.tiles = (int)((rows + r.rows - 1) / r.rows);
-  const int64_t items = (int64_t)n_layers * batch * H_kv * r.tiles;
-  // key blocks that an item can have: all rows, or the sinks and a window
-  int64_t blocks = ((int64_t)max_len + kBn - 1) / kBn;
-  if (window)
-    blocks = plan_min(blocks, ((int64_t)window + max_new + kBn - 2) / kBn + 1 + ((int64_t)sink + kBn - 1) / kBn);
-  // some waves of the CTAs that the 152 SMs of a GB300 hold, as lengths differ
-  const int64_t want = (int64_t)152 * (r.rows <= 8 ? 4 : r.rows <= 16 ? 3 : 2) * kWaves;
-  int64_t per = (blocks * items + want - 1) / want;
-  if (per < 1) per = 1;
-  if (per > kMostBlocks) per = kMostBlocks;
-  r.blocks = (int)per;
-  r.chunks = (int)((blocks + per - 1) / per);
-  // room for any division of as many blocks or fewer, so that a call with a window fits the workspace of
-  // one without: a CTA has its share of `want` at least, or kMostBlocks
-  const int64_t most = plan_max(plan_min(blocks, (want + items - 1) / items),
-                                (blocks + kMostBlocks - 1) / kMostBlocks);
-  r.part_bytes = ((size_t)items * most * r.rows * (d + 4) * sizeof(float) + 255) / 256 * 256;
+  const int64_t tiles = (rows + r.rows - 1) / r.rows;
+  const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
+  // what the 152 SMs of a GB300 hold at once, over the layers; no more than there are blocks
+  const int64_t fit = 152 * (r.rows <= 8 ? 4 : r.rows <= 16 ? 3 : 2);
+  const int64_t most = batch * H_kv * tiles * (blocks + kQ4ItemUnits);
+  r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
+  r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
+  r.part_bytes = (r.part_bytes + 255) / 256 * 256;
   return r;
 }
 
