@@ -30,8 +30,8 @@ LG_API size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch);
    target's logits after token tokens[t] of sequence b; for j < m_b - 1 the draft of what follows is
    y = tokens[t + 1].  With temperature tau_b:
      p_t(i) = exp((x_t(i) - max x_t) / tau_b) / sum of the same; for tau_b = 0 (and what is not above
-              2^-100, or NaN) one for the lowest token with the largest logit; for tau_b > 2^100 as
-              for 2^100.  A NaN counts as -infinity; the mass of a row with infinite logits is shared
+              2^-60, or NaN) one for the lowest token with the largest logit; for tau_b > 2^40 as for
+              2^40.  A NaN counts as -infinity; the mass of a row with infinite logits is shared
               evenly among those; a row with nothing left has p = 0
      q_t(i)   the probability that the draft gave i: row t of `draft` (an entry that is not above zero
               counts as zero), or, without `draft`, one for i = y and zero elsewhere

@@ -29,11 +29,37 @@ struct Q4AppendArgs {
   int guard;     // the layer whose V rows are sketched, -1: none
   int groups;    // threads that share a token's heads: every groups-th head each
   int tok;       // tokens a CTA
+  int parts;     // CTAs that share a token's heads
   int T;
 };
 
 constexpr int kQ4Threads = 256;
 constexpr int kQ4Tokens = 64;  // tokens a CTA at most
+constexpr int kQ4Together = 4; // heads of a thread in flight
+
+// token_slots in one round trip where a lane can hold a sequence
+__device__ __forceinline__ void token_slots_near(const lg_cache &c, const lg_chunk &ch, int t0, int n,
+                                                 int64_t *s_slot) {
+  const int lane = threadIdx.x & 31;
+  if (c.batch < 32) {
+    const bool mine = lane < c.batch;
+    const int at = lane <= c.batch ? ch.off[lane] : 0x7fffffff;
+    const int len = mine ? c.len[lane] : 0, cap = mine ? c.cap[lane] : 0;
+    const int64_t seq = mine ? c.seq_off[lane] : 0;
+    for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) {
+      const int t = t0 + i;
+      const unsigned below = __ballot_sync(0xffffffffu, mine && at <= t);
+      const int b = below ? 31 - __clz((int)below) : 0;  // the last sequence that starts at or before t
+      const int end = __shfl_sync(0xffffffffu, at, b + 1);
+      const int64_t row = (int64_t)__shfl_sync(0xffffffffu, len, b) - end + t;
+      const bool in = below && t < ch.T && end > t && row >= 0 && row < __shfl_sync(0xffffffffu, cap, b);
+      const int64_t slot = __shfl_sync(0xffffffffu, seq, b) + row;
+      if (lane == 0) s_slot[i] = in ? slot : -1;
+    }
+    return;
+  }
+  token_slots(c, ch, t0, n, s_slot);
+}
 
 // ONE: token t is the one new row of sequence t, and blockIdx.y the layer
 template <int D, bool ONE>
@@ -41,9 +67,10 @@ __global__ void __launch_bounds__(kQ4Threads)
     q4_append_kernel(lg_cache c, lg_chunk ch, Q4AppendArgs a, const __grid_constant__ RopeTable tab) {
   constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
   __shared__ int64_t s_slot[kQ4Tokens];
+  __shared__ int s_bad;
   // no early trigger: the loop-onset test reads sketches before its own wait
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (cta_status_bad(c.dev_status)) return;
+  if (threadIdx.x == 0) s_bad = status_bad(c.dev_status);
   const int t0 = blockIdx.x * a.tok;
   const int layer = a.layer + (ONE ? (int)blockIdx.y : 0);
   if constexpr (ONE) {
@@ -52,19 +79,20 @@ __global__ void __launch_bounds__(kQ4Threads)
       int64_t slot = -1;
       if (b < c.batch) {
         const int n = c.len[b];
-        if (n > 0)
-          slot = c.seq_off[b] + n - 1;
-        else
-          set_status(c.dev_status, LG_ERR_CAPACITY);
+        const int64_t at = c.seq_off[b];
+        if (n > 0) slot = at + n - 1;
+        else set_status(c.dev_status, LG_ERR_CAPACITY);
       }
       s_slot[i] = slot;
     }
   } else {
-    token_slots(c, ch, t0, a.tok, s_slot);
+    token_slots_near(c, ch, t0, a.tok, s_slot);
   }
   __syncthreads();
+  if (s_bad) return;
   const int pc = threadIdx.x % kLanes;
-  const int unit = threadIdx.x / kLanes, i = unit / a.groups, grp = unit % a.groups;
+  const int unit = threadIdx.x / kLanes, i = unit / a.groups;
+  const int groups = a.groups * a.parts, grp = blockIdx.z * a.groups + unit % a.groups;
   const int t = t0 + i;
   const int64_t slot = i < a.tok && t < a.T ? s_slot[i] : -1;
   const bool live = slot >= 0;
@@ -90,59 +118,68 @@ __global__ void __launch_bounds__(kQ4Threads)
   const int64_t layer_row = (int64_t)layer * c.H_kv * c.S_total;
   const int64_t in = ONE ? (int64_t)blockIdx.y * c.batch + t : t;  // token row of the inputs
   const int h1 = a.H_q + c.H_kv, h2 = h1 + c.H_kv;
-  // every lane of a warp makes the same number of turns, as the groups' shuffles need them all
-  const int turns = (h2 + a.groups - 1) / a.groups;
-  for (int n = 0; n < turns; ++n) {
-    const int h = grp + n * a.groups;
-    const bool mine = live && h < h2;
-    const bool isq = h < a.H_q, isk = !isq && h < h1;
-    float x[8];
-    uint4 raw = make_uint4(0, 0, 0, 0), far;
-    if (mine) {
-      const __nv_bfloat16 *src = isq   ? a.q + in * a.q_stride + (int64_t)h * D
-                                 : isk ? a.k + in * a.k_stride + (int64_t)(h - a.H_q) * D
-                                       : a.v + in * a.v_stride + (int64_t)(h - h1) * D;
-      raw = *(const uint4 *)(src + 8 * pc);
-    }
-    if (half_lay && a.rot) {  // the other elements of its pairs
-      far.x = __shfl_sync(0xffffffffu, raw.x, other);
-      far.y = __shfl_sync(0xffffffffu, raw.y, other);
-      far.z = __shfl_sync(0xffffffffu, raw.z, other);
-      far.w = __shfl_sync(0xffffffffu, raw.w, other);
-    } else {
-      far = raw;
-    }
-    if (mine && (isq || isk)) {
-      if (turned) {
-        float2 f[4], g[4];
-        Elem<__nv_bfloat16>::unpack(raw, f);
-        Elem<__nv_bfloat16>::unpack(far, g);
-        uint32_t r[4];
+  // Every lane of a warp makes the same number of turns, as the shuffles need them all; the pieces of
+  // kQ4Together heads are requested before the first is worked on.
+  const int turns = (h2 + groups - 1) / groups;
+  for (int n0 = 0; n0 < turns; n0 += kQ4Together) {
+    uint4 in4[kQ4Together];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float gx = half_lay ? g[e].x : g[e].y, gy = half_lay ? g[e].y : g[e].x;
-          const __nv_bfloat162 y =
-              __floats2bfloat162_rn(__fmaf_rn(f[e].x, co[2 * e], gx * si[2 * e]),
-                                    __fmaf_rn(f[e].y, co[2 * e + 1], gy * si[2 * e + 1]));
-          r[e] = *(const uint32_t *)&y;
-        }
-        raw = make_uint4(r[0], r[1], r[2], r[3]);
-      }
-      if (isq) *(uint4 *)(a.q_out + ((int64_t)t * a.H_q + h) * D + 8 * pc) = raw;
+    for (int k = 0; k < kQ4Together; ++k) {
+      const int h = grp + (n0 + k) * groups;
+      in4[k] = make_uint4(0, 0, 0, 0);
+      if (!live || h >= h2) continue;
+      const __nv_bfloat16 *src = h < a.H_q ? a.q + in * a.q_stride + (int64_t)h * D
+                                 : h < h1  ? a.k + in * a.k_stride + (int64_t)(h - a.H_q) * D
+                                           : a.v + in * a.v_stride + (int64_t)(h - h1) * D;
+      in4[k] = *(const uint4 *)(src + 8 * pc);
     }
-    if (__all_sync(0xffffffffu, !mine || isq)) continue;
-    Elem<__nv_bfloat16>::unpack(raw, (float2 *)x);
-    uint32_t par;
-    const uint32_t word = q4_encode<kGroup>(x, par);
-    if (!mine || isq) continue;
-    const int kvh = isk ? h - a.H_q : h - h1;
-    uint8_t *row = (uint8_t *)(isk ? c.k : c.v) +
-                   (layer_row + kvh * c.S_total + slot) * (int64_t)kRow;
-    ((uint32_t *)row)[pc] = word;
-    if (pc % kGroup == 0) ((uint32_t *)row)[kLanes + pc / kGroup] = par;
-    if (!isk && layer == a.guard)  // signs of the values as they came
-      ((uint8_t *)c.sketch)[slot * (c.H_kv * D / 8) + kvh * kLanes + pc] =
-          (uint8_t)Elem<__nv_bfloat16>::signs(raw);
+#pragma unroll
+    for (int k = 0; k < kQ4Together; ++k) {
+      if (n0 + k >= turns) break;
+      const int h = grp + (n0 + k) * groups;
+      const bool mine = live && h < h2;
+      const bool isq = h < a.H_q, isk = !isq && h < h1;
+      uint4 raw = in4[k];
+      if (__any_sync(0xffffffffu, h < h1) && a.rot) {
+        uint4 far = raw;
+        if (half_lay) {  // the other elements of its pairs
+          far.x = __shfl_sync(0xffffffffu, raw.x, other);
+          far.y = __shfl_sync(0xffffffffu, raw.y, other);
+          far.z = __shfl_sync(0xffffffffu, raw.z, other);
+          far.w = __shfl_sync(0xffffffffu, raw.w, other);
+        }
+        if (h < h1 && turned) {
+          float2 f[4], g[4];
+          Elem<__nv_bfloat16>::unpack(raw, f);
+          Elem<__nv_bfloat16>::unpack(far, g);
+          uint32_t r[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 o = half_lay ? g[e] : make_float2(g[e].y, g[e].x);
+            const float2 y = __ffma2_rn(f[e], make_float2(co[2 * e], co[2 * e + 1]),
+                                        __fmul2_rn(o, make_float2(si[2 * e], si[2 * e + 1])));
+            const __nv_bfloat162 p = __floats2bfloat162_rn(y.x, y.y);
+            r[e] = *(const uint32_t *)&p;
+          }
+          raw = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+      }
+      if (mine && isq) *(uint4 *)(a.q_out + ((int64_t)t * a.H_q + h) * D + 8 * pc) = raw;
+      if (__all_sync(0xffffffffu, !mine || isq)) continue;
+      float x[8];
+      Elem<__nv_bfloat16>::unpack(raw, (float2 *)x);
+      uint32_t par;
+      const uint32_t word = q4_encode<kGroup>(x, par);
+      if (!mine || isq) continue;
+      const int kvh = isk ? h - a.H_q : h - h1;
+      uint8_t *row = (uint8_t *)(isk ? c.k : c.v) +
+                     (layer_row + kvh * c.S_total + slot) * (int64_t)kRow;
+      ((uint32_t *)row)[pc] = word;
+      if (pc % kGroup == 0) ((uint32_t *)row)[kLanes + pc / kGroup] = par;
+      if (!isk && layer == a.guard)  // signs of the values as they came
+        ((uint8_t *)c.sketch)[slot * (c.H_kv * D / 8) + kvh * kLanes + pc] =
+            (uint8_t)Elem<__nv_bfloat16>::signs(raw);
+    }
   }
 }
 
@@ -151,14 +188,18 @@ cudaError_t launch_append_d(const lg_cache &c, const lg_chunk *ch, Q4AppendArgs 
                             const RopeTable &tab, cudaStream_t s) {
   constexpr int kLanes = D / 8;
   const int heads = a.H_q + 2 * c.H_kv;
-  // as many heads a thread, for its cosines and sines to serve, as leave the GPU four CTAs an SM
+  // as many heads a thread, for its cosines and sines to serve, as leave the GPU four CTAs an SM; a few
+  // tokens' heads over several CTAs
   const int64_t full = (int64_t)4 * 152 * kQ4Threads;
   a.groups = 1;
   while (a.groups * 2 <= kQ4Threads / kLanes && a.groups < heads &&
          (int64_t)a.T * n_layers * a.groups * kLanes < full)
     a.groups *= 2;
   a.tok = kQ4Threads / kLanes / a.groups;
-  const dim3 grid((a.T + a.tok - 1) / a.tok, n_layers);
+  const int64_t ctas = (int64_t)((a.T + a.tok - 1) / a.tok) * n_layers;
+  a.parts = 1;
+  while (a.parts * a.groups < heads && ctas * a.parts < 2 * 152) a.parts *= 2;
+  const dim3 grid((a.T + a.tok - 1) / a.tok, n_layers, a.parts);
   if (ch)
     LG_TRY(launch_pdl(q4_append_kernel<D, false>, grid, kQ4Threads, 0, s, c, *ch, a, tab));
   else
@@ -180,11 +221,13 @@ __global__ void __launch_bounds__(kQ4Threads)
     q4_read_kernel(lg_cache c, lg_chunk ch, Q4ReadArgs a) {
   constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
   __shared__ int64_t s_slot[kQ4Tokens];
+  __shared__ int s_bad;
   pdl_enter();
-  if (cta_status_bad(c.dev_status)) return;
+  if (threadIdx.x == 0) s_bad = status_bad(c.dev_status);
   const int t0 = blockIdx.x * a.tok;
-  token_slots(c, ch, t0, a.tok, s_slot);
+  token_slots_near(c, ch, t0, a.tok, s_slot);
   __syncthreads();
+  if (s_bad) return;
   const int units = c.H_kv * kLanes;
   for (int u = threadIdx.x; u < a.tok * units; u += kQ4Threads) {
     const int i = u / units, x = u - i * units, h = x / kLanes, pc = x % kLanes;

@@ -40,14 +40,17 @@ struct RowPart {     // of a slice of a row
   uint64_t z;        // sum of exp((x - m) / temperature) in 2^-40
 };
 
-// log2(e) / temperature in two terms; a temperature of zero (or nothing above it) takes the top token
+// log2(e) / temperature in two terms, the second times ln 2; a temperature of zero (or nothing above it)
+// takes the top token.  Temperatures are kept in [2^-60, 2^40] and distances from the maximum above -2^60,
+// so every product is a number and what is further down, or masked, weighs nothing.
 struct Heat {
   float hi, lo;
   bool greedy;
 };
+constexpr float kFar = -0x1p60f;
 
 __device__ __forceinline__ float clamp_temperature(float t) {
-  return t > 0x1p-100f ? fminf(t, 0x1p100f) : 0.f;
+  return t > 0x1p-60f ? fminf(t, 0x1p40f) : 0.f;
 }
 
 __device__ __forceinline__ Heat heat_of(float t) {
@@ -56,18 +59,22 @@ __device__ __forceinline__ Heat heat_of(float t) {
   const double e = 1.4426950408889634;
   const float e_hi = (float)e, e_lo = (float)(e - (double)e_hi);
   h.hi = __fdiv_rn(e_hi, t);
-  h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t);
+  h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t) * 0.6931471805599453f;
   return h;
 }
 
-// exp((x - m) / temperature), within some 2^-22 and without a drift over the range; the maximum
-// itself is 1 also where it is infinite
-__device__ __forceinline__ float weight(float x, float m, const Heat &h) {
-  const float d = x == m ? 0.f : x - m;
-  const float y = d * h.hi;
-  const float rest = __fmaf_rn(d, h.hi, -y) + d * h.lo;
-  const float e = exp2_fast(y);
-  return y > -126.f ? __fmaf_rn(e, rest * 0.6931471805599453f, e) : 0.f;
+// exp(d / temperature) of two distances d = x - m from a finite maximum, within some 2^-22 and without a
+// drift over the range: 2^y (1 + rest), y the product with the first term
+__device__ __forceinline__ float2 weights(float2 d, const Heat &h) {
+  d.x = fmaxf(d.x, kFar);
+  d.y = fmaxf(d.y, kFar);
+  const float2 hi = make_float2(h.hi, h.hi);
+  const float2 y = __fmul2_rn(d, hi);
+  float2 rest = __ffma2_rn(d, hi, make_float2(-y.x, -y.y));
+  rest = __ffma2_rn(rest, make_float2(0.6931471805599453f, 0.6931471805599453f),
+                    __fmul2_rn(d, make_float2(h.lo, h.lo)));
+  const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+  return __ffma2_rn(e, rest, e);
 }
 
 template <typename T>
@@ -117,9 +124,10 @@ __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) 
   }
 #pragma unroll
   for (int e = 0; e < kN; ++e) {
-    v[e] = v[e] == v[e] ? v[e] : -INFINITY;
+    v[e] = fmaxf(v[e], -INFINITY);  // a NaN counts as masked
     m = fmaxf(m, v[e]);
   }
+  const float own = m;
   const float wm = warp_max(m);
   if (lane == 0) s_m[warp] = wm;
   __syncthreads();
@@ -128,17 +136,27 @@ __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) 
 #pragma unroll
   for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, s_m[w]);
   const Heat h = heat_of(t);
-  float sum = 0.f;
-  int at = 0x7fffffff;
+  float2 sums = make_float2(0.f, 0.f);
+  if (m == INFINITY) {
 #pragma unroll
-  for (int e = 0; e < kN; ++e) {
-    if (!h.greedy) sum += weight(v[e], m, h);
-    if (v[e] == m) {
-      const int i = ((blockIdx.x * kRowVecs + e / kVec) * kRowThreads + tid) * kVec - head + e % kVec;
-      at = min(at, i);
+    for (int e = 0; e < kN; ++e) sums.x += v[e] == m ? 1.f : 0.f;
+  } else if (!h.greedy && m != -INFINITY) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+      const float2 w = weights(make_float2(v[e] - m, v[e + 1] - m), h);
+      sums.x += w.x;
+      sums.y += w.y;
     }
   }
-  uint64_t z = m == -INFINITY ? 0 : __float2ull_rn(sum * 0x1p40f);
+  const float sum = sums.x + sums.y;
+  int at = 0x7fffffff;
+  if (own == m) {
+#pragma unroll
+    for (int e = kN - 1; e >= 0; --e)
+      if (v[e] == m)
+        at = ((blockIdx.x * kRowVecs + e / kVec) * kRowThreads + tid) * kVec - head + e % kVec;
+  }
+  uint64_t z = __float2ull_rn(sum * 0x1p40f);
 #pragma unroll
   for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
   at = __reduce_min_sync(0xffffffffu, at);
@@ -162,6 +180,7 @@ constexpr int kPickThreads = 512;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kSeg = 16;             // elements a lane and segment
 constexpr int kSegElems = 32 * kSeg;
+constexpr int kRowsKept = 64;        // rows of a sequence that are joined once
 constexpr float kUnit = 0x1p62f;     // a mass of one
 
 struct Row {
@@ -199,44 +218,44 @@ __device__ __forceinline__ float draft_at(const VerifyArgs &a, int64_t row, int 
   return q > 0.f ? q : 0.f;
 }
 
+struct Part {      // of the vocabulary, a CTA's
+  uint64_t total;
+  int bad;         // the device status
+};
+
 template <typename T, typename Q>
-__global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a) {
+__global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs a) {
   cg::cluster_group cl = cg::this_cluster();
   const int n_cta = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int b = blockIdx.x / n_cta;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ uint64_t s_total;                // of this CTA's part of the vocabulary
+  __shared__ Part s_part;
   __shared__ uint64_t s_warp[kPickWarps];
   __shared__ int s_first, s_bad;
-  __shared__ Row s_row;
+  __shared__ Row s_row, s_rows[kRowsKept];
   pdl_enter();
-  // one decision for the cluster (its CTAs meet at barriers): the first CTA's
-  if (rank == 0 && tid == 0) s_bad = status_bad(a.status);
+  if (tid == 0) s_bad = status_bad(a.status);
   const int o0 = a.off[b], o1 = a.off[b + 1], m = o1 - o0, V = a.x.V;
-  cl.sync();
-  const bool wrong = o0 < 0 || m < 0 || m > a.max_new || o1 > a.T;
-  const bool bad = *cl.map_shared_rank(&s_bad, 0) != 0;
-  cl.sync();  // read before the first CTA may end
-  if (bad) return;
-  if (wrong) {
+  const float t = clamp_temperature(a.temp ? a.temp[b] : 1.f);
+  const float rnd = a.r[b];
+  if (o0 < 0 || m < 0 || m > a.max_new || o1 > a.T) {  // (the same for the cluster)
     if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
     return;
   }
-  if (m == 0) {
-    if (rank == 0 && tid == 0) a.accepted[b] = 0;
-    return;
-  }
-  const float t = clamp_temperature(a.temp ? a.temp[b] : 1.f);
-  const Heat h = heat_of(t);
-  if (tid == 0) s_first = m - 1;
+  if (tid == 0) s_first = max(m - 1, 0);
   __syncthreads();
+  const Heat h = heat_of(t);
+  // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have read
+  // another one
+  const bool bad = s_bad != 0;
   // the first draft that does not stand: a warp a row
-  for (int j = warp; j < m - 1; j += kPickWarps) {
+  for (int j = warp; j < m && !bad; j += kPickWarps) {
     const int64_t row = o0 + j;
-    const int y = a.tokens[row + 1];
     const Row r = join_row(a, row, t, lane);
     if (lane == 0) {
-      bool stands = false;
+      if (j < kRowsKept) s_rows[j] = r;
+      bool stands = j == m - 1;
+      const int y = stands ? -1 : a.tokens[row + 1];
       if (y >= 0 && y < V && r.z > 0.0) {
         const float q = a.has_draft ? draft_at<Q>(a, row, y) : 1.f;
         const float x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
@@ -253,98 +272,125 @@ __global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a)
   __syncthreads();
   const int first = s_first;
   const int64_t row = o0 + first;
-  if (warp == 0) {
-    const Row r = join_row(a, row, t, lane);
-    if (lane == 0) s_row = r;
+  Row r{-INFINITY, 0x7fffffff, 0.0};
+  if (m > 0 && !bad) {
+    if (first < kRowsKept) {
+      r = s_rows[first];
+    } else {
+      if (warp == 0) {
+        const Row j = join_row(a, row, t, lane);
+        if (lane == 0) s_row = j;
+      }
+      __syncthreads();
+      r = s_row;
+    }
   }
-  __syncthreads();
-  const Row r = s_row;
-  const int fallen = first < m - 1 ? a.tokens[row + 1] : -1;
+  const bool fell = first < m - 1;
+  const int fallen = fell && !bad ? a.tokens[row + 1] : -1;
   // the distribution of the next token, p less what the draft had of it
   const T *x = (const T *)a.x.x + row * a.x.stride;
+  const Q *dq = a.has_draft && fell && fallen >= 0 && fallen < V
+                    ? (const Q *)a.draft.x + row * a.draft.stride
+                    : nullptr;
   const double inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
   const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
-  bool less = first < m - 1;
-  auto mass = [&](int i) -> uint64_t {  // of token i in 2^-62
-    float q = 0.f;
-    if (less) q = a.has_draft ? (fallen >= 0 && fallen < V ? draft_at<Q>(a, row, i) : 0.f)
-                              : (i == fallen ? 2.f : 0.f);
-    float w;
-    if (h.greedy) {
-      w = i == r.at ? 1.f - q : 0.f;
-    } else {
-      const float e = weight(logit<T>(x, i), r.m, h);
-      w = __fmaf_rn(e, inv_hi, __fmaf_rn(e, inv_lo, -q));
-    }
-    return w > 0.f ? __float2ull_rn(fminf(w, 1.f) * kUnit) : 0;
-  };
-  // whole segments a warp, in order over the cluster's warps
-  const int segs = (V + kSegElems - 1) / kSegElems;
-  const int per = (segs + n_cta * kPickWarps - 1) / (n_cta * kPickWarps);
-  const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
-  auto segment = [&](int g) {  // a lane's share: elements lane, lane + 32, ..
-    uint64_t s = 0;
-    const int base = g * kSegElems + lane;
+  bool less = fell && (dq || !a.has_draft);
+  // the masses of a lane's elements i0, i0 + 32, .. of a segment in 2^-62, all of them loaded first
+  auto masses = [&](int i0, uint64_t (&w)[kSeg]) {
+    float v[kSeg], q[kSeg];
 #pragma unroll
-    for (int k = 0; k < kSeg; ++k)
-      if (base + 32 * k < V) s += mass(base + 32 * k);
-    return s;
+    for (int k = 0; k < kSeg; ++k) v[k] = i0 + 32 * k < V ? Elem<T>::load(x, i0 + 32 * k) : -INFINITY;
+    if (less && dq) {
+#pragma unroll
+      for (int k = 0; k < kSeg; ++k) q[k] = i0 + 32 * k < V ? Elem<Q>::load(dq, i0 + 32 * k) : 0.f;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSeg; ++k) q[k] = less && i0 + 32 * k == fallen ? 2.f : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kSeg; k += 2) {
+      float2 e;
+      if (r.m == INFINITY) {
+        e = make_float2(v[k] == r.m ? 1.f : 0.f, v[k + 1] == r.m ? 1.f : 0.f);
+      } else {  // (a NaN's distance counts as far, like a masked one's)
+        e = weights(make_float2(v[k] - r.m, v[k + 1] - r.m), h);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float ec = c ? e.y : e.x, qc = fmaxf(q[k + c], 0.f);
+        const float p = __fmaf_rn(ec, inv_hi, __fmaf_rn(ec, inv_lo, -qc));
+        w[k + c] = __float2ull_rn(fminf(fmaxf(p, 0.f), 1.f) * kUnit);
+      }
+    }
   };
   auto warp_sum = [&](uint64_t s) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     return s;
   };
+  // whole segments a warp, in order over the cluster's warps
+  const int segs = (V + kSegElems - 1) / kSegElems;
+  const int per = (segs + n_cta * kPickWarps - 1) / (n_cta * kPickWarps);
+  const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
+  const bool look = m > 0 && !bad && !h.greedy && r.z > 0.0;  // (the top token needs no search)
   uint64_t total = 0, before = 0;
   for (int pass = 0; pass < 2; ++pass) {  // a second one where the draft leaves nothing: p itself
     uint64_t s = 0;
-    if (r.z > 0.0)
-      for (int g = g0; g < g1; ++g) s += segment(g);
+    if (look)
+      for (int g = g0; g < g1; ++g) {
+        uint64_t w[kSeg];
+        masses(g * kSegElems + lane, w);
+#pragma unroll
+        for (int k = 0; k < kSeg; ++k) s += w[k];
+      }
     s = warp_sum(s);
     if (lane == 0) s_warp[warp] = s;
     __syncthreads();
     if (tid == 0) {
       uint64_t sum = 0;
       for (int w = 0; w < kPickWarps; ++w) sum += s_warp[w];
-      s_total = sum;
+      s_part = Part{sum, bad};
     }
     cl.sync();
     total = before = 0;
+    bool stop = false;
     for (int c = 0; c < n_cta; ++c) {
-      const uint64_t v = *cl.map_shared_rank(&s_total, c);
-      if (c < rank) before += v;
-      total += v;
+      const Part v = *cl.map_shared_rank(&s_part, c);
+      if (c < rank) before += v.total;
+      total += v.total;
+      stop |= v.bad != 0;
     }
     cl.sync();  // read by all before it is written again, or its CTA ends
-    if (total || !less) break;
+    if (stop) return;
+    if (total || !less || !look) break;
     less = false;
   }
   // the lowest token whose sum passes r of the total
-  const float rnd = a.r[b];
   uint64_t want = rnd > 0.f ? (rnd < 1.f ? __double2ull_rd((double)rnd * (double)total) : total) : 0;
   if (want >= total) want = total ? total - 1 : 0;
   for (int w = 0; w < warp; ++w) before += s_warp[w];
   if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
     int token = -1;
     for (int g = g0; g < g1; ++g) {
-      const uint64_t s = warp_sum(segment(g));
+      uint64_t w[kSeg], s = 0;
+      masses(g * kSegElems + lane, w);
+#pragma unroll
+      for (int k = 0; k < kSeg; ++k) s += w[k];
+      s = warp_sum(s);
       if (want >= before + s) {
         before += s;
         continue;
       }
+#pragma unroll
       for (int k = 0; k < kSeg; ++k) {
-        const int i = g * kSegElems + 32 * k + lane;
-        uint64_t c = i < V ? mass(i) : 0;
+        uint64_t c = w[k];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const uint64_t u = __shfl_up_sync(0xffffffffu, c, o);
           if (lane >= o) c += u;
         }
         const unsigned over = __ballot_sync(0xffffffffu, before + c > want);
-        if (over) {
-          token = g * kSegElems + 32 * k + __ffs((int)over) - 1;
-          break;
-        }
+        if (over && token < 0) token = g * kSegElems + 32 * k + __ffs((int)over) - 1;
         before += __shfl_sync(0xffffffffu, c, 31);
       }
       break;
@@ -354,7 +400,7 @@ __global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a)
   if (rank == 0) {
     if (tid == 0) {
       a.accepted[b] = first;
-      if (total == 0) a.picked[row] = -1;
+      if (m > 0 && total == 0) a.picked[row] = h.greedy && r.z > 0.0 ? r.at : -1;
     }
     for (int j = tid; j < m; j += kPickThreads)
       if (j != first) a.picked[o0 + j] = j < first ? a.tokens[o0 + j + 1] : -1;

@@ -187,13 +187,13 @@ def verify(x, ms, tokens, draft, temp, u, r):
             p = torch.zeros(V, dtype=torch.float64)
             if top == -math.inf:
                 return p
-            if not tau > 2.0 ** -100:
+            if not tau > 2.0 ** -60:
                 p[int(torch.nonzero(z == top)[0])] = 1.0
                 return p
             if top == math.inf:
                 e = (z == top).double()
             else:
-                e = ((z - top) / min(tau, 2.0 ** 100)).exp()
+                e = ((z - top) / min(tau, 2.0 ** 40)).exp()
                 e[z == -math.inf] = 0.0
             return e / e.sum()
 
