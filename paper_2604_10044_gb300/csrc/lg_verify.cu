@@ -16,6 +16,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "lg_common.cuh"
 #include "lg_internal.h"
 #include "lg_rope.cuh"
@@ -180,8 +182,8 @@ constexpr int kPickThreads = 512;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kSeg = 16;             // elements a lane and segment
 constexpr int kSegElems = 32 * kSeg;
+constexpr int kSegsKept = 32;        // sums of a warp's segments that are kept
 constexpr int kRowsKept = 64;        // rows of a sequence that are joined once
-constexpr float kUnit = 0x1p62f;     // a mass of one
 
 struct Row {
   float m;    // largest logit
@@ -189,8 +191,27 @@ struct Row {
   double z;   // sum of exp((x - m) / temperature); 0: nothing is left
 };
 
-// a row's slices joined; every lane of a warp calls it
-__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, float t, int lane) {
+// 2^y, y <= 0, in 64 bits within 2^-40: the whole part into the exponent, the power series of the rest
+// (2^f = sum of (f ln 2)^k / k!, |f| <= 1/2, to k = 10)
+__device__ __forceinline__ double power_of_two(double y) {
+  if (!(y > -1000.0)) return 0.0;
+  const double whole = rint(y), f = (y - whole) * 0.6931471805599453;
+  double p = 1.0 / 3628800.0;
+  p = fma(p, f, 1.0 / 362880.0);
+  p = fma(p, f, 1.0 / 40320.0);
+  p = fma(p, f, 1.0 / 5040.0);
+  p = fma(p, f, 1.0 / 720.0);
+  p = fma(p, f, 1.0 / 120.0);
+  p = fma(p, f, 1.0 / 24.0);
+  p = fma(p, f, 1.0 / 6.0);
+  p = fma(p, f, 0.5);
+  p = fma(p, f, 1.0);
+  p = fma(p, f, 1.0);
+  return p * __hiloint2double(((int)whole + 1023) << 20, 0);
+}
+
+// a row's slices joined; every lane of a warp calls it.  heat: log2(e) / temperature, 0 for the top token
+__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double heat, int lane) {
   const RowPart *p = a.part + row * a.slices;
   Row r{-INFINITY, 0x7fffffff, 0.0};
   for (int i = lane; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
@@ -199,15 +220,14 @@ __device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, float 
   for (int i = lane; i < a.slices; i += 32) {
     const RowPart s = p[i];
     if (s.m == r.m) r.at = min(r.at, s.at);
-    if (t > 0.f && s.z) {
-      const double d = s.m == r.m ? 0.0 : ((double)s.m - (double)r.m) / (double)t;
-      r.z += (double)s.z * 0x1p-40 * (d == 0.0 ? 1.0 : exp(d));
-    }
+    if (heat > 0.0 && s.z)
+      r.z += (double)s.z * 0x1p-40 *
+             (s.m == r.m ? 1.0 : power_of_two(((double)s.m - (double)r.m) * heat));
   }
   r.at = __reduce_min_sync(0xffffffffu, r.at);
 #pragma unroll
   for (int o = 16; o; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
-  if (!(t > 0.f)) r.z = 1.0;
+  if (!(heat > 0.0)) r.z = 1.0;
   return r;
 }
 
@@ -216,6 +236,14 @@ template <typename Q>
 __device__ __forceinline__ float draft_at(const VerifyArgs &a, int64_t row, int i) {
   const float q = Elem<Q>::load((const Q *)a.draft.x + row * a.draft.stride, i);
   return q > 0.f ? q : 0.f;
+}
+
+// a mass of [0, 1] in 2^-62, its last bits cut off below 2^-39 (by shifts: the conversion instruction for 64
+// bits took most of this kernel's time)
+__device__ __forceinline__ uint64_t units_of(float w) {
+  const uint32_t bits = __float_as_uint(w), mant = (bits & 0x7fffffu) | 0x800000u;
+  const int sh = (int)(bits >> 23) - (127 - 39);
+  return sh >= 0 ? (uint64_t)mant << sh : (uint64_t)(mant >> min(-sh, 31));
 }
 
 struct Part {      // of the vocabulary, a CTA's
@@ -230,8 +258,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int b = blockIdx.x / n_cta;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __shared__ Part s_part;
-  __shared__ uint64_t s_warp[kPickWarps];
+  __shared__ uint64_t s_warp[kPickWarps], s_seg[kPickWarps][kSegsKept];
   __shared__ int s_first, s_bad;
+  __shared__ double s_heat, s_inv;
   __shared__ Row s_row, s_rows[kRowsKept];
   pdl_enter();
   if (tid == 0) s_bad = status_bad(a.status);
@@ -242,16 +271,20 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
     return;
   }
-  if (tid == 0) s_first = max(m - 1, 0);
+  if (tid == 0) {
+    s_first = max(m - 1, 0);
+    s_heat = t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
+  }
   __syncthreads();
   const Heat h = heat_of(t);
+  const double heat = s_heat;
   // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have read
   // another one
   const bool bad = s_bad != 0;
   // the first draft that does not stand: a warp a row
   for (int j = warp; j < m && !bad; j += kPickWarps) {
     const int64_t row = o0 + j;
-    const Row r = join_row(a, row, t, lane);
+    const Row r = join_row(a, row, heat, lane);
     if (lane == 0) {
       if (j < kRowsKept) s_rows[j] = r;
       bool stands = j == m - 1;
@@ -263,7 +296,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
         if (h.greedy)
           e = y == r.at ? 1.0 : 0.0;
         else
-          e = x == r.m ? 1.0 : exp(((double)x - (double)r.m) / (double)t);
+          e = x == r.m ? 1.0 : power_of_two(((double)x - (double)r.m) * heat);
         stands = (double)a.u[row] * (double)q * r.z < e;
       }
       if (!stands) atomicMin(&s_first, j);
@@ -278,7 +311,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       r = s_rows[first];
     } else {
       if (warp == 0) {
-        const Row j = join_row(a, row, t, lane);
+        const Row j = join_row(a, row, heat, lane);
         if (lane == 0) s_row = j;
       }
       __syncthreads();
@@ -292,36 +325,53 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const Q *dq = a.has_draft && fell && fallen >= 0 && fallen < V
                     ? (const Q *)a.draft.x + row * a.draft.stride
                     : nullptr;
-  const double inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
+  if (tid == 0) s_inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
+  __syncthreads();
+  const double inv = s_inv;
   const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
-  bool less = fell && (dq || !a.has_draft);
-  // the masses of a lane's elements i0, i0 + 32, .. of a segment in 2^-62, all of them loaded first
-  auto masses = [&](int i0, uint64_t (&w)[kSeg]) {
-    float v[kSeg], q[kSeg];
+  // what is taken off p: nothing, the draft's row, or all of the fallen token
+  enum { kNothing, kRow, kToken };
+  int less = !fell ? kNothing : dq ? kRow : a.has_draft ? kNothing : kToken;
+  // the masses of a lane's elements i0, i0 + 32, .. of a segment in 2^-62, all of them loaded first (from
+  // the last place on where the row ends: their masses are zeros)
+  auto masses_of = [&](auto kind, int i0, uint64_t (&w)[kSeg]) {
+    constexpr int kKind = decltype(kind)::value;
+    T v[kSeg];
+    Q q[kSeg];
 #pragma unroll
-    for (int k = 0; k < kSeg; ++k) v[k] = i0 + 32 * k < V ? Elem<T>::load(x, i0 + 32 * k) : -INFINITY;
-    if (less && dq) {
+    for (int k = 0; k < kSeg; ++k) v[k] = x[min(i0 + 32 * k, V - 1)];
+    if constexpr (kKind == kRow) {
 #pragma unroll
-      for (int k = 0; k < kSeg; ++k) q[k] = i0 + 32 * k < V ? Elem<Q>::load(dq, i0 + 32 * k) : 0.f;
-    } else {
-#pragma unroll
-      for (int k = 0; k < kSeg; ++k) q[k] = less && i0 + 32 * k == fallen ? 2.f : 0.f;
+      for (int k = 0; k < kSeg; ++k) q[k] = dq[min(i0 + 32 * k, V - 1)];
     }
 #pragma unroll
     for (int k = 0; k < kSeg; k += 2) {
+      const float va = (float)v[k], vb = (float)v[k + 1];
       float2 e;
       if (r.m == INFINITY) {
-        e = make_float2(v[k] == r.m ? 1.f : 0.f, v[k + 1] == r.m ? 1.f : 0.f);
+        e = make_float2(va == r.m ? 1.f : 0.f, vb == r.m ? 1.f : 0.f);
       } else {  // (a NaN's distance counts as far, like a masked one's)
-        e = weights(make_float2(v[k] - r.m, v[k + 1] - r.m), h);
+        e = weights(make_float2(va - r.m, vb - r.m), h);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const float ec = c ? e.y : e.x, qc = fmaxf(q[k + c], 0.f);
+        const int i = i0 + 32 * (k + c);
+        const float ec = c ? e.y : e.x;
+        float qc = 0.f;
+        if constexpr (kKind == kRow) qc = fmaxf((float)q[k + c], 0.f);
+        if constexpr (kKind == kToken) qc = i == fallen ? 2.f : 0.f;
         const float p = __fmaf_rn(ec, inv_hi, __fmaf_rn(ec, inv_lo, -qc));
-        w[k + c] = __float2ull_rn(fminf(fmaxf(p, 0.f), 1.f) * kUnit);
+        w[k + c] = i < V ? units_of(fminf(fmaxf(p, 0.f), 1.f)) : 0;
       }
     }
+  };
+  auto masses = [&](int i0, uint64_t (&w)[kSeg]) {
+    if (less == kRow)
+      masses_of(std::integral_constant<int, kRow>(), i0, w);
+    else if (less == kToken)
+      masses_of(std::integral_constant<int, kToken>(), i0, w);
+    else
+      masses_of(std::integral_constant<int, kNothing>(), i0, w);
   };
   auto warp_sum = [&](uint64_t s) {
 #pragma unroll
@@ -338,12 +388,14 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     uint64_t s = 0;
     if (look)
       for (int g = g0; g < g1; ++g) {
-        uint64_t w[kSeg];
+        uint64_t w[kSeg], sum = 0;
         masses(g * kSegElems + lane, w);
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) s += w[k];
+        for (int k = 0; k < kSeg; ++k) sum += w[k];
+        sum = warp_sum(sum);
+        if (g - g0 < kSegsKept && lane == 0) s_seg[warp][g - g0] = sum;
+        s += sum;
       }
-    s = warp_sum(s);
     if (lane == 0) s_warp[warp] = s;
     __syncthreads();
     if (tid == 0) {
@@ -362,8 +414,8 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     }
     cl.sync();  // read by all before it is written again, or its CTA ends
     if (stop) return;
-    if (total || !less || !look) break;
-    less = false;
+    if (total || less == kNothing || !look) break;
+    less = kNothing;
   }
   // the lowest token whose sum passes r of the total
   uint64_t want = rnd > 0.f ? (rnd < 1.f ? __double2ull_rd((double)rnd * (double)total) : total) : 0;
@@ -372,6 +424,10 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
     int token = -1;
     for (int g = g0; g < g1; ++g) {
+      if (g - g0 < kSegsKept && want >= before + s_seg[warp][g - g0]) {
+        before += s_seg[warp][g - g0];
+        continue;
+      }
       uint64_t w[kSeg], s = 0;
       masses(g * kSegElems + lane, w);
 #pragma unroll
