@@ -85,6 +85,19 @@ __device__ __forceinline__ float logit(const void *p, int64_t i) {
   return x == x ? x : -INFINITY;  // a NaN counts as masked
 }
 
+// the largest of 16 bytes of logits
+template <typename T>
+__device__ __forceinline__ float largest(const uint4 &u) {
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162 *h = (const __nv_bfloat162 *)&u;
+    const __nv_bfloat162 r = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(r), __high2float(r));
+  } else {
+    const float *f = (const float *)&u;
+    return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
+  }
+}
+
 struct VerifyArgs {
   lg_logits x, draft;
   int has_draft, batch, T, max_new, slices;
@@ -96,7 +109,7 @@ struct VerifyArgs {
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) {
-  constexpr int kVec = 16 / (int)sizeof(T), kN = kRowVecs * kVec;
+  constexpr int kVec = 16 / (int)sizeof(T);
   __shared__ float s_m[kRowThreads / 32];
   __shared__ int s_at[kRowThreads / 32];
   __shared__ uint64_t s_z[kRowThreads / 32];
@@ -111,24 +124,22 @@ __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) 
   }
   const T *x = (const T *)a.x.x + row * a.x.stride;
   const int head = (int)(((uintptr_t)x & 15) / sizeof(T));  // elements of the first vector before the row
-  float v[kN];
-  float m = -INFINITY;
+  uint4 v[kRowVecs];  // as they are: half the registers for bf16
 #pragma unroll
   for (int k = 0; k < kRowVecs; ++k) {
     const int i0 = ((blockIdx.x * kRowVecs + k) * kRowThreads + tid) * kVec - head;
     if (i0 >= 0 && i0 + kVec <= V) {
-      Elem<T>::unpack(*(const uint4 *)(x + i0), (float2 *)(v + k * kVec));
+      v[k] = *(const uint4 *)(x + i0);
     } else {
+      T y[kVec];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        v[k * kVec + e] = i0 + e >= 0 && i0 + e < V ? Elem<T>::load(x, i0 + e) : -INFINITY;
+      for (int e = 0; e < kVec; ++e) y[e] = i0 + e >= 0 && i0 + e < V ? x[i0 + e] : (T)-INFINITY;
+      v[k] = *(const uint4 *)y;
     }
   }
+  float m = -INFINITY;  // (a maximum passes a NaN over)
 #pragma unroll
-  for (int e = 0; e < kN; ++e) {
-    v[e] = fmaxf(v[e], -INFINITY);  // a NaN counts as masked
-    m = fmaxf(m, v[e]);
-  }
+  for (int k = 0; k < kRowVecs; ++k) m = fmaxf(m, largest<T>(v[k]));
   const float own = m;
   const float wm = warp_max(m);
   if (lane == 0) s_m[warp] = wm;
@@ -139,25 +150,29 @@ __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) 
   for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, s_m[w]);
   const Heat h = heat_of(t);
   float2 sums = make_float2(0.f, 0.f);
-  if (m == INFINITY) {
+  int at = 0x7fffffff;
 #pragma unroll
-    for (int e = 0; e < kN; ++e) sums.x += v[e] == m ? 1.f : 0.f;
-  } else if (!h.greedy && m != -INFINITY) {
+  for (int k = 0; k < kRowVecs; ++k) {
+    float2 f[kVec / 2];
+    Elem<T>::unpack(v[k], f);
+    if (m == INFINITY) {
 #pragma unroll
-    for (int e = 0; e < kN; e += 2) {
-      const float2 w = weights(make_float2(v[e] - m, v[e + 1] - m), h);
-      sums.x += w.x;
-      sums.y += w.y;
+      for (int e = 0; e < kVec / 2; ++e) sums.x += (f[e].x == m ? 1.f : 0.f) + (f[e].y == m ? 1.f : 0.f);
+    } else if (!h.greedy && m != -INFINITY) {
+#pragma unroll
+      for (int e = 0; e < kVec / 2; ++e)
+        sums = __fadd2_rn(sums, weights(make_float2(f[e].x - m, f[e].y - m), h));
+    }
+    if (own == m) {
+      const int i0 = ((blockIdx.x * kRowVecs + k) * kRowThreads + tid) * kVec - head;
+#pragma unroll
+      for (int e = 0; e < kVec / 2; ++e) {
+        if (f[e].x == m) at = min(at, i0 + 2 * e);
+        if (f[e].y == m) at = min(at, i0 + 2 * e + 1);
+      }
     }
   }
   const float sum = sums.x + sums.y;
-  int at = 0x7fffffff;
-  if (own == m) {
-#pragma unroll
-    for (int e = kN - 1; e >= 0; --e)
-      if (v[e] == m)
-        at = ((blockIdx.x * kRowVecs + e / kVec) * kRowThreads + tid) * kVec - head + e % kVec;
-  }
   uint64_t z = __float2ull_rn(sum * 0x1p40f);
 #pragma unroll
   for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
@@ -246,6 +261,15 @@ __device__ __forceinline__ uint64_t units_of(float w) {
   return sh >= 0 ? (uint64_t)mant << sh : (uint64_t)(mant >> min(-sh, 31));
 }
 
+// a lane's elements of a segment, summed in fp32 before they become units (half the work of this kernel
+// otherwise): over the lanes of a vocabulary the roundings leave some 2^-30 of the mass
+__device__ __forceinline__ uint64_t lane_units(const float (&w)[kSeg]) {
+  float2 s = make_float2(w[0], w[1]);
+#pragma unroll
+  for (int k = 2; k < kSeg; k += 2) s = __fadd2_rn(s, make_float2(w[k], w[k + 1]));
+  return units_of(s.x + s.y);
+}
+
 struct Part {      // of the vocabulary, a CTA's
   uint64_t total;
   int bad;         // the device status
@@ -332,9 +356,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   // what is taken off p: nothing, the draft's row, or all of the fallen token
   enum { kNothing, kRow, kToken };
   int less = !fell ? kNothing : dq ? kRow : a.has_draft ? kNothing : kToken;
-  // the masses of a lane's elements i0, i0 + 32, .. of a segment in 2^-62, all of them loaded first (from
+  // the masses of a lane's elements i0, i0 + 32, .. of a segment, all of them loaded first (from
   // the last place on where the row ends: their masses are zeros)
-  auto masses_of = [&](auto kind, int i0, uint64_t (&w)[kSeg]) {
+  auto masses_of = [&](auto kind, int i0, float (&w)[kSeg]) {
     constexpr int kKind = decltype(kind)::value;
     T v[kSeg];
     Q q[kSeg];
@@ -361,11 +385,11 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
         if constexpr (kKind == kRow) qc = fmaxf((float)q[k + c], 0.f);
         if constexpr (kKind == kToken) qc = i == fallen ? 2.f : 0.f;
         const float p = __fmaf_rn(ec, inv_hi, __fmaf_rn(ec, inv_lo, -qc));
-        w[k + c] = i < V ? units_of(fminf(fmaxf(p, 0.f), 1.f)) : 0;
+        w[k + c] = i < V ? fmaxf(p, 0.f) : 0.f;
       }
     }
   };
-  auto masses = [&](int i0, uint64_t (&w)[kSeg]) {
+  auto masses = [&](int i0, float (&w)[kSeg]) {
     if (less == kRow)
       masses_of(std::integral_constant<int, kRow>(), i0, w);
     else if (less == kToken)
@@ -388,11 +412,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     uint64_t s = 0;
     if (look)
       for (int g = g0; g < g1; ++g) {
-        uint64_t w[kSeg], sum = 0;
+        float w[kSeg];
         masses(g * kSegElems + lane, w);
-#pragma unroll
-        for (int k = 0; k < kSeg; ++k) sum += w[k];
-        sum = warp_sum(sum);
+        const uint64_t sum = warp_sum(lane_units(w));
         if (g - g0 < kSegsKept && lane == 0) s_seg[warp][g - g0] = sum;
         s += sum;
       }
@@ -422,24 +444,25 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (want >= total) want = total ? total - 1 : 0;
   for (int w = 0; w < warp; ++w) before += s_warp[w];
   if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
-    int token = -1;
+    int token = -1, last = -1;
     for (int g = g0; g < g1; ++g) {
       if (g - g0 < kSegsKept && want >= before + s_seg[warp][g - g0]) {
         before += s_seg[warp][g - g0];
         continue;
       }
-      uint64_t w[kSeg], s = 0;
+      float w[kSeg];
       masses(g * kSegElems + lane, w);
-#pragma unroll
-      for (int k = 0; k < kSeg; ++k) s += w[k];
-      s = warp_sum(s);
+      const uint64_t s = warp_sum(lane_units(w));
       if (want >= before + s) {
         before += s;
         continue;
       }
+      // (the elements' own units may stay short of their lanes' sums by roundings: the last then)
 #pragma unroll
       for (int k = 0; k < kSeg; ++k) {
-        uint64_t c = w[k];
+        const unsigned any = __ballot_sync(0xffffffffu, w[k] > 0.f);
+        if (any) last = g * kSegElems + 32 * k + 31 - __clz((int)any);
+        uint64_t c = units_of(w[k]);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const uint64_t u = __shfl_up_sync(0xffffffffu, c, o);
@@ -451,7 +474,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       }
       break;
     }
-    if (lane == 0) a.picked[row] = token;
+    if (lane == 0) a.picked[row] = token >= 0 ? token : last;
   }
   if (rank == 0) {
     if (tid == 0) {
@@ -482,7 +505,7 @@ __global__ void end_chunk_kernel(lg_cache c, lg_chunk ch, const int32_t *accepte
 template <typename T, typename Q>
 cudaError_t launch_pick_typed(const VerifyArgs &a, cudaStream_t s) {
   // as many CTAs a sequence as leave each an SM of its own
-  int n = 8;
+  int n = 16;
   while (n > 1 && a.batch * n > 152) n /= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.batch * n));
@@ -496,6 +519,7 @@ cudaError_t launch_pick_typed(const VerifyArgs &a, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
+  LG_TRY(cudaFuncSetAttribute(verify_pick_kernel<T, Q>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   return cudaLaunchKernelEx(&cfg, verify_pick_kernel<T, Q>, a);
 }
 
