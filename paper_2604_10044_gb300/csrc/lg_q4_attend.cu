@@ -34,6 +34,30 @@
 
 #include "lg_q4.cuh"
 
+#ifndef Q4_C1
+#define Q4_C1 3
+#endif
+#ifndef Q4_C2
+#define Q4_C2 3
+#endif
+#ifndef Q4_C3
+#define Q4_C3 2
+#endif
+#ifndef Q4_C4
+#define Q4_C4 2
+#endif
+#ifndef Q4_J1
+#define Q4_J1 2
+#endif
+#ifndef Q4_S1
+#define Q4_S1 2
+#endif
+#ifndef Q4_S2
+#define Q4_S2 3
+#endif
+#ifndef Q4_S3
+#define Q4_S3 4
+#endif
 namespace lg {
 namespace {
 
@@ -50,8 +74,9 @@ template <int D, int NT>
 struct Q4Cfg {
   static constexpr int kRow = q4_row_bytes(D);
   static constexpr int kTile = kSub * kRow;         // of keys, or of values
-  static constexpr int kStages = D == 64 ? 4 : NT == 1 ? 2 : NT == 2 ? 3 : 4;
-  static constexpr int kJoint = NT == 1 ? 2 : 1;    // products of 16 rows that go through the softmax together
+  static constexpr int kCtas = NT == 1 ? Q4_C1 : NT == 2 ? Q4_C2 : NT == 3 ? Q4_C3 : Q4_C4;  // of an SM
+  static constexpr int kStages = D == 64 ? 4 : NT == 1 ? Q4_S1 : NT == 2 ? Q4_S2 : NT == 3 ? Q4_S3 : 4;
+  static constexpr int kJoint = NT == 1 ? Q4_J1 : 1;    // products of 16 rows that go through the softmax together
   static constexpr int kRing = kWarps * kStages * 2 * kTile;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
@@ -243,7 +268,7 @@ __device__ __forceinline__ Q4Cut *cut_at(const Q4AttendArgs &a, int d, int layer
 }
 
 template <int D, int NT, bool STATS>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2) q4_attend_kernel(Q4AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_kernel(Q4AttendArgs a) {
   using C = Q4Cfg<D, NT>;
   constexpr int kPieces = D / 32;  // 16-byte pieces of a row's codes
   extern __shared__ __align__(128) uint8_t smem[];
@@ -834,8 +859,9 @@ __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs
 template <int D, int NT, bool STATS>
 cudaError_t launch_nt(const Q4AttendArgs &a, cudaStream_t s) {
   using C = Q4Cfg<D, NT>;
-  LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+  if constexpr (C::kSmem > 48 * 1024)
+    LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
   LG_TRY(launch_pdl(q4_attend_kernel<D, NT, STATS>, dim3(a.ctas, a.n_layers), kThreads, C::kSmem, s, a));
   return cudaGetLastError();
 }
@@ -862,7 +888,7 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   const int64_t tiles = (rows + r.rows - 1) / r.rows;
   const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
   // what the 152 SMs of a GB300 hold at once, over the layers; no more than there are blocks
-  const int64_t fit = 152 * (r.rows <= 8 ? 4 : r.rows <= 16 ? 3 : 2);
+  const int64_t fit = 152 * (r.rows <= 8 ? Q4_C1 : r.rows <= 16 ? Q4_C2 : r.rows <= 24 ? Q4_C3 : Q4_C4);
   const int64_t most = batch * H_kv * tiles * (blocks + kQ4ItemUnits);
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));

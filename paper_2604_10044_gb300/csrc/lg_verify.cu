@@ -519,7 +519,9 @@ cudaError_t launch_pick_typed(const VerifyArgs &a, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  LG_TRY(cudaFuncSetAttribute(verify_pick_kernel<T, Q>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  if (n > 8)
+    LG_TRY(cudaFuncSetAttribute(verify_pick_kernel<T, Q>,
+                                cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   return cudaLaunchKernelEx(&cfg, verify_pick_kernel<T, Q>, a);
 }
 

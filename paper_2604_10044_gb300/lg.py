@@ -488,7 +488,7 @@ def lg_count_tokens(tokens, off, V, generated, seen, counts, status=None, stream
           _ptr(seen), _ptr(counts), _ptr(status), _stream(stream))
 
 
-_I32, _F32 = torch.int32, torch.float32
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
 _lg_logits = struct.Struct("@Piiiiq").pack  # an lg_logits, in a quarter of the structure's time
 _LOGITS = {torch.bfloat16: LG_BF16, torch.float32: LG_F32}
 
@@ -561,10 +561,11 @@ def lg_pick_token(logits, seen, counts, penalty, bias, allowed, tokens, pmax, st
 
 def _logits_of(t, name):
     """an lg_logits of [rows][V] with whole rows that do not overlap"""
-    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    sh, st = t.shape, t.stride()
+    if len(sh) != 2 or st[1] != 1 or sh[0] > 1 and st[0] < sh[1]:
         raise ValueError("%s: [T][V] with whole rows that do not overlap" % name)
-    B, V = t.shape
-    return _lg_logits(t.data_ptr(), _LOGITS.get(t.dtype, -1), B, V, 0, t.stride(0) if B > 1 else V)
+    B, V = sh
+    return _lg_logits(t.data_ptr(), _LOGITS.get(t.dtype, -1), B, V, 0, st[0] if B > 1 else V)
 
 
 def lg_verify_workspace_size(logits, chunk) -> int:
@@ -576,17 +577,22 @@ def lg_verify_draft(logits, chunk, tokens, draft, temperature, u, r, picked, acc
     """logits [T][V], row t the target's after tokens[t]; draft: probabilities [T][V] (its own type and
     stride) or None; temperature [batch] or None, u [T], r [batch] fp32; picked [T], accepted [batch]
     int32; ws: lg_verify_workspace_size bytes"""
-    T, batch, at = chunk.T, chunk.off.numel() - 1, _device()
+    off = chunk.off
+    T, batch, at = chunk.T, off.numel() - 1, _device()
     x = _logits_of(logits, "logits")
     y = None if draft is None else _logits_of(draft, "draft")
-    if chunk.off.get_device() != at:
+    if off.get_device() != at:
         _refuse("off", "[batch + 1] int32")
     if logits.get_device() != at or draft is not None and draft.get_device() != at:
         _refuse("logits, draft", "[T][V]")
-    if not (_dense(tokens, _I32, T, at) and _dense(picked, _I32, T, at) and
-            _dense(accepted, _I32, batch, at)):
+    # (in place what _dense asks, as in lg_pick_token)
+    if not (tokens.dtype is _I32 and tokens.numel() >= T and tokens.is_contiguous() and
+            tokens.get_device() == at and picked.dtype is _I32 and picked.numel() >= T and
+            picked.is_contiguous() and picked.get_device() == at and accepted.dtype is _I32 and
+            accepted.numel() >= batch and accepted.is_contiguous() and accepted.get_device() == at):
         _refuse("tokens, picked, accepted", "[T], [T], [batch] int32")
-    if not (_dense(u, _F32, T, at) and _dense(r, _F32, batch, at) and
+    if not (u.dtype is _F32 and u.numel() >= T and u.is_contiguous() and u.get_device() == at and
+            r.dtype is _F32 and r.numel() >= batch and r.is_contiguous() and r.get_device() == at and
             (temperature is None or _dense(temperature, _F32, batch, at))):
         _refuse("u, r, temperature", "[T], [batch], [batch] fp32")
     if status is not None and not _dense(status, _I32, 1, at):
@@ -594,8 +600,10 @@ def lg_verify_draft(logits, chunk, tokens, draft, temperature, u, r, picked, acc
     if not ws.is_contiguous() or ws.get_device() != at:
         _refuse("ws", "bytes")
     rc = (_lib or lib()).lg_verify_draft(
-        x, ctypes.byref(chunk.c), batch, tokens.data_ptr(), y, _ptr(temperature), u.data_ptr(),
-        r.data_ptr(), picked.data_ptr(), accepted.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(status),
+        x, ctypes.byref(chunk.c), batch, tokens.data_ptr(), y,
+        None if temperature is None else temperature.data_ptr(), u.data_ptr(), r.data_ptr(),
+        picked.data_ptr(), accepted.data_ptr(), ws.data_ptr(), ws.nbytes,
+        None if status is None else status.data_ptr(),
         _raw_stream(at) if stream is None and _raw_stream else _stream(stream))
     if rc:
         raise LgError("lg_verify_draft", rc)
@@ -612,7 +620,9 @@ def lg_end_chunk(cache, chunk, accepted, stream=None):
 def lg_read_rows(cache, chunk, layer, k_out, v_out, stream=None):
     """the chunk's rows of a 4-bit cache as values: k_out, v_out [T][H_kv][d] bf16"""
     n, at = chunk.T * cache.H_kv * cache.d, _device_of(cache, chunk)
-    if not (_dense(k_out, torch.bfloat16, n, at) and _dense(v_out, torch.bfloat16, n, at)):
+    if not (k_out.dtype is _BF16 and k_out.numel() >= n and k_out.is_contiguous() and
+            k_out.get_device() == at and v_out.dtype is _BF16 and v_out.numel() >= n and
+            v_out.is_contiguous() and v_out.get_device() == at):
         _refuse("k_out, v_out", "[T][H_kv][d] bf16")
     rc = (_lib or lib()).lg_read_rows(
         ctypes.byref(cache.c), ctypes.byref(chunk.c), layer, k_out.data_ptr(), v_out.data_ptr(),
