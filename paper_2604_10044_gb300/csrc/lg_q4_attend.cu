@@ -767,28 +767,27 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   }
 }
 
-// The CTAs' results of a row of a cut item, a CTA a row (blockIdx = (row, the CTA whose start cuts it,
-// layer)): the maximum of all parts first, a lane a part, then their sums with nothing but additions
-// between the loads, a warp every fourth part.
-constexpr int kMergeWarps = 4;
+// The CTAs' results of a cut item (blockIdx = (the CTA whose start cuts it, 16 rows, layer)): the warps
+// share out the rows, then the parts of a row.  The maximum of all parts comes first, a lane a part, then
+// their sums with nothing but additions between the loads.
+constexpr int kMergeWarps = 16;
 
 template <int D, bool STATS>
 __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs a) {
   constexpr int kE = D / 32;
   __shared__ float s_x[kMergeWarps][D];
   __shared__ float4 s_v[kMergeWarps];
-  __shared__ float s_m[kMergeWarps];
   __shared__ int s_bad;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int r = blockIdx.x, layer = blockIdx.z;
+  const int layer = blockIdx.z, r0 = blockIdx.y * kMergeWarps;
   pdl_enter();
-  const Q4Cut w = *cut_at(a, D, layer, blockIdx.y);
+  const Q4Cut w = *cut_at(a, D, layer, blockIdx.x);
   if (tid == 0) s_bad = status_bad(a.status);
   __syncthreads();
   if (s_bad) return;
-  if (STATS && r == 0) {  // empty sequences attend to nothing
+  if (STATS && r0 == 0) {  // empty sequences attend to nothing
     const int H_q = a.H_kv * a.g;
-    for (int b = blockIdx.y; b < a.batch; b += a.ctas) {
+    for (int b = blockIdx.x; b < a.batch; b += a.ctas) {
       if (a.len[b] != 0) continue;
       const int64_t head = ((int64_t)layer * a.T + b) * H_q;
       for (int e = tid; e < H_q * D / 2; e += 32 * kMergeWarps) ((uint32_t *)a.out)[head * D / 2 + e] = 0u;
@@ -796,62 +795,66 @@ __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs
         ((float4 *)a.stats)[head + h] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     }
   }
-  if (w.step == 0 || r >= w.used) return;
-  const int c0 = blockIdx.y - 1;  // the CTA that the item began in
+  if (w.step == 0 || r0 >= w.used) return;
+  const int c0 = blockIdx.x - 1;  // the CTA that the item began in
   auto cut = [&](int c) { return q4_cut(c * w.step - w.x0, w.count); };  // blocks before CTA c
   // one part has every block and wrote the result: the first that has any, then
   int some = c0 + 1;
   while (cut(some) == 0) ++some;
   if (cut(some) == w.count) return;
-  int parts = 1;
-  for (int64_t y = (c0 + 1) * w.step; y < w.x0 + w.units; y += w.step) ++parts;
-  auto part_of = [&](int k) { return part_row<D>(a, layer, c0 + k, k == 0, r); };
+  int parts = (int)plan_div(w.x0 + w.units - 1, w.step) + 1 - c0;
   auto has = [&](int k) { return cut(c0 + k) < cut(c0 + k + 1); };
-  float mx = kNone;
-  for (int c = tid; c < parts; c += 32 * kMergeWarps)
-    if (has(c)) mx = fmaxf(mx, part_of(c)[D]);
-  mx = warp_max(mx);
-  if (lane == 0) s_m[warp] = mx;
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kMergeWarps; ++k) mx = fmaxf(mx, s_m[k]);
-  float sl = 0.f, sh = 0.f, ss = 0.f, x[kE] = {};
+  int share2 = 0;  // log2 of the warps of a row
+  while (min(w.used - r0, kMergeWarps) << (share2 + 1) <= kMergeWarps) ++share2;
+  const int r = r0 + (warp >> share2), sub = warp & ((1 << share2) - 1);
+  float mx = kNone, sl = 0.f, sh = 0.f, ss = 0.f, x[kE] = {};
+  if (r < w.used) {
+    auto part_of = [&](int k) { return part_row<D>(a, layer, c0 + k, k == 0, r); };
+    for (int c = lane; c < parts; c += 32)
+      if (has(c)) mx = fmaxf(mx, part_of(c)[D]);
+    mx = warp_max(mx);
 #pragma unroll 4
-  for (int c = warp; c < parts; c += kMergeWarps) {
-    if (!has(c)) continue;
-    const float *part = part_of(c);
-    const float4 v = *(const float4 *)(part + D);
-    float y[kE];
+    for (int c = sub; c < parts; c += 1 << share2) {
+      if (!has(c)) continue;
+      const float *part = part_of(c);
+      const float4 v = *(const float4 *)(part + D);
+      float y[kE];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) y[e] = part[lane + 32 * e];
-    const bool any = v.y != 0.f;
-    const float by = v.x - mx, f = any ? exp2_fast(by) : 0.f;
-    sl += f * v.y;
-    if (STATS) {
-      sh += any ? f * __fmaf_rn(by, v.y, v.z) : 0.f;
-      ss += f * v.w;
+      for (int e = 0; e < kE; ++e) y[e] = part[lane + 32 * e];
+      const bool any = v.y != 0.f;
+      const float by = v.x - mx, f = any ? exp2_fast(by) : 0.f;
+      sl += f * v.y;
+      if (STATS) {
+        sh += any ? f * __fmaf_rn(by, v.y, v.z) : 0.f;
+        ss += f * v.w;
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) x[e] += any ? f * y[e] : 0.f;
     }
-#pragma unroll
-    for (int e = 0; e < kE; ++e) x[e] += any ? f * y[e] : 0.f;
   }
+  if (share2) {
 #pragma unroll
-  for (int e = 0; e < kE; ++e) s_x[warp][lane + 32 * e] = x[e];
-  if (lane == 0) s_v[warp] = make_float4(0.f, sl, sh, ss);
-  __syncthreads();
-  if (warp >= kE) return;
-  sl = sh = ss = x[0] = 0.f;
+    for (int e = 0; e < kE; ++e) s_x[warp][lane + 32 * e] = x[e];
+    if (lane == 0) s_v[warp] = make_float4(0.f, sl, sh, ss);
+    __syncthreads();
+    if (sub) return;
+    for (int k = 1; k < 1 << share2; ++k) {
+      const float4 v = s_v[warp + k];
+      sl += v.y;
+      sh += v.z;
+      ss += v.w;
 #pragma unroll
-  for (int k = 0; k < kMergeWarps; ++k) {
-    sl += s_v[k].y;
-    sh += s_v[k].z;
-    ss += s_v[k].w;
-    x[0] += s_x[k][32 * warp + lane];
+      for (int e = 0; e < kE; ++e) x[e] += s_x[warp + k][lane + 32 * e];
+    }
   }
+  if (r >= w.used) return;
   const float inv = sl != 0.f ? 1.f / sl : 0.f;
   const int rr = r + w.row_1, H_q = a.H_kv * a.g;
   const int64_t head = w.head + (int64_t)(rr / a.g) * H_q + rr % a.g;
-  ((__nv_bfloat16 *)a.out)[head * D + 32 * warp + lane] = __float2bfloat16_rn(x[0] * inv);
-  if (STATS && tid == 0)
+#pragma unroll
+  for (int e = 0; e < kE; ++e)
+    ((__nv_bfloat16 *)a.out)[head * D + 32 * e + lane] = __float2bfloat16_rn(x[e] * inv);
+  if (STATS && lane == 0)
     ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
                                             logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
 }
@@ -859,7 +862,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs
 template <int D, int NT, bool STATS>
 cudaError_t launch_nt(const Q4AttendArgs &a, cudaStream_t s) {
   using C = Q4Cfg<D, NT>;
-  if constexpr (C::kSmem > 48 * 1024)
+  if constexpr (C::kSmem > 44 * 1024)  // (48 KB with the static arrays need no leave)
     LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
   LG_TRY(launch_pdl(q4_attend_kernel<D, NT, STATS>, dim3(a.ctas, a.n_layers), kThreads, C::kSmem, s, a));
@@ -874,8 +877,9 @@ cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
     case 24: if constexpr (!STATS) LG_TRY((launch_nt<D, 3, STATS>(a, s))); break;
     default: if constexpr (!STATS) LG_TRY((launch_nt<D, 4, STATS>(a, s))); break;
   }
-  LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>, dim3(a.shape.rows, a.ctas, a.n_layers), 32 * kMergeWarps, 0,
-                    s, a));
+  LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>, 
+                    dim3(a.ctas, (a.shape.rows + kMergeWarps - 1) / kMergeWarps, a.n_layers),
+                    32 * kMergeWarps, 0, s, a));
   return cudaGetLastError();
 }
 

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "lg_q4.cuh"
 #include "lg_rope.cuh"
 
@@ -12,11 +14,12 @@ namespace {
 
 // ---------------------------------------------------------------- new rows
 //
-// A thread holds 16 bytes (8 elements) of a token's heads: one word of codes.  It takes its cosines
-// and sines once and walks over heads: queries (rotated, stored as they are), keys (rotated, rounded
-// to bf16 as a 16-bit cache would hold them, quantised), values.  The other elements of its pairs come
-// by shuffles (so queries may be rotated in place), as do the least and largest element of a group, over
-// the 4 (d = 128) or 2 lanes that hold it.
+// A thread holds 16 bytes (8 elements) of a token's heads, one word of codes, or two such where halves of
+// the whole head are rotated together.  It takes its cosines and sines once and walks over heads: queries
+// (rotated, stored as they are), keys (rotated, rounded to bf16 as a 16-bit cache would hold them,
+// quantised), values.  Otherwise the other elements of its pairs come by shuffles (so queries may be
+// rotated in place), as do the least and largest element of a group, over the 4 (d = 128) or 2 lanes
+// that hold it.
 
 struct Q4AppendArgs {
   const __nv_bfloat16 *q, *k, *v;
@@ -34,8 +37,8 @@ struct Q4AppendArgs {
 };
 
 constexpr int kQ4Threads = 256;
-constexpr int kQ4Tokens = 64;  // tokens a CTA at most
-constexpr int kQ4Together = 4; // heads of a thread in flight
+constexpr int kQ4Tokens = 64;  // tokens a CTA at most (256 / 4 lanes)
+constexpr int kQ4InFlight = 4; // words of a thread in flight
 
 // token_slots in one round trip where a lane can hold a sequence
 __device__ __forceinline__ void token_slots_near(const lg_cache &c, const lg_chunk &ch, int t0, int n,
@@ -61,11 +64,14 @@ __device__ __forceinline__ void token_slots_near(const lg_cache &c, const lg_chu
   token_slots(c, ch, t0, n, s_slot);
 }
 
-// ONE: token t is the one new row of sequence t, and blockIdx.y the layer
-template <int D, bool ONE>
+// ONE: token t is the one new row of sequence t, and blockIdx.y the layer.  PAIR: halves of the whole head
+// are rotated together, so a thread holds both elements of its pairs, words pc and pc + D / 16.
+template <int D, bool ONE, bool PAIR>
 __global__ void __launch_bounds__(kQ4Threads)
     q4_append_kernel(lg_cache c, lg_chunk ch, Q4AppendArgs a, const __grid_constant__ RopeTable tab) {
-  constexpr int kLanes = D / 8, kGroup = D / 32, kRow = q4_row_bytes(D);
+  constexpr int kW = PAIR ? 2 : 1;  // words of a thread
+  constexpr int kTogether = kQ4InFlight / kW;
+  constexpr int kLanes = D / 8 / kW, kGroup = D / 32, kRow = q4_row_bytes(D);
   __shared__ int64_t s_slot[kQ4Tokens];
   __shared__ int s_bad;
   // no early trigger: the loop-onset test reads sketches before its own wait
@@ -96,97 +102,127 @@ __global__ void __launch_bounds__(kQ4Threads)
   const int t = t0 + i;
   const int64_t slot = i < a.tok && t < a.T ? s_slot[i] : -1;
   const bool live = slot >= 0;
-  const bool turned = 8 * pc < a.rot, half_lay = a.layout == LG_ROPE_HALF;
-  const int hp = a.rot / 16;  // 16-byte pieces of half of the rotated elements
+  // !PAIR: the lane that holds the other elements of the word's pairs
+  const bool half_lay = a.layout == LG_ROPE_HALF, turned = PAIR || 8 * pc < a.rot;
+  const int hp = a.rot / 16;  // words of half of the rotated elements
   const int other = (threadIdx.x & 31) - pc + (turned && half_lay ? (pc < hp ? pc + hp : pc - hp) : pc);
-  float co[8], si[8];  // of the element's pair; si with the sign of its product with the other element
-  if (live && turned) {
+  float2 co[4], si[4];  // of the elements' pairs; si with the sign of its product with the other element
+  if (live && turned && a.rot) {
     const uint64_t p = (uint64_t)(int64_t)a.pos[t];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int pair = half_lay ? (pc < hp ? pc : pc - hp) * 8 + e : pc * 4 + e / 2;
-      if (half_lay || e % 2 == 0) {
-        turn_cos_sin(p * tab.turn[pair], co[e], si[e]);
-        co[e] *= a.mscale;
-        si[e] *= half_lay && pc >= hp ? a.mscale : -a.mscale;
+    for (int e = 0; e < 4; ++e) {
+      if (PAIR || half_lay) {
+        const int pair = (PAIR || pc < hp ? pc : pc - hp) * 8 + 2 * e;
+        turn_cos_sin(p * tab.turn[pair], co[e].x, si[e].x);
+        turn_cos_sin(p * tab.turn[pair + 1], co[e].y, si[e].y);
+        const float m = !PAIR && pc >= hp ? a.mscale : -a.mscale;
+        si[e].x *= m;
+        si[e].y *= m;
+        co[e].y *= a.mscale;
       } else {
-        co[e] = co[e - 1];
-        si[e] = -si[e - 1];
+        turn_cos_sin(p * tab.turn[pc * 4 + e], co[e].x, si[e].x);
+        si[e].x *= -a.mscale;
+        si[e].y = -si[e].x;
+        co[e].y = co[e].x * a.mscale;
       }
+      co[e].x *= a.mscale;
     }
   }
-  const int64_t layer_row = (int64_t)layer * c.H_kv * c.S_total;
+  auto rotated = [&](const uint4 &own, const uint4 &far, bool second) {  // second: of a PAIR
+    float2 f[4], g[4];
+    Elem<__nv_bfloat16>::unpack(own, f);
+    Elem<__nv_bfloat16>::unpack(far, g);
+    uint32_t r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 o = PAIR || half_lay ? g[e] : make_float2(g[e].y, g[e].x);
+      const float2 s = second ? make_float2(-si[e].x, -si[e].y) : si[e];
+      const float2 y = __ffma2_rn(f[e], co[e], __fmul2_rn(o, s));
+      const __nv_bfloat162 p = __floats2bfloat162_rn(y.x, y.y);
+      r[e] = *(const uint32_t *)&p;
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  };
   const int64_t in = ONE ? (int64_t)blockIdx.y * c.batch + t : t;  // token row of the inputs
-  const int h1 = a.H_q + c.H_kv, h2 = h1 + c.H_kv;
-  // Every lane of a warp makes the same number of turns, as the shuffles need them all; the pieces of
-  // kQ4Together heads are requested before the first is worked on.
-  const int turns = (h2 + groups - 1) / groups;
-  for (int n0 = 0; n0 < turns; n0 += kQ4Together) {
-    uint4 in4[kQ4Together];
+  // Heads of one kind, head h of the combined line of queries, keys and values with thread h mod groups.
+  // Every lane of a warp makes the same number of turns, as the shuffles need them all; the words of
+  // kTogether heads are requested before the first is worked on.
+  auto heads = [&](auto kind, const __nv_bfloat16 *src, int before, int count, uint8_t *dst) {
+    constexpr int kKind = decltype(kind)::value;  // 0: queries, 1: keys, 2: values
+    const int first = (grp - before % groups + groups) % groups;
+    const int turns = (count + groups - 1) / groups;
+    src += (int64_t)first * D + 8 * pc;
+    for (int n0 = 0; n0 < turns; n0 += kTogether) {
+      uint4 own[kTogether][kW];
 #pragma unroll
-    for (int k = 0; k < kQ4Together; ++k) {
-      const int h = grp + (n0 + k) * groups;
-      in4[k] = make_uint4(0, 0, 0, 0);
-      if (!live || h >= h2) continue;
-      const __nv_bfloat16 *src = h < a.H_q ? a.q + in * a.q_stride + (int64_t)h * D
-                                 : h < h1  ? a.k + in * a.k_stride + (int64_t)(h - a.H_q) * D
-                                           : a.v + in * a.v_stride + (int64_t)(h - h1) * D;
-      in4[k] = *(const uint4 *)(src + 8 * pc);
-    }
+      for (int k = 0; k < kTogether; ++k) {
+        const bool mine = live && first + (n0 + k) * groups < count;
 #pragma unroll
-    for (int k = 0; k < kQ4Together; ++k) {
-      if (n0 + k >= turns) break;
-      const int h = grp + (n0 + k) * groups;
-      const bool mine = live && h < h2;
-      const bool isq = h < a.H_q, isk = !isq && h < h1;
-      uint4 raw = in4[k];
-      if (__any_sync(0xffffffffu, h < h1) && a.rot) {
-        uint4 far = raw;
-        if (half_lay) {  // the other elements of its pairs
-          far.x = __shfl_sync(0xffffffffu, raw.x, other);
-          far.y = __shfl_sync(0xffffffffu, raw.y, other);
-          far.z = __shfl_sync(0xffffffffu, raw.z, other);
-          far.w = __shfl_sync(0xffffffffu, raw.w, other);
-        }
-        if (h < h1 && turned) {
-          float2 f[4], g[4];
-          Elem<__nv_bfloat16>::unpack(raw, f);
-          Elem<__nv_bfloat16>::unpack(far, g);
-          uint32_t r[4];
+        for (int w = 0; w < kW; ++w)
+          own[k][w] = mine ? *(const uint4 *)(src + (int64_t)(n0 + k) * groups * D + w * (D / 2))
+                           : make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 o = half_lay ? g[e] : make_float2(g[e].y, g[e].x);
-            const float2 y = __ffma2_rn(f[e], make_float2(co[2 * e], co[2 * e + 1]),
-                                        __fmul2_rn(o, make_float2(si[2 * e], si[2 * e + 1])));
-            const __nv_bfloat162 p = __floats2bfloat162_rn(y.x, y.y);
-            r[e] = *(const uint32_t *)&p;
+      for (int k = 0; k < kTogether; ++k) {
+        if (n0 + k >= turns) break;
+        const int h = first + (n0 + k) * groups;
+        const bool mine = live && h < count;
+        uint4(&x)[kW] = own[k];
+        if (kKind < 2 && a.rot) {
+          if constexpr (PAIR) {
+            const uint4 y = rotated(x[0], x[1], false);
+            x[1] = rotated(x[1], x[0], true);
+            x[0] = y;
+          } else {
+            uint4 far = x[0];
+            if (half_lay) {
+              far.x = __shfl_sync(0xffffffffu, far.x, other);
+              far.y = __shfl_sync(0xffffffffu, far.y, other);
+              far.z = __shfl_sync(0xffffffffu, far.z, other);
+              far.w = __shfl_sync(0xffffffffu, far.w, other);
+            }
+            if (turned) x[0] = rotated(x[0], far, false);
           }
-          raw = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+        if constexpr (kKind == 0) {
+          if (!mine) continue;
+#pragma unroll
+          for (int w = 0; w < kW; ++w)
+            *(uint4 *)(dst + ((int64_t)h * D + 8 * pc + w * (D / 2)) * 2) = x[w];
+        } else {
+          uint32_t *row = (uint32_t *)(dst + ((int64_t)h * c.S_total + slot) * kRow);
+#pragma unroll
+          for (int w = 0; w < kW; ++w) {
+            float y[8];
+            Elem<__nv_bfloat16>::unpack(x[w], (float2 *)y);
+            uint32_t par;
+            const uint32_t word = q4_encode<kGroup>(y, par);
+            if (!mine) continue;
+            const int at = pc + w * kLanes;
+            row[at] = word;
+            if (pc % kGroup == 0) row[D / 8 + at / kGroup] = par;
+            if (kKind == 2 && layer == a.guard)  // signs of the values as they came
+              ((uint8_t *)c.sketch)[slot * (c.H_kv * D / 8) + h * (D / 8) + at] =
+                  (uint8_t)Elem<__nv_bfloat16>::signs(x[w]);
+          }
         }
       }
-      if (mine && isq) *(uint4 *)(a.q_out + ((int64_t)t * a.H_q + h) * D + 8 * pc) = raw;
-      if (__all_sync(0xffffffffu, !mine || isq)) continue;
-      float x[8];
-      Elem<__nv_bfloat16>::unpack(raw, (float2 *)x);
-      uint32_t par;
-      const uint32_t word = q4_encode<kGroup>(x, par);
-      if (!mine || isq) continue;
-      const int kvh = isk ? h - a.H_q : h - h1;
-      uint8_t *row = (uint8_t *)(isk ? c.k : c.v) +
-                     (layer_row + kvh * c.S_total + slot) * (int64_t)kRow;
-      ((uint32_t *)row)[pc] = word;
-      if (pc % kGroup == 0) ((uint32_t *)row)[kLanes + pc / kGroup] = par;
-      if (!isk && layer == a.guard)  // signs of the values as they came
-        ((uint8_t *)c.sketch)[slot * (c.H_kv * D / 8) + kvh * kLanes + pc] =
-            (uint8_t)Elem<__nv_bfloat16>::signs(raw);
     }
-  }
+  };
+  const int64_t layer_row = (int64_t)layer * c.H_kv * c.S_total * kRow;
+  if (a.H_q)
+    heads(std::integral_constant<int, 0>(), a.q + in * a.q_stride, 0, a.H_q,
+          (uint8_t *)(a.q_out + (int64_t)t * a.H_q * D));
+  heads(std::integral_constant<int, 1>(), a.k + in * a.k_stride, a.H_q, c.H_kv,
+        (uint8_t *)c.k + layer_row);
+  heads(std::integral_constant<int, 2>(), a.v + in * a.v_stride, a.H_q + c.H_kv, c.H_kv,
+        (uint8_t *)c.v + layer_row);
 }
 
-template <int D>
-cudaError_t launch_append_d(const lg_cache &c, const lg_chunk *ch, Q4AppendArgs &a, int n_layers,
-                            const RopeTable &tab, cudaStream_t s) {
-  constexpr int kLanes = D / 8;
+template <int D, bool ONE, bool PAIR>
+cudaError_t launch_append_as(const lg_cache &c, const lg_chunk &ch, Q4AppendArgs &a, int n_layers,
+                             const RopeTable &tab, cudaStream_t s) {
+  constexpr int kLanes = D / 8 / (PAIR ? 2 : 1);
   const int heads = a.H_q + 2 * c.H_kv;
   // as many heads a thread, for its cosines and sines to serve, as leave the GPU four CTAs an SM; a few
   // tokens' heads over several CTAs
@@ -200,11 +236,17 @@ cudaError_t launch_append_d(const lg_cache &c, const lg_chunk *ch, Q4AppendArgs 
   a.parts = 1;
   while (a.parts * a.groups < heads && ctas * a.parts < 2 * 152) a.parts *= 2;
   const dim3 grid((a.T + a.tok - 1) / a.tok, n_layers, a.parts);
-  if (ch)
-    LG_TRY(launch_pdl(q4_append_kernel<D, false>, grid, kQ4Threads, 0, s, c, *ch, a, tab));
-  else
-    LG_TRY(launch_pdl(q4_append_kernel<D, true>, grid, kQ4Threads, 0, s, c, lg_chunk{}, a, tab));
+  LG_TRY(launch_pdl(q4_append_kernel<D, ONE, PAIR>, grid, kQ4Threads, 0, s, c, ch, a, tab));
   return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_append_d(const lg_cache &c, const lg_chunk *ch, Q4AppendArgs &a, int n_layers,
+                            const RopeTable &tab, cudaStream_t s) {
+  const bool pair = a.rot == D && a.layout == LG_ROPE_HALF;
+  if (!ch) return launch_append_as<D, true, false>(c, lg_chunk{}, a, n_layers, tab, s);
+  return pair ? launch_append_as<D, false, true>(c, *ch, a, n_layers, tab, s)
+              : launch_append_as<D, false, false>(c, *ch, a, n_layers, tab, s);
 }
 
 // ---------------------------------------------------------------- rows read back
