@@ -115,6 +115,7 @@ struct Q4AttendArgs {
   int64_t S_total;
   int layer0, n_layers, batch, H_kv, g, T, max_new, max_len;
   int ctas;                // of a layer
+  bool cluster;            // a cluster of CTAs an item
   int suffix_w;
   float qscale;            // softmax scale * log2(e)
   Q4Shape shape;
@@ -123,6 +124,7 @@ struct Q4AttendArgs {
 // how a call is divided, and the bytes of its partial results
 struct Q4Grid {
   int rows, ctas;
+  bool cluster;
   size_t part_bytes;
 };
 Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len);
@@ -148,6 +150,7 @@ inline void q4_fill(Q4AttendArgs &a, const lg_cache &c, int g, float scale, cons
   a.g = a.shape.g = g;
   a.shape.rows = grid.rows;
   a.ctas = grid.ctas;
+  a.cluster = grid.cluster;
   a.qscale = scale * 1.4426950408889634f;
 }
 

@@ -26,6 +26,7 @@
 //
 // Every warp copies its own 32 rows a block (bulk copies into a ring of its own), so warps never wait
 // for one another.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -61,10 +62,17 @@
 namespace lg {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
 constexpr int kBn2 = kQ4Bn2;         // a CTA's block: kWarps tiles
+constexpr unsigned kCluster = 8;
+#ifndef Q4_CB
+#define Q4_CB 8
+#endif
+constexpr int kClusterBlocks = Q4_CB;    // key blocks of a cluster's CTA up to which it is used
 constexpr float kLazy = 8.f;         // log2 units that a weight may pass 1 by
 constexpr float kHidden = -1e38f;    // score of a row that a query does not see
 constexpr float kNone = -1e30f;      // maximum of a query that has seen nothing
@@ -81,7 +89,8 @@ struct Q4Cfg {
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
   static constexpr int kQ = NT > 2 ? NT * 4 * 32 * 16 : 0;   // fragments of q, unless in registers
-  static constexpr int kSmem = (kRing > kOut ? kRing : kOut) + kQ;
+  static constexpr int kPart = kRows * (D + 4) * 4;          // a CTA's results, for its cluster
+  static constexpr int kSmem = (kRing > kOut + kPart ? kRing : kOut + kPart) + kQ;
 };
 
 // The 16-byte piece of a row that holds group gr, and whether word (or half word) i of it, of four
@@ -267,7 +276,7 @@ __device__ __forceinline__ Q4Cut *cut_at(const Q4AttendArgs &a, int d, int layer
          (int64_t)layer * a.ctas + cta;
 }
 
-template <int D, int NT, bool STATS>
+template <int D, int NT, bool STATS, bool CL>
 __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_kernel(Q4AttendArgs a) {
   using C = Q4Cfg<D, NT>;
   constexpr int kPieces = D / 32;  // 16-byte pieces of a row's codes
@@ -281,47 +290,70 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   }
   __syncwarp();
   pdl_enter();
-  if (cta_status_bad(a.status)) return;
+  // (CTAs of a cluster, which meet at barriers, may find another status each: they go on without work)
+  const bool bad = cta_status_bad(a.status);
+  if (!CL && bad) return;
   const int layer = blockIdx.y, cta = blockIdx.x;  // (layer of the call)
   const int H_q = a.H_kv * a.g;
   float *s_o = (float *)smem;  // [warp][row][D + 1], the warps' results
   __shared__ float4 s_st[kWarps][8 * NT];
-  Q4Line line;
-  if (!q4_line(a, cta, line)) return;
-  const int64_t y0 = cta * line.step, y1 = plan_min(y0 + line.step, line.W);
-  if (y0 >= y1) {
-    if (tid == 0) cut_at(a, D, layer, cta)->step = 0;
-    return;
-  }
   struct {
     ChunkSeq q;
     TileRows rows;
     TileBlocks blocks;
     int kvh, tile, off, used;
   } w;
-  int seq = line.b;
-  int64_t x = line.x;  // the item's start
-  w.q = line.q;
-  w.off = line.off;
-  int units = q4_units(w.q, a.shape), tiles = q4_tiles(w.q, a.shape);
-  {
+  int seq, units, tiles;
+  int64_t x, y0, y1;  // the item's start in the line, the CTA's share
+  if constexpr (CL) {  // a cluster an item
+    unsigned item = blockIdx.x / kCluster;
+    tiles = (int)(((int64_t)a.max_new * a.g + a.shape.rows - 1) / a.shape.rows);
+    w.tile = (int)(item % (unsigned)tiles);
+    item /= (unsigned)tiles;
+    w.kvh = (int)(item % (unsigned)a.H_kv);
+    seq = (int)(item / (unsigned)a.H_kv);
+    if (!q4_seq(a, seq, w.q, w.off)) {  // (the same in the cluster, as what returns below)
+      if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
+      return;
+    }
+    if (STATS && w.q.n == 0 && !bad && blockIdx.x % kCluster == 0) {
+      const int64_t head = ((int64_t)layer * a.T + w.off) * H_q + w.kvh * a.g;  // attends to nothing
+      for (int e = tid; e < a.g * D / 2; e += kThreads) ((uint32_t *)a.out)[head * D / 2 + e] = 0u;
+      if (tid < a.g) ((float4 *)a.stats)[head + tid] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    }
+    if (w.tile >= q4_tiles(w.q, a.shape)) return;
+    x = y0 = 0;
+    y1 = units = 1;
+  } else {
+    Q4Line line;
+    if (!q4_line(a, cta, line)) return;
+    y0 = cta * line.step, y1 = plan_min(y0 + line.step, line.W);
+    if (y0 >= y1) {
+      if (tid == 0) cut_at(a, D, layer, cta)->step = 0;
+      return;
+    }
+    seq = line.b;
+    x = line.x;
+    w.q = line.q;
+    w.off = line.off;
+    units = q4_units(w.q, a.shape), tiles = q4_tiles(w.q, a.shape);
     const int64_t k = plan_div(y0 - x, units);
     x += k * units;
     w.kvh = (int)plan_div(k, tiles);
     w.tile = (int)(k - (int64_t)w.kvh * tiles);
-  }
-  if (tid == 0) {
-    Q4Cut c = {};
-    if (x < y0 && y0 - line.step <= x) {
-      const TileRows rows = q4_rows(w.q, a.shape, w.tile, c.used);
-      c.x0 = x;
-      c.step = line.step;
-      c.head = ((int64_t)layer * a.T + w.off) * H_q + w.kvh * a.g;
-      c.units = units;
-      c.count = tile_blocks(rows, kBn2).count;
-      c.row_1 = w.tile * a.shape.rows;
+    if (tid == 0) {
+      Q4Cut c = {};
+      if (x < y0 && y0 - line.step <= x) {
+        const TileRows rows = q4_rows(w.q, a.shape, w.tile, c.used);
+        c.x0 = x;
+        c.step = line.step;
+        c.head = ((int64_t)layer * a.T + w.off) * H_q + w.kvh * a.g;
+        c.units = units;
+        c.count = tile_blocks(rows, kBn2).count;
+        c.row_1 = w.tile * a.shape.rows;
+      }
+      *cut_at(a, D, layer, cta) = c;
     }
-    *cut_at(a, D, layer, cta) = c;
   }
   // this lane's row and 16-byte piece of an ldmatrix of four, and its row of one of two
   const uint32_t at4 = (lane & 15) * C::kRow + 16 * (lane >> 4);
@@ -333,8 +365,15 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   for (; x < y1 && !gave_up; x += units) {
   w.rows = q4_rows(w.q, a.shape, w.tile, w.used);
   w.blocks = tile_blocks(w.rows, kBn2);
-  const int blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
-  if (blk0 < blk1) {
+  int blk0, blk1;
+  if constexpr (CL) {
+    const int rank = blockIdx.x % kCluster;
+    blk0 = rank * w.blocks.count / kCluster;
+    blk1 = bad ? blk0 : (rank + 1) * w.blocks.count / kCluster;
+  } else {
+    blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
+  }
+  if (CL || blk0 < blk1) {
   // this warp's copies: its rows of each block
   const int64_t row0 = ((int64_t)(a.layer0 + layer) * a.H_kv + w.kvh) * a.S_total + a.seq_off[seq];
   const uint8_t *gk = a.K + row0 * C::kRow, *gv = a.V + row0 * C::kRow;
@@ -705,7 +744,8 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
     }
   }
   __syncthreads();
-  const bool alone = blk0 == 0 && blk1 == w.blocks.count;
+  const bool alone = !CL && blk0 == 0 && blk1 == w.blocks.count;
+  float *s_part = (float *)(smem + C::kOut);  // [row][D + 4], as in the workspace
   for (int r = warp; r < w.used; r += kWarps) {
     float mx = kNone;
 #pragma unroll
@@ -724,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
     }
     const int rr = r + row_1;
     const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
-    float *part = part_row<D>(a, layer, cta, x < y0 ? 0 : 1, r);
+    float *part = CL ? s_part + r * (D + 4) : part_row<D>(a, layer, cta, x < y0 ? 0 : 1, r);
     const float inv = sl != 0.f ? 1.f / sl : 0.f;
 #pragma unroll
     for (int e = lane; e < D; e += 32) {
@@ -745,6 +785,46 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
             make_float4(mx * 0.6931471805599453f, sl,
                         logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
     }
+  }
+  if constexpr (CL) {
+    // the cluster's results: a warp 32 elements of a row, lane k the k-th CTA's statistics
+    cg::cluster_group cl = cg::this_cluster();
+    __shared__ int s_no;
+    if (tid == 0) s_no = bad || gave_up;
+    cl.sync();
+    bool no = false;
+    for (int k = 0; k < kCluster; ++k) no |= *cl.map_shared_rank(&s_no, k) != 0;
+    const int n = no ? 0 : w.used * (D / 32);
+    for (int i = (int)cl.block_rank() * kWarps + warp; i < n; i += kCluster * kWarps) {
+      const int r = i / (D / 32), e = i % (D / 32) * 32 + lane;
+      const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % kCluster) + r * (D + 4) + D);
+      const bool any = v.y != 0.f;
+      const float mx = warp_max(any ? v.x : kNone), by = v.x - mx;
+      const float f = any ? exp2_fast(by) : 0.f;
+      float sl = f * v.y, sh = any ? f * __fmaf_rn(by, v.y, v.z) : 0.f, ss = f * v.w;
+#pragma unroll
+      for (int o = 1; o < kCluster; o <<= 1) {
+        sl += __shfl_xor_sync(0xffffffffu, sl, o);
+        sh += __shfl_xor_sync(0xffffffffu, sh, o);
+        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      }
+      float y = 0.f;
+#pragma unroll
+      for (int k = 0; k < kCluster; ++k) {
+        const float fk = __shfl_sync(0xffffffffu, f, k);
+        const float z = cl.map_shared_rank(s_part, k)[r * (D + 4) + e];
+        if (fk != 0.f) y += fk * z;
+      }
+      const float inv = sl != 0.f ? 1.f / sl : 0.f;
+      const int rr = r + row_1;
+      const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
+      ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(y * inv);
+      if (STATS && e == 0)
+        ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
+                                                logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
+    }
+    cl.sync();  // read before a CTA ends
+    return;
   }
   fence_proxy_async_smem();
   __syncthreads();  // the results have been read: the ring is the next piece's
@@ -859,14 +939,31 @@ __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs
                                             logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
 }
 
-template <int D, int NT, bool STATS>
-cudaError_t launch_nt(const Q4AttendArgs &a, cudaStream_t s) {
+template <int D, int NT, bool STATS, bool CL>
+cudaError_t launch_as(const Q4AttendArgs &a, cudaStream_t s) {
   using C = Q4Cfg<D, NT>;
   if constexpr (C::kSmem > 44 * 1024)  // (48 KB with the static arrays need no leave)
-    LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS>,
+    LG_TRY(cudaFuncSetAttribute(q4_attend_kernel<D, NT, STATS, CL>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
-  LG_TRY(launch_pdl(q4_attend_kernel<D, NT, STATS>, dim3(a.ctas, a.n_layers), kThreads, C::kSmem, s, a));
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.ctas, a.n_layers);
+  cfg.blockDim = kThreads;
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, q4_attend_kernel<D, NT, STATS, CL>, a);
+}
+
+template <int D, int NT, bool STATS>
+cudaError_t launch_nt(const Q4AttendArgs &a, cudaStream_t s) {
+  return a.cluster ? launch_as<D, NT, STATS, true>(a, s) : launch_as<D, NT, STATS, false>(a, s);
 }
 
 template <int D, bool STATS>
@@ -877,9 +974,10 @@ cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
     case 24: if constexpr (!STATS) LG_TRY((launch_nt<D, 3, STATS>(a, s))); break;
     default: if constexpr (!STATS) LG_TRY((launch_nt<D, 4, STATS>(a, s))); break;
   }
-  LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>, 
-                    dim3(a.ctas, (a.shape.rows + kMergeWarps - 1) / kMergeWarps, a.n_layers),
-                    32 * kMergeWarps, 0, s, a));
+  if (!a.cluster)
+    LG_TRY(launch_pdl(q4_merge_kernel<D, STATS>,
+                      dim3(a.ctas, (a.shape.rows + kMergeWarps - 1) / kMergeWarps, a.n_layers),
+                      32 * kMergeWarps, 0, s, a));
   return cudaGetLastError();
 }
 
@@ -893,8 +991,12 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
   // what the 152 SMs of a GB300 hold at once, over the layers; no more than there are blocks
   const int64_t fit = 152 * (r.rows <= 8 ? Q4_C1 : r.rows <= 16 ? Q4_C2 : r.rows <= 24 ? Q4_C3 : Q4_C4);
-  const int64_t most = batch * H_kv * tiles * (blocks + kQ4ItemUnits);
+  const int64_t most = (int64_t)batch * H_kv * tiles * (blocks + kQ4ItemUnits);
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
+  // few items of few blocks: a cluster each, which joins its results itself
+  const int64_t items = (int64_t)batch * H_kv * tiles;
+  r.cluster = items * n_layers * kCluster <= fit && blocks <= kCluster * kClusterBlocks;
+  if (r.cluster) r.ctas = (int)items * kCluster;
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
   r.part_bytes = (r.part_bytes + 255) / 256 * 256;
   return r;

@@ -36,6 +36,20 @@ def test_windows(cuda, d, g, window, sink):
     _check(q4_ref.Batch([300, 1, 900, 77], [4, 1, 2, 0], g=g, d=d, device=cuda).to_device(), window, sink)
 
 
+@pytest.mark.parametrize("d,g,most", [(64, 1, 1), (128, 4, 1), (64, 7, 4), (128, 2, 8), (128, 5, 5),
+                                      (128, 4, 13)])
+@pytest.mark.parametrize("window,sink", [(0, 0), (90, 5)])
+def test_many_sequences_in_one_line(cuda, d, g, most, window, sink):
+    """more items than clusters: CTAs whose share begins and ends inside items, empty sequences among
+    them"""
+    rng = np.random.default_rng(most)
+    ns = [int(x) for x in rng.integers(0, 700, 45)]
+    ns[3], ns[7], ns[44] = 1, 0, 1500
+    ms = [int(min(n, rng.integers(0, most + 1))) if most > 1 else int(n > 0) for n in ns]
+    ms[44] = most
+    _check(q4_ref.Batch(ns, ms, g=g, d=d, device=cuda).to_device(), window, sink)
+
+
 @pytest.mark.parametrize("d,g", [(64, 8), (128, 4), (128, 1)])
 @pytest.mark.parametrize("window,sink", [(0, 0), (50, 3)])
 def test_chunks(cuda, d, g, window, sink):
