@@ -103,7 +103,7 @@ AttendLayout attend_layout(const lg_cache *c, int H_q, int n_layers, int max_len
 }
 
 lg::Q4Grid q4_decode_grid(const lg_cache *c, int H_q, int n_layers, int max_len) {
-  return lg::q4_grid(n_layers, c->batch, c->H_kv, H_q / c->H_kv, c->d, 1, max_len);
+  return lg::q4_grid(n_layers, c->batch, c->H_kv, H_q / c->H_kv, c->d, 1, max_len, 0, 0);
 }
 
 // lg_decode_attend over a 4-bit cache

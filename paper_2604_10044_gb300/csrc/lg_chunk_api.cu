@@ -119,7 +119,7 @@ size_t q4_plane_bytes(const lg_cache *c) {
 
 size_t q4_chunk_bytes(const lg_cache *c, const lg_chunk *ch, int g, int max_len) {
   if (q4_few(ch, g)) {
-    const size_t n = lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len).part_bytes;
+    const size_t n = lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, 0, 0).part_bytes;
     return n > 256 ? n : 256;
   }
   return 2 * q4_plane_bytes(c) + part_bytes(lg::chunk_grid(LG_BF16, c->d, g, ch->max_new), c->d);
@@ -222,7 +222,7 @@ lg_status lg_chunk_attend(const lg_cache *c, const lg_chunk *ch, int layer, cons
     if (overlap(q, bytes, out, bytes)) return LG_ERR_INVALID_ARG;
     if (q4_few(ch, g)) {
       const lg::Q4Grid grid =
-          lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len);
+          lg::q4_grid(1, c->batch, c->H_kv, g, c->d, ch->max_new, max_len, window, n_sink);
       if (!lg::q4_grid_fits(1, c->batch, c->H_kv)) return LG_ERR_UNSUPPORTED;
       lg::Q4AttendArgs a = {};
       a.q = q;

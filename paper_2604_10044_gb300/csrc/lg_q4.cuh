@@ -127,7 +127,8 @@ struct Q4Grid {
   bool cluster;
   size_t part_bytes;
 };
-Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len);
+Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,
+               int sink);
 cudaError_t launch_q4_attend(const Q4AttendArgs &a, int d, cudaStream_t s);
 
 // the kernels' grids fit their limits

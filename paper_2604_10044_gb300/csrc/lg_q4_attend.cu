@@ -39,7 +39,7 @@
 #define Q4_C1 3
 #endif
 #ifndef Q4_C2
-#define Q4_C2 3
+#define Q4_C2 2
 #endif
 #ifndef Q4_C3
 #define Q4_C3 2
@@ -52,6 +52,9 @@
 #endif
 #ifndef Q4_S1
 #define Q4_S1 2
+#endif
+#ifndef Q4_J2
+#define Q4_J2 2
 #endif
 #ifndef Q4_S2
 #define Q4_S2 3
@@ -69,6 +72,9 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
 constexpr int kBn2 = kQ4Bn2;         // a CTA's block: kWarps tiles
 constexpr unsigned kCluster = 8;
+#ifndef Q4_CW
+#define Q4_CW 1
+#endif
 #ifndef Q4_CB
 #define Q4_CB 8
 #endif
@@ -84,7 +90,7 @@ struct Q4Cfg {
   static constexpr int kTile = kSub * kRow;         // of keys, or of values
   static constexpr int kCtas = NT == 1 ? Q4_C1 : NT == 2 ? Q4_C2 : NT == 3 ? Q4_C3 : Q4_C4;  // of an SM
   static constexpr int kStages = D == 64 ? 4 : NT == 1 ? Q4_S1 : NT == 2 ? Q4_S2 : NT == 3 ? Q4_S3 : 4;
-  static constexpr int kJoint = NT == 1 ? Q4_J1 : 1;    // products of 16 rows that go through the softmax together
+  static constexpr int kJoint = NT == 1 ? Q4_J1 : NT == 2 ? Q4_J2 : 1;    // products of 16 rows that go through the softmax together
   static constexpr int kRing = kWarps * kStages * 2 * kTile;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
@@ -983,7 +989,8 @@ cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
 
 }  // namespace
 
-Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len) {
+Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,
+               int sink) {
   Q4Grid r;
   const int64_t rows = (int64_t)max_new * g;
   r.rows = rows >= 32 ? 32 : (int)((rows + 7) / 8 * 8);
@@ -993,12 +1000,14 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   const int64_t fit = 152 * (r.rows <= 8 ? Q4_C1 : r.rows <= 16 ? Q4_C2 : r.rows <= 24 ? Q4_C3 : Q4_C4);
   const int64_t most = (int64_t)batch * H_kv * tiles * (blocks + kQ4ItemUnits);
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
-  // few items of few blocks: a cluster each, which joins its results itself
-  const int64_t items = (int64_t)batch * H_kv * tiles;
-  r.cluster = items * n_layers * kCluster <= fit && blocks <= kCluster * kClusterBlocks;
-  if (r.cluster) r.ctas = (int)items * kCluster;
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
   r.part_bytes = (r.part_bytes + 255) / 256 * 256;
+  // few items of few blocks: a cluster each, which joins its results itself
+  const int64_t items = (int64_t)batch * H_kv * tiles;
+  const Q4Shape shape{r.rows, g, window, sink, H_kv};
+  const int one = q4_units(ChunkSeq{max_len, max_new < max_len ? max_new : max_len}, shape) - kQ4ItemUnits;
+  r.cluster = items * n_layers * kCluster <= fit * Q4_CW && one <= (int)kCluster * kClusterBlocks;
+  if (r.cluster) r.ctas = (int)items * kCluster;
   return r;
 }
 

@@ -48,6 +48,7 @@ struct RowPart {     // of a slice of a row
 struct Heat {
   float hi, lo;
   bool greedy;
+  double both;  // log2(e) / temperature again, 0 for the top token
 };
 constexpr float kFar = -0x1p60f;
 
@@ -56,12 +57,14 @@ __device__ __forceinline__ float clamp_temperature(float t) {
 }
 
 __device__ __forceinline__ Heat heat_of(float t) {
-  Heat h{0.f, 0.f, !(t > 0.f)};
+  Heat h{0.f, 0.f, !(t > 0.f), 0.0};
   if (h.greedy) return h;
   const double e = 1.4426950408889634;
   const float e_hi = (float)e, e_lo = (float)(e - (double)e_hi);
   h.hi = __fdiv_rn(e_hi, t);
-  h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t) * 0.6931471805599453f;
+  h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t);
+  h.both = (double)h.hi + (double)h.lo;
+  h.lo *= 0.6931471805599453f;
   return h;
 }
 
@@ -204,6 +207,8 @@ struct Row {
   float m;    // largest logit
   int at;     // its lowest place
   double z;   // sum of exp((x - m) / temperature); 0: nothing is left
+  float inv_hi, inv_lo;  // 1 / z
+  int fallen; // the row's draft, -1 for a last row
 };
 
 // 2^y, y <= 0, in 64 bits within 2^-40: the whole part into the exponent, the power series of the rest
@@ -228,7 +233,7 @@ __device__ __forceinline__ double power_of_two(double y) {
 // a row's slices joined; every lane of a warp calls it.  heat: log2(e) / temperature, 0 for the top token
 __device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double heat, int lane) {
   const RowPart *p = a.part + row * a.slices;
-  Row r{-INFINITY, 0x7fffffff, 0.0};
+  Row r{-INFINITY, 0x7fffffff, 0.0, 0.f, 0.f, -1};
   for (int i = lane; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
   r.m = warp_max(r.m);
   if (r.m == -INFINITY) return r;
@@ -284,7 +289,6 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   __shared__ Part s_part;
   __shared__ uint64_t s_warp[kPickWarps], s_seg[kPickWarps][kSegsKept];
   __shared__ int s_first, s_bad;
-  __shared__ double s_heat, s_inv;
   __shared__ Row s_row, s_rows[kRowsKept];
   pdl_enter();
   if (tid == 0) s_bad = status_bad(a.status);
@@ -295,78 +299,87 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
     return;
   }
-  if (tid == 0) {
-    s_first = max(m - 1, 0);
-    s_heat = t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
-  }
+  if (tid == 0) s_first = max(m - 1, 0);
   __syncthreads();
   const Heat h = heat_of(t);
-  const double heat = s_heat;
+  const double heat = h.both;
   // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have read
   // another one
   const bool bad = s_bad != 0;
   // the first draft that does not stand: a warp a row
   for (int j = warp; j < m && !bad; j += kPickWarps) {
     const int64_t row = o0 + j;
-    const Row r = join_row(a, row, heat, lane);
+    // (the draft's numbers are asked for before the row's slices)
+    const int y = j < m - 1 ? a.tokens[row + 1] : -1;
+    const float u = j < m - 1 ? a.u[row] : 0.f;
+    float q = 1.f, x = 0.f;
+    if (y >= 0 && y < V) {
+      if (a.has_draft) q = draft_at<Q>(a, row, y);
+      x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
+    }
+    Row r = join_row(a, row, heat, lane);
     if (lane == 0) {
-      if (j < kRowsKept) s_rows[j] = r;
       bool stands = j == m - 1;
-      const int y = stands ? -1 : a.tokens[row + 1];
       if (y >= 0 && y < V && r.z > 0.0) {
-        const float q = a.has_draft ? draft_at<Q>(a, row, y) : 1.f;
-        const float x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
         double e;  // the token's weight
         if (h.greedy)
           e = y == r.at ? 1.0 : 0.0;
         else
           e = x == r.m ? 1.0 : power_of_two(((double)x - (double)r.m) * heat);
-        stands = (double)a.u[row] * (double)q * r.z < e;
+        stands = (double)u * (double)q * r.z < e;
       }
       if (!stands) atomicMin(&s_first, j);
+      const double inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
+      r.inv_hi = (float)inv;
+      r.inv_lo = (float)(inv - (double)r.inv_hi);
+      r.fallen = y;
+      if (j < kRowsKept) s_rows[j] = r;
     }
   }
   __syncthreads();
   const int first = s_first;
   const int64_t row = o0 + first;
-  Row r{-INFINITY, 0x7fffffff, 0.0};
+  Row r{-INFINITY, 0x7fffffff, 0.0, 0.f, 0.f, -1};
   if (m > 0 && !bad) {
     if (first < kRowsKept) {
       r = s_rows[first];
     } else {
       if (warp == 0) {
-        const Row j = join_row(a, row, heat, lane);
-        if (lane == 0) s_row = j;
+        Row j = join_row(a, row, heat, lane);
+        if (lane == 0) {
+          const double inv = j.z > 0.0 ? 1.0 / j.z : 0.0;
+          j.inv_hi = (float)inv;
+          j.inv_lo = (float)(inv - (double)j.inv_hi);
+          j.fallen = first < m - 1 ? a.tokens[row + 1] : -1;
+          s_row = j;
+        }
       }
       __syncthreads();
       r = s_row;
     }
   }
   const bool fell = first < m - 1;
-  const int fallen = fell && !bad ? a.tokens[row + 1] : -1;
+  const int fallen = r.fallen;
   // the distribution of the next token, p less what the draft had of it
   const T *x = (const T *)a.x.x + row * a.x.stride;
   const Q *dq = a.has_draft && fell && fallen >= 0 && fallen < V
                     ? (const Q *)a.draft.x + row * a.draft.stride
                     : nullptr;
-  if (tid == 0) s_inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
-  __syncthreads();
-  const double inv = s_inv;
-  const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
+  const float inv_hi = r.inv_hi, inv_lo = r.inv_lo;
   // what is taken off p: nothing, the draft's row, or all of the fallen token
   enum { kNothing, kRow, kToken };
   int less = !fell ? kNothing : dq ? kRow : a.has_draft ? kNothing : kToken;
-  // the masses of a lane's elements i0, i0 + 32, .. of a segment, all of them loaded first (from
+  // the masses of a lane's elements i0, i0 + step, .. of a segment, all of them loaded first (from
   // the last place on where the row ends: their masses are zeros)
-  auto masses_of = [&](auto kind, int i0, float (&w)[kSeg]) {
+  auto masses_of = [&](auto kind, int i0, int step, float (&w)[kSeg]) {
     constexpr int kKind = decltype(kind)::value;
     T v[kSeg];
     Q q[kSeg];
 #pragma unroll
-    for (int k = 0; k < kSeg; ++k) v[k] = x[min(i0 + 32 * k, V - 1)];
+    for (int k = 0; k < kSeg; ++k) v[k] = x[min(i0 + step * k, V - 1)];
     if constexpr (kKind == kRow) {
 #pragma unroll
-      for (int k = 0; k < kSeg; ++k) q[k] = dq[min(i0 + 32 * k, V - 1)];
+      for (int k = 0; k < kSeg; ++k) q[k] = dq[min(i0 + step * k, V - 1)];
     }
 #pragma unroll
     for (int k = 0; k < kSeg; k += 2) {
@@ -379,7 +392,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int i = i0 + 32 * (k + c);
+        const int i = i0 + step * (k + c);
         const float ec = c ? e.y : e.x;
         float qc = 0.f;
         if constexpr (kKind == kRow) qc = fmaxf((float)q[k + c], 0.f);
@@ -389,13 +402,13 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       }
     }
   };
-  auto masses = [&](int i0, float (&w)[kSeg]) {
+  auto masses = [&](int i0, int step, float (&w)[kSeg]) {
     if (less == kRow)
-      masses_of(std::integral_constant<int, kRow>(), i0, w);
+      masses_of(std::integral_constant<int, kRow>(), i0, step, w);
     else if (less == kToken)
-      masses_of(std::integral_constant<int, kToken>(), i0, w);
+      masses_of(std::integral_constant<int, kToken>(), i0, step, w);
     else
-      masses_of(std::integral_constant<int, kNothing>(), i0, w);
+      masses_of(std::integral_constant<int, kNothing>(), i0, step, w);
   };
   auto warp_sum = [&](uint64_t s) {
 #pragma unroll
@@ -413,7 +426,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     if (look)
       for (int g = g0; g < g1; ++g) {
         float w[kSeg];
-        masses(g * kSegElems + lane, w);
+        masses(g * kSegElems + lane, 32, w);
         const uint64_t sum = warp_sum(lane_units(w));
         if (g - g0 < kSegsKept && lane == 0) s_seg[warp][g - g0] = sum;
         s += sum;
@@ -444,37 +457,50 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (want >= total) want = total ? total - 1 : 0;
   for (int w = 0; w < warp; ++w) before += s_warp[w];
   if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
-    int token = -1, last = -1;
-    for (int g = g0; g < g1; ++g) {
-      if (g - g0 < kSegsKept && want >= before + s_seg[warp][g - g0]) {
-        before += s_seg[warp][g - g0];
-        continue;
+    int g = g0;
+    for (; g < g1 - 1; ++g) {
+      uint64_t sum;
+      if (g - g0 < kSegsKept) {
+        sum = s_seg[warp][g - g0];
+      } else {
+        float w[kSeg];
+        masses(g * kSegElems + lane, 32, w);
+        sum = warp_sum(lane_units(w));
       }
-      float w[kSeg];
-      masses(g * kSegElems + lane, w);
-      const uint64_t s = warp_sum(lane_units(w));
-      if (want >= before + s) {
-        before += s;
-        continue;
-      }
-      // (the elements' own units may stay short of their lanes' sums by roundings: the last then)
+      if (want < before + sum) break;
+      before += sum;
+    }
+    // the segment again with neighbours in a lane: the lanes' sums, then the elements of one lane.  (They
+    // may stay short of the sum above by roundings: the last element that has a mass then.)
+    const int i0 = g * kSegElems + lane * kSeg;
+    float w[kSeg];
+    masses(i0, 1, w);
+    uint64_t own = 0;
+    int last = -1;
+#pragma unroll
+    for (int k = 0; k < kSeg; ++k) {
+      own += units_of(w[k]);
+      if (w[k] > 0.f) last = i0 + k;
+    }
+    uint64_t upto = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t u = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += u;
+    }
+    const unsigned over = __ballot_sync(0xffffffffu, before + upto > want);
+    const unsigned any = __ballot_sync(0xffffffffu, last >= 0);
+    if (over ? lane == __ffs((int)over) - 1 : any && lane == 31 - __clz((int)any)) {
+      uint64_t c = before + upto - own;
+      int token = last;
 #pragma unroll
       for (int k = 0; k < kSeg; ++k) {
-        const unsigned any = __ballot_sync(0xffffffffu, w[k] > 0.f);
-        if (any) last = g * kSegElems + 32 * k + 31 - __clz((int)any);
-        uint64_t c = units_of(w[k]);
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint64_t u = __shfl_up_sync(0xffffffffu, c, o);
-          if (lane >= o) c += u;
-        }
-        const unsigned over = __ballot_sync(0xffffffffu, before + c > want);
-        if (over && token < 0) token = g * kSegElems + 32 * k + __ffs((int)over) - 1;
-        before += __shfl_sync(0xffffffffu, c, 31);
+        const bool below = c <= want;
+        c += units_of(w[k]);
+        if (below && c > want) token = i0 + k;
       }
-      break;
+      a.picked[row] = token;
     }
-    if (lane == 0) a.picked[row] = token >= 0 ? token : last;
   }
   if (rank == 0) {
     if (tid == 0) {
