@@ -25,18 +25,24 @@ constexpr uint32_t kQ4NaN = 0x7fffu;  // the word of such a group: scale NaN, le
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// the eight values of a word as bf16, lo + s c rounded once
+// Masked codes of a word as they stand: c (bits 0-3 of either half) or 16 c (bits 4-7) in units of 2^-133,
+// the least bf16 number.
+constexpr uint32_t kQ4Low = 0x000f000fu, kQ4High = 0x00f000f0u;
+
+// the eight values of a word as bf16, lo + s c rounded once: a code times 2^127 is c / 64 or c / 4 exactly,
+// which 64 s or 4 s make up for
 __device__ __forceinline__ uint4 q4_values(uint32_t word, uint32_t par) {
-  const float s = bf16_low(par), lo = bf16_high(par);
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t x = word >> (4 * i);
-    const float a = (float)(x & 15u), b = (float)(x >> 16 & 15u);
-    const __nv_bfloat162 h = __floats2bfloat162_rn(__fmaf_rn(a, s, lo), __fmaf_rn(b, s, lo));
-    r[i] = *(const uint32_t *)&h;
-  }
-  return make_uint4(r[0], r[1], r[2], r[3]);
+  auto two = [](uint32_t x) { return *(const __nv_bfloat162 *)&x; };
+  const __nv_bfloat162 by = two(0x7f007f00u);
+  const __nv_bfloat162 s = two(__byte_perm(par, par, 0x1010)), lo = two(__byte_perm(par, par, 0x3232));
+  const __nv_bfloat162 s64 = __hmul2(s, two(0x42804280u)), s4 = __hmul2(s, two(0x40804080u));
+  auto value = [&](uint32_t raw, const __nv_bfloat162 &scale) {
+    const __nv_bfloat162 r = __hfma2(__hmul2(two(raw), by), scale, lo);
+    return *(const uint32_t *)&r;
+  };
+  const uint32_t up = word >> 8;
+  return make_uint4(value(word & kQ4Low, s64), value(word & kQ4High, s4), value(up & kQ4Low, s64),
+                    value(up & kQ4High, s4));
 }
 
 // The word of eight elements and their group's parameter word.  LANES neighbouring lanes hold the

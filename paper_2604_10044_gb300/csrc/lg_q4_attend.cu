@@ -139,8 +139,6 @@ __device__ __forceinline__ uint32_t centred(uint32_t raw, bool high) {
   return *(const uint32_t *)&r;
 }
 
-constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
-
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -512,8 +510,8 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
               const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
-              const uint32_t fa[4] = {wa & kLow, wa & kHigh, va & kLow, va & kHigh};
-              const uint32_t fb[4] = {wb & kLow, wb & kHigh, vb & kLow, vb & kHigh};
+              const uint32_t fa[4] = {wa & kQ4Low, wa & kQ4High, va & kQ4Low, va & kQ4High};
+              const uint32_t fb[4] = {wb & kQ4Low, wb & kQ4High, vb & kQ4Low, vb & kQ4High};
 #pragma unroll
               for (int gi = 0; gi < 4 / kPieces; ++gi) {
                 const int gr = (j2 + jj) * (4 / kPieces) + gi;
@@ -663,10 +661,10 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
               const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
-              const uint32_t fa[4] = {centred(wa & kLow, false), centred(wa & kHigh, true),
-                                      centred(ua & kLow, false), centred(ua & kHigh, true)};
-              const uint32_t fb[4] = {centred(wb & kLow, false), centred(wb & kHigh, true),
-                                      centred(ub & kLow, false), centred(ub & kHigh, true)};
+              const uint32_t fa[4] = {centred(wa & kQ4Low, false), centred(wa & kQ4High, true),
+                                      centred(ua & kQ4Low, false), centred(ua & kQ4High, true)};
+              const uint32_t fb[4] = {centred(wb & kQ4Low, false), centred(wb & kQ4High, true),
+                                      centred(ub & kQ4Low, false), centred(ub & kQ4High, true)};
 #pragma unroll
               for (int gi = 0; gi < 4 / kPieces; ++gi) {
                 const int gr = (j2 + jj) * (4 / kPieces) + gi;
@@ -884,24 +882,21 @@ __global__ void __launch_bounds__(32 * kMergeWarps) q4_merge_kernel(Q4AttendArgs
   if (w.step == 0 || r0 >= w.used) return;
   const int c0 = blockIdx.x - 1;  // the CTA that the item began in
   auto cut = [&](int c) { return q4_cut(c * w.step - w.x0, w.count); };  // blocks before CTA c
-  // one part has every block and wrote the result: the first that has any, then
-  int some = c0 + 1;
-  while (cut(some) == 0) ++some;
-  if (cut(some) == w.count) return;
-  int parts = (int)plan_div(w.x0 + w.units - 1, w.step) + 1 - c0;
-  auto has = [&](int k) { return cut(c0 + k) < cut(c0 + k + 1); };
+  // where one part has every block, its CTA wrote the result
+  int p0 = 0, p1 = (int)plan_div(w.x0 + w.units - 1, w.step) + 1 - c0;  // the parts with blocks
+  while (cut(c0 + p0 + 1) == 0) ++p0;
+  while (cut(c0 + p1 - 1) == w.count) --p1;
+  if (p1 - p0 == 1) return;
   int share2 = 0;  // log2 of the warps of a row
   while (min(w.used - r0, kMergeWarps) << (share2 + 1) <= kMergeWarps) ++share2;
   const int r = r0 + (warp >> share2), sub = warp & ((1 << share2) - 1);
   float mx = kNone, sl = 0.f, sh = 0.f, ss = 0.f, x[kE] = {};
   if (r < w.used) {
     auto part_of = [&](int k) { return part_row<D>(a, layer, c0 + k, k == 0, r); };
-    for (int c = lane; c < parts; c += 32)
-      if (has(c)) mx = fmaxf(mx, part_of(c)[D]);
+    for (int c = p0 + lane; c < p1; c += 32) mx = fmaxf(mx, part_of(c)[D]);
     mx = warp_max(mx);
 #pragma unroll 4
-    for (int c = sub; c < parts; c += 1 << share2) {
-      if (!has(c)) continue;
+    for (int c = p0 + sub; c < p1; c += 1 << share2) {
       const float *part = part_of(c);
       const float4 v = *(const float4 *)(part + D);
       float y[kE];

@@ -230,13 +230,17 @@ __device__ __forceinline__ double power_of_two(double y) {
   return p * __hiloint2double(((int)whole + 1023) << 20, 0);
 }
 
-// a row's slices joined; every lane of a warp calls it.  heat: log2(e) / temperature, 0 for the top token
-__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double heat, int lane) {
+// a row's slices joined, and the weight e of a logit x; every lane of a warp calls it.  heat:
+// log2(e) / temperature, 0 for the top token
+__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double heat, int lane, float x,
+                                        double &e) {
   const RowPart *p = a.part + row * a.slices;
   Row r{-INFINITY, 0x7fffffff, 0.0, 0.f, 0.f, -1};
   for (int i = lane; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
   r.m = warp_max(r.m);
+  e = 0.0;
   if (r.m == -INFINITY) return r;
+  e = x == r.m ? 1.0 : power_of_two(((double)x - (double)r.m) * heat);
   for (int i = lane; i < a.slices; i += 32) {
     const RowPart s = p[i];
     if (s.m == r.m) r.at = min(r.at, s.at);
@@ -248,6 +252,10 @@ __device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double
 #pragma unroll
   for (int o = 16; o; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
   if (!(heat > 0.0)) r.z = 1.0;
+  if (r.z > 0.0) {  // its reciprocal in two terms
+    r.inv_hi = __frcp_rn((float)r.z);
+    r.inv_lo = (float)(fma(-(double)r.inv_hi, r.z, 1.0) * (double)r.inv_hi);
+  }
   return r;
 }
 
@@ -286,7 +294,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int n_cta = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int b = blockIdx.x / n_cta;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ Part s_part;
+  __shared__ Part s_part[2][16];  // of every CTA of the cluster, for each pass: put there by that CTA
   __shared__ uint64_t s_warp[kPickWarps], s_seg[kPickWarps][kSegsKept];
   __shared__ int s_first, s_bad;
   __shared__ Row s_row, s_rows[kRowsKept];
@@ -317,21 +325,15 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       if (a.has_draft) q = draft_at<Q>(a, row, y);
       x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
     }
-    Row r = join_row(a, row, heat, lane);
+    double e;  // the draft's weight
+    Row r = join_row(a, row, heat, lane, x, e);
     if (lane == 0) {
       bool stands = j == m - 1;
       if (y >= 0 && y < V && r.z > 0.0) {
-        double e;  // the token's weight
-        if (h.greedy)
-          e = y == r.at ? 1.0 : 0.0;
-        else
-          e = x == r.m ? 1.0 : power_of_two(((double)x - (double)r.m) * heat);
+        if (h.greedy) e = y == r.at ? 1.0 : 0.0;
         stands = (double)u * (double)q * r.z < e;
       }
       if (!stands) atomicMin(&s_first, j);
-      const double inv = r.z > 0.0 ? 1.0 / r.z : 0.0;
-      r.inv_hi = (float)inv;
-      r.inv_lo = (float)(inv - (double)r.inv_hi);
       r.fallen = y;
       if (j < kRowsKept) s_rows[j] = r;
     }
@@ -345,11 +347,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       r = s_rows[first];
     } else {
       if (warp == 0) {
-        Row j = join_row(a, row, heat, lane);
+        double e;
+        Row j = join_row(a, row, heat, lane, 0.f, e);
         if (lane == 0) {
-          const double inv = j.z > 0.0 ? 1.0 / j.z : 0.0;
-          j.inv_hi = (float)inv;
-          j.inv_lo = (float)(inv - (double)j.inv_hi);
           j.fallen = first < m - 1 ? a.tokens[row + 1] : -1;
           s_row = j;
         }
@@ -433,21 +433,21 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       }
     if (lane == 0) s_warp[warp] = s;
     __syncthreads();
-    if (tid == 0) {
+    if (tid < n_cta) {
       uint64_t sum = 0;
+#pragma unroll
       for (int w = 0; w < kPickWarps; ++w) sum += s_warp[w];
-      s_part = Part{sum, bad};
+      cl.map_shared_rank(s_part[pass], tid)[rank] = Part{sum, bad};
     }
     cl.sync();
     total = before = 0;
     bool stop = false;
     for (int c = 0; c < n_cta; ++c) {
-      const Part v = *cl.map_shared_rank(&s_part, c);
+      const Part v = s_part[pass][c];
       if (c < rank) before += v.total;
       total += v.total;
       stop |= v.bad != 0;
     }
-    cl.sync();  // read by all before it is written again, or its CTA ends
     if (stop) return;
     if (total || less == kNothing || !look) break;
     less = kNothing;
