@@ -9,7 +9,7 @@
 // moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's bounds
 // on the way.  So weights go into the sums as integers in units of 2^-62 (of a mass of one), which add
 // up in any order and division to the same; the quotient by a temperature keeps a second term; and
-// what is formed once a row (the joining of slices, the test of a draft) is in 64 bits.
+// the joining of a row's slices is in integers too, with powers of two to 2^-31.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -48,7 +48,7 @@ struct RowPart {     // of a slice of a row
 struct Heat {
   float hi, lo;
   bool greedy;
-  double both;  // log2(e) / temperature again, 0 for the top token
+  float lo2;  // the second term as it is
 };
 constexpr float kFar = -0x1p60f;
 
@@ -57,13 +57,13 @@ __device__ __forceinline__ float clamp_temperature(float t) {
 }
 
 __device__ __forceinline__ Heat heat_of(float t) {
-  Heat h{0.f, 0.f, !(t > 0.f), 0.0};
+  Heat h{0.f, 0.f, !(t > 0.f), 0.f};
   if (h.greedy) return h;
   const double e = 1.4426950408889634;
   const float e_hi = (float)e, e_lo = (float)(e - (double)e_hi);
   h.hi = __fdiv_rn(e_hi, t);
   h.lo = __fdiv_rn(__fmaf_rn(-h.hi, t, e_hi) + e_lo, t);
-  h.both = (double)h.hi + (double)h.lo;
+  h.lo2 = h.lo;
   h.lo *= 0.6931471805599453f;
   return h;
 }
@@ -200,61 +200,68 @@ constexpr int kPickThreads = 512;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kSeg = 16;             // elements a lane and segment
 constexpr int kSegElems = 32 * kSeg;
-constexpr int kSegsKept = 32;        // sums of a warp's segments that are kept
+constexpr int kSegsKept = ((1 << 20) / kSegElems + kPickWarps - 1) / kPickWarps;  // of a warp, at most
 constexpr int kRowsKept = 64;        // rows of a sequence that are joined once
 
 struct Row {
   float m;    // largest logit
   int at;     // its lowest place
-  double z;   // sum of exp((x - m) / temperature); 0: nothing is left
+  uint64_t z; // sum of exp((x - m) / temperature) in 2^-40; 0: nothing is left
   float inv_hi, inv_lo;  // 1 / z
   int fallen; // the row's draft, -1 for a last row
 };
 
-// 2^y, y <= 0, in 64 bits within 2^-40: the whole part into the exponent, the power series of the rest
-// (2^f = sum of (f ln 2)^k / k!, |f| <= 1/2, to k = 10)
-__device__ __forceinline__ double power_of_two(double y) {
-  if (!(y > -1000.0)) return 0.0;
-  const double whole = rint(y), f = (y - whole) * 0.6931471805599453;
-  double p = 1.0 / 3628800.0;
-  p = fma(p, f, 1.0 / 362880.0);
-  p = fma(p, f, 1.0 / 40320.0);
-  p = fma(p, f, 1.0 / 5040.0);
-  p = fma(p, f, 1.0 / 720.0);
-  p = fma(p, f, 1.0 / 120.0);
-  p = fma(p, f, 1.0 / 24.0);
-  p = fma(p, f, 1.0 / 6.0);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.0);
-  p = fma(p, f, 1.0);
-  return p * __hiloint2double(((int)whole + 1023) << 20, 0);
+// v exp((x - m) / temperature), x <= m, in integers (64-bit floating point runs at a hundredth of their
+// speed here: it made this step 5 us of a call).  The exponent is a distance without error times two
+// terms, in units of 2^-32; the power of two of its fraction is the power series sum of (f ln 2)^k / k!
+// to k = 11, every term positive, cut to 2^-32 at each step.
+__device__ __forceinline__ uint64_t scaled(uint64_t v, float x, float m, const Heat &h) {
+  if (x == m) return v;
+  const float d = x - m, back = d - x, rest = (x - (d - back)) - (m + back);  // x - m = d + rest
+  const float y = d * h.hi;
+  if (!(y > -100.f)) return 0;
+  const float y2 = __fmaf_rn(d, h.hi, -y) + __fmaf_rn(d, h.lo2, rest * h.hi);
+  const int64_t e = __float2ll_rd(y * 0x1p32f) + __float2ll_rd(y2 * 0x1p32f);
+  const int down = -(int)(e >> 32);
+  const uint32_t f = (uint32_t)e;
+  uint32_t p = 2u;  // (ln 2)^11 / 11! in 2^-32, and so on
+  p = 30u + __umulhi(p, f);
+  p = 437u + __umulhi(p, f);
+  p = 5676u + __umulhi(p, f);
+  p = 65510u + __umulhi(p, f);
+  p = 661577u + __umulhi(p, f);
+  p = 5726720u + __umulhi(p, f);
+  p = 41309550u + __umulhi(p, f);
+  p = 238388332u + __umulhi(p, f);
+  p = 1031764991u + __umulhi(p, f);
+  p = 2977044472u + __umulhi(p, f);
+  const uint64_t all = v + __umul64hi(v, (uint64_t)__umulhi(p, f) << 32);
+  return down < 64 ? all >> down : 0;
 }
 
-// a row's slices joined, and the weight e of a logit x; every lane of a warp calls it.  heat:
-// log2(e) / temperature, 0 for the top token
-__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, double heat, int lane, float x,
-                                        double &e) {
+// a row's slices joined; every lane of a warp calls it
+__device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, const Heat &h, int lane) {
   const RowPart *p = a.part + row * a.slices;
-  Row r{-INFINITY, 0x7fffffff, 0.0, 0.f, 0.f, -1};
-  for (int i = lane; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
+  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, -1};
+  const RowPart mine = lane < a.slices ? p[lane] : RowPart{-INFINITY, 0, 0};
+  r.m = mine.m;
+  for (int i = lane + 32; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
   r.m = warp_max(r.m);
-  e = 0.0;
   if (r.m == -INFINITY) return r;
-  e = x == r.m ? 1.0 : power_of_two(((double)x - (double)r.m) * heat);
   for (int i = lane; i < a.slices; i += 32) {
-    const RowPart s = p[i];
+    const RowPart s = i == lane ? mine : p[i];
     if (s.m == r.m) r.at = min(r.at, s.at);
-    if (heat > 0.0 && s.z)
-      r.z += (double)s.z * 0x1p-40 *
-             (s.m == r.m ? 1.0 : power_of_two(((double)s.m - (double)r.m) * heat));
+    if (!h.greedy && s.z) r.z += scaled(s.z, s.m, r.m, h);
   }
   r.at = __reduce_min_sync(0xffffffffu, r.at);
 #pragma unroll
   for (int o = 16; o; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
-  if (!(heat > 0.0)) r.z = 1.0;
-  if (r.z > 0.0) {  // its reciprocal in two terms
-    r.inv_hi = __frcp_rn((float)r.z);
-    r.inv_lo = (float)(fma(-(double)r.inv_hi, r.z, 1.0) * (double)r.inv_hi);
+  if (h.greedy) r.z = 1ull << 40;
+  if (r.z) {  // its reciprocal in two terms
+    const float zh = (float)r.z, zl = (float)(int64_t)(r.z - (uint64_t)zh);
+    const float inv = __frcp_rn(zh);
+    r.inv_hi = inv * 0x1p40f;
+    r.inv_lo = (__fmaf_rn(-inv, zh, 1.f) - inv * zl) * r.inv_hi;
   }
   return r;
 }
@@ -310,7 +317,6 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (tid == 0) s_first = max(m - 1, 0);
   __syncthreads();
   const Heat h = heat_of(t);
-  const double heat = h.both;
   // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have read
   // another one
   const bool bad = s_bad != 0;
@@ -325,13 +331,13 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       if (a.has_draft) q = draft_at<Q>(a, row, y);
       x = logit<T>((const T *)a.x.x + row * a.x.stride, y);
     }
-    double e;  // the draft's weight
-    Row r = join_row(a, row, heat, lane, x, e);
+    Row r = join_row(a, row, h, lane);
     if (lane == 0) {
       bool stands = j == m - 1;
-      if (y >= 0 && y < V && r.z > 0.0) {
-        if (h.greedy) e = y == r.at ? 1.0 : 0.0;
-        stands = (double)u * (double)q * r.z < e;
+      if (y >= 0 && y < V && r.z) {
+        // the draft's weight in the same units as z
+        const uint64_t e = h.greedy ? (y == r.at ? 1ull << 40 : 0) : scaled(1ull << 62, x, r.m, h);
+        stands = u * q * (float)r.z < (float)e * (h.greedy ? 1.f : 0x1p-22f);
       }
       if (!stands) atomicMin(&s_first, j);
       r.fallen = y;
@@ -341,14 +347,13 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   __syncthreads();
   const int first = s_first;
   const int64_t row = o0 + first;
-  Row r{-INFINITY, 0x7fffffff, 0.0, 0.f, 0.f, -1};
+  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, -1};
   if (m > 0 && !bad) {
     if (first < kRowsKept) {
       r = s_rows[first];
     } else {
       if (warp == 0) {
-        double e;
-        Row j = join_row(a, row, heat, lane, 0.f, e);
+        Row j = join_row(a, row, h, lane);
         if (lane == 0) {
           j.fallen = first < m - 1 ? a.tokens[row + 1] : -1;
           s_row = j;
@@ -419,7 +424,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int segs = (V + kSegElems - 1) / kSegElems;
   const int per = (segs + n_cta * kPickWarps - 1) / (n_cta * kPickWarps);
   const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
-  const bool look = m > 0 && !bad && !h.greedy && r.z > 0.0;  // (the top token needs no search)
+  const bool look = m > 0 && !bad && !h.greedy && r.z;  // (the top token needs no search)
   uint64_t total = 0, before = 0;
   for (int pass = 0; pass < 2; ++pass) {  // a second one where the draft leaves nothing: p itself
     uint64_t s = 0;
@@ -428,7 +433,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
         float w[kSeg];
         masses(g * kSegElems + lane, 32, w);
         const uint64_t sum = warp_sum(lane_units(w));
-        if (g - g0 < kSegsKept && lane == 0) s_seg[warp][g - g0] = sum;
+        if (lane == 0) s_seg[warp][g - g0] = sum;
         s += sum;
       }
     if (lane == 0) s_warp[warp] = s;
@@ -453,20 +458,20 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     less = kNothing;
   }
   // the lowest token whose sum passes r of the total
-  uint64_t want = rnd > 0.f ? (rnd < 1.f ? __double2ull_rd((double)rnd * (double)total) : total) : 0;
+  uint64_t want = 0;
+  if (rnd > 0.f) {  // rnd total, rounded down: rnd is mant 2^-(24 + down)
+    const uint32_t bits = __float_as_uint(rnd);
+    const uint64_t mant = (bits & 0x7fffffu) | (bits >> 23 ? 0x800000u : 0u);
+    const int down = 126 - max((int)(bits >> 23), 1);
+    if (rnd >= 1.f) want = total;
+    else if (down < 64) want = __umul64hi(total, mant << 40) >> down;
+  }
   if (want >= total) want = total ? total - 1 : 0;
   for (int w = 0; w < warp; ++w) before += s_warp[w];
   if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
     int g = g0;
     for (; g < g1 - 1; ++g) {
-      uint64_t sum;
-      if (g - g0 < kSegsKept) {
-        sum = s_seg[warp][g - g0];
-      } else {
-        float w[kSeg];
-        masses(g * kSegElems + lane, 32, w);
-        sum = warp_sum(lane_units(w));
-      }
+      const uint64_t sum = s_seg[warp][g - g0];
       if (want < before + sum) break;
       before += sum;
     }
@@ -505,7 +510,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (rank == 0) {
     if (tid == 0) {
       a.accepted[b] = first;
-      if (m > 0 && total == 0) a.picked[row] = h.greedy && r.z > 0.0 ? r.at : -1;
+      if (m > 0 && total == 0) a.picked[row] = h.greedy && r.z ? r.at : -1;
     }
     for (int j = tid; j < m; j += kPickThreads)
       if (j != first) a.picked[o0 + j] = j < first ? a.tokens[o0 + j + 1] : -1;
