@@ -224,9 +224,10 @@ cudaError_t launch_append_as(const lg_cache &c, const lg_chunk &ch, Q4AppendArgs
                              const RopeTable &tab, cudaStream_t s) {
   constexpr int kLanes = D / 8 / (PAIR ? 2 : 1);
   const int heads = a.H_q + 2 * c.H_kv;
-  // as many heads a thread, for its cosines and sines to serve, as leave the GPU four CTAs an SM; a few
-  // tokens' heads over several CTAs
-  const int64_t full = (int64_t)4 * 152 * kQ4Threads;
+  // as many heads a thread, for its cosines and sines to serve, as leave the GPU some waves of
+  // CTAs (ragged prompts of up to 4096 tokens: one wave 84 us, two 77, four 75, eight 104); a few tokens'
+  // heads over several CTAs
+  const int64_t full = (int64_t)16 * 152 * kQ4Threads;
   a.groups = 1;
   while (a.groups * 2 <= kQ4Threads / kLanes && a.groups < heads &&
          (int64_t)a.T * n_layers * a.groups * kLanes < full)
