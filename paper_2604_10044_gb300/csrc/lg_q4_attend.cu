@@ -35,33 +35,6 @@
 
 #include "lg_q4.cuh"
 
-#ifndef Q4_C1
-#define Q4_C1 3
-#endif
-#ifndef Q4_C2
-#define Q4_C2 2
-#endif
-#ifndef Q4_C3
-#define Q4_C3 2
-#endif
-#ifndef Q4_C4
-#define Q4_C4 2
-#endif
-#ifndef Q4_J1
-#define Q4_J1 2
-#endif
-#ifndef Q4_S1
-#define Q4_S1 2
-#endif
-#ifndef Q4_J2
-#define Q4_J2 2
-#endif
-#ifndef Q4_S2
-#define Q4_S2 3
-#endif
-#ifndef Q4_S3
-#define Q4_S3 4
-#endif
 namespace lg {
 namespace {
 
@@ -72,13 +45,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
 constexpr int kBn2 = kQ4Bn2;         // a CTA's block: kWarps tiles
 constexpr unsigned kCluster = 8;
-#ifndef Q4_CW
-#define Q4_CW 1
-#endif
-#ifndef Q4_CB
-#define Q4_CB 8
-#endif
-constexpr int kClusterBlocks = Q4_CB;    // key blocks of a cluster's CTA up to which it is used
+constexpr int kClusterBlocks = 8;    // key blocks of a cluster's CTA up to which it is used
 constexpr float kLazy = 8.f;         // log2 units that a weight may pass 1 by
 constexpr float kHidden = -1e38f;    // score of a row that a query does not see
 constexpr float kNone = -1e30f;      // maximum of a query that has seen nothing
@@ -88,9 +55,9 @@ template <int D, int NT>
 struct Q4Cfg {
   static constexpr int kRow = q4_row_bytes(D);
   static constexpr int kTile = kSub * kRow;         // of keys, or of values
-  static constexpr int kCtas = NT == 1 ? Q4_C1 : NT == 2 ? Q4_C2 : NT == 3 ? Q4_C3 : Q4_C4;  // of an SM
-  static constexpr int kStages = D == 64 ? 4 : NT == 1 ? Q4_S1 : NT == 2 ? Q4_S2 : NT == 3 ? Q4_S3 : 4;
-  static constexpr int kJoint = NT == 1 ? Q4_J1 : NT == 2 ? Q4_J2 : 1;    // products of 16 rows that go through the softmax together
+  static constexpr int kCtas = NT == 1 ? 3 : 2;  // of an SM
+  static constexpr int kStages = D == 64 ? 4 : NT == 1 ? 2 : NT == 2 ? 3 : 4;
+  static constexpr int kJoint = NT <= 2 ? 2 : 1;     // products of 16 rows that go through the softmax together
   static constexpr int kRing = kWarps * kStages * 2 * kTile;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
@@ -992,7 +959,7 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   const int64_t tiles = (rows + r.rows - 1) / r.rows;
   const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
   // what the 152 SMs of a GB300 hold at once, over the layers; no more than there are blocks
-  const int64_t fit = 152 * (r.rows <= 8 ? Q4_C1 : r.rows <= 16 ? Q4_C2 : r.rows <= 24 ? Q4_C3 : Q4_C4);
+  const int64_t fit = 152 * (r.rows <= 8 ? 3 : 2);
   const int64_t most = (int64_t)batch * H_kv * tiles * (blocks + kQ4ItemUnits);
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
@@ -1001,7 +968,7 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   const int64_t items = (int64_t)batch * H_kv * tiles;
   const Q4Shape shape{r.rows, g, window, sink, H_kv};
   const int one = q4_units(ChunkSeq{max_len, max_new < max_len ? max_new : max_len}, shape) - kQ4ItemUnits;
-  r.cluster = items * n_layers * kCluster <= fit * Q4_CW && one <= (int)kCluster * kClusterBlocks;
+  r.cluster = items * n_layers * kCluster <= fit && one <= (int)kCluster * kClusterBlocks;
   if (r.cluster) r.ctas = (int)items * kCluster;
   return r;
 }
