@@ -289,7 +289,9 @@ __global__ void __launch_bounds__(kQ4Threads)
 }
 
 // A layer's rows as values at the same slots of two 16-bit caches of one layer, for the kernels of
-// many query rows: what some query of the chunk sees.  blockIdx = (rows, kv-head, sequence).
+// many query rows: what some query of the chunk sees.  blockIdx = (rows, kv-head, sequence).  Bound by its
+// stores: with all loads of a thread's 4 (2) words and parameters of keys and of values asked for before
+// the first store 55 us for 8 sequences of 8192 rows (352 MB, 6.4 TB/s), word by word 71.
 constexpr int kExpandRows = 64;
 
 template <int D>
@@ -310,7 +312,26 @@ __global__ void __launch_bounds__(kQ4Threads)
       const int64_t src = ((int64_t)layer * c.H_kv + h) * c.S_total + c.seq_off[b] + r0;
       const int64_t dst = h * c.S_total + c.seq_off[b] + r0;
       const int rows = n - r0 < kExpandRows ? (int)(n - r0) : kExpandRows;
-#pragma unroll 4
+      if (rows == kExpandRows) {  // all of its loads before the first store
+        constexpr int kN = kExpandRows * kLanes / kQ4Threads;
+        uint32_t kw[kN], kp[kN], vw[kN], vp[kN];
+        const int pc = threadIdx.x % kLanes, i0 = threadIdx.x / kLanes;
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          const int64_t at = (src + i0 + n * (kQ4Threads / kLanes)) * kRow;
+          const uint32_t *k = (const uint32_t *)((const uint8_t *)c.k + at);
+          const uint32_t *v = (const uint32_t *)((const uint8_t *)c.v + at);
+          kw[n] = k[pc], kp[n] = k[kLanes + pc / kGroup];
+          vw[n] = v[pc], vp[n] = v[kLanes + pc / kGroup];
+        }
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          const int64_t to = (dst + i0 + n * (kQ4Threads / kLanes)) * D + 8 * pc;
+          *(uint4 *)(K + to) = q4_values(kw[n], kp[n]);
+          *(uint4 *)(V + to) = q4_values(vw[n], vp[n]);
+        }
+        continue;
+      }
       for (int u = threadIdx.x; u < rows * kLanes; u += kQ4Threads) {
         const int i = u / kLanes, pc = u % kLanes;
         const uint32_t *k = (const uint32_t *)((const uint8_t *)c.k + (src + i) * kRow);
