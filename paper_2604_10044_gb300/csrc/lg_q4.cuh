@@ -121,7 +121,7 @@ struct Q4AttendArgs {
   int64_t S_total;
   int layer0, n_layers, batch, H_kv, g, T, max_new, max_len;
   int ctas;                // of a layer
-  bool cluster;            // a cluster of CTAs an item
+  int cluster;             // CTAs of an item that joins its results itself; 0: items in a line
   int suffix_w;
   float qscale;            // softmax scale * log2(e)
   Q4Shape shape;
@@ -129,8 +129,7 @@ struct Q4AttendArgs {
 
 // how a call is divided, and the bytes of its partial results
 struct Q4Grid {
-  int rows, ctas;
-  bool cluster;
+  int rows, ctas, cluster;
   size_t part_bytes;
 };
 Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,

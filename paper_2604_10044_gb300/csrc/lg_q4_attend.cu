@@ -22,10 +22,19 @@
 //
 // Weights are 2^(z - m) with a maximum m that may lag: it is formed anew only when a score passes it
 // by 8, so a tile asks one vote.  Every warp has its own m and sums; the CTA's four are merged at its
-// end, and the CTAs of an item by a second kernel.
+// end, and the CTAs of an item by a second kernel (or, as a cluster, by themselves: q4_grid).
 //
 // Every warp copies its own 32 rows a block (bulk copies into a ring of its own), so warps never wait
 // for one another.
+//
+// GB300, 8 kv-heads of 128, 4 query heads each: 64 sequences of 1024 to 16381 rows (477 MB) 84 us in this
+// kernel, 5.7 TB/s, and 92 with the merge; one of 262143 rows (336 MB) 58 and 66; what bounds it is issue: the
+// warps issue in 55 to 60 % of the cycles, half of that masks and fused conversions of codes, while HBM
+// is at 83 %.  Steps that led here: codes as 128 + c with the 128 taken off afterwards 166 us (64
+// sequences); codes as they stand and ldmatrix 144; 32 rows a warp and stage 110; equal shares of a line
+// 95; three CTAs an SM of 168 registers instead of four of 128 (whose spills cost more than their warps
+// gave) 91.  Not kept: five CTAs an SM 129; one product of 16 rows at a time through the softmax 98; three
+// and four stages the same and 135.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -44,8 +53,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kSub = 32;             // rows of a warp's tile, 16 a product
 constexpr int kBn2 = kQ4Bn2;         // a CTA's block: kWarps tiles
-constexpr unsigned kCluster = 8;
-constexpr int kClusterBlocks = 8;    // key blocks of a cluster's CTA up to which it is used
+constexpr int kClusterMost = 8;      // CTAs of a cluster
 constexpr float kLazy = 8.f;         // log2 units that a weight may pass 1 by
 constexpr float kHidden = -1e38f;    // score of a row that a query does not see
 constexpr float kNone = -1e30f;      // maximum of a query that has seen nothing
@@ -277,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   int seq, units, tiles;
   int64_t x, y0, y1;  // the item's start in the line, the CTA's share
   if constexpr (CL) {  // a cluster an item
-    unsigned item = blockIdx.x / kCluster;
+    unsigned item = blockIdx.x / (unsigned)a.cluster;
     tiles = (int)(((int64_t)a.max_new * a.g + a.shape.rows - 1) / a.shape.rows);
     w.tile = (int)(item % (unsigned)tiles);
     item /= (unsigned)tiles;
@@ -287,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
       if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
       return;
     }
-    if (STATS && w.q.n == 0 && !bad && blockIdx.x % kCluster == 0) {
+    if (STATS && w.q.n == 0 && !bad && blockIdx.x % (unsigned)a.cluster == 0) {
       const int64_t head = ((int64_t)layer * a.T + w.off) * H_q + w.kvh * a.g;  // attends to nothing
       for (int e = tid; e < a.g * D / 2; e += kThreads) ((uint32_t *)a.out)[head * D / 2 + e] = 0u;
       if (tid < a.g) ((float4 *)a.stats)[head + tid] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
@@ -338,9 +346,9 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   w.blocks = tile_blocks(w.rows, kBn2);
   int blk0, blk1;
   if constexpr (CL) {
-    const int rank = blockIdx.x % kCluster;
-    blk0 = rank * w.blocks.count / kCluster;
-    blk1 = bad ? blk0 : (rank + 1) * w.blocks.count / kCluster;
+    const int rank = (int)(blockIdx.x % (unsigned)a.cluster);
+    blk0 = (int)((int64_t)rank * w.blocks.count / a.cluster);
+    blk1 = bad ? blk0 : (int)((int64_t)(rank + 1) * w.blocks.count / a.cluster);
   } else {
     blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
   }
@@ -764,24 +772,26 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
     if (tid == 0) s_no = bad || gave_up;
     cl.sync();
     bool no = false;
-    for (int k = 0; k < kCluster; ++k) no |= *cl.map_shared_rank(&s_no, k) != 0;
+    for (int k = 0; k < a.cluster; ++k) no |= *cl.map_shared_rank(&s_no, k) != 0;
     const int n = no ? 0 : w.used * (D / 32);
-    for (int i = (int)cl.block_rank() * kWarps + warp; i < n; i += kCluster * kWarps) {
+    for (int i = (int)cl.block_rank() * kWarps + warp; i < n; i += a.cluster * kWarps) {
       const int r = i / (D / 32), e = i % (D / 32) * 32 + lane;
-      const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % kCluster) + r * (D + 4) + D);
+      const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % a.cluster) + r * (D + 4) + D);
       const bool any = v.y != 0.f;
       const float mx = warp_max(any ? v.x : kNone), by = v.x - mx;
       const float f = any ? exp2_fast(by) : 0.f;
       float sl = f * v.y, sh = any ? f * __fmaf_rn(by, v.y, v.z) : 0.f, ss = f * v.w;
 #pragma unroll
-      for (int o = 1; o < kCluster; o <<= 1) {
+      for (int o = 1; o < kClusterMost; o <<= 1) {
+        if (o >= a.cluster) break;
         sl += __shfl_xor_sync(0xffffffffu, sl, o);
         sh += __shfl_xor_sync(0xffffffffu, sh, o);
         ss += __shfl_xor_sync(0xffffffffu, ss, o);
       }
       float y = 0.f;
 #pragma unroll
-      for (int k = 0; k < kCluster; ++k) {
+      for (int k = 0; k < kClusterMost; ++k) {
+        if (k >= a.cluster) break;
         const float fk = __shfl_sync(0xffffffffu, f, k);
         const float z = cl.map_shared_rank(s_part, k)[r * (D + 4) + e];
         if (fk != 0.f) y += fk * z;
@@ -922,7 +932,7 @@ cudaError_t launch_as(const Q4AttendArgs &a, cudaStream_t s) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCluster;
+  attr[1].val.clusterDim.x = a.cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL ? 2 : 1;
@@ -964,12 +974,17 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
   r.part_bytes = (r.part_bytes + 255) / 256 * 256;
-  // few items of few blocks: a cluster each, which joins its results itself
+  // Few items of few blocks: as many CTAs each as the GPU holds of them, up to eight, which join their results
+  // themselves; while a CTA has at most 16 blocks of eight query rows, or 5 of more.  (us in a line with its
+  // second kernel and in clusters, 8 kv-heads: one sequence of 1025 rows 11.2 and 7.8, 24 of 700 17.0 and
+  // 11.8, 24 of 2049 22.8 and 19.6; with 16 query rows 12 of 1500 16.0 and, at 6 blocks a CTA, 18.4.)
   const int64_t items = (int64_t)batch * H_kv * tiles;
   const Q4Shape shape{r.rows, g, window, sink, H_kv};
   const int one = q4_units(ChunkSeq{max_len, max_new < max_len ? max_new : max_len}, shape) - kQ4ItemUnits;
-  r.cluster = items * n_layers * kCluster <= fit && one <= (int)kCluster * kClusterBlocks;
-  if (r.cluster) r.ctas = (int)items * kCluster;
+  r.cluster = 0;
+  for (int n = kClusterMost; n >= 1 && !r.cluster; n /= 2)
+    if (items * n_layers * n <= fit && one <= n * (r.rows <= 8 ? 16 : 5)) r.cluster = n;
+  if (r.cluster) r.ctas = (int)items * r.cluster;
   return r;
 }
 

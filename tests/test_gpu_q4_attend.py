@@ -50,6 +50,17 @@ def test_many_sequences_in_one_line(cuda, d, g, most, window, sink):
     _check(q4_ref.Batch(ns, ms, g=g, d=d, device=cuda).to_device(), window, sink)
 
 
+@pytest.mark.parametrize("d,g,most,count", [(64, 1, 1, 20), (64, 2, 3, 110), (128, 1, 1, 200),
+                                            (128, 3, 1, 300), (64, 8, 2, 30), (64, 3, 5, 70)])
+def test_items_of_every_division(cuda, d, g, most, count):
+    """as many items as give clusters of eight CTAs, of two, single ones, and a line"""
+    rng = np.random.default_rng(count)
+    ns = [int(x) for x in rng.integers(0, 300, count)]
+    ms = [int(min(n, rng.integers(0, most + 1))) if most > 1 else int(n > 0) for n in ns]
+    ns[0], ms[0] = 301, most
+    _check(q4_ref.Batch(ns, ms, g=g, d=d, device=cuda).to_device())
+
+
 @pytest.mark.parametrize("d,g", [(64, 8), (128, 4), (128, 1)])
 @pytest.mark.parametrize("window,sink", [(0, 0), (50, 3)])
 def test_chunks(cuda, d, g, window, sink):
@@ -91,7 +102,7 @@ def test_a_row_without_numbers_reaches_those_that_see_it(cuda, d):
     assert ((out - ref).abs() <= tol)[fine].all()
 
 
-@pytest.mark.parametrize("d,g,batch", [(128, 2, 1), (128, 4, 5), (64, 7, 3), (64, 8, 70), (128, 8, 9)])
+@pytest.mark.parametrize("d,g,batch", [(128, 2, 1), (128, 4, 5), (64, 7, 3), (64, 8, 70), (128, 8, 9), (64, 1, 250)])
 def test_single_tokens_with_statistics(cuda, d, g, batch):
     gen = np.random.default_rng(batch)
     ns = [int(x) for x in gen.integers(1, 1500 if batch < 20 else 200, batch)]
