@@ -38,14 +38,14 @@ LG_API size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch);
      draft j stands when all before it do and u[t] q_t(y) < p_t(y)
      accepted[b] = the number of drafts that stand, a
      the next token is drawn from row t = off[b] + a with weights w = max(p_t - q_t, 0), or p_t where a
-              counts all drafts or the w are all zero (at a resolution of 2^-62): the lowest i with
+              counts all drafts or the w are all zero (to 2^-62 of the mass): the lowest i with
               sum_{k <= i} w(k) > r[b] sum w.  r below zero or NaN counts as 0, from one on as just
               below one.  -1 where p_t = 0
      picked[off[b] + j] = draft j for j < a, the next token for j = a, -1 for j > a
    so that the tokens of sequence b are distributed as the target's whatever the draft is, when u and r
    are uniform on [0, 1) and independent.  A draft outside [0, V) falls, with q_t = 0.
-   Sums are integers in units of 2^-62 of the mass (2^-40 of the largest weight in p's own sum), so the
-   same call gives the same tokens, in whatever batch a sequence is; a weight is within about 2^-22.
+   A weight is within about 2^-22; what 16 of them sum to is added up in integers, in units of 2^-62 of the
+   mass (2^-40 of the largest weight in p's own sum), so the same call gives the same tokens.
    x: rows [0, T) at least (x->batch >= T); draft: nullable, as many rows of the same V, its own dtype and
    stride.  tokens: device [T]; temperature: nullable (1), device [batch]; u: device [T] (the entry of a
    sequence's last row is not used); r: device [batch]; picked: device [T], accepted: device [batch];

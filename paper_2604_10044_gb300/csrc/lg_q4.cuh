@@ -160,8 +160,9 @@ inline void q4_fill(Q4AttendArgs &a, const lg_cache &c, int g, float scale, cons
   a.qscale = scale * 1.4426950408889634f;
 }
 
-// query rows of a kv-head above which a call expands the layer's rows to bf16 for the kernels of
-// 16-bit caches
+// Query rows of a kv-head above which a call expands the layer's rows to bf16 for the kernels of 16-bit
+// caches.  (us, the codes themselves and expanded, 4 query heads of 128, 16 sequences of 8192 rows: 32 query rows
+// 103 and 209, 64 178 and 215, 96 257 and 215; 32 sequences of 1000: 48 and 62, 74 and 71, 101 and 73.)
 constexpr int kQ4FewRows = 64;
 
 }  // namespace lg

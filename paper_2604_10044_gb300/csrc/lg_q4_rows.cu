@@ -20,6 +20,9 @@ namespace {
 // quantised), values.  Otherwise the other elements of its pairs come by shuffles (so queries may be
 // rotated in place), as do the least and largest element of a group, over the 4 (d = 128) or 2 lanes
 // that hold it.
+// (GB300, ragged prompts of up to 4096 tokens, 32 query heads and 8 of keys and values of 128, 246 MB: 62 us,
+// 4 TB/s, the warps issuing in 64 % of the cycles; queries, keys and values in one loop with their
+// pointers chosen a head 95, a word a thread with the other half of its pairs by shuffles 103.)
 
 struct Q4AppendArgs {
   const __nv_bfloat16 *q, *k, *v;

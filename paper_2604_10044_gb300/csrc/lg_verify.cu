@@ -7,9 +7,18 @@
 //
 // Which token a number falls on is exact only as far as the sums are: a bound between two tokens that
 // moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's bounds
-// on the way.  So weights go into the sums as integers in units of 2^-62 (of a mass of one), which add
-// up in any order and division to the same; the quotient by a temperature keeps a second term; and
-// the joining of a row's slices is in integers too, with powers of two to 2^-31.
+// on the way.  So what a lane sums (16 weights) goes into the totals as an integer in units of 2^-62 of a
+// mass of one, and integers add up to the same in any order; the quotient by a temperature keeps a
+// second term; and the joining of a row's slices is in integers too, with powers of two to 2^-30.
+//
+// GB300, 261 rows of 128257 bf16 logits of 64 sequences: 19 us in the first kernel (67 MB, 3.5 TB/s; an element
+// takes some ten instructions, and the CTAs issue in 60 % of the cycles), 18 in the second, 37 a call;
+// one sequence's five rows of 151936 fp32: 4 and 10, all latency (the draft's and the slices' loads, two
+// rounds over 512 elements a warp, a cluster barrier).  What it took, for 64 sequences and for one: loads
+// and work element by element 196 and 59 us; packed fp32 in place of scalar, all of a segment loaded first
+// 51 and 21; logits kept packed, lanes' sums in fp32 41 and 20; the slices joined in integers instead of in
+// 64-bit floating point 37 and 14.  Not kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence
+// more 41 to 50.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
