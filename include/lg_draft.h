@@ -61,7 +61,7 @@ LG_API lg_status lg_verify_draft(const lg_logits *x, const lg_chunk *ch, int bat
                                  int32_t *dev_status, cudaStream_t s);
 
 /* Ends a chunk of which only the first accepted[b] + 1 rows stay: len[b] -= m_b - 1 - accepted[b]
-   (m_b = 0: nothing).  The counterpart of lg_begin_chunk after lg_verify_draft; the rows' slots are
+   (m_b = 0: nothing, whatever accepted[b] holds).  The counterpart of lg_begin_chunk after lg_verify_draft; the rows' slots are
    taken by the next tokens.  An accepted[b] outside [0, m_b - 1], an m_b outside [0, max_new] or above
    len[b], or an off[] outside [0, T] sets LG_ERR_CAPACITY on the device and leaves that sequence's
    length.  accepted: device [batch]. */

@@ -329,12 +329,11 @@ lg_status lg_verify_draft(const lg_logits *x, const lg_chunk *ch, int batch, con
       !aligned(r, 4) || !aligned(temperature, 4) || !aligned(picked, 4) || !aligned(accepted, 4) ||
       !aligned(dev_status, 4))
     return LG_ERR_INVALID_ARG;
-  if (ch->T == 0) return LG_OK;
   if (!ws || !aligned(ws, 16) || ws_bytes < lg::verify_ws_bytes(*x, ch->T)) return LG_ERR_WORKSPACE;
   // results over anything that is read, or over one another
   const uint64_t n = (uint64_t)ch->T * 4, nb = (uint64_t)batch * 4;
   auto rows = [&](const lg_logits *l) {
-    return ((uint64_t)(ch->T - 1) * l->stride + l->V) * (l->dtype == LG_BF16 ? 2 : 4);
+    return ch->T ? ((uint64_t)(ch->T - 1) * l->stride + l->V) * (l->dtype == LG_BF16 ? 2 : 4) : 0;
   };
   auto taken = [&](const void *p, uint64_t bytes) {
     return p && (overlap(picked, n, p, bytes) || overlap(accepted, nb, p, bytes));

@@ -1,9 +1,9 @@
 // Rows of a 4-bit cache (lg.h, LG_Q4) and what the kernels that read and write them share.
 //
-// A head of d elements is four groups of d / 4.  Its row is d / 8 words of eight codes, element 2i of
-// a word in bits 4i and element 2i + 1 in bits 16 + 4i, i < 4, so that one shift and one mask leave a
-// pair of neighbours in the halves of a word; then a word a group, bf16 scale s below bf16 least value
-// lo.  A code c stands for lo + s c.
+// A head of d elements is four groups of d / 4.  Its row is d / 8 words of eight codes, element 2i
+// of a word in bits 4i and element 2i + 1 in bits 16 + 4i, i < 4, so that one shift and one mask
+// leave a pair of neighbours in the halves of a word; then a word a group, bf16 scale s below bf16
+// least value lo.  A code c stands for lo + s c.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -17,24 +17,25 @@ namespace lg {
 
 __host__ __device__ constexpr int q4_row_bytes(int d) { return d / 2 + 16; }
 
-// A group whose range reaches this, or that holds a NaN or an infinity, is held as NaN: weights of up
-// to 2^8 times a scale stay within fp32 and bf16.
+// A group whose range reaches this, or that holds a NaN or an infinity, is held as NaN: weights of
+// up to 2^8 times a scale stay within fp32 and bf16.
 constexpr float kQ4Range = 0x1p118f;
 constexpr uint32_t kQ4NaN = 0x7fffu;  // the word of such a group: scale NaN, least value 0
 
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Masked codes of a word as they stand: c (bits 0-3 of either half) or 16 c (bits 4-7) in units of 2^-133,
-// the least bf16 number.
+// Masked codes of a word as they stand: c (bits 0-3 of either half) or 16 c (bits 4-7) in units of
+// 2^-133, the least bf16 number.
 constexpr uint32_t kQ4Low = 0x000f000fu, kQ4High = 0x00f000f0u;
 
-// the eight values of a word as bf16, lo + s c rounded once: a code times 2^127 is c / 64 or c / 4 exactly,
-// which 64 s or 4 s make up for
+// the eight values of a word as bf16, lo + s c rounded once: a code times 2^127 is c / 64 or c / 4
+// exactly, which 64 s or 4 s make up for
 __device__ __forceinline__ uint4 q4_values(uint32_t word, uint32_t par) {
   auto two = [](uint32_t x) { return *(const __nv_bfloat162 *)&x; };
   const __nv_bfloat162 by = two(0x7f007f00u);
-  const __nv_bfloat162 s = two(__byte_perm(par, par, 0x1010)), lo = two(__byte_perm(par, par, 0x3232));
+  const __nv_bfloat162 s = two(__byte_perm(par, par, 0x1010));
+  const __nv_bfloat162 lo = two(__byte_perm(par, par, 0x3232));
   const __nv_bfloat162 s64 = __hmul2(s, two(0x42804280u)), s4 = __hmul2(s, two(0x40804080u));
   auto value = [&](uint32_t raw, const __nv_bfloat162 &scale) {
     const __nv_bfloat162 r = __hfma2(__hmul2(two(raw), by), scale, lo);
@@ -49,10 +50,10 @@ __device__ __forceinline__ uint4 q4_values(uint32_t word, uint32_t par) {
 // group; every lane of the warp calls it.
 //
 // A code is the integer nearest to (x - lo) / s, ties to even.  The product with 1 / s is within
-// 2^-22 of the quotient, which settles all but quotients next to a half: with s of 8 bits and a code of 4 the
-// residual x - lo - s c is exact, and where none of the eight is half a step or more from its code
-// the codes are right.  Otherwise the quotients are divided out (s (c + 1/2) has 13 bits, so a
-// correctly rounded quotient of 24-bit numbers is never a half that it should not be).
+// 2^-22 of the quotient, which settles all but quotients next to a half: with s of 8 bits and a
+// code of 4 the residual x - lo - s c is exact, and where none of the eight is half a step or more
+// from its code the codes are right.  Otherwise the quotients are divided out (s (c + 1/2) has 13
+// bits, so a correctly rounded quotient of 24-bit numbers is never a half that it should not be).
 template <int LANES>
 __device__ __forceinline__ uint32_t q4_encode(const float *x, uint32_t &par) {
   float lo = x[0], hi = x[0], odd = 0.f;
@@ -160,9 +161,10 @@ inline void q4_fill(Q4AttendArgs &a, const lg_cache &c, int g, float scale, cons
   a.qscale = scale * 1.4426950408889634f;
 }
 
-// Query rows of a kv-head above which a call expands the layer's rows to bf16 for the kernels of 16-bit
-// caches.  (us, the codes themselves and expanded, 4 query heads of 128, 16 sequences of 8192 rows: 32 query rows
-// 103 and 209, 64 178 and 215, 96 257 and 215; 32 sequences of 1000: 48 and 62, 74 and 71, 101 and 73.)
+// Query rows of a kv-head above which a call expands the layer's rows to bf16 for the kernels of
+// 16-bit caches.  (us, the codes themselves and expanded, 4 query heads of 128, 16 sequences of
+// 8192 rows: 32 query rows 103 and 209, 64 178 and 215, 96 257 and 215; 32 sequences of 1000: 48
+// and 62, 74 and 71, 101 and 73.)
 constexpr int kQ4FewRows = 64;
 
 }  // namespace lg

@@ -1,40 +1,42 @@
-// Attention of few query rows of a kv-head (a token, or some drafted tokens, a sequence) over a 4-bit
-// cache, with the statistics that the guard reads of a single token.
+// Attention of few query rows of a kv-head (a token, or some drafted tokens, a sequence) over a
+// 4-bit cache, with the statistics that the guard reads of a single token.
 //
-// A warp takes 16 rows of keys and values at a time through mma.sync (M = 16 keys or 16 elements, N = 8
-// query rows, K = 16), and a value is never formed from its code and parameters:
-//   scores   q . k = sum over groups of (s_g sum_e q_e c_e) + sum_g lo_g sum_{e in g} q_e.  A code masked out
-//            of its word is a bf16 number as it stands: the low eight bits of one count in units of 2^-133
-//            (its subnormal numbers, and the first normal ones), so bits 0-3 are c and bits 4-7 16 c of them.
-//            The queries bring the factor, 2^120 over the power of two of the row's largest element (and a
-//            sixteenth of that for the 16 c); both are exact, so are the products.  The groups' sums are
-//            joined by the rows' scales in fp32; the least values are one more product, with sums of q
-//            in two bf16 terms.
-//   results  sum_k p_k v_k = sum_k (p_k s_kg)(c - 8) + sum_k p_k lo_kg + 8 sum_k p_k s_kg: the second operand
-//            is the weights times a group's scales, rounded to bf16; the last two are one product whose
-//            first operand is the rows' parameters.  One fused operation turns the masked code into
-//            (c - 8) / 64 or / 4: with codes about zero sums stay small beside what the matrix unit drops
-//            of them, and a weight's second rounding meets |c - 8|, not c.
-// Codes and parameters come by ldmatrix: a 16-byte piece of a row is a group (two of them, for d = 64), and
-// transposed a register holds a half word of codes of two neighbouring keys, which is a pair of each of
-// its nibbles.  For d = 64 a product of the scores takes one group of the two, the other's queries being
-// zero, and of the results half of the rows are of use.
+// A warp takes 16 rows of keys and values at a time through mma.sync (M = 16 keys or 16 elements, N
+// = 8 query rows, K = 16), and a value is never formed from its code and parameters:
+//   scores   q . k = sum over groups of (s_g sum_e q_e c_e) + sum_g lo_g sum_{e in g} q_e.  A code
+//            masked out of its word is a bf16 number as it stands: the low eight bits of one count
+//            in units of 2^-133 (its subnormal numbers, and the first normal ones), so bits 0-3 are
+//            c and bits 4-7 16 c of them.  The queries bring the factor, 2^120 over the power of
+//            two of the row's largest element (and a sixteenth of that for the 16 c); both are
+//            exact, so are the products.  The groups' sums are joined by the rows' scales in fp32;
+//            the least values are one more product, with sums of q in two bf16 terms.
+//   results  sum_k p_k v_k = sum_k (p_k s_kg)(c - 8) + sum_k p_k lo_kg + 8 sum_k p_k s_kg: the
+//            second operand is the weights times a group's scales, rounded to bf16; the last two
+//            are one product whose first operand is the rows' parameters.  One fused operation
+//            turns the masked code into (c - 8) / 64 or / 4: with codes about zero sums stay small
+//            beside what the matrix unit drops of them, and a weight's second rounding meets |c -
+//            8|, not c.
+// Codes and parameters come by ldmatrix: a 16-byte piece of a row is a group (two of them, for d =
+// 64), and transposed a register holds a half word of codes of two neighbouring keys, which is a
+// pair of each of its nibbles.  For d = 64 a product of the scores takes one group of the two, the
+// other's queries being zero, and of the results half of the rows are of use.
 //
-// Weights are 2^(z - m) with a maximum m that may lag: it is formed anew only when a score passes it
-// by 8, so a tile asks one vote.  Every warp has its own m and sums; the CTA's four are merged at its
-// end, and the CTAs of an item by a second kernel (or, as a cluster, by themselves: q4_grid).
+// Weights are 2^(z - m) with a maximum m that may lag: it is formed anew only when a score passes
+// it by 8, so a tile asks one vote.  Every warp has its own m and sums; the CTA's four are merged
+// at its end, and the CTAs of an item by a second kernel (or, as a cluster, by themselves:
+// q4_grid).
 //
-// Every warp copies its own 32 rows a block (bulk copies into a ring of its own), so warps never wait
-// for one another.
+// Every warp copies its own 32 rows a block (bulk copies into a ring of its own), so warps never
+// wait for one another.
 //
-// GB300, 8 kv-heads of 128, 4 query heads each: 64 sequences of 1024 to 16381 rows (477 MB) 84 us in this
-// kernel, 5.7 TB/s, and 92 with the merge; one of 262143 rows (336 MB) 58 and 66; what bounds it is issue: the
-// warps issue in 55 to 60 % of the cycles, half of that masks and fused conversions of codes, while HBM
-// is at 83 %.  Steps that led here: codes as 128 + c with the 128 taken off afterwards 166 us (64
-// sequences); codes as they stand and ldmatrix 144; 32 rows a warp and stage 110; equal shares of a line
-// 95; three CTAs an SM of 168 registers instead of four of 128 (whose spills cost more than their warps
-// gave) 91.  Not kept: five CTAs an SM 129; one product of 16 rows at a time through the softmax 98; three
-// and four stages the same and 135.
+// GB300, 8 kv-heads of 128, 4 query heads each: 64 sequences of 1024 to 16381 rows (477 MB) 84 us
+// in this kernel, 5.7 TB/s, and 92 with the merge; one of 262143 rows (336 MB) 58 and 66; what
+// bounds it is issue: the warps issue in 55 to 60 % of the cycles, half of that masks and fused
+// conversions of codes, while HBM is at 83 %.  Steps that led here: codes as 128 + c with the 128
+// taken off afterwards 166 us (64 sequences); codes as they stand and ldmatrix 144; 32 rows a warp
+// and stage 110; equal shares of a line 95; three CTAs an SM of 168 registers instead of four of
+// 128 (whose spills cost more than their warps gave) 91.  Not kept: five CTAs an SM 129; one
+// product of 16 rows at a time through the softmax 98; three and four stages the same and 135.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -65,7 +67,7 @@ struct Q4Cfg {
   static constexpr int kTile = kSub * kRow;         // of keys, or of values
   static constexpr int kCtas = NT == 1 ? 3 : 2;  // of an SM
   static constexpr int kStages = D == 64 ? 4 : NT == 1 ? 2 : NT == 2 ? 3 : 4;
-  static constexpr int kJoint = NT <= 2 ? 2 : 1;     // products of 16 rows that go through the softmax together
+  static constexpr int kJoint = NT <= 2 ? 2 : 1;  // products of 16 rows with one softmax step
   static constexpr int kRing = kWarps * kStages * 2 * kTile;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOut = kWarps * kRows * (D + 1) * 4;  // the warps' results, for their merge
@@ -85,7 +87,8 @@ __device__ __forceinline__ bool of_group(int gr, int i) {
   return D == 128 || i / (N / 2) == (gr & 1);
 }
 
-// the element of row r (g or g + 8) of result tile u of group gr: nibble 2u or 2u + 1 of half word g
+// the element of row r (g or g + 8) of result tile u of group gr: nibble 2u or 2u + 1 of half word
+// g
 template <int D>
 __device__ __forceinline__ int value_element(int gr, int u, int g, int up) {
   return 8 * (4 * piece_of<D>(gr) + (g >> 1)) + 2 * (2 * u + up) + (g & 1);
@@ -97,7 +100,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 __device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 r = __hmax2(__habs2(*(const __nv_bfloat162 *)&a), __habs2(*(const __nv_bfloat162 *)&b));
+  const __nv_bfloat162 r =
+      __hmax2(__habs2(*(const __nv_bfloat162 *)&a), __habs2(*(const __nv_bfloat162 *)&b));
   return *(const uint32_t *)&r;
 }
 
@@ -151,13 +155,14 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 
 // a partial result: [rows][D + 4], the sums and {m, l, sum p (z - m), suffix}; m the true maximum
 template <int D>
-__device__ __forceinline__ float *part_row(const Q4AttendArgs &a, int layer, int cta, int slot, int r) {
+__device__ __forceinline__ float *part_row(const Q4AttendArgs &a, int layer, int cta, int slot,
+                                           int r) {
   return a.part + (((int64_t)layer * a.ctas + cta) * 2 + slot) * a.shape.rows * (int64_t)(D + 4) +
          r * (D + 4);
 }
 
-// A sequence's numbers; false where they are out of bounds.  Without offsets every sequence that has
-// rows has one query, for its last.
+// A sequence's numbers; false where they are out of bounds.  Without offsets every sequence that
+// has rows has one query, for its last.
 __device__ __forceinline__ bool q4_seq(const Q4AttendArgs &a, int b, ChunkSeq &q, int &off) {
   q.n = a.len[b];
   off = a.off ? a.off[b] : b;
@@ -175,9 +180,9 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {  // inclusiv
   return v;
 }
 
-// The line's units W, and the sequence that CTA `cta`'s first unit falls into, with its start and its
-// numbers (nothing where the CTA's share starts at the end of the line).  False when a number is out of
-// bounds (recorded).  Every lane of a warp calls it; a batch of at most 32 is read once.
+// The line's units W, and the sequence that CTA `cta`'s first unit falls into, with its start and
+// its numbers (nothing where the CTA's share starts at the end of the line).  False when a number
+// is out of bounds (recorded).  Every lane of a warp calls it; a batch of at most 32 is read once.
 struct Q4Line {
   int64_t W, step;
   int64_t x;
@@ -256,7 +261,8 @@ __device__ __forceinline__ Q4Cut *cut_at(const Q4AttendArgs &a, int d, int layer
 }
 
 template <int D, int NT, bool STATS, bool CL>
-__global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_kernel(Q4AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
+    q4_attend_kernel(Q4AttendArgs a) {
   using C = Q4Cfg<D, NT>;
   constexpr int kPieces = D / 32;  // 16-byte pieces of a row's codes
   extern __shared__ __align__(128) uint8_t smem[];
@@ -269,7 +275,8 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   }
   __syncwarp();
   pdl_enter();
-  // (CTAs of a cluster, which meet at barriers, may find another status each: they go on without work)
+  // (CTAs of a cluster, which meet at barriers, may find another status each: they go on without
+  // work)
   const bool bad = cta_status_bad(a.status);
   if (!CL && bad) return;
   const int layer = blockIdx.y, cta = blockIdx.x;  // (layer of the call)
@@ -342,495 +349,500 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas)) q4_attend_ker
   bool gave_up = false;
 
   for (; x < y1 && !gave_up; x += units) {
-  w.rows = q4_rows(w.q, a.shape, w.tile, w.used);
-  w.blocks = tile_blocks(w.rows, kBn2);
-  int blk0, blk1;
-  if constexpr (CL) {
-    const int rank = (int)(blockIdx.x % (unsigned)a.cluster);
-    blk0 = (int)((int64_t)rank * w.blocks.count / a.cluster);
-    blk1 = bad ? blk0 : (int)((int64_t)(rank + 1) * w.blocks.count / a.cluster);
-  } else {
-    blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
-  }
-  if (CL || blk0 < blk1) {
-  // this warp's copies: its rows of each block
-  const int64_t row0 = ((int64_t)(a.layer0 + layer) * a.H_kv + w.kvh) * a.S_total + a.seq_off[seq];
-  const uint8_t *gk = a.K + row0 * C::kRow, *gv = a.V + row0 * C::kRow;
-  auto tile_row = [&](int i) { return (w.blocks.index(i) << kBn2) + warp * kSub; };
-  auto copy = [&](int i, uint8_t *to, uint64_t *bar) {  // lane 0: block i into a stage
-    const int r = tile_row(i);
-    const int n = min(kSub, w.rows.last + 1 - r);
-    if (n <= 0) return;
-    const int bytes = n * C::kRow;
-    const int64_t from = (int64_t)r * C::kRow;
-    mbar_arrive_expect_tx(bar, 2 * bytes);
-    bulk_load(to, gk + from, bytes, bar);
-    bulk_load(to + C::kTile, gv + from, bytes, bar);
-  };
-  if (lane == 0)
-    for (int k = 0, to = st; k < C::kStages && blk0 + k < blk1; ++k) {
-      copy(blk0 + k, ring + to * 2 * C::kTile, &s_full[warp][to]);
-      if (++to == C::kStages) to = 0;
+    w.rows = q4_rows(w.q, a.shape, w.tile, w.used);
+    w.blocks = tile_blocks(w.rows, kBn2);
+    int blk0, blk1;
+    if constexpr (CL) {
+      const int rank = (int)(blockIdx.x % (unsigned)a.cluster);
+      blk0 = (int)((int64_t)rank * w.blocks.count / a.cluster);
+      blk1 = bad ? blk0 : (int)((int64_t)(rank + 1) * w.blocks.count / a.cluster);
+    } else {
+      blk0 = q4_cut(y0 - x, w.blocks.count), blk1 = q4_cut(y1 - x, w.blocks.count);
     }
+    if (CL || blk0 < blk1) {
+      // this warp's copies: its rows of each block
+      const int64_t row0 = ((int64_t)(a.layer0 + layer) * a.H_kv + w.kvh) * a.S_total + a.seq_off[seq];
+      const uint8_t *gk = a.K + row0 * C::kRow, *gv = a.V + row0 * C::kRow;
+      auto tile_row = [&](int i) { return (w.blocks.index(i) << kBn2) + warp * kSub; };
+      auto copy = [&](int i, uint8_t *to, uint64_t *bar) {  // lane 0: block i into a stage
+        const int r = tile_row(i);
+        const int n = min(kSub, w.rows.last + 1 - r);
+        if (n <= 0) return;
+        const int bytes = n * C::kRow;
+        const int64_t from = (int64_t)r * C::kRow;
+        mbar_arrive_expect_tx(bar, 2 * bytes);
+        bulk_load(to, gk + from, bytes, bar);
+        bulk_load(to + C::kTile, gv + from, bytes, bar);
+      };
+      if (lane == 0)
+        for (int k = 0, to = st; k < C::kStages && blk0 + k < blk1; ++k) {
+          copy(blk0 + k, ring + to * 2 * C::kTile, &s_full[warp][to]);
+          if (++to == C::kStages) to = 0;
+        }
 
-  // q as second operands, and its groups' sums in two terms for the least values
-  const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q +
-                           ((int64_t)layer * a.T + w.off) * H_q * D + (int64_t)w.kvh * a.g * D;
-  const int row_1 = w.tile * a.shape.rows;  // the tile's first query row
-  auto q_row = [&](int r) {  // row r of the item, or null
-    r += row_1;
-    return r < row_1 + w.used ? q + ((int64_t)(r / a.g) * H_q + r % a.g) * D : nullptr;
-  };
-  uint32_t qf[NT <= 2 ? NT : 1][4][4];
-  uint4 *s_q = (uint4 *)(smem + C::kSmem - C::kQ);
-  uint32_t sum_hi[NT], sum_lo[NT];
-  float cm[NT][2];  // column 2t, 2t+1: what turns its sums into log2 units
+      // q as second operands, and its groups' sums in two terms for the least values
+      const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q +
+                               ((int64_t)layer * a.T + w.off) * H_q * D + (int64_t)w.kvh * a.g * D;
+      const int row_1 = w.tile * a.shape.rows;  // the tile's first query row
+      auto q_row = [&](int r) {  // row r of the item, or null
+        r += row_1;
+        return r < row_1 + w.used ? q + ((int64_t)(r / a.g) * H_q + r % a.g) * D : nullptr;
+      };
+      uint32_t qf[NT <= 2 ? NT : 1][4][4];
+      uint4 *s_q = (uint4 *)(smem + C::kSmem - C::kQ);
+      uint32_t sum_hi[NT], sum_lo[NT];
+      float cm[NT][2];  // column 2t, 2t+1: what turns its sums into log2 units
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const __nv_bfloat16 *src = q_row(8 * nt + g);
-    uint4 v[kPieces];  // words t of the pieces: eight elements each
-    uint32_t most = 0;
+      for (int nt = 0; nt < NT; ++nt) {
+        const __nv_bfloat16 *src = q_row(8 * nt + g);
+        uint4 v[kPieces];  // words t of the pieces: eight elements each
+        uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      v[j] = src ? *(const uint4 *)(src + 8 * (4 * j + t)) : make_uint4(0, 0, 0, 0);
-      most = max_abs(max_abs(max_abs(most, v[j].x), max_abs(v[j].y, v[j].z)), v[j].w);
-    }
-    float big = fmaxf(bf16_low(most), bf16_high(most));
-    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-    // the power of two of the largest, kept where 2^120 over it is a number
-    const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -7), 114);
-    const float up = __uint_as_float((uint32_t)(120 - ex + 127) << 23);
-    const float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
-    cm[nt][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
-    cm[nt][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
-    const uint32_t up_even = pack_bf16(up, up), up_odd = pack_bf16(up * 0.0625f, up * 0.0625f);
-    float mine = 0.f;
+        for (int j = 0; j < kPieces; ++j) {
+          v[j] = src ? *(const uint4 *)(src + 8 * (4 * j + t)) : make_uint4(0, 0, 0, 0);
+          most = max_abs(max_abs(max_abs(most, v[j].x), max_abs(v[j].y, v[j].z)), v[j].w);
+        }
+        float big = fmaxf(bf16_low(most), bf16_high(most));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // the power of two of the largest, kept where 2^120 over it is a number
+        const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -7), 114);
+        const float up = __uint_as_float((uint32_t)(120 - ex + 127) << 23);
+        const float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
+        cm[nt][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
+        cm[nt][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
+        const uint32_t up_even = pack_bf16(up, up), up_odd = pack_bf16(up * 0.0625f, up * 0.0625f);
+        float mine = 0.f;
 #pragma unroll
-    for (int gr = 0; gr < 4; ++gr) {
-      const uint4 w4 = v[piece_of<D>(gr)];
-      const uint32_t x[4] = {w4.x, w4.y, w4.z, w4.w};
-      const bool in = of_group<D, 4>(gr, t);
-      uint32_t f[4];
-      float sum = 0.f;
+        for (int gr = 0; gr < 4; ++gr) {
+          const uint4 w4 = v[piece_of<D>(gr)];
+          const uint32_t x[4] = {w4.x, w4.y, w4.z, w4.w};
+          const bool in = of_group<D, 4>(gr, t);
+          uint32_t f[4];
+          float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {  // pair i of a word; odd ones meet 16 c
-        f[i] = in ? mul_bf16x2(x[i], i & 1 ? up_odd : up_even) : 0u;
-        sum += bf16_low(x[i]) + bf16_high(x[i]);
+          for (int i = 0; i < 4; ++i) {  // pair i of a word; odd ones meet 16 c
+            f[i] = in ? mul_bf16x2(x[i], i & 1 ? up_odd : up_even) : 0u;
+            sum += bf16_low(x[i]) + bf16_high(x[i]);
+          }
+          sum = in ? sum : 0.f;
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          if (t == gr) mine = sum * (up * 0x1p-120f) * 0x1p-13f;
+          if constexpr (NT <= 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qf[nt][gr][i] = f[i];
+          } else if (warp == 0) {
+            s_q[(nt * 4 + gr) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
+          }
+        }
+        const float hi = __bfloat162float(__float2bfloat16_rn(mine));
+        sum_hi[nt] = pack_bf16(0.f, hi);
+        sum_lo[nt] = pack_bf16(0.f, mine - hi);
       }
-      sum = in ? sum : 0.f;
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (t == gr) mine = sum * (up * 0x1p-120f) * 0x1p-13f;
-      if constexpr (NT <= 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qf[nt][gr][i] = f[i];
-      } else if (warp == 0) {
-        s_q[(nt * 4 + gr) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
-      }
-    }
-    const float hi = __bfloat162float(__float2bfloat16_rn(mine));
-    sum_hi[nt] = pack_bf16(0.f, hi);
-    sum_lo[nt] = pack_bf16(0.f, mine - hi);
-  }
-  if constexpr (NT > 2) __syncthreads();
+      if constexpr (NT > 2) __syncthreads();
 
-  const int low_max = a.shape.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.shape.window) : 0;
-  const int suffix0 = w.q.n - a.suffix_w;  // (n and suffix_w are positive)
+      const int low_max =
+          a.shape.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.shape.window) : 0;
+      const int suffix0 = w.q.n - a.suffix_w;  // (n and suffix_w are positive)
 
-  float o[NT][4][2][4] = {};
-  float ox[NT][4] = {};  // rows 2 gr: the weights times group gr's scales; rows 2 gr + 1: times least values
-  float m[NT][2], top[NT][2], l[NT][2], hs[NT][2], sf[NT][2];  // top: the largest score, less m
+      float o[NT][4][2][4] = {};
+      // rows 2 gr: the weights times group gr's scales; rows 2 gr + 1: times its least values
+      float ox[NT][4] = {};
+      float m[NT][2], top[NT][2], l[NT][2], hs[NT][2], sf[NT][2];  // top: the largest score, less m
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      m[nt][c] = top[nt][c] = kNone;
-      l[nt][c] = hs[nt][c] = sf[nt][c] = 0.f;
-    }
+        for (int c = 0; c < 2; ++c) {
+          m[nt][c] = top[nt][c] = kNone;
+          l[nt][c] = hs[nt][c] = sf[nt][c] = 0.f;
+        }
 
-  constexpr int J = C::kJoint;
-  for (int i = blk0; i < blk1; ++i) {
-    const int r0 = tile_row(i);
-    uint8_t *stage = ring + st * 2 * C::kTile;
-    uint64_t *bar = &s_full[warp][st];
-    if (r0 <= w.rows.last) {  // (the same for the whole warp)
-      if (!mbar_wait_warp(bar, phase)) {
-        gave_up = true;
-        break;
-      }
-      // `open`: every query sees every row (and, for the statistics, none is in the suffix)
-      auto tile = [&](auto open_tile, int h0) {
-        constexpr bool open = decltype(open_tile)::value;
-        const uint8_t *sk = stage + h0 * 16 * C::kRow;
-        const uint32_t k_at = smem_addr(sk), v_at = k_at + C::kTile;
-        const int rh = r0 + 16 * h0;
-        // ---- scores
-        float raw[J][NT][4], z[J][NT][4];
+      constexpr int J = C::kJoint;
+      for (int i = blk0; i < blk1; ++i) {
+        const int r0 = tile_row(i);
+        uint8_t *stage = ring + st * 2 * C::kTile;
+        uint64_t *bar = &s_full[warp][st];
+        if (r0 <= w.rows.last) {  // (the same for the whole warp)
+          if (!mbar_wait_warp(bar, phase)) {
+            gave_up = true;
+            break;
+          }
+          // `open`: every query sees every row (and, for the statistics, none is in the suffix)
+          auto tile = [&](auto open_tile, int h0) {
+            constexpr bool open = decltype(open_tile)::value;
+            const uint8_t *sk = stage + h0 * 16 * C::kRow;
+            const uint32_t k_at = smem_addr(sk), v_at = k_at + C::kTile;
+            const int rh = r0 + 16 * h0;
+            // ---- scores
+            float raw[J][NT][4], z[J][NT][4];
 #pragma unroll
-        for (int h = 0; h < J; ++h) {
-          uint32_t ga, gb;
-          ldmatrix2(ga, gb, k_at + at2 + h * 16 * C::kRow);
-          // (the scales in the even slots meet zeros)
+            for (int h = 0; h < J; ++h) {
+              uint32_t ga, gb;
+              ldmatrix2(ga, gb, k_at + at2 + h * 16 * C::kRow);
+              // (the scales in the even slots meet zeros)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            mma_bf16(raw[h][nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
-          const uint4 pa = *(const uint4 *)(sk + (16 * h + g) * C::kRow + D / 2);
-          const uint4 pb = *(const uint4 *)(sk + (16 * h + g + 8) * C::kRow + D / 2);
-          const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
+              for (int nt = 0; nt < NT; ++nt)
+                mma_bf16(raw[h][nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
+              const uint4 pa = *(const uint4 *)(sk + (16 * h + g) * C::kRow + D / 2);
+              const uint4 pb = *(const uint4 *)(sk + (16 * h + g + 8) * C::kRow + D / 2);
+              const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
-          for (int j2 = 0; j2 < kPieces; j2 += 2) {
-            uint32_t kw[4];
-            ldmatrix4(kw, k_at + at4 + h * 16 * C::kRow + 16 * j2);
+              for (int j2 = 0; j2 < kPieces; j2 += 2) {
+                uint32_t kw[4];
+                ldmatrix4(kw, k_at + at4 + h * 16 * C::kRow + 16 * j2);
 #pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-              const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
-              const uint32_t fa[4] = {wa & kQ4Low, wa & kQ4High, va & kQ4Low, va & kQ4High};
-              const uint32_t fb[4] = {wb & kQ4Low, wb & kQ4High, vb & kQ4Low, vb & kQ4High};
+                for (int jj = 0; jj < 2; ++jj) {
+                  const uint32_t wa = kw[2 * jj], wb = kw[2 * jj + 1], va = wa >> 8, vb = wb >> 8;
+                  const uint32_t fa[4] = {wa & kQ4Low, wa & kQ4High, va & kQ4Low, va & kQ4High};
+                  const uint32_t fb[4] = {wb & kQ4Low, wb & kQ4High, vb & kQ4Low, vb & kQ4High};
 #pragma unroll
-              for (int gi = 0; gi < 4 / kPieces; ++gi) {
-                const int gr = (j2 + jj) * (4 / kPieces) + gi;
-                const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
+                  for (int gi = 0; gi < 4 / kPieces; ++gi) {
+                    const int gr = (j2 + jj) * (4 / kPieces) + gi;
+                    const float s_a = bf16_low(par_a[gr]), s_b = bf16_low(par_b[gr]);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                  uint32_t f[4];
-                  if constexpr (NT <= 2) {
+                    for (int nt = 0; nt < NT; ++nt) {
+                      uint32_t f[4];
+                      if constexpr (NT <= 2) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[e] = qf[nt][gr][e];
-                  } else {
-                    const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
-                    f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+                        for (int e = 0; e < 4; ++e) f[e] = qf[nt][gr][e];
+                      } else {
+                        const uint4 v = s_q[(nt * 4 + gr) * 32 + lane];
+                        f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+                      }
+                      float d[4];
+                      mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], 0.f, 0.f, 0.f, 0.f);
+                      mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
+                      raw[h][nt][0] = __fmaf_rn(s_a, d[0], raw[h][nt][0]);
+                      raw[h][nt][1] = __fmaf_rn(s_a, d[1], raw[h][nt][1]);
+                      raw[h][nt][2] = __fmaf_rn(s_b, d[2], raw[h][nt][2]);
+                      raw[h][nt][3] = __fmaf_rn(s_b, d[3], raw[h][nt][3]);
+                    }
                   }
-                  float d[4];
-                  mma_bf16(d, fa[0], fb[0], fa[1], fb[1], f[0], f[1], 0.f, 0.f, 0.f, 0.f);
-                  mma_bf16(d, fa[2], fb[2], fa[3], fb[3], f[2], f[3], d[0], d[1], d[2], d[3]);
-                  raw[h][nt][0] = __fmaf_rn(s_a, d[0], raw[h][nt][0]);
-                  raw[h][nt][1] = __fmaf_rn(s_a, d[1], raw[h][nt][1]);
-                  raw[h][nt][2] = __fmaf_rn(s_b, d[2], raw[h][nt][2]);
-                  raw[h][nt][3] = __fmaf_rn(s_b, d[3], raw[h][nt][3]);
                 }
               }
+              // in log2 units, less the maximum in use
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  z[h][nt][j] = __fmaf_rn(raw[h][nt][j], cm[nt][j & 1], -m[nt][j & 1]);
+            }
+            // ---- what each query may see
+            if (!open) {
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  const int qr = min(8 * nt + 2 * t + c, w.used - 1) + row_1;
+                  const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
+                  const int low =
+                      a.shape.window ? (int)plan_max(0, (int64_t)last + 1 - a.shape.window) : 0;
+#pragma unroll
+                  for (int h = 0; h < J; ++h)
+#pragma unroll
+                    for (int j = c; j < 4; j += 2) {
+                      const int r = rh + 16 * h + g + 8 * (j >> 1);
+                      if (r > last || (r < low && r >= a.shape.sink)) z[h][nt][j] = kHidden;
+                    }
+                }
+            }
+            // ---- maxima, kept while no score passes them by kLazy
+            float past = kHidden;
+#pragma unroll
+            for (int h = 0; h < J; ++h)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) past = fmaxf(past, z[h][nt][j]);
+            if (__any_sync(0xffffffffu, past > kLazy)) {
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  // (from the sums again: a first maximum is no difference to kNone)
+                  float x = m[nt][c];
+#pragma unroll
+                  for (int h = 0; h < J; ++h)
+#pragma unroll
+                    for (int j = c; j < 4; j += 2) {
+                      raw[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] * cm[nt][c];
+                      x = fmaxf(x, raw[h][nt][j]);
+                    }
+                  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                  const float by = m[nt][c] - x, f = exp2_fast(by);
+                  m[nt][c] = x;
+#pragma unroll
+                  for (int h = 0; h < J; ++h)
+#pragma unroll
+                    for (int j = c; j < 4; j += 2)
+                      z[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] - x;
+                  if (STATS) {
+                    top[nt][c] += by;
+                    hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
+                    sf[nt][c] *= f;
+                  }
+                  l[nt][c] *= f;
+#pragma unroll
+                  for (int j = c; j < 4; j += 2) {
+                    ox[nt][j] *= f;
+#pragma unroll
+                    for (int gr = 0; gr < 4; ++gr)
+#pragma unroll
+                      for (int u = 0; u < 2; ++u) o[nt][gr][u][j] *= f;
+                  }
+                }
+            }
+            // ---- weights: p0 = keys 2t, 2t+1 and p1 = keys 2t+8, 2t+9 of query row g
+            uint32_t p0[J][NT], p1[J][NT];
+#pragma unroll
+            for (int h = 0; h < J; ++h)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float p[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const int c = j & 1;
+                  p[j] = exp2_fast(z[h][nt][j]);
+                  l[nt][c] += p[j];
+                  if (STATS) {
+                    top[nt][c] = fmaxf(top[nt][c], z[h][nt][j]);
+                    hs[nt][c] = __fmaf_rn(p[j], z[h][nt][j], hs[nt][c]);
+                  }
+                }
+                if (STATS && !open) {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    if (rh + 16 * h + g + 8 * (j >> 1) >= suffix0) sf[nt][j & 1] += p[j];
+                }
+                p0[h][nt] = transposed(pack_bf16(p[0], p[1]));
+                p1[h][nt] = transposed(pack_bf16(p[2], p[3]));
+              }
+            // ---- results: this thread's keys
+#pragma unroll
+            for (int h = 0; h < J; ++h) {
+              // half word g of the parameters of two keys: scales (g even) or least values
+              uint32_t xa, xb;
+              ldmatrix2_trans(xa, xb, v_at + at2 + h * 16 * C::kRow);
+              uint32_t sa[4], sb[4];
+#pragma unroll
+              for (int gr = 0; gr < 4; ++gr) {
+                sa[gr] = __shfl_sync(0xffffffffu, xa, 8 * gr + t);
+                sb[gr] = __shfl_sync(0xffffffffu, xb, 8 * gr + t);
+              }
+              if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
+                const int r = rh + 16 * h + 2 * t, e = w.rows.last;
+                xa = finite_pair(xa, r <= e, r + 1 <= e);
+                xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
+              }
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_bf16(ox[nt], xa, 0u, xb, 0u, p0[h][nt], p1[h][nt], ox[nt][0], ox[nt][1],
+                         ox[nt][2], ox[nt][3]);
+#pragma unroll
+              for (int j2 = 0; j2 < kPieces; j2 += 2) {
+                uint32_t vw[4];
+                ldmatrix4_trans(vw, v_at + at4 + h * 16 * C::kRow + 16 * j2);
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj) {
+                  const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
+                  const uint32_t fa[4] = {centred(wa & kQ4Low, false), centred(wa & kQ4High, true),
+                                          centred(ua & kQ4Low, false), centred(ua & kQ4High, true)};
+                  const uint32_t fb[4] = {centred(wb & kQ4Low, false), centred(wb & kQ4High, true),
+                                          centred(ub & kQ4Low, false), centred(ub & kQ4High, true)};
+#pragma unroll
+                  for (int gi = 0; gi < 4 / kPieces; ++gi) {
+                    const int gr = (j2 + jj) * (4 / kPieces) + gi;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                      const uint32_t pa = p0[h][nt], pb = p1[h][nt];
+                      uint32_t b0 = mul_bf16x2(pa, sa[gr]), b1 = mul_bf16x2(pb, sb[gr]);
+                      if (!open) {  // a weight of zero stays zero, whatever the scale holds
+                        b0 &= (pa & 0xffffu ? 0xffffu : 0u) | (pa >> 16 ? 0xffff0000u : 0u);
+                        b1 &= (pb & 0xffffu ? 0xffffu : 0u) | (pb >> 16 ? 0xffff0000u : 0u);
+                      }
+#pragma unroll
+                      for (int u = 0; u < 2; ++u)
+                        mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
+                                 o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
+                    }
+                  }
+                }
+              }
+            }
+          };
+          if (r0 + kSub - 1 <= w.rows.first && r0 >= low_max && (!STATS || r0 + kSub <= suffix0)) {
+#pragma unroll 1
+            for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::true_type(), h0);
+          } else {
+#pragma unroll 1
+            for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::false_type(), h0);
+          }
+          __syncwarp();  // the stage has been read
+          if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages, stage, bar);
+          if (++st == C::kStages) {
+            st = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      if (gave_up && lane == 0) {
+        set_status(a.status, LG_ERR_TIMEOUT);
+        linger();
+      }
+      // every warp's copies have landed (or lingered): the ring becomes the results' place
+      gave_up = __syncthreads_or(gave_up);
+
+      // ---- the warps' results: sums of a query row over the key lanes, then over the warps
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x[4] = {m[nt][c] + (STATS ? top[nt][c] : 0.f), l[nt][c], hs[nt][c], sf[nt][c]};
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) {
+            if (STATS) x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], off));
+            x[1] += __shfl_xor_sync(0xffffffffu, x[1], off);
+            if (STATS) {
+              x[2] += __shfl_xor_sync(0xffffffffu, x[2], off);
+              x[3] += __shfl_xor_sync(0xffffffffu, x[3], off);
             }
           }
-          // in log2 units, less the maximum in use
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              z[h][nt][j] = __fmaf_rn(raw[h][nt][j], cm[nt][j & 1], -m[nt][j & 1]);
-        }
-        // ---- what each query may see
-        if (!open) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const int qr = min(8 * nt + 2 * t + c, w.used - 1) + row_1;
-              const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
-              const int low = a.shape.window ? (int)plan_max(0, (int64_t)last + 1 - a.shape.window) : 0;
-#pragma unroll
-              for (int h = 0; h < J; ++h)
-#pragma unroll
-                for (int j = c; j < 4; j += 2) {
-                  const int r = rh + 16 * h + g + 8 * (j >> 1);
-                  if (r > last || (r < low && r >= a.shape.sink)) z[h][nt][j] = kHidden;
-                }
-            }
-        }
-        // ---- maxima, kept while no score passes them by kLazy
-        float past = kHidden;
-#pragma unroll
-        for (int h = 0; h < J; ++h)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) past = fmaxf(past, z[h][nt][j]);
-        if (__any_sync(0xffffffffu, past > kLazy)) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              // (from the sums again: a first maximum is no difference to kNone)
-              float x = m[nt][c];
-#pragma unroll
-              for (int h = 0; h < J; ++h)
-#pragma unroll
-                for (int j = c; j < 4; j += 2) {
-                  raw[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] * cm[nt][c];
-                  x = fmaxf(x, raw[h][nt][j]);
-                }
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-              const float by = m[nt][c] - x, f = exp2_fast(by);
-              m[nt][c] = x;
-#pragma unroll
-              for (int h = 0; h < J; ++h)
-#pragma unroll
-                for (int j = c; j < 4; j += 2)
-                  z[h][nt][j] = z[h][nt][j] == kHidden ? kHidden : raw[h][nt][j] - x;
-              if (STATS) {
-                top[nt][c] += by;
-                hs[nt][c] = l[nt][c] > 0.f ? f * __fmaf_rn(by, l[nt][c], hs[nt][c]) : 0.f;
-                sf[nt][c] *= f;
-              }
-              l[nt][c] *= f;
-#pragma unroll
-              for (int j = c; j < 4; j += 2) {
-                ox[nt][j] *= f;
-#pragma unroll
-                for (int gr = 0; gr < 4; ++gr)
-#pragma unroll
-                  for (int u = 0; u < 2; ++u) o[nt][gr][u][j] *= f;
-              }
-            }
-        }
-        // ---- weights: p0 = keys 2t, 2t+1 and p1 = keys 2t+8, 2t+9 of query row g
-        uint32_t p0[J][NT], p1[J][NT];
-#pragma unroll
-        for (int h = 0; h < J; ++h)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float p[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int c = j & 1;
-              p[j] = exp2_fast(z[h][nt][j]);
-              l[nt][c] += p[j];
-              if (STATS) {
-                top[nt][c] = fmaxf(top[nt][c], z[h][nt][j]);
-                hs[nt][c] = __fmaf_rn(p[j], z[h][nt][j], hs[nt][c]);
-              }
-            }
-            if (STATS && !open) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (rh + 16 * h + g + 8 * (j >> 1) >= suffix0) sf[nt][j & 1] += p[j];
-            }
-            p0[h][nt] = transposed(pack_bf16(p[0], p[1]));
-            p1[h][nt] = transposed(pack_bf16(p[2], p[3]));
+          float f = 1.f;
+          if (STATS) {  // from the lagging maximum to the true one
+            const float by = m[nt][c] - x[0];
+            f = x[1] > 0.f ? exp2_fast(by) : 1.f;
+            x[2] = x[1] > 0.f ? f * __fmaf_rn(by, x[1], x[2]) : 0.f;
+            x[1] *= f;
+            x[3] *= f;
           }
-        // ---- results: this thread's keys
-#pragma unroll
-        for (int h = 0; h < J; ++h) {
-          uint32_t xa, xb;  // half word g of the parameters of two keys: scales (g even) or least values
-          ldmatrix2_trans(xa, xb, v_at + at2 + h * 16 * C::kRow);
-          uint32_t sa[4], sb[4];
+          const int row = 8 * nt + 2 * t + c;
+          if (g == 0) s_st[warp][row] = make_float4(x[0], x[1], x[2], x[3]);
 #pragma unroll
           for (int gr = 0; gr < 4; ++gr) {
-            sa[gr] = __shfl_sync(0xffffffffu, xa, 8 * gr + t);
-            sb[gr] = __shfl_sync(0xffffffffu, xb, 8 * gr + t);
-          }
-          if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
-            const int r = rh + 16 * h + 2 * t, e = w.rows.last;
-            xa = finite_pair(xa, r <= e, r + 1 <= e);
-            xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
-          }
+            const float base = __fmaf_rn(8.f, __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + t),
+                                         __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + 4 + t));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            mma_bf16(ox[nt], xa, 0u, xb, 0u, p0[h][nt], p1[h][nt], ox[nt][0], ox[nt][1], ox[nt][2], ox[nt][3]);
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int j2 = 0; j2 < kPieces; j2 += 2) {
-            uint32_t vw[4];
-            ldmatrix4_trans(vw, v_at + at4 + h * 16 * C::kRow + 16 * j2);
-#pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-              const uint32_t wa = vw[2 * jj], wb = vw[2 * jj + 1], ua = wa >> 8, ub = wb >> 8;
-              const uint32_t fa[4] = {centred(wa & kQ4Low, false), centred(wa & kQ4High, true),
-                                      centred(ua & kQ4Low, false), centred(ua & kQ4High, true)};
-              const uint32_t fb[4] = {centred(wb & kQ4Low, false), centred(wb & kQ4High, true),
-                                      centred(ub & kQ4Low, false), centred(ub & kQ4High, true)};
-#pragma unroll
-              for (int gi = 0; gi < 4 / kPieces; ++gi) {
-                const int gr = (j2 + jj) * (4 / kPieces) + gi;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                  const uint32_t pa = p0[h][nt], pb = p1[h][nt];
-                  uint32_t b0 = mul_bf16x2(pa, sa[gr]), b1 = mul_bf16x2(pb, sb[gr]);
-                  if (!open) {  // a weight of zero stays zero, whatever the scale holds
-                    b0 &= (pa & 0xffffu ? 0xffffu : 0u) | (pa >> 16 ? 0xffff0000u : 0u);
-                    b1 &= (pb & 0xffffu ? 0xffffu : 0u) | (pb >> 16 ? 0xffff0000u : 0u);
-                  }
-#pragma unroll
-                  for (int u = 0; u < 2; ++u)
-                    mma_bf16(o[nt][gr][u], fa[2 * u], fa[2 * u + 1], fb[2 * u], fb[2 * u + 1], b0, b1,
-                             o[nt][gr][u][0], o[nt][gr][u][1], o[nt][gr][u][2], o[nt][gr][u][3]);
-                }
-              }
-            }
+              for (int up = 0; up < 2; ++up)
+                if (of_group<D, 8>(gr, g))
+                  s_o[(warp * C::kRows + row) * (D + 1) + value_element<D>(gr, u, g, up)] =
+                      f * __fmaf_rn(up ? 4.f : 64.f, o[nt][gr][u][2 * up + c], base);
           }
         }
-      };
-      if (r0 + kSub - 1 <= w.rows.first && r0 >= low_max && (!STATS || r0 + kSub <= suffix0)) {
-#pragma unroll 1
-        for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::true_type(), h0);
-      } else {
-#pragma unroll 1
-        for (int h0 = 0; h0 < kSub / 16; h0 += J) tile(std::false_type(), h0);
       }
-      __syncwarp();  // the stage has been read
-      if (lane == 0 && i + C::kStages < blk1) copy(i + C::kStages, stage, bar);
-      if (++st == C::kStages) {
-        st = 0;
-        phase ^= 1;
-      }
-    }
-  }
-  if (gave_up && lane == 0) {
-    set_status(a.status, LG_ERR_TIMEOUT);
-    linger();
-  }
-  // every warp's copies have landed (or lingered): the ring becomes the results' place
-  gave_up = __syncthreads_or(gave_up);
-
-  // ---- the warps' results: sums of a query row over the key lanes, then over the warps
+      __syncthreads();
+      const bool alone = !CL && blk0 == 0 && blk1 == w.blocks.count;
+      float *s_part = (float *)(smem + C::kOut);  // [row][D + 4], as in the workspace
+      for (int r = warp; r < w.used; r += kWarps) {
+        float mx = kNone;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+        for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, s_st[k][r].x);
+        float f[kWarps], sl = 0.f, sh = 0.f, ss = 0.f;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      float x[4] = {m[nt][c] + (STATS ? top[nt][c] : 0.f), l[nt][c], hs[nt][c], sf[nt][c]};
+        for (int k = 0; k < kWarps; ++k) {
+          const float4 v = s_st[k][r];
+          const float by = v.x - mx;
+          f[k] = v.y != 0.f ? exp2_fast(by) : 0.f;
+          sl += f[k] * v.y;
+          if (STATS) {
+            sh += v.y != 0.f ? f[k] * __fmaf_rn(by, v.y, v.z) : 0.f;
+            ss += f[k] * v.w;
+          }
+        }
+        const int rr = r + row_1;
+        const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
+        float *part = CL ? s_part + r * (D + 4) : part_row<D>(a, layer, cta, x < y0 ? 0 : 1, r);
+        const float inv = sl != 0.f ? 1.f / sl : 0.f;
 #pragma unroll
-      for (int off = 4; off < 32; off <<= 1) {
-        if (STATS) x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], off));
-        x[1] += __shfl_xor_sync(0xffffffffu, x[1], off);
-        if (STATS) {
-          x[2] += __shfl_xor_sync(0xffffffffu, x[2], off);
-          x[3] += __shfl_xor_sync(0xffffffffu, x[3], off);
+        for (int e = lane; e < D; e += 32) {
+          float x = 0.f;
+#pragma unroll
+          for (int k = 0; k < kWarps; ++k)
+            if (f[k] != 0.f) x += f[k] * s_o[(k * C::kRows + r) * (D + 1) + e];
+          if (alone)
+            ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(x * inv);
+          else
+            part[e] = x;
+        }
+        if (lane == 0) {
+          if (!alone)
+            *(float4 *)(part + D) = make_float4(mx, sl, sh, ss);
+          else if (STATS)
+            ((float4 *)a.stats)[head] =
+                make_float4(mx * 0.6931471805599453f, sl,
+                            logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
         }
       }
-      float f = 1.f;
-      if (STATS) {  // from the lagging maximum to the true one
-        const float by = m[nt][c] - x[0];
-        f = x[1] > 0.f ? exp2_fast(by) : 1.f;
-        x[2] = x[1] > 0.f ? f * __fmaf_rn(by, x[1], x[2]) : 0.f;
-        x[1] *= f;
-        x[3] *= f;
+      if constexpr (CL) {
+        // the cluster's results: a warp 32 elements of a row, lane k the k-th CTA's statistics
+        cg::cluster_group cl = cg::this_cluster();
+        __shared__ int s_no;
+        if (tid == 0) s_no = bad || gave_up;
+        cl.sync();
+        bool no = false;
+        for (int k = 0; k < a.cluster; ++k) no |= *cl.map_shared_rank(&s_no, k) != 0;
+        const int n = no ? 0 : w.used * (D / 32);
+        for (int i = (int)cl.block_rank() * kWarps + warp; i < n; i += a.cluster * kWarps) {
+          const int r = i / (D / 32), e = i % (D / 32) * 32 + lane;
+          const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % a.cluster) + r * (D + 4) + D);
+          const bool any = v.y != 0.f;
+          const float mx = warp_max(any ? v.x : kNone), by = v.x - mx;
+          const float f = any ? exp2_fast(by) : 0.f;
+          float sl = f * v.y, sh = any ? f * __fmaf_rn(by, v.y, v.z) : 0.f, ss = f * v.w;
+#pragma unroll
+          for (int o = 1; o < kClusterMost; o <<= 1) {
+            if (o >= a.cluster) break;
+            sl += __shfl_xor_sync(0xffffffffu, sl, o);
+            sh += __shfl_xor_sync(0xffffffffu, sh, o);
+            ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          }
+          float y = 0.f;
+#pragma unroll
+          for (int k = 0; k < kClusterMost; ++k) {
+            if (k >= a.cluster) break;
+            const float fk = __shfl_sync(0xffffffffu, f, k);
+            const float z = cl.map_shared_rank(s_part, k)[r * (D + 4) + e];
+            if (fk != 0.f) y += fk * z;
+          }
+          const float inv = sl != 0.f ? 1.f / sl : 0.f;
+          const int rr = r + row_1;
+          const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
+          ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(y * inv);
+          if (STATS && e == 0)
+            ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
+                                                    logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
+        }
+        cl.sync();  // read before a CTA ends
+        return;
       }
-      const int row = 8 * nt + 2 * t + c;
-      if (g == 0) s_st[warp][row] = make_float4(x[0], x[1], x[2], x[3]);
-#pragma unroll
-      for (int gr = 0; gr < 4; ++gr) {
-        const float base = __fmaf_rn(8.f, __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + t),
-                                     __shfl_sync(0xffffffffu, ox[nt][c], 8 * gr + 4 + t));
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int up = 0; up < 2; ++up)
-            if (of_group<D, 8>(gr, g))
-              s_o[(warp * C::kRows + row) * (D + 1) + value_element<D>(gr, u, g, up)] =
-                  f * __fmaf_rn(up ? 4.f : 64.f, o[nt][gr][u][2 * up + c], base);
+      fence_proxy_async_smem();
+      __syncthreads();  // the results have been read: the ring is the next piece's
+    }
+    // the next item
+    if (++w.tile == tiles) {
+      w.tile = 0;
+      if (++w.kvh == a.H_kv) {
+        w.kvh = 0;
+        if (x + units >= y1) break;
+        do q4_seq(a, ++seq, w.q, w.off);
+        while (w.q.m == 0);
+        // (x is the old sequence's last item: the loop adds its units)
+        x += units;
+        units = q4_units(w.q, a.shape);
+        x -= units;
+        tiles = q4_tiles(w.q, a.shape);
       }
     }
-  }
-  __syncthreads();
-  const bool alone = !CL && blk0 == 0 && blk1 == w.blocks.count;
-  float *s_part = (float *)(smem + C::kOut);  // [row][D + 4], as in the workspace
-  for (int r = warp; r < w.used; r += kWarps) {
-    float mx = kNone;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, s_st[k][r].x);
-    float f[kWarps], sl = 0.f, sh = 0.f, ss = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-      const float4 v = s_st[k][r];
-      const float by = v.x - mx;
-      f[k] = v.y != 0.f ? exp2_fast(by) : 0.f;
-      sl += f[k] * v.y;
-      if (STATS) {
-        sh += v.y != 0.f ? f[k] * __fmaf_rn(by, v.y, v.z) : 0.f;
-        ss += f[k] * v.w;
-      }
-    }
-    const int rr = r + row_1;
-    const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
-    float *part = CL ? s_part + r * (D + 4) : part_row<D>(a, layer, cta, x < y0 ? 0 : 1, r);
-    const float inv = sl != 0.f ? 1.f / sl : 0.f;
-#pragma unroll
-    for (int e = lane; e < D; e += 32) {
-      float x = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k)
-        if (f[k] != 0.f) x += f[k] * s_o[(k * C::kRows + r) * (D + 1) + e];
-      if (alone)
-        ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(x * inv);
-      else
-        part[e] = x;
-    }
-    if (lane == 0) {
-      if (!alone)
-        *(float4 *)(part + D) = make_float4(mx, sl, sh, ss);
-      else if (STATS)
-        ((float4 *)a.stats)[head] =
-            make_float4(mx * 0.6931471805599453f, sl,
-                        logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
-    }
-  }
-  if constexpr (CL) {
-    // the cluster's results: a warp 32 elements of a row, lane k the k-th CTA's statistics
-    cg::cluster_group cl = cg::this_cluster();
-    __shared__ int s_no;
-    if (tid == 0) s_no = bad || gave_up;
-    cl.sync();
-    bool no = false;
-    for (int k = 0; k < a.cluster; ++k) no |= *cl.map_shared_rank(&s_no, k) != 0;
-    const int n = no ? 0 : w.used * (D / 32);
-    for (int i = (int)cl.block_rank() * kWarps + warp; i < n; i += a.cluster * kWarps) {
-      const int r = i / (D / 32), e = i % (D / 32) * 32 + lane;
-      const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % a.cluster) + r * (D + 4) + D);
-      const bool any = v.y != 0.f;
-      const float mx = warp_max(any ? v.x : kNone), by = v.x - mx;
-      const float f = any ? exp2_fast(by) : 0.f;
-      float sl = f * v.y, sh = any ? f * __fmaf_rn(by, v.y, v.z) : 0.f, ss = f * v.w;
-#pragma unroll
-      for (int o = 1; o < kClusterMost; o <<= 1) {
-        if (o >= a.cluster) break;
-        sl += __shfl_xor_sync(0xffffffffu, sl, o);
-        sh += __shfl_xor_sync(0xffffffffu, sh, o);
-        ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      }
-      float y = 0.f;
-#pragma unroll
-      for (int k = 0; k < kClusterMost; ++k) {
-        if (k >= a.cluster) break;
-        const float fk = __shfl_sync(0xffffffffu, f, k);
-        const float z = cl.map_shared_rank(s_part, k)[r * (D + 4) + e];
-        if (fk != 0.f) y += fk * z;
-      }
-      const float inv = sl != 0.f ? 1.f / sl : 0.f;
-      const int rr = r + row_1;
-      const int64_t head = ((int64_t)layer * a.T + w.off + rr / a.g) * H_q + w.kvh * a.g + rr % a.g;
-      ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(y * inv);
-      if (STATS && e == 0)
-        ((float4 *)a.stats)[head] = make_float4(mx * 0.6931471805599453f, sl,
-                                                logf(sl) - 0.6931471805599453f * sh * inv, ss * inv);
-    }
-    cl.sync();  // read before a CTA ends
-    return;
-  }
-  fence_proxy_async_smem();
-  __syncthreads();  // the results have been read: the ring is the next piece's
-  }
-  // the next item
-  if (++w.tile == tiles) {
-    w.tile = 0;
-    if (++w.kvh == a.H_kv) {
-      w.kvh = 0;
-      if (x + units >= y1) break;
-      do q4_seq(a, ++seq, w.q, w.off);
-      while (w.q.m == 0);
-      // (x is the old sequence's last item: the loop adds its units)
-      x += units;
-      units = q4_units(w.q, a.shape);
-      x -= units;
-      tiles = q4_tiles(w.q, a.shape);
-    }
-  }
   }
 }
 
-// The CTAs' results of a cut item (blockIdx = (the CTA whose start cuts it, 16 rows, layer)): the warps
-// share out the rows, then the parts of a row.  The maximum of all parts comes first, a lane a part, then
-// their sums with nothing but additions between the loads.
+// The CTAs' results of a cut item (blockIdx = (the CTA whose start cuts it, 16 rows, layer)): the
+// warps share out the rows, then the parts of a row.  The maximum of all parts comes first, a lane
+// a part, then their sums with nothing but additions between the loads.
 constexpr int kMergeWarps = 16;
 
 template <int D, bool STATS>
@@ -974,10 +986,11 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
   r.part_bytes = (r.part_bytes + 255) / 256 * 256;
-  // Few items of few blocks: as many CTAs each as the GPU holds of them, up to eight, which join their results
-  // themselves; while a CTA has at most 16 blocks of eight query rows, or 5 of more.  (us in a line with its
-  // second kernel and in clusters, 8 kv-heads: one sequence of 1025 rows 11.2 and 7.8, 24 of 700 17.0 and
-  // 11.8, 24 of 2049 22.8 and 19.6; with 16 query rows 12 of 1500 16.0 and, at 6 blocks a CTA, 18.4.)
+  // Few items of few blocks: as many CTAs each as the GPU holds of them, up to eight, which join
+  // their results themselves; while a CTA has at most 16 blocks of eight query rows, or 5 of more.
+  // (us in a line with its second kernel and in clusters, 8 kv-heads: one sequence of 1025 rows
+  // 11.2 and 7.8, 24 of 700 17.0 and 11.8, 24 of 2049 22.8 and 19.6; with 16 query rows 12 of 1500
+  // 16.0 and, at 6 blocks a CTA, 18.4.)
   const int64_t items = (int64_t)batch * H_kv * tiles;
   const Q4Shape shape{r.rows, g, window, sink, H_kv};
   const int one = q4_units(ChunkSeq{max_len, max_new < max_len ? max_new : max_len}, shape) - kQ4ItemUnits;

@@ -1,12 +1,13 @@
-// How the work of attention over a 4-bit cache is divided, in closed form, so that every CTA finds its
-// share from the lengths alone.
+// How the work of attention over a 4-bit cache is divided, in closed form, so that every CTA finds
+// its share from the lengths alone.
 //
-// An item is (sequence, kv-head, tile of query rows).  The items of a layer stand in one line, ordered
-// like that; an item takes the key blocks that any query of its sequence sees, and kQ4ItemUnits more
-// for its start and end, so all items of a sequence take the same.  Each of G CTAs takes ceil(W / G) units
-// of the line's W.  Its share of an item's blocks is a piece; an item of which one piece has every block
-// is finished by that CTA, the pieces of the others go through the workspace (slot 0 of a CTA for an
-// item that began before its share, slot 1 for one that begins in it) to a second kernel.
+// An item is (sequence, kv-head, tile of query rows).  The items of a layer stand in one line,
+// ordered like that; an item takes the key blocks that any query of its sequence sees, and
+// kQ4ItemUnits more for its start and end, so all items of a sequence take the same.  Each of G
+// CTAs takes ceil(W / G) units of the line's W.  Its share of an item's blocks is a piece; an item
+// of which one piece has every block is finished by that CTA, the pieces of the others go through
+// the workspace (slot 0 of a CTA for an item that began before its share, slot 1 for one that
+// begins in it) to a second kernel.
 #pragma once
 #include "lg_chunk_plan.cuh"
 

@@ -1,5 +1,5 @@
-// Rows of a 4-bit cache: new keys and values rotated, quantised and stored, and rows read back as the
-// bf16 values that they stand for.
+// Rows of a 4-bit cache: new keys and values rotated, quantised and stored, and rows read back as
+// the bf16 values that they stand for.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -14,15 +14,15 @@ namespace {
 
 // ---------------------------------------------------------------- new rows
 //
-// A thread holds 16 bytes (8 elements) of a token's heads, one word of codes, or two such where halves of
-// the whole head are rotated together.  It takes its cosines and sines once and walks over heads: queries
-// (rotated, stored as they are), keys (rotated, rounded to bf16 as a 16-bit cache would hold them,
-// quantised), values.  Otherwise the other elements of its pairs come by shuffles (so queries may be
-// rotated in place), as do the least and largest element of a group, over the 4 (d = 128) or 2 lanes
-// that hold it.
-// (GB300, ragged prompts of up to 4096 tokens, 32 query heads and 8 of keys and values of 128, 246 MB: 62 us,
-// 4 TB/s, the warps issuing in 64 % of the cycles; queries, keys and values in one loop with their
-// pointers chosen a head 95, a word a thread with the other half of its pairs by shuffles 103.)
+// A thread holds 16 bytes (8 elements) of a token's heads, one word of codes, or two such where
+// halves of the whole head are rotated together.  It takes its cosines and sines once and walks
+// over heads: queries (rotated, stored as they are), keys (rotated, rounded to bf16 as a 16-bit
+// cache would hold them, quantised), values.  Otherwise the other elements of its pairs come by
+// shuffles (so queries may be rotated in place), as do the least and largest element of a group,
+// over the 4 (d = 128) or 2 lanes that hold it. (GB300, ragged prompts of up to 4096 tokens, 32
+// query heads and 8 of keys and values of 128, 246 MB: 62 us, 4 TB/s, the warps issuing in 64 % of
+// the cycles; queries, keys and values in one loop with their pointers chosen a head 95, a word a
+// thread with the other half of its pairs by shuffles 103.)
 
 struct Q4AppendArgs {
   const __nv_bfloat16 *q, *k, *v;
@@ -67,8 +67,9 @@ __device__ __forceinline__ void token_slots_near(const lg_cache &c, const lg_chu
   token_slots(c, ch, t0, n, s_slot);
 }
 
-// ONE: token t is the one new row of sequence t, and blockIdx.y the layer.  PAIR: halves of the whole head
-// are rotated together, so a thread holds both elements of its pairs, words pc and pc + D / 16.
+// ONE: token t is the one new row of sequence t, and blockIdx.y the layer.  PAIR: halves of the
+// whole head are rotated together, so a thread holds both elements of its pairs, words pc and pc +
+// D / 16.
 template <int D, bool ONE, bool PAIR>
 __global__ void __launch_bounds__(kQ4Threads)
     q4_append_kernel(lg_cache c, lg_chunk ch, Q4AppendArgs a, const __grid_constant__ RopeTable tab) {
@@ -147,9 +148,9 @@ __global__ void __launch_bounds__(kQ4Threads)
     return make_uint4(r[0], r[1], r[2], r[3]);
   };
   const int64_t in = ONE ? (int64_t)blockIdx.y * c.batch + t : t;  // token row of the inputs
-  // Heads of one kind, head h of the combined line of queries, keys and values with thread h mod groups.
-  // Every lane of a warp makes the same number of turns, as the shuffles need them all; the words of
-  // kTogether heads are requested before the first is worked on.
+  // Heads of one kind, head h of the combined line of queries, keys and values with thread h mod
+  // groups. Every lane of a warp makes the same number of turns, as the shuffles need them all; the
+  // words of kTogether heads are requested before the first is worked on.
   auto heads = [&](auto kind, const __nv_bfloat16 *src, int before, int count, uint8_t *dst) {
     constexpr int kKind = decltype(kind)::value;  // 0: queries, 1: keys, 2: values
     const int first = (grp - before % groups + groups) % groups;
@@ -227,9 +228,9 @@ cudaError_t launch_append_as(const lg_cache &c, const lg_chunk &ch, Q4AppendArgs
                              const RopeTable &tab, cudaStream_t s) {
   constexpr int kLanes = D / 8 / (PAIR ? 2 : 1);
   const int heads = a.H_q + 2 * c.H_kv;
-  // as many heads a thread, for its cosines and sines to serve, as leave the GPU some waves of
-  // CTAs (ragged prompts of up to 4096 tokens: one wave 84 us, two 77, four 75, eight 104); a few tokens'
-  // heads over several CTAs
+  // as many heads a thread, for its cosines and sines to serve, as leave the GPU some waves of CTAs
+  // (ragged prompts of up to 4096 tokens: one wave 84 us, two 77, four 75, eight 104); a few
+  // tokens' heads over several CTAs
   const int64_t full = (int64_t)16 * 152 * kQ4Threads;
   a.groups = 1;
   while (a.groups * 2 <= kQ4Threads / kLanes && a.groups < heads &&
@@ -292,9 +293,10 @@ __global__ void __launch_bounds__(kQ4Threads)
 }
 
 // A layer's rows as values at the same slots of two 16-bit caches of one layer, for the kernels of
-// many query rows: what some query of the chunk sees.  blockIdx = (rows, kv-head, sequence).  Bound by its
-// stores: with all loads of a thread's 4 (2) words and parameters of keys and of values asked for before
-// the first store 55 us for 8 sequences of 8192 rows (352 MB, 6.4 TB/s), word by word 71.
+// many query rows: what some query of the chunk sees.  blockIdx = (rows, kv-head, sequence).  Bound
+// by its stores: with all loads of a thread's 4 (2) words and parameters of keys and of values
+// asked for before the first store 55 us for 8 sequences of 8192 rows (352 MB, 6.4 TB/s), word by
+// word 71.
 constexpr int kExpandRows = 64;
 
 template <int D>

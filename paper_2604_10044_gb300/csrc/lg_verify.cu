@@ -1,24 +1,25 @@
 // Drafted tokens against the target's probabilities, and the rows of those that fall.
 //
-// lg_verify_draft is two kernels.  The first reads every row of logits once: a CTA a slice of a row,
-// kept in registers between its maximum and its sum of exponentials.  The second, a cluster a
+// lg_verify_draft is two kernels.  The first reads every row of logits once: a CTA a slice of a
+// row, kept in registers between its maximum and its sum of exponentials.  The second, a cluster a
 // sequence, joins the slices, decides which drafts stand, and looks the random number up in the
 // distribution of the one row that the next token comes from.
 //
-// Which token a number falls on is exact only as far as the sums are: a bound between two tokens that
-// moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's bounds
-// on the way.  So what a lane sums (16 weights) goes into the totals as an integer in units of 2^-62 of a
-// mass of one, and integers add up to the same in any order; the quotient by a temperature keeps a
-// second term; and the joining of a row's slices is in integers too, with powers of two to 2^-30.
+// Which token a number falls on is exact only as far as the sums are: a bound between two tokens
+// that moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's
+// bounds on the way.  So what a lane sums (16 weights) goes into the totals as an integer in units
+// of 2^-62 of a mass of one, and integers add up to the same in any order; the quotient by a
+// temperature keeps a second term; and the joining of a row's slices is in integers too, with
+// powers of two to 2^-30.
 //
-// GB300, 261 rows of 128257 bf16 logits of 64 sequences: 19 us in the first kernel (67 MB, 3.5 TB/s; an element
-// takes some ten instructions, and the CTAs issue in 60 % of the cycles), 18 in the second, 37 a call;
-// one sequence's five rows of 151936 fp32: 4 and 10, all latency (the draft's and the slices' loads, two
-// rounds over 512 elements a warp, a cluster barrier).  What it took, for 64 sequences and for one: loads
-// and work element by element 196 and 59 us; packed fp32 in place of scalar, all of a segment loaded first
-// 51 and 21; logits kept packed, lanes' sums in fp32 41 and 20; the slices joined in integers instead of in
-// 64-bit floating point 37 and 14.  Not kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence
-// more 41 to 50.
+// GB300, 261 rows of 128257 bf16 logits of 64 sequences: 19 us in the first kernel (67 MB, 3.5
+// TB/s; an element takes some ten instructions, and the CTAs issue in 60 % of the cycles), 18 in
+// the second, 37 a call; one sequence's five rows of 151936 fp32: 4 and 10, all latency (the
+// draft's and the slices' loads, two rounds over 512 elements a warp, a cluster barrier).  What it
+// took, for 64 sequences and for one: loads and work element by element 196 and 59 us; packed fp32
+// in place of scalar, all of a segment loaded first 51 and 21; logits kept packed, lanes' sums in
+// fp32 41 and 20; the slices joined in integers instead of in 64-bit floating point 37 and 14.  Not
+// kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence more 41 to 50.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -51,9 +52,10 @@ struct RowPart {     // of a slice of a row
   uint64_t z;        // sum of exp((x - m) / temperature) in 2^-40
 };
 
-// log2(e) / temperature in two terms, the second times ln 2; a temperature of zero (or nothing above it)
-// takes the top token.  Temperatures are kept in [2^-60, 2^40] and distances from the maximum above -2^60,
-// so every product is a number and what is further down, or masked, weighs nothing.
+// log2(e) / temperature in two terms, the second times ln 2; a temperature of zero (or nothing
+// above it) takes the top token.  Temperatures are kept in [2^-60, 2^40] and distances from the
+// maximum above -2^60, so every product is a number and what is further down, or masked, weighs
+// nothing.
 struct Heat {
   float hi, lo;
   bool greedy;
@@ -77,8 +79,8 @@ __device__ __forceinline__ Heat heat_of(float t) {
   return h;
 }
 
-// exp(d / temperature) of two distances d = x - m from a finite maximum, within some 2^-22 and without a
-// drift over the range: 2^y (1 + rest), y the product with the first term
+// exp(d / temperature) of two distances d = x - m from a finite maximum, within some 2^-22 and
+// without a drift over the range: 2^y (1 + rest), y the product with the first term
 __device__ __forceinline__ float2 weights(float2 d, const Heat &h) {
   d.x = fmaxf(d.x, kFar);
   d.y = fmaxf(d.y, kFar);
@@ -220,10 +222,10 @@ struct Row {
   int fallen; // the row's draft, -1 for a last row
 };
 
-// v exp((x - m) / temperature), x <= m, in integers (64-bit floating point runs at a hundredth of their
-// speed here: it made this step 5 us of a call).  The exponent is a distance without error times two
-// terms, in units of 2^-32; the power of two of its fraction is the power series sum of (f ln 2)^k / k!
-// to k = 11, every term positive, cut to 2^-32 at each step.
+// v exp((x - m) / temperature), x <= m, in integers (64-bit floating point runs at a hundredth of
+// their speed here: it made this step 5 us of a call).  The exponent is a distance without error
+// times two terms, in units of 2^-32; the power of two of its fraction is the power series sum of
+// (f ln 2)^k / k! to k = 11, every term positive, cut to 2^-32 at each step.
 __device__ __forceinline__ uint64_t scaled(uint64_t v, float x, float m, const Heat &h) {
   if (x == m) return v;
   const float d = x - m, back = d - x, rest = (x - (d - back)) - (m + back);  // x - m = d + rest
@@ -282,16 +284,16 @@ __device__ __forceinline__ float draft_at(const VerifyArgs &a, int64_t row, int 
   return q > 0.f ? q : 0.f;
 }
 
-// a mass of [0, 1] in 2^-62, its last bits cut off below 2^-39 (by shifts: the conversion instruction for 64
-// bits took most of this kernel's time)
+// a mass of [0, 1] in 2^-62, its last bits cut off below 2^-39 (by shifts: the conversion
+// instruction for 64 bits took most of this kernel's time)
 __device__ __forceinline__ uint64_t units_of(float w) {
   const uint32_t bits = __float_as_uint(w), mant = (bits & 0x7fffffu) | 0x800000u;
   const int sh = (int)(bits >> 23) - (127 - 39);
   return sh >= 0 ? (uint64_t)mant << sh : (uint64_t)(mant >> min(-sh, 31));
 }
 
-// a lane's elements of a segment, summed in fp32 before they become units (half the work of this kernel
-// otherwise): over the lanes of a vocabulary the roundings leave some 2^-30 of the mass
+// a lane's elements of a segment, summed in fp32 before they become units (half the work of this
+// kernel otherwise): over the lanes of a vocabulary the roundings leave some 2^-30 of the mass
 __device__ __forceinline__ uint64_t lane_units(const float (&w)[kSeg]) {
   float2 s = make_float2(w[0], w[1]);
 #pragma unroll
@@ -326,8 +328,8 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   if (tid == 0) s_first = max(m - 1, 0);
   __syncthreads();
   const Heat h = heat_of(t);
-  // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have read
-  // another one
+  // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have
+  // read another one
   const bool bad = s_bad != 0;
   // the first draft that does not stand: a warp a row
   for (int j = warp; j < m && !bad; j += kPickWarps) {
@@ -484,8 +486,8 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       if (want < before + sum) break;
       before += sum;
     }
-    // the segment again with neighbours in a lane: the lanes' sums, then the elements of one lane.  (They
-    // may stay short of the sum above by roundings: the last element that has a mass then.)
+    // the segment again with neighbours in a lane: the lanes' sums, then the elements of one lane.
+    // (They may stay short of the sum above by roundings: the last element that has a mass then.)
     const int i0 = g * kSegElems + lane * kSeg;
     float w[kSeg];
     masses(i0, 1, w);
@@ -536,7 +538,7 @@ __global__ void end_chunk_kernel(lg_cache c, lg_chunk ch, const int32_t *accepte
   const int n = c.len[b], a = accepted[b];
   if (status_bad(c.dev_status)) return;
   const int64_t m = o1 - o0;
-  if (o0 < 0 || m < 0 || o1 > ch.T || m > ch.max_new || m > n || a < 0 || (m > 0 && a > m - 1))
+  if (o0 < 0 || m < 0 || o1 > ch.T || m > ch.max_new || m > n || (m > 0 && (a < 0 || a > m - 1)))
     set_status(c.dev_status, LG_ERR_CAPACITY);
   else if (m > 0)
     c.len[b] = n - (int)(m - 1 - a);
@@ -567,7 +569,8 @@ cudaError_t launch_pick_typed(const VerifyArgs &a, cudaStream_t s) {
 
 template <typename T>
 cudaError_t launch_verify_typed(const VerifyArgs &a, cudaStream_t s) {
-  LG_TRY(launch_pdl(verify_rows_kernel<T>, dim3(a.slices, a.T), kRowThreads, 0, s, a));
+  if (a.T)  // (a chunk without rows has its counts to set)
+    LG_TRY(launch_pdl(verify_rows_kernel<T>, dim3(a.slices, a.T), kRowThreads, 0, s, a));
   return a.draft.dtype == LG_BF16 ? launch_pick_typed<T, __nv_bfloat16>(a, s)
                                   : launch_pick_typed<T, float>(a, s);
 }

@@ -71,7 +71,7 @@ def test_verify_refusals():
             (dict(accepted=(F << 5) + 4 * T - 4), 1), (dict(temp=(F << 6) + 4), 1),
             (dict(draft=rows(x=F << 5)), 1), (dict(picked=F << 7), 1)]:
         assert verify(**kw) == code, kw
-    assert verify(ch=lg.LgChunk(off=F, T=0, max_new=0)) == 0
+    assert verify(ch=lg.LgChunk(off=F, T=0, max_new=0), ws=None) == 6
     L = lg.lib()
     assert L.lg_verify_workspace_size(None, by(lg.LgChunk(off=F, T=T, max_new=5))) == 0
     assert L.lg_verify_workspace_size(ctypes.addressof(rows()), None) == 0

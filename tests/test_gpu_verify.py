@@ -181,11 +181,27 @@ def test_status_and_captured_calls(cuda):
     assert (picked == 9).all()
 
 
+def test_a_step_of_no_rows(cuda):
+    """every sequence rests: nothing is read, nothing stands"""
+    x = torch.full((1, 50), math.nan, device=cuda)
+    ch = lg.Chunk.of([0, 0, 0], cuda)
+    z = torch.zeros(3, device=cuda)
+    picked = torch.full((1,), 9, dtype=torch.int32, device=cuda)
+    acc = torch.full((3,), 9, dtype=torch.int32, device=cuda)
+    ws = torch.empty(lg.lg_verify_workspace_size(x, ch), dtype=torch.uint8, device=cuda)
+    lg.lg_verify_draft(x, ch, picked.clone(), None, None, z, z, picked, acc, ws)
+    assert acc.tolist() == [0, 0, 0] and picked.tolist() == [9]
+
+
 def test_end_chunk(cuda):
     ns, ms = [10, 7, 5, 3], [4, 1, 0, 3]
     c = lg.Cache(1, 2, 64, "bf16", [0, 20, 40, 60], [20] * 4, ns, cuda)
     ch = lg.Chunk.of(ms, cuda)
     acc = torch.tensor([1, 0, 0, 2], dtype=torch.int32, device=cuda)
+    lg.lg_end_chunk(c, ch, acc)
+    assert lg.lg_read_device_status(c) == 0 and c.lengths().tolist() == [8, 7, 5, 3]
+    c = lg.Cache(1, 2, 64, "bf16", [0, 20, 40, 60], [20] * 4, ns, cuda)
+    acc[2] = -7                                       # of a sequence that had no rows
     lg.lg_end_chunk(c, ch, acc)
     assert lg.lg_read_device_status(c) == 0 and c.lengths().tolist() == [8, 7, 5, 3]
     for bad in ([4, 0, 0, 2], [-1, 0, 0, 2], [1, 1, 0, 2]):
