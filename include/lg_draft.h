@@ -44,8 +44,10 @@ LG_API size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch);
      picked[off[b] + j] = draft j for j < a, the next token for j = a, -1 for j > a
    so that the tokens of sequence b are distributed as the target's whatever the draft is, when u and r
    are uniform on [0, 1) and independent.  A draft outside [0, V) falls, with q_t = 0.
-   A weight is within about 2^-22; what 16 of them sum to is added up in integers, in units of 2^-62 of the
-   mass (2^-40 of the largest weight in p's own sum), so the same call gives the same tokens.
+   A weight is within about 2^-22 (2^-38 from 2^-10 of the mass on); what 16 of them sum to is added up in
+   integers, in units of 2^-62 of the mass (2^-40 of the largest weight in p's own sum), so the same call
+   gives the same tokens.  Where r falls within 2^-27 of the mass of a bound between two tokens, the row is
+   gone through again with every weight within 2^-38 (a call with such a sequence takes 100 to 200 us more).
    x: rows [0, T) at least (x->batch >= T); draft: nullable, as many rows of the same V, its own dtype and
    stride.  tokens: device [T]; temperature: nullable (1), device [batch]; u: device [T] (the entry of a
    sequence's last row is not used); r: device [batch]; picked: device [T], accepted: device [batch];
@@ -61,8 +63,8 @@ LG_API lg_status lg_verify_draft(const lg_logits *x, const lg_chunk *ch, int bat
                                  int32_t *dev_status, cudaStream_t s);
 
 /* Ends a chunk of which only the first accepted[b] + 1 rows stay: len[b] -= m_b - 1 - accepted[b]
-   (m_b = 0: nothing, whatever accepted[b] holds).  The counterpart of lg_begin_chunk after lg_verify_draft; the rows' slots are
-   taken by the next tokens.  An accepted[b] outside [0, m_b - 1], an m_b outside [0, max_new] or above
+   (m_b = 0: nothing, whatever accepted[b] holds).  The counterpart of lg_begin_chunk after
+   lg_verify_draft; the rows' slots are taken by the next tokens.  An accepted[b] outside [0, m_b - 1], an m_b outside [0, max_new] or above
    len[b], or an off[] outside [0, T] sets LG_ERR_CAPACITY on the device and leaves that sequence's
    length.  accepted: device [batch]. */
 LG_API lg_status lg_end_chunk(const lg_cache *c, const lg_chunk *ch, const int32_t *accepted,

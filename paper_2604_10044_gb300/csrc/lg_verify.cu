@@ -9,17 +9,23 @@
 // that moves by 1e-7 of the mass moves past one number in ten million for each of the vocabulary's
 // bounds on the way.  So what a lane sums (16 weights) goes into the totals as an integer in units
 // of 2^-62 of a mass of one, and integers add up to the same in any order; the quotient by a
-// temperature keeps a second term; and the joining of a row's slices is in integers too, with
-// powers of two to 2^-30.
+// temperature keeps a second term; a row's slices are joined, and its large masses computed, in
+// integers too, with powers of two to 2^-38; and a number nearer to a bound than 2^-27 of the mass
+// is looked up again with every mass in integers.  Sequences whose token was not the one of 64-bit
+// sums: 4 in 10^5 without the large masses and the second search; 4 of 1.44 million so (5 in 10^6
+// with a second search from 2^-28 on, 1 in 10^6 from 2^-26 on, met by a third and twice as many calls).
 //
 // GB300, 261 rows of 128257 bf16 logits of 64 sequences: 19 us in the first kernel (67 MB, 3.5
-// TB/s; an element takes some ten instructions, and the CTAs issue in 60 % of the cycles), 18 in
-// the second, 37 a call; one sequence's five rows of 151936 fp32: 4 and 10, all latency (the
-// draft's and the slices' loads, two rounds over 512 elements a warp, a cluster barrier).  What it
-// took, for 64 sequences and for one: loads and work element by element 196 and 59 us; packed fp32
-// in place of scalar, all of a segment loaded first 51 and 21; logits kept packed, lanes' sums in
-// fp32 41 and 20; the slices joined in integers instead of in 64-bit floating point 37 and 14.  Not
-// kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence more 41 to 50.
+// TB/s; an element takes some ten instructions, and the CTAs issue in 60 % of the cycles), 20 in
+// the second, 40 to 42 a call, 100 or 190 more in the one in eleven in which a sequence searches
+// twice (100 a round over the row on two SMs); one sequence's five rows of 151936 fp32: 17, all
+// latency (the draft's and the slices' loads, two rounds over 512 elements a warp, two cluster
+// barriers).  What it took, for 64 sequences and for one: loads and work element by element 196 and
+// 59 us; packed fp32 in place of scalar, all of a segment loaded first 51 and 21; logits kept
+// packed, lanes' sums in fp32 41 and 20; the slices joined in integers instead of in 64-bit
+// floating point 37 and 14; large masses in integers 39 and 16; a barrier for the second search 40
+// and 17.  Not kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence more 41 to
+// 50; large weights of the first kernel in integers 49; the second search in one CTA 260 to 550 more.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -91,6 +97,45 @@ __device__ __forceinline__ float2 weights(float2 d, const Heat &h) {
                     __fmul2_rn(d, make_float2(h.lo, h.lo)));
   const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
   return __ffma2_rn(e, rest, e);
+}
+
+// v exp((x - m) / temperature), x <= m, in integers (64-bit floating point runs at a hundredth of
+// their speed here: it made the joining of slices 5 us of a call), within 2^-38: the exponent is a
+// distance without error times two terms, in units of 2^-40; the power of two of its fraction f is
+// the series sum of (f ln 2)^k / k!, from k = 5 to 13 in units of 2^-41 in one word, the rest in
+// 2^-64 in two.  Out of line: its copies in unrolled loops took longer to fetch than to run.
+__device__ __forceinline__ uint64_t scaled_here(uint64_t v, float x, float m, float hi, float lo) {
+  if (x == m) return v;
+  const float d = x - m, back = d - x, rest = (x - (d - back)) - (m + back);  // x - m = d + rest
+  const float y = d * hi;
+  if (!(y > -100.f)) return 0;
+  const float y2 = __fmaf_rn(d, hi, -y) + __fmaf_rn(d, lo, rest * hi);
+  const int64_t e = __float2ll_rn(y * 0x1p40f) + __float2ll_rn(y2 * 0x1p40f);
+  const int down = -(int)(e >> 40);
+  const uint64_t f = (uint64_t)e << 24;
+  const uint32_t g = (uint32_t)(f >> 32);
+  uint32_t s = 3u;
+  s = 56u + __umulhi(s, g);
+  s = 978u + __umulhi(s, g);
+  s = 15514u + __umulhi(s, g);
+  s = 223818u + __umulhi(s, g);
+  s = 2906116u + __umulhi(s, g);
+  s = 33541116u + __umulhi(s, g);
+  s = 338727216u + __umulhi(s, g);
+  s = 2932080444u + __umulhi(s, g);
+  uint64_t p = (uint64_t)s << 23;
+  p = 177423166116318949ull + __umul64hi(p, f);
+  p = 1023870087579328454ull + __umul64hi(p, f);
+  p = 4431396893595737425ull + __umul64hi(p, f);
+  p = 12786308645202655660ull + __umul64hi(p, f);
+  const uint64_t all = v + __umul64hi(v, __umul64hi(p, f));
+  return down < 64 ? all >> down : 0;
+}
+__device__ __noinline__ uint64_t scaled_by(uint64_t v, float x, float m, float hi, float lo) {
+  return scaled_here(v, x, m, hi, lo);
+}
+__device__ __forceinline__ uint64_t scaled(uint64_t v, float x, float m, const Heat &h) {
+  return scaled_by(v, x, m, h.hi, h.lo2);
 }
 
 template <typename T>
@@ -186,8 +231,7 @@ __global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(VerifyArgs a) 
       }
     }
   }
-  const float sum = sums.x + sums.y;
-  uint64_t z = __float2ull_rn(sum * 0x1p40f);
+  uint64_t z = __float2ull_rn((sums.x + sums.y) * 0x1p40f);
 #pragma unroll
   for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
   at = __reduce_min_sync(0xffffffffu, at);
@@ -212,6 +256,7 @@ constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kSeg = 16;             // elements a lane and segment
 constexpr int kSegElems = 32 * kSeg;
 constexpr int kSegsKept = ((1 << 20) / kSegElems + kPickWarps - 1) / kPickWarps;  // of a warp, at most
+constexpr uint64_t kNear = 1ull << 35;  // in 2^-62: what the fp32 masses are sure of
 constexpr int kRowsKept = 64;        // rows of a sequence that are joined once
 
 struct Row {
@@ -219,41 +264,23 @@ struct Row {
   int at;     // its lowest place
   uint64_t z; // sum of exp((x - m) / temperature) in 2^-40; 0: nothing is left
   float inv_hi, inv_lo;  // 1 / z
+  uint64_t inv;          // ... in 2^-63
   int fallen; // the row's draft, -1 for a last row
 };
 
-// v exp((x - m) / temperature), x <= m, in integers (64-bit floating point runs at a hundredth of
-// their speed here: it made this step 5 us of a call).  The exponent is a distance without error
-// times two terms, in units of 2^-32; the power of two of its fraction is the power series sum of
-// (f ln 2)^k / k! to k = 11, every term positive, cut to 2^-32 at each step.
-__device__ __forceinline__ uint64_t scaled(uint64_t v, float x, float m, const Heat &h) {
-  if (x == m) return v;
-  const float d = x - m, back = d - x, rest = (x - (d - back)) - (m + back);  // x - m = d + rest
-  const float y = d * h.hi;
-  if (!(y > -100.f)) return 0;
-  const float y2 = __fmaf_rn(d, h.hi, -y) + __fmaf_rn(d, h.lo2, rest * h.hi);
-  const int64_t e = __float2ll_rd(y * 0x1p32f) + __float2ll_rd(y2 * 0x1p32f);
-  const int down = -(int)(e >> 32);
-  const uint32_t f = (uint32_t)e;
-  uint32_t p = 2u;  // (ln 2)^11 / 11! in 2^-32, and so on
-  p = 30u + __umulhi(p, f);
-  p = 437u + __umulhi(p, f);
-  p = 5676u + __umulhi(p, f);
-  p = 65510u + __umulhi(p, f);
-  p = 661577u + __umulhi(p, f);
-  p = 5726720u + __umulhi(p, f);
-  p = 41309550u + __umulhi(p, f);
-  p = 238388332u + __umulhi(p, f);
-  p = 1031764991u + __umulhi(p, f);
-  p = 2977044472u + __umulhi(p, f);
-  const uint64_t all = v + __umul64hi(v, (uint64_t)__umulhi(p, f) << 32);
-  return down < 64 ? all >> down : 0;
+// 1 / z in two terms, and in 2^-63; z in units of 2^-units
+__device__ __forceinline__ void reciprocal(Row &r, int units = 40) {
+  const float zh = (float)r.z, zl = (float)(int64_t)(r.z - (uint64_t)zh);
+  const float inv = __frcp_rn(zh);
+  r.inv_hi = inv * __int_as_float((127 + units) << 23);
+  r.inv_lo = (__fmaf_rn(-inv, zh, 1.f) - inv * zl) * r.inv_hi;
+  r.inv = __float2ull_rn(r.inv_hi * 0x1p62f) * 2 + (uint64_t)__float2ll_rn(r.inv_lo * 0x1p63f);
 }
 
 // a row's slices joined; every lane of a warp calls it
 __device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, const Heat &h, int lane) {
   const RowPart *p = a.part + row * a.slices;
-  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, -1};
+  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, 0, -1};
   const RowPart mine = lane < a.slices ? p[lane] : RowPart{-INFINITY, 0, 0};
   r.m = mine.m;
   for (int i = lane + 32; i < a.slices; i += 32) r.m = fmaxf(r.m, p[i].m);
@@ -268,12 +295,7 @@ __device__ __forceinline__ Row join_row(const VerifyArgs &a, int64_t row, const 
 #pragma unroll
   for (int o = 16; o; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
   if (h.greedy) r.z = 1ull << 40;
-  if (r.z) {  // its reciprocal in two terms
-    const float zh = (float)r.z, zl = (float)(int64_t)(r.z - (uint64_t)zh);
-    const float inv = __frcp_rn(zh);
-    r.inv_hi = inv * 0x1p40f;
-    r.inv_lo = (__fmaf_rn(-inv, zh, 1.f) - inv * zl) * r.inv_hi;
-  }
+  if (r.z) reciprocal(r);
   return r;
 }
 
@@ -290,6 +312,16 @@ __device__ __forceinline__ uint64_t units_of(float w) {
   const uint32_t bits = __float_as_uint(w), mant = (bits & 0x7fffffu) | 0x800000u;
   const int sh = (int)(bits >> 23) - (127 - 39);
   return sh >= 0 ? (uint64_t)mant << sh : (uint64_t)(mant >> min(-sh, 31));
+}
+
+// rnd of a total, rounded down; the last place for rnd >= 1, the first for what is not above zero
+__device__ __forceinline__ uint64_t place_of(float rnd, uint64_t total) {
+  if (!(rnd > 0.f) || total == 0) return 0;
+  if (rnd >= 1.f) return total - 1;
+  const uint32_t bits = __float_as_uint(rnd);  // rnd is mant 2^-(24 + down)
+  const uint64_t mant = (bits & 0x7fffffu) | (bits >> 23 ? 0x800000u : 0u);
+  const int down = 126 - max((int)(bits >> 23), 1);
+  return down < 64 ? __umul64hi(total, mant << 40) >> down : 0;
 }
 
 // a lane's elements of a segment, summed in fp32 before they become units (half the work of this
@@ -312,9 +344,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int n_cta = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int b = blockIdx.x / n_cta;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ Part s_part[2][16];  // of every CTA of the cluster, for each pass: put there by that CTA
+  __shared__ Part s_part[4][16];  // of every CTA of the cluster, for each pass: put there by that CTA
   __shared__ uint64_t s_warp[kPickWarps], s_seg[kPickWarps][kSegsKept];
-  __shared__ int s_first, s_bad;
+  __shared__ int s_first, s_bad, s_again;
   __shared__ Row s_row, s_rows[kRowsKept];
   pdl_enter();
   if (tid == 0) s_bad = status_bad(a.status);
@@ -325,7 +357,10 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
     if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
     return;
   }
-  if (tid == 0) s_first = max(m - 1, 0);
+  if (tid == 0) {
+    s_first = max(m - 1, 0);
+    s_again = 0;
+  }
   __syncthreads();
   const Heat h = heat_of(t);
   // a status that is set leaves nothing to do but to meet the cluster's other CTAs, which may have
@@ -358,7 +393,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   __syncthreads();
   const int first = s_first;
   const int64_t row = o0 + first;
-  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, -1};
+  Row r{-INFINITY, 0x7fffffff, 0, 0.f, 0.f, 0, -1};
   if (m > 0 && !bad) {
     if (first < kRowsKept) {
       r = s_rows[first];
@@ -382,15 +417,18 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
                     ? (const Q *)a.draft.x + row * a.draft.stride
                     : nullptr;
   const float inv_hi = r.inv_hi, inv_lo = r.inv_lo;
+  const float far = 0x1p-10f / inv_hi;
   // what is taken off p: nothing, the draft's row, or all of the fallen token
   enum { kNothing, kRow, kToken };
   int less = !fell ? kNothing : dq ? kRow : a.has_draft ? kNothing : kToken;
-  // the masses of a lane's elements i0, i0 + step, .. of a segment, all of them loaded first (from
-  // the last place on where the row ends: their masses are zeros)
-  auto masses_of = [&](auto kind, int i0, int step, float (&w)[kSeg]) {
+  // The masses of a lane's elements i0, i0 + step, .. of a segment, but for those (returned as bits)
+  // whose share of the row passes 2^-10: their fp32 roundings would not average out.  All loaded first
+  // (from the last place on where the row ends: their masses are zeros)
+  auto masses_of = [&](auto kind, int i0, int step, float (&w)[kSeg]) -> uint32_t {
     constexpr int kKind = decltype(kind)::value;
     T v[kSeg];
     Q q[kSeg];
+    uint32_t big = 0;
 #pragma unroll
     for (int k = 0; k < kSeg; ++k) v[k] = x[min(i0 + step * k, V - 1)];
     if constexpr (kKind == kRow) {
@@ -414,17 +452,46 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
         if constexpr (kKind == kRow) qc = fmaxf((float)q[k + c], 0.f);
         if constexpr (kKind == kToken) qc = i == fallen ? 2.f : 0.f;
         const float p = __fmaf_rn(ec, inv_hi, __fmaf_rn(ec, inv_lo, -qc));
-        w[k + c] = i < V ? fmaxf(p, 0.f) : 0.f;
+        const bool large = ec > far;
+        if (large && i < V) big |= 1u << (k + c);
+        w[k + c] = i < V && !large ? fmaxf(p, 0.f) : 0.f;
       }
     }
+    return big;
   };
-  auto masses = [&](int i0, int step, float (&w)[kSeg]) {
+  auto masses = [&](int i0, int step, float (&w)[kSeg]) -> uint32_t {
     if (less == kRow)
-      masses_of(std::integral_constant<int, kRow>(), i0, step, w);
+      return masses_of(std::integral_constant<int, kRow>(), i0, step, w);
     else if (less == kToken)
-      masses_of(std::integral_constant<int, kToken>(), i0, step, w);
+      return masses_of(std::integral_constant<int, kToken>(), i0, step, w);
     else
-      masses_of(std::integral_constant<int, kNothing>(), i0, step, w);
+      return masses_of(std::integral_constant<int, kNothing>(), i0, step, w);
+  };
+  uint64_t inv = r.inv;
+  // one mass in integers, in 2^-62, of the weight e in the same units
+  auto mass_of = [&](int i, uint64_t e) -> uint64_t {
+    const uint64_t p = __umul64hi(e, inv) * 2;
+    const float q = less == kRow ? fmaxf((float)dq[i], 0.f) : less == kToken && i == fallen ? 2.f : 0.f;
+    const uint64_t off = q < 1.5f ? units_of(q) : ~0ull;
+    return p > off ? p - off : 0;
+  };
+  auto precise = [&](int i) -> uint64_t {
+    const float v = (float)x[i];
+    return mass_of(i, r.m == INFINITY ? (v == r.m ? 1ull << 62 : 0) : scaled(1ull << 62, v, r.m, h));
+  };
+  // one times its power of two in line, four at a time: a lane's elements of a segment, summed
+  auto all_of = [&](int i0, bool weights_only, int up) -> uint64_t {
+    uint64_t sum = 0;
+#pragma unroll 4
+    for (int k = 0; k < kSeg; ++k) {
+      const int i = i0 + 32 * k;
+      const float v = i < V ? (float)x[i] : -INFINITY;
+      const uint64_t e = r.m == INFINITY ? (v == r.m ? 1ull << up : 0)
+                         : v == v        ? scaled_here(1ull << up, v, r.m, h.hi, h.lo2)
+                                         : 0;
+      if (i < V) sum += weights_only ? e : mass_of(i, e);
+    }
+    return sum;
   };
   auto warp_sum = [&](uint64_t s) {
 #pragma unroll
@@ -437,13 +504,12 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
   const bool look = m > 0 && !bad && !h.greedy && r.z;  // (the top token needs no search)
   uint64_t total = 0, before = 0;
-  for (int pass = 0; pass < 2; ++pass) {  // a second one where the draft leaves nothing: p itself
+  // the sums of the segments and of the warps; of the cluster total, of the CTAs in front before
+  auto add_up = [&](int pass, auto segment) -> bool {
     uint64_t s = 0;
     if (look)
       for (int g = g0; g < g1; ++g) {
-        float w[kSeg];
-        masses(g * kSegElems + lane, 32, w);
-        const uint64_t sum = warp_sum(lane_units(w));
+        const uint64_t sum = warp_sum(segment(g * kSegElems + lane));
         if (lane == 0) s_seg[warp][g - g0] = sum;
         s += sum;
       }
@@ -464,58 +530,100 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       total += v.total;
       stop |= v.bad != 0;
     }
+    return stop;
+  };
+  for (int pass = 0; pass < 2; ++pass) {  // a second one where the draft leaves nothing: p itself
+    const bool stop = add_up(pass, [&](int i0) {
+      float w[kSeg];
+      uint32_t big = masses(i0, 32, w);
+      uint64_t sum = lane_units(w);
+      for (; big; big &= big - 1) sum += precise(i0 + 32 * (__ffs(big) - 1));
+      return sum;
+    });
     if (stop) return;
     if (total || less == kNothing || !look) break;
     less = kNothing;
   }
-  // the lowest token whose sum passes r of the total
-  uint64_t want = 0;
-  if (rnd > 0.f) {  // rnd total, rounded down: rnd is mant 2^-(24 + down)
-    const uint32_t bits = __float_as_uint(rnd);
-    const uint64_t mant = (bits & 0x7fffffu) | (bits >> 23 ? 0x800000u : 0u);
-    const int down = 126 - max((int)(bits >> 23), 1);
-    if (rnd >= 1.f) want = total;
-    else if (down < 64) want = __umul64hi(total, mant << 40) >> down;
-  }
-  if (want >= total) want = total ? total - 1 : 0;
-  for (int w = 0; w < warp; ++w) before += s_warp[w];
-  if (total && want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
-    int g = g0;
-    for (; g < g1 - 1; ++g) {
-      const uint64_t sum = s_seg[warp][g - g0];
-      if (want < before + sum) break;
-      before += sum;
-    }
-    // the segment again with neighbours in a lane: the lanes' sums, then the elements of one lane.
-    // (They may stay short of the sum above by roundings: the last element that has a mass then.)
-    const int i0 = g * kSegElems + lane * kSeg;
-    float w[kSeg];
-    masses(i0, 1, w);
-    uint64_t own = 0;
-    int last = -1;
+  // The lowest token whose sum passes r of the total.  Next to a bound between two tokens, nearer
+  // than the fp32 masses are sure of, the cluster goes through the row once more, with every mass
+  // in integers.
+  for (int turn = 0; total; ++turn) {
+    const uint64_t want = place_of(rnd, total);
+    for (int w = 0; w < warp; ++w) before += s_warp[w];
+    if (want >= before && want < before + s_warp[warp]) {  // one warp of the cluster
+      int g = g0;
+      for (; g < g1 - 1; ++g) {
+        const uint64_t sum = s_seg[warp][g - g0];
+        if (want < before + sum) break;
+        before += sum;
+      }
+      // the segment again with neighbours in a lane: the lanes' sums, then the elements of one lane.
+      // (They may stay short of the sum above by roundings: the last element that has a mass then.)
+      const int i0 = g * kSegElems + lane * kSeg;
+      uint64_t own = 0, units[kSeg];
+      int last = -1;
+      uint32_t big = i0 >= V ? 0 : i0 + kSeg <= V ? (1u << kSeg) - 1 : (1u << (V - i0)) - 1;
+      if (turn == 0) {
+        float w[kSeg];
+        big = masses(i0, 1, w);
 #pragma unroll
-    for (int k = 0; k < kSeg; ++k) {
-      own += units_of(w[k]);
-      if (w[k] > 0.f) last = i0 + k;
-    }
-    uint64_t upto = own;
+        for (int k = 0; k < kSeg; ++k) units[k] = units_of(w[k]);
+      } else {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t u = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += u;
-    }
-    const unsigned over = __ballot_sync(0xffffffffu, before + upto > want);
-    const unsigned any = __ballot_sync(0xffffffffu, last >= 0);
-    if (over ? lane == __ffs((int)over) - 1 : any && lane == 31 - __clz((int)any)) {
-      uint64_t c = before + upto - own;
-      int token = last;
+        for (int k = 0; k < kSeg; ++k) units[k] = 0;
+      }
+      for (; big; big &= big - 1) {
+        const int n = __ffs(big) - 1;
+        const uint64_t u = precise(i0 + n);
+#pragma unroll
+        for (int k = 0; k < kSeg; ++k) units[k] = k == n ? u : units[k];
+      }
 #pragma unroll
       for (int k = 0; k < kSeg; ++k) {
-        const bool below = c <= want;
-        c += units_of(w[k]);
-        if (below && c > want) token = i0 + k;
+        own += units[k];
+        if (units[k]) last = i0 + k;
       }
-      a.picked[row] = token;
+      uint64_t upto = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
+      }
+      const unsigned over = __ballot_sync(0xffffffffu, before + upto > want);
+      const unsigned any = __ballot_sync(0xffffffffu, last >= 0);
+      if (over ? lane == __ffs((int)over) - 1 : any && lane == 31 - __clz((int)any)) {
+        uint64_t c = before + upto - own;
+        int token = last;
+        uint64_t near = 0;  // how far it is to another token
+#pragma unroll
+        for (int k = 0; k < kSeg; ++k) {
+          const uint64_t from = c;
+          c += units[k];
+          if (from <= want && c > want) {
+            token = i0 + k;
+            near = min(want - from, c - 1 - want);
+          }
+        }
+        if (near < kNear && turn == 0)
+          for (int c = 0; c < n_cta; ++c) *cl.map_shared_rank(&s_again, c) = 1;
+        else
+          a.picked[row] = token;
+      }
+    }
+    if (turn) break;
+    cl.sync();
+    if (!s_again) break;
+    if (less == kRow && r.m != INFINITY) {  // (where all masses have one factor it does not count)
+      const int up = 38 + __clzll(r.z);     // the sum comes to 2^61 or 2^62
+      add_up(2, [&](int i0) { return all_of(i0, true, up); });
+      Row sum{r.m, 0, total, 0.f, 0.f, 0, -1};
+      reciprocal(sum, up);
+      inv = sum.inv;
+    }
+    add_up(3, [&](int i0) { return all_of(i0, false, 62); });
+    if (!total && less != kNothing) {
+      less = kNothing;
+      add_up(2, [&](int i0) { return all_of(i0, false, 62); });
     }
   }
   if (rank == 0) {

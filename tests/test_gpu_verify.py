@@ -110,6 +110,55 @@ def test_borders_of_the_random_numbers(cuda, r):
             assert a == b or b >= V - 8 and a >= V - 8
 
 
+@pytest.mark.parametrize("batch", [1, 3, 40, 160])  # clusters of sixteen CTAs to one
+def test_a_number_on_a_bound(cuda, batch):
+    """equal tokens, every sum exact: r = j / n is the bound below token j, which it belongs to"""
+    n = 4096
+    j = torch.randint(0, n, (batch,), generator=torch.Generator().manual_seed(3))
+    x = torch.full((batch, n), 0.25)
+    c = (x, [1] * batch, torch.zeros(batch, dtype=torch.int32), None, None, torch.zeros(batch))
+    picked, _ = _run(cuda, *c, j / n)
+    assert picked == j.tolist()
+    # of a draft's row what it lacks: the upper half (its first token falls, 0.75 q = 1.5 p)
+    m = 2 * batch
+    q = torch.zeros((m, n))
+    q[:, :n // 2] = 2 / n
+    c = (torch.full((m, n), 0.25), [2] * batch, torch.full((m,), 7, dtype=torch.int32), q, None,
+         torch.full((m,), 0.75))
+    j = j // 2
+    picked, accepted = _run(cuda, *c, j / (n // 2))
+    assert accepted == [0] * batch
+    assert picked[0::2] == (n // 2 + j).tolist()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("certain", [False, True])
+@pytest.mark.parametrize("batch", [2, 40, 160])
+def test_numbers_next_to_a_bound(cuda, dtype, certain, batch):
+    """r the 32-bit number before or after a bound of 64-bit sums, some 2^-32 from it: fp32 masses
+    are some 2^-28 off"""
+    V = 9001
+    x, ms, tokens, q, _, u, _ = _case([2] * batch, V, dtype, certain, 21, hot=False)
+    u[:] = 1 - 2 ** -24  # most drafts fall
+    p = x.double().softmax(-1)
+    r = torch.zeros(batch)
+    for b in range(batch):
+        first = not (u[2 * b].double() * (1 if certain else q[2 * b, tokens[2 * b + 1]].double())
+                     < p[2 * b, tokens[2 * b + 1]])
+        w = p[2 * b] if first else p[2 * b + 1]
+        if first and certain:
+            w = w.clone()
+            w[tokens[2 * b + 1]] = 0
+        elif first:
+            w = (w - q[2 * b].double()).clamp(min=0)
+        cum = w.cumsum(0) / w.sum()
+        bound = cum[int((cum < 2 ** -7).sum()) + b % 5]
+        at = np.float32(bound.item())
+        r[b] = float(np.nextafter(at, np.float32(b % 2)))
+    c = (x, ms, tokens, q, None, u, r)
+    assert _run(cuda, *c) == q4_ref.verify(*c)
+
+
 def test_temperatures_out_of_range(cuda):
     x, ms, tokens, q, _, u, r = _case([2, 2, 2, 2], 500, "f32", False, 4)
     temp = torch.tensor([-1.0, math.nan, math.inf, 1e-35])
