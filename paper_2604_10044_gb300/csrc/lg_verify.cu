@@ -338,6 +338,15 @@ struct Part {      // of the vocabulary, a CTA's
   int bad;         // the device status
 };
 
+// A CTA of a cluster may send to its peers once they are known to run: each says so on entry, and
+// waits for the others before it sends anything, or ends.
+__device__ __forceinline__ void peers_arrive() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void peers_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 template <typename T, typename Q>
 __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs a) {
   cg::cluster_group cl = cg::this_cluster();
@@ -348,6 +357,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   __shared__ uint64_t s_warp[kPickWarps], s_seg[kPickWarps][kSegsKept];
   __shared__ int s_first, s_bad, s_again;
   __shared__ Row s_row, s_rows[kRowsKept];
+  peers_arrive();
   pdl_enter();
   if (tid == 0) s_bad = status_bad(a.status);
   const int o0 = a.off[b], o1 = a.off[b + 1], m = o1 - o0, V = a.x.V;
@@ -355,6 +365,8 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const float rnd = a.r[b];
   if (o0 < 0 || m < 0 || m > a.max_new || o1 > a.T) {  // (the same for the cluster)
     if (tid == 0) set_status(a.status, LG_ERR_CAPACITY);
+    __syncwarp();
+    peers_wait();
     return;
   }
   if (tid == 0) {
@@ -504,6 +516,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
   const int g0 = (rank * kPickWarps + warp) * per, g1 = min(g0 + per, segs);
   const bool look = m > 0 && !bad && !h.greedy && r.z;  // (the top token needs no search)
   uint64_t total = 0, before = 0;
+  peers_wait();
   // the sums of the segments and of the warps; of the cluster total, of the CTAs in front before
   auto add_up = [&](int pass, auto segment) -> bool {
     uint64_t s = 0;
