@@ -38,7 +38,7 @@ LG_API size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch);
      draft j stands when all before it do and u[t] q_t(y) < p_t(y)
      accepted[b] = the number of drafts that stand, a
      the next token is drawn from row t = off[b] + a with weights w = max(p_t - q_t, 0), or p_t where a
-              counts all drafts or the w are all zero (to 2^-62 of the mass): the lowest i with
+              counts all drafts or the w are all zero (to 2^-60 of the mass): the lowest i with
               sum_{k <= i} w(k) > r[b] sum w.  r below zero or NaN counts as 0, from one on as just
               below one.  -1 where p_t = 0
      picked[off[b] + j] = draft j for j < a, the next token for j = a, -1 for j > a

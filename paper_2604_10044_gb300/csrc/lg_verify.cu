@@ -604,7 +604,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
       }
       const unsigned over = __ballot_sync(0xffffffffu, before + upto > want);
       const unsigned any = __ballot_sync(0xffffffffu, last >= 0);
-      if (over ? lane == __ffs((int)over) - 1 : any && lane == 31 - __clz((int)any)) {
+      // Masses below a unit each leave a segment a sum, of 16 in fp32, but no element: the search in
+      // integers settles those, where what an element has is what its segment's sum has of it.
+      if (lane == (over ? __ffs((int)over) - 1 : any ? 31 - __clz((int)any) : 0)) {
         uint64_t c = before + upto - own;
         int token = last;
         uint64_t near = 0;  // how far it is to another token
