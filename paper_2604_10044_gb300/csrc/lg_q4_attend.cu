@@ -976,7 +976,8 @@ cudaError_t launch_d(const Q4AttendArgs &a, cudaStream_t s) {
 Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int max_len, int window,
                int sink) {
   Q4Grid r;
-  const int64_t rows = (int64_t)max_new * g;
+  // (a step in which every sequence rests, of no new rows, has a size too)
+  const int64_t rows = plan_max(1, max_new) * g;
   r.rows = rows >= 32 ? 32 : (int)((rows + 7) / 8 * 8);
   const int64_t tiles = (rows + r.rows - 1) / r.rows;
   const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
