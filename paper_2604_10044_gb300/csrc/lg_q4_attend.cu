@@ -981,10 +981,13 @@ Q4Grid q4_grid(int n_layers, int batch, int H_kv, int g, int d, int max_new, int
   r.rows = rows >= 32 ? 32 : (int)((rows + 7) / 8 * 8);
   const int64_t tiles = (rows + r.rows - 1) / r.rows;
   const int64_t blocks = ((int64_t)max_len + (1 << kBn2) - 1) >> kBn2;
-  // what the 152 SMs of a GB300 hold at once, over the layers; no more than there are blocks
+  // What the 152 SMs of a GB300 hold at once, over the layers, rounded down: all shares are equal, so
+  // CTAs past that are a second wave (28 layers of 64 sequences of up to 4096 rows: 476 CTAs 919 us, 448
+  // 643; 64 layers of up to 2048: 512 and 448, 1212 and 869; one layer is 456 either way).  No more than
+  // there are blocks.
   const int64_t fit = 152 * (r.rows <= 8 ? 3 : 2);
   const int64_t most = (int64_t)batch * H_kv * tiles * (blocks + kQ4ItemUnits);
-  r.ctas = (int)plan_max(1, plan_min(most, (fit + n_layers - 1) / n_layers));
+  r.ctas = (int)plan_max(1, plan_min(most, fit / n_layers));
   r.part_bytes = (size_t)n_layers * r.ctas * (2 * r.rows * (d + 4) * sizeof(float) + sizeof(Q4Cut));
   r.part_bytes = (r.part_bytes + 255) / 256 * 256;
   // Few items of few blocks: as many CTAs each as the GPU holds of them, up to eight, which join
