@@ -46,8 +46,10 @@ LG_API size_t lg_verify_workspace_size(const lg_logits *x, const lg_chunk *ch);
    are uniform on [0, 1) and independent.  A draft outside [0, V) falls, with q_t = 0.
    A weight is within about 2^-22 (2^-38 from 2^-10 of the mass on); what 16 of them sum to is added up in
    integers, in units of 2^-62 of the mass (2^-40 of the largest weight in p's own sum), so the same call
-   gives the same tokens.  Where r falls within 2^-27 of the mass of a bound between two tokens, the row is
-   gone through again with every weight within 2^-38 (a call with such a sequence takes 100 to 200 us more).
+   gives the same tokens.  Where r falls within 2^-27 of the mass of a bound between two tokens, or of the end of
+   the last one, the row is gone through again with every weight within 2^-38: a call with such a sequence takes
+   100 to 200 us more.  (r = 0, the start of the first, is as good as any other number, but next to p - q, for
+   which the row is gone through again there too.)
    x: rows [0, T) at least (x->batch >= T); draft: nullable, as many rows of the same V, its own dtype and
    stride.  tokens: device [T]; temperature: nullable (1), device [batch]; u: device [T] (the entry of a
    sequence's last row is not used); r: device [batch]; picked: device [T], accepted: device [batch];

@@ -616,7 +616,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) verify_pick_kernel(VerifyArgs
           c += units[k];
           if (from <= want && c > want) {
             token = i0 + k;
-            near = min(want - from, c - 1 - want);
+            // (No token ends where the line begins: r = 0 asks for the first mass.  But next to a draft's
+            // row fp32 may leave a mass where there is none, and at the line's end sums of lanes decide.)
+            near = min(from == 0 && less != kRow ? UINT64_MAX : want - from, c - 1 - want);
           }
         }
         if (near < kNear && turn == 0)
