@@ -445,6 +445,15 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
       const int low_max =
           a.shape.window ? (int)plan_max(0, (int64_t)w.rows.last + 1 - a.shape.window) : 0;
       const int suffix0 = w.q.n - a.suffix_w;  // (n and suffix_w are positive)
+      auto last_seen = [&](int r) {            // the own row of the query of row r of the item
+        return w.q.n - w.q.m + (min(r, w.used - 1) + row_1) / a.g;
+      };
+      auto low_seen = [&](int last) {
+        return a.shape.window ? (int)plan_max(0, (int64_t)last + 1 - a.shape.window) : 0;
+      };
+      auto hides = [&](int r, int last, int low) {
+        return r > last || (r < low && r >= a.shape.sink);
+      };
 
       float o[NT][4][2][4] = {};
       // rows 2 gr: the weights times group gr's scales; rows 2 gr + 1: times its least values
@@ -534,16 +543,13 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                  const int qr = min(8 * nt + 2 * t + c, w.used - 1) + row_1;
-                  const int last = w.q.n - w.q.m + qr / a.g;  // the query's own row
-                  const int low =
-                      a.shape.window ? (int)plan_max(0, (int64_t)last + 1 - a.shape.window) : 0;
+                  const int last = last_seen(8 * nt + 2 * t + c), low = low_seen(last);
 #pragma unroll
                   for (int h = 0; h < J; ++h)
 #pragma unroll
                     for (int j = c; j < 4; j += 2) {
                       const int r = rh + 16 * h + g + 8 * (j >> 1);
-                      if (r > last || (r < low && r >= a.shape.sink)) z[h][nt][j] = kHidden;
+                      if (hides(r, last, low)) z[h][nt][j] = kHidden;
                     }
                 }
             }
@@ -632,10 +638,27 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
                 sa[gr] = __shfl_sync(0xffffffffu, xa, 8 * gr + t);
                 sb[gr] = __shfl_sync(0xffffffffu, xb, 8 * gr + t);
               }
-              if (!open) {  // rows past the last hold anything, and a hidden row may hold a NaN
+              // Rows past the last hold anything, and a hidden row may hold a NaN.  Where one does: which of
+              // this thread's four keys query row g of a product sees (a weight of zero does not say it: a
+              // row that is seen may weigh less than the least number).
+              uint32_t see0[NT], see1[NT];
+              if (!open) {
                 const int r = rh + 16 * h + 2 * t, e = w.rows.last;
+                const bool odd =
+                    finite_pair(xa, true, true) != xa || finite_pair(xb, true, true) != xb;
                 xa = finite_pair(xa, r <= e, r + 1 <= e);
                 xb = finite_pair(xb, r + 8 <= e, r + 9 <= e);
+                const bool careful = __any_sync(0xffffffffu, odd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  see0[nt] = see1[nt] = 0xffffffffu;
+                  if (careful) {
+                    const int last = last_seen(8 * nt + g), low = low_seen(last);
+                    auto half = [&](int r) { return !hides(r, last, low) ? 0xffffu : 0u; };
+                    see0[nt] = half(r) | half(r + 1) << 16;
+                    see1[nt] = half(r + 8) | half(r + 9) << 16;
+                  }
+                }
               }
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
@@ -659,9 +682,9 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
                     for (int nt = 0; nt < NT; ++nt) {
                       const uint32_t pa = p0[h][nt], pb = p1[h][nt];
                       uint32_t b0 = mul_bf16x2(pa, sa[gr]), b1 = mul_bf16x2(pb, sb[gr]);
-                      if (!open) {  // a weight of zero stays zero, whatever the scale holds
-                        b0 &= (pa & 0xffffu ? 0xffffu : 0u) | (pa >> 16 ? 0xffff0000u : 0u);
-                        b1 &= (pb & 0xffffu ? 0xffffu : 0u) | (pb >> 16 ? 0xffff0000u : 0u);
+                      if (!open) {  // a hidden row weighs nothing, also times a NaN
+                        b0 &= see0[nt];
+                        b1 &= see1[nt];
                       }
 #pragma unroll
                       for (int u = 0; u < 2; ++u)
@@ -741,12 +764,15 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
         float mx = kNone;
 #pragma unroll
         for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, s_st[k][r].x);
+        // (a part that has seen rows counts, be its factor zero: 0 x NaN)
         float f[kWarps], sl = 0.f, sh = 0.f, ss = 0.f;
+        bool any[kWarps];
 #pragma unroll
         for (int k = 0; k < kWarps; ++k) {
           const float4 v = s_st[k][r];
           const float by = v.x - mx;
-          f[k] = v.y != 0.f ? exp2_fast(by) : 0.f;
+          any[k] = v.y != 0.f;
+          f[k] = any[k] ? exp2_fast(by) : 0.f;
           sl += f[k] * v.y;
           if (STATS) {
             sh += v.y != 0.f ? f[k] * __fmaf_rn(by, v.y, v.z) : 0.f;
@@ -762,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
           float x = 0.f;
 #pragma unroll
           for (int k = 0; k < kWarps; ++k)
-            if (f[k] != 0.f) x += f[k] * s_o[(k * C::kRows + r) * (D + 1) + e];
+            if (any[k]) x += f[k] * s_o[(k * C::kRows + r) * (D + 1) + e];
           if (alone)
             ((__nv_bfloat16 *)a.out)[head * D + e] = __float2bfloat16_rn(x * inv);
           else
@@ -790,6 +816,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
           const int r = i / (D / 32), e = i % (D / 32) * 32 + lane;
           const float4 v = *(const float4 *)(cl.map_shared_rank(s_part, lane % a.cluster) + r * (D + 4) + D);
           const bool any = v.y != 0.f;
+          const unsigned seen = __ballot_sync(0xffffffffu, any);
           const float mx = warp_max(any ? v.x : kNone), by = v.x - mx;
           const float f = any ? exp2_fast(by) : 0.f;
           float sl = f * v.y, sh = any ? f * __fmaf_rn(by, v.y, v.z) : 0.f, ss = f * v.w;
@@ -806,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
             if (k >= a.cluster) break;
             const float fk = __shfl_sync(0xffffffffu, f, k);
             const float z = cl.map_shared_rank(s_part, k)[r * (D + 4) + e];
-            if (fk != 0.f) y += fk * z;
+            if (seen >> k & 1) y += fk * z;
           }
           const float inv = sl != 0.f ? 1.f / sl : 0.f;
           const int rr = r + row_1;
