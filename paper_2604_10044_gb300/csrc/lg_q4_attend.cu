@@ -408,7 +408,9 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
         // the power of two of the largest, kept where 2^120 over it is a number
         const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -7), 114);
         const float up = __uint_as_float((uint32_t)(120 - ex + 127) << 23);
-        const float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
+        // (a query whose products would leave fp32 or bf16 gives NaN)
+        float mult = a.qscale * __uint_as_float((uint32_t)(13 + ex + 127) << 23);
+        if (!(big < 0x1p121f) || mult == INFINITY) mult = __int_as_float(0x7fffffff);
         cm[nt][0] = __shfl_sync(0xffffffffu, mult, 8 * t);
         cm[nt][1] = __shfl_sync(0xffffffffu, mult, 8 * t + 4);
         const uint32_t up_even = pack_bf16(up, up), up_odd = pack_bf16(up * 0.0625f, up * 0.0625f);
