@@ -9,7 +9,8 @@
 //            c and bits 4-7 16 c of them.  The queries bring the factor, 2^120 over the power of
 //            two of the row's largest element (and a sixteenth of that for the 16 c); both are
 //            exact, so are the products.  The groups' sums are joined by the rows' scales in fp32;
-//            the least values are one more product, with sums of q in two bf16 terms.
+//            the least values are one more product, with sums of q in three bf16 terms (two left
+//            the statistics 2^-17 of |lo| |sum q| off, 1e-6 of a score, for the same time).
 //   results  sum_k p_k v_k = sum_k (p_k s_kg)(c - 8) + sum_k p_k lo_kg + 8 sum_k p_k s_kg: the
 //            second operand is the weights times a group's scales, rounded to bf16; the last two
 //            are one product whose first operand is the rows' parameters.  One fused operation
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
           if (++to == C::kStages) to = 0;
         }
 
-      // q as second operands, and its groups' sums in two terms for the least values
+      // q as second operands, and its groups' sums in three terms for the least values
       const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q +
                                ((int64_t)layer * a.T + w.off) * H_q * D + (int64_t)w.kvh * a.g * D;
       const int row_1 = w.tile * a.shape.rows;  // the tile's first query row
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
       };
       uint32_t qf[NT <= 2 ? NT : 1][4][4];
       uint4 *s_q = (uint4 *)(smem + C::kSmem - C::kQ);
-      uint32_t sum_hi[NT], sum_lo[NT];
+      uint32_t sum_12[NT], sum_3[NT];
       float cm[NT][2];  // column 2t, 2t+1: what turns its sums into log2 units
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -439,8 +440,9 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
           }
         }
         const float hi = __bfloat162float(__float2bfloat16_rn(mine));
-        sum_hi[nt] = pack_bf16(0.f, hi);
-        sum_lo[nt] = pack_bf16(0.f, mine - hi);
+        const float mid = __bfloat162float(__float2bfloat16_rn(mine - hi));
+        sum_12[nt] = pack_bf16(hi, mid);
+        sum_3[nt] = pack_bf16(mine - hi - mid, 0.f);
       }
       if constexpr (NT > 2) __syncthreads();
 
@@ -491,10 +493,11 @@ __global__ void __launch_bounds__(kThreads, (Q4Cfg<D, NT>::kCtas))
             for (int h = 0; h < J; ++h) {
               uint32_t ga, gb;
               ldmatrix2(ga, gb, k_at + at2 + h * 16 * C::kRow);
-              // (the scales in the even slots meet zeros)
+              ga = __byte_perm(ga, ga, 0x3232);  // the least value twice, for three terms
+              gb = __byte_perm(gb, gb, 0x3232);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
-                mma_bf16(raw[h][nt], ga, gb, ga, gb, sum_hi[nt], sum_lo[nt], 0.f, 0.f, 0.f, 0.f);
+                mma_bf16(raw[h][nt], ga, gb, ga, gb, sum_12[nt], sum_3[nt], 0.f, 0.f, 0.f, 0.f);
               const uint4 pa = *(const uint4 *)(sk + (16 * h + g) * C::kRow + D / 2);
               const uint4 pb = *(const uint4 *)(sk + (16 * h + g + 8) * C::kRow + D / 2);
               const uint32_t par_a[4] = {pa.x, pa.y, pa.z, pa.w}, par_b[4] = {pb.x, pb.y, pb.z, pb.w};
