@@ -86,9 +86,13 @@ typedef enum {
    s = (largest - lo) times the fp32 number 1/15, rounded to bf16 (0 where that is below 2^-126: every element
    is held as lo), c the integer nearest to (x - lo) / s, ties to even.  So an element is off by half a
    scale at most, and the largest by 2^-9 of the range more.  A group that holds a NaN or an infinity, or whose range is 2^118 or more,
-   reads back as NaN.  Queries, new rows and results of such a cache are bf16; up to 64 query rows of a kv-head
-   in a call (lg_chunk.h) want a query's elements below 2^121, and times the softmax scale below 2^114: the
-   results of a query beyond that are NaN.
+   reads back as NaN.  Queries, new rows and results of such a cache are bf16.
+   Attention over it takes keys and values as lo + s c, not rounded; scores, statistics and sums are fp32.  The
+   weights enter the products with values in bf16, and rounded once more times a group's scale (off by 2^-7 at most
+   of a weight times s |c - 8|, by 2^-8 times |lo + 8 s|; 2.8e-3 of random values' results where the rounding of
+   the result is 1.7e-3).  A query's elements are to be below 2^121, and times the softmax scale below 2^114: the
+   results of a query beyond that are NaN.  lg_chunk_attend with more than 64 query rows of a kv-head is described
+   in lg_chunk.h.
    Its calls: lg_begin_step, lg_append, lg_decode_attend (and _noalloc), lg_state_init, the detect and
    prune calls, lg_read_device_status, and those of lg_chunk.h and lg_draft.h.  lg_sketch_build is
    refused (rows near zero have lost their sign; every append writes its sketch from the values as they

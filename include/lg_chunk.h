@@ -102,7 +102,9 @@ LG_API lg_status lg_rope_append(const lg_cache *c, const lg_chunk *ch, int layer
                                 cudaStream_t s);
 
 /* Workspace bytes lg_chunk_attend needs (partial results of sequences whose rows several CTAs
-   share); 0 on invalid arguments. */
+   share); 0 on invalid arguments.  Over LG_Q4 with more than 64 query rows of a kv-head
+   (max_new H_q / H_kv > 64) two more arrays of H_kv S_total d bf16 each, a layer of the whole cache,
+   whatever the chunk sees of it: 3.2 times that layer's rows in four bits for d = 128, 2.7 for 64. */
 LG_API size_t lg_chunk_workspace_size(const lg_cache *c, const lg_chunk *ch, int H_q, int max_len);
 
 /* Attention of the chunk's queries over the cache (Eq. 1 restricted to what each query may see):
@@ -113,8 +115,14 @@ LG_API size_t lg_chunk_workspace_size(const lg_cache *c, const lg_chunk *ch, int
    q: device [T][H_q][d] dense, dtype; out: device same shape, dtype, may not overlap q.  Query
    head h reads kv-head h / (H_q/H_kv).  What lies in rows that a query does not see never reaches
    its result, whatever it holds.  bf16: the weights enter the product with the values in bf16
-   (off by 2^-8 of each at most; lg_decode_attend carries them in two terms), scores and sums are
-   fp32.  max_len: host bound on every len[b], best a near one, as the division
+   (off by 2^-8 of each at most; lg_decode_attend carries them in two terms over a bf16 cache), scores
+   and sums are fp32.  LG_Q4: up to 64 query rows of a kv-head (max_new H_q / H_kv) as lg_decode_attend
+   (lg.h); a call with more first writes the rows of every sequence of the chunk that some query sees to
+   the workspace as bf16 values, lo + s c rounded, and goes on as over a bf16 cache (3.2e-3 of random
+   values' results).  So a sequence's result changes a little, and its time, with the longest chunk that
+   shares its call: where one sequence brings a prompt and others a token each, two chunks with a call
+   each are better (512 tokens beside 63 single ones, 361000 rows in all: 276 us instead of 566).
+   max_len: host bound on every len[b], best a near one, as the division
    of the work (and so the order of sums) goes by it.  A longer sequence sets LG_ERR_CAPACITY, as
    does an m_b above max_new or len[b], or an off[] outside [0, T]; nothing of that call's output is
    then defined.

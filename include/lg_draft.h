@@ -8,9 +8,9 @@
  *   lg_begin_chunk, for each layer lg_rope_append -> lg_chunk_attend, then
  *   lg_verify_draft on the chunk's logits -> lg_end_chunk -> lg_count_tokens on what was picked
  * after which row 0 of the next chunk is picked[off[b] + accepted[b]].
- * The monitors of lg.h take one token a step: such a step is not followed by lg_detect, and by
- * lg_token_detect only where it is called for each picked token in turn, before the rows of later ones
- * join the cache.
+ * The monitors of lg.h do not follow such a step: lg_chunk_attend gives lg_detect no statistics, and
+ * lg_token_detect takes one token a call, whose row is the cache's last, where the rows of all drafts
+ * have joined before any is checked.  A guarded decode is one of single tokens.
  *
  * These calls have no counterpart in the paper (arXiv 2604.10044), which decodes a token a step.
  */

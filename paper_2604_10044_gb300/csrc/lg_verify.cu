@@ -16,11 +16,11 @@
 // with a second search from 2^-28 on, 1 in 10^6 from 2^-26 on, met by a third and twice as many calls).
 //
 // GB300, 261 rows of 128257 bf16 logits of 64 sequences: 19 us in the first kernel (67 MB, 3.5
-// TB/s; an element takes some ten instructions, and the CTAs issue in 60 % of the cycles), 20 in
-// the second, 40 to 42 a call, 100 or 190 more in the one in eleven in which a sequence searches
-// twice (100 a round over the row on two SMs); one sequence's five rows of 151936 fp32: 17, all
-// latency (the draft's and the slices' loads, two rounds over 512 elements a warp, two cluster
-// barriers).  What it took, for 64 sequences and for one: loads and work element by element 196 and
+// TB/s; an element takes some ten instructions, and the CTAs issue in 60 % of the cycles), 21 in
+// the second, 40 to 45 a call, 100 or 190 more in the one in ten in which a sequence searches
+// twice (100 a round over the row on two SMs): 58 the mean of 60 calls; one sequence's five rows of
+// 151936 fp32: 16, of which 13 in the second kernel (the draft's and the slices' loads, two rounds
+// over 512 elements a warp, two cluster barriers, all of it latency).  What it took, for 64 sequences and for one: loads and work element by element 196 and
 // 59 us; packed fp32 in place of scalar, all of a segment loaded first 51 and 21; logits kept
 // packed, lanes' sums in fp32 41 and 20; the slices joined in integers instead of in 64-bit
 // floating point 37 and 14; large masses in integers 39 and 16; a barrier for the second search 40
