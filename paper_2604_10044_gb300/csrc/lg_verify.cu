@@ -21,11 +21,12 @@
 // twice (100 a round over the row on two SMs): 58 the mean of 60 calls; one sequence's five rows of
 // 151936 fp32: 16, of which 13 in the second kernel (the draft's and the slices' loads, two rounds
 // over 512 elements a warp, two cluster barriers, all of it latency).  What it took, for 64 sequences
-// and for one: loads and work element by element 196 and 59 us; packed fp32 in place of scalar, all of a segment loaded first 51 and 21; logits kept
-// packed, lanes' sums in fp32 41 and 20; the slices joined in integers instead of in 64-bit
-// floating point 37 and 14; large masses in integers 39 and 16; a barrier for the second search 40
-// and 17.  Not kept: a warp a slice without the CTA's barriers 41; two CTAs a sequence more 41 to
-// 50; large weights of the first kernel in integers 49; the second search in one CTA 260 to 550 more.
+// and for one: loads and work element by element 196 and 59 us; packed fp32 in place of scalar, all
+// of a segment loaded first 51 and 21; logits kept packed, lanes' sums in fp32 41 and 20; the
+// slices joined in integers instead of in 64-bit floating point 37 and 14; large masses in integers
+// 39 and 16; a barrier for the second search 40 and 17.  Not kept: a warp a slice without the CTA's
+// barriers 41; two CTAs a sequence more 41 to 50; large weights of the first kernel in integers 49;
+// the second search in one CTA 260 to 550 more.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
